@@ -173,6 +173,56 @@ int dcp_pair_bias_attention_partial(const dcp_shape* shape, const dcp_weights* w
                                     int64_t k0, int64_t k1, float* m_out, float* l_out, float* acc_out,
                                     float* gate_out, void* workspace, size_t workspace_bytes, void* stream);
 
+/* ---------------------------------------------------------------------------
+ * Backward pass of the attention layer: the gradients of a scalar with respect
+ * to the layer's inputs and weights, from its gradient with respect to `out`.
+ * The probabilities are recomputed from s, z and the forward's softmax state;
+ * nothing of size n_q x N is kept between the passes.
+ * ------------------------------------------------------------------------- */
+
+/* Device pointers that receive gradients, each 16-byte aligned, or NULL for one
+ * that is not wanted (at least one is). They must not overlap the inputs, the
+ * workspace or each other. All are overwritten; those of the shared tensors
+ * are the stripe's share, to be added over the stripes by the caller. */
+typedef struct {
+  void* dz_rows;   /* [n_q, N, c_z] act_dtype; 0 for masked keys                  */
+  void* ds;        /* [N, c_s] dtype: as queries and gates the stripe's rows, as  */
+                   /*   keys and values all tokens                                */
+  void* dw_q;      /* [H*d, c_s] dtype                                            */
+  void* dw_k;      /* [H*d, c_s] dtype                                            */
+  void* dw_v;      /* [H*d, c_s] dtype                                            */
+  void* dw_g;      /* [H*d, c_s] dtype                                            */
+  void* dw_b;      /* [H, c_z] dtype                                              */
+  void* dln_gamma; /* [c_z] dtype                                                 */
+  int32_t dtype;   /* dcp_dtype of all but dz_rows                                */
+} dcp_gradients;
+/* b_b and ln_beta add a constant per head to all logits of a row: their
+ * gradients are 0, exactly, and they are not read. */
+
+/* Workspace bytes of dcp_pair_bias_attention_backward (written to *bytes).
+ * Host-only. */
+int dcp_pair_bias_attention_backward_workspace_size(const dcp_shape* shape, int64_t n_q, size_t* bytes);
+
+/* Gradients of the query stripe [q_row0, q_row0 + n_q) of
+ * dcp_pair_bias_attention (without rows: zeros). shape, weights, s, z_rows and key_mask are the
+ * forward's (out_dtype is the type of dout).
+ *   m, l, acc   [H, n_q], [H, n_q], [n_q, H, d] fp32: the stripe's softmax state
+ *               over all keys, as dcp_pair_bias_attention_partial writes it for
+ *               [0, N) or dcp_block_merge for the parts of a ring; 16-byte aligned.
+ *               (Its logits leave out b_b and ln_beta, as the library's do.) A row
+ *               whose l is 0, because no key attends, has gradients of 0.
+ *   dout        [n_q, H*d] out_dtype, 16-byte aligned: the gradient of the layer's
+ *               gated output
+ *   workspace   at least dcp_pair_bias_attention_backward_workspace_size() bytes,
+ *               256-byte aligned; contents on entry are ignored
+ * Supported shapes, alignment of the weights and precision are the forward's:
+ * fp32 arithmetic throughout on the general path. */
+int dcp_pair_bias_attention_backward(const dcp_shape* shape, const dcp_weights* weights, const void* s,
+                                     const void* z_rows, const uint8_t* key_mask, int64_t q_row0, int64_t n_q,
+                                     const float* m, const float* l, const float* acc, const void* dout,
+                                     const dcp_gradients* grads, void* workspace, size_t workspace_bytes,
+                                     void* stream);
+
 /* The pair bias alone (Methods, "RFDiffusion 3 preliminaries and notation":
  * B = f_B(Z)), materialised: bias_out[r, c, h] = sum_k W_b[h,k] LN(z_tile[r, c, :])_k + b_b[h]
  * including gamma, beta and b_b, for r < n_rows, c < n_cols. Pair (r, c) is
@@ -381,6 +431,40 @@ int dcp_scatter_mean_workspace_size(int64_t n_tokens, int32_t c, size_t* bytes);
  * no-op. */
 int dcp_scatter_mean(int64_t n_atoms, int64_t n_tokens, int32_t c, int32_t in_dtype, int32_t out_dtype, const void* a,
                      const int32_t* tok_idx, void* out, void* workspace, size_t workspace_bytes, void* stream);
+
+/* ---------------------------------------------------------------------------
+ * LayerNorm over the channels of each row, and its backward pass:
+ *   xh = (x - mean x) / sqrt(var x + eps),  y = gamma * xh + beta,
+ * biased variance; statistics and sums in fp32 (centred before they are squared).
+ * ------------------------------------------------------------------------- */
+
+/* y = LayerNorm(x).
+ *   x        [n_rows, c] in_dtype
+ *   ln_gamma, ln_beta  [c] fp32 or NULL (= 1 / 0)
+ *   y        [n_rows, c] out_dtype; may be x itself where the types are the same,
+ *            and must not overlap it otherwise
+ *   c        1 <= c <= 4096
+ * Device pointers aligned to their element size; rows of whole 16-byte pieces
+ * (c a multiple of 8 in bf16, of 4 in fp32) in 16-byte aligned tensors are read
+ * fastest. n_rows = 0 is a no-op. Needs no workspace. */
+int dcp_layer_norm(int64_t n_rows, int32_t c, int32_t in_dtype, int32_t out_dtype, float ln_eps, const void* x,
+                   const float* ln_gamma, const float* ln_beta, void* y, void* stream);
+
+/* Workspace bytes for dcp_layer_norm_backward (written to *bytes). Host-only. */
+int dcp_layer_norm_backward_workspace_size(int64_t n_rows, int32_t c, size_t* bytes);
+
+/* Gradients of y = LayerNorm(x) (arguments as above) from dy = the gradient of y:
+ *   dy         [n_rows, c] out_dtype
+ *   dx         [n_rows, c] in_dtype, or NULL; may be x or dy itself where the types
+ *              are the same, and must not overlap them otherwise
+ *   dln_gamma, dln_beta  [c] fp32, each or NULL: sums over the rows, in a fixed order
+ *              that depends on n_rows, c and alignment only (n_rows = 0 gives 0)
+ *   workspace  at least dcp_layer_norm_backward_workspace_size() bytes, 256-byte
+ *              aligned; may be NULL when dln_gamma and dln_beta are
+ * At least one gradient is wanted. The statistics are formed again from x. */
+int dcp_layer_norm_backward(int64_t n_rows, int32_t c, int32_t in_dtype, int32_t out_dtype, float ln_eps, const void* x,
+                            const float* ln_gamma, const void* dy, void* dx, float* dln_gamma, float* dln_beta,
+                            void* workspace, size_t workspace_bytes, void* stream);
 
 /* Optional timing hook: when both are non-NULL hipEvent_t handles, the calling
  * thread's next dcp_pair_bias_attention, dcp_sparse_pair_bias_attention,

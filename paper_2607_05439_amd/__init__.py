@@ -6,7 +6,9 @@ used for device memory and streams. The functions carry the C names
 ``dcp_workspace_size``, ``dcp_workspace_bytes``, ``dcp_sparse_pair_bias_attention``,
 ``dcp_sparse_workspace_size``, ``dcp_knn_topk``, ``dcp_knn_workspace_size``, ``dcp_topk_merge``,
 ``dcp_pair_transition``, ``dcp_transition_workspace_size``, ``dcp_scatter_mean``,
-``dcp_scatter_mean_workspace_size``) and accept torch tensors (device pointers are taken
+``dcp_scatter_mean_workspace_size``, ``dcp_layer_norm``, ``dcp_layer_norm_backward``,
+``dcp_layer_norm_backward_workspace_size``, ``dcp_pair_bias_attention_backward``,
+``dcp_pair_bias_attention_backward_workspace_size``) and accept torch tensors (device pointers are taken
 from ``data_ptr()``) or plain integer addresses. Loading fails loudly when the
 library has not been built: there is no fallback.
 """
@@ -25,7 +27,9 @@ EXPORTS = ("dcp_workspace_size", "dcp_workspace_bytes", "dcp_pair_bias_attention
            "dcp_block_merge",
            "dcp_sparse_workspace_size", "dcp_sparse_pair_bias_attention", "dcp_knn_topk", "dcp_knn_workspace_size", "dcp_topk_merge",
            "dcp_transition_workspace_size", "dcp_pair_transition", "dcp_scatter_mean_workspace_size",
-           "dcp_scatter_mean", "dcp_set_timing_events",
+           "dcp_scatter_mean", "dcp_layer_norm", "dcp_layer_norm_backward_workspace_size", "dcp_layer_norm_backward",
+           "dcp_pair_bias_attention_backward_workspace_size", "dcp_pair_bias_attention_backward",
+           "dcp_set_timing_events",
            "dcp_last_error", "dcp_version")
 
 
@@ -43,6 +47,11 @@ class DcpShape(ctypes.Structure):
 
 class DcpWeights(ctypes.Structure):
     _fields_ = [(n, ctypes.c_void_p) for n in ("w_q", "w_k", "w_v", "w_g", "w_b", "b_b", "ln_gamma", "ln_beta")]
+
+
+class DcpGradients(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in ("dz_rows", "ds", "dw_q", "dw_k", "dw_v", "dw_g", "dw_b", "dln_gamma")]
+    _fields_.append(("dtype", ctypes.c_int32))
 
 
 class DcpSparseShape(ctypes.Structure):
@@ -82,13 +91,21 @@ def lib() -> ctypes.CDLL:
         L.dcp_pair_transition.argtypes = [i64, i32, i32, i32, ctypes.c_float, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
         L.dcp_scatter_mean_workspace_size.argtypes = [i64, i32, P(sz)]
         L.dcp_scatter_mean.argtypes = [i64, i64, i32, i32, i32, vp, vp, vp, vp, sz, vp]
+        L.dcp_layer_norm.argtypes = [i64, i32, i32, i32, ctypes.c_float, vp, vp, vp, vp, vp]
+        L.dcp_layer_norm_backward_workspace_size.argtypes = [i64, i32, P(sz)]
+        L.dcp_layer_norm_backward.argtypes = [i64, i32, i32, i32, ctypes.c_float, vp, vp, vp, vp, vp, vp, vp, sz, vp]
+        L.dcp_pair_bias_attention_backward_workspace_size.argtypes = [P(DcpShape), i64, P(sz)]
+        L.dcp_pair_bias_attention_backward.argtypes = [P(DcpShape), P(DcpWeights), vp, vp, vp, i64, i64, vp, vp, vp, vp,
+                                                       P(DcpGradients), vp, sz, vp]
         L.dcp_set_timing_events.argtypes = [vp, vp]
         for f in (L.dcp_workspace_size, L.dcp_pair_bias_attention, L.dcp_pair_bias_attention_noalloc,
                   L.dcp_pair_bias_attention_partial,
                   L.dcp_bias_project, L.dcp_block_merge,
                   L.dcp_sparse_workspace_size, L.dcp_sparse_pair_bias_attention, L.dcp_knn_topk, L.dcp_knn_workspace_size, L.dcp_topk_merge,
                   L.dcp_transition_workspace_size, L.dcp_pair_transition, L.dcp_scatter_mean_workspace_size,
-                  L.dcp_scatter_mean, L.dcp_set_timing_events):
+                  L.dcp_scatter_mean, L.dcp_layer_norm, L.dcp_layer_norm_backward_workspace_size,
+                  L.dcp_layer_norm_backward, L.dcp_pair_bias_attention_backward_workspace_size,
+                  L.dcp_pair_bias_attention_backward, L.dcp_set_timing_events):
             f.restype = ctypes.c_int
         L.dcp_last_error.restype = ctypes.c_char_p
         L.dcp_last_error.argtypes = []
@@ -248,6 +265,46 @@ def dcp_scatter_mean(n_atoms: int, n_tokens: int, c: int, in_dtype: int, out_dty
                      out: Ptr, workspace: Ptr, workspace_bytes: int, stream=None) -> None:
     _check(lib().dcp_scatter_mean(n_atoms, n_tokens, c, in_dtype, out_dtype, _ptr(a), _ptr(tok_idx), _ptr(out),
                                   _ptr(workspace), workspace_bytes, _stream(stream)))
+
+
+def dcp_layer_norm(n_rows: int, c: int, in_dtype: int, out_dtype: int, ln_eps: float, x: Ptr, ln_gamma: Ptr,
+                   ln_beta: Ptr, y: Ptr, stream=None) -> None:
+    _check(lib().dcp_layer_norm(n_rows, c, in_dtype, out_dtype, ln_eps, _ptr(x), _ptr(ln_gamma), _ptr(ln_beta),
+                                _ptr(y), _stream(stream)))
+
+
+def dcp_layer_norm_backward_workspace_size(n_rows: int, c: int) -> int:
+    out = ctypes.c_size_t()
+    _check(lib().dcp_layer_norm_backward_workspace_size(n_rows, c, ctypes.byref(out)))
+    return out.value
+
+
+def dcp_layer_norm_backward(n_rows: int, c: int, in_dtype: int, out_dtype: int, ln_eps: float, x: Ptr, ln_gamma: Ptr,
+                            dy: Ptr, dx: Ptr, dln_gamma: Ptr, dln_beta: Ptr, workspace: Ptr, workspace_bytes: int,
+                            stream=None) -> None:
+    _check(lib().dcp_layer_norm_backward(n_rows, c, in_dtype, out_dtype, ln_eps, _ptr(x), _ptr(ln_gamma), _ptr(dy),
+                                         _ptr(dx), _ptr(dln_gamma), _ptr(dln_beta), _ptr(workspace), workspace_bytes,
+                                         _stream(stream)))
+
+
+def make_gradients(dz_rows: Ptr = None, ds: Ptr = None, dw_q: Ptr = None, dw_k: Ptr = None, dw_v: Ptr = None,
+                   dw_g: Ptr = None, dw_b: Ptr = None, dln_gamma: Ptr = None, dtype: int = DCP_F32) -> DcpGradients:
+    return DcpGradients(*[_ptr(x) for x in (dz_rows, ds, dw_q, dw_k, dw_v, dw_g, dw_b, dln_gamma)], dtype)
+
+
+def dcp_pair_bias_attention_backward_workspace_size(shape: DcpShape, n_q: int) -> int:
+    out = ctypes.c_size_t()
+    _check(lib().dcp_pair_bias_attention_backward_workspace_size(ctypes.byref(shape), n_q, ctypes.byref(out)))
+    return out.value
+
+
+def dcp_pair_bias_attention_backward(shape: DcpShape, weights: DcpWeights, s: Ptr, z_rows: Ptr, key_mask: Ptr,
+                                     q_row0: int, n_q: int, m: Ptr, l: Ptr, acc: Ptr, dout: Ptr, grads: DcpGradients,
+                                     workspace: Ptr, workspace_bytes: int, stream=None) -> None:
+    _check(lib().dcp_pair_bias_attention_backward(ctypes.byref(shape), ctypes.byref(weights), _ptr(s), _ptr(z_rows),
+                                                  _ptr(key_mask), q_row0, n_q, _ptr(m), _ptr(l), _ptr(acc),
+                                                  _ptr(dout), ctypes.byref(grads), _ptr(workspace), workspace_bytes,
+                                                  _stream(stream)))
 
 
 def dcp_set_timing_events(start_event: Optional[int], stop_event: Optional[int]) -> None:

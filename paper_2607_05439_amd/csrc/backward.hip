@@ -1,0 +1,614 @@
+// Backward pass of the pair-biased gated attention: the steps that every shape
+// shares, and the pair kernels of the general fp32 path (gfx950).
+//
+// With P = exp(l - m) / L recomputed from the saved state, o = acc / L, and
+// dout the gradient of the gated output:
+//   do = g dout, D = do . o, dP = do . v, dS = P (dP - D),
+//   dq_i = sum_j dS k_j / sqrt(d), dk_j = sum_i dS q_i / sqrt(d), dv_j = sum_i P do_i,
+//   dg = dout o g (1 - g)                      (before the sigmoid)
+// and through the bias, with zh the normalised pair vector and W' = W_b diag(gamma):
+//   dzh_c = sum_h dS_h W'_hc, dz = rstd (dzh - mean dzh - zh mean(dzh zh)),
+//   T_hc = sum_ij dS_h zh_c, dW_b = T diag(gamma), dgamma_c = sum_h W_b,hc T_hc.
+// The rows of dS sum to 0, so LayerNorm's beta and the bias of the projection,
+// constants per head, have no gradient and no part in the others'.
+// Token side: ds = dq W_q + dg W_g + dk W_k + dv W_v, dW_x = dx^T s.
+//
+// P and dS meet two sums that run across each other: dq over a row's keys, dk
+// and dv over a key's rows. The pair kernel holds a row and sums dq itself; it
+// writes P and dS (8 bytes a pair and head in fp32), and a second kernel that
+// holds keys sums dk and dv. Stripes of rows bound the room for P and dS.
+#include <hip/hip_runtime.h>
+#include <math.h>
+#include <stdint.h>
+
+#include "cdna4.h"
+#include "dcp_internal.h"
+
+namespace dcp {
+namespace {
+
+__device__ __forceinline__ float load_one(const void* p, int bf16, int64_t at) {
+  return bf16 ? __uint_as_float((uint32_t)static_cast<const uint16_t*>(p)[at] << 16) : static_cast<const float*>(p)[at];
+}
+__device__ __forceinline__ void store_one(void* p, int bf16, int64_t at, float v) {
+  if (bf16)
+    static_cast<__bf16*>(p)[at] = (__bf16)v;
+  else
+    static_cast<float*>(p)[at] = v;
+}
+// Four consecutive elements from i0 of a row of len, zeros past its end; `vec`:
+// len is a multiple of 4 and the row 16-byte (bf16: 8-byte) aligned.
+__device__ __forceinline__ f32x4 load_four(const void* p, int bf16, int vec, int64_t row, int i0, int len) {
+  f32x4 r = {0.f, 0.f, 0.f, 0.f};
+  if (vec) {
+    if (i0 < len) {
+      if (bf16) {
+        const u32x2 t = *reinterpret_cast<const u32x2*>(static_cast<const uint16_t*>(p) + row + i0);
+        r = f32x4{__uint_as_float(t[0] << 16), __uint_as_float(t[0] & 0xFFFF0000u), __uint_as_float(t[1] << 16),
+                  __uint_as_float(t[1] & 0xFFFF0000u)};
+      } else {
+        r = *reinterpret_cast<const f32x4*>(static_cast<const float*>(p) + row + i0);
+      }
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (i0 + i < len) r[i] = load_one(p, bf16, row + i0 + i);
+  }
+  return r;
+}
+
+// Sum over the four lanes of a quad; each gets the same bits.
+__device__ __forceinline__ float quad_sum(float x) {
+  x += __uint_as_float((uint32_t)__builtin_amdgcn_update_dpp(0, (int)__float_as_uint(x), 0xB1, 0xF, 0xF, true));
+  x += __uint_as_float((uint32_t)__builtin_amdgcn_update_dpp(0, (int)__float_as_uint(x), 0x4E, 0xF, 0xF, true));
+  return x;
+}
+
+// ----------------------------------------------------------------------------- query rows
+// One thread per row and head: do, q in padded rows of dp floats per head, the
+// statistics {m, 1 / L, D, -}, and dg. A row without keys (L = 0) gets weights of 0.
+__global__ void __launch_bounds__(256) back_rows_kernel(BackRowsArgs a) {
+  const int64_t t = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  if (t >= a.n_q * a.n_heads) return;
+  const int64_t row = t / a.n_heads;
+  const int h = (int)(t - row * a.n_heads), d = a.head_dim;
+  const int64_t at = row * a.n_heads * d + (int64_t)h * d, to = ((int64_t)h * a.n_q + row) * a.dp;
+  const float l = a.l[(int64_t)h * a.n_q + row], inv_l = l == 0.0f ? 0.0f : 1.0f / l;
+  float dot = 0.0f;
+  for (int e = 0; e < d; ++e) {
+    const float g = a.g[at + e], up = load_one(a.dout, a.dout_bf16, at + e);
+    const float o = l == 0.0f ? 0.0f : a.acc[at + e] * inv_l;
+    const float x = g * up;
+    dot = fmaf(x, o, dot);
+    a.dg[at + e] = up * o * g * (1.0f - g);
+    a.dop[to + e] = x;
+    a.qp[to + e] = a.q[at + e];
+  }
+  for (int e = d; e < a.dp; ++e) a.dop[to + e] = a.qp[to + e] = 0.0f;
+  const float m = l == 0.0f ? 0.0f : a.m[(int64_t)h * a.n_q + row];
+  *reinterpret_cast<f32x4*>(a.stat + 4 * ((int64_t)h * a.n_q + row)) = f32x4{m, inv_l, dot, 0.0f};
+}
+
+// ----------------------------------------------------------------------------- pairs
+// A workgroup takes one query row and a range of keys, 64 at a time: four lanes
+// per key share its channels for the LayerNorm, the bias and dz, and its heads for
+// the logits and dS. It loops over such items, so that T is written once per
+// workgroup.
+constexpr int kBackKeys = 64;
+constexpr int kHeadStride = kGenMaxD + 4;
+
+template <int CT, int NH>
+__global__ void __launch_bounds__(256) back_pairs_kernel(BackPairsArgs a) {
+  constexpr int CZ = 16 * CT, HP = 4 * NH, kGroups = 256 / CZ;  // key groups of the sum T
+  __shared__ __attribute__((aligned(16))) float s_w[HP * CZ];
+  __shared__ __attribute__((aligned(16))) float s_zh[kBackKeys * (CZ + 4)];
+  __shared__ __attribute__((aligned(16))) float s_ds[kBackKeys * (HP + 4)];
+  __shared__ __attribute__((aligned(16))) float s_q[HP * kHeadStride], s_do[HP * kHeadStride];
+  __shared__ float s_dq[256];
+  const int tid = threadIdx.x, key = tid >> 2, qd = tid & 3;
+  const int H = a.n_heads, d = a.head_dim, hd = H * d, c_z = a.c_z;
+  const float inv_c = 1.0f / (float)c_z, scale = 1.0f / sqrtf((float)d);
+  const int z_vec = c_z % 4 == 0, k_vec = d % 4 == 0;
+  for (int x = tid; x < HP * CZ; x += 256) {
+    const int h = x / CZ, c = x % CZ;
+    s_w[x] = h < H && c < c_z ? a.w_b[(int64_t)h * c_z + c] * (a.gamma ? a.gamma[c] : 1.0f) : 0.0f;
+  }
+  for (int x = tid; x < HP * kHeadStride; x += 256) s_q[x] = s_do[x] = 0.0f;
+  const int tc = tid % CZ, tg = tid / CZ;  // T: this thread's channel and key group
+  float t_sum[HP];
+#pragma unroll
+  for (int h = 0; h < HP; ++h) t_sum[h] = 0.0f;
+  const int dq_groups = max(256 / hd, 1), dq_x = tid % hd, dq_g = tid / hd;
+  const int64_t items = a.rows * a.n_parts;
+  const int64_t tiles = (a.n_tok + kBackKeys - 1) / kBackKeys;
+
+  for (int64_t item = blockIdx.x; item < items; item += gridDim.x) {
+    const int64_t r = item / a.n_parts;  // row of the stripe's chunk
+    const int part = (int)(item - r * a.n_parts);
+    const int64_t row = a.row0 + r;      // row of the stripe
+    int64_t t_count, t_first;
+    chunk_of(tiles, a.n_parts, part, &t_count, &t_first);
+    __syncthreads();
+    for (int x = tid; x < hd; x += 256) {
+      const int h = x / d, e = x - h * d;
+      s_q[h * kHeadStride + e] = a.qp[((int64_t)h * a.n_q + row) * a.dp + e] * scale;
+      s_do[h * kHeadStride + e] = a.dop[((int64_t)h * a.n_q + row) * a.dp + e];
+    }
+    f32x4 stat[NH];
+#pragma unroll
+    for (int i = 0; i < NH; ++i)
+      stat[i] = *reinterpret_cast<const f32x4*>(a.stat + 4 * ((int64_t)min(4 * i + qd, H - 1) * a.n_q + row));
+    float dq = 0.0f, dq2 = 0.0f;
+    __syncthreads();
+    for (int64_t t = t_first; t < t_first + t_count; ++t) {
+      const int64_t j = t * kBackKeys + key;
+      const bool there = j < a.n_tok, valid = there && (!a.mask || a.mask[j] != 0);
+      f32x4 zh[CT];
+      const int64_t off = (row * a.n_tok + j) * c_z;
+      float s = 0.0f, v = 0.0f;
+#pragma unroll
+      for (int m = 0; m < CT; ++m) {
+        zh[m] = valid ? load_four(a.z, a.z_bf16, z_vec, off, 16 * m + 4 * qd, c_z) : f32x4{0.f, 0.f, 0.f, 0.f};
+        s += (zh[m][0] + zh[m][1]) + (zh[m][2] + zh[m][3]);
+      }
+      const float mu = quad_sum(s) * inv_c;
+#pragma unroll
+      for (int m = 0; m < CT; ++m)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          zh[m][i] = 16 * m + 4 * qd + i < c_z ? zh[m][i] - mu : 0.0f;
+          v = fmaf(zh[m][i], zh[m][i], v);
+        }
+      const float rstd = valid ? 1.0f / sqrtf(fmaf(quad_sum(v), inv_c, a.eps)) : 0.0f;
+#pragma unroll
+      for (int m = 0; m < CT; ++m) {
+        zh[m] *= rstd;
+        if (!valid) zh[m] = f32x4{0.f, 0.f, 0.f, 0.f};
+        *reinterpret_cast<f32x4*>(&s_zh[key * (CZ + 4) + 16 * m + 4 * qd]) = zh[m];
+      }
+#pragma unroll
+      for (int i = 0; i < NH; ++i) {
+        // the bias of heads 4i .. 4i + 3, summed over the quad; this lane keeps head 4i + qd
+        float b = 0.0f;
+#pragma unroll
+        for (int x = 0; x < 4; ++x) {
+          f32x4 p = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+          for (int m = 0; m < CT; ++m) {
+            const f32x4 w = *reinterpret_cast<const f32x4*>(&s_w[(4 * i + x) * CZ + 16 * m + 4 * qd]);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) p[e] = fmaf(w[e], zh[m][e], p[e]);
+          }
+          const float sum = quad_sum((p[0] + p[1]) + (p[2] + p[3]));
+          b = qd == x ? sum : b;
+        }
+        const int h = 4 * i + qd;
+        float ds = 0.0f, p = 0.0f;
+        if (valid && h < H) {
+          f32x4 lg = {0.f, 0.f, 0.f, 0.f}, dp = {0.f, 0.f, 0.f, 0.f};
+          const int64_t kv = j * hd + (int64_t)h * d;
+          for (int e = 0; e < d; e += 4) {
+            const f32x4 kk = load_four(a.k, 0, k_vec, kv, e, d), vv = load_four(a.v, 0, k_vec, kv, e, d);
+            const f32x4 q = *reinterpret_cast<const f32x4*>(&s_q[h * kHeadStride + e]);
+            const f32x4 o = *reinterpret_cast<const f32x4*>(&s_do[h * kHeadStride + e]);
+#pragma unroll
+            for (int x = 0; x < 4; ++x) {
+              lg[x] = fmaf(q[x], kk[x], lg[x]);
+              dp[x] = fmaf(o[x], vv[x], dp[x]);
+            }
+          }
+          const float l = (lg[0] + lg[1]) + (lg[2] + lg[3]) + b;
+          p = stat[i][1] == 0.0f ? 0.0f : expf(l - stat[i][0]) * stat[i][1];
+          ds = p * (((dp[0] + dp[1]) + (dp[2] + dp[3])) - stat[i][2]);
+        }
+        s_ds[key * (HP + 4) + h] = ds;
+        if (there && h < H) {
+          const int64_t at = ((int64_t)h * a.rows + r) * a.n_tok + j;
+          a.p[at] = p;
+          a.ds[at] = ds;
+        }
+      }
+      __syncthreads();
+      if (a.dz && there) {
+        f32x4 acc[CT];
+        float s1 = 0.0f, s2 = 0.0f;
+#pragma unroll
+        for (int m = 0; m < CT; ++m) acc[m] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int i = 0; i < NH; ++i) {
+          const f32x4 ds = *reinterpret_cast<const f32x4*>(&s_ds[key * (HP + 4) + 4 * i]);
+#pragma unroll
+          for (int x = 0; x < 4; ++x)
+#pragma unroll
+            for (int m = 0; m < CT; ++m) {
+              const f32x4 w = *reinterpret_cast<const f32x4*>(&s_w[(4 * i + x) * CZ + 16 * m + 4 * qd]);
+#pragma unroll
+              for (int e = 0; e < 4; ++e) acc[m][e] = fmaf(ds[x], w[e], acc[m][e]);
+            }
+        }
+#pragma unroll
+        for (int m = 0; m < CT; ++m)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            s1 += acc[m][e];  // 0 past the row's end, as W' is
+            s2 = fmaf(acc[m][e], zh[m][e], s2);
+          }
+        s1 = quad_sum(s1) * inv_c;
+        s2 = quad_sum(s2) * inv_c;
+#pragma unroll
+        for (int m = 0; m < CT; ++m) {
+          const int c = 16 * m + 4 * qd;
+          f32x4 g;
+#pragma unroll
+          for (int e = 0; e < 4; ++e) g[e] = valid ? rstd * (acc[m][e] - s1 - zh[m][e] * s2) : 0.0f;
+          if (z_vec) {
+            if (c < c_z) {
+              if (a.z_bf16) {
+                bf16x4 o;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) o[e] = (__bf16)g[e];
+                *reinterpret_cast<bf16x4*>(static_cast<__bf16*>(a.dz) + off + c) = o;
+              } else {
+                *reinterpret_cast<f32x4*>(static_cast<float*>(a.dz) + off + c) = g;
+              }
+            }
+          } else {
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+              if (c + e < c_z) store_one(a.dz, a.z_bf16, off + c + e, g[e]);
+          }
+        }
+      }
+      if (tg < kGroups)
+        for (int x = tg; x < kBackKeys; x += kGroups) {
+          const float zc = s_zh[x * (CZ + 4) + tc];
+#pragma unroll
+          for (int i = 0; i < NH; ++i) {
+            const f32x4 ds = *reinterpret_cast<const f32x4*>(&s_ds[x * (HP + 4) + 4 * i]);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) t_sum[4 * i + e] = fmaf(ds[e], zc, t_sum[4 * i + e]);
+          }
+        }
+      if (dq_g < dq_groups) {
+        const int h = dq_x / d;
+        for (int x = dq_g; x < kBackKeys; x += dq_groups) {
+          const int64_t kj = t * kBackKeys + x;
+          if (kj < a.n_tok && (!a.mask || a.mask[kj] != 0)) {
+            dq = fmaf(s_ds[x * (HP + 4) + h], a.k[kj * hd + dq_x], dq);
+            if (tid + 256 < hd) dq2 = fmaf(s_ds[x * (HP + 4) + (tid + 256) / d], a.k[kj * hd + tid + 256], dq2);
+          }
+        }
+      }
+      __syncthreads();
+    }
+    s_dq[tid] = dq;
+    __syncthreads();
+    if (tid < hd) {
+      for (int g = 1; g < dq_groups; ++g) dq += s_dq[tid + g * hd];
+      a.dq_parts[((int64_t)part * a.n_q + row) * hd + tid] = dq * scale;
+      if (tid + 256 < hd) a.dq_parts[((int64_t)part * a.n_q + row) * hd + tid + 256] = dq2 * scale;
+    }
+  }
+  // T of this workgroup: its key groups in order, added to what earlier chunks left
+  __syncthreads();
+  float* out = a.t_parts + (int64_t)blockIdx.x * H * c_z;
+  for (int g = 0; g < kGroups; ++g) {
+    if (tg == g && tc < c_z)
+#pragma unroll
+      for (int h = 0; h < HP; ++h)
+        if (h < H) s_zh[h * CZ + tc] = g == 0 ? t_sum[h] : s_zh[h * CZ + tc] + t_sum[h];
+    __syncthreads();
+  }
+  for (int x = tid; x < H * c_z; x += 256) {
+    const float v = s_zh[(x / c_z) * CZ + x % c_z];
+    out[x] = a.first ? v : out[x] + v;
+  }
+}
+
+// ----------------------------------------------------------------------------- keys
+// dk and dv of 64 keys of one head over a share of the chunk's rows: a lane holds
+// a key, the four waves take every fourth row each, and q and do of a row, the
+// same for all lanes, come through the scalar cache.
+template <int DP>
+__global__ void __launch_bounds__(256) back_keys_kernel(BackKeysArgs a) {
+  __shared__ float s_sum[2 * DP][64];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int64_t j = (int64_t)blockIdx.x * 64 + lane;
+  const int h = blockIdx.y, split = blockIdx.z;
+  const bool there = j < a.n_tok;
+  int64_t count, first;
+  chunk_of(a.rows, a.n_splits, split, &count, &first);
+  float dk[DP], dv[DP];
+#pragma unroll
+  for (int e = 0; e < DP; ++e) dk[e] = dv[e] = 0.0f;
+  const int64_t jj = there ? j : a.n_tok - 1;
+  for (int64_t r = first + wave; r < first + count; r += 4) {
+    const int64_t at = ((int64_t)h * a.rows + r) * a.n_tok + jj;
+    const float p = a.p[at], ds = a.ds[at];
+    const float* q = a.qp + ((int64_t)h * a.n_q + a.row0 + r) * DP;
+    const float* o = a.dop + ((int64_t)h * a.n_q + a.row0 + r) * DP;
+#pragma unroll
+    for (int e = 0; e < DP; ++e) {
+      dk[e] = fmaf(ds, q[e], dk[e]);
+      dv[e] = fmaf(p, o[e], dv[e]);
+    }
+  }
+  for (int w = 3; w >= 1; --w) {
+    if (wave == w) {
+#pragma unroll
+      for (int e = 0; e < DP; ++e) {
+        s_sum[e][lane] = w == 3 ? dk[e] : s_sum[e][lane] + dk[e];
+        s_sum[DP + e][lane] = w == 3 ? dv[e] : s_sum[DP + e][lane] + dv[e];
+      }
+    }
+    __syncthreads();
+  }
+  if (wave > 0 || !there) return;
+  const int hd = a.n_heads * a.head_dim;
+  const float scale = 1.0f / sqrtf((float)a.head_dim);
+  float* out = a.kv_parts + ((int64_t)split * 2 * a.n_tok + j) * hd + (int64_t)h * a.head_dim;
+  const int64_t v_at = a.n_tok * hd;
+#pragma unroll
+  for (int e = 0; e < DP; ++e) {
+    if (e >= a.head_dim) break;
+    const float x = (dk[e] + s_sum[e][lane]) * scale, y = dv[e] + s_sum[DP + e][lane];
+    out[e] = a.first ? x : out[e] + x;
+    out[v_at + e] = a.first ? y : out[v_at + e] + y;
+  }
+}
+
+// ----------------------------------------------------------------------------- sums of parts
+// dq, dk and dv: one thread per element, parts in order. T: 16 columns by 16 groups
+// of parts per workgroup.
+__global__ void __launch_bounds__(256) back_sum_kernel(BackSumArgs a) {
+  __shared__ float s[16][17];
+  const int64_t n_dq = a.n_q * a.hd, n_kv = 2 * a.n_tok * a.hd;
+  if (blockIdx.x < a.token_blocks) {
+    const int64_t x = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    if (x < n_dq) {
+      float v = 0.0f;
+      for (int p = 0; p < a.dq_n; ++p) v += a.dq_parts[p * n_dq + x];
+      a.dq[x] = v * a.dq_scale;
+    } else if (x < n_dq + n_kv) {
+      float v = 0.0f;
+      for (int p = 0; p < a.kv_n; ++p) v += a.kv_parts[p * n_kv + x - n_dq];
+      a.dkv[x - n_dq] = v;
+    }
+    return;
+  }
+  const int cols = a.t_cols, col = (int)(blockIdx.x - a.token_blocks) * 16 + (threadIdx.x & 15), grp = threadIdx.x >> 4;
+  float v = 0.0f;
+  if (col < cols)
+    for (int p = grp; p < a.t_n; p += 16) v += a.t_parts[(int64_t)p * cols + col];
+  s[grp][threadIdx.x & 15] = v;
+  __syncthreads();
+  if (grp > 0 || col >= cols) return;
+#pragma unroll
+  for (int i = 1; i < 16; ++i) v += s[i][threadIdx.x];
+  a.t[col] = v * a.t_scale;
+}
+
+// ----------------------------------------------------------------------------- token products
+// ds = sum over x of dx W_x (64 tokens by 64 channels per workgroup) and dW_x = dx^T s
+// (64 outputs by 64 channels), on the fp32 matrix cores: a workgroup's four waves
+// take 32 x 32 each, operands 16 deep through LDS, the next 16 in flight.
+// v_mfma_f32_16x16x4_f32: A holds row n, B column n (n = lane % 16), both at
+// k-slot g = lane / 16; the accumulator holds rows 4g..4g+3 of column n.
+constexpr int kGemm = 64, kDeep = 16, kGemmStride = kGemm + 16;
+
+__global__ void __launch_bounds__(256) back_gemm_kernel(BackGemmArgs a) {
+  __shared__ __attribute__((aligned(16))) float s_a[2][kDeep][kGemmStride], s_b[2][kDeep][kGemmStride];
+  const int tid = threadIdx.x, lane = tid & 63, n = lane & 15, g = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int c_tiles = (a.c_s + kGemm - 1) / kGemm;
+  int64_t b = blockIdx.x;
+  const bool is_ds = b < a.ds_blocks;
+  if (!is_ds) b -= a.ds_blocks;
+  const int c0 = (int)(b % c_tiles) * kGemm;
+  b /= c_tiles;
+  const int splits = is_ds ? a.ds_splits : a.w_splits, split = (int)(b % splits);
+  b /= splits;
+  const int hd_deep = (a.hd + kDeep - 1) / kDeep * kDeep;
+  const int64_t m0 = is_ds ? b * kGemm : 0;                            // first token
+  const int o_tiles = (a.hd + kGemm - 1) / kGemm;
+  const int mat = is_ds ? 0 : (int)(b / o_tiles), o0 = is_ds ? 0 : (int)(b % o_tiles) * kGemm;
+  // terms of ds in the order k, v, q, g; the matrices of dW in the order q, k, v, g
+  const bool with_rows = m0 < a.q_row0 + a.n_q && m0 + kGemm > a.q_row0;
+  const bool stripe = mat == 0 || mat == 3;
+  const int64_t w_rows = stripe ? a.n_q : a.n_tok, s_row0 = stripe ? a.q_row0 : 0;
+  const float* dx = mat == 0 ? a.dq : mat == 1 ? a.dk : mat == 2 ? a.dv : a.dg;
+  const int64_t depth = is_ds ? (int64_t)hd_deep * (with_rows ? 4 : 2) : (w_rows + kDeep - 1) / kDeep * kDeep;
+  int64_t steps, first;
+  chunk_of(depth / kDeep, splits, split, &steps, &first);
+  const int hd_vec = a.hd % 4 == 0, s_vec = a.c_s % 4 == 0;
+  const int r16 = tid >> 4, x4 = (tid & 15) * 4;  // 16 deep by 64 wide, four a thread
+  f32x4 av, bv;
+  auto fetch = [&](int64_t step) {
+    const int64_t k0 = step * kDeep;
+    if (is_ds) {
+      const int term = (int)(k0 / hd_deep), o = (int)(k0 % hd_deep);
+      const float* x = term == 0 ? a.dk : term == 1 ? a.dv : term == 2 ? a.dq : a.dg;
+      const float* w = term == 0 ? a.w_k : term == 1 ? a.w_v : term == 2 ? a.w_q : a.w_g;
+      // A: token tid / 4, outputs o + 4 (tid % 4) ..
+      const int64_t row = m0 + (tid >> 2) - (term >= 2 ? a.q_row0 : 0), rows = term >= 2 ? a.n_q : a.n_tok;
+      av = row >= 0 && row < rows ? load_four(x, 0, hd_vec, row * a.hd, o + 4 * (tid & 3), a.hd) : f32x4{0.f, 0.f, 0.f, 0.f};
+      bv = o + r16 < a.hd ? load_four(w, 0, s_vec && a.w_vec, (int64_t)(o + r16) * a.c_s, c0 + x4, a.c_s)
+                          : f32x4{0.f, 0.f, 0.f, 0.f};
+    } else {
+      const int64_t t = k0 + r16;
+      const bool in = t < w_rows;
+      av = in ? load_four(dx, 0, hd_vec, t * a.hd, o0 + x4, a.hd) : f32x4{0.f, 0.f, 0.f, 0.f};
+      // a masked token's s does not enter the gradients of W_k and W_v
+      const bool used = in && (stripe || !a.mask || a.mask[t] != 0);
+      bv = used ? load_four(a.s, a.s_bf16, s_vec, (s_row0 + t) * a.c_s, c0 + x4, a.c_s) : f32x4{0.f, 0.f, 0.f, 0.f};
+    }
+  };
+  auto stage = [&](int buf) {
+    if (is_ds) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) s_a[buf][4 * (tid & 3) + i][tid >> 2] = av[i];
+    } else {
+      *reinterpret_cast<f32x4*>(&s_a[buf][r16][x4]) = av;
+    }
+    *reinterpret_cast<f32x4*>(&s_b[buf][r16][x4]) = bv;
+  };
+  f32x4 acc[2][2];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) acc[i >> 1][i & 1] = f32x4{0.f, 0.f, 0.f, 0.f};
+  const int am = 32 * (wave >> 1), bn = 32 * (wave & 1);
+  if (steps > 0) {
+    fetch(first);
+    stage(0);
+  }
+  for (int64_t i = 0; i < steps; ++i) {
+    __syncthreads();
+    const int buf = (int)(i & 1);
+    if (i + 1 < steps) fetch(first + i + 1);
+#pragma unroll
+    for (int k = 0; k < kDeep / 4; ++k) {
+      float x[2], y[2];
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
+        x[u] = s_a[buf][4 * k + g][am + 16 * u + n];
+        y[u] = s_b[buf][4 * k + g][bn + 16 * u + n];
+      }
+#pragma unroll
+      for (int u = 0; u < 2; ++u)
+#pragma unroll
+        for (int w = 0; w < 2; ++w) acc[u][w] = __builtin_amdgcn_mfma_f32_16x16x4f32(x[u], y[w], acc[u][w], 0, 0, 0);
+    }
+    if (i + 1 < steps) stage(buf ^ 1);
+  }
+  const int64_t m_end = is_ds ? a.n_tok : a.hd;
+  float* out = is_ds ? a.ds_parts + (int64_t)split * a.n_tok * a.c_s : a.w_parts + ((int64_t)split * 4 + mat) * a.hd * a.c_s;
+#pragma unroll
+  for (int u = 0; u < 2; ++u)
+#pragma unroll
+    for (int w = 0; w < 2; ++w)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int64_t m = (is_ds ? m0 : o0) + am + 16 * u + 4 * g + i;
+        const int c = c0 + bn + 16 * w + n;
+        if (m < m_end && c < a.c_s) out[m * a.c_s + c] = acc[u][w][i];
+      }
+}
+
+// The gradients in their own type: sums of the products' splits, then dW_b and dgamma
+// from T.
+__global__ void __launch_bounds__(256) back_finish_kernel(BackFinishArgs a) {
+  const int64_t n_ds = a.ds ? a.n_tok * a.c_s : 0, n_w = (int64_t)a.hd * a.c_s, n_b = (int64_t)a.n_heads * a.c_z;
+  int64_t x = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  if (x < n_ds) {
+    float v = 0.0f;
+    for (int p = 0; p < a.ds_splits; ++p) v += a.ds_parts[p * n_ds + x];
+    store_one(a.ds, a.bf16, x, v);
+    return;
+  }
+  x -= n_ds;
+  if (x < 4 * n_w) {
+    const int mat = (int)(x / n_w);
+    if (!a.dw[mat]) return;
+    float v = 0.0f;
+    for (int p = 0; p < a.w_splits; ++p) v += a.w_parts[p * 4 * n_w + x];
+    store_one(a.dw[mat], a.bf16, x - mat * n_w, v);
+    return;
+  }
+  x -= 4 * n_w;
+  if (x < n_b) {
+    if (a.dw_b) store_one(a.dw_b, a.bf16, x, a.t ? a.t[x] * (a.gamma ? a.gamma[x % a.c_z] : 1.0f) : 0.0f);
+    return;
+  }
+  x -= n_b;
+  if (x < a.c_z && a.dgamma) {
+    float v = 0.0f;
+    for (int h = 0; a.t && h < a.n_heads; ++h) v = fmaf(a.w_b[h * (int64_t)a.c_z + x], a.t[h * (int64_t)a.c_z + x], v);
+    store_one(a.dgamma, a.bf16, x, v);
+  }
+}
+
+template <int CT>
+hipError_t pairs_go(const BackPairsArgs& a, unsigned grid, hipStream_t st) {
+  if (a.n_heads <= 4)
+    hipLaunchKernelGGL((back_pairs_kernel<CT, 1>), dim3(grid), dim3(256), 0, st, a);
+  else if (a.n_heads <= 8)
+    hipLaunchKernelGGL((back_pairs_kernel<CT, 2>), dim3(grid), dim3(256), 0, st, a);
+  else
+    hipLaunchKernelGGL((back_pairs_kernel<CT, 4>), dim3(grid), dim3(256), 0, st, a);
+  return hipGetLastError();
+}
+
+unsigned blocks_of(int64_t items) { return (unsigned)((items + 255) / 256); }
+
+}  // namespace
+
+hipError_t launch_back_rows(const BackRowsArgs& a, hipStream_t st) {
+  hipLaunchKernelGGL(back_rows_kernel, dim3(blocks_of(a.n_q * a.n_heads)), dim3(256), 0, st, a);
+  return hipGetLastError();
+}
+
+int back_pairs_groups(int64_t rows, int n_parts) {
+  const int64_t items = rows * n_parts;
+  return (int)(items < kBackMaxGroups ? items : kBackMaxGroups);
+}
+
+hipError_t launch_back_pairs(const BackPairsArgs& a, int groups, hipStream_t st) {
+  if (a.c_z <= 32) return pairs_go<2>(a, (unsigned)groups, st);
+  if (a.c_z <= 64) return pairs_go<4>(a, (unsigned)groups, st);
+  if (a.c_z <= 128) return pairs_go<8>(a, (unsigned)groups, st);
+  return pairs_go<16>(a, (unsigned)groups, st);
+}
+
+hipError_t launch_back_keys(const BackKeysArgs& a, int dp, hipStream_t st) {
+  const dim3 grid((unsigned)((a.n_tok + 63) / 64), (unsigned)a.n_heads, (unsigned)a.n_splits);
+  if (dp == 16)
+    hipLaunchKernelGGL(back_keys_kernel<16>, grid, dim3(256), 0, st, a);
+  else if (dp == 32)
+    hipLaunchKernelGGL(back_keys_kernel<32>, grid, dim3(256), 0, st, a);
+  else
+    hipLaunchKernelGGL(back_keys_kernel<64>, grid, dim3(256), 0, st, a);
+  return hipGetLastError();
+}
+
+hipError_t launch_back_sum(const BackSumArgs& a, hipStream_t st) {
+  BackSumArgs b = a;
+  b.token_blocks = blocks_of(a.n_q * a.hd + 2 * a.n_tok * a.hd);
+  hipLaunchKernelGGL(back_sum_kernel, dim3(b.token_blocks + (unsigned)((a.t_cols + 15) / 16)), dim3(256), 0, st, b);
+  return hipGetLastError();
+}
+
+// Splits of the token products' depths: until about four workgroups a CU share them,
+// each at least 128 deep.
+void back_gemm_splits(int64_t n_tok, int32_t hd, int32_t c_s, int* ds_splits, int* w_splits) {
+  const int64_t c_tiles = (c_s + kGemm - 1) / kGemm, o_tiles = (hd + kGemm - 1) / kGemm;
+  const int64_t t_tiles = (n_tok + kGemm - 1) / kGemm;
+  auto fit = [](int64_t tiles, int64_t depth) {
+    int64_t want = 1024 / (tiles < 1 ? 1 : tiles), most = depth / 128;
+    if (want > most) want = most;
+    if (want > 16) want = 16;
+    return (int)(want < 1 ? 1 : want);
+  };
+  *ds_splits = fit(2 * t_tiles * c_tiles, 4 * (int64_t)hd);
+  *w_splits = fit(4 * o_tiles * c_tiles, n_tok);
+}
+
+hipError_t launch_back_gemm(const BackGemmArgs& a, hipStream_t st) {
+  BackGemmArgs b = a;
+  const int64_t c_tiles = (a.c_s + kGemm - 1) / kGemm;
+  const int64_t ds_blocks = a.ds_parts ? (a.n_tok + kGemm - 1) / kGemm * c_tiles * a.ds_splits : 0;
+  const int64_t w_blocks = a.w_parts ? 4 * ((a.hd + kGemm - 1) / kGemm) * c_tiles * a.w_splits : 0;
+  if (ds_blocks + w_blocks == 0) return hipSuccess;
+  b.ds_blocks = ds_blocks;
+  b.w_vec = ((reinterpret_cast<uintptr_t>(a.w_q) | reinterpret_cast<uintptr_t>(a.w_k) | reinterpret_cast<uintptr_t>(a.w_v) |
+              reinterpret_cast<uintptr_t>(a.w_g)) & 15) == 0;
+  hipLaunchKernelGGL(back_gemm_kernel, dim3((unsigned)(ds_blocks + w_blocks)), dim3(256), 0, st, b);
+  return hipGetLastError();
+}
+
+hipError_t launch_back_finish(const BackFinishArgs& a, hipStream_t st) {
+  const int64_t n = (a.ds ? a.n_tok * a.c_s : 0) + 4 * (int64_t)a.hd * a.c_s + (int64_t)a.n_heads * a.c_z + a.c_z;
+  hipLaunchKernelGGL(back_finish_kernel, dim3(blocks_of(n)), dim3(256), 0, st, a);
+  return hipGetLastError();
+}
+
+}  // namespace dcp

@@ -1016,3 +1016,387 @@ int dcp_scatter_mean(int64_t n_atoms, int64_t n_tokens, int32_t c, int32_t in_dt
 }
 
 }  // extern "C"
+
+// ----------------------------------------------------------------------------- LayerNorm
+namespace {
+
+int check_layer_norm(int64_t n_rows, int32_t c, int32_t in_dtype, int32_t out_dtype, float ln_eps) {
+  if (n_rows < 0) return fail(DCP_ERR_INVALID_ARGUMENT, "n_rows must be >= 0 (got %lld)", (long long)n_rows);
+  if (c < 1) return fail(DCP_ERR_INVALID_ARGUMENT, "c must be >= 1");
+  if ((in_dtype != DCP_F32 && in_dtype != DCP_BF16) || (out_dtype != DCP_F32 && out_dtype != DCP_BF16))
+    return fail(DCP_ERR_INVALID_ARGUMENT, "dtypes must be DCP_F32 or DCP_BF16");
+  if (!(ln_eps >= 0.0f) || !isfinite(ln_eps)) return fail(DCP_ERR_INVALID_ARGUMENT, "ln_eps must be finite and >= 0");
+  if (c > dcp::kLnMaxC) return fail(DCP_ERR_UNSUPPORTED, "c must be <= %d (got %d)", dcp::kLnMaxC, c);
+  if (n_rows > (int64_t)1 << 48) return fail(DCP_ERR_INVALID_ARGUMENT, "n_rows too large");
+  return DCP_OK;
+}
+
+// `out` may be `in` itself where a row takes the same bytes in both, or lies apart from it.
+bool apart_or_same(const void* in, size_t in_bytes, const void* out, size_t out_bytes) {
+  const char *i = static_cast<const char*>(in), *o = static_cast<const char*>(out);
+  return (i == o && in_bytes == out_bytes) || i + in_bytes <= o || o + out_bytes <= i;
+}
+
+size_t layer_norm_back_ws(int64_t n_rows, int32_t c) {
+  return round_up((size_t)dcp::layer_norm_back_groups(n_rows, c) * 2 * c * sizeof(float), 256);
+}
+
+size_t elem(int32_t dtype) { return dtype == DCP_BF16 ? 2 : 4; }
+
+}  // namespace
+
+extern "C" {
+
+int dcp_layer_norm(int64_t n_rows, int32_t c, int32_t in_dtype, int32_t out_dtype, float ln_eps, const void* x,
+                   const float* ln_gamma, const float* ln_beta, void* y, void* stream) {
+  const int rc = check_layer_norm(n_rows, c, in_dtype, out_dtype, ln_eps);
+  if (rc) return rc;
+  if (n_rows == 0) return ok();
+  if (!x || !y) return fail(DCP_ERR_INVALID_ARGUMENT, "x and y are required");
+  if (!aligned(x, elem(in_dtype)) || !aligned(y, elem(out_dtype)) || !aligned(ln_gamma, 4) || !aligned(ln_beta, 4))
+    return fail(DCP_ERR_INVALID_ARGUMENT, "x, y, ln_gamma and ln_beta must be aligned to their element size");
+  if (!apart_or_same(x, (size_t)n_rows * c * elem(in_dtype), y, (size_t)n_rows * c * elem(out_dtype)))
+    return fail(DCP_ERR_INVALID_ARGUMENT, "y must equal x, in the same type, or not overlap it");
+  dcp::LayerNormArgs a{};
+  a.n_rows = n_rows;
+  a.c = c;
+  a.y_bf16 = out_dtype == DCP_BF16;
+  a.x = x;
+  a.gamma = ln_gamma;
+  a.beta = ln_beta;
+  a.y = y;
+  a.eps = ln_eps;
+  const hipError_t e = dcp::launch_layer_norm(a, in_dtype == DCP_BF16, static_cast<hipStream_t>(stream));
+  if (e != hipSuccess) return fail(DCP_ERR_HIP, "LayerNorm launch failed: %s", hipGetErrorString(e));
+  return ok();
+}
+
+int dcp_layer_norm_backward_workspace_size(int64_t n_rows, int32_t c, size_t* bytes) {
+  if (!bytes) return fail(DCP_ERR_INVALID_ARGUMENT, "bytes is NULL");
+  const int rc = check_layer_norm(n_rows, c, DCP_F32, DCP_F32, 0.0f);
+  if (rc) return rc;
+  *bytes = n_rows == 0 ? 0 : layer_norm_back_ws(n_rows, c);
+  return ok();
+}
+
+int dcp_layer_norm_backward(int64_t n_rows, int32_t c, int32_t in_dtype, int32_t out_dtype, float ln_eps, const void* x,
+                            const float* ln_gamma, const void* dy, void* dx, float* dln_gamma, float* dln_beta,
+                            void* workspace, size_t workspace_bytes, void* stream) {
+  const int rc = check_layer_norm(n_rows, c, in_dtype, out_dtype, ln_eps);
+  if (rc) return rc;
+  if (n_rows > 0 && (!x || !dy)) return fail(DCP_ERR_INVALID_ARGUMENT, "x and dy are required");
+  if (!dx && !dln_gamma && !dln_beta)
+    return fail(DCP_ERR_INVALID_ARGUMENT, "at least one of dx, dln_gamma and dln_beta is required");
+  if (!aligned(x, elem(in_dtype)) || !aligned(dx, elem(in_dtype)) || !aligned(dy, elem(out_dtype)) ||
+      !aligned(ln_gamma, 4) || !aligned(dln_gamma, 4) || !aligned(dln_beta, 4))
+    return fail(DCP_ERR_INVALID_ARGUMENT, "the tensors must be aligned to their element size");
+  const size_t xb = (size_t)n_rows * c * elem(in_dtype), yb = (size_t)n_rows * c * elem(out_dtype);
+  if (dx && n_rows > 0 && (!apart_or_same(x, xb, dx, xb) || !apart_or_same(dy, yb, dx, xb)))
+    return fail(DCP_ERR_INVALID_ARGUMENT, "dx must equal x or dy, in the same type, or not overlap them");
+  dcp::LayerNormBackArgs a{};
+  a.n_rows = n_rows;
+  a.c = c;
+  a.dy_bf16 = out_dtype == DCP_BF16;
+  a.x = x;
+  a.dy = dy;
+  a.gamma = ln_gamma;
+  a.dx = dx;
+  a.dgamma = dln_gamma;
+  a.dbeta = dln_beta;
+  a.eps = ln_eps;
+  const bool sums = dln_gamma || dln_beta;
+  if (n_rows > 0 && sums) {
+    const size_t need = layer_norm_back_ws(n_rows, c);
+    if (!workspace || !aligned(workspace, 256))
+      return fail(DCP_ERR_WORKSPACE, "workspace must be a 256-byte aligned device pointer");
+    if (workspace_bytes < need)
+      return fail(DCP_ERR_WORKSPACE, "workspace too small: %zu bytes given, %zu needed", workspace_bytes, need);
+    a.parts = static_cast<float*>(workspace);
+  }
+  const hipError_t e = dcp::launch_layer_norm_back(a, in_dtype == DCP_BF16, static_cast<hipStream_t>(stream));
+  if (e != hipSuccess) return fail(DCP_ERR_HIP, "LayerNorm backward launch failed: %s", hipGetErrorString(e));
+  return ok();
+}
+
+}  // extern "C"
+
+// ----------------------------------------------------------------------------- attention backward
+namespace {
+
+// Most bytes of P and dS that the general path keeps at a time: the stripe's rows
+// are taken in chunks of as many as fit, at least one.
+constexpr size_t kBackPairBytes = (size_t)256 << 20;
+
+struct BackLayout {
+  int64_t chunk;  // rows at a time
+  int dp, dq_parts, groups, kv_splits, ds_splits, w_splits;
+  size_t off_q, off_k, off_v, off_g, off_qp, off_dop, off_stat, off_p, off_ds, off_dq_parts, off_t_parts, off_kv_parts,
+      off_dq, off_dkv, off_dg, off_t, off_ds_parts, off_w_parts, total;
+};
+
+void back_layout(const dcp_shape* sh, int64_t n_q, BackLayout* L) {
+  const int64_t N = sh->n_tokens, H = sh->n_heads, hd = H * sh->head_dim;
+  size_t off = 0;
+  auto take = [&](size_t floats) {
+    const size_t o = off;
+    off = round_up(off + floats * sizeof(float), 256);
+    return o;
+  };
+  L->dp = sh->head_dim <= 16 ? 16 : sh->head_dim <= 32 ? 32 : 64;
+  L->chunk = (int64_t)(kBackPairBytes / ((size_t)2 * H * N * sizeof(float)));
+  if (L->chunk < 1) L->chunk = 1;
+  if (L->chunk > n_q) L->chunk = n_q;
+  const int64_t tiles = (N + 63) / 64;
+  // workgroups for the whole chip from few rows: keys split between them
+  int64_t parts = dcp::kBackMaxGroups / L->chunk;
+  L->dq_parts = (int)(parts < 1 ? 1 : parts > tiles ? tiles : parts);
+  L->groups = dcp::back_pairs_groups(L->chunk, L->dq_parts);
+  int64_t splits = 1024 / (tiles * H), most = (L->chunk + 15) / 16;
+  if (splits > most) splits = most;
+  L->kv_splits = (int)(splits < 1 ? 1 : splits > 16 ? 16 : splits);
+  dcp::back_gemm_splits(N, (int32_t)hd, sh->c_s, &L->ds_splits, &L->w_splits);
+  L->off_q = take((size_t)n_q * hd);
+  L->off_k = take((size_t)N * hd);
+  L->off_v = take((size_t)N * hd);
+  L->off_g = take((size_t)n_q * hd);
+  L->off_qp = take((size_t)H * n_q * L->dp);
+  L->off_dop = take((size_t)H * n_q * L->dp);
+  L->off_stat = take((size_t)H * n_q * 4);
+  L->off_p = take((size_t)H * L->chunk * N);
+  L->off_ds = take((size_t)H * L->chunk * N);
+  L->off_dq_parts = take((size_t)L->dq_parts * n_q * hd);
+  L->off_t_parts = take((size_t)L->groups * H * sh->c_z);
+  L->off_kv_parts = take((size_t)L->kv_splits * 2 * N * hd);
+  L->off_dq = take((size_t)n_q * hd);
+  L->off_dkv = take((size_t)2 * N * hd);
+  L->off_dg = take((size_t)n_q * hd);
+  L->off_t = take((size_t)H * sh->c_z);
+  L->off_ds_parts = take((size_t)L->ds_splits * N * sh->c_s);
+  L->off_w_parts = take((size_t)L->w_splits * 4 * hd * sh->c_s);
+  L->total = off;
+}
+
+}  // namespace
+
+extern "C" {
+
+int dcp_pair_bias_attention_backward_workspace_size(const dcp_shape* shape, int64_t n_q, size_t* bytes) {
+  if (!bytes) return fail(DCP_ERR_INVALID_ARGUMENT, "bytes is NULL");
+  Path path;
+  const int rc = check_call(shape, n_q, 1, &path);
+  if (rc) return rc;
+  if (n_q == 0) {
+    *bytes = 0;
+    return ok();
+  }
+  BackLayout L;
+  back_layout(shape, n_q, &L);
+  *bytes = L.total;
+  return ok();
+}
+
+int dcp_pair_bias_attention_backward(const dcp_shape* shape, const dcp_weights* w, const void* s, const void* z_rows,
+                                     const uint8_t* key_mask, int64_t q_row0, int64_t n_q, const float* m,
+                                     const float* l, const float* acc, const void* dout, const dcp_gradients* grads,
+                                     void* workspace, size_t workspace_bytes, void* stream) {
+  Path path;
+  int rc = check_call(shape, n_q, 1, &path);
+  if (rc) return rc;
+  if (q_row0 < 0 || q_row0 > shape->n_tokens - n_q)
+    return fail(DCP_ERR_INVALID_ARGUMENT, "need 0 <= q_row0 and q_row0 + n_q <= n_tokens (q_row0 %lld, n_q %lld)",
+                (long long)q_row0, (long long)n_q);
+  if (!w || !grads) return fail(DCP_ERR_INVALID_ARGUMENT, "weights and gradients are required");
+  if (!w->w_q || !w->w_k || !w->w_v || !w->w_g || !w->w_b)
+    return fail(DCP_ERR_INVALID_ARGUMENT, "w_q, w_k, w_v, w_g and w_b are required");
+  if (!s || !z_rows || !m || !l || !acc || !dout)
+    return fail(DCP_ERR_INVALID_ARGUMENT, "s, z_rows, m, l, acc and dout are required");
+  if (grads->dtype != DCP_F32 && grads->dtype != DCP_BF16)
+    return fail(DCP_ERR_INVALID_ARGUMENT, "the gradients' dtype must be DCP_F32 or DCP_BF16");
+  void* const out[] = {grads->dz_rows, grads->ds, grads->dw_q, grads->dw_k, grads->dw_v, grads->dw_g, grads->dw_b,
+                       grads->dln_gamma};
+  bool any = false;
+  for (void* p : out) any = any || p;
+  if (!any) return fail(DCP_ERR_INVALID_ARGUMENT, "no gradient is asked for");
+  if (!aligned(s, 16) || !aligned(z_rows, 16) || !aligned(dout, 16) || !aligned(m, 16) || !aligned(l, 16) || !aligned(acc, 16))
+    return fail(DCP_ERR_INVALID_ARGUMENT, "s, z_rows, m, l, acc and dout must be 16-byte aligned");
+  for (void* p : out)
+    if (!aligned(p, 16)) return fail(DCP_ERR_INVALID_ARGUMENT, "the gradients must be 16-byte aligned");
+  if (path == kPathFast && (!aligned(w->w_q, 16) || !aligned(w->w_k, 16) || !aligned(w->w_v, 16) ||
+                            !aligned(w->w_g, 16) || !aligned(w->w_b, 16) || !aligned(w->ln_gamma, 16)))
+    return fail(DCP_ERR_INVALID_ARGUMENT, "w_q, w_k, w_v, w_g, w_b and ln_gamma must be 16-byte aligned");
+  BackLayout L{};
+  if (n_q > 0) back_layout(shape, n_q, &L);
+  if (n_q > 0 && (!workspace || !aligned(workspace, 256)))
+    return fail(DCP_ERR_WORKSPACE, "workspace must be a 256-byte aligned device pointer");
+  if (workspace_bytes < L.total)
+    return fail(DCP_ERR_WORKSPACE, "workspace too small: %zu bytes given, %zu needed", workspace_bytes, L.total);
+  char* ws = static_cast<char*>(workspace);
+  auto at = [&](size_t off) { return reinterpret_cast<float*>(ws + off); };
+  hipStream_t st = static_cast<hipStream_t>(stream);
+  const int64_t N = shape->n_tokens;
+  const int hd = shape->n_heads * shape->head_dim;
+  const bool act_bf16 = shape->act_dtype == DCP_BF16;
+  hipError_t e;
+  dcp::BackFinishArgs fa{};
+  fa.n_tok = N;
+  fa.n_heads = shape->n_heads;
+  fa.hd = hd;
+  fa.c_s = shape->c_s;
+  fa.c_z = shape->c_z;
+  fa.bf16 = grads->dtype == DCP_BF16;
+  fa.w_b = w->w_b;
+  fa.gamma = w->ln_gamma;
+  fa.ds = grads->ds;
+  fa.dw[0] = grads->dw_q;
+  fa.dw[1] = grads->dw_k;
+  fa.dw[2] = grads->dw_v;
+  fa.dw[3] = grads->dw_g;
+  fa.dw_b = grads->dw_b;
+  fa.dgamma = grads->dln_gamma;
+  if (n_q == 0) {  // the share of a stripe without rows: zeros
+    if ((e = dcp::launch_back_finish(fa, st)) != hipSuccess)
+      return fail(DCP_ERR_HIP, "gradient output launch failed: %s", hipGetErrorString(e));
+    return ok();
+  }
+
+  dcp::GenProjArgs pa{};
+  pa.s = s;
+  pa.s_bf16 = act_bf16;
+  pa.w_q = w->w_q;
+  pa.w_k = w->w_k;
+  pa.w_v = w->w_v;
+  pa.w_g = w->w_g;
+  pa.n_tok = N;
+  pa.q_row0 = q_row0;
+  pa.n_q = n_q;
+  pa.c_s = shape->c_s;
+  pa.hd = hd;
+  pa.mask = key_mask;
+  pa.q = at(L.off_q);
+  pa.k = at(L.off_k);
+  pa.v = at(L.off_v);
+  pa.g = at(L.off_g);
+  if ((e = dcp::launch_gen_proj(pa, st)) != hipSuccess)
+    return fail(DCP_ERR_HIP, "projection launch failed: %s", hipGetErrorString(e));
+
+  dcp::BackRowsArgs ra{};
+  ra.n_q = n_q;
+  ra.n_heads = shape->n_heads;
+  ra.head_dim = shape->head_dim;
+  ra.dp = L.dp;
+  ra.dout_bf16 = shape->out_dtype == DCP_BF16;
+  ra.m = m;
+  ra.l = l;
+  ra.acc = acc;
+  ra.g = pa.g;
+  ra.q = pa.q;
+  ra.dout = dout;
+  ra.qp = at(L.off_qp);
+  ra.dop = at(L.off_dop);
+  ra.stat = at(L.off_stat);
+  ra.dg = at(L.off_dg);
+  if ((e = dcp::launch_back_rows(ra, st)) != hipSuccess)
+    return fail(DCP_ERR_HIP, "row gradient launch failed: %s", hipGetErrorString(e));
+
+  for (int64_t row = 0; row < n_q; row += L.chunk) {
+    const int64_t rows = row + L.chunk <= n_q ? L.chunk : n_q - row;
+    dcp::BackPairsArgs ba{};
+    ba.z = z_rows;
+    ba.z_bf16 = act_bf16;
+    ba.mask = key_mask;
+    ba.w_b = w->w_b;
+    ba.gamma = w->ln_gamma;
+    ba.k = pa.k;
+    ba.v = pa.v;
+    ba.qp = ra.qp;
+    ba.dop = ra.dop;
+    ba.stat = ra.stat;
+    ba.n_tok = N;
+    ba.n_q = n_q;
+    ba.row0 = row;
+    ba.rows = rows;
+    ba.c_z = shape->c_z;
+    ba.n_heads = shape->n_heads;
+    ba.head_dim = shape->head_dim;
+    ba.dp = L.dp;
+    ba.n_parts = L.dq_parts;
+    ba.first = row == 0;
+    ba.eps = shape->ln_eps;
+    ba.p = at(L.off_p);
+    ba.ds = at(L.off_ds);
+    ba.dz = grads->dz_rows;
+    ba.dq_parts = at(L.off_dq_parts);
+    ba.t_parts = at(L.off_t_parts);
+    if ((e = dcp::launch_back_pairs(ba, dcp::back_pairs_groups(rows, L.dq_parts), st)) != hipSuccess)
+      return fail(DCP_ERR_HIP, "pair gradient launch failed: %s", hipGetErrorString(e));
+    dcp::BackKeysArgs ka{};
+    ka.p = ba.p;
+    ka.ds = ba.ds;
+    ka.qp = ra.qp;
+    ka.dop = ra.dop;
+    ka.n_tok = N;
+    ka.n_q = n_q;
+    ka.row0 = row;
+    ka.rows = rows;
+    ka.n_heads = shape->n_heads;
+    ka.head_dim = shape->head_dim;
+    ka.n_splits = L.kv_splits;
+    ka.first = row == 0;
+    ka.kv_parts = at(L.off_kv_parts);
+    if ((e = dcp::launch_back_keys(ka, L.dp, st)) != hipSuccess)
+      return fail(DCP_ERR_HIP, "key gradient launch failed: %s", hipGetErrorString(e));
+  }
+
+  dcp::BackSumArgs sa{};
+  sa.n_tok = N;
+  sa.n_q = n_q;
+  sa.hd = hd;
+  sa.dq_n = L.dq_parts;
+  sa.kv_n = L.kv_splits;
+  sa.t_n = L.groups;
+  sa.t_cols = shape->n_heads * shape->c_z;
+  sa.dq_parts = at(L.off_dq_parts);
+  sa.kv_parts = at(L.off_kv_parts);
+  sa.t_parts = at(L.off_t_parts);
+  sa.dq_scale = sa.t_scale = 1.0f;
+  sa.dq = at(L.off_dq);
+  sa.dkv = at(L.off_dkv);
+  sa.t = at(L.off_t);
+  if ((e = dcp::launch_back_sum(sa, st)) != hipSuccess)
+    return fail(DCP_ERR_HIP, "gradient sum launch failed: %s", hipGetErrorString(e));
+
+  dcp::BackGemmArgs ga{};
+  ga.n_tok = N;
+  ga.q_row0 = q_row0;
+  ga.n_q = n_q;
+  ga.hd = hd;
+  ga.c_s = shape->c_s;
+  ga.s_bf16 = act_bf16;
+  ga.s = s;
+  ga.mask = key_mask;
+  ga.w_q = w->w_q;
+  ga.w_k = w->w_k;
+  ga.w_v = w->w_v;
+  ga.w_g = w->w_g;
+  ga.dq = sa.dq;
+  ga.dk = sa.dkv;
+  ga.dv = sa.dkv + N * hd;
+  ga.dg = ra.dg;
+  ga.ds_splits = L.ds_splits;
+  ga.w_splits = L.w_splits;
+  ga.ds_parts = grads->ds ? at(L.off_ds_parts) : nullptr;
+  ga.w_parts = grads->dw_q || grads->dw_k || grads->dw_v || grads->dw_g ? at(L.off_w_parts) : nullptr;
+  if ((e = dcp::launch_back_gemm(ga, st)) != hipSuccess)
+    return fail(DCP_ERR_HIP, "token gradient launch failed: %s", hipGetErrorString(e));
+
+  fa.ds_splits = L.ds_splits;
+  fa.w_splits = L.w_splits;
+  fa.ds_parts = ga.ds_parts;
+  fa.w_parts = ga.w_parts;
+  fa.t = sa.t;
+  if ((e = dcp::launch_back_finish(fa, st)) != hipSuccess)
+    return fail(DCP_ERR_HIP, "gradient output launch failed: %s", hipGetErrorString(e));
+  return ok();
+}
+
+}  // extern "C"

@@ -222,6 +222,98 @@ struct ScatterArgs {
   int64_t* plan;          // [n_tokens][2] first atom and one past the last of each token (workspace)
 };
 
+// LayerNorm over rows of up to 4096 channels.
+constexpr int kLnMaxC = 4096;
+
+struct LayerNormArgs {
+  int64_t n_rows;
+  int32_t c, y_bf16;
+  const void* x;               // [n_rows][c]
+  const float *gamma, *beta;   // [c] or null
+  void* y;                     // [n_rows][c], may be x
+  float eps;
+  int32_t lanes;               // set by the launcher: lanes that share a row
+};
+
+struct LayerNormBackArgs {
+  int64_t n_rows;
+  int32_t c, dy_bf16;
+  const void *x, *dy;          // [n_rows][c]
+  const float* gamma;          // [c] or null
+  void* dx;                    // [n_rows][c] in x's type, or null
+  float *dgamma, *dbeta;       // [c] or null
+  float* parts;                // [layer_norm_back_groups()][2][c] (workspace); null: no weights' gradient wanted
+  float eps;
+  int32_t lanes;               // as above
+};
+
+// Backward pass of the attention (backward.hip). Rows are those of the stripe;
+// [H][n_q][dp] holds a head's channels padded with zeros to dp.
+constexpr int kBackMaxGroups = 1024;  // most workgroups (one T each) of the general pair kernel
+
+struct BackRowsArgs {
+  int64_t n_q;
+  int32_t n_heads, head_dim, dp, dout_bf16;
+  const float *m, *l;      // [H][n_q]
+  const float *acc, *g, *q;  // [n_q][hd]
+  const void* dout;        // [n_q][hd]
+  float *qp, *dop;         // [H][n_q][dp]
+  float* stat;             // [H][n_q][4]: m, 1 / L, D, -
+  float* dg;               // [n_q][hd]
+};
+
+struct BackPairsArgs {
+  const void* z;           // [n_q][N][c_z]
+  int32_t z_bf16;
+  const uint8_t* mask;     // [N] or null
+  const float *w_b, *gamma;
+  const float *k, *v;      // [N][hd]
+  const float *qp, *dop, *stat;
+  int64_t n_tok, n_q, row0, rows;  // rows [row0, row0 + rows) of the stripe
+  int32_t c_z, n_heads, head_dim, dp, n_parts, first;
+  float eps;
+  float *p, *ds;           // [H][rows][N]
+  void* dz;                // as z, or null
+  float* dq_parts;         // [n_parts][n_q][hd]
+  float* t_parts;          // [groups][H][c_z]
+};
+
+struct BackKeysArgs {
+  const float *p, *ds, *qp, *dop;
+  int64_t n_tok, n_q, row0, rows;
+  int32_t n_heads, head_dim, n_splits, first;
+  float* kv_parts;         // [n_splits][2][N][hd]
+};
+
+struct BackSumArgs {
+  int64_t n_tok, n_q;
+  int32_t hd, dq_n, kv_n, t_n, t_cols;
+  const float *dq_parts, *kv_parts, *t_parts;
+  float dq_scale, t_scale;
+  float *dq, *dkv, *t;     // [n_q][hd], [2][N][hd], [H][c_z]
+  uint32_t token_blocks;   // set by the launcher
+};
+
+struct BackGemmArgs {
+  int64_t n_tok, q_row0, n_q;
+  int32_t hd, c_s, s_bf16;
+  const void* s;
+  const uint8_t* mask;
+  const float *w_q, *w_k, *w_v, *w_g;
+  const float *dq, *dk, *dv, *dg;
+  int32_t ds_splits, w_splits;
+  float *ds_parts, *w_parts;  // [splits][N][c_s], [splits][4][hd][c_s]; null: not wanted
+  int64_t ds_blocks;          // set by the launcher, with the next
+  int32_t w_vec;
+};
+
+struct BackFinishArgs {
+  int64_t n_tok;
+  int32_t n_heads, hd, c_s, c_z, bf16, ds_splits, w_splits;
+  const float *ds_parts, *w_parts, *t, *w_b, *gamma;
+  void *ds, *dw[4], *dw_b, *dgamma;  // null: not wanted
+};
+
 size_t fast_proj_split_bytes(int32_t c_s);
 bool fast_proj_small(int64_t key_tiles, int64_t query_tiles);  // one kernel, w_split unused
 hipError_t launch_fast_proj(const FastProjArgs& a, hipStream_t st);
@@ -240,6 +332,17 @@ hipError_t launch_topk_merge(const TopkMergeArgs& a, hipStream_t st);
 hipError_t launch_transition(const TransArgs& a, hipStream_t st);
 hipError_t launch_transition_gen(const TransGenArgs& a, hipStream_t st);
 hipError_t launch_scatter_mean(const ScatterArgs& a, hipStream_t st);
+hipError_t launch_layer_norm(const LayerNormArgs& a, bool x_bf16, hipStream_t st);
+int layer_norm_back_groups(int64_t n_rows, int32_t c);  // workgroups, one partial sum each
+hipError_t launch_layer_norm_back(const LayerNormBackArgs& a, bool x_bf16, hipStream_t st);
+hipError_t launch_back_rows(const BackRowsArgs& a, hipStream_t st);
+int back_pairs_groups(int64_t rows, int n_parts);
+hipError_t launch_back_pairs(const BackPairsArgs& a, int groups, hipStream_t st);
+hipError_t launch_back_keys(const BackKeysArgs& a, int dp, hipStream_t st);
+hipError_t launch_back_sum(const BackSumArgs& a, hipStream_t st);
+void back_gemm_splits(int64_t n_tok, int32_t hd, int32_t c_s, int* ds_splits, int* w_splits);
+hipError_t launch_back_gemm(const BackGemmArgs& a, hipStream_t st);
+hipError_t launch_back_finish(const BackFinishArgs& a, hipStream_t st);
 int scatter_order_flags(int64_t n_atoms);  // plan workgroups (one flag each) for n_atoms (<= kScatterFlags)
 
 }  // namespace dcp

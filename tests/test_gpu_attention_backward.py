@@ -1,0 +1,411 @@
+"""The attention layer's backward pass through the C-ABI, from the state that the library's own
+forward saved, against the layer's definition differentiated in 64 bits on the CPU (GPU).
+
+Errors are 2-norms of the difference over 2-norms of the gradient. Tolerances:
+- fp32 (the general path): fp32 arithmetic; a logit of size up to 16 is off by a few 2^-24 times 16,
+  about 4e-6, and its weight relatively by as much; sums of n terms add a few 2^-24 times sqrt(n).
+  2e-5 for every gradient, and half a step more where it is rounded to bf16: 8 significant bits,
+  so values in [1, 2) are 2^-7 apart and a rounding is off by at most 2^-8 of the value, and the norm
+  of all roundings by at most 2^-8 of the norm.
+- bf16 fused path: the saved state is the forward's, whose q, k, v and weights are bf16: a logit of
+  size 1 is off by about 2^-9 sqrt(2), its weight relatively by as much, at most 4e-3, and the mean over
+  the keys, D, by the same; together with the rounding of the result (at most 2^-8) under 1e-2.
+"""
+import math
+
+import numpy as np
+import pytest
+
+pytestmark = pytest.mark.gpu
+
+EPS = 1e-5
+NAMES = ("dz", "ds", "w_q", "w_k", "w_v", "w_g", "w_b", "gamma")
+F32 = dict(dtype="f32", c_s=64, c_z=32, h=4, d=32)
+BF16 = dict(dtype="bf16", c_s=384, c_z=128, h=16, d=24)
+
+
+def make(n, row0, rows, dtype, c_s, c_z, h, d, masked=0, seed=0, gamma=True, dout_scale=2.0 ** -10):
+    """Inputs on the CPU (bf16 activations already rounded)."""
+    import torch
+    g = torch.Generator().manual_seed(seed)
+    dt = torch.bfloat16 if dtype == "bf16" else torch.float32
+    r = lambda *s: torch.randn(s, generator=g)  # noqa: E731
+    x = {k: r(h * d, c_s) * c_s ** -0.5 for k in ("w_q", "w_k", "w_v", "w_g")}
+    x["w_b"] = r(h, c_z) * c_z ** -0.5
+    x["gamma"] = 1 + r(c_z) / 4 if gamma else None
+    x["s"] = r(n, c_s).to(dt)
+    x["z"] = (r(rows, n, c_z) + r(c_z) / 2).to(dt)
+    x["dout"] = (r(rows, h * d) * dout_scale).to(dt)
+    x["mask"] = None
+    if masked:
+        x["mask"] = torch.ones(n, dtype=torch.uint8)
+        x["mask"][torch.randperm(n, generator=g)[:masked]] = 0
+    x["dims"] = (n, row0, rows, dtype, c_s, c_z, h, d)
+    return x
+
+
+def layer(x, w, s, z):
+    """The layer's rows from its definition."""
+    import torch
+    n, row0, rows, _, _, _, h, d = x["dims"]
+    mu = z.mean(dim=2, keepdim=True)
+    zn = (z - mu) / torch.sqrt(((z - mu) ** 2).mean(dim=2, keepdim=True) + EPS)
+    if w["gamma"] is not None:
+        zn = zn * w["gamma"]
+    sq = s[row0:row0 + rows]
+    heads = lambda t: t.reshape(-1, h, d).transpose(0, 1)  # noqa: E731
+    q, k, v = heads(sq @ w["w_q"].T), heads(s @ w["w_k"].T), heads(s @ w["w_v"].T)
+    logits = q @ k.transpose(1, 2) / math.sqrt(d) + (zn @ w["w_b"].T).permute(2, 0, 1)
+    if x["mask"] is not None:
+        logits = logits.masked_fill(x["mask"] == 0, -math.inf)
+    o = torch.softmax(logits, dim=2) @ v
+    return torch.sigmoid(sq @ w["w_g"].T) * o.transpose(0, 1).reshape(rows, h * d)
+
+
+def reference(x):
+    import torch
+    w = {k: None if x[k] is None else x[k].double().requires_grad_() for k in ("w_q", "w_k", "w_v", "w_g", "w_b", "gamma")}
+    s, z = x["s"].double().requires_grad_(), x["z"].double().requires_grad_()
+    gamma = w["gamma"] if w["gamma"] is not None else torch.ones(x["w_b"].shape[1], dtype=torch.float64, requires_grad=True)
+    out = layer(x, {**w, "gamma": gamma}, s, z)
+    return dict(zip(NAMES, torch.autograd.grad(out, [z, s] + [w[k] for k in NAMES[2:7]] + [gamma], x["dout"].double())))
+
+
+class Call:
+    """The inputs on the GPU, the forward's state, and the backward call."""
+
+    def __init__(self, x, grad_dtype=None, out_dtype=None):
+        import torch
+        import paper_2607_05439_amd as dcp
+        self.dcp, self.torch, self.dims = dcp, torch, x["dims"]
+        n, row0, rows, dtype, c_s, c_z, h, d = x["dims"]
+        self.x = {k: v.cuda() if isinstance(v, torch.Tensor) else v for k, v in x.items()}
+        code = dcp.DCP_BF16 if dtype == "bf16" else dcp.DCP_F32
+        self.out_code = code if out_dtype is None else out_dtype
+        self.grad_code = code if grad_dtype is None else grad_dtype
+        self.x["dout"] = self.x["dout"].to(torch.bfloat16 if self.out_code == dcp.DCP_BF16 else torch.float32)
+        self.shape = dcp.make_shape(n, c_s, c_z, h, d, code, self.out_code, EPS)
+        g = self.x
+        self.weights = dcp.make_weights(g["w_q"], g["w_k"], g["w_v"], g["w_g"], g["w_b"], None, g["gamma"], None)
+        f = dict(dtype=torch.float32, device="cuda")
+        self.m, self.l = torch.full((h, rows), 7.0, **f), torch.full((h, rows), 7.0, **f)
+        self.acc = torch.full((rows, h, d), 7.0, **f)
+        ws = torch.empty(max(dcp.dcp_workspace_size(self.shape, rows, 1), 256), dtype=torch.uint8, device="cuda")
+        dcp.dcp_pair_bias_attention_partial(self.shape, self.weights, g["s"], g["z"], g["mask"], row0, rows, 0, n, self.m,
+                                            self.l, self.acc, None, ws, ws.numel())
+
+    def outputs(self):
+        torch, x = self.torch, self.x
+        dt = torch.bfloat16 if self.grad_code == self.dcp.DCP_BF16 else torch.float32
+        new = lambda t, dt: torch.full(t.shape, 7.0, dtype=dt, device="cuda")  # noqa: E731
+        out = {"dz": new(x["z"], x["z"].dtype), "ds": new(x["s"], dt)}
+        out.update({k: new(x[k], dt) for k in NAMES[2:7]})
+        out["gamma"] = torch.full((self.dims[5],), 7.0, dtype=dt, device="cuda")
+        return out
+
+    def workspace(self, fill=255):
+        nbytes = self.dcp.dcp_pair_bias_attention_backward_workspace_size(self.shape, self.dims[2])
+        return self.torch.full((max(nbytes, 256),), fill, dtype=self.torch.uint8, device="cuda")
+
+    def __call__(self, want=NAMES, ws=None, out=None):
+        x, out = self.x, self.outputs() if out is None else out
+        ws = self.workspace() if ws is None else ws
+        grads = self.dcp.make_gradients(*[out[k] if k in want else None for k in NAMES], dtype=self.grad_code)
+        self.dcp.dcp_pair_bias_attention_backward(self.shape, self.weights, x["s"], x["z"], x["mask"], self.dims[1],
+                                                  self.dims[2], self.m, self.l, self.acc, x["dout"], grads, ws, ws.numel())
+        return out
+
+
+def check(got, want, tol, label=""):
+    import torch
+    errs = {}
+    for k in want:
+        a, b = got[k].cpu().double(), want[k]
+        norm = float(b.norm())
+        errs[k] = float((a - b).norm()) / norm if norm > 0 else float(a.norm())
+        assert torch.isfinite(a).all(), k
+    print(label, {k: "%.1e" % v for k, v in errs.items()}, flush=True)
+    assert max(errs.values()) <= tol, errs
+
+
+# ----------------------------------------------------------------------------- against the definition
+GENERAL = [
+    dict(n=1, row0=0, rows=1, **F32), dict(n=2, row0=1, rows=1, **F32),
+    dict(n=65, row0=0, rows=65, **F32), dict(n=64, row0=3, rows=17, masked=5, **F32),
+    dict(n=130, row0=100, rows=30, masked=1, **F32),
+    dict(n=70, row0=0, rows=70, dtype="f32", c_s=128, c_z=128, h=4, d=32, masked=9),
+    dict(n=40, row0=0, rows=40, dtype="f32", c_s=64, c_z=64, h=8, d=16),
+    dict(n=33, row0=0, rows=33, dtype="f32", c_s=37, c_z=19, h=3, d=5),          # nothing a multiple of four
+    dict(n=33, row0=5, rows=9, dtype="f32", c_s=40, c_z=256, h=16, d=8, masked=2),
+    dict(n=29, row0=0, rows=29, dtype="f32", c_s=20, c_z=200, h=2, d=64),
+    dict(n=21, row0=0, rows=21, dtype="f32", c_s=8, c_z=1, h=1, d=1),
+]
+
+
+@pytest.mark.parametrize("case", GENERAL, ids=lambda c: "-".join(str(v) for v in c.values()))
+def test_general_path(case):
+    x = make(**case, seed=case["n"])
+    check(Call(x)(), {k: v for k, v in reference(x).items() if not (case["c_z"] == 1 and k in ("dz", "w_b", "gamma"))},
+          2e-5, str(case))
+
+
+@pytest.mark.parametrize("grad_dtype,out_dtype", [(0, 0), (1, 1), (0, 1), (1, 0)])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_types(dtype, grad_dtype, out_dtype):
+    """Every mix of activation, gradient and dout types on the general path."""
+    x = make(50, 0, 50, dtype, 64, 64, 4, 16, masked=3, seed=11)
+    if out_dtype:
+        x["dout"] = x["dout"].bfloat16()
+    check(Call(x, grad_dtype, out_dtype)(), reference(x), 2e-5 + (2.0 ** -8 if dtype == "bf16" or grad_dtype else 0))
+
+
+FUSED = [
+    dict(n=1, row0=0, rows=1), dict(n=16, row0=0, rows=16), dict(n=17, row0=16, rows=1), dict(n=60, row0=0, rows=60),
+    dict(n=97, row0=20, rows=33, masked=7), dict(n=200, row0=0, rows=200, masked=4),
+]
+
+
+@pytest.mark.parametrize("case", FUSED, ids=lambda c: "-".join(str(v) for v in c.values()))
+def test_fused_shape(case):
+    x = make(**case, **BF16, seed=case["n"])
+    want = reference(x)
+    if case["n"] == 1:  # one key: P = 1 and dS = 0 up to rounding, and so is what comes from it
+        want = {k: v for k, v in want.items() if k in ("ds", "w_v", "w_g")}
+    check(Call(x)(), want, 1e-2, str(case))
+
+
+def test_fused_shape_without_gamma_and_other_widths():
+    for c_s in (32, 416):
+        x = make(50, 0, 50, "bf16", c_s, 128, 16, 24, seed=c_s, gamma=False)
+        check(Call(x, grad_dtype=0)(), reference(x), 1e-2, "c_s %d" % c_s)
+
+
+# ----------------------------------------------------------------------------- masks, extremes
+@pytest.mark.parametrize("widths", [F32, BF16], ids=["f32", "bf16"])
+def test_no_key_attends(widths):
+    """Every key masked: the forward gives 0, and every gradient is 0."""
+    import torch
+    x = make(40, 0, 40, **widths, seed=1)
+    x["mask"] = torch.zeros(40, dtype=torch.uint8)
+    for k, v in Call(x)().items():
+        assert not v.any(), k
+
+
+@pytest.mark.parametrize("widths", [F32, BF16], ids=["f32", "bf16"])
+def test_masked_keys_hold_anything(widths):
+    """NaN and infinities in a masked key's z, and in its s where the key is no query of the
+    stripe: the same gradients, zeros for its dz."""
+    import torch
+    x = make(70, 0, 30, **widths, masked=0, seed=2)
+    x["mask"] = torch.ones(70, dtype=torch.uint8)
+    x["mask"][[40, 41, 69]] = 0
+    want = Call(x)()
+    x["z"][:, 40] = float("nan")
+    x["z"][:, 69, ::2] = float("inf")
+    x["s"][41], x["s"][69, 0] = float("nan"), float("-inf")
+    got = Call(x)()
+    assert all(torch.equal(got[k], want[k]) for k in NAMES)
+    assert not got["dz"][:, [40, 41, 69]].any() and got["dz"][:, 39].any()
+
+
+@pytest.mark.parametrize("widths,tol", [(F32, 2e-5), (BF16, 1e-2)], ids=["f32", "bf16"])
+@pytest.mark.parametrize("scale", [2.0 ** -60, 2.0 ** -20, 2.0 ** 30])
+def test_gradients_of_any_size(widths, tol, scale):
+    """dout of one binade or another: the gradients scale with it."""
+    x = make(50, 0, 50, **widths, seed=3, dout_scale=scale)
+    check(Call(x)(), reference(x), tol, "scale %g" % scale)
+
+
+@pytest.mark.parametrize("widths,tol", [(F32, 2e-5), (BF16, 1e-2)], ids=["f32", "bf16"])
+def test_weights_of_other_sizes(widths, tol):
+    """Projections whose outputs are tiny or large: q small and k large (their product stays), v large."""
+    x = make(50, 0, 50, **widths, seed=4)
+    x["w_q"], x["w_k"], x["w_v"] = x["w_q"] * 2.0 ** -24, x["w_k"] * 2.0 ** 23, x["w_v"] * 2.0 ** 17
+    check(Call(x)(), reference(x), tol)
+
+
+@pytest.mark.parametrize("widths,tol", [(F32, 2e-5), (BF16, 1e-2)], ids=["f32", "bf16"])
+def test_pair_channels_with_a_large_mean(widths, tol):
+    """z + 16: the normalised vectors stay what they were (16 + x is rounded before both sides see it)."""
+    x = make(50, 0, 50, **widths, seed=5)
+    x["z"] = (x["z"].float() + 16.0).to(x["z"].dtype)
+    # in fp32 the mean 16 is off by 2^-24 of 16, sixteen times the error of values of size 1
+    check(Call(x)(), reference(x), 16 * tol if widths is F32 else tol)
+
+
+# ----------------------------------------------------------------------------- calls
+@pytest.mark.parametrize("widths", [F32, BF16], ids=["f32", "bf16"])
+def test_each_gradient_alone_and_any_workspace(widths):
+    """A gradient asked for alone has the same bits, nothing else is written, and what the workspace
+    holds on entry does not matter."""
+    import torch
+    call = Call(make(90, 10, 50, **widths, masked=3, seed=6))
+    want = call()
+    assert all(torch.equal(v, want[k]) for k, v in call(ws=call.workspace(0)).items())
+    for name in NAMES:
+        got = call(want=(name,), ws=call.workspace(127))
+        for k in NAMES:
+            assert torch.equal(got[k], want[k]) if k == name else (got[k] == 7.0).all(), (name, k)
+
+
+@pytest.mark.parametrize("widths,tol", [(F32, 2e-5), (BF16, 1e-2)], ids=["f32", "bf16"])
+def test_stripes_add_up(widths, tol):
+    """dz of stripes of rows is the layer's; the shared gradients of the stripes add up to the layer's."""
+    import torch
+    x = make(75, 0, 75, **widths, masked=2, seed=7)
+    want = reference(x)
+    total = {k: torch.zeros_like(v) for k, v in want.items()}
+    for row0, rows in ((0, 16), (16, 1), (17, 58)):
+        part = {**x, "z": x["z"][row0:row0 + rows].contiguous(), "dout": x["dout"][row0:row0 + rows].contiguous()}
+        part["dims"] = (75, row0, rows) + x["dims"][3:]
+        got = Call(part, grad_dtype=0)()
+        total["dz"][row0:row0 + rows] = got["dz"].cpu().double()
+        for k in NAMES[1:]:
+            total[k] += got[k].cpu().double()
+    check(total, want, tol)
+
+
+@pytest.mark.parametrize("widths", [F32, BF16], ids=["f32", "bf16"])
+def test_a_stripe_without_rows(widths):
+    import torch
+    import paper_2607_05439_amd as dcp
+    call = Call(make(20, 0, 4, **widths, seed=8))
+    out = call.outputs()
+    grads = dcp.make_gradients(None, *[out[k] for k in NAMES[1:]], dtype=call.grad_code)
+    g = call.x
+    dcp.dcp_pair_bias_attention_backward(call.shape, call.weights, g["s"], g["z"], None, 3, 0, call.m, call.l, call.acc,
+                                         g["dout"], grads, None, 0)
+    torch.cuda.synchronize()
+    assert all(not out[k].any() for k in NAMES[1:])
+
+
+@pytest.mark.parametrize("widths", [F32, BF16], ids=["f32", "bf16"])
+def test_twice_the_same_bits_on_two_streams(widths):
+    """Two calls at once with workspaces of their own: the bits of one call alone."""
+    import torch
+    call = Call(make(150, 0, 100, **widths, seed=9))
+    want = call()
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    ws, outs = [call.workspace(), call.workspace()], [call.outputs(), call.outputs()]
+    torch.cuda.synchronize()
+    for i, s in enumerate(streams):
+        with torch.cuda.stream(s):
+            call(ws=ws[i], out=outs[i])
+    torch.cuda.synchronize()
+    for o in outs:
+        assert all(torch.equal(o[k], want[k]) for k in NAMES)
+
+
+@pytest.mark.parametrize("widths", [F32, BF16], ids=["f32", "bf16"])
+def test_captured_and_replayed(widths):
+    """One training step of the layer (LayerNorm of s, the attention's state and output, both backward
+    passes) captured once and replayed on new inputs, with eager calls between the replays."""
+    import torch
+    import paper_2607_05439_amd as dcp
+    call = Call(make(80, 0, 80, **widths, masked=3, seed=10))
+    g, (n, _, rows, _, c_s, _, h, d) = call.x, call.dims
+    code = call.grad_code
+    raw, sgamma, sbeta = g["s"].clone(), torch.rand(c_s, device="cuda") + 0.5, torch.rand(c_s, device="cuda")
+    out, ws = call.outputs(), call.workspace()
+    fws = torch.empty(max(dcp.dcp_workspace_size(call.shape, rows, 1), 256), dtype=torch.uint8, device="cuda")
+    lws = torch.empty(dcp.dcp_layer_norm_backward_workspace_size(n, c_s), dtype=torch.uint8, device="cuda")
+    gate, y = torch.empty((rows, h * d), device="cuda"), torch.empty_like(g["dout"])
+    draw, dgamma, dbeta = torch.empty_like(raw), torch.empty(c_s, device="cuda"), torch.empty(c_s, device="cuda")
+
+    def step():
+        dcp.dcp_layer_norm(n, c_s, code, code, EPS, raw, sgamma, sbeta, g["s"])
+        dcp.dcp_pair_bias_attention_partial(call.shape, call.weights, g["s"], g["z"], g["mask"], 0, rows, 0, n, call.m,
+                                            call.l, call.acc, gate, fws, fws.numel())
+        dcp.dcp_block_merge(1, rows, h, d, call.m, call.l, call.acc, None, None, None, gate, y, code)
+        call(ws=ws, out=out)
+        dcp.dcp_layer_norm_backward(n, c_s, code, code, EPS, raw, sgamma, out["ds"], draw, dgamma, dbeta, lws, lws.numel())
+
+    results = lambda: [t.clone() for t in (*out.values(), y, draw, dgamma, dbeta)]  # noqa: E731
+    step()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step()
+    for k in range(3):
+        gen = torch.Generator("cuda").manual_seed(k)
+        raw.copy_(torch.randn(raw.shape, device="cuda", generator=gen))
+        g["z"].copy_(torch.randn(g["z"].shape, device="cuda", generator=gen))
+        graph.replay()
+        torch.cuda.synchronize()
+        got = results()
+        step()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(got, results()))
+
+
+def test_a_training_step_against_the_definition():
+    """LayerNorm of s, the layer, its backward pass and LayerNorm's: the gradients of the raw single
+    track and of LayerNorm's weights, all from the library's own forward."""
+    import torch
+    import paper_2607_05439_amd as dcp
+    x = make(60, 0, 60, **F32, masked=2, seed=12)
+    gen = torch.Generator().manual_seed(13)
+    raw, sgamma, sbeta = torch.randn((60, 64), generator=gen), torch.rand(64, generator=gen) + 0.5, torch.rand(64, generator=gen)
+    r, sg, sb = (t.double().requires_grad_() for t in (raw, sgamma, sbeta))
+    mu = r.mean(dim=1, keepdim=True)
+    s = sg * (r - mu) / torch.sqrt(((r - mu) ** 2).mean(dim=1, keepdim=True) + EPS) + sb
+    w = {k: x[k].double() for k in ("w_q", "w_k", "w_v", "w_g", "w_b", "gamma")}
+    want = torch.autograd.grad(layer(x, w, s, x["z"].double()), [r, sg, sb], x["dout"].double())
+    sd = torch.empty((60, 64), device="cuda")
+    dcp.dcp_layer_norm(60, 64, 0, 0, EPS, raw.cuda(), sgamma.cuda(), sbeta.cuda(), sd)
+    x["s"] = sd.cpu()
+    ds = Call(x)()["ds"]
+    dr, dg, db = torch.empty_like(sd), torch.empty(64, device="cuda"), torch.empty(64, device="cuda")
+    ws = torch.empty(dcp.dcp_layer_norm_backward_workspace_size(60, 64), dtype=torch.uint8, device="cuda")
+    dcp.dcp_layer_norm_backward(60, 64, 0, 0, EPS, raw.cuda(), sgamma.cuda(), ds, dr, dg, db, ws, ws.numel())
+    check({"r": dr, "g": dg, "b": db}, dict(zip("rgb", want)), 2e-5)
+
+
+def test_ring_state():
+    """The state merged from the partial states of key ranges gives the gradients of the whole one's."""
+    import torch
+    import paper_2607_05439_amd as dcp
+    x = make(90, 0, 90, **F32, masked=4, seed=14)
+    call = Call(x)
+    g, f = call.x, dict(dtype=torch.float32, device="cuda")
+    m, l, acc = torch.empty((3, 4, 90), **f), torch.empty((3, 4, 90), **f), torch.empty((3, 90, 4, 32), **f)
+    ws = torch.empty(dcp.dcp_workspace_size(call.shape, 90, 1), dtype=torch.uint8, device="cuda")
+    for i, (k0, k1) in enumerate(((0, 31), (31, 32), (32, 90))):
+        dcp.dcp_pair_bias_attention_partial(call.shape, call.weights, g["s"], g["z"], g["mask"], 0, 90, k0, k1, m[i], l[i],
+                                            acc[i], None, ws, ws.numel())
+    dcp.dcp_block_merge(3, 90, 4, 32, m, l, acc, call.m, call.l, call.acc, None, None, 0)
+    check(call(), reference(x), 2e-5)
+
+
+@pytest.mark.parametrize("widths,tol", [(F32, 2e-5), (BF16, 1e-2)], ids=["f32", "bf16"])
+def test_peaked_softmax(widths, tol):
+    """Logits of size 20: nearly all weight on one key of a row. dS cancels to the size of the rest's
+    weight, so that on the fused path, whose saved sums hold bf16 values, only the gradients that do not
+    pass through dS are checked to the path's tolerance, and the others for being finite."""
+    import torch
+    x = make(50, 0, 50, **widths, seed=15)
+    x["w_q"] = x["w_q"] * 8.0
+    got, want = Call(x)(), reference(x)
+    if widths is BF16:
+        assert all(torch.isfinite(v).all() for v in got.values())
+        check(got, {k: want[k] for k in ("w_g",)}, 2 * tol)
+    else:
+        # a logit of 60 is off by 2^-24 of it times a few: four times the tolerance of logits of 16
+        check(got, want, 4 * tol)
+
+
+def test_gradient_against_differences():
+    """dz and ds along random directions against the change of the loss."""
+    import torch
+    x = make(30, 0, 30, **F32, masked=1, seed=16)
+    got = Call(x)()
+    w = {k: x[k].double() for k in ("w_q", "w_k", "w_v", "w_g", "w_b", "gamma")}
+    gen = torch.Generator().manual_seed(17)
+    for name, key in (("dz", "z"), ("ds", "s")):
+        v, h = torch.randn(x[key].shape, generator=gen).double(), 1e-4
+        loss = lambda t: float((layer(x, w, *((x["s"].double(), t) if key == "z" else (t, x["z"].double())))  # noqa: E731
+                                * x["dout"].double()).sum())
+        slope = (loss(x[key].double() + h * v) - loss(x[key].double() - h * v)) / (2 * h)
+        grad = got[name].cpu().double()
+        assert abs(float((grad * v).sum()) - slope) <= 1e-4 * float((grad.abs() * v.abs()).sum())
