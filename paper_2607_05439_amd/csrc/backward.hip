@@ -119,7 +119,7 @@ __global__ void __launch_bounds__(256) back_pairs_kernel(BackPairsArgs a) {
   float t_sum[HP];
 #pragma unroll
   for (int h = 0; h < HP; ++h) t_sum[h] = 0.0f;
-  const int dq_groups = max(256 / hd, 1), dq_x = tid % hd, dq_g = tid / hd;
+  const int dq_groups = 256 / hd, dq_x = tid % hd, dq_g = tid / hd;  // hd <= 128
   const int64_t items = a.rows * a.n_parts;
   const int64_t tiles = (a.n_tok + kBackKeys - 1) / kBackKeys;
 
@@ -139,7 +139,7 @@ __global__ void __launch_bounds__(256) back_pairs_kernel(BackPairsArgs a) {
 #pragma unroll
     for (int i = 0; i < NH; ++i)
       stat[i] = *reinterpret_cast<const f32x4*>(a.stat + 4 * ((int64_t)min(4 * i + qd, H - 1) * a.n_q + row));
-    float dq = 0.0f, dq2 = 0.0f;
+    float dq = 0.0f;
     __syncthreads();
     for (int64_t t = t_first; t < t_first + t_count; ++t) {
       const int64_t j = t * kBackKeys + key;
@@ -274,10 +274,7 @@ __global__ void __launch_bounds__(256) back_pairs_kernel(BackPairsArgs a) {
         const int h = dq_x / d;
         for (int x = dq_g; x < kBackKeys; x += dq_groups) {
           const int64_t kj = t * kBackKeys + x;
-          if (kj < a.n_tok && (!a.mask || a.mask[kj] != 0)) {
-            dq = fmaf(s_ds[x * (HP + 4) + h], a.k[kj * hd + dq_x], dq);
-            if (tid + 256 < hd) dq2 = fmaf(s_ds[x * (HP + 4) + (tid + 256) / d], a.k[kj * hd + tid + 256], dq2);
-          }
+          if (kj < a.n_tok && (!a.mask || a.mask[kj] != 0)) dq = fmaf(s_ds[x * (HP + 4) + h], a.k[kj * hd + dq_x], dq);
         }
       }
       __syncthreads();
@@ -287,7 +284,6 @@ __global__ void __launch_bounds__(256) back_pairs_kernel(BackPairsArgs a) {
     if (tid < hd) {
       for (int g = 1; g < dq_groups; ++g) dq += s_dq[tid + g * hd];
       a.dq_parts[((int64_t)part * a.n_q + row) * hd + tid] = dq * scale;
-      if (tid + 256 < hd) a.dq_parts[((int64_t)part * a.n_q + row) * hd + tid + 256] = dq2 * scale;
     }
   }
   // T of this workgroup: its key groups in order, added to what earlier chunks left
@@ -369,7 +365,7 @@ __global__ void __launch_bounds__(256) back_sum_kernel(BackSumArgs a) {
     if (x < n_dq) {
       float v = 0.0f;
       for (int p = 0; p < a.dq_n; ++p) v += a.dq_parts[p * n_dq + x];
-      a.dq[x] = v * a.dq_scale;
+      a.dq[x] = v;
     } else if (x < n_dq + n_kv) {
       float v = 0.0f;
       for (int p = 0; p < a.kv_n; ++p) v += a.kv_parts[p * n_kv + x - n_dq];
@@ -386,7 +382,7 @@ __global__ void __launch_bounds__(256) back_sum_kernel(BackSumArgs a) {
   if (grp > 0 || col >= cols) return;
 #pragma unroll
   for (int i = 1; i < 16; ++i) v += s[i][threadIdx.x];
-  a.t[col] = v * a.t_scale;
+  a.t[col] = v;
 }
 
 // ----------------------------------------------------------------------------- token products

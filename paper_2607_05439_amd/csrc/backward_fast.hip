@@ -1,0 +1,563 @@
+// Backward pass of the attention on the matrix cores: c_z = 128, H = 16, d = 24, bf16
+// activations (gfx950). The formulas are in backward.hip.
+//
+// Kernels, in order:
+//   prep_kernel   the bias weights as operands; the largest |dout|
+//   (the fp32 projections of the general path, which also leave the largest |q|, |k|, |v|)
+//   pack_kernel   q, do of the rows and k, v of the keys as fp16 operands; the row statistics
+//   pairs_kernel  16 query rows and a range of keys per workgroup: bias, P, dS, dz, dq, T
+//   keys_kernel   64 keys of a head per wave: dk, dv from the stored P and dS
+// then the token products of backward.hip.
+//
+// Operands are fp16, not bf16: 11 significant bits where bf16 has 8, at the same rate, so
+// that the roundings inside stay an eighth of the result's own rounding to bf16. Their
+// range is served by powers of two: every tensor is scaled so that its largest
+// magnitude lies in [2^11, 2^12) (P, at most 1, by 2^14; dS then by what keeps it below
+// 2^16), fp16 holds 11 bits down to 2^-26 of that, and the fp32 results are scaled
+// back exactly. Only z enters as the bf16 it is, against bias weights split into
+// bf16 hi + lo (pair_bias.h).
+#include <hip/hip_runtime.h>
+#include <math.h>
+#include <stdint.h>
+
+#include "cdna4.h"
+#include "dcp_internal.h"
+#include "pair_bias.h"
+
+namespace dcp {
+namespace {
+
+constexpr int kCz = kFastCz, kH = kFastH, kD = kFastD, kDp = kFastDp, kHD = kFastH * kFastD;
+constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
+constexpr float kInvSqrtD = 0.20412414523193150818f;  // 1 / sqrt(24)
+constexpr int kPShift = 14;       // P is stored times 2^14
+constexpr int kTop = 11;          // operands have their largest magnitude in [2^11, 2^12)
+constexpr int kDsShift = 14;      // dS = P (dP' - D') 2^-14: |dP' - D'| <= 2 * 24 * 2^24
+
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+typedef _Float16 f16x4 __attribute__((ext_vector_type(4)));
+
+__device__ __forceinline__ f32x4 mfma32h(f16x8 a, f16x8 b, f32x4 c) {
+  return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0);
+}
+__device__ __forceinline__ f32x4 mfma16h(f16x4 a, f16x4 b, f32x4 c) {
+  return __builtin_amdgcn_mfma_f32_16x16x16f16(a, b, c, 0, 0, 0);
+}
+__device__ __forceinline__ f16x8 as_f16x8(u32x4 u) { return __builtin_bit_cast(f16x8, u); }
+__device__ __forceinline__ f16x4 to_f16(f32x4 v) {
+  f16x4 r;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) r[i] = (_Float16)v[i];
+  return r;
+}
+
+// The power of two that takes a largest magnitude into [2^kTop, 2^(kTop + 1)): 1 where
+// there is none (all zero) or it is not finite.
+__device__ __forceinline__ int scale_exp(float top) {
+  if (!(top > 0.0f) || top == INFINITY) return 0;
+  int e;
+  (void)frexpf(top, &e);  // top = f 2^e, f in [0.5, 1)
+  return max(-100, min(100, kTop + 1 - e));
+}
+
+// ----------------------------------------------------------------------------- weights, dout
+// Block 0: the weights. Blocks 1 .. kBackTops: the largest |dout| of a share each.
+__global__ void __launch_bounds__(256) prep_kernel(FastBackArgs a) {
+  const int tid = threadIdx.x, lane = tid & 63;
+  __shared__ float s_top[4];
+  if (blockIdx.x > 0) {
+    const int64_t n8 = a.n_q * kHD / 8;  // 16-byte pieces of bf16, pairs of them of fp32
+    float top = 0.0f;
+    for (int64_t x = (int64_t)(blockIdx.x - 1) * 256 + tid; x < n8; x += (int64_t)kBackTops * 256) {
+      if (a.dout_bf16) {
+        const u32x4 r = reinterpret_cast<const u32x4*>(a.dout)[x];
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          top = fmaxf(top, fmaxf(fabsf(__uint_as_float(r[i] << 16)), fabsf(__uint_as_float(r[i] & 0xFFFF0000u))));
+      } else {
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+          const f32x4 r = reinterpret_cast<const f32x4*>(a.dout)[2 * x + j];
+          top = fmaxf(top, fmaxf(fmaxf(fabsf(r[0]), fabsf(r[1])), fmaxf(fabsf(r[2]), fabsf(r[3]))));
+        }
+      }
+    }
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor(top, o));
+    if (lane == 0) s_top[tid >> 6] = top;
+    __syncthreads();
+    if (tid == 0) a.tops[3 + blockIdx.x - 1] = __float_as_uint(fmaxf(fmaxf(s_top[0], s_top[1]), fmaxf(s_top[2], s_top[3])));
+    return;
+  }
+  if (tid < 3) a.tops[tid] = 0u;  // |q|, |k|, |v|: the projection's maxima go here
+  if (tid >= 64) return;
+  const int n = lane & 15, g = lane >> 4;
+  bf16x8 hi[4], lo[4];
+  bias_weights(a.w_b, a.gamma, kLog2e, lane, hi, lo);
+#pragma unroll
+  for (int s = 0; s < 4; ++s) {
+    a.w_ops[64 * s + lane] = __builtin_bit_cast(u32x4, hi[s]);
+    a.w_ops[64 * (4 + s) + lane] = __builtin_bit_cast(u32x4, lo[s]);
+  }
+  // W'' = W' - mean, natural units, as the A operand of dz: tile m = 2 s + half, row r =
+  // channel 32 s + 8 (r / 4) + 4 half + r % 4, k-slots = heads 4g..4g+3
+  float mean[4], top = 0.0f;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    float sum = 0.0f;
+    for (int c = n; c < kCz; c += 16) sum += a.w_b[(4 * g + i) * kCz + c] * (a.gamma ? a.gamma[c] : 1.0f);
+#pragma unroll
+    for (int o = 8; o > 0; o >>= 1) sum += __shfl_xor(sum, o);
+    mean[i] = sum * (1.0f / kCz);
+    for (int c = n; c < kCz; c += 16)
+      top = fmaxf(top, fabsf(a.w_b[(4 * g + i) * kCz + c] * (a.gamma ? a.gamma[c] : 1.0f) - mean[i]));
+  }
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor(top, o));
+  const int ew = scale_exp(top);
+  for (int m = 0; m < 8; ++m) {
+    const int c = 32 * (m >> 1) + 8 * (n >> 2) + 4 * (m & 1) + (n & 3);
+    f16x4 w;
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      w[i] = (_Float16)ldexpf(a.w_b[(4 * g + i) * kCz + c] * (a.gamma ? a.gamma[c] : 1.0f) - mean[i], ew);
+    reinterpret_cast<u32x2*>(a.w_ops + 512)[64 * m + lane] = __builtin_bit_cast(u32x2, w);
+  }
+  if (lane == 0) a.exps[4] = ew;
+}
+
+// ----------------------------------------------------------------------------- operands
+// A workgroup takes 16 tokens, a thread one of them and one head: first the tiles of the
+// stripe's rows, then those of the keys. [H][tokens][32] operands hold a head's channels
+// and 8 zeros; transposed ones, [H][tile][64 lanes][2][4], hold in lane (n, g) and slot
+// (u, i) channel 16 u + n of token 4g + i.
+__device__ __forceinline__ void pack_one(const float (&x)[kD], int e2, int h, int64_t tok, int64_t padded, uint16_t* rows,
+                                         uint16_t* transposed) {
+  f16x8 v[4];
+#pragma unroll
+  for (int e = 0; e < kDp; ++e) v[e >> 3][e & 7] = (_Float16)(e < kD ? ldexpf(x[e < kD ? e : 0], e2) : 0.0f);
+  u32x4* to = reinterpret_cast<u32x4*>(rows + ((int64_t)h * padded + tok) * kDp);
+#pragma unroll
+  for (int j = 0; j < 4; ++j) to[j] = __builtin_bit_cast(u32x4, v[j]);
+  if (!transposed) return;
+  const int t = (int)(tok & 15), g = t >> 2, i = t & 3;
+  _Float16* tt = reinterpret_cast<_Float16*>(transposed) + ((int64_t)h * (padded >> 4) + (tok >> 4)) * 512;
+#pragma unroll
+  for (int e = 0; e < kDp; ++e) tt[(16 * g + (e & 15)) * 8 + (e >> 4) * 4 + i] = v[e >> 3][e & 7];
+}
+
+__global__ void __launch_bounds__(256) pack_kernel(FastBackArgs a) {
+  __shared__ int s_exp[4];
+  const int tid = threadIdx.x, h = tid >> 4;
+  if (tid < 64) {
+    float top = __uint_as_float(a.tops[3 + tid]);
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor(top, o));
+    if (tid == 0) {
+      s_exp[0] = scale_exp(__uint_as_float(a.tops[0]) * (kLog2e * kInvSqrtD));
+      s_exp[1] = scale_exp(__uint_as_float(a.tops[1]));
+      s_exp[2] = scale_exp(__uint_as_float(a.tops[2]));
+      s_exp[3] = scale_exp(top);  // |do| <= |dout|
+      if (blockIdx.x == 0)
+        for (int i = 0; i < 4; ++i) a.exps[i] = s_exp[i];
+    }
+  }
+  __syncthreads();
+  const int eq = s_exp[0], ek = s_exp[1], ev = s_exp[2], ed = s_exp[3];
+  float x[kD], y[kD];
+  if (blockIdx.x < a.nq_pad / 16) {
+    const int64_t row = (int64_t)blockIdx.x * 16 + (tid & 15), at = row * kHD + h * kD;
+    const bool there = row < a.n_q;
+    float dot = 0.0f, lse = INFINITY;
+#pragma unroll
+    for (int e = 0; e < kD; ++e) x[e] = y[e] = 0.0f;
+    if (there) {
+      const float l = a.l[(int64_t)h * a.n_q + row], m = a.m[(int64_t)h * a.n_q + row];
+      const float inv_l = l == 0.0f ? 0.0f : 1.0f / l;
+      if (l != 0.0f) lse = fmaf(m, kLog2e, log2f(l));
+#pragma unroll
+      for (int e = 0; e < kD; e += 4) {
+        const f32x4 q = *reinterpret_cast<const f32x4*>(a.q + at + e), gt = *reinterpret_cast<const f32x4*>(a.g + at + e);
+        const f32x4 ac = *reinterpret_cast<const f32x4*>(a.acc + at + e);
+        f32x4 up;
+        if (a.dout_bf16) {
+          const u32x2 r = *reinterpret_cast<const u32x2*>(static_cast<const uint16_t*>(a.dout) + at + e);
+          up = f32x4{__uint_as_float(r[0] << 16), __uint_as_float(r[0] & 0xFFFF0000u), __uint_as_float(r[1] << 16),
+                     __uint_as_float(r[1] & 0xFFFF0000u)};
+        } else {
+          up = *reinterpret_cast<const f32x4*>(static_cast<const float*>(a.dout) + at + e);
+        }
+        f32x4 dg;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const float o = l == 0.0f ? 0.0f : ac[i] * inv_l, d = gt[i] * up[i];
+          x[e + i] = q[i] * (kLog2e * kInvSqrtD);
+          y[e + i] = d;
+          dot = fmaf(d, o, dot);
+          dg[i] = up[i] * o * gt[i] * (1.0f - gt[i]);
+        }
+        *reinterpret_cast<f32x4*>(a.dg + at + e) = dg;
+      }
+    }
+    pack_one(x, eq, h, row, a.nq_pad, a.qf, a.qt);
+    pack_one(y, ed, h, row, a.nq_pad, a.of, a.ot);
+    a.lse[(int64_t)h * a.nq_pad + row] = lse;
+    a.dot[(int64_t)h * a.nq_pad + row] = ldexpf(dot, ev + ed);
+  } else {
+    const int64_t tile = (int64_t)blockIdx.x - a.nq_pad / 16, key = tile * 16 + (tid & 15), at = key * kHD + h * kD;
+    const bool valid = key < a.n_tok && (!a.mask || a.mask[key] != 0);
+#pragma unroll
+    for (int e = 0; e < kD; e += 4) {
+      const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
+      const f32x4 k = valid ? *reinterpret_cast<const f32x4*>(a.k + at + e) : zero;
+      const f32x4 v = valid ? *reinterpret_cast<const f32x4*>(a.v + at + e) : zero;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) x[e + i] = k[i], y[e + i] = v[i];
+    }
+    pack_one(x, ek, h, key, a.n_pad, a.kf, a.kt);
+    pack_one(y, ev, h, key, a.n_pad, a.vf, nullptr);
+    if (tid < 64) {
+      const uint32_t bits = (uint32_t)(__ballot(valid) & 0xFFFFull);
+      if (tid == 0) a.tile_valid[tile] = bits;
+    }
+  }
+}
+
+// ----------------------------------------------------------------------------- pairs
+// A workgroup of four waves takes 16 query rows and a range of 16-key tiles. Per tile:
+//   1. the waves split the keys: LayerNorm statistics and bias of all heads
+//      (pair_bias), z staying in the registers; the bias goes through LDS
+//      [head][row][key];
+//   2. the waves split the heads: S = K Q^T, P = exp2(S + bias - lse), dP = V dO^T,
+//      dS = P (dP - D), dq += K^T dS; P and dS, transposed on the matrix cores
+//      (the accumulator's registers as the A operand of a product with the identity:
+//      exact), go to memory as the operands of the keys kernel, and dS to LDS
+//      [key][row][head];
+//   3. the waves split the keys again: dzh = W''^T dS, dz = rstd (dzh - zh t) with
+//      t = sum_h dS_h b_h / c_z (the mean of dzh zh; W'' is centred, so dzh has no mean),
+//      and T += dS^T zh over the rows. dz leaves through LDS, four whole rows of 256
+//      bytes to a store. A key's registers are refilled with the next tile's z as soon
+//      as its dz is formed.
+struct PairLds {
+  f32x4 bias[kH][kTileQ][4];           // 16 KB: [head][row][4 keys, chunk ^ row / 4]
+  u32x2 ds[kTileK][kTileQ][4];         // 8 KB: [key][row][4 heads]
+  float t[4][kTileK][kTileQ];          // 4 KB: each wave's heads' share of sum dS b
+  u32x4 out[4][kTileQ][16];            // 16 KB: a key's dz per wave, 16-byte chunk ^ row
+  u32x4 w[8][64];                      // 8 KB: bias weights, hi then lo
+  u32x2 wt[8][64];                     // 4 KB: W'' for dz
+  float stat[kH][kTileQ][2];           // 2 KB: log-sum-exp and D of the rows
+};
+
+__global__ void __launch_bounds__(256, 2) pairs_kernel(FastBackArgs a) {
+  __shared__ PairLds s;
+  const int tid = threadIdx.x, lane = tid & 63, n = lane & 15, g = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int part = blockIdx.y;
+  const int64_t r0 = (int64_t)blockIdx.x * kTileQ, q0 = a.row0 + r0;  // within the chunk, within the stripe
+  int64_t t_count, t_begin;
+  chunk_of(a.n_pad / 16, a.n_parts, part, &t_count, &t_begin);
+  const int64_t t_end = t_begin + t_count;
+  constexpr int kHw = kH / 4;
+
+  for (int x = tid; x < 512; x += 256) {
+    (&s.w[0][0])[x] = a.w_ops[x];
+    (&s.wt[0][0])[x] = reinterpret_cast<const u32x2*>(a.w_ops + 512)[x];
+  }
+  const int eq = a.exps[0], ek = a.exps[1], ev = a.exps[2], ed = a.exps[3], ew = a.exps[4];
+  const float s_scale = ldexpf(1.0f, -eq - ek);
+  const int ds_exp = ev + ed - kDsShift;          // the stored dS is dS 2^ds_exp
+  const float t_scale = ldexpf(kLn2 / kCz, ew);   // sum dS b (base 2) -> t, in dzh's units
+  f16x4 id;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) id[i] = (_Float16)(4 * g + i == n ? 1.0f : 0.0f);
+
+  const int64_t rows_here = min((int64_t)kTileQ, a.n_q - q0);
+  const int row_bytes = (int)(a.n_tok * (kCz * 2));
+  const __amdgpu_buffer_rsrc_t zres = __builtin_amdgcn_make_buffer_rsrc(
+      const_cast<uint16_t*>(a.z) + q0 * a.n_tok * kCz, 0, (int)(rows_here * row_bytes), kRawBufferFlags);
+  const __amdgpu_buffer_rsrc_t dzres = __builtin_amdgcn_make_buffer_rsrc(
+      a.dz ? a.dz + q0 * a.n_tok * kCz : nullptr, 0, a.dz ? (int)(rows_here * row_bytes) : 0, kRawBufferFlags);
+  const int zoff = n * row_bytes + 16 * g;
+  auto load_z = [&](int64_t t, uint32_t bits, int kk, u32x4 (&z)[4]) {
+    const int k = 4 * wave + kk;
+    const int at = (bits >> k) & 1u ? zoff + (int)(t * 16 + k) * (kCz * 2) : kOutOfRange;
+#pragma unroll
+    for (int x = 0; x < 4; ++x) z[x] = __builtin_amdgcn_raw_buffer_load_b128(zres, at + 64 * x, 0, 2);
+  };
+  const __amdgpu_buffer_rsrc_t kres = __builtin_amdgcn_make_buffer_rsrc(a.kf, 0, (int)(kH * a.n_pad * kDp * 2), kRawBufferFlags);
+  const __amdgpu_buffer_rsrc_t vres = __builtin_amdgcn_make_buffer_rsrc(a.vf, 0, (int)(kH * a.n_pad * kDp * 2), kRawBufferFlags);
+  const __amdgpu_buffer_rsrc_t ktres = __builtin_amdgcn_make_buffer_rsrc(a.kt, 0, (int)(kH * a.n_pad * kDp * 2), kRawBufferFlags);
+  const __amdgpu_buffer_rsrc_t qres =
+      __builtin_amdgcn_make_buffer_rsrc(a.qf + q0 * kDp, 0, (int)(kH * a.nq_pad * kDp * 2 - q0 * kDp * 2), kRawBufferFlags);
+  const __amdgpu_buffer_rsrc_t ores =
+      __builtin_amdgcn_make_buffer_rsrc(a.of + q0 * kDp, 0, (int)(kH * a.nq_pad * kDp * 2 - q0 * kDp * 2), kRawBufferFlags);
+  const int n_tiles = (int)(a.n_pad / 16);
+
+  {
+    const int64_t at = (int64_t)(tid >> 4) * a.nq_pad + q0 + n;
+    s.stat[tid >> 4][n][0] = a.lse[at];
+    s.stat[tid >> 4][n][1] = a.dot[at];
+  }
+  f32x4 dq[kHw][2], T[8];
+  const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+  for (int j = 0; j < kHw; ++j) dq[j][0] = dq[j][1] = zero;
+#pragma unroll
+  for (int m = 0; m < 8; ++m) T[m] = zero;
+  const bool row_there = n < rows_here;
+  __syncthreads();
+  f32x4 wsum;
+  {
+    bf16x8 whi[4], wlo[4];
+#pragma unroll
+    for (int x = 0; x < 4; ++x) {
+      whi[x] = as_bf16x8(s.w[x][lane]);
+      wlo[x] = as_bf16x8(s.w[4 + x][lane]);
+    }
+    wsum = bias_weight_sums(whi, wlo);
+  }
+
+  u32x4 z[4][4];
+  uint32_t bits = t_begin < t_end ? a.tile_valid[t_begin] : 0u;
+#pragma unroll
+  for (int kk = 0; kk < 4; ++kk) load_z(t_begin, bits, kk, z[kk]);
+
+  for (int64_t t = t_begin; t < t_end; ++t) {
+    const uint32_t bits_next = t + 1 < t_end ? a.tile_valid[t + 1] : 0u;
+    float mu[4], rstd[4];
+    {
+      f32x4 b[4];
+#pragma unroll
+      for (int kk = 0; kk < 4; ++kk) {
+        // the weights again for each key: held over all four they would not fit the registers
+        asm volatile("" ::: "memory");
+        bf16x8 whi[4], wlo[4];
+#pragma unroll
+        for (int x = 0; x < 4; ++x) {
+          whi[x] = as_bf16x8(s.w[x][lane]);
+          wlo[x] = as_bf16x8(s.w[4 + x][lane]);
+        }
+        f32x4 acc;
+        pair_bias(z[kk], whi, wlo, wsum, a.eps, n, acc, rstd[kk], mu[kk]);
+        const bool valid = (bits >> (4 * wave + kk)) & 1u;
+        if (!valid || !row_there) rstd[kk] = mu[kk] = 0.0f;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) b[i][kk] = valid ? acc[i] * rstd[kk] : -INFINITY;
+      }
+#pragma unroll
+      for (int i = 0; i < 4; ++i) s.bias[4 * g + i][n][wave ^ (n >> 2)] = b[i];
+    }
+    barrier_lds();
+
+    f16x4 dsh[kHw];
+    f32x4 tp = zero;
+#pragma unroll
+    for (int j = 0; j < kHw; ++j) {
+      const int h = kHw * wave + j, so = (h * n_tiles + (int)t) * 1024;
+      const f16x8 k = as_f16x8(__builtin_amdgcn_raw_buffer_load_b128(kres, 64 * n + 16 * g, so, 0));
+      const f16x8 v = as_f16x8(__builtin_amdgcn_raw_buffer_load_b128(vres, 64 * n + 16 * g, so, 0));
+      // the rows' operands again for each tile (from L2): they do not fit the registers
+      const f16x8 q = as_f16x8(__builtin_amdgcn_raw_buffer_load_b128(qres, 64 * n + 16 * g, h * (int)(a.nq_pad * kDp * 2), 0));
+      const f16x8 o = as_f16x8(__builtin_amdgcn_raw_buffer_load_b128(ores, 64 * n + 16 * g, h * (int)(a.nq_pad * kDp * 2), 0));
+      const u32x4 kt = __builtin_amdgcn_raw_buffer_load_b128(ktres, 16 * lane, so, 0);
+      const f32x4 bias = s.bias[h][n][g ^ (n >> 2)];
+      const float lse = s.stat[h][n][0], dot = s.stat[h][n][1];
+      const f32x4 x = mfma32h(k, q, zero), dp = mfma32h(v, o, zero);
+      f32x4 p, ds;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        p[i] = __builtin_amdgcn_exp2f(fmaf(x[i], s_scale, bias[i] - lse));
+        ds[i] = p[i] * (dp[i] - dot) * (1.0f / (1 << kDsShift));
+        p[i] *= (float)(1 << kPShift);
+        tp[i] = fmaf(ds[i], p[i] == 0.0f ? 0.0f : bias[i], tp[i]);
+      }
+      const f16x4 p16 = to_f16(p), ds16 = to_f16(ds);
+      dsh[j] = ds16;
+      const u32x2 kt0 = {kt[0], kt[1]}, kt1 = {kt[2], kt[3]};
+      dq[j][0] = mfma16h(__builtin_bit_cast(f16x4, kt0), ds16, dq[j][0]);
+      dq[j][1] = mfma16h(__builtin_bit_cast(f16x4, kt1), ds16, dq[j][1]);
+      const u32x2 pt = __builtin_bit_cast(u32x2, to_f16(mfma16h(p16, id, zero)));
+      const u32x2 dt = __builtin_bit_cast(u32x2, to_f16(mfma16h(ds16, id, zero)));
+      a.pd[(((int64_t)h * (a.chunk_pad >> 4) + (r0 >> 4)) * n_tiles + t) * 64 + lane] = u32x4{pt[0], pt[1], dt[0], dt[1]};
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      f16x4 v;
+#pragma unroll
+      for (int j = 0; j < kHw; ++j) v[j] = dsh[j][i];
+      s.ds[4 * g + i][n][wave] = __builtin_bit_cast(u32x2, v);
+      s.t[wave][4 * g + i][n] = tp[i];
+    }
+    barrier_lds();
+
+#pragma unroll
+    for (int kk = 0; kk < 4; ++kk) {
+      const int k = 4 * wave + kk;
+      const bool valid = (bits >> k) & 1u;
+      const f16x4 d8 = __builtin_bit_cast(f16x4, s.ds[k][n][g]);
+      const float tt = ((s.t[0][k][n] + s.t[1][k][n]) + (s.t[2][k][n] + s.t[3][k][n])) * t_scale;
+      const f16x4 dst = to_f16(mfma16h(d8, id, zero));
+      const float shift = -mu[kk] * rstd[kk], out_scale = ldexpf(rstd[kk], -ds_exp - ew);
+#pragma unroll
+      for (int x = 0; x < 4; ++x) {
+        bf16x8 r;
+#pragma unroll
+        for (int half = 0; half < 2; ++half) {
+          f32x4 zh;
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const uint32_t w = z[kk][x][2 * half + (i >> 1)];
+            zh[i] = fmaf(__uint_as_float(i & 1 ? w & 0xFFFF0000u : w << 16), rstd[kk], shift);
+          }
+          const f32x4 acc = mfma16h(__builtin_bit_cast(f16x4, s.wt[2 * x + half][lane]), d8, zero);
+          const f16x4 zt = to_f16(mfma16h(to_f16(zh), id, zero));
+          T[2 * x + half] = mfma16h(dst, zt, T[2 * x + half]);
+#pragma unroll
+          for (int i = 0; i < 4; ++i) r[4 * half + i] = (__bf16)(out_scale * fmaf(-zh[i], tt, acc[i]));
+        }
+        s.out[wave][n][(4 * x + g) ^ n] = __builtin_bit_cast(u32x4, r);
+      }
+      load_z(t + 1, bits_next, kk, z[kk]);
+      if (a.dz) {
+        // the wave's own LDS: its writes complete before its reads, in order
+        const bool there = t * 16 + k < a.n_tok;
+#pragma unroll
+        for (int x = 0; x < 4; ++x) {
+          const int row = 4 * x + g;
+          u32x4 v = s.out[wave][row][n ^ row];
+          if (!valid) v = u32x4{0u, 0u, 0u, 0u};
+          __builtin_amdgcn_raw_buffer_store_b128(v, dzres, there ? row * row_bytes + (int)(t * 16 + k) * (kCz * 2) + 16 * n : kOutOfRange,
+                                                 0, 2);
+        }
+      }
+    }
+    bits = bits_next;
+  }
+
+  // dq of the part: accumulator rows = channels 4g..4g+3 (+ 16), column = row n
+  if (row_there) {
+#pragma unroll
+    for (int j = 0; j < kHw; ++j) {
+      float* to = a.dq_parts + ((int64_t)part * a.n_q + q0 + n) * kHD + (kHw * wave + j) * kD;
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
+        if (u == 1 && g >= 2) break;  // channels 24 .. 31
+        f32x4 v;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[i] = ldexpf(dq[j][u][i] * kInvSqrtD, -ds_exp - ek);
+        *reinterpret_cast<f32x4*>(to + 16 * u + 4 * g) = v;
+      }
+    }
+  }
+  // T: the four waves' keys in order. Tile m = 2 x + half, accumulator rows = heads
+  // 4g..4g+3, column n = channel 32 x + 8 (n / 4) + 4 half + n % 4
+  __syncthreads();
+  float* st = reinterpret_cast<float*>(&s.bias[0][0][0]);
+  for (int w = 0; w < 4; ++w) {
+    if (wave == w) {
+#pragma unroll
+      for (int m = 0; m < 8; ++m) {
+        const int c = 32 * (m >> 1) + 8 * (n >> 2) + 4 * (m & 1) + (n & 3);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          float* at = st + (4 * g + i) * kCz + c;
+          *at = w == 0 ? T[m][i] : *at + T[m][i];
+        }
+      }
+    }
+    __syncthreads();
+  }
+  float* to = a.t_parts + ((int64_t)blockIdx.y * gridDim.x + blockIdx.x) * kH * kCz;
+  for (int x = tid; x < kH * kCz; x += 256) {
+    const float v = ldexpf(st[x], -ds_exp);
+    to[x] = a.first ? v : to[x] + v;
+  }
+}
+
+// ----------------------------------------------------------------------------- keys
+// dk and dv of 64 keys of one head over a share of the chunk's row tiles: the four waves
+// take every fourth of them, and their sums meet in LDS. Bound by the reads of P and dS.
+__global__ void __launch_bounds__(256) keys_kernel(FastBackArgs a) {
+  __shared__ f32x4 s_sum[16][64];
+  const int lane = threadIdx.x & 63, n = lane & 15, g = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int h = blockIdx.y, split = blockIdx.z, n_tiles = (int)(a.n_pad / 16);
+  const int t0 = blockIdx.x * 4;
+  int64_t count, first;
+  chunk_of((a.rows + 15) / 16, a.kv_splits, split, &count, &first);
+  f32x4 acc[4][2][2];  // [key tile][dk, dv][channels 0..15, 16..31]
+#pragma unroll
+  for (int x = 0; x < 16; ++x) acc[x >> 2][(x >> 1) & 1][x & 1] = f32x4{0.f, 0.f, 0.f, 0.f};
+  for (int64_t r = first + wave; r < first + count; r += 4) {
+    const int64_t row_tile = (int64_t)h * (a.nq_pad >> 4) + (a.row0 >> 4) + r;
+    const u32x4 qt = reinterpret_cast<const u32x4*>(a.qt)[row_tile * 64 + lane];
+    const u32x4 ot = reinterpret_cast<const u32x4*>(a.ot)[row_tile * 64 + lane];
+    const u32x4* pd = a.pd + (((int64_t)h * (a.chunk_pad >> 4) + r) * n_tiles + t0) * 64 + lane;
+    u32x4 x[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) x[k] = t0 + k < n_tiles ? __builtin_nontemporal_load(pd + 64 * k) : u32x4{0u, 0u, 0u, 0u};
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      const u32x2 qu = {qt[2 * u], qt[2 * u + 1]}, ou = {ot[2 * u], ot[2 * u + 1]};
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const u32x2 p = {x[k][0], x[k][1]}, ds = {x[k][2], x[k][3]};
+        acc[k][0][u] = mfma16h(__builtin_bit_cast(f16x4, ds), __builtin_bit_cast(f16x4, qu), acc[k][0][u]);
+        acc[k][1][u] = mfma16h(__builtin_bit_cast(f16x4, p), __builtin_bit_cast(f16x4, ou), acc[k][1][u]);
+      }
+    }
+  }
+  for (int w = 3; w >= 1; --w) {
+    if (wave == w) {
+#pragma unroll
+      for (int x = 0; x < 16; ++x) {
+        const f32x4 v = acc[x >> 2][(x >> 1) & 1][x & 1];
+        s_sum[x][lane] = w == 3 ? v : s_sum[x][lane] + v;
+      }
+    }
+    __syncthreads();
+  }
+  if (wave > 0) return;
+  const int eq = a.exps[0], ev = a.exps[2], ed = a.exps[3];
+  const int64_t v_at = a.n_tok * kHD;
+#pragma unroll
+  for (int k = 0; k < 4; ++k)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int64_t key = 16 * (int64_t)(t0 + k) + 4 * g + i;
+      if (key >= a.n_tok) continue;
+      float* to = a.kv_parts + ((int64_t)split * 2 * a.n_tok + key) * kHD + h * kD + n;
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
+        if (16 * u + n >= kD) continue;
+        const float dk = ldexpf((acc[k][0][u][i] + s_sum[4 * k + u][lane][i]) * kLn2, kDsShift - ev - ed - eq);
+        const float dv = ldexpf(acc[k][1][u][i] + s_sum[4 * k + 2 + u][lane][i], -kPShift - ed);
+        to[16 * u] = a.first ? dk : to[16 * u] + dk;
+        to[v_at + 16 * u] = a.first ? dv : to[v_at + 16 * u] + dv;
+      }
+    }
+}
+
+}  // namespace
+
+hipError_t launch_fast_back_prep(const FastBackArgs& a, hipStream_t st) {
+  hipLaunchKernelGGL(prep_kernel, dim3(1 + kBackTops), dim3(256), 0, st, a);
+  return hipGetLastError();
+}
+
+hipError_t launch_fast_back_pack(const FastBackArgs& a, hipStream_t st) {
+  hipLaunchKernelGGL(pack_kernel, dim3((unsigned)((a.nq_pad + a.n_pad) / 16)), dim3(256), 0, st, a);
+  return hipGetLastError();
+}
+
+hipError_t launch_fast_back_pairs(const FastBackArgs& a, hipStream_t st) {
+  hipLaunchKernelGGL(pairs_kernel, dim3((unsigned)((a.rows + 15) / 16), (unsigned)a.n_parts), dim3(256), 0, st, a);
+  return hipGetLastError();
+}
+
+hipError_t launch_fast_back_keys(const FastBackArgs& a, hipStream_t st) {
+  hipLaunchKernelGGL(keys_kernel, dim3((unsigned)((a.n_pad / 16 + 3) / 4), kH, (unsigned)a.kv_splits), dim3(256), 0, st, a);
+  return hipGetLastError();
+}
+
+}  // namespace dcp

@@ -1123,56 +1123,103 @@ int dcp_layer_norm_backward(int64_t n_rows, int32_t c, int32_t in_dtype, int32_t
 // ----------------------------------------------------------------------------- attention backward
 namespace {
 
-// Most bytes of P and dS that the general path keeps at a time: the stripe's rows
-// are taken in chunks of as many as fit, at least one.
-constexpr size_t kBackPairBytes = (size_t)256 << 20;
+// Most bytes of P and dS kept at a time: the stripe's rows are taken in chunks of as
+// many as fit, at least one (the fused path: 16).
+constexpr size_t kBackGenBytes = (size_t)256 << 20;
+constexpr size_t kBackFastBytes = (size_t)2 << 30;
 
 struct BackLayout {
-  int64_t chunk;  // rows at a time
-  int dp, dq_parts, groups, kv_splits, ds_splits, w_splits;
-  size_t off_q, off_k, off_v, off_g, off_qp, off_dop, off_stat, off_p, off_ds, off_dq_parts, off_t_parts, off_kv_parts,
-      off_dq, off_dkv, off_dg, off_t, off_ds_parts, off_w_parts, total;
+  int64_t chunk, nq_pad, n_pad;  // chunk: rows at a time
+  int dp, dq_parts, t_parts, kv_splits, ds_splits, w_splits;
+  // projections, general and fused rows' operands, fused keys' operands
+  size_t off_q, off_k, off_v, off_g, off_qp, off_dop, off_stat, off_qf, off_qt, off_of, off_ot, off_lse, off_dot, off_kf,
+      off_kt, off_vf, off_tv, off_tops, off_exps, off_wops;
+  size_t off_p, off_ds, off_dq_parts, off_t_parts, off_kv_parts, off_dq, off_dkv, off_dg, off_t, off_ds_parts, off_w_parts,
+      total;
 };
 
-void back_layout(const dcp_shape* sh, int64_t n_q, BackLayout* L) {
+// Parts that the fused backward splits a row tile's keys into: two workgroups fit a CU,
+// so a launch runs in rounds of 512, each as long as its part's tiles and about two
+// tiles' time for its start and end; the fewest parts within 3% of the cheapest.
+int fast_back_parts(int64_t groups, int64_t tiles) {
+  const int64_t cap = tiles < 64 ? tiles : 64;
+  double cost[65], best = 0.0;
+  for (int64_t p = 1; p <= cap; ++p) {
+    const int64_t rounds = (groups * p + 511) / 512;
+    cost[p] = (double)rounds * ((double)((tiles + p - 1) / p) + 2.0);
+    if (p == 1 || cost[p] < best) best = cost[p];
+  }
+  for (int64_t p = 1; p <= cap; ++p)
+    if (cost[p] <= 1.03 * best) return (int)p;
+  return 1;
+}
+
+void back_layout(const dcp_shape* sh, Path path, int64_t n_q, BackLayout* L) {
   const int64_t N = sh->n_tokens, H = sh->n_heads, hd = H * sh->head_dim;
   size_t off = 0;
-  auto take = [&](size_t floats) {
+  auto take = [&](size_t bytes) {
     const size_t o = off;
-    off = round_up(off + floats * sizeof(float), 256);
+    off = round_up(off + bytes, 256);
     return o;
   };
-  L->dp = sh->head_dim <= 16 ? 16 : sh->head_dim <= 32 ? 32 : 64;
-  L->chunk = (int64_t)(kBackPairBytes / ((size_t)2 * H * N * sizeof(float)));
-  if (L->chunk < 1) L->chunk = 1;
-  if (L->chunk > n_q) L->chunk = n_q;
-  const int64_t tiles = (N + 63) / 64;
-  // workgroups for the whole chip from few rows: keys split between them
-  int64_t parts = dcp::kBackMaxGroups / L->chunk;
-  L->dq_parts = (int)(parts < 1 ? 1 : parts > tiles ? tiles : parts);
-  L->groups = dcp::back_pairs_groups(L->chunk, L->dq_parts);
-  int64_t splits = 1024 / (tiles * H), most = (L->chunk + 15) / 16;
+  *L = BackLayout{};
+  L->off_q = take((size_t)n_q * hd * 4);
+  L->off_k = take((size_t)N * hd * 4);
+  L->off_v = take((size_t)N * hd * 4);
+  L->off_g = take((size_t)n_q * hd * 4);
+  const int64_t key_groups = (N + 63) / 64;
+  int64_t splits, most;
+  if (path == kPathFast) {
+    L->nq_pad = (n_q + 15) / 16 * 16;
+    L->n_pad = (N + 15) / 16 * 16;
+    const size_t per_tile = (size_t)16 * L->n_pad * H * 4;  // P and dS of 16 rows, fp16
+    L->chunk = 16 * (int64_t)(kBackFastBytes / per_tile);
+    if (L->chunk < 16) L->chunk = 16;
+    if (L->chunk > L->nq_pad) L->chunk = L->nq_pad;
+    const int64_t groups = L->chunk / 16;
+    L->dq_parts = fast_back_parts(groups, L->n_pad / 16);
+    L->t_parts = (int)groups * L->dq_parts;
+    const size_t rows = (size_t)H * L->nq_pad * dcp::kFastDp * 2, keys = (size_t)H * L->n_pad * dcp::kFastDp * 2;
+    for (size_t* o : {&L->off_qf, &L->off_qt, &L->off_of, &L->off_ot}) *o = take(rows);
+    for (size_t* o : {&L->off_kf, &L->off_kt, &L->off_vf}) *o = take(keys);
+    L->off_lse = take((size_t)H * L->nq_pad * 4);
+    L->off_dot = take((size_t)H * L->nq_pad * 4);
+    L->off_tv = take((size_t)(L->n_pad / 16) * 4);
+    L->off_tops = take((3 + dcp::kBackTops) * 4);
+    L->off_exps = take(5 * 4);
+    L->off_wops = take(768 * 16);
+    L->off_p = take((size_t)groups * per_tile);
+    splits = 512 / (key_groups * H);
+    most = groups / 8;
+  } else {
+    L->dp = sh->head_dim <= 16 ? 16 : sh->head_dim <= 32 ? 32 : 64;
+    L->chunk = (int64_t)(kBackGenBytes / ((size_t)2 * H * N * 4));
+    if (L->chunk < 1) L->chunk = 1;
+    if (L->chunk > n_q) L->chunk = n_q;
+    // workgroups for the whole chip from few rows: keys split between them
+    const int64_t parts = dcp::kBackMaxGroups / L->chunk;
+    L->dq_parts = (int)(parts < 1 ? 1 : parts > key_groups ? key_groups : parts);
+    L->t_parts = dcp::back_pairs_groups(L->chunk, L->dq_parts);
+    L->off_qp = take((size_t)H * n_q * L->dp * 4);
+    L->off_dop = take((size_t)H * n_q * L->dp * 4);
+    L->off_stat = take((size_t)H * n_q * 16);
+    L->off_p = take((size_t)H * L->chunk * N * 4);
+    L->off_ds = take((size_t)H * L->chunk * N * 4);
+    splits = 1024 / (key_groups * H);
+    most = (L->chunk + 15) / 16;
+  }
   if (splits > most) splits = most;
   L->kv_splits = (int)(splits < 1 ? 1 : splits > 16 ? 16 : splits);
   dcp::back_gemm_splits(N, (int32_t)hd, sh->c_s, &L->ds_splits, &L->w_splits);
-  L->off_q = take((size_t)n_q * hd);
-  L->off_k = take((size_t)N * hd);
-  L->off_v = take((size_t)N * hd);
-  L->off_g = take((size_t)n_q * hd);
-  L->off_qp = take((size_t)H * n_q * L->dp);
-  L->off_dop = take((size_t)H * n_q * L->dp);
-  L->off_stat = take((size_t)H * n_q * 4);
-  L->off_p = take((size_t)H * L->chunk * N);
-  L->off_ds = take((size_t)H * L->chunk * N);
-  L->off_dq_parts = take((size_t)L->dq_parts * n_q * hd);
-  L->off_t_parts = take((size_t)L->groups * H * sh->c_z);
-  L->off_kv_parts = take((size_t)L->kv_splits * 2 * N * hd);
-  L->off_dq = take((size_t)n_q * hd);
-  L->off_dkv = take((size_t)2 * N * hd);
-  L->off_dg = take((size_t)n_q * hd);
-  L->off_t = take((size_t)H * sh->c_z);
-  L->off_ds_parts = take((size_t)L->ds_splits * N * sh->c_s);
-  L->off_w_parts = take((size_t)L->w_splits * 4 * hd * sh->c_s);
+  L->off_dq_parts = take((size_t)L->dq_parts * n_q * hd * 4);
+  L->off_t_parts = take((size_t)L->t_parts * H * sh->c_z * 4);
+  L->off_kv_parts = take((size_t)L->kv_splits * 2 * N * hd * 4);
+  L->off_dq = take((size_t)n_q * hd * 4);
+  L->off_dkv = take((size_t)2 * N * hd * 4);
+  L->off_dg = take((size_t)n_q * hd * 4);
+  L->off_t = take((size_t)H * sh->c_z * 4);
+  L->off_ds_parts = take((size_t)L->ds_splits * N * sh->c_s * 4);
+  L->off_w_parts = take((size_t)L->w_splits * 4 * hd * sh->c_s * 4);
   L->total = off;
 }
 
@@ -1190,7 +1237,7 @@ int dcp_pair_bias_attention_backward_workspace_size(const dcp_shape* shape, int6
     return ok();
   }
   BackLayout L;
-  back_layout(shape, n_q, &L);
+  back_layout(shape, path, n_q, &L);
   *bytes = L.total;
   return ok();
 }
@@ -1225,7 +1272,7 @@ int dcp_pair_bias_attention_backward(const dcp_shape* shape, const dcp_weights* 
                             !aligned(w->w_g, 16) || !aligned(w->w_b, 16) || !aligned(w->ln_gamma, 16)))
     return fail(DCP_ERR_INVALID_ARGUMENT, "w_q, w_k, w_v, w_g, w_b and ln_gamma must be 16-byte aligned");
   BackLayout L{};
-  if (n_q > 0) back_layout(shape, n_q, &L);
+  if (n_q > 0) back_layout(shape, path, n_q, &L);
   if (n_q > 0 && (!workspace || !aligned(workspace, 256)))
     return fail(DCP_ERR_WORKSPACE, "workspace must be a 256-byte aligned device pointer");
   if (workspace_bytes < L.total)
@@ -1276,75 +1323,135 @@ int dcp_pair_bias_attention_backward(const dcp_shape* shape, const dcp_weights* 
   pa.k = at(L.off_k);
   pa.v = at(L.off_v);
   pa.g = at(L.off_g);
-  if ((e = dcp::launch_gen_proj(pa, st)) != hipSuccess)
-    return fail(DCP_ERR_HIP, "projection launch failed: %s", hipGetErrorString(e));
-
-  dcp::BackRowsArgs ra{};
-  ra.n_q = n_q;
-  ra.n_heads = shape->n_heads;
-  ra.head_dim = shape->head_dim;
-  ra.dp = L.dp;
-  ra.dout_bf16 = shape->out_dtype == DCP_BF16;
-  ra.m = m;
-  ra.l = l;
-  ra.acc = acc;
-  ra.g = pa.g;
-  ra.q = pa.q;
-  ra.dout = dout;
-  ra.qp = at(L.off_qp);
-  ra.dop = at(L.off_dop);
-  ra.stat = at(L.off_stat);
-  ra.dg = at(L.off_dg);
-  if ((e = dcp::launch_back_rows(ra, st)) != hipSuccess)
-    return fail(DCP_ERR_HIP, "row gradient launch failed: %s", hipGetErrorString(e));
-
-  for (int64_t row = 0; row < n_q; row += L.chunk) {
-    const int64_t rows = row + L.chunk <= n_q ? L.chunk : n_q - row;
-    dcp::BackPairsArgs ba{};
-    ba.z = z_rows;
-    ba.z_bf16 = act_bf16;
+  float *dg = at(L.off_dg), *dq_parts = at(L.off_dq_parts), *t_parts = at(L.off_t_parts), *kv_parts = at(L.off_kv_parts);
+  if (path == kPathFast) {
+    auto half = [&](size_t off) { return reinterpret_cast<uint16_t*>(ws + off); };
+    dcp::FastBackArgs ba{};
+    ba.z = static_cast<const uint16_t*>(z_rows);
     ba.mask = key_mask;
     ba.w_b = w->w_b;
     ba.gamma = w->ln_gamma;
+    ba.q = pa.q;
+    ba.g = pa.g;
     ba.k = pa.k;
     ba.v = pa.v;
-    ba.qp = ra.qp;
-    ba.dop = ra.dop;
-    ba.stat = ra.stat;
+    ba.m = m;
+    ba.l = l;
+    ba.acc = acc;
+    ba.dout = dout;
+    ba.dout_bf16 = shape->out_dtype == DCP_BF16;
     ba.n_tok = N;
     ba.n_q = n_q;
-    ba.row0 = row;
-    ba.rows = rows;
-    ba.c_z = shape->c_z;
-    ba.n_heads = shape->n_heads;
-    ba.head_dim = shape->head_dim;
-    ba.dp = L.dp;
-    ba.n_parts = L.dq_parts;
-    ba.first = row == 0;
+    ba.nq_pad = L.nq_pad;
+    ba.n_pad = L.n_pad;
+    ba.tops = reinterpret_cast<uint32_t*>(ws + L.off_tops);
+    ba.exps = reinterpret_cast<int32_t*>(ws + L.off_exps);
+    ba.w_ops = reinterpret_cast<dcp::u32x4*>(ws + L.off_wops);
+    ba.qf = half(L.off_qf);
+    ba.qt = half(L.off_qt);
+    ba.of = half(L.off_of);
+    ba.ot = half(L.off_ot);
+    ba.kf = half(L.off_kf);
+    ba.kt = half(L.off_kt);
+    ba.vf = half(L.off_vf);
+    ba.lse = at(L.off_lse);
+    ba.dot = at(L.off_dot);
+    ba.dg = dg;
+    ba.tile_valid = reinterpret_cast<uint32_t*>(ws + L.off_tv);
     ba.eps = shape->ln_eps;
-    ba.p = at(L.off_p);
-    ba.ds = at(L.off_ds);
-    ba.dz = grads->dz_rows;
-    ba.dq_parts = at(L.off_dq_parts);
-    ba.t_parts = at(L.off_t_parts);
-    if ((e = dcp::launch_back_pairs(ba, dcp::back_pairs_groups(rows, L.dq_parts), st)) != hipSuccess)
-      return fail(DCP_ERR_HIP, "pair gradient launch failed: %s", hipGetErrorString(e));
-    dcp::BackKeysArgs ka{};
-    ka.p = ba.p;
-    ka.ds = ba.ds;
-    ka.qp = ra.qp;
-    ka.dop = ra.dop;
-    ka.n_tok = N;
-    ka.n_q = n_q;
-    ka.row0 = row;
-    ka.rows = rows;
-    ka.n_heads = shape->n_heads;
-    ka.head_dim = shape->head_dim;
-    ka.n_splits = L.kv_splits;
-    ka.first = row == 0;
-    ka.kv_parts = at(L.off_kv_parts);
-    if ((e = dcp::launch_back_keys(ka, L.dp, st)) != hipSuccess)
-      return fail(DCP_ERR_HIP, "key gradient launch failed: %s", hipGetErrorString(e));
+    ba.chunk_pad = L.chunk;
+    ba.n_parts = L.dq_parts;
+    ba.kv_splits = L.kv_splits;
+    ba.pd = reinterpret_cast<dcp::u32x4*>(ws + L.off_p);
+    ba.dz = static_cast<uint16_t*>(grads->dz_rows);
+    ba.dq_parts = dq_parts;
+    ba.t_parts = t_parts;
+    ba.kv_parts = kv_parts;
+    pa.tops = ba.tops;
+    if ((e = dcp::launch_fast_back_prep(ba, st)) != hipSuccess)
+      return fail(DCP_ERR_HIP, "gradient preparation launch failed: %s", hipGetErrorString(e));
+    if ((e = dcp::launch_gen_proj(pa, st)) != hipSuccess)
+      return fail(DCP_ERR_HIP, "projection launch failed: %s", hipGetErrorString(e));
+    if ((e = dcp::launch_fast_back_pack(ba, st)) != hipSuccess)
+      return fail(DCP_ERR_HIP, "operand launch failed: %s", hipGetErrorString(e));
+    for (ba.row0 = 0; ba.row0 < n_q; ba.row0 += L.chunk) {
+      ba.rows = ba.row0 + L.chunk <= n_q ? L.chunk : n_q - ba.row0;
+      ba.first = ba.row0 == 0;
+      if ((e = dcp::launch_fast_back_pairs(ba, st)) != hipSuccess)
+        return fail(DCP_ERR_HIP, "pair gradient launch failed: %s", hipGetErrorString(e));
+      if ((e = dcp::launch_fast_back_keys(ba, st)) != hipSuccess)
+        return fail(DCP_ERR_HIP, "key gradient launch failed: %s", hipGetErrorString(e));
+    }
+  } else {
+    if ((e = dcp::launch_gen_proj(pa, st)) != hipSuccess)
+      return fail(DCP_ERR_HIP, "projection launch failed: %s", hipGetErrorString(e));
+    dcp::BackRowsArgs ra{};
+    ra.n_q = n_q;
+    ra.n_heads = shape->n_heads;
+    ra.head_dim = shape->head_dim;
+    ra.dp = L.dp;
+    ra.dout_bf16 = shape->out_dtype == DCP_BF16;
+    ra.m = m;
+    ra.l = l;
+    ra.acc = acc;
+    ra.g = pa.g;
+    ra.q = pa.q;
+    ra.dout = dout;
+    ra.qp = at(L.off_qp);
+    ra.dop = at(L.off_dop);
+    ra.stat = at(L.off_stat);
+    ra.dg = dg;
+    if ((e = dcp::launch_back_rows(ra, st)) != hipSuccess)
+      return fail(DCP_ERR_HIP, "row gradient launch failed: %s", hipGetErrorString(e));
+
+    for (int64_t row = 0; row < n_q; row += L.chunk) {
+      const int64_t rows = row + L.chunk <= n_q ? L.chunk : n_q - row;
+      dcp::BackPairsArgs ba{};
+      ba.z = z_rows;
+      ba.z_bf16 = act_bf16;
+      ba.mask = key_mask;
+      ba.w_b = w->w_b;
+      ba.gamma = w->ln_gamma;
+      ba.k = pa.k;
+      ba.v = pa.v;
+      ba.qp = ra.qp;
+      ba.dop = ra.dop;
+      ba.stat = ra.stat;
+      ba.n_tok = N;
+      ba.n_q = n_q;
+      ba.row0 = row;
+      ba.rows = rows;
+      ba.c_z = shape->c_z;
+      ba.n_heads = shape->n_heads;
+      ba.head_dim = shape->head_dim;
+      ba.dp = L.dp;
+      ba.n_parts = L.dq_parts;
+      ba.first = row == 0;
+      ba.eps = shape->ln_eps;
+      ba.p = at(L.off_p);
+      ba.ds = at(L.off_ds);
+      ba.dz = grads->dz_rows;
+      ba.dq_parts = dq_parts;
+      ba.t_parts = t_parts;
+      if ((e = dcp::launch_back_pairs(ba, dcp::back_pairs_groups(rows, L.dq_parts), st)) != hipSuccess)
+        return fail(DCP_ERR_HIP, "pair gradient launch failed: %s", hipGetErrorString(e));
+      dcp::BackKeysArgs ka{};
+      ka.p = ba.p;
+      ka.ds = ba.ds;
+      ka.qp = ra.qp;
+      ka.dop = ra.dop;
+      ka.n_tok = N;
+      ka.n_q = n_q;
+      ka.row0 = row;
+      ka.rows = rows;
+      ka.n_heads = shape->n_heads;
+      ka.head_dim = shape->head_dim;
+      ka.n_splits = L.kv_splits;
+      ka.first = row == 0;
+      ka.kv_parts = kv_parts;
+      if ((e = dcp::launch_back_keys(ka, L.dp, st)) != hipSuccess)
+        return fail(DCP_ERR_HIP, "key gradient launch failed: %s", hipGetErrorString(e));
+    }
   }
 
   dcp::BackSumArgs sa{};
@@ -1353,12 +1460,11 @@ int dcp_pair_bias_attention_backward(const dcp_shape* shape, const dcp_weights* 
   sa.hd = hd;
   sa.dq_n = L.dq_parts;
   sa.kv_n = L.kv_splits;
-  sa.t_n = L.groups;
+  sa.t_n = L.t_parts;
   sa.t_cols = shape->n_heads * shape->c_z;
-  sa.dq_parts = at(L.off_dq_parts);
-  sa.kv_parts = at(L.off_kv_parts);
-  sa.t_parts = at(L.off_t_parts);
-  sa.dq_scale = sa.t_scale = 1.0f;
+  sa.dq_parts = dq_parts;
+  sa.kv_parts = kv_parts;
+  sa.t_parts = t_parts;
   sa.dq = at(L.off_dq);
   sa.dkv = at(L.off_dkv);
   sa.t = at(L.off_t);
@@ -1381,7 +1487,7 @@ int dcp_pair_bias_attention_backward(const dcp_shape* shape, const dcp_weights* 
   ga.dq = sa.dq;
   ga.dk = sa.dkv;
   ga.dv = sa.dkv + N * hd;
-  ga.dg = ra.dg;
+  ga.dg = dg;
   ga.ds_splits = L.ds_splits;
   ga.w_splits = L.w_splits;
   ga.ds_parts = grads->ds ? at(L.off_ds_parts) : nullptr;

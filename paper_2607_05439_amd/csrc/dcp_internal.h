@@ -5,6 +5,8 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include "cdna4.h"
+
 namespace dcp {
 
 // Shape of the fused MFMA path.
@@ -84,6 +86,7 @@ struct GenProjArgs {
   const uint8_t* mask;   // [N] or null: v of masked keys is written as 0
   int32_t kv_head_dim;   // k, v in the tiled attention's layout, with this head size; 0: row-major [N][hd]
   int32_t s_vec;         // set by the launcher: rows of s take 4-element loads
+  uint32_t* tops;        // largest |q|, |k|, |v| (bits of the floats, cleared before), or null
 };
 
 struct GenAttnArgs {
@@ -285,11 +288,39 @@ struct BackKeysArgs {
   float* kv_parts;         // [n_splits][2][N][hd]
 };
 
+// The fused shape (backward_fast.hip). fp16 operands: *f [H][tokens][32], *t
+// [H][tokens / 16][64][2][4].
+constexpr int kBackTops = 64;
+struct FastBackArgs {
+  const uint16_t* z;       // [n_q][N][128] bf16
+  const uint8_t* mask;     // [N] or null
+  const float *w_b, *gamma;
+  const float *q, *g, *k, *v;  // [n_q][384], [N][384] fp32
+  const float *m, *l, *acc;
+  const void* dout;
+  int32_t dout_bf16;
+  int64_t n_tok, n_q, nq_pad, n_pad;
+  uint32_t* tops;          // [3 + kBackTops]: largest |q|, |k|, |v|, and of shares of |dout|
+  int32_t* exps;           // [5]: the powers of two of q, k, v, do and W''
+  u32x4* w_ops;            // [768]: bias weights, W''
+  uint16_t *qf, *qt, *of, *ot, *kf, *kt, *vf;
+  float *lse, *dot, *dg;   // [H][nq_pad] twice, [n_q][384]
+  uint32_t* tile_valid;    // [n_pad / 16]
+  float eps;
+  // per chunk of rows
+  int64_t row0, rows, chunk_pad;  // row0 and chunk_pad multiples of 16
+  int32_t n_parts, kv_splits, first;
+  u32x4* pd;               // [H][chunk_pad / 16][n_pad / 16][64]: P and dS of 16 rows by 16 keys
+  uint16_t* dz;            // as z, or null
+  float* dq_parts;         // [n_parts][n_q][384]
+  float* t_parts;          // [n_parts * row tiles][16][128]
+  float* kv_parts;         // [kv_splits][2][N][384]
+};
+
 struct BackSumArgs {
   int64_t n_tok, n_q;
   int32_t hd, dq_n, kv_n, t_n, t_cols;
   const float *dq_parts, *kv_parts, *t_parts;
-  float dq_scale, t_scale;
   float *dq, *dkv, *t;     // [n_q][hd], [2][N][hd], [H][c_z]
   uint32_t token_blocks;   // set by the launcher
 };
@@ -339,6 +370,10 @@ hipError_t launch_back_rows(const BackRowsArgs& a, hipStream_t st);
 int back_pairs_groups(int64_t rows, int n_parts);
 hipError_t launch_back_pairs(const BackPairsArgs& a, int groups, hipStream_t st);
 hipError_t launch_back_keys(const BackKeysArgs& a, int dp, hipStream_t st);
+hipError_t launch_fast_back_prep(const FastBackArgs& a, hipStream_t st);
+hipError_t launch_fast_back_pack(const FastBackArgs& a, hipStream_t st);
+hipError_t launch_fast_back_pairs(const FastBackArgs& a, hipStream_t st);
+hipError_t launch_fast_back_keys(const FastBackArgs& a, hipStream_t st);
 hipError_t launch_back_sum(const BackSumArgs& a, hipStream_t st);
 void back_gemm_splits(int64_t n_tok, int32_t hd, int32_t c_s, int* ds_splits, int* w_splits);
 hipError_t launch_back_gemm(const BackGemmArgs& a, hipStream_t st);
