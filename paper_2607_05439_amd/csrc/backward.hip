@@ -66,28 +66,42 @@ __device__ __forceinline__ float quad_sum(float x) {
 }
 
 // ----------------------------------------------------------------------------- query rows
-// One thread per row and head: do, q in padded rows of dp floats per head, the
-// statistics {m, 1 / L, D, -}, and dg. A row without keys (L = 0) gets weights of 0.
+// Eight lanes per row and head: do, q in padded rows of dp floats per head, the
+// statistics {m, 1 / L, D, -}, and dg. A row without keys (L = 0) gets weights of 0. All
+// loads before the first store, which the compiler could not tell from them.
 __global__ void __launch_bounds__(256) back_rows_kernel(BackRowsArgs a) {
-  const int64_t t = (int64_t)blockIdx.x * 256 + threadIdx.x;
-  if (t >= a.n_q * a.n_heads) return;
+  constexpr int kMost = kGenMaxD / 8;
+  const int64_t t = ((int64_t)blockIdx.x * 256 + threadIdx.x) >> 3;
+  if (t >= a.n_q * a.n_heads) return;  // eight lanes alike
+  const int sub = threadIdx.x & 7, d = a.head_dim;
   const int64_t row = t / a.n_heads;
-  const int h = (int)(t - row * a.n_heads), d = a.head_dim;
+  const int h = (int)(t - row * a.n_heads);
   const int64_t at = row * a.n_heads * d + (int64_t)h * d, to = ((int64_t)h * a.n_q + row) * a.dp;
   const float l = a.l[(int64_t)h * a.n_q + row], inv_l = l == 0.0f ? 0.0f : 1.0f / l;
-  float dot = 0.0f;
-  for (int e = 0; e < d; ++e) {
-    const float g = a.g[at + e], up = load_one(a.dout, a.dout_bf16, at + e);
-    const float o = l == 0.0f ? 0.0f : a.acc[at + e] * inv_l;
-    const float x = g * up;
-    dot = fmaf(x, o, dot);
-    a.dg[at + e] = up * o * g * (1.0f - g);
-    a.dop[to + e] = x;
-    a.qp[to + e] = a.q[at + e];
-  }
-  for (int e = d; e < a.dp; ++e) a.dop[to + e] = a.qp[to + e] = 0.0f;
   const float m = l == 0.0f ? 0.0f : a.m[(int64_t)h * a.n_q + row];
-  *reinterpret_cast<f32x4*>(a.stat + 4 * ((int64_t)h * a.n_q + row)) = f32x4{m, inv_l, dot, 0.0f};
+  float g[kMost], up[kMost], o[kMost], q[kMost], dot = 0.0f;
+#pragma unroll
+  for (int i = 0; i < kMost; ++i) {
+    const int e = sub + 8 * i;
+    const bool in = e < d;
+    g[i] = in ? a.g[at + e] : 0.0f;
+    up[i] = in ? load_one(a.dout, a.dout_bf16, at + e) : 0.0f;
+    o[i] = in && l != 0.0f ? a.acc[at + e] * inv_l : 0.0f;
+    q[i] = in ? a.q[at + e] : 0.0f;
+  }
+#pragma unroll
+  for (int i = 0; i < kMost; ++i) dot = fmaf(g[i] * up[i], o[i], dot);
+  dot = quad_sum(dot);
+  dot += __shfl_xor(dot, 4);
+#pragma unroll
+  for (int i = 0; i < kMost; ++i) {
+    const int e = sub + 8 * i;
+    if (e >= a.dp) break;
+    a.dop[to + e] = g[i] * up[i];
+    a.qp[to + e] = q[i];
+    if (e < d) a.dg[at + e] = up[i] * o[i] * g[i] * (1.0f - g[i]);
+  }
+  if (sub == 0) *reinterpret_cast<f32x4*>(a.stat + 4 * ((int64_t)h * a.n_q + row)) = f32x4{m, inv_l, dot, 0.0f};
 }
 
 // ----------------------------------------------------------------------------- pairs
@@ -539,7 +553,7 @@ unsigned blocks_of(int64_t items) { return (unsigned)((items + 255) / 256); }
 }  // namespace
 
 hipError_t launch_back_rows(const BackRowsArgs& a, hipStream_t st) {
-  hipLaunchKernelGGL(back_rows_kernel, dim3(blocks_of(a.n_q * a.n_heads)), dim3(256), 0, st, a);
+  hipLaunchKernelGGL(back_rows_kernel, dim3(blocks_of(8 * a.n_q * a.n_heads)), dim3(256), 0, st, a);
   return hipGetLastError();
 }
 

@@ -1060,13 +1060,12 @@ int dcp_layer_norm(int64_t n_rows, int32_t c, int32_t in_dtype, int32_t out_dtyp
   dcp::LayerNormArgs a{};
   a.n_rows = n_rows;
   a.c = c;
-  a.y_bf16 = out_dtype == DCP_BF16;
   a.x = x;
   a.gamma = ln_gamma;
   a.beta = ln_beta;
   a.y = y;
   a.eps = ln_eps;
-  const hipError_t e = dcp::launch_layer_norm(a, in_dtype == DCP_BF16, static_cast<hipStream_t>(stream));
+  const hipError_t e = dcp::launch_layer_norm(a, in_dtype == DCP_BF16, out_dtype == DCP_BF16, static_cast<hipStream_t>(stream));
   if (e != hipSuccess) return fail(DCP_ERR_HIP, "LayerNorm launch failed: %s", hipGetErrorString(e));
   return ok();
 }
@@ -1096,7 +1095,6 @@ int dcp_layer_norm_backward(int64_t n_rows, int32_t c, int32_t in_dtype, int32_t
   dcp::LayerNormBackArgs a{};
   a.n_rows = n_rows;
   a.c = c;
-  a.dy_bf16 = out_dtype == DCP_BF16;
   a.x = x;
   a.dy = dy;
   a.gamma = ln_gamma;
@@ -1113,7 +1111,8 @@ int dcp_layer_norm_backward(int64_t n_rows, int32_t c, int32_t in_dtype, int32_t
       return fail(DCP_ERR_WORKSPACE, "workspace too small: %zu bytes given, %zu needed", workspace_bytes, need);
     a.parts = static_cast<float*>(workspace);
   }
-  const hipError_t e = dcp::launch_layer_norm_back(a, in_dtype == DCP_BF16, static_cast<hipStream_t>(stream));
+  const hipError_t e = dcp::launch_layer_norm_back(a, in_dtype == DCP_BF16, out_dtype == DCP_BF16,
+                                                   static_cast<hipStream_t>(stream));
   if (e != hipSuccess) return fail(DCP_ERR_HIP, "LayerNorm backward launch failed: %s", hipGetErrorString(e));
   return ok();
 }

@@ -230,7 +230,7 @@ constexpr int kLnMaxC = 4096;
 
 struct LayerNormArgs {
   int64_t n_rows;
-  int32_t c, y_bf16;
+  int32_t c;
   const void* x;               // [n_rows][c]
   const float *gamma, *beta;   // [c] or null
   void* y;                     // [n_rows][c], may be x
@@ -240,7 +240,7 @@ struct LayerNormArgs {
 
 struct LayerNormBackArgs {
   int64_t n_rows;
-  int32_t c, dy_bf16;
+  int32_t c;
   const void *x, *dy;          // [n_rows][c]
   const float* gamma;          // [c] or null
   void* dx;                    // [n_rows][c] in x's type, or null
@@ -363,9 +363,9 @@ hipError_t launch_topk_merge(const TopkMergeArgs& a, hipStream_t st);
 hipError_t launch_transition(const TransArgs& a, hipStream_t st);
 hipError_t launch_transition_gen(const TransGenArgs& a, hipStream_t st);
 hipError_t launch_scatter_mean(const ScatterArgs& a, hipStream_t st);
-hipError_t launch_layer_norm(const LayerNormArgs& a, bool x_bf16, hipStream_t st);
+hipError_t launch_layer_norm(const LayerNormArgs& a, bool x_bf16, bool y_bf16, hipStream_t st);
 int layer_norm_back_groups(int64_t n_rows, int32_t c);  // workgroups, one partial sum each
-hipError_t launch_layer_norm_back(const LayerNormBackArgs& a, bool x_bf16, hipStream_t st);
+hipError_t launch_layer_norm_back(const LayerNormBackArgs& a, bool x_bf16, bool dy_bf16, hipStream_t st);
 hipError_t launch_back_rows(const BackRowsArgs& a, hipStream_t st);
 int back_pairs_groups(int64_t rows, int n_parts);
 hipError_t launch_back_pairs(const BackPairsArgs& a, int groups, hipStream_t st);
