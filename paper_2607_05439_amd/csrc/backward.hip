@@ -378,10 +378,12 @@ __global__ void __launch_bounds__(256) back_sum_kernel(BackSumArgs a) {
     const int64_t x = (int64_t)blockIdx.x * 256 + threadIdx.x;
     if (x < n_dq) {
       float v = 0.0f;
+#pragma unroll 4
       for (int p = 0; p < a.dq_n; ++p) v += a.dq_parts[p * n_dq + x];
       a.dq[x] = v;
     } else if (x < n_dq + n_kv) {
       float v = 0.0f;
+#pragma unroll 4
       for (int p = 0; p < a.kv_n; ++p) v += a.kv_parts[p * n_kv + x - n_dq];
       a.dkv[x - n_dq] = v;
     }
@@ -390,6 +392,7 @@ __global__ void __launch_bounds__(256) back_sum_kernel(BackSumArgs a) {
   const int cols = a.t_cols, col = (int)(blockIdx.x - a.token_blocks) * 16 + (threadIdx.x & 15), grp = threadIdx.x >> 4;
   float v = 0.0f;
   if (col < cols)
+#pragma unroll 8
     for (int p = grp; p < a.t_n; p += 16) v += a.t_parts[(int64_t)p * cols + col];
   s[grp][threadIdx.x & 15] = v;
   __syncthreads();

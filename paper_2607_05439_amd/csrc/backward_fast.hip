@@ -99,29 +99,38 @@ __global__ void __launch_bounds__(256) prep_kernel(FastBackArgs a) {
     a.w_ops[64 * s + lane] = __builtin_bit_cast(u32x4, hi[s]);
     a.w_ops[64 * (4 + s) + lane] = __builtin_bit_cast(u32x4, lo[s]);
   }
-  // W'' = W' - mean, natural units, as the A operand of dz: tile m = 2 s + half, row r =
-  // channel 32 s + 8 (r / 4) + 4 half + r % 4, k-slots = heads 4g..4g+3
-  float mean[4], top = 0.0f;
+  // W'' = W' - mean, natural units, as the A operand of dz: tile m = 2 x + half, row r =
+  // channel 32 x + 8 (r / 4) + 4 half + r % 4, k-slots = heads 4g..4g+3
+  float w[4][8], top = 0.0f;
+#pragma unroll
+  for (int m = 0; m < 8; ++m) {
+    const int c = 32 * (m >> 1) + 8 * (n >> 2) + 4 * (m & 1) + (n & 3);
+    const float gamma = a.gamma ? a.gamma[c] : 1.0f;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) w[i][m] = a.w_b[(4 * g + i) * kCz + c] * gamma;
+  }
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     float sum = 0.0f;
-    for (int c = n; c < kCz; c += 16) sum += a.w_b[(4 * g + i) * kCz + c] * (a.gamma ? a.gamma[c] : 1.0f);
+#pragma unroll
+    for (int m = 0; m < 8; ++m) sum += w[i][m];
 #pragma unroll
     for (int o = 8; o > 0; o >>= 1) sum += __shfl_xor(sum, o);
-    mean[i] = sum * (1.0f / kCz);
-    for (int c = n; c < kCz; c += 16)
-      top = fmaxf(top, fabsf(a.w_b[(4 * g + i) * kCz + c] * (a.gamma ? a.gamma[c] : 1.0f) - mean[i]));
+#pragma unroll
+    for (int m = 0; m < 8; ++m) {
+      w[i][m] -= sum * (1.0f / kCz);
+      top = fmaxf(top, fabsf(w[i][m]));
+    }
   }
 #pragma unroll
   for (int o = 32; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor(top, o));
   const int ew = scale_exp(top);
-  for (int m = 0; m < 8; ++m) {
-    const int c = 32 * (m >> 1) + 8 * (n >> 2) + 4 * (m & 1) + (n & 3);
-    f16x4 w;
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
-      w[i] = (_Float16)ldexpf(a.w_b[(4 * g + i) * kCz + c] * (a.gamma ? a.gamma[c] : 1.0f) - mean[i], ew);
-    reinterpret_cast<u32x2*>(a.w_ops + 512)[64 * m + lane] = __builtin_bit_cast(u32x2, w);
+  for (int m = 0; m < 8; ++m) {
+    f16x4 v;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[i] = (_Float16)ldexpf(w[i][m], ew);
+    reinterpret_cast<u32x2*>(a.w_ops + 512)[64 * m + lane] = __builtin_bit_cast(u32x2, v);
   }
   if (lane == 0) a.exps[4] = ew;
 }

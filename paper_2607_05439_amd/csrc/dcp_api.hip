@@ -1369,7 +1369,7 @@ int dcp_pair_bias_attention_backward(const dcp_shape* shape, const dcp_weights* 
     pa.tops = ba.tops;
     if ((e = dcp::launch_fast_back_prep(ba, st)) != hipSuccess)
       return fail(DCP_ERR_HIP, "gradient preparation launch failed: %s", hipGetErrorString(e));
-    if ((e = dcp::launch_gen_proj(pa, st)) != hipSuccess)
+    if ((e = dcp::launch_token_proj(pa, st)) != hipSuccess)
       return fail(DCP_ERR_HIP, "projection launch failed: %s", hipGetErrorString(e));
     if ((e = dcp::launch_fast_back_pack(ba, st)) != hipSuccess)
       return fail(DCP_ERR_HIP, "operand launch failed: %s", hipGetErrorString(e));
@@ -1491,7 +1491,8 @@ int dcp_pair_bias_attention_backward(const dcp_shape* shape, const dcp_weights* 
   ga.w_splits = L.w_splits;
   ga.ds_parts = grads->ds ? at(L.off_ds_parts) : nullptr;
   ga.w_parts = grads->dw_q || grads->dw_k || grads->dw_v || grads->dw_g ? at(L.off_w_parts) : nullptr;
-  if ((e = dcp::launch_back_gemm(ga, st)) != hipSuccess)
+  e = path == kPathFast ? dcp::launch_token_grad(ga, st) : dcp::launch_back_gemm(ga, st);
+  if (e != hipSuccess)
     return fail(DCP_ERR_HIP, "token gradient launch failed: %s", hipGetErrorString(e));
 
   fa.ds_splits = L.ds_splits;

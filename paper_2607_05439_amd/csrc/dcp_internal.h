@@ -377,6 +377,8 @@ hipError_t launch_fast_back_keys(const FastBackArgs& a, hipStream_t st);
 hipError_t launch_back_sum(const BackSumArgs& a, hipStream_t st);
 void back_gemm_splits(int64_t n_tok, int32_t hd, int32_t c_s, int* ds_splits, int* w_splits);
 hipError_t launch_back_gemm(const BackGemmArgs& a, hipStream_t st);
+hipError_t launch_token_proj(const GenProjArgs& a, hipStream_t st);  // the fused shape: hd = 384, s in bf16, tops wanted
+hipError_t launch_token_grad(const BackGemmArgs& a, hipStream_t st);
 hipError_t launch_back_finish(const BackFinishArgs& a, hipStream_t st);
 int scatter_order_flags(int64_t n_atoms);  // plan workgroups (one flag each) for n_atoms (<= kScatterFlags)
 

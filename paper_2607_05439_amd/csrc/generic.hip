@@ -147,24 +147,6 @@ __global__ void __launch_bounds__(256) gen_proj_kernel(GenProjArgs a) {
       }
     }
   }
-  if (a.tops && !(q_side && second)) {
-    // the largest magnitude of the tile, NaN and masked keys left out (a maximum does
-    // not depend on its order)
-    float top = 0.0f;
-#pragma unroll
-    for (int y = 0; y < T; ++y) {
-      const int64_t row = row0 + 16 * y + n;
-      if (row >= rows || (!q_side && a.mask && a.mask[row] == 0)) continue;
-#pragma unroll
-      for (int x = 0; x < T; ++x)
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-          if (o0 + 16 * x + 4 * g + i < a.hd) top = fmaxf(top, fabsf(acc[x][y][i]));
-    }
-#pragma unroll
-    for (int x = 32; x > 0; x >>= 1) top = fmaxf(top, __shfl_xor(top, x));
-    if (lane == 0) atomicMax(a.tops + (q_side ? 0 : second ? 2 : 1), __float_as_uint(top));
-  }
 #pragma unroll
   for (int y = 0; y < T; ++y) {
     const int64_t row = row0 + 16 * y + n;
