@@ -68,9 +68,17 @@ __device__ __forceinline__ float quad_sum(float x) {
 // ----------------------------------------------------------------------------- query rows
 // Eight lanes per row and head: do, q in padded rows of dp floats per head, the
 // statistics {m, 1 / L, D, -}, and dg. A row without keys (L = 0) gets weights of 0. All
-// loads before the first store, which the compiler could not tell from them.
+// loads before the first store, which the compiler could not tell from them. The
+// blocks behind those clear k of masked keys, which may hold anything (v's the
+// projection clears), so that a weight of 0 times it is 0.
 __global__ void __launch_bounds__(256) back_rows_kernel(BackRowsArgs a) {
   constexpr int kMost = kGenMaxD / 8;
+  if (blockIdx.x >= a.row_blocks) {
+    const int64_t x = (int64_t)(blockIdx.x - a.row_blocks) * 256 + threadIdx.x;
+    const int hd = a.n_heads * a.head_dim;
+    if (x < a.n_tok * hd && a.mask[x / hd] == 0) a.k[x] = 0.0f;
+    return;
+  }
   const int64_t t = ((int64_t)blockIdx.x * 256 + threadIdx.x) >> 3;
   if (t >= a.n_q * a.n_heads) return;  // eight lanes alike
   const int sub = threadIdx.x & 7, d = a.head_dim;
@@ -107,14 +115,55 @@ __global__ void __launch_bounds__(256) back_rows_kernel(BackRowsArgs a) {
 // ----------------------------------------------------------------------------- pairs
 // A workgroup takes one query row and a range of keys, 64 at a time: four lanes
 // per key share its channels for the LayerNorm, the bias and dz, and its heads for
-// the logits and dS. It loops over such items, so that T is written once per
-// workgroup.
+// the logits and dS; dq and T are then sums over the tile's keys by output element.
+// It loops over such items, so that T is written once per workgroup. The next
+// tile's z is loaded during this one's arithmetic. CT: pieces of 16 channels of z; NH:
+// heads per lane.
 constexpr int kBackKeys = 64;
 constexpr int kHeadStride = kGenMaxD + 4;
 
-template <int CT, int NH>
-__global__ void __launch_bounds__(256) back_pairs_kernel(BackPairsArgs a) {
+// Four consecutive elements as loaded. vec: whole pieces, aligned; else one by one,
+// indices past the last repeating it.
+template <bool BF16>
+struct Raw4 {
+  uint32_t w[BF16 ? 2 : 4];
+  __device__ __forceinline__ void load(const void* p, int vec, int64_t row, int i0, int len) {
+    if (vec) {
+      const int at = min(i0, len - 4);
+      if constexpr (BF16) {
+        const u32x2 r = *reinterpret_cast<const u32x2*>(static_cast<const uint16_t*>(p) + row + at);
+        w[0] = r[0], w[1] = r[1];
+      } else {
+        const u32x4 r = *reinterpret_cast<const u32x4*>(static_cast<const float*>(p) + row + at);
+        w[0] = r[0], w[1] = r[1], w[2] = r[2], w[3] = r[3];
+      }
+    } else {
+      uint32_t e[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int64_t x = row + min(i0 + i, len - 1);
+        e[i] = BF16 ? (uint32_t)static_cast<const uint16_t*>(p)[x] : static_cast<const uint32_t*>(p)[x];
+      }
+      if constexpr (BF16) {
+        w[0] = e[0] | (e[1] << 16), w[1] = e[2] | (e[3] << 16);
+      } else {
+        w[0] = e[0], w[1] = e[1], w[2] = e[2], w[3] = e[3];
+      }
+    }
+  }
+  __device__ __forceinline__ f32x4 get() const {
+    if constexpr (BF16)
+      return f32x4{__uint_as_float(w[0] << 16), __uint_as_float(w[0] & 0xFFFF0000u), __uint_as_float(w[1] << 16),
+                   __uint_as_float(w[1] & 0xFFFF0000u)};
+    else
+      return f32x4{__uint_as_float(w[0]), __uint_as_float(w[1]), __uint_as_float(w[2]), __uint_as_float(w[3])};
+  }
+};
+
+template <int CT, int NH, bool BF16>
+__global__ void __launch_bounds__(256, CT <= 8 ? 2 : 1) back_pairs_kernel(BackPairsArgs a) {
   constexpr int CZ = 16 * CT, HP = 4 * NH, kGroups = 256 / CZ;  // key groups of the sum T
+  constexpr bool kHeld = CT * HP <= 16;  // W' of the lane's channels stays in registers
   __shared__ __attribute__((aligned(16))) float s_w[HP * CZ];
   __shared__ __attribute__((aligned(16))) float s_zh[kBackKeys * (CZ + 4)];
   __shared__ __attribute__((aligned(16))) float s_ds[kBackKeys * (HP + 4)];
@@ -129,11 +178,24 @@ __global__ void __launch_bounds__(256) back_pairs_kernel(BackPairsArgs a) {
     s_w[x] = h < H && c < c_z ? a.w_b[(int64_t)h * c_z + c] * (a.gamma ? a.gamma[c] : 1.0f) : 0.0f;
   }
   for (int x = tid; x < HP * kHeadStride; x += 256) s_q[x] = s_do[x] = 0.0f;
+  __syncthreads();
+  f32x4 w_held[kHeld ? HP : 1][kHeld ? CT : 1];
+  if constexpr (kHeld)
+#pragma unroll
+    for (int h = 0; h < HP; ++h)
+#pragma unroll
+      for (int m = 0; m < CT; ++m) w_held[h][m] = *reinterpret_cast<const f32x4*>(&s_w[h * CZ + 16 * m + 4 * qd]);
+  auto weights = [&](int h, int m) {
+    if constexpr (kHeld)
+      return w_held[h][m];
+    else
+      return *reinterpret_cast<const f32x4*>(&s_w[h * CZ + 16 * m + 4 * qd]);
+  };
   const int tc = tid % CZ, tg = tid / CZ;  // T: this thread's channel and key group
   float t_sum[HP];
 #pragma unroll
   for (int h = 0; h < HP; ++h) t_sum[h] = 0.0f;
-  const int dq_groups = 256 / hd, dq_x = tid % hd, dq_g = tid / hd;  // hd <= 128
+  const int dq_groups = 256 / hd, dq_x = tid % hd, dq_g = tid / hd, dq_h = dq_x / d;  // hd <= 128
   const int64_t items = a.rows * a.n_parts;
   const int64_t tiles = (a.n_tok + kBackKeys - 1) / kBackKeys;
 
@@ -143,6 +205,19 @@ __global__ void __launch_bounds__(256) back_pairs_kernel(BackPairsArgs a) {
     const int64_t row = a.row0 + r;      // row of the stripe
     int64_t t_count, t_first;
     chunk_of(tiles, a.n_parts, part, &t_count, &t_first);
+    // z and the mask of a tile, keys past the last reading that one's
+    Raw4<BF16> raw[CT];
+    uint8_t attends = 1;
+    auto load_z = [&](int64_t t) {
+      const int64_t j = min(t * kBackKeys + key, a.n_tok - 1);
+      const int64_t off = (row * a.n_tok + j) * c_z;
+      if (a.mask) attends = a.mask[j];
+      int c = 4 * qd;
+      asm volatile("" : "+v"(c));  // (or the indices of the one-by-one loads would fill the registers)
+#pragma unroll
+      for (int m = 0; m < CT; ++m) raw[m].load(a.z, z_vec, off, 16 * m + c, c_z);
+    };
+    load_z(t_first);
     __syncthreads();
     for (int x = tid; x < hd; x += 256) {
       const int h = x / d, e = x - h * d;
@@ -156,16 +231,21 @@ __global__ void __launch_bounds__(256) back_pairs_kernel(BackPairsArgs a) {
     float dq = 0.0f;
     __syncthreads();
     for (int64_t t = t_first; t < t_first + t_count; ++t) {
-      const int64_t j = t * kBackKeys + key;
-      const bool there = j < a.n_tok, valid = there && (!a.mask || a.mask[j] != 0);
-      f32x4 zh[CT];
+      asm volatile("" ::: "memory");  // q, do and W' come from LDS again for each tile, not from registers
+      const int64_t j = t * kBackKeys + key, jj = min(j, a.n_tok - 1);
+      const bool there = j < a.n_tok, valid = there && attends != 0;
       const int64_t off = (row * a.n_tok + j) * c_z;
+      f32x4 zh[CT];
       float s = 0.0f, v = 0.0f;
 #pragma unroll
       for (int m = 0; m < CT; ++m) {
-        zh[m] = valid ? load_four(a.z, a.z_bf16, z_vec, off, 16 * m + 4 * qd, c_z) : f32x4{0.f, 0.f, 0.f, 0.f};
+        const int c = 16 * m + 4 * qd;
+        zh[m] = raw[m].get();
+#pragma unroll
+        for (int i = 0; i < 4; ++i) zh[m][i] = valid && c + i < c_z ? zh[m][i] : 0.0f;
         s += (zh[m][0] + zh[m][1]) + (zh[m][2] + zh[m][3]);
       }
+      if (t + 1 < t_first + t_count) load_z(t + 1);
       const float mu = quad_sum(s) * inv_c;
 #pragma unroll
       for (int m = 0; m < CT; ++m)
@@ -190,7 +270,7 @@ __global__ void __launch_bounds__(256) back_pairs_kernel(BackPairsArgs a) {
           f32x4 p = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
           for (int m = 0; m < CT; ++m) {
-            const f32x4 w = *reinterpret_cast<const f32x4*>(&s_w[(4 * i + x) * CZ + 16 * m + 4 * qd]);
+            const f32x4 w = weights(4 * i + x, m);
 #pragma unroll
             for (int e = 0; e < 4; ++e) p[e] = fmaf(w[e], zh[m][e], p[e]);
           }
@@ -198,20 +278,29 @@ __global__ void __launch_bounds__(256) back_pairs_kernel(BackPairsArgs a) {
           b = qd == x ? sum : b;
         }
         const int h = 4 * i + qd;
-        float ds = 0.0f, p = 0.0f;
-        if (valid && h < H) {
-          f32x4 lg = {0.f, 0.f, 0.f, 0.f}, dp = {0.f, 0.f, 0.f, 0.f};
-          const int64_t kv = j * hd + (int64_t)h * d;
-          for (int e = 0; e < d; e += 4) {
-            const f32x4 kk = load_four(a.k, 0, k_vec, kv, e, d), vv = load_four(a.v, 0, k_vec, kv, e, d);
-            const f32x4 q = *reinterpret_cast<const f32x4*>(&s_q[h * kHeadStride + e]);
-            const f32x4 o = *reinterpret_cast<const f32x4*>(&s_do[h * kHeadStride + e]);
+        f32x4 lg = {0.f, 0.f, 0.f, 0.f}, dp = {0.f, 0.f, 0.f, 0.f};
+        const int64_t kv = jj * hd + (int64_t)min(h, H - 1) * d;
+        for (int e0 = 0; e0 < d; e0 += 16) {
+          Raw4<false> kk[4], vv[4];  // (channels past the head's last repeat it, times 0 of q and do)
 #pragma unroll
-            for (int x = 0; x < 4; ++x) {
-              lg[x] = fmaf(q[x], kk[x], lg[x]);
-              dp[x] = fmaf(o[x], vv[x], dp[x]);
+          for (int x = 0; x < 4; ++x) {
+            kk[x].load(a.k, k_vec, kv, e0 + 4 * x, d);
+            vv[x].load(a.v, k_vec, kv, e0 + 4 * x, d);
+          }
+#pragma unroll
+          for (int x = 0; x < 4; ++x) {
+            const f32x4 q = *reinterpret_cast<const f32x4*>(&s_q[h * kHeadStride + e0 + 4 * x]);
+            const f32x4 o = *reinterpret_cast<const f32x4*>(&s_do[h * kHeadStride + e0 + 4 * x]);
+            const f32x4 kf = kk[x].get(), vf = vv[x].get();
+#pragma unroll
+            for (int y = 0; y < 4; ++y) {
+              lg[y] = fmaf(q[y], kf[y], lg[y]);
+              dp[y] = fmaf(o[y], vf[y], dp[y]);
             }
           }
+        }
+        float ds = 0.0f, p = 0.0f;
+        if (valid && h < H) {
           const float l = (lg[0] + lg[1]) + (lg[2] + lg[3]) + b;
           p = stat[i][1] == 0.0f ? 0.0f : expf(l - stat[i][0]) * stat[i][1];
           ds = p * (((dp[0] + dp[1]) + (dp[2] + dp[3])) - stat[i][2]);
@@ -236,7 +325,7 @@ __global__ void __launch_bounds__(256) back_pairs_kernel(BackPairsArgs a) {
           for (int x = 0; x < 4; ++x)
 #pragma unroll
             for (int m = 0; m < CT; ++m) {
-              const f32x4 w = *reinterpret_cast<const f32x4*>(&s_w[(4 * i + x) * CZ + 16 * m + 4 * qd]);
+              const f32x4 w = weights(4 * i + x, m);
 #pragma unroll
               for (int e = 0; e < 4; ++e) acc[m][e] = fmaf(ds[x], w[e], acc[m][e]);
             }
@@ -258,7 +347,7 @@ __global__ void __launch_bounds__(256) back_pairs_kernel(BackPairsArgs a) {
           for (int e = 0; e < 4; ++e) g[e] = valid ? rstd * (acc[m][e] - s1 - zh[m][e] * s2) : 0.0f;
           if (z_vec) {
             if (c < c_z) {
-              if (a.z_bf16) {
+              if (BF16) {
                 bf16x4 o;
 #pragma unroll
                 for (int e = 0; e < 4; ++e) o[e] = (__bf16)g[e];
@@ -270,29 +359,29 @@ __global__ void __launch_bounds__(256) back_pairs_kernel(BackPairsArgs a) {
           } else {
 #pragma unroll
             for (int e = 0; e < 4; ++e)
-              if (c + e < c_z) store_one(a.dz, a.z_bf16, off + c + e, g[e]);
+              if (c + e < c_z) store_one(a.dz, BF16, off + c + e, g[e]);
           }
         }
       }
-      if (tg < kGroups)
-        for (int x = tg; x < kBackKeys; x += kGroups) {
-          const float zc = s_zh[x * (CZ + 4) + tc];
+#pragma unroll 4
+      for (int x = tg; x < kBackKeys; x += kGroups) {
+        const float zc = s_zh[x * (CZ + 4) + tc];
 #pragma unroll
-          for (int i = 0; i < NH; ++i) {
-            const f32x4 ds = *reinterpret_cast<const f32x4*>(&s_ds[x * (HP + 4) + 4 * i]);
+        for (int i = 0; i < NH; ++i) {
+          const f32x4 ds = *reinterpret_cast<const f32x4*>(&s_ds[x * (HP + 4) + 4 * i]);
 #pragma unroll
-            for (int e = 0; e < 4; ++e) t_sum[4 * i + e] = fmaf(ds[e], zc, t_sum[4 * i + e]);
-          }
+          for (int e = 0; e < 4; ++e) t_sum[4 * i + e] = fmaf(ds[e], zc, t_sum[4 * i + e]);
         }
+      }
       if (dq_g < dq_groups) {
-        const int h = dq_x / d;
-        for (int x = dq_g; x < kBackKeys; x += dq_groups) {
-          const int64_t kj = t * kBackKeys + x;
-          if (kj < a.n_tok && (!a.mask || a.mask[kj] != 0)) dq = fmaf(s_ds[x * (HP + 4) + h], a.k[kj * hd + dq_x], dq);
-        }
+        const float* kp = a.k + t * kBackKeys * hd + dq_x;
+        const int last = (int)min((int64_t)kBackKeys, a.n_tok - t * kBackKeys) - 1;  // dS is 0 past it
+#pragma unroll 8
+        for (int x = dq_g; x < kBackKeys; x += dq_groups) dq = fmaf(s_ds[x * (HP + 4) + dq_h], kp[min(x, last) * hd], dq);
       }
       __syncthreads();
     }
+    // dq: the key groups in order
     s_dq[tid] = dq;
     __syncthreads();
     if (tid < hd) {
@@ -508,47 +597,69 @@ __global__ void __launch_bounds__(256) back_gemm_kernel(BackGemmArgs a) {
 }
 
 // The gradients in their own type: sums of the products' splits, then dW_b and dgamma
-// from T.
+// from T. W consecutive elements a thread: 4 where every tensor has a multiple of that.
+template <int W>
+__device__ __forceinline__ void finish_sum(const float* parts, int n, int64_t stride, void* out, int bf16, int64_t at) {
+  f32x4 v = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 4
+  for (int p = 0; p < n; ++p) {
+    if constexpr (W == 4)
+      v += *reinterpret_cast<const f32x4*>(parts + p * stride);
+    else
+      v[0] += parts[p * stride];
+  }
+  if constexpr (W == 1) {
+    store_one(out, bf16, at, v[0]);
+  } else if (bf16) {
+    bf16x4 r;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) r[i] = (__bf16)v[i];
+    *reinterpret_cast<bf16x4*>(static_cast<__bf16*>(out) + at) = r;
+  } else {
+    *reinterpret_cast<f32x4*>(static_cast<float*>(out) + at) = v;
+  }
+}
+template <int W>
 __global__ void __launch_bounds__(256) back_finish_kernel(BackFinishArgs a) {
   const int64_t n_ds = a.ds ? a.n_tok * a.c_s : 0, n_w = (int64_t)a.hd * a.c_s, n_b = (int64_t)a.n_heads * a.c_z;
-  int64_t x = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  int64_t x = ((int64_t)blockIdx.x * 256 + threadIdx.x) * W;
   if (x < n_ds) {
-    float v = 0.0f;
-    for (int p = 0; p < a.ds_splits; ++p) v += a.ds_parts[p * n_ds + x];
-    store_one(a.ds, a.bf16, x, v);
+    finish_sum<W>(a.ds_parts + x, a.ds_splits, n_ds, a.ds, a.bf16, x);
     return;
   }
   x -= n_ds;
   if (x < 4 * n_w) {
     const int mat = (int)(x / n_w);
-    if (!a.dw[mat]) return;
-    float v = 0.0f;
-    for (int p = 0; p < a.w_splits; ++p) v += a.w_parts[p * 4 * n_w + x];
-    store_one(a.dw[mat], a.bf16, x - mat * n_w, v);
+    if (a.dw[mat]) finish_sum<W>(a.w_parts + x, a.w_splits, 4 * n_w, a.dw[mat], a.bf16, x - mat * n_w);
     return;
   }
   x -= 4 * n_w;
-  if (x < n_b) {
-    if (a.dw_b) store_one(a.dw_b, a.bf16, x, a.t ? a.t[x] * (a.gamma ? a.gamma[x % a.c_z] : 1.0f) : 0.0f);
-    return;
-  }
-  x -= n_b;
-  if (x < a.c_z && a.dgamma) {
-    float v = 0.0f;
-    for (int h = 0; a.t && h < a.n_heads; ++h) v = fmaf(a.w_b[h * (int64_t)a.c_z + x], a.t[h * (int64_t)a.c_z + x], v);
-    store_one(a.dgamma, a.bf16, x, v);
+#pragma unroll
+  for (int64_t end = x + W; x < end; ++x) {
+    if (x < n_b) {
+      if (a.dw_b) store_one(a.dw_b, a.bf16, x, a.t ? a.t[x] * (a.gamma ? a.gamma[x % a.c_z] : 1.0f) : 0.0f);
+    } else if (x - n_b < a.c_z && a.dgamma) {
+      const int64_t c = x - n_b;
+      float v = 0.0f;
+      for (int h = 0; a.t && h < a.n_heads; ++h) v = fmaf(a.w_b[h * (int64_t)a.c_z + c], a.t[h * (int64_t)a.c_z + c], v);
+      store_one(a.dgamma, a.bf16, c, v);
+    }
   }
 }
 
-template <int CT>
+template <int CT, bool BF16>
 hipError_t pairs_go(const BackPairsArgs& a, unsigned grid, hipStream_t st) {
   if (a.n_heads <= 4)
-    hipLaunchKernelGGL((back_pairs_kernel<CT, 1>), dim3(grid), dim3(256), 0, st, a);
+    hipLaunchKernelGGL((back_pairs_kernel<CT, 1, BF16>), dim3(grid), dim3(256), 0, st, a);
   else if (a.n_heads <= 8)
-    hipLaunchKernelGGL((back_pairs_kernel<CT, 2>), dim3(grid), dim3(256), 0, st, a);
+    hipLaunchKernelGGL((back_pairs_kernel<CT, 2, BF16>), dim3(grid), dim3(256), 0, st, a);
   else
-    hipLaunchKernelGGL((back_pairs_kernel<CT, 4>), dim3(grid), dim3(256), 0, st, a);
+    hipLaunchKernelGGL((back_pairs_kernel<CT, 4, BF16>), dim3(grid), dim3(256), 0, st, a);
   return hipGetLastError();
+}
+template <int CT>
+hipError_t pairs_go(const BackPairsArgs& a, unsigned grid, hipStream_t st) {
+  return a.z_bf16 ? pairs_go<CT, true>(a, grid, st) : pairs_go<CT, false>(a, grid, st);
 }
 
 unsigned blocks_of(int64_t items) { return (unsigned)((items + 255) / 256); }
@@ -556,7 +667,10 @@ unsigned blocks_of(int64_t items) { return (unsigned)((items + 255) / 256); }
 }  // namespace
 
 hipError_t launch_back_rows(const BackRowsArgs& a, hipStream_t st) {
-  hipLaunchKernelGGL(back_rows_kernel, dim3(blocks_of(8 * a.n_q * a.n_heads)), dim3(256), 0, st, a);
+  BackRowsArgs b = a;
+  b.row_blocks = blocks_of(8 * a.n_q * a.n_heads);
+  const unsigned key_blocks = a.mask ? blocks_of(a.n_tok * a.n_heads * a.head_dim) : 0;
+  hipLaunchKernelGGL(back_rows_kernel, dim3(b.row_blocks + key_blocks), dim3(256), 0, st, b);
   return hipGetLastError();
 }
 
@@ -591,12 +705,12 @@ hipError_t launch_back_sum(const BackSumArgs& a, hipStream_t st) {
 }
 
 // Splits of the token products' depths: until about four workgroups a CU share them,
-// each at least 128 deep.
-void back_gemm_splits(int64_t n_tok, int32_t hd, int32_t c_s, int* ds_splits, int* w_splits) {
+// each at least min_depth deep.
+void back_gemm_splits(int64_t n_tok, int32_t hd, int32_t c_s, int32_t min_depth, int* ds_splits, int* w_splits) {
   const int64_t c_tiles = (c_s + kGemm - 1) / kGemm, o_tiles = (hd + kGemm - 1) / kGemm;
   const int64_t t_tiles = (n_tok + kGemm - 1) / kGemm;
-  auto fit = [](int64_t tiles, int64_t depth) {
-    int64_t want = 1024 / (tiles < 1 ? 1 : tiles), most = depth / 128;
+  auto fit = [min_depth](int64_t tiles, int64_t depth) {
+    int64_t want = 1024 / (tiles < 1 ? 1 : tiles), most = depth / min_depth;
     if (want > most) want = most;
     if (want > 16) want = 16;
     return (int)(want < 1 ? 1 : want);
@@ -620,7 +734,10 @@ hipError_t launch_back_gemm(const BackGemmArgs& a, hipStream_t st) {
 
 hipError_t launch_back_finish(const BackFinishArgs& a, hipStream_t st) {
   const int64_t n = (a.ds ? a.n_tok * a.c_s : 0) + 4 * (int64_t)a.hd * a.c_s + (int64_t)a.n_heads * a.c_z + a.c_z;
-  hipLaunchKernelGGL(back_finish_kernel, dim3(blocks_of(n)), dim3(256), 0, st, a);
+  if (a.c_s % 4 == 0)
+    hipLaunchKernelGGL(back_finish_kernel<4>, dim3(blocks_of((n + 3) / 4)), dim3(256), 0, st, a);
+  else
+    hipLaunchKernelGGL(back_finish_kernel<1>, dim3(blocks_of(n)), dim3(256), 0, st, a);
   return hipGetLastError();
 }
 

@@ -86,10 +86,10 @@ __global__ void __launch_bounds__(256) prep_kernel(FastBackArgs a) {
     for (int o = 32; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor(top, o));
     if (lane == 0) s_top[tid >> 6] = top;
     __syncthreads();
-    if (tid == 0) a.tops[3 + blockIdx.x - 1] = __float_as_uint(fmaxf(fmaxf(s_top[0], s_top[1]), fmaxf(s_top[2], s_top[3])));
+    if (tid == 0) a.tops[3 * kBackTops + blockIdx.x - 1] = __float_as_uint(fmaxf(fmaxf(s_top[0], s_top[1]), fmaxf(s_top[2], s_top[3])));
     return;
   }
-  if (tid < 3) a.tops[tid] = 0u;  // |q|, |k|, |v|: the projection's maxima go here
+  if (tid < 3 * kBackTops) a.tops[tid] = 0u;  // |q|, |k|, |v|: the projection's maxima go here
   if (tid >= 64) return;
   const int n = lane & 15, g = lane >> 4;
   bf16x8 hi[4], lo[4];
@@ -136,46 +136,53 @@ __global__ void __launch_bounds__(256) prep_kernel(FastBackArgs a) {
 }
 
 // ----------------------------------------------------------------------------- operands
-// A workgroup takes 16 tokens, a thread one of them and one head: first the tiles of the
+// A wave takes 16 tokens and four heads, a lane one of each: first the tiles of the
 // stripe's rows, then those of the keys. [H][tokens][32] operands hold a head's channels
 // and 8 zeros; transposed ones, [H][tile][64 lanes][2][4], hold in lane (n, g) and slot
-// (u, i) channel 16 u + n of token 4g + i.
-__device__ __forceinline__ void pack_one(const float (&x)[kD], int e2, int h, int64_t tok, int64_t padded, uint16_t* rows,
-                                         uint16_t* transposed) {
+// (u, i) channel 16 u + n of token 4g + i. Both leave through LDS in kilobytes, the
+// transposed one by the transposing LDS read, which hands lane i of 16 column i of
+// four rows.
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef __attribute__((address_space(3))) s16x4* lds_s16x4;
+struct PackTile {
+  u32x4 w[kTileQ][4];  // [token][32 halfs]
+};
+__device__ __forceinline__ void pack_row(const float (&x)[kD], int e2, PackTile& to, int tok) {
   f16x8 v[4];
 #pragma unroll
   for (int e = 0; e < kDp; ++e) v[e >> 3][e & 7] = (_Float16)(e < kD ? ldexpf(x[e < kD ? e : 0], e2) : 0.0f);
-  u32x4* to = reinterpret_cast<u32x4*>(rows + ((int64_t)h * padded + tok) * kDp);
 #pragma unroll
-  for (int j = 0; j < 4; ++j) to[j] = __builtin_bit_cast(u32x4, v[j]);
+  for (int j = 0; j < 4; ++j) to.w[tok][j] = __builtin_bit_cast(u32x4, v[j]);
+}
+__device__ __forceinline__ void pack_out(const PackTile& t, int h, int64_t tile, int64_t padded, int lane, uint16_t* rows,
+                                         uint16_t* transposed) {
+  const int64_t at = ((int64_t)h * (padded >> 4) + tile) * 64 + lane;  // 1 KB per head and tile in both layouts
+  reinterpret_cast<u32x4*>(rows)[at] = (&t.w[0][0])[lane];
   if (!transposed) return;
-  const int t = (int)(tok & 15), g = t >> 2, i = t & 3;
-  _Float16* tt = reinterpret_cast<_Float16*>(transposed) + ((int64_t)h * (padded >> 4) + (tok >> 4)) * 512;
-#pragma unroll
-  for (int e = 0; e < kDp; ++e) tt[(16 * g + (e & 15)) * 8 + (e >> 4) * 4 + i] = v[e >> 3][e & 7];
+  const int n = lane & 15, g = lane >> 4;
+  const uint32_t from = lds_addr(&t) + 64 * (4 * g + (n >> 2)) + 8 * (n & 3);
+  const u32x2 a = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4)(uintptr_t)from));
+  const u32x2 b = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4)(uintptr_t)(from + 32)));
+  reinterpret_cast<u32x4*>(transposed)[at] = u32x4{a[0], a[1], b[0], b[1]};
 }
 
-__global__ void __launch_bounds__(256) pack_kernel(FastBackArgs a) {
-  __shared__ int s_exp[4];
-  const int tid = threadIdx.x, h = tid >> 4;
-  if (tid < 64) {
-    float top = __uint_as_float(a.tops[3 + tid]);
+__global__ void __launch_bounds__(64) pack_kernel(FastBackArgs a) {
+  __shared__ PackTile s_x[4], s_y[4];
+  const int lane = threadIdx.x, h = 4 * blockIdx.y + (lane >> 4);
+  int e2[4];  // powers of two of q (with its factor), k, v, and of dout for do (|do| <= |dout|)
+#pragma unroll
+  for (int x = 0; x < 4; ++x) {
+    float top = __uint_as_float(a.tops[kBackTops * x + lane]);
 #pragma unroll
     for (int o = 32; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor(top, o));
-    if (tid == 0) {
-      s_exp[0] = scale_exp(__uint_as_float(a.tops[0]) * (kLog2e * kInvSqrtD));
-      s_exp[1] = scale_exp(__uint_as_float(a.tops[1]));
-      s_exp[2] = scale_exp(__uint_as_float(a.tops[2]));
-      s_exp[3] = scale_exp(top);  // |do| <= |dout|
-      if (blockIdx.x == 0)
-        for (int i = 0; i < 4; ++i) a.exps[i] = s_exp[i];
-    }
+    e2[x] = scale_exp(x == 0 ? top * (kLog2e * kInvSqrtD) : top);
+    if (blockIdx.x == 0 && blockIdx.y == 0 && lane == 0) a.exps[x] = e2[x];
   }
-  __syncthreads();
-  const int eq = s_exp[0], ek = s_exp[1], ev = s_exp[2], ed = s_exp[3];
+  const bool is_row = blockIdx.x < a.nq_pad / 16;
+  const int64_t tile = (int64_t)blockIdx.x - (is_row ? 0 : a.nq_pad / 16);
   float x[kD], y[kD];
-  if (blockIdx.x < a.nq_pad / 16) {
-    const int64_t row = (int64_t)blockIdx.x * 16 + (tid & 15), at = row * kHD + h * kD;
+  if (is_row) {
+    const int64_t row = tile * 16 + (lane & 15), at = row * kHD + h * kD;
     const bool there = row < a.n_q;
     float dot = 0.0f, lse = INFINITY;
 #pragma unroll
@@ -208,12 +215,10 @@ __global__ void __launch_bounds__(256) pack_kernel(FastBackArgs a) {
         *reinterpret_cast<f32x4*>(a.dg + at + e) = dg;
       }
     }
-    pack_one(x, eq, h, row, a.nq_pad, a.qf, a.qt);
-    pack_one(y, ed, h, row, a.nq_pad, a.of, a.ot);
     a.lse[(int64_t)h * a.nq_pad + row] = lse;
-    a.dot[(int64_t)h * a.nq_pad + row] = ldexpf(dot, ev + ed);
+    a.dot[(int64_t)h * a.nq_pad + row] = ldexpf(dot, e2[2] + e2[3]);
   } else {
-    const int64_t tile = (int64_t)blockIdx.x - a.nq_pad / 16, key = tile * 16 + (tid & 15), at = key * kHD + h * kD;
+    const int64_t key = tile * 16 + (lane & 15), at = key * kHD + h * kD;
     const bool valid = key < a.n_tok && (!a.mask || a.mask[key] != 0);
 #pragma unroll
     for (int e = 0; e < kD; e += 4) {
@@ -223,11 +228,21 @@ __global__ void __launch_bounds__(256) pack_kernel(FastBackArgs a) {
 #pragma unroll
       for (int i = 0; i < 4; ++i) x[e + i] = k[i], y[e + i] = v[i];
     }
-    pack_one(x, ek, h, key, a.n_pad, a.kf, a.kt);
-    pack_one(y, ev, h, key, a.n_pad, a.vf, nullptr);
-    if (tid < 64) {
-      const uint32_t bits = (uint32_t)(__ballot(valid) & 0xFFFFull);
-      if (tid == 0) a.tile_valid[tile] = bits;
+    const uint32_t bits = (uint32_t)(__ballot(valid) & 0xFFFFull);
+    if (blockIdx.y == 0 && lane == 0) a.tile_valid[tile] = bits;
+  }
+  pack_row(x, e2[is_row ? 0 : 1], s_x[lane >> 4], lane & 15);
+  pack_row(y, e2[is_row ? 3 : 2], s_y[lane >> 4], lane & 15);
+  __syncthreads();
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    const int hh = 4 * blockIdx.y + j;
+    if (is_row) {
+      pack_out(s_x[j], hh, tile, a.nq_pad, lane, a.qf, a.qt);
+      pack_out(s_y[j], hh, tile, a.nq_pad, lane, a.of, a.ot);
+    } else {
+      pack_out(s_x[j], hh, tile, a.n_pad, lane, a.kf, a.kt);
+      pack_out(s_y[j], hh, tile, a.n_pad, lane, a.vf, nullptr);
     }
   }
 }
@@ -268,10 +283,7 @@ __global__ void __launch_bounds__(256, 2) pairs_kernel(FastBackArgs a) {
   const int64_t t_end = t_begin + t_count;
   constexpr int kHw = kH / 4;
 
-  for (int x = tid; x < 512; x += 256) {
-    (&s.w[0][0])[x] = a.w_ops[x];
-    (&s.wt[0][0])[x] = reinterpret_cast<const u32x2*>(a.w_ops + 512)[x];
-  }
+  uint32_t bits = t_begin < t_end ? a.tile_valid[t_begin] : 0u;
   const int eq = a.exps[0], ek = a.exps[1], ev = a.exps[2], ed = a.exps[3], ew = a.exps[4];
   const float s_scale = ldexpf(1.0f, -eq - ek);
   const int ds_exp = ev + ed - kDsShift;          // the stored dS is dS 2^ds_exp
@@ -293,6 +305,13 @@ __global__ void __launch_bounds__(256, 2) pairs_kernel(FastBackArgs a) {
 #pragma unroll
     for (int x = 0; x < 4; ++x) z[x] = __builtin_amdgcn_raw_buffer_load_b128(zres, at + 64 * x, 0, 2);
   };
+  u32x4 z[4][4];
+#pragma unroll
+  for (int kk = 0; kk < 4; ++kk) load_z(t_begin, bits, kk, z[kk]);
+  for (int x = tid; x < 512; x += 256) {
+    (&s.w[0][0])[x] = a.w_ops[x];
+    (&s.wt[0][0])[x] = reinterpret_cast<const u32x2*>(a.w_ops + 512)[x];
+  }
   const __amdgpu_buffer_rsrc_t kres = __builtin_amdgcn_make_buffer_rsrc(a.kf, 0, (int)(kH * a.n_pad * kDp * 2), kRawBufferFlags);
   const __amdgpu_buffer_rsrc_t vres = __builtin_amdgcn_make_buffer_rsrc(a.vf, 0, (int)(kH * a.n_pad * kDp * 2), kRawBufferFlags);
   const __amdgpu_buffer_rsrc_t ktres = __builtin_amdgcn_make_buffer_rsrc(a.kt, 0, (int)(kH * a.n_pad * kDp * 2), kRawBufferFlags);
@@ -325,11 +344,6 @@ __global__ void __launch_bounds__(256, 2) pairs_kernel(FastBackArgs a) {
     }
     wsum = bias_weight_sums(whi, wlo);
   }
-
-  u32x4 z[4][4];
-  uint32_t bits = t_begin < t_end ? a.tile_valid[t_begin] : 0u;
-#pragma unroll
-  for (int kk = 0; kk < 4; ++kk) load_z(t_begin, bits, kk, z[kk]);
 
   for (int64_t t = t_begin; t < t_end; ++t) {
     const uint32_t bits_next = t + 1 < t_end ? a.tile_valid[t + 1] : 0u;
@@ -555,7 +569,7 @@ hipError_t launch_fast_back_prep(const FastBackArgs& a, hipStream_t st) {
 }
 
 hipError_t launch_fast_back_pack(const FastBackArgs& a, hipStream_t st) {
-  hipLaunchKernelGGL(pack_kernel, dim3((unsigned)((a.nq_pad + a.n_pad) / 16)), dim3(256), 0, st, a);
+  hipLaunchKernelGGL(pack_kernel, dim3((unsigned)((a.nq_pad + a.n_pad) / 16), kH / 4), dim3(64), 0, st, a);
   return hipGetLastError();
 }
 

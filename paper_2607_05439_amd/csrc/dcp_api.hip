@@ -1184,7 +1184,7 @@ void back_layout(const dcp_shape* sh, Path path, int64_t n_q, BackLayout* L) {
     L->off_lse = take((size_t)H * L->nq_pad * 4);
     L->off_dot = take((size_t)H * L->nq_pad * 4);
     L->off_tv = take((size_t)(L->n_pad / 16) * 4);
-    L->off_tops = take((3 + dcp::kBackTops) * 4);
+    L->off_tops = take(4 * dcp::kBackTops * 4);
     L->off_exps = take(5 * 4);
     L->off_wops = take(768 * 16);
     L->off_p = take((size_t)groups * per_tile);
@@ -1195,8 +1195,9 @@ void back_layout(const dcp_shape* sh, Path path, int64_t n_q, BackLayout* L) {
     L->chunk = (int64_t)(kBackGenBytes / ((size_t)2 * H * N * 4));
     if (L->chunk < 1) L->chunk = 1;
     if (L->chunk > n_q) L->chunk = n_q;
-    // workgroups for the whole chip from few rows: keys split between them
-    const int64_t parts = dcp::kBackMaxGroups / L->chunk;
+    // at least four items (a row's part of the keys) for each of the workgroups that
+    // loop over them, so that no CU waits long for the last
+    const int64_t parts = 4 * dcp::kBackMaxGroups / L->chunk;
     L->dq_parts = (int)(parts < 1 ? 1 : parts > key_groups ? key_groups : parts);
     L->t_parts = dcp::back_pairs_groups(L->chunk, L->dq_parts);
     L->off_qp = take((size_t)H * n_q * L->dp * 4);
@@ -1209,7 +1210,7 @@ void back_layout(const dcp_shape* sh, Path path, int64_t n_q, BackLayout* L) {
   }
   if (splits > most) splits = most;
   L->kv_splits = (int)(splits < 1 ? 1 : splits > 16 ? 16 : splits);
-  dcp::back_gemm_splits(N, (int32_t)hd, sh->c_s, &L->ds_splits, &L->w_splits);
+  dcp::back_gemm_splits(N, (int32_t)hd, sh->c_s, path == kPathFast ? 256 : 128, &L->ds_splits, &L->w_splits);
   L->off_dq_parts = take((size_t)L->dq_parts * n_q * hd * 4);
   L->off_t_parts = take((size_t)L->t_parts * H * sh->c_z * 4);
   L->off_kv_parts = take((size_t)L->kv_splits * 2 * N * hd * 4);
@@ -1400,6 +1401,9 @@ int dcp_pair_bias_attention_backward(const dcp_shape* shape, const dcp_weights* 
     ra.dop = at(L.off_dop);
     ra.stat = at(L.off_stat);
     ra.dg = dg;
+    ra.n_tok = N;
+    ra.mask = key_mask;
+    ra.k = pa.k;
     if ((e = dcp::launch_back_rows(ra, st)) != hipSuccess)
       return fail(DCP_ERR_HIP, "row gradient launch failed: %s", hipGetErrorString(e));
 

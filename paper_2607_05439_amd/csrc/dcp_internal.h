@@ -86,7 +86,7 @@ struct GenProjArgs {
   const uint8_t* mask;   // [N] or null: v of masked keys is written as 0
   int32_t kv_head_dim;   // k, v in the tiled attention's layout, with this head size; 0: row-major [N][hd]
   int32_t s_vec;         // set by the launcher: rows of s take 4-element loads
-  uint32_t* tops;        // largest |q|, |k|, |v| (bits of the floats, cleared before), or null
+  uint32_t* tops;        // launch_token_proj: [3][64] largest |q|, |k|, |v| (bits of floats, cleared before)
 };
 
 struct GenAttnArgs {
@@ -252,7 +252,7 @@ struct LayerNormBackArgs {
 
 // Backward pass of the attention (backward.hip). Rows are those of the stripe;
 // [H][n_q][dp] holds a head's channels padded with zeros to dp.
-constexpr int kBackMaxGroups = 1024;  // most workgroups (one T each) of the general pair kernel
+constexpr int kBackMaxGroups = 512;  // workgroups (one T each) of the general pair kernel: two fit a CU
 
 struct BackRowsArgs {
   int64_t n_q;
@@ -263,6 +263,10 @@ struct BackRowsArgs {
   float *qp, *dop;         // [H][n_q][dp]
   float* stat;             // [H][n_q][4]: m, 1 / L, D, -
   float* dg;               // [n_q][hd]
+  int64_t n_tok;
+  const uint8_t* mask;     // [N] or null: k of masked keys is cleared
+  float* k;                // [N][hd]
+  uint32_t row_blocks;     // set by the launcher
 };
 
 struct BackPairsArgs {
@@ -290,7 +294,7 @@ struct BackKeysArgs {
 
 // The fused shape (backward_fast.hip). fp16 operands: *f [H][tokens][32], *t
 // [H][tokens / 16][64][2][4].
-constexpr int kBackTops = 64;
+constexpr int kBackTops = 64;  // one wave's lanes
 struct FastBackArgs {
   const uint16_t* z;       // [n_q][N][128] bf16
   const uint8_t* mask;     // [N] or null
@@ -300,7 +304,7 @@ struct FastBackArgs {
   const void* dout;
   int32_t dout_bf16;
   int64_t n_tok, n_q, nq_pad, n_pad;
-  uint32_t* tops;          // [3 + kBackTops]: largest |q|, |k|, |v|, and of shares of |dout|
+  uint32_t* tops;          // [4][kBackTops]: largest |q|, |k|, |v|, |dout| of shares of each (bits of floats)
   int32_t* exps;           // [5]: the powers of two of q, k, v, do and W''
   u32x4* w_ops;            // [768]: bias weights, W''
   uint16_t *qf, *qt, *of, *ot, *kf, *kt, *vf;
@@ -375,7 +379,7 @@ hipError_t launch_fast_back_pack(const FastBackArgs& a, hipStream_t st);
 hipError_t launch_fast_back_pairs(const FastBackArgs& a, hipStream_t st);
 hipError_t launch_fast_back_keys(const FastBackArgs& a, hipStream_t st);
 hipError_t launch_back_sum(const BackSumArgs& a, hipStream_t st);
-void back_gemm_splits(int64_t n_tok, int32_t hd, int32_t c_s, int* ds_splits, int* w_splits);
+void back_gemm_splits(int64_t n_tok, int32_t hd, int32_t c_s, int32_t min_depth, int* ds_splits, int* w_splits);
 hipError_t launch_back_gemm(const BackGemmArgs& a, hipStream_t st);
 hipError_t launch_token_proj(const GenProjArgs& a, hipStream_t st);  // the fused shape: hd = 384, s in bf16, tops wanted
 hipError_t launch_token_grad(const BackGemmArgs& a, hipStream_t st);

@@ -184,7 +184,10 @@ __global__ void __launch_bounds__(256) token_proj_kernel(GenProjArgs p) {
   if (q_side && second) return;
 #pragma unroll
   for (int x = 32; x > 0; x >>= 1) top = fmaxf(top, __shfl_xor(top, x));
-  if (lane == 0) atomicMax(p.tops + (q_side ? 0 : second ? 2 : 1), __float_as_uint(top));  // any order: the same
+  // a maximum does not depend on its order; 64 words per tensor, since atomics on one
+  // word go one after another
+  if (lane == 0)
+    atomicMax(p.tops + 64 * (q_side ? 0 : second ? 2 : 1) + ((4 * (int)blockIdx.x + wave) & 63), __float_as_uint(top));
 }
 
 // ----------------------------------------------------------------------------- ds, dW
