@@ -13,10 +13,10 @@
 // constants per head, have no gradient and no part in the others'.
 // Token side: ds = dq W_q + dg W_g + dk W_k + dv W_v, dW_x = dx^T s.
 //
-// P and dS meet two sums that run across each other: dq over a row's keys, dk
-// and dv over a key's rows. The pair kernel holds a row and sums dq itself; it
-// writes P and dS (8 bytes a pair and head in fp32), and a second kernel that
-// holds keys sums dk and dv. Stripes of rows bound the room for P and dS.
+// P and dS meet sums that run across each other: dq over a row's keys, dk and dv
+// over a key's rows. The pair kernel writes P and dS (8 bytes a pair and head in
+// fp32), and a second kernel sums dq in workgroups that hold rows, dk and dv in
+// workgroups that hold keys. Stripes of rows bound the room for P and dS.
 #include <hip/hip_runtime.h>
 #include <math.h>
 #include <stdint.h>
@@ -69,14 +69,28 @@ __device__ __forceinline__ float quad_sum(float x) {
 // Eight lanes per row and head: do, q in padded rows of dp floats per head, the
 // statistics {m, 1 / L, D, -}, and dg. A row without keys (L = 0) gets weights of 0. All
 // loads before the first store, which the compiler could not tell from them. The
-// blocks behind those clear k of masked keys, which may hold anything (v's the
-// projection clears), so that a weight of 0 times it is 0.
+// blocks behind those lay out k and v in padded rows too, with zeros for masked keys,
+// which may hold anything, so that a weight of 0 times them is 0.
 __global__ void __launch_bounds__(256) back_rows_kernel(BackRowsArgs a) {
   constexpr int kMost = kGenMaxD / 8;
   if (blockIdx.x >= a.row_blocks) {
+    // a piece of four channels a thread: [H][N][dp / 4]
     const int64_t x = (int64_t)(blockIdx.x - a.row_blocks) * 256 + threadIdx.x;
-    const int hd = a.n_heads * a.head_dim;
-    if (x < a.n_tok * hd && a.mask[x / hd] == 0) a.k[x] = 0.0f;
+    const int pieces = a.dp / 4, c = 4 * (int)(x % pieces);
+    const int64_t hj = x / pieces, j = hj % a.n_tok;
+    const int h = (int)(hj / a.n_tok);
+    if (h >= a.n_heads) return;
+    const bool valid = !a.mask || a.mask[j] != 0;
+    const int64_t at = (j * a.n_heads + h) * a.head_dim;
+    f32x4 k = {0.f, 0.f, 0.f, 0.f}, v = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (valid && c + i < a.head_dim) {
+        k[i] = a.k[at + c + i];
+        v[i] = a.v[at + c + i];
+      }
+    reinterpret_cast<f32x4*>(a.kp)[x] = k;
+    reinterpret_cast<f32x4*>(a.vp)[x] = v;
     return;
   }
   const int64_t t = ((int64_t)blockIdx.x * 256 + threadIdx.x) >> 3;
@@ -115,9 +129,8 @@ __global__ void __launch_bounds__(256) back_rows_kernel(BackRowsArgs a) {
 // ----------------------------------------------------------------------------- pairs
 // A workgroup takes one query row and a range of keys, 64 at a time: four lanes
 // per key share its channels for the LayerNorm, the bias and dz, and its heads for
-// the logits and dS; dq and T are then sums over the tile's keys by output element.
-// It loops over such items, so that T is written once per workgroup. The next
-// tile's z is loaded during this one's arithmetic. CT: pieces of 16 channels of z; NH:
+// the logits and dS; T is then a sum over the tile's keys by output element. It
+// loops over such items, so that T is written once per workgroup. CT: pieces of 16 channels of z; NH:
 // heads per lane.
 constexpr int kBackKeys = 64;
 constexpr int kHeadStride = kGenMaxD + 4;
@@ -161,18 +174,18 @@ struct Raw4 {
 };
 
 template <int CT, int NH, bool BF16>
-__global__ void __launch_bounds__(256, CT <= 8 ? 2 : 1) back_pairs_kernel(BackPairsArgs a) {
+__global__ void __launch_bounds__(256, CT <= 8 && NH == 1 ? 3 : CT <= 8 ? 2 : 1) back_pairs_kernel(BackPairsArgs a) {
   constexpr int CZ = 16 * CT, HP = 4 * NH, kGroups = 256 / CZ;  // key groups of the sum T
-  constexpr bool kHeld = CT * HP <= 16;  // W' of the lane's channels stays in registers
+  constexpr bool kHeld = CT * HP <= 8;  // W' of the lane's channels stays in registers
   __shared__ __attribute__((aligned(16))) float s_w[HP * CZ];
   __shared__ __attribute__((aligned(16))) float s_zh[kBackKeys * (CZ + 4)];
   __shared__ __attribute__((aligned(16))) float s_ds[kBackKeys * (HP + 4)];
+  __shared__ f32x4 s_stat[HP];
   __shared__ __attribute__((aligned(16))) float s_q[HP * kHeadStride], s_do[HP * kHeadStride];
-  __shared__ float s_dq[256];
   const int tid = threadIdx.x, key = tid >> 2, qd = tid & 3;
   const int H = a.n_heads, d = a.head_dim, hd = H * d, c_z = a.c_z;
   const float inv_c = 1.0f / (float)c_z, scale = 1.0f / sqrtf((float)d);
-  const int z_vec = c_z % 4 == 0, k_vec = d % 4 == 0;
+  const int z_vec = c_z % 4 == 0;
   for (int x = tid; x < HP * CZ; x += 256) {
     const int h = x / CZ, c = x % CZ;
     s_w[x] = h < H && c < c_z ? a.w_b[(int64_t)h * c_z + c] * (a.gamma ? a.gamma[c] : 1.0f) : 0.0f;
@@ -195,7 +208,6 @@ __global__ void __launch_bounds__(256, CT <= 8 ? 2 : 1) back_pairs_kernel(BackPa
   float t_sum[HP];
 #pragma unroll
   for (int h = 0; h < HP; ++h) t_sum[h] = 0.0f;
-  const int dq_groups = 256 / hd, dq_x = tid % hd, dq_g = tid / hd, dq_h = dq_x / d;  // hd <= 128
   const int64_t items = a.rows * a.n_parts;
   const int64_t tiles = (a.n_tok + kBackKeys - 1) / kBackKeys;
 
@@ -224,17 +236,12 @@ __global__ void __launch_bounds__(256, CT <= 8 ? 2 : 1) back_pairs_kernel(BackPa
       s_q[h * kHeadStride + e] = a.qp[((int64_t)h * a.n_q + row) * a.dp + e] * scale;
       s_do[h * kHeadStride + e] = a.dop[((int64_t)h * a.n_q + row) * a.dp + e];
     }
-    f32x4 stat[NH];
-#pragma unroll
-    for (int i = 0; i < NH; ++i)
-      stat[i] = *reinterpret_cast<const f32x4*>(a.stat + 4 * ((int64_t)min(4 * i + qd, H - 1) * a.n_q + row));
-    float dq = 0.0f;
+    if (tid < HP) s_stat[tid] = *reinterpret_cast<const f32x4*>(a.stat + 4 * ((int64_t)min(tid, H - 1) * a.n_q + row));
     __syncthreads();
     for (int64_t t = t_first; t < t_first + t_count; ++t) {
       asm volatile("" ::: "memory");  // q, do and W' come from LDS again for each tile, not from registers
       const int64_t j = t * kBackKeys + key, jj = min(j, a.n_tok - 1);
       const bool there = j < a.n_tok, valid = there && attends != 0;
-      const int64_t off = (row * a.n_tok + j) * c_z;
       f32x4 zh[CT];
       float s = 0.0f, v = 0.0f;
 #pragma unroll
@@ -245,7 +252,6 @@ __global__ void __launch_bounds__(256, CT <= 8 ? 2 : 1) back_pairs_kernel(BackPa
         for (int i = 0; i < 4; ++i) zh[m][i] = valid && c + i < c_z ? zh[m][i] : 0.0f;
         s += (zh[m][0] + zh[m][1]) + (zh[m][2] + zh[m][3]);
       }
-      if (t + 1 < t_first + t_count) load_z(t + 1);
       const float mu = quad_sum(s) * inv_c;
 #pragma unroll
       for (int m = 0; m < CT; ++m)
@@ -279,31 +285,31 @@ __global__ void __launch_bounds__(256, CT <= 8 ? 2 : 1) back_pairs_kernel(BackPa
         }
         const int h = 4 * i + qd;
         f32x4 lg = {0.f, 0.f, 0.f, 0.f}, dp = {0.f, 0.f, 0.f, 0.f};
-        const int64_t kv = jj * hd + (int64_t)min(h, H - 1) * d;
-        for (int e0 = 0; e0 < d; e0 += 16) {
-          Raw4<false> kk[4], vv[4];  // (channels past the head's last repeat it, times 0 of q and do)
+        const int64_t kv = ((int64_t)min(h, H - 1) * a.n_tok + jj) * a.dp;
+        for (int e0 = 0; e0 < a.dp; e0 += 8) {
+          f32x4 kk[2], vv[2];
 #pragma unroll
-          for (int x = 0; x < 4; ++x) {
-            kk[x].load(a.k, k_vec, kv, e0 + 4 * x, d);
-            vv[x].load(a.v, k_vec, kv, e0 + 4 * x, d);
+          for (int x = 0; x < 2; ++x) {
+            kk[x] = *reinterpret_cast<const f32x4*>(a.k + kv + e0 + 4 * x);
+            vv[x] = *reinterpret_cast<const f32x4*>(a.v + kv + e0 + 4 * x);
           }
 #pragma unroll
-          for (int x = 0; x < 4; ++x) {
+          for (int x = 0; x < 2; ++x) {
             const f32x4 q = *reinterpret_cast<const f32x4*>(&s_q[h * kHeadStride + e0 + 4 * x]);
             const f32x4 o = *reinterpret_cast<const f32x4*>(&s_do[h * kHeadStride + e0 + 4 * x]);
-            const f32x4 kf = kk[x].get(), vf = vv[x].get();
 #pragma unroll
             for (int y = 0; y < 4; ++y) {
-              lg[y] = fmaf(q[y], kf[y], lg[y]);
-              dp[y] = fmaf(o[y], vf[y], dp[y]);
+              lg[y] = fmaf(q[y], kk[x][y], lg[y]);
+              dp[y] = fmaf(o[y], vv[x][y], dp[y]);
             }
           }
         }
         float ds = 0.0f, p = 0.0f;
         if (valid && h < H) {
+          const f32x4 stat = s_stat[h];
           const float l = (lg[0] + lg[1]) + (lg[2] + lg[3]) + b;
-          p = stat[i][1] == 0.0f ? 0.0f : expf(l - stat[i][0]) * stat[i][1];
-          ds = p * (((dp[0] + dp[1]) + (dp[2] + dp[3])) - stat[i][2]);
+          p = stat[1] == 0.0f ? 0.0f : expf(l - stat[0]) * stat[1];
+          ds = p * (((dp[0] + dp[1]) + (dp[2] + dp[3])) - stat[2]);
         }
         s_ds[key * (HP + 4) + h] = ds;
         if (there && h < H) {
@@ -312,8 +318,13 @@ __global__ void __launch_bounds__(256, CT <= 8 ? 2 : 1) back_pairs_kernel(BackPa
           a.ds[at] = ds;
         }
       }
+      // in flight during dz and T, and behind k and v, which wait for nothing else
+      if (t + 1 < t_first + t_count) load_z(t + 1);
       __syncthreads();
       if (a.dz && there) {
+        int at = key;
+        asm volatile("" : "+v"(at));  // (formed here, not held from the top)
+        const int64_t off = (row * a.n_tok + t * kBackKeys + at) * c_z;
         f32x4 acc[CT];
         float s1 = 0.0f, s2 = 0.0f;
 #pragma unroll
@@ -373,20 +384,7 @@ __global__ void __launch_bounds__(256, CT <= 8 ? 2 : 1) back_pairs_kernel(BackPa
           for (int e = 0; e < 4; ++e) t_sum[4 * i + e] = fmaf(ds[e], zc, t_sum[4 * i + e]);
         }
       }
-      if (dq_g < dq_groups) {
-        const float* kp = a.k + t * kBackKeys * hd + dq_x;
-        const int last = (int)min((int64_t)kBackKeys, a.n_tok - t * kBackKeys) - 1;  // dS is 0 past it
-#pragma unroll 8
-        for (int x = dq_g; x < kBackKeys; x += dq_groups) dq = fmaf(s_ds[x * (HP + 4) + dq_h], kp[min(x, last) * hd], dq);
-      }
       __syncthreads();
-    }
-    // dq: the key groups in order
-    s_dq[tid] = dq;
-    __syncthreads();
-    if (tid < hd) {
-      for (int g = 1; g < dq_groups; ++g) dq += s_dq[tid + g * hd];
-      a.dq_parts[((int64_t)part * a.n_q + row) * hd + tid] = dq * scale;
     }
   }
   // T of this workgroup: its key groups in order, added to what earlier chunks left
@@ -406,54 +404,116 @@ __global__ void __launch_bounds__(256, CT <= 8 ? 2 : 1) back_pairs_kernel(BackPa
 }
 
 // ----------------------------------------------------------------------------- keys
-// dk and dv of 64 keys of one head over a share of the chunk's rows: a lane holds
-// a key, the four waves take every fourth row each, and q and do of a row, the
-// same for all lanes, come through the scalar cache.
+// The sums over pairs on the fp32 matrix cores, 16 keys or rows of one head a wave.
+// Blocks of keys: dk^T, dv^T of 64 keys (a wave each 16) over a share of the chunk's rows,
+// 16 rows a step. Blocks of rows: dq of 16 rows over all keys, 16 keys a step, every
+// fourth step a wave. A step's loads are all in flight at once; past the last row or
+// key they repeat that one, with a P and dS of 0.
+// v_mfma_f32_16x16x4_f32: A holds row n, B column n (n = lane % 16), both at
+// k-slot g = lane / 16; the accumulator holds rows 4g..4g+3 of column n.
+__device__ __forceinline__ f32x4 mfma4(float a, float b, f32x4 c) {
+  return __builtin_amdgcn_mfma_f32_16x16x4f32(a, b, c, 0, 0, 0);
+}
+
+template <int DP>
+__device__ __forceinline__ void row_sums(const BackKeysArgs& a, int h, int64_t r0, f32x4 (&s_sum)[4][DP / 16][64]) {
+  constexpr int U = DP / 16;
+  const int lane = threadIdx.x & 63, n = lane & 15, g = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int64_t last = a.n_tok - 1;
+  const float* ds = a.ds + ((int64_t)h * a.rows + min(r0 + n, a.rows - 1)) * a.n_tok;
+  const float* k = a.k + (int64_t)h * a.n_tok * DP + n;
+  f32x4 acc[U];
+#pragma unroll
+  for (int u = 0; u < U; ++u) acc[u] = f32x4{0.f, 0.f, 0.f, 0.f};
+  for (int64_t j0 = 16 * wave; j0 <= last; j0 += 64) {
+    float x[4], y[4][U];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int64_t j = j0 + 4 * g + i, jj = min(j, last);
+      x[i] = ds[jj];
+#pragma unroll
+      for (int u = 0; u < U; ++u) y[i][u] = k[jj * DP + 16 * u];
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const float v = j0 + 4 * g + i <= last ? x[i] : 0.0f;
+#pragma unroll
+      for (int u = 0; u < U; ++u) acc[u] = mfma4(v, y[i][u], acc[u]);
+    }
+  }
+#pragma unroll
+  for (int u = 0; u < U; ++u) s_sum[wave][u][lane] = acc[u];
+  __syncthreads();
+  if (wave >= U) return;
+  // wave u: channels 16 u + n of rows 4g..4g+3
+  const f32x4 v = (s_sum[0][wave][lane] + s_sum[1][wave][lane]) + (s_sum[2][wave][lane] + s_sum[3][wave][lane]);
+  const int hd = a.n_heads * a.head_dim, e = 16 * wave + n;
+  const float scale = 1.0f / sqrtf((float)a.head_dim);
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+    if (r0 + 4 * g + i < a.rows && e < a.head_dim)
+      a.dq[(a.row0 + r0 + 4 * g + i) * hd + (int64_t)h * a.head_dim + e] = v[i] * scale;
+}
+
 template <int DP>
 __global__ void __launch_bounds__(256) back_keys_kernel(BackKeysArgs a) {
-  __shared__ float s_sum[2 * DP][64];
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int64_t j = (int64_t)blockIdx.x * 64 + lane;
-  const int h = blockIdx.y, split = blockIdx.z;
-  const bool there = j < a.n_tok;
+  constexpr int U = DP / 16;
+  __shared__ f32x4 s_sum[4][U][64];
+  const int lane = threadIdx.x & 63, n = lane & 15, g = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int h = blockIdx.y;
+  if (blockIdx.x >= a.key_blocks) {
+    row_sums<DP>(a, h, (int64_t)(blockIdx.x - a.key_blocks) * 16, s_sum);
+    return;
+  }
+  const int64_t j0 = (int64_t)(blockIdx.x / a.n_splits) * 64 + 16 * wave;
+  const int split = blockIdx.x % a.n_splits;
   int64_t count, first;
   chunk_of(a.rows, a.n_splits, split, &count, &first);
-  float dk[DP], dv[DP];
+  const int64_t jj = min(j0 + n, a.n_tok - 1), end = first + count;
+  const float *q = a.qp + ((int64_t)h * a.n_q + a.row0) * DP + n, *o = a.dop + ((int64_t)h * a.n_q + a.row0) * DP + n;
+  f32x4 dk[U], dv[U];
 #pragma unroll
-  for (int e = 0; e < DP; ++e) dk[e] = dv[e] = 0.0f;
-  const int64_t jj = there ? j : a.n_tok - 1;
-  for (int64_t r = first + wave; r < first + count; r += 4) {
-    const int64_t at = ((int64_t)h * a.rows + r) * a.n_tok + jj;
-    const float p = a.p[at], ds = a.ds[at];
-    const float* q = a.qp + ((int64_t)h * a.n_q + a.row0 + r) * DP;
-    const float* o = a.dop + ((int64_t)h * a.n_q + a.row0 + r) * DP;
+  for (int u = 0; u < U; ++u) dk[u] = dv[u] = f32x4{0.f, 0.f, 0.f, 0.f};
+  for (int64_t r0 = first; r0 < end; r0 += 16) {
+    float p[4], ds[4], x[4][U], y[4][U];
 #pragma unroll
-    for (int e = 0; e < DP; ++e) {
-      dk[e] = fmaf(ds, q[e], dk[e]);
-      dv[e] = fmaf(p, o[e], dv[e]);
-    }
-  }
-  for (int w = 3; w >= 1; --w) {
-    if (wave == w) {
+    for (int i = 0; i < 4; ++i) {
+      const int64_t r = min(r0 + 4 * i + g, end - 1), at = ((int64_t)h * a.rows + r) * a.n_tok + jj;
+      p[i] = a.p[at];
+      ds[i] = a.ds[at];
 #pragma unroll
-      for (int e = 0; e < DP; ++e) {
-        s_sum[e][lane] = w == 3 ? dk[e] : s_sum[e][lane] + dk[e];
-        s_sum[DP + e][lane] = w == 3 ? dv[e] : s_sum[DP + e][lane] + dv[e];
+      for (int u = 0; u < U; ++u) {
+        x[i][u] = q[r * DP + 16 * u];
+        y[i][u] = o[r * DP + 16 * u];
       }
     }
-    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const bool in = r0 + 4 * i + g < end;
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        dk[u] = mfma4(in ? ds[i] : 0.0f, x[i][u], dk[u]);
+        dv[u] = mfma4(in ? p[i] : 0.0f, y[i][u], dv[u]);
+      }
+    }
   }
-  if (wave > 0 || !there) return;
   const int hd = a.n_heads * a.head_dim;
   const float scale = 1.0f / sqrtf((float)a.head_dim);
-  float* out = a.kv_parts + ((int64_t)split * 2 * a.n_tok + j) * hd + (int64_t)h * a.head_dim;
-  const int64_t v_at = a.n_tok * hd;
 #pragma unroll
-  for (int e = 0; e < DP; ++e) {
-    if (e >= a.head_dim) break;
-    const float x = (dk[e] + s_sum[e][lane]) * scale, y = dv[e] + s_sum[DP + e][lane];
-    out[e] = a.first ? x : out[e] + x;
-    out[v_at + e] = a.first ? y : out[v_at + e] + y;
+  for (int i = 0; i < 4; ++i) {
+    const int64_t j = j0 + 4 * g + i;
+    if (j >= a.n_tok) continue;
+    float* out = a.kv_parts + ((int64_t)split * 2 * a.n_tok + j) * hd + (int64_t)h * a.head_dim + n;
+    const int64_t v_at = a.n_tok * hd;
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      if (16 * u + n >= a.head_dim) continue;
+      const float x = dk[u][i] * scale, y = dv[u][i];
+      out[16 * u] = a.first ? x : out[16 * u] + x;
+      out[v_at + 16 * u] = a.first ? y : out[v_at + 16 * u] + y;
+    }
   }
 }
 
@@ -462,7 +522,7 @@ __global__ void __launch_bounds__(256) back_keys_kernel(BackKeysArgs a) {
 // of parts per workgroup.
 __global__ void __launch_bounds__(256) back_sum_kernel(BackSumArgs a) {
   __shared__ float s[16][17];
-  const int64_t n_dq = a.n_q * a.hd, n_kv = 2 * a.n_tok * a.hd;
+  const int64_t n_dq = a.dq_parts ? a.n_q * a.hd : 0, n_kv = 2 * a.n_tok * a.hd;
   if (blockIdx.x < a.token_blocks) {
     const int64_t x = (int64_t)blockIdx.x * 256 + threadIdx.x;
     if (x < n_dq) {
@@ -495,8 +555,6 @@ __global__ void __launch_bounds__(256) back_sum_kernel(BackSumArgs a) {
 // ds = sum over x of dx W_x (64 tokens by 64 channels per workgroup) and dW_x = dx^T s
 // (64 outputs by 64 channels), on the fp32 matrix cores: a workgroup's four waves
 // take 32 x 32 each, operands 16 deep through LDS, the next 16 in flight.
-// v_mfma_f32_16x16x4_f32: A holds row n, B column n (n = lane % 16), both at
-// k-slot g = lane / 16; the accumulator holds rows 4g..4g+3 of column n.
 constexpr int kGemm = 64, kDeep = 16, kGemmStride = kGemm + 16;
 
 __global__ void __launch_bounds__(256) back_gemm_kernel(BackGemmArgs a) {
@@ -578,7 +636,7 @@ __global__ void __launch_bounds__(256) back_gemm_kernel(BackGemmArgs a) {
 #pragma unroll
       for (int u = 0; u < 2; ++u)
 #pragma unroll
-        for (int w = 0; w < 2; ++w) acc[u][w] = __builtin_amdgcn_mfma_f32_16x16x4f32(x[u], y[w], acc[u][w], 0, 0, 0);
+        for (int w = 0; w < 2; ++w) acc[u][w] = mfma4(x[u], y[w], acc[u][w]);
     }
     if (i + 1 < steps) stage(buf ^ 1);
   }
@@ -621,30 +679,29 @@ __device__ __forceinline__ void finish_sum(const float* parts, int n, int64_t st
 }
 template <int W>
 __global__ void __launch_bounds__(256) back_finish_kernel(BackFinishArgs a) {
-  const int64_t n_ds = a.ds ? a.n_tok * a.c_s : 0, n_w = (int64_t)a.hd * a.c_s, n_b = (int64_t)a.n_heads * a.c_z;
+  const int64_t n_ds = a.ds ? a.n_tok * a.c_s : 0, n_w = (int64_t)a.hd * a.c_s;
+  if (blockIdx.x >= a.sum_blocks) {
+    const int n_b = a.n_heads * a.c_z, x = (int)(blockIdx.x - a.sum_blocks) * 256 + threadIdx.x;
+    if (x < n_b) {
+      if (a.dw_b) store_one(a.dw_b, a.bf16, x, a.t ? a.t[x] * (a.gamma ? a.gamma[x % a.c_z] : 1.0f) : 0.0f);
+    } else if (x < n_b + a.c_z && a.dgamma) {
+      float v = 0.0f;
+#pragma unroll 4
+      for (int h = 0; h < (a.t ? a.n_heads : 0); ++h) v = fmaf(a.w_b[h * a.c_z + x - n_b], a.t[h * a.c_z + x - n_b], v);
+      store_one(a.dgamma, a.bf16, x - n_b, v);
+    }
+    return;
+  }
   int64_t x = ((int64_t)blockIdx.x * 256 + threadIdx.x) * W;
   if (x < n_ds) {
     finish_sum<W>(a.ds_parts + x, a.ds_splits, n_ds, a.ds, a.bf16, x);
     return;
   }
   x -= n_ds;
-  if (x < 4 * n_w) {
-    const int mat = (int)(x / n_w);
-    if (a.dw[mat]) finish_sum<W>(a.w_parts + x, a.w_splits, 4 * n_w, a.dw[mat], a.bf16, x - mat * n_w);
-    return;
-  }
-  x -= 4 * n_w;
-#pragma unroll
-  for (int64_t end = x + W; x < end; ++x) {
-    if (x < n_b) {
-      if (a.dw_b) store_one(a.dw_b, a.bf16, x, a.t ? a.t[x] * (a.gamma ? a.gamma[x % a.c_z] : 1.0f) : 0.0f);
-    } else if (x - n_b < a.c_z && a.dgamma) {
-      const int64_t c = x - n_b;
-      float v = 0.0f;
-      for (int h = 0; a.t && h < a.n_heads; ++h) v = fmaf(a.w_b[h * (int64_t)a.c_z + c], a.t[h * (int64_t)a.c_z + c], v);
-      store_one(a.dgamma, a.bf16, c, v);
-    }
-  }
+  if (x >= 4 * n_w) return;
+  const int mat = (x >= n_w) + (x >= 2 * n_w) + (x >= 3 * n_w);
+  void* const out = mat == 0 ? a.dw[0] : mat == 1 ? a.dw[1] : mat == 2 ? a.dw[2] : a.dw[3];
+  if (out) finish_sum<W>(a.w_parts + x, a.w_splits, 4 * n_w, out, a.bf16, x - mat * n_w);
 }
 
 template <int CT, bool BF16>
@@ -669,7 +726,7 @@ unsigned blocks_of(int64_t items) { return (unsigned)((items + 255) / 256); }
 hipError_t launch_back_rows(const BackRowsArgs& a, hipStream_t st) {
   BackRowsArgs b = a;
   b.row_blocks = blocks_of(8 * a.n_q * a.n_heads);
-  const unsigned key_blocks = a.mask ? blocks_of(a.n_tok * a.n_heads * a.head_dim) : 0;
+  const unsigned key_blocks = blocks_of(a.n_tok * a.n_heads * (a.dp / 4));
   hipLaunchKernelGGL(back_rows_kernel, dim3(b.row_blocks + key_blocks), dim3(256), 0, st, b);
   return hipGetLastError();
 }
@@ -687,19 +744,21 @@ hipError_t launch_back_pairs(const BackPairsArgs& a, int groups, hipStream_t st)
 }
 
 hipError_t launch_back_keys(const BackKeysArgs& a, int dp, hipStream_t st) {
-  const dim3 grid((unsigned)((a.n_tok + 63) / 64), (unsigned)a.n_heads, (unsigned)a.n_splits);
+  BackKeysArgs b = a;
+  b.key_blocks = (uint32_t)((a.n_tok + 63) / 64 * a.n_splits);
+  const dim3 grid(b.key_blocks + (unsigned)((a.rows + 15) / 16), (unsigned)a.n_heads);
   if (dp == 16)
-    hipLaunchKernelGGL(back_keys_kernel<16>, grid, dim3(256), 0, st, a);
+    hipLaunchKernelGGL(back_keys_kernel<16>, grid, dim3(256), 0, st, b);
   else if (dp == 32)
-    hipLaunchKernelGGL(back_keys_kernel<32>, grid, dim3(256), 0, st, a);
+    hipLaunchKernelGGL(back_keys_kernel<32>, grid, dim3(256), 0, st, b);
   else
-    hipLaunchKernelGGL(back_keys_kernel<64>, grid, dim3(256), 0, st, a);
+    hipLaunchKernelGGL(back_keys_kernel<64>, grid, dim3(256), 0, st, b);
   return hipGetLastError();
 }
 
 hipError_t launch_back_sum(const BackSumArgs& a, hipStream_t st) {
   BackSumArgs b = a;
-  b.token_blocks = blocks_of(a.n_q * a.hd + 2 * a.n_tok * a.hd);
+  b.token_blocks = blocks_of((a.dq_parts ? a.n_q * a.hd : 0) + 2 * a.n_tok * a.hd);
   hipLaunchKernelGGL(back_sum_kernel, dim3(b.token_blocks + (unsigned)((a.t_cols + 15) / 16)), dim3(256), 0, st, b);
   return hipGetLastError();
 }
@@ -733,11 +792,17 @@ hipError_t launch_back_gemm(const BackGemmArgs& a, hipStream_t st) {
 }
 
 hipError_t launch_back_finish(const BackFinishArgs& a, hipStream_t st) {
-  const int64_t n = (a.ds ? a.n_tok * a.c_s : 0) + 4 * (int64_t)a.hd * a.c_s + (int64_t)a.n_heads * a.c_z + a.c_z;
-  if (a.c_s % 4 == 0)
-    hipLaunchKernelGGL(back_finish_kernel<4>, dim3(blocks_of((n + 3) / 4)), dim3(256), 0, st, a);
+  BackFinishArgs b = a;
+  const int64_t n = (a.ds ? a.n_tok * a.c_s : 0) + (a.dw[0] || a.dw[1] || a.dw[2] || a.dw[3] ? 4 * (int64_t)a.hd * a.c_s : 0);
+  const int64_t tail = a.dw_b || a.dgamma ? (int64_t)a.n_heads * a.c_z + a.c_z : 0;
+  const bool four = a.c_s % 4 == 0;
+  b.sum_blocks = blocks_of(four ? (n + 3) / 4 : n);
+  const unsigned blocks = b.sum_blocks + blocks_of(tail);
+  if (blocks == 0) return hipSuccess;
+  if (four)
+    hipLaunchKernelGGL(back_finish_kernel<4>, dim3(blocks), dim3(256), 0, st, b);
   else
-    hipLaunchKernelGGL(back_finish_kernel<1>, dim3(blocks_of(n)), dim3(256), 0, st, a);
+    hipLaunchKernelGGL(back_finish_kernel<1>, dim3(blocks), dim3(256), 0, st, b);
   return hipGetLastError();
 }
 

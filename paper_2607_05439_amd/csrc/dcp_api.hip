@@ -1131,7 +1131,7 @@ struct BackLayout {
   int64_t chunk, nq_pad, n_pad;  // chunk: rows at a time
   int dp, dq_parts, t_parts, kv_splits, ds_splits, w_splits;
   // projections, general and fused rows' operands, fused keys' operands
-  size_t off_q, off_k, off_v, off_g, off_qp, off_dop, off_stat, off_qf, off_qt, off_of, off_ot, off_lse, off_dot, off_kf,
+  size_t off_q, off_k, off_v, off_g, off_qp, off_dop, off_kp, off_vp, off_stat, off_qf, off_qt, off_of, off_ot, off_lse, off_dot, off_kf,
       off_kt, off_vf, off_tv, off_tops, off_exps, off_wops;
   size_t off_p, off_ds, off_dq_parts, off_t_parts, off_kv_parts, off_dq, off_dkv, off_dg, off_t, off_ds_parts, off_w_parts,
       total;
@@ -1195,13 +1195,15 @@ void back_layout(const dcp_shape* sh, Path path, int64_t n_q, BackLayout* L) {
     L->chunk = (int64_t)(kBackGenBytes / ((size_t)2 * H * N * 4));
     if (L->chunk < 1) L->chunk = 1;
     if (L->chunk > n_q) L->chunk = n_q;
-    // at least four items (a row's part of the keys) for each of the workgroups that
+    // at least three items (a row's part of the keys) for each of the workgroups that
     // loop over them, so that no CU waits long for the last
-    const int64_t parts = 4 * dcp::kBackMaxGroups / L->chunk;
+    const int64_t parts = 3 * dcp::kBackMaxGroups / L->chunk;
     L->dq_parts = (int)(parts < 1 ? 1 : parts > key_groups ? key_groups : parts);
     L->t_parts = dcp::back_pairs_groups(L->chunk, L->dq_parts);
     L->off_qp = take((size_t)H * n_q * L->dp * 4);
     L->off_dop = take((size_t)H * n_q * L->dp * 4);
+    L->off_kp = take((size_t)H * N * L->dp * 4);
+    L->off_vp = take((size_t)H * N * L->dp * 4);
     L->off_stat = take((size_t)H * n_q * 16);
     L->off_p = take((size_t)H * L->chunk * N * 4);
     L->off_ds = take((size_t)H * L->chunk * N * 4);
@@ -1211,7 +1213,7 @@ void back_layout(const dcp_shape* sh, Path path, int64_t n_q, BackLayout* L) {
   if (splits > most) splits = most;
   L->kv_splits = (int)(splits < 1 ? 1 : splits > 16 ? 16 : splits);
   dcp::back_gemm_splits(N, (int32_t)hd, sh->c_s, path == kPathFast ? 256 : 128, &L->ds_splits, &L->w_splits);
-  L->off_dq_parts = take((size_t)L->dq_parts * n_q * hd * 4);
+  L->off_dq_parts = path == kPathFast ? take((size_t)L->dq_parts * n_q * hd * 4) : 0;
   L->off_t_parts = take((size_t)L->t_parts * H * sh->c_z * 4);
   L->off_kv_parts = take((size_t)L->kv_splits * 2 * N * hd * 4);
   L->off_dq = take((size_t)n_q * hd * 4);
@@ -1404,6 +1406,9 @@ int dcp_pair_bias_attention_backward(const dcp_shape* shape, const dcp_weights* 
     ra.n_tok = N;
     ra.mask = key_mask;
     ra.k = pa.k;
+    ra.v = pa.v;
+    ra.kp = at(L.off_kp);
+    ra.vp = at(L.off_vp);
     if ((e = dcp::launch_back_rows(ra, st)) != hipSuccess)
       return fail(DCP_ERR_HIP, "row gradient launch failed: %s", hipGetErrorString(e));
 
@@ -1415,8 +1420,8 @@ int dcp_pair_bias_attention_backward(const dcp_shape* shape, const dcp_weights* 
       ba.mask = key_mask;
       ba.w_b = w->w_b;
       ba.gamma = w->ln_gamma;
-      ba.k = pa.k;
-      ba.v = pa.v;
+      ba.k = ra.kp;
+      ba.v = ra.vp;
       ba.qp = ra.qp;
       ba.dop = ra.dop;
       ba.stat = ra.stat;
@@ -1434,7 +1439,6 @@ int dcp_pair_bias_attention_backward(const dcp_shape* shape, const dcp_weights* 
       ba.p = at(L.off_p);
       ba.ds = at(L.off_ds);
       ba.dz = grads->dz_rows;
-      ba.dq_parts = dq_parts;
       ba.t_parts = t_parts;
       if ((e = dcp::launch_back_pairs(ba, dcp::back_pairs_groups(rows, L.dq_parts), st)) != hipSuccess)
         return fail(DCP_ERR_HIP, "pair gradient launch failed: %s", hipGetErrorString(e));
@@ -1452,6 +1456,8 @@ int dcp_pair_bias_attention_backward(const dcp_shape* shape, const dcp_weights* 
       ka.n_splits = L.kv_splits;
       ka.first = row == 0;
       ka.kv_parts = kv_parts;
+      ka.k = ra.kp;
+      ka.dq = at(L.off_dq);
       if ((e = dcp::launch_back_keys(ka, L.dp, st)) != hipSuccess)
         return fail(DCP_ERR_HIP, "key gradient launch failed: %s", hipGetErrorString(e));
     }
@@ -1465,7 +1471,7 @@ int dcp_pair_bias_attention_backward(const dcp_shape* shape, const dcp_weights* 
   sa.kv_n = L.kv_splits;
   sa.t_n = L.t_parts;
   sa.t_cols = shape->n_heads * shape->c_z;
-  sa.dq_parts = dq_parts;
+  sa.dq_parts = path == kPathFast ? dq_parts : nullptr;
   sa.kv_parts = kv_parts;
   sa.t_parts = t_parts;
   sa.dq = at(L.off_dq);

@@ -252,7 +252,7 @@ struct LayerNormBackArgs {
 
 // Backward pass of the attention (backward.hip). Rows are those of the stripe;
 // [H][n_q][dp] holds a head's channels padded with zeros to dp.
-constexpr int kBackMaxGroups = 512;  // workgroups (one T each) of the general pair kernel: two fit a CU
+constexpr int kBackMaxGroups = 768;  // workgroups (one T each) of the general pair kernel: three fit a CU
 
 struct BackRowsArgs {
   int64_t n_q;
@@ -264,8 +264,9 @@ struct BackRowsArgs {
   float* stat;             // [H][n_q][4]: m, 1 / L, D, -
   float* dg;               // [n_q][hd]
   int64_t n_tok;
-  const uint8_t* mask;     // [N] or null: k of masked keys is cleared
-  float* k;                // [N][hd]
+  const uint8_t* mask;     // [N] or null
+  const float *k, *v;      // [N][hd]
+  float *kp, *vp;          // [H][N][dp], zeros for masked keys
   uint32_t row_blocks;     // set by the launcher
 };
 
@@ -274,22 +275,23 @@ struct BackPairsArgs {
   int32_t z_bf16;
   const uint8_t* mask;     // [N] or null
   const float *w_b, *gamma;
-  const float *k, *v;      // [N][hd]
+  const float *k, *v;      // [H][N][dp]
   const float *qp, *dop, *stat;
   int64_t n_tok, n_q, row0, rows;  // rows [row0, row0 + rows) of the stripe
   int32_t c_z, n_heads, head_dim, dp, n_parts, first;
   float eps;
   float *p, *ds;           // [H][rows][N]
   void* dz;                // as z, or null
-  float* dq_parts;         // [n_parts][n_q][hd]
   float* t_parts;          // [groups][H][c_z]
 };
 
 struct BackKeysArgs {
-  const float *p, *ds, *qp, *dop;
+  const float *p, *ds, *qp, *dop, *k;  // k [H][N][dp]
   int64_t n_tok, n_q, row0, rows;
   int32_t n_heads, head_dim, n_splits, first;
   float* kv_parts;         // [n_splits][2][N][hd]
+  float* dq;               // [n_q][hd]
+  uint32_t key_blocks;     // set by the launcher
 };
 
 // The fused shape (backward_fast.hip). fp16 operands: *f [H][tokens][32], *t
@@ -324,7 +326,7 @@ struct FastBackArgs {
 struct BackSumArgs {
   int64_t n_tok, n_q;
   int32_t hd, dq_n, kv_n, t_n, t_cols;
-  const float *dq_parts, *kv_parts, *t_parts;
+  const float *dq_parts, *kv_parts, *t_parts;  // dq_parts null: dq is there already
   float *dq, *dkv, *t;     // [n_q][hd], [2][N][hd], [H][c_z]
   uint32_t token_blocks;   // set by the launcher
 };
@@ -347,6 +349,7 @@ struct BackFinishArgs {
   int32_t n_heads, hd, c_s, c_z, bf16, ds_splits, w_splits;
   const float *ds_parts, *w_parts, *t, *w_b, *gamma;
   void *ds, *dw[4], *dw_b, *dgamma;  // null: not wanted
+  uint32_t sum_blocks;               // set by the launcher
 };
 
 size_t fast_proj_split_bytes(int32_t c_s);
