@@ -58,6 +58,12 @@ __device__ __forceinline__ f32x4 load_four(const void* p, int bf16, int vec, int
   return r;
 }
 
+// v_mfma_f32_16x16x4_f32: A holds row n, B column n (n = lane % 16), both at
+// k-slot g = lane / 16; the accumulator holds rows 4g..4g+3 of column n.
+__device__ __forceinline__ f32x4 mfma4(float a, float b, f32x4 c) {
+  return __builtin_amdgcn_mfma_f32_16x16x4f32(a, b, c, 0, 0, 0);
+}
+
 // Sum over the four lanes of a quad; each gets the same bits.
 __device__ __forceinline__ float quad_sum(float x) {
   x += __uint_as_float((uint32_t)__builtin_amdgcn_update_dpp(0, (int)__float_as_uint(x), 0xB1, 0xF, 0xF, true));
@@ -127,42 +133,42 @@ __global__ void __launch_bounds__(256) back_rows_kernel(BackRowsArgs a) {
 }
 
 // ----------------------------------------------------------------------------- pairs
-// A workgroup takes one query row and a range of keys, 64 at a time: four lanes
-// per key share its channels for the LayerNorm, the bias and dz, and its heads for
-// the logits and dS; T is then a sum over the tile's keys by output element. It
-// loops over such items, so that T is written once per workgroup. CT: pieces of 16 channels of z; NH:
+// A workgroup takes an equal share of the chunk's tiles, 64 keys of one query row each,
+// in row order. Four lanes per key share its channels for the LayerNorm, the bias
+// and dz, and its heads for the logits and dS; T is then a sum over the tile's keys
+// by output element, written once per workgroup. CT: pieces of 16 channels of z; NH:
 // heads per lane.
 constexpr int kBackKeys = 64;
 constexpr int kHeadStride = kGenMaxD + 4;
 
-// Four consecutive elements as loaded. vec: whole pieces, aligned; else one by one,
-// indices past the last repeating it.
+// Four consecutive elements from i0 of a row of len as loaded: whole pieces (len a
+// multiple of four, the row aligned) or one by one; past the end, the last ones again.
 template <bool BF16>
 struct Raw4 {
   uint32_t w[BF16 ? 2 : 4];
-  __device__ __forceinline__ void load(const void* p, int vec, int64_t row, int i0, int len) {
-    if (vec) {
-      const int at = min(i0, len - 4);
-      if constexpr (BF16) {
-        const u32x2 r = *reinterpret_cast<const u32x2*>(static_cast<const uint16_t*>(p) + row + at);
-        w[0] = r[0], w[1] = r[1];
-      } else {
-        const u32x4 r = *reinterpret_cast<const u32x4*>(static_cast<const float*>(p) + row + at);
-        w[0] = r[0], w[1] = r[1], w[2] = r[2], w[3] = r[3];
-      }
+  __device__ __forceinline__ void load(const void* p, int64_t row, int i0, int len) {
+    const int at = min(i0, len - 4);
+    if constexpr (BF16) {
+      const u32x2 r = *reinterpret_cast<const u32x2*>(static_cast<const uint16_t*>(p) + row + at);
+      w[0] = r[0], w[1] = r[1];
     } else {
-      uint32_t e[4];
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const int64_t x = row + min(i0 + i, len - 1);
-        e[i] = BF16 ? (uint32_t)static_cast<const uint16_t*>(p)[x] : static_cast<const uint32_t*>(p)[x];
-      }
-      if constexpr (BF16) {
-        w[0] = e[0] | (e[1] << 16), w[1] = e[2] | (e[3] << 16);
-      } else {
-        w[0] = e[0], w[1] = e[1], w[2] = e[2], w[3] = e[3];
-      }
+      const u32x4 r = *reinterpret_cast<const u32x4*>(static_cast<const float*>(p) + row + at);
+      w[0] = r[0], w[1] = r[1], w[2] = r[2], w[3] = r[3];
     }
+  }
+  __device__ __forceinline__ void load_each(const void* p, int64_t row, int i0, int len) {
+    uint32_t e[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int64_t x = row + min(i0 + i, len - 1);
+      e[i] = BF16 ? (uint32_t)static_cast<const uint16_t*>(p)[x] : static_cast<const uint32_t*>(p)[x];
+    }
+    if constexpr (BF16) {
+      w[0] = e[0] | (e[1] << 16), w[1] = e[2] | (e[3] << 16);
+    } else {
+      w[0] = e[0], w[1] = e[1], w[2] = e[2], w[3] = e[3];
+    }
+    __builtin_amdgcn_sched_barrier(0);  // (four addresses at a time)
   }
   __device__ __forceinline__ f32x4 get() const {
     if constexpr (BF16)
@@ -175,7 +181,7 @@ struct Raw4 {
 
 template <int CT, int NH, bool BF16>
 __global__ void __launch_bounds__(256, CT <= 8 && NH == 1 ? 3 : CT <= 8 ? 2 : 1) back_pairs_kernel(BackPairsArgs a) {
-  constexpr int CZ = 16 * CT, HP = 4 * NH, kGroups = 256 / CZ;  // key groups of the sum T
+  constexpr int CZ = 16 * CT, HP = 4 * NH;
   constexpr bool kHeld = CT * HP <= 8;  // W' of the lane's channels stays in registers
   __shared__ __attribute__((aligned(16))) float s_w[HP * CZ];
   __shared__ __attribute__((aligned(16))) float s_zh[kBackKeys * (CZ + 4)];
@@ -186,6 +192,7 @@ __global__ void __launch_bounds__(256, CT <= 8 && NH == 1 ? 3 : CT <= 8 ? 2 : 1)
   const int H = a.n_heads, d = a.head_dim, hd = H * d, c_z = a.c_z;
   const float inv_c = 1.0f / (float)c_z, scale = 1.0f / sqrtf((float)d);
   const int z_vec = c_z % 4 == 0;
+  const bool whole = c_z == CZ;
   for (int x = tid; x < HP * CZ; x += 256) {
     const int h = x / CZ, c = x % CZ;
     s_w[x] = h < H && c < c_z ? a.w_b[(int64_t)h * c_z + c] * (a.gamma ? a.gamma[c] : 1.0f) : 0.0f;
@@ -204,52 +211,60 @@ __global__ void __launch_bounds__(256, CT <= 8 && NH == 1 ? 3 : CT <= 8 ? 2 : 1)
     else
       return *reinterpret_cast<const f32x4*>(&s_w[h * CZ + 16 * m + 4 * qd]);
   };
-  const int tc = tid % CZ, tg = tid / CZ;  // T: this thread's channel and key group
-  float t_sum[HP];
+  const int lane = tid & 63, n = lane & 15, g = lane >> 4, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  constexpr int kTiles = (CT + 3) / 4;
+  f32x4 T[kTiles];
 #pragma unroll
-  for (int h = 0; h < HP; ++h) t_sum[h] = 0.0f;
-  const int64_t items = a.rows * a.n_parts;
-  const int64_t tiles = (a.n_tok + kBackKeys - 1) / kBackKeys;
-
-  for (int64_t item = blockIdx.x; item < items; item += gridDim.x) {
-    const int64_t r = item / a.n_parts;  // row of the stripe's chunk
-    const int part = (int)(item - r * a.n_parts);
-    const int64_t row = a.row0 + r;      // row of the stripe
-    int64_t t_count, t_first;
-    chunk_of(tiles, a.n_parts, part, &t_count, &t_first);
-    // z and the mask of a tile, keys past the last reading that one's
-    Raw4<BF16> raw[CT];
-    uint8_t attends = 1;
-    auto load_z = [&](int64_t t) {
-      const int64_t j = min(t * kBackKeys + key, a.n_tok - 1);
-      const int64_t off = (row * a.n_tok + j) * c_z;
-      if (a.mask) attends = a.mask[j];
-      int c = 4 * qd;
-      asm volatile("" : "+v"(c));  // (or the indices of the one-by-one loads would fill the registers)
+  for (int y = 0; y < kTiles; ++y) T[y] = f32x4{0.f, 0.f, 0.f, 0.f};
+  const int64_t tiles = (a.n_tok + kBackKeys - 1) / kBackKeys;  // of a row
+  int64_t share, begin;
+  chunk_of(a.rows * tiles, gridDim.x, blockIdx.x, &share, &begin);
+  int64_t r = begin / tiles, t_first = begin - r * tiles, left = share;  // row of the stripe's chunk, tile
+  // z and the mask of a tile, keys past the last reading that one's
+  Raw4<BF16> raw[CT];
+  uint8_t attends = 1;
+  auto load_z = [&](int64_t rr, int64_t t) {
+    const int64_t j = min(t * kBackKeys + key, a.n_tok - 1);
+    const int64_t off = ((a.row0 + rr) * a.n_tok + j) * c_z;
+    if (a.mask) attends = a.mask[j];
+    int c = 4 * qd;
+    asm volatile("" : "+v"(c));  // (or the indices of the one-by-one loads would fill the registers)
+    if (z_vec) {
 #pragma unroll
-      for (int m = 0; m < CT; ++m) raw[m].load(a.z, z_vec, off, 16 * m + c, c_z);
-    };
-    load_z(t_first);
-    __syncthreads();
-    for (int x = tid; x < hd; x += 256) {
+      for (int m = 0; m < CT; ++m) raw[m].load(a.z, off, 16 * m + c, c_z);
+    } else {
+#pragma unroll
+      for (int m = 0; m < CT; ++m) raw[m].load_each(a.z, off, 16 * m + c, c_z);
+    }
+  };
+  if (left > 0) load_z(r, t_first);
+  for (; left > 0; ++r, t_first = 0) {
+    const int64_t row = a.row0 + r;  // row of the stripe
+    const int64_t t_end = min(tiles, t_first + left);
+    left -= t_end - t_first;
+    int first = tid;
+    asm volatile("" : "+v"(first));  // (as above)
+    for (int x = first; x < hd; x += 256) {
       const int h = x / d, e = x - h * d;
       s_q[h * kHeadStride + e] = a.qp[((int64_t)h * a.n_q + row) * a.dp + e] * scale;
       s_do[h * kHeadStride + e] = a.dop[((int64_t)h * a.n_q + row) * a.dp + e];
     }
-    if (tid < HP) s_stat[tid] = *reinterpret_cast<const f32x4*>(a.stat + 4 * ((int64_t)min(tid, H - 1) * a.n_q + row));
+    if (first < HP) s_stat[first] = *reinterpret_cast<const f32x4*>(a.stat + 4 * ((int64_t)min(first, H - 1) * a.n_q + row));
     __syncthreads();
-    for (int64_t t = t_first; t < t_first + t_count; ++t) {
+    for (int64_t t = t_first; t < t_end; ++t) {
       asm volatile("" ::: "memory");  // q, do and W' come from LDS again for each tile, not from registers
       const int64_t j = t * kBackKeys + key, jj = min(j, a.n_tok - 1);
       const bool there = j < a.n_tok, valid = there && attends != 0;
       f32x4 zh[CT];
       float s = 0.0f, v = 0.0f;
+      int c4 = 4 * qd;
+      asm volatile("" : "+v"(c4));  // (as above)
 #pragma unroll
       for (int m = 0; m < CT; ++m) {
-        const int c = 16 * m + 4 * qd;
+        const int c = 16 * m + c4;
         zh[m] = raw[m].get();
 #pragma unroll
-        for (int i = 0; i < 4; ++i) zh[m][i] = valid && c + i < c_z ? zh[m][i] : 0.0f;
+        for (int i = 0; i < 4; ++i) zh[m][i] = valid && (whole || c + i < c_z) ? zh[m][i] : 0.0f;
         s += (zh[m][0] + zh[m][1]) + (zh[m][2] + zh[m][3]);
       }
       const float mu = quad_sum(s) * inv_c;
@@ -257,14 +272,13 @@ __global__ void __launch_bounds__(256, CT <= 8 && NH == 1 ? 3 : CT <= 8 ? 2 : 1)
       for (int m = 0; m < CT; ++m)
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          zh[m][i] = 16 * m + 4 * qd + i < c_z ? zh[m][i] - mu : 0.0f;
+          zh[m][i] = whole || 16 * m + c4 + i < c_z ? zh[m][i] - mu : 0.0f;
           v = fmaf(zh[m][i], zh[m][i], v);
         }
       const float rstd = valid ? 1.0f / sqrtf(fmaf(quad_sum(v), inv_c, a.eps)) : 0.0f;
 #pragma unroll
       for (int m = 0; m < CT; ++m) {
-        zh[m] *= rstd;
-        if (!valid) zh[m] = f32x4{0.f, 0.f, 0.f, 0.f};
+        zh[m] *= rstd;  // 0 for a key that does not attend, whose mean is 0 too
         *reinterpret_cast<f32x4*>(&s_zh[key * (CZ + 4) + 16 * m + 4 * qd]) = zh[m];
       }
 #pragma unroll
@@ -319,7 +333,10 @@ __global__ void __launch_bounds__(256, CT <= 8 && NH == 1 ? 3 : CT <= 8 ? 2 : 1)
         }
       }
       // in flight during dz and T, and behind k and v, which wait for nothing else
-      if (t + 1 < t_first + t_count) load_z(t + 1);
+      if (t + 1 < t_end)
+        load_z(r, t + 1);
+      else if (left > 0)
+        load_z(r + 1, 0);
       __syncthreads();
       if (a.dz && there) {
         int at = key;
@@ -352,7 +369,7 @@ __global__ void __launch_bounds__(256, CT <= 8 && NH == 1 ? 3 : CT <= 8 ? 2 : 1)
         s2 = quad_sum(s2) * inv_c;
 #pragma unroll
         for (int m = 0; m < CT; ++m) {
-          const int c = 16 * m + 4 * qd;
+          const int c = 16 * m + c4;
           f32x4 g;
 #pragma unroll
           for (int e = 0; e < 4; ++e) g[e] = valid ? rstd * (acc[m][e] - s1 - zh[m][e] * s2) : 0.0f;
@@ -374,33 +391,26 @@ __global__ void __launch_bounds__(256, CT <= 8 && NH == 1 ? 3 : CT <= 8 ? 2 : 1)
           }
         }
       }
+      // T += dS^T zh: heads by 16 channels, four keys a step; wave w takes tiles w, w + 4, ..
 #pragma unroll 4
-      for (int x = tg; x < kBackKeys; x += kGroups) {
-        const float zc = s_zh[x * (CZ + 4) + tc];
+      for (int x = 0; x < kBackKeys; x += 4) {
+        const float ds = n < HP ? s_ds[(x + g) * (HP + 4) + n] : 0.0f;
 #pragma unroll
-        for (int i = 0; i < NH; ++i) {
-          const f32x4 ds = *reinterpret_cast<const f32x4*>(&s_ds[x * (HP + 4) + 4 * i]);
-#pragma unroll
-          for (int e = 0; e < 4; ++e) t_sum[4 * i + e] = fmaf(ds[e], zc, t_sum[4 * i + e]);
-        }
+        for (int y = 0; y < kTiles; ++y)
+          if (CT >= 4 || wave < CT) T[y] = mfma4(ds, s_zh[(x + g) * (CZ + 4) + 16 * (wave + 4 * y) + n], T[y]);
       }
       __syncthreads();
     }
   }
-  // T of this workgroup: its key groups in order, added to what earlier chunks left
-  __syncthreads();
+  // T of this workgroup, added to what earlier chunks left
   float* out = a.t_parts + (int64_t)blockIdx.x * H * c_z;
-  for (int g = 0; g < kGroups; ++g) {
-    if (tg == g && tc < c_z)
 #pragma unroll
-      for (int h = 0; h < HP; ++h)
-        if (h < H) s_zh[h * CZ + tc] = g == 0 ? t_sum[h] : s_zh[h * CZ + tc] + t_sum[h];
-    __syncthreads();
-  }
-  for (int x = tid; x < H * c_z; x += 256) {
-    const float v = s_zh[(x / c_z) * CZ + x % c_z];
-    out[x] = a.first ? v : out[x] + v;
-  }
+  for (int y = 0; y < kTiles; ++y)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int h = 4 * g + i, c = 16 * (wave + 4 * y) + n;
+      if (h < H && c < c_z) out[h * c_z + c] = a.first ? T[y][i] : out[h * c_z + c] + T[y][i];
+    }
 }
 
 // ----------------------------------------------------------------------------- keys
@@ -409,12 +419,6 @@ __global__ void __launch_bounds__(256, CT <= 8 && NH == 1 ? 3 : CT <= 8 ? 2 : 1)
 // 16 rows a step. Blocks of rows: dq of 16 rows over all keys, 16 keys a step, every
 // fourth step a wave. A step's loads are all in flight at once; past the last row or
 // key they repeat that one, with a P and dS of 0.
-// v_mfma_f32_16x16x4_f32: A holds row n, B column n (n = lane % 16), both at
-// k-slot g = lane / 16; the accumulator holds rows 4g..4g+3 of column n.
-__device__ __forceinline__ f32x4 mfma4(float a, float b, f32x4 c) {
-  return __builtin_amdgcn_mfma_f32_16x16x4f32(a, b, c, 0, 0, 0);
-}
-
 template <int DP>
 __device__ __forceinline__ void row_sums(const BackKeysArgs& a, int h, int64_t r0, f32x4 (&s_sum)[4][DP / 16][64]) {
   constexpr int U = DP / 16;
@@ -554,8 +558,8 @@ __global__ void __launch_bounds__(256) back_sum_kernel(BackSumArgs a) {
 // ----------------------------------------------------------------------------- token products
 // ds = sum over x of dx W_x (64 tokens by 64 channels per workgroup) and dW_x = dx^T s
 // (64 outputs by 64 channels), on the fp32 matrix cores: a workgroup's four waves
-// take 32 x 32 each, operands 16 deep through LDS, the next 16 in flight.
-constexpr int kGemm = 64, kDeep = 16, kGemmStride = kGemm + 16;
+// take 32 x 32 each, operands 32 deep through LDS, the next 32 in flight.
+constexpr int kGemm = 64, kDeep = 32, kGemmStride = kGemm + 16;
 
 __global__ void __launch_bounds__(256) back_gemm_kernel(BackGemmArgs a) {
   __shared__ __attribute__((aligned(16))) float s_a[2][kDeep][kGemmStride], s_b[2][kDeep][kGemmStride];
@@ -582,36 +586,42 @@ __global__ void __launch_bounds__(256) back_gemm_kernel(BackGemmArgs a) {
   int64_t steps, first;
   chunk_of(depth / kDeep, splits, split, &steps, &first);
   const int hd_vec = a.hd % 4 == 0, s_vec = a.c_s % 4 == 0;
-  const int r16 = tid >> 4, x4 = (tid & 15) * 4;  // 16 deep by 64 wide, four a thread
-  f32x4 av, bv;
+  const int r16 = tid >> 4, x4 = (tid & 15) * 4;  // 16 deep by 64 wide, four a thread, twice
+  f32x4 av[2], bv[2];
+  const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
   auto fetch = [&](int64_t step) {
-    const int64_t k0 = step * kDeep;
-    if (is_ds) {
-      const int term = (int)(k0 / hd_deep), o = (int)(k0 % hd_deep);
-      const float* x = term == 0 ? a.dk : term == 1 ? a.dv : term == 2 ? a.dq : a.dg;
-      const float* w = term == 0 ? a.w_k : term == 1 ? a.w_v : term == 2 ? a.w_q : a.w_g;
-      // A: token tid / 4, outputs o + 4 (tid % 4) ..
-      const int64_t row = m0 + (tid >> 2) - (term >= 2 ? a.q_row0 : 0), rows = term >= 2 ? a.n_q : a.n_tok;
-      av = row >= 0 && row < rows ? load_four(x, 0, hd_vec, row * a.hd, o + 4 * (tid & 3), a.hd) : f32x4{0.f, 0.f, 0.f, 0.f};
-      bv = o + r16 < a.hd ? load_four(w, 0, s_vec && a.w_vec, (int64_t)(o + r16) * a.c_s, c0 + x4, a.c_s)
-                          : f32x4{0.f, 0.f, 0.f, 0.f};
-    } else {
-      const int64_t t = k0 + r16;
-      const bool in = t < w_rows;
-      av = in ? load_four(dx, 0, hd_vec, t * a.hd, o0 + x4, a.hd) : f32x4{0.f, 0.f, 0.f, 0.f};
-      // a masked token's s does not enter the gradients of W_k and W_v
-      const bool used = in && (stripe || !a.mask || a.mask[t] != 0);
-      bv = used ? load_four(a.s, a.s_bf16, s_vec, (s_row0 + t) * a.c_s, c0 + x4, a.c_s) : f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      if (is_ds) {
+        const int64_t k0 = step * kDeep;
+        const int term = (int)(k0 / hd_deep), o = (int)(k0 % hd_deep) + 16 * u;
+        const float* x = term == 0 ? a.dk : term == 1 ? a.dv : term == 2 ? a.dq : a.dg;
+        const float* w = term == 0 ? a.w_k : term == 1 ? a.w_v : term == 2 ? a.w_q : a.w_g;
+        // A: token tid / 4, outputs o + 4 (tid % 4) ..
+        const int64_t row = m0 + (tid >> 2) - (term >= 2 ? a.q_row0 : 0), rows = term >= 2 ? a.n_q : a.n_tok;
+        av[u] = row >= 0 && row < rows ? load_four(x, 0, hd_vec, row * a.hd, o + 4 * (tid & 3), a.hd) : zero;
+        bv[u] = o + r16 < a.hd ? load_four(w, 0, s_vec && a.w_vec, (int64_t)(o + r16) * a.c_s, c0 + x4, a.c_s) : zero;
+      } else {
+        const int64_t t = step * kDeep + 16 * u + r16;
+        const bool in = t < w_rows;
+        av[u] = in ? load_four(dx, 0, hd_vec, t * a.hd, o0 + x4, a.hd) : zero;
+        // a masked token's s does not enter the gradients of W_k and W_v
+        const bool used = in && (stripe || !a.mask || a.mask[t] != 0);
+        bv[u] = used ? load_four(a.s, a.s_bf16, s_vec, (s_row0 + t) * a.c_s, c0 + x4, a.c_s) : zero;
+      }
     }
   };
   auto stage = [&](int buf) {
-    if (is_ds) {
 #pragma unroll
-      for (int i = 0; i < 4; ++i) s_a[buf][4 * (tid & 3) + i][tid >> 2] = av[i];
-    } else {
-      *reinterpret_cast<f32x4*>(&s_a[buf][r16][x4]) = av;
+    for (int u = 0; u < 2; ++u) {
+      if (is_ds) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) s_a[buf][16 * u + 4 * (tid & 3) + i][tid >> 2] = av[u][i];
+      } else {
+        *reinterpret_cast<f32x4*>(&s_a[buf][16 * u + r16][x4]) = av[u];
+      }
+      *reinterpret_cast<f32x4*>(&s_b[buf][16 * u + r16][x4]) = bv[u];
     }
-    *reinterpret_cast<f32x4*>(&s_b[buf][r16][x4]) = bv;
   };
   f32x4 acc[2][2];
 #pragma unroll
@@ -731,9 +741,9 @@ hipError_t launch_back_rows(const BackRowsArgs& a, hipStream_t st) {
   return hipGetLastError();
 }
 
-int back_pairs_groups(int64_t rows, int n_parts) {
-  const int64_t items = rows * n_parts;
-  return (int)(items < kBackMaxGroups ? items : kBackMaxGroups);
+int back_pairs_groups(int64_t rows, int64_t n_tok) {
+  const int64_t tiles = rows * ((n_tok + kBackKeys - 1) / kBackKeys);
+  return (int)(tiles < kBackMaxGroups ? tiles : kBackMaxGroups);
 }
 
 hipError_t launch_back_pairs(const BackPairsArgs& a, int groups, hipStream_t st) {

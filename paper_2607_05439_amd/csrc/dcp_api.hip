@@ -1195,11 +1195,7 @@ void back_layout(const dcp_shape* sh, Path path, int64_t n_q, BackLayout* L) {
     L->chunk = (int64_t)(kBackGenBytes / ((size_t)2 * H * N * 4));
     if (L->chunk < 1) L->chunk = 1;
     if (L->chunk > n_q) L->chunk = n_q;
-    // at least three items (a row's part of the keys) for each of the workgroups that
-    // loop over them, so that no CU waits long for the last
-    const int64_t parts = 3 * dcp::kBackMaxGroups / L->chunk;
-    L->dq_parts = (int)(parts < 1 ? 1 : parts > key_groups ? key_groups : parts);
-    L->t_parts = dcp::back_pairs_groups(L->chunk, L->dq_parts);
+    L->t_parts = dcp::back_pairs_groups(L->chunk, N);
     L->off_qp = take((size_t)H * n_q * L->dp * 4);
     L->off_dop = take((size_t)H * n_q * L->dp * 4);
     L->off_kp = take((size_t)H * N * L->dp * 4);
@@ -1212,7 +1208,7 @@ void back_layout(const dcp_shape* sh, Path path, int64_t n_q, BackLayout* L) {
   }
   if (splits > most) splits = most;
   L->kv_splits = (int)(splits < 1 ? 1 : splits > 16 ? 16 : splits);
-  dcp::back_gemm_splits(N, (int32_t)hd, sh->c_s, path == kPathFast ? 256 : 128, &L->ds_splits, &L->w_splits);
+  dcp::back_gemm_splits(N, (int32_t)hd, sh->c_s, path == kPathFast ? 256 : 64, &L->ds_splits, &L->w_splits);
   L->off_dq_parts = path == kPathFast ? take((size_t)L->dq_parts * n_q * hd * 4) : 0;
   L->off_t_parts = take((size_t)L->t_parts * H * sh->c_z * 4);
   L->off_kv_parts = take((size_t)L->kv_splits * 2 * N * hd * 4);
@@ -1433,14 +1429,13 @@ int dcp_pair_bias_attention_backward(const dcp_shape* shape, const dcp_weights* 
       ba.n_heads = shape->n_heads;
       ba.head_dim = shape->head_dim;
       ba.dp = L.dp;
-      ba.n_parts = L.dq_parts;
       ba.first = row == 0;
       ba.eps = shape->ln_eps;
       ba.p = at(L.off_p);
       ba.ds = at(L.off_ds);
       ba.dz = grads->dz_rows;
       ba.t_parts = t_parts;
-      if ((e = dcp::launch_back_pairs(ba, dcp::back_pairs_groups(rows, L.dq_parts), st)) != hipSuccess)
+      if ((e = dcp::launch_back_pairs(ba, dcp::back_pairs_groups(rows, N), st)) != hipSuccess)
         return fail(DCP_ERR_HIP, "pair gradient launch failed: %s", hipGetErrorString(e));
       dcp::BackKeysArgs ka{};
       ka.p = ba.p;

@@ -278,7 +278,7 @@ struct BackPairsArgs {
   const float *k, *v;      // [H][N][dp]
   const float *qp, *dop, *stat;
   int64_t n_tok, n_q, row0, rows;  // rows [row0, row0 + rows) of the stripe
-  int32_t c_z, n_heads, head_dim, dp, n_parts, first;
+  int32_t c_z, n_heads, head_dim, dp, first;
   float eps;
   float *p, *ds;           // [H][rows][N]
   void* dz;                // as z, or null
@@ -374,7 +374,7 @@ hipError_t launch_layer_norm(const LayerNormArgs& a, bool x_bf16, bool y_bf16, h
 int layer_norm_back_groups(int64_t n_rows, int32_t c);  // workgroups, one partial sum each
 hipError_t launch_layer_norm_back(const LayerNormBackArgs& a, bool x_bf16, bool dy_bf16, hipStream_t st);
 hipError_t launch_back_rows(const BackRowsArgs& a, hipStream_t st);
-int back_pairs_groups(int64_t rows, int n_parts);
+int back_pairs_groups(int64_t rows, int64_t n_tok);
 hipError_t launch_back_pairs(const BackPairsArgs& a, int groups, hipStream_t st);
 hipError_t launch_back_keys(const BackKeysArgs& a, int dp, hipStream_t st);
 hipError_t launch_fast_back_prep(const FastBackArgs& a, hipStream_t st);
