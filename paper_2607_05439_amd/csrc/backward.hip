@@ -522,24 +522,33 @@ __global__ void __launch_bounds__(256) back_keys_kernel(BackKeysArgs a) {
 }
 
 // ----------------------------------------------------------------------------- sums of parts
-// dq, dk and dv: one thread per element, parts in order. T: 16 columns by 16 groups
-// of parts per workgroup.
+// dq, dk and dv: W elements a thread (4 where H d is a multiple of that), parts in
+// order. T: 16 columns by 16 groups of parts per workgroup.
+template <int W>
+__device__ __forceinline__ void sum_parts(const float* parts, int n, int64_t stride, float* out) {
+  f32x4 v = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 4
+  for (int p = 0; p < n; ++p) {
+    if constexpr (W == 4)
+      v += *reinterpret_cast<const f32x4*>(parts + p * stride);
+    else
+      v[0] += parts[p * stride];
+  }
+  if constexpr (W == 4)
+    *reinterpret_cast<f32x4*>(out) = v;
+  else
+    *out = v[0];
+}
+template <int W>
 __global__ void __launch_bounds__(256) back_sum_kernel(BackSumArgs a) {
   __shared__ float s[16][17];
   const int64_t n_dq = a.dq_parts ? a.n_q * a.hd : 0, n_kv = 2 * a.n_tok * a.hd;
   if (blockIdx.x < a.token_blocks) {
-    const int64_t x = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    if (x < n_dq) {
-      float v = 0.0f;
-#pragma unroll 4
-      for (int p = 0; p < a.dq_n; ++p) v += a.dq_parts[p * n_dq + x];
-      a.dq[x] = v;
-    } else if (x < n_dq + n_kv) {
-      float v = 0.0f;
-#pragma unroll 4
-      for (int p = 0; p < a.kv_n; ++p) v += a.kv_parts[p * n_kv + x - n_dq];
-      a.dkv[x - n_dq] = v;
-    }
+    const int64_t x = ((int64_t)blockIdx.x * 256 + threadIdx.x) * W;
+    if (x < n_dq)
+      sum_parts<W>(a.dq_parts + x, a.dq_n, n_dq, a.dq + x);
+    else if (x < n_dq + n_kv)
+      sum_parts<W>(a.kv_parts + x - n_dq, a.kv_n, n_kv, a.dkv + x - n_dq);
     return;
   }
   const int cols = a.t_cols, col = (int)(blockIdx.x - a.token_blocks) * 16 + (threadIdx.x & 15), grp = threadIdx.x >> 4;
@@ -768,8 +777,14 @@ hipError_t launch_back_keys(const BackKeysArgs& a, int dp, hipStream_t st) {
 
 hipError_t launch_back_sum(const BackSumArgs& a, hipStream_t st) {
   BackSumArgs b = a;
-  b.token_blocks = blocks_of((a.dq_parts ? a.n_q * a.hd : 0) + 2 * a.n_tok * a.hd);
-  hipLaunchKernelGGL(back_sum_kernel, dim3(b.token_blocks + (unsigned)((a.t_cols + 15) / 16)), dim3(256), 0, st, b);
+  const int64_t n = (a.dq_parts ? a.n_q * a.hd : 0) + 2 * a.n_tok * a.hd;
+  const bool four = a.hd % 4 == 0;
+  b.token_blocks = blocks_of(four ? n / 4 : n);
+  const dim3 grid(b.token_blocks + (unsigned)((a.t_cols + 15) / 16));
+  if (four)
+    hipLaunchKernelGGL(back_sum_kernel<4>, grid, dim3(256), 0, st, b);
+  else
+    hipLaunchKernelGGL(back_sum_kernel<1>, grid, dim3(256), 0, st, b);
   return hipGetLastError();
 }
 

@@ -8,13 +8,15 @@
 // times the fp32 matrix rate. bf16 has fp32's range, so nothing is scaled.
 //
 // A workgroup of four waves takes 64 x 64 outputs, 32 x 32 a wave; operands 32 deep go
-// through LDS in two buffers, the next in flight in registers. An operand whose
+// through LDS in two buffers, the next two steps in flight in registers. An operand whose
 // depth runs along its rows lies in LDS by rows of 32 (16-byte pieces XOR-swizzled by
 // row); one whose depth runs across them lies as it came, and is read with the
 // transposing LDS read, which hands lane i of 16 column i of four rows.
 #include <hip/hip_runtime.h>
 #include <math.h>
 #include <stdint.h>
+
+#include <type_traits>
 
 #include "cdna4.h"
 #include "dcp_internal.h"
@@ -94,28 +96,28 @@ __device__ __forceinline__ bf16x8 operand(const Side& s, int r0, int lane) {
   }
 }
 
-// acc += A B over `steps` steps of 32; fetch(step, a, b) loads a thread's pieces.
+// acc += A B over `steps` steps of 32; fetch(step, a, b) loads a thread's pieces, two
+// steps ahead of their use.
 template <bool A_ALONG, bool A_SPLIT, bool B_ALONG, bool B_SPLIT, typename Fetch>
 __device__ __forceinline__ void product(GemmLds& s, int64_t steps, Fetch fetch, f32x4 (&acc)[2][2]) {
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int am = 32 * (wave >> 1), bn = 32 * (wave & 1);
-  Eight a, b;
-  if (steps > 0) {
-    fetch(0, a, b);
-    stage<A_ALONG, A_SPLIT>(s.a[0], a, tid);
-    stage<B_ALONG, B_SPLIT>(s.b[0], b, tid);
-  }
-  for (int64_t i = 0; i < steps; ++i) {
-    const int buf = (int)(i & 1);
+  Eight a[2], b[2];
+  auto put = [&](auto buf) {
+    stage<A_ALONG, A_SPLIT>(s.a[buf], a[buf], tid);
+    stage<B_ALONG, B_SPLIT>(s.b[buf], b[buf], tid);
+  };
+  auto step = [&](int64_t i, auto buf) {
+    constexpr int kBuf = decltype(buf)::value;
     __syncthreads();  // the buffer is staged, and the other one read
-    if (i + 1 < steps) fetch(i + 1, a, b);
+    if (i + 2 < steps) fetch(i + 2, a[kBuf], b[kBuf]);
     bf16x8 ah[2], al[2], bh[2], bl[2];
 #pragma unroll
     for (int u = 0; u < 2; ++u) {
-      ah[u] = operand<A_ALONG>(s.a[buf][0], am + 16 * u, lane);
-      bh[u] = operand<B_ALONG>(s.b[buf][0], bn + 16 * u, lane);
-      if constexpr (A_SPLIT) al[u] = operand<A_ALONG>(s.a[buf][1], am + 16 * u, lane);
-      if constexpr (B_SPLIT) bl[u] = operand<B_ALONG>(s.b[buf][1], bn + 16 * u, lane);
+      ah[u] = operand<A_ALONG>(s.a[kBuf][0], am + 16 * u, lane);
+      bh[u] = operand<B_ALONG>(s.b[kBuf][0], bn + 16 * u, lane);
+      if constexpr (A_SPLIT) al[u] = operand<A_ALONG>(s.a[kBuf][1], am + 16 * u, lane);
+      if constexpr (B_SPLIT) bl[u] = operand<B_ALONG>(s.b[kBuf][1], bn + 16 * u, lane);
     }
 #pragma unroll
     for (int u = 0; u < 2; ++u)
@@ -125,10 +127,16 @@ __device__ __forceinline__ void product(GemmLds& s, int64_t steps, Fetch fetch, 
         if constexpr (B_SPLIT) acc[u][w] = mfma32(ah[u], bl[w], acc[u][w]);
         if constexpr (A_SPLIT) acc[u][w] = mfma32(al[u], bh[w], acc[u][w]);
       }
-    if (i + 1 < steps) {
-      stage<A_ALONG, A_SPLIT>(s.a[buf ^ 1], a, tid);
-      stage<B_ALONG, B_SPLIT>(s.b[buf ^ 1], b, tid);
-    }
+    if (i + 1 < steps) put(std::integral_constant<int, 1 - kBuf>());
+  };
+  const std::integral_constant<int, 0> even;
+  const std::integral_constant<int, 1> odd;
+  if (steps > 0) fetch(0, a[0], b[0]);
+  if (steps > 1) fetch(1, a[1], b[1]);
+  if (steps > 0) put(even);
+  for (int64_t i = 0; i < steps; i += 2) {
+    step(i, even);
+    if (i + 1 < steps) step(i + 1, odd);
   }
 }
 
