@@ -525,19 +525,27 @@ __global__ void __launch_bounds__(256) back_keys_kernel(BackKeysArgs a) {
 // dq, dk and dv: W elements a thread (4 where H d is a multiple of that), parts in
 // order. T: 16 columns by 16 groups of parts per workgroup.
 template <int W>
-__device__ __forceinline__ void sum_parts(const float* parts, int n, int64_t stride, float* out) {
+__device__ __forceinline__ void sum_parts(const float* parts, int n, int64_t stride, float* out, int64_t x, int split) {
   f32x4 v = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll 4
   for (int p = 0; p < n; ++p) {
     if constexpr (W == 4)
-      v += *reinterpret_cast<const f32x4*>(parts + p * stride);
+      v += *reinterpret_cast<const f32x4*>(parts + p * stride + x);
     else
-      v[0] += parts[p * stride];
+      v[0] += parts[p * stride + x];
   }
-  if constexpr (W == 4)
-    *reinterpret_cast<f32x4*>(out) = v;
-  else
-    *out = v[0];
+  if constexpr (W == 4) {
+    if (split) {
+      u32x2 hi, lo;
+      split4(v, hi, lo);
+      *reinterpret_cast<u32x2*>(reinterpret_cast<uint16_t*>(out) + x) = hi;
+      *reinterpret_cast<u32x2*>(reinterpret_cast<uint16_t*>(out) + stride + x) = lo;
+      return;
+    }
+    *reinterpret_cast<f32x4*>(out + x) = v;
+  } else {
+    out[x] = v[0];
+  }
 }
 template <int W>
 __global__ void __launch_bounds__(256) back_sum_kernel(BackSumArgs a) {
@@ -546,9 +554,9 @@ __global__ void __launch_bounds__(256) back_sum_kernel(BackSumArgs a) {
   if (blockIdx.x < a.token_blocks) {
     const int64_t x = ((int64_t)blockIdx.x * 256 + threadIdx.x) * W;
     if (x < n_dq)
-      sum_parts<W>(a.dq_parts + x, a.dq_n, n_dq, a.dq + x);
+      sum_parts<W>(a.dq_parts, a.dq_n, n_dq, a.dq, x, a.split);
     else if (x < n_dq + n_kv)
-      sum_parts<W>(a.kv_parts + x - n_dq, a.kv_n, n_kv, a.dkv + x - n_dq);
+      sum_parts<W>(a.kv_parts, a.kv_n, n_kv, a.dkv, x - n_dq, a.split);
     return;
   }
   const int cols = a.t_cols, col = (int)(blockIdx.x - a.token_blocks) * 16 + (threadIdx.x & 15), grp = threadIdx.x >> 4;

@@ -61,10 +61,22 @@ __device__ __forceinline__ int scale_exp(float top) {
 }
 
 // ----------------------------------------------------------------------------- weights, dout
-// Block 0: the weights. Blocks 1 .. kBackTops: the largest |dout| of a share each.
+// Block 0: the bias weights. Blocks 1 .. kBackTops: the largest |dout| of a share each.
+// The others: the projections' weights split into bf16 hi + lo, four a thread.
 __global__ void __launch_bounds__(256) prep_kernel(FastBackArgs a) {
   const int tid = threadIdx.x, lane = tid & 63;
   __shared__ float s_top[4];
+  if (blockIdx.x > kBackTops) {
+    const int64_t n = (int64_t)kHD * a.c_s, x = ((int64_t)(blockIdx.x - 1 - kBackTops) * 256 + tid) * 4;
+    if (x >= 4 * n) return;
+    const int mat = (x >= n) + (x >= 2 * n) + (x >= 3 * n);
+    const float* w = mat == 0 ? a.w[0] : mat == 1 ? a.w[1] : mat == 2 ? a.w[2] : a.w[3];
+    u32x2 hi, lo;
+    split4(*reinterpret_cast<const f32x4*>(w + x - mat * n), hi, lo);
+    *reinterpret_cast<u32x2*>(a.w_split + x) = hi;
+    *reinterpret_cast<u32x2*>(a.w_split + 4 * n + x) = lo;
+    return;
+  }
   if (blockIdx.x > 0) {
     const int64_t n8 = a.n_q * kHD / 8;  // 16-byte pieces of bf16, pairs of them of fp32
     float top = 0.0f;
@@ -212,7 +224,10 @@ __global__ void __launch_bounds__(64) pack_kernel(FastBackArgs a) {
           dot = fmaf(d, o, dot);
           dg[i] = up[i] * o * gt[i] * (1.0f - gt[i]);
         }
-        *reinterpret_cast<f32x4*>(a.dg + at + e) = dg;
+        u32x2 hi, lo;
+        split4(dg, hi, lo);
+        *reinterpret_cast<u32x2*>(a.dg + at + e) = hi;
+        *reinterpret_cast<u32x2*>(a.dg + a.n_q * kHD + at + e) = lo;
       }
     }
     a.lse[(int64_t)h * a.nq_pad + row] = lse;
@@ -564,7 +579,8 @@ __global__ void __launch_bounds__(256) keys_kernel(FastBackArgs a) {
 }  // namespace
 
 hipError_t launch_fast_back_prep(const FastBackArgs& a, hipStream_t st) {
-  hipLaunchKernelGGL(prep_kernel, dim3(1 + kBackTops), dim3(256), 0, st, a);
+  const unsigned split_blocks = (unsigned)((4 * (int64_t)kHD * a.c_s / 4 + 255) / 256);
+  hipLaunchKernelGGL(prep_kernel, dim3(1 + kBackTops + split_blocks), dim3(256), 0, st, a);
   return hipGetLastError();
 }
 

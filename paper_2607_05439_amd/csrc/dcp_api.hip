@@ -1132,7 +1132,7 @@ struct BackLayout {
   int dp, dq_parts, t_parts, kv_splits, ds_splits, w_splits;
   // projections, general and fused rows' operands, fused keys' operands
   size_t off_q, off_k, off_v, off_g, off_qp, off_dop, off_kp, off_vp, off_stat, off_qf, off_qt, off_of, off_ot, off_lse, off_dot, off_kf,
-      off_kt, off_vf, off_tv, off_tops, off_exps, off_wops;
+      off_kt, off_vf, off_tv, off_tops, off_exps, off_wops, off_wsplit;
   size_t off_p, off_ds, off_dq_parts, off_t_parts, off_kv_parts, off_dq, off_dkv, off_dg, off_t, off_ds_parts, off_w_parts,
       total;
 };
@@ -1187,6 +1187,7 @@ void back_layout(const dcp_shape* sh, Path path, int64_t n_q, BackLayout* L) {
     L->off_tops = take(4 * dcp::kBackTops * 4);
     L->off_exps = take(5 * 4);
     L->off_wops = take(768 * 16);
+    L->off_wsplit = take((size_t)4 * hd * sh->c_s * 4);
     L->off_p = take((size_t)groups * per_tile);
     splits = 512 / (key_groups * H);
     most = groups / 8;
@@ -1304,24 +1305,8 @@ int dcp_pair_bias_attention_backward(const dcp_shape* shape, const dcp_weights* 
     return ok();
   }
 
-  dcp::GenProjArgs pa{};
-  pa.s = s;
-  pa.s_bf16 = act_bf16;
-  pa.w_q = w->w_q;
-  pa.w_k = w->w_k;
-  pa.w_v = w->w_v;
-  pa.w_g = w->w_g;
-  pa.n_tok = N;
-  pa.q_row0 = q_row0;
-  pa.n_q = n_q;
-  pa.c_s = shape->c_s;
-  pa.hd = hd;
-  pa.mask = key_mask;
-  pa.q = at(L.off_q);
-  pa.k = at(L.off_k);
-  pa.v = at(L.off_v);
-  pa.g = at(L.off_g);
   float *dg = at(L.off_dg), *dq_parts = at(L.off_dq_parts), *t_parts = at(L.off_t_parts), *kv_parts = at(L.off_kv_parts);
+  dcp::TokenArgs ta{};
   if (path == kPathFast) {
     auto half = [&](size_t off) { return reinterpret_cast<uint16_t*>(ws + off); };
     dcp::FastBackArgs ba{};
@@ -1329,10 +1314,10 @@ int dcp_pair_bias_attention_backward(const dcp_shape* shape, const dcp_weights* 
     ba.mask = key_mask;
     ba.w_b = w->w_b;
     ba.gamma = w->ln_gamma;
-    ba.q = pa.q;
-    ba.g = pa.g;
-    ba.k = pa.k;
-    ba.v = pa.v;
+    ba.q = at(L.off_q);
+    ba.g = at(L.off_g);
+    ba.k = at(L.off_k);
+    ba.v = at(L.off_v);
     ba.m = m;
     ba.l = l;
     ba.acc = acc;
@@ -1354,7 +1339,13 @@ int dcp_pair_bias_attention_backward(const dcp_shape* shape, const dcp_weights* 
     ba.vf = half(L.off_vf);
     ba.lse = at(L.off_lse);
     ba.dot = at(L.off_dot);
-    ba.dg = dg;
+    ba.w[0] = w->w_q;
+    ba.w[1] = w->w_k;
+    ba.w[2] = w->w_v;
+    ba.w[3] = w->w_g;
+    ba.c_s = shape->c_s;
+    ba.w_split = half(L.off_wsplit);
+    ba.dg = half(L.off_dg);
     ba.tile_valid = reinterpret_cast<uint32_t*>(ws + L.off_tv);
     ba.eps = shape->ln_eps;
     ba.chunk_pad = L.chunk;
@@ -1365,10 +1356,26 @@ int dcp_pair_bias_attention_backward(const dcp_shape* shape, const dcp_weights* 
     ba.dq_parts = dq_parts;
     ba.t_parts = t_parts;
     ba.kv_parts = kv_parts;
-    pa.tops = ba.tops;
+    ta.n_tok = N;
+    ta.q_row0 = q_row0;
+    ta.n_q = n_q;
+    ta.c_s = shape->c_s;
+    ta.s = static_cast<const uint16_t*>(s);
+    ta.mask = key_mask;
+    ta.w = ba.w_split;
+    ta.q = at(L.off_q);
+    ta.k = at(L.off_k);
+    ta.v = at(L.off_v);
+    ta.g = at(L.off_g);
+    ta.tops = ba.tops;
+    ta.dq = half(L.off_dq);
+    ta.dg = ba.dg;
+    ta.dkv = half(L.off_dkv);
+    ta.ds_splits = L.ds_splits;
+    ta.w_splits = L.w_splits;
     if ((e = dcp::launch_fast_back_prep(ba, st)) != hipSuccess)
       return fail(DCP_ERR_HIP, "gradient preparation launch failed: %s", hipGetErrorString(e));
-    if ((e = dcp::launch_token_proj(pa, st)) != hipSuccess)
+    if ((e = dcp::launch_token_proj(ta, st)) != hipSuccess)
       return fail(DCP_ERR_HIP, "projection launch failed: %s", hipGetErrorString(e));
     if ((e = dcp::launch_fast_back_pack(ba, st)) != hipSuccess)
       return fail(DCP_ERR_HIP, "operand launch failed: %s", hipGetErrorString(e));
@@ -1381,6 +1388,23 @@ int dcp_pair_bias_attention_backward(const dcp_shape* shape, const dcp_weights* 
         return fail(DCP_ERR_HIP, "key gradient launch failed: %s", hipGetErrorString(e));
     }
   } else {
+    dcp::GenProjArgs pa{};
+    pa.s = s;
+    pa.s_bf16 = act_bf16;
+    pa.w_q = w->w_q;
+    pa.w_k = w->w_k;
+    pa.w_v = w->w_v;
+    pa.w_g = w->w_g;
+    pa.n_tok = N;
+    pa.q_row0 = q_row0;
+    pa.n_q = n_q;
+    pa.c_s = shape->c_s;
+    pa.hd = hd;
+    pa.mask = key_mask;
+    pa.q = at(L.off_q);
+    pa.k = at(L.off_k);
+    pa.v = at(L.off_v);
+    pa.g = at(L.off_g);
     if ((e = dcp::launch_gen_proj(pa, st)) != hipSuccess)
       return fail(DCP_ERR_HIP, "projection launch failed: %s", hipGetErrorString(e));
     dcp::BackRowsArgs ra{};
@@ -1469,41 +1493,49 @@ int dcp_pair_bias_attention_backward(const dcp_shape* shape, const dcp_weights* 
   sa.dq_parts = path == kPathFast ? dq_parts : nullptr;
   sa.kv_parts = kv_parts;
   sa.t_parts = t_parts;
+  sa.split = path == kPathFast;
   sa.dq = at(L.off_dq);
   sa.dkv = at(L.off_dkv);
   sa.t = at(L.off_t);
   if ((e = dcp::launch_back_sum(sa, st)) != hipSuccess)
     return fail(DCP_ERR_HIP, "gradient sum launch failed: %s", hipGetErrorString(e));
 
-  dcp::BackGemmArgs ga{};
-  ga.n_tok = N;
-  ga.q_row0 = q_row0;
-  ga.n_q = n_q;
-  ga.hd = hd;
-  ga.c_s = shape->c_s;
-  ga.s_bf16 = act_bf16;
-  ga.s = s;
-  ga.mask = key_mask;
-  ga.w_q = w->w_q;
-  ga.w_k = w->w_k;
-  ga.w_v = w->w_v;
-  ga.w_g = w->w_g;
-  ga.dq = sa.dq;
-  ga.dk = sa.dkv;
-  ga.dv = sa.dkv + N * hd;
-  ga.dg = dg;
-  ga.ds_splits = L.ds_splits;
-  ga.w_splits = L.w_splits;
-  ga.ds_parts = grads->ds ? at(L.off_ds_parts) : nullptr;
-  ga.w_parts = grads->dw_q || grads->dw_k || grads->dw_v || grads->dw_g ? at(L.off_w_parts) : nullptr;
-  e = path == kPathFast ? dcp::launch_token_grad(ga, st) : dcp::launch_back_gemm(ga, st);
-  if (e != hipSuccess)
-    return fail(DCP_ERR_HIP, "token gradient launch failed: %s", hipGetErrorString(e));
+  float* const ds_parts = grads->ds ? at(L.off_ds_parts) : nullptr;
+  float* const w_parts = grads->dw_q || grads->dw_k || grads->dw_v || grads->dw_g ? at(L.off_w_parts) : nullptr;
+  if (path == kPathFast) {
+    ta.ds_parts = ds_parts;
+    ta.w_parts = w_parts;
+    e = dcp::launch_token_grad(ta, st);
+  } else {
+    dcp::BackGemmArgs ga{};
+    ga.n_tok = N;
+    ga.q_row0 = q_row0;
+    ga.n_q = n_q;
+    ga.hd = hd;
+    ga.c_s = shape->c_s;
+    ga.s_bf16 = act_bf16;
+    ga.s = s;
+    ga.mask = key_mask;
+    ga.w_q = w->w_q;
+    ga.w_k = w->w_k;
+    ga.w_v = w->w_v;
+    ga.w_g = w->w_g;
+    ga.dq = sa.dq;
+    ga.dk = sa.dkv;
+    ga.dv = sa.dkv + N * hd;
+    ga.dg = dg;
+    ga.ds_splits = L.ds_splits;
+    ga.w_splits = L.w_splits;
+    ga.ds_parts = ds_parts;
+    ga.w_parts = w_parts;
+    e = dcp::launch_back_gemm(ga, st);
+  }
+  if (e != hipSuccess) return fail(DCP_ERR_HIP, "token gradient launch failed: %s", hipGetErrorString(e));
 
   fa.ds_splits = L.ds_splits;
   fa.w_splits = L.w_splits;
-  fa.ds_parts = ga.ds_parts;
-  fa.w_parts = ga.w_parts;
+  fa.ds_parts = ds_parts;
+  fa.w_parts = w_parts;
   fa.t = sa.t;
   if ((e = dcp::launch_back_finish(fa, st)) != hipSuccess)
     return fail(DCP_ERR_HIP, "gradient output launch failed: %s", hipGetErrorString(e));

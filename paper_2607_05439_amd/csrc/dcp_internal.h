@@ -86,7 +86,6 @@ struct GenProjArgs {
   const uint8_t* mask;   // [N] or null: v of masked keys is written as 0
   int32_t kv_head_dim;   // k, v in the tiled attention's layout, with this head size; 0: row-major [N][hd]
   int32_t s_vec;         // set by the launcher: rows of s take 4-element loads
-  uint32_t* tops;        // launch_token_proj: [3][64] largest |q|, |k|, |v| (bits of floats, cleared before)
 };
 
 struct GenAttnArgs {
@@ -310,7 +309,10 @@ struct FastBackArgs {
   int32_t* exps;           // [5]: the powers of two of q, k, v, do and W''
   u32x4* w_ops;            // [768]: bias weights, W''
   uint16_t *qf, *qt, *of, *ot, *kf, *kt, *vf;
-  float *lse, *dot, *dg;   // [H][nq_pad] twice, [n_q][384]
+  float *lse, *dot;        // [H][nq_pad]
+  const float* w[4];       // W_q, W_k, W_v, W_g [384][c_s]
+  int32_t c_s;
+  uint16_t *w_split, *dg;  // [2][4][384][c_s], [2][n_q][384]: bf16 hi, then lo
   uint32_t* tile_valid;    // [n_pad / 16]
   float eps;
   // per chunk of rows
@@ -328,6 +330,7 @@ struct BackSumArgs {
   int32_t hd, dq_n, kv_n, t_n, t_cols;
   const float *dq_parts, *kv_parts, *t_parts;  // dq_parts null: dq is there already
   float *dq, *dkv, *t;     // [n_q][hd], [2][N][hd], [H][c_z]
+  int32_t split;           // dq and dkv in bf16, hi then lo, in the same room (hd a multiple of four)
   uint32_t token_blocks;   // set by the launcher
 };
 
@@ -342,6 +345,21 @@ struct BackGemmArgs {
   float *ds_parts, *w_parts;  // [splits][N][c_s], [splits][4][hd][c_s]; null: not wanted
   int64_t ds_blocks;          // set by the launcher, with the next
   int32_t w_vec;
+};
+
+// Token products of the fused shape (token_gemm.hip). Split operands: bf16 hi, then lo.
+struct TokenArgs {
+  int64_t n_tok, q_row0, n_q;
+  int32_t c_s;
+  const uint16_t* s;       // [N][c_s] bf16
+  const uint8_t* mask;
+  const uint16_t* w;       // [2][4][384][c_s]: W_q, W_k, W_v, W_g
+  float *q, *k, *v, *g;    // [n_q][384] (q, g), [N][384]
+  uint32_t* tops;          // [3][kBackTops]: largest |q|, |k|, |v| of shares of each (cleared before)
+  const uint16_t *dq, *dg, *dkv;  // [2][n_q][384] twice, [2][2][N][384]
+  int32_t ds_splits, w_splits;
+  float *ds_parts, *w_parts;      // as in BackGemmArgs
+  int64_t ds_blocks;              // set by the launcher
 };
 
 struct BackFinishArgs {
@@ -384,8 +402,8 @@ hipError_t launch_fast_back_keys(const FastBackArgs& a, hipStream_t st);
 hipError_t launch_back_sum(const BackSumArgs& a, hipStream_t st);
 void back_gemm_splits(int64_t n_tok, int32_t hd, int32_t c_s, int32_t min_depth, int* ds_splits, int* w_splits);
 hipError_t launch_back_gemm(const BackGemmArgs& a, hipStream_t st);
-hipError_t launch_token_proj(const GenProjArgs& a, hipStream_t st);  // the fused shape: hd = 384, s in bf16, tops wanted
-hipError_t launch_token_grad(const BackGemmArgs& a, hipStream_t st);
+hipError_t launch_token_proj(const TokenArgs& a, hipStream_t st);
+hipError_t launch_token_grad(const TokenArgs& a, hipStream_t st);
 hipError_t launch_back_finish(const BackFinishArgs& a, hipStream_t st);
 int scatter_order_flags(int64_t n_atoms);  // plan workgroups (one flag each) for n_atoms (<= kScatterFlags)
 

@@ -5,7 +5,10 @@
 //   dW_x = dx^T s
 // fp32 operands enter the bf16 matrix cores as hi + lo, 16 significant bits, s as it
 // is: two products each for q, k, v, g and dW, three (hi hi, hi lo, lo hi) for ds, at 16
-// times the fp32 matrix rate. bf16 has fp32's range, so nothing is scaled.
+// times the fp32 matrix rate. bf16 has fp32's range, so nothing is scaled. The kernels
+// that write an operand split it (prep_kernel and pack_kernel in backward_fast.hip,
+// back_sum_kernel in backward.hip): splitting each time it is staged took longer than
+// the products.
 //
 // A workgroup of four waves takes 64 x 64 outputs, 32 x 32 a wave; operands 32 deep go
 // through LDS in two buffers, the next two steps in flight in registers. An operand whose
@@ -36,28 +39,15 @@ struct GemmLds {
   Side a[2][2], b[2][2];  // [buffer][hi, lo]
 };
 
-// Eight consecutive elements, as loaded.
+// Eight consecutive elements: hi and, of a split operand, lo.
 struct Eight {
-  f32x4 x, y;  // fp32; or x alone, eight of bf16
+  u32x4 hi, lo;
 };
-__device__ __forceinline__ Eight load8(const float* p) {
-  return {*reinterpret_cast<const f32x4*>(p), *reinterpret_cast<const f32x4*>(p + 4)};
-}
-__device__ __forceinline__ Eight load8(const uint16_t* p) {
-  return {*reinterpret_cast<const f32x4*>(p), f32x4{0.f, 0.f, 0.f, 0.f}};
-}
-__device__ __forceinline__ Eight zero8() { return {f32x4{0.f, 0.f, 0.f, 0.f}, f32x4{0.f, 0.f, 0.f, 0.f}}; }
-
-__device__ __forceinline__ void split8(const Eight& e, u32x4& hi, u32x4& lo) {
-  bf16x8 h, l;
-#pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    const float v = i < 4 ? e.x[i] : e.y[i - 4];
-    h[i] = (__bf16)v;
-    l[i] = (__bf16)(v - (float)h[i]);
-  }
-  hi = __builtin_bit_cast(u32x4, h);
-  lo = __builtin_bit_cast(u32x4, l);
+template <bool SPLIT>
+__device__ __forceinline__ void load8(Eight& e, bool in, const uint16_t* p, int64_t lo) {
+  const u32x4 zero = {0u, 0u, 0u, 0u};
+  e.hi = in ? *reinterpret_cast<const u32x4*>(p) : zero;
+  if constexpr (SPLIT) e.lo = in ? *reinterpret_cast<const u32x4*>(p + lo) : zero;
 }
 
 // Where a thread's eight elements go. Depth along the rows (ALONG): row tid / 4, depth
@@ -69,14 +59,8 @@ __device__ __forceinline__ int piece_at(int tid) {
 }
 template <bool ALONG, bool SPLIT>
 __device__ __forceinline__ void stage(Side (&to)[2], const Eight& e, int tid) {
-  if constexpr (SPLIT) {
-    u32x4 hi, lo;
-    split8(e, hi, lo);
-    to[0].w[piece_at<ALONG>(tid)] = hi;
-    to[1].w[piece_at<ALONG>(tid)] = lo;
-  } else {
-    to[0].w[piece_at<ALONG>(tid)] = __builtin_bit_cast(u32x4, e.x);
-  }
+  to[0].w[piece_at<ALONG>(tid)] = e.hi;
+  if constexpr (SPLIT) to[1].w[piece_at<ALONG>(tid)] = e.lo;
 }
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef __attribute__((address_space(3))) s16x4* lds_s16x4;
@@ -148,7 +132,7 @@ __device__ __forceinline__ void clear(f32x4 (&acc)[2][2]) {
 // ----------------------------------------------------------------------------- q, k, v, g
 // Blocks: 12 tiles of the side's two projections, token tiles of the keys then of the
 // stripe's rows.
-__global__ void __launch_bounds__(256) token_proj_kernel(GenProjArgs p) {
+__global__ void __launch_bounds__(256) token_proj_kernel(TokenArgs p) {
   __shared__ GemmLds s;
   const int tid = threadIdx.x, lane = tid & 63, n = lane & 15, g = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -159,18 +143,19 @@ __global__ void __launch_bounds__(256) token_proj_kernel(GenProjArgs p) {
   const bool q_side = tile >= key_tiles, second = col >= kTiles;
   const int64_t row0 = (tile - (q_side ? key_tiles : 0)) * kTile, rows = q_side ? p.n_q : p.n_tok;
   const int o0 = (col % kTiles) * kTile;
-  const float* w = q_side ? (second ? p.w_g : p.w_q) : (second ? p.w_v : p.w_k);
-  float* dst = q_side ? (second ? p.g : p.q) : (second ? p.v : p.k);
+  const int which = q_side ? (second ? 3 : 0) : (second ? 2 : 1);  // q, k, v, g
+  float* dst = which == 0 ? p.q : which == 1 ? p.k : which == 2 ? p.v : p.g;
   const int64_t row = min(row0 + (tid >> 2), rows - 1);  // rows past the last repeat it
-  const uint16_t* sp = static_cast<const uint16_t*>(p.s) + ((q_side ? p.q_row0 : 0) + row) * p.c_s + 8 * (tid & 3);
-  const float* wp = w + (int64_t)(o0 + (tid >> 2)) * p.c_s + 8 * (tid & 3);
+  const uint16_t* sp = p.s + ((q_side ? p.q_row0 : 0) + row) * p.c_s + 8 * (tid & 3);
+  const uint16_t* wp = p.w + ((int64_t)which * kHD + o0 + (tid >> 2)) * p.c_s + 8 * (tid & 3);
+  const int64_t w_lo = (int64_t)4 * kHD * p.c_s;
   f32x4 acc[2][2];
   clear(acc);
   product<true, false, true, true>(
       s, p.c_s / kDeep,
       [&](int64_t i, Eight& a, Eight& b) {
-        a = load8(sp + i * kDeep);
-        b = load8(wp + i * kDeep);
+        load8<false>(a, true, sp + i * kDeep, 0);
+        load8<true>(b, true, wp + i * kDeep, w_lo);
       },
       acc);
   float top = 0.0f;
@@ -199,7 +184,7 @@ __global__ void __launch_bounds__(256) token_proj_kernel(GenProjArgs p) {
 }
 
 // ----------------------------------------------------------------------------- ds, dW
-__global__ void __launch_bounds__(256) token_grad_kernel(BackGemmArgs p) {
+__global__ void __launch_bounds__(256) token_grad_kernel(TokenArgs p) {
   __shared__ GemmLds s;
   const int tid = threadIdx.x, lane = tid & 63, n = lane & 15, g = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -213,6 +198,7 @@ __global__ void __launch_bounds__(256) token_grad_kernel(BackGemmArgs p) {
   b /= splits;
   const int c = c0 + 8 * (tid & 7);
   const bool c_in = c < p.c_s;
+  const int64_t kv_lo = 2 * p.n_tok * kHD, q_lo = p.n_q * kHD;
   f32x4 acc[2][2];
   clear(acc);
   int64_t m0, m_end;
@@ -226,37 +212,39 @@ __global__ void __launch_bounds__(256) token_grad_kernel(BackGemmArgs p) {
     constexpr int kSteps = kHD / kDeep;
     int64_t steps, first;
     chunk_of(kSteps * (with_rows ? 4 : 2), splits, split, &steps, &first);
-    const int64_t t = m0 + (tid >> 2);
+    const int64_t t = m0 + (tid >> 2), tq = t - p.q_row0, w_lo = (int64_t)4 * kHD * p.c_s;
+    const bool kv_in = t < p.n_tok, q_in = tq >= 0 && tq < p.n_q;
+    const int64_t kv_at = t * kHD + 8 * (tid & 3), q_at = tq * kHD + 8 * (tid & 3), w_at = (int64_t)(tid >> 3) * p.c_s + c;
     product<true, true, false, true>(
         s, steps,
         [&](int64_t i, Eight& a, Eight& bb) {
           const int step = (int)(first + i), term = step / kSteps, o = (step - term * kSteps) * kDeep;
-          const float* x = term == 0 ? p.dk : term == 1 ? p.dv : term == 2 ? p.dq : p.dg;
-          const float* w = term == 0 ? p.w_k : term == 1 ? p.w_v : term == 2 ? p.w_q : p.w_g;
-          const int64_t row = t - (term >= 2 ? p.q_row0 : 0), rows = term >= 2 ? p.n_q : p.n_tok;
-          a = row >= 0 && row < rows ? load8(x + row * kHD + o + 8 * (tid & 3)) : zero8();
-          bb = c_in ? load8(w + (int64_t)(o + (tid >> 3)) * p.c_s + c) : zero8();
+          const uint16_t* x = term == 0 ? p.dkv : term == 1 ? p.dkv + p.n_tok * kHD : term == 2 ? p.dq : p.dg;
+          const int mat = term == 0 ? 1 : term == 1 ? 2 : term == 2 ? 0 : 3;
+          load8<true>(a, term < 2 ? kv_in : q_in, x + (term < 2 ? kv_at : q_at) + o, term < 2 ? kv_lo : q_lo);
+          load8<true>(bb, c_in, p.w + ((int64_t)mat * kHD + o) * p.c_s + w_at, w_lo);
         },
         acc);
   } else {
-    const int mat = (int)(b / (kHD / kTile));
+    const int mat = (int)(b / (kHD / kTile));  // q, k, v, g
     m0 = (b % (kHD / kTile)) * kTile;
     m_end = kHD;
     out = p.w_parts + ((int64_t)split * 4 + mat) * kHD * p.c_s;
     const bool stripe = mat == 0 || mat == 3;
     const int64_t rows = stripe ? p.n_q : p.n_tok, s_row0 = stripe ? p.q_row0 : 0;
-    const float* x = mat == 0 ? p.dq : mat == 1 ? p.dk : mat == 2 ? p.dv : p.dg;
+    const uint16_t* x = mat == 0 ? p.dq : mat == 1 ? p.dkv : mat == 2 ? p.dkv + p.n_tok * kHD : p.dg;
     int64_t steps, first;
     chunk_of((rows + kDeep - 1) / kDeep, splits, split, &steps, &first);
+    const int64_t t0 = first * kDeep + (tid >> 3);
+    const uint16_t *xp = x + t0 * kHD + m0 + 8 * (tid & 7), *sp = p.s + (s_row0 + t0) * p.c_s + c;
     product<false, true, false, false>(
         s, steps,
         [&](int64_t i, Eight& a, Eight& bb) {
-          const int64_t t = (first + i) * kDeep + (tid >> 3);
+          const int64_t t = t0 + i * kDeep;
           const bool in = t < rows;
-          a = in ? load8(x + t * kHD + m0 + 8 * (tid & 7)) : zero8();
+          load8<true>(a, in, xp + i * kDeep * kHD, stripe ? q_lo : kv_lo);
           // a masked token's s does not enter the gradients of W_k and W_v
-          const bool used = in && c_in && (stripe || !p.mask || p.mask[t] != 0);
-          bb = used ? load8(static_cast<const uint16_t*>(p.s) + (s_row0 + t) * p.c_s + c) : zero8();
+          load8<false>(bb, in && c_in && (stripe || !p.mask || p.mask[t] != 0), sp + i * kDeep * p.c_s, 0);
         },
         acc);
   }
@@ -274,14 +262,14 @@ __global__ void __launch_bounds__(256) token_grad_kernel(BackGemmArgs p) {
 
 }  // namespace
 
-hipError_t launch_token_proj(const GenProjArgs& a, hipStream_t st) {
+hipError_t launch_token_proj(const TokenArgs& a, hipStream_t st) {
   const int64_t tiles = (a.n_tok + kTile - 1) / kTile + (a.n_q + kTile - 1) / kTile;
   hipLaunchKernelGGL(token_proj_kernel, dim3((unsigned)(tiles * 2 * (kHD / kTile))), dim3(256), 0, st, a);
   return hipGetLastError();
 }
 
-hipError_t launch_token_grad(const BackGemmArgs& a, hipStream_t st) {
-  BackGemmArgs b = a;
+hipError_t launch_token_grad(const TokenArgs& a, hipStream_t st) {
+  TokenArgs b = a;
   const int64_t c_tiles = (a.c_s + kTile - 1) / kTile;
   b.ds_blocks = a.ds_parts ? (a.n_tok + kTile - 1) / kTile * c_tiles * a.ds_splits : 0;
   const int64_t w_blocks = a.w_parts ? 4 * (kHD / kTile) * c_tiles * a.w_splits : 0;
