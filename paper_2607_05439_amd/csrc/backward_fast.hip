@@ -6,7 +6,7 @@
 //   (the fp32 projections of the general path, which also leave the largest |q|, |k|, |v|)
 //   pack_kernel   q, do of the rows and k, v of the keys as fp16 operands; the row statistics
 //   pairs_kernel  16 query rows and a range of keys per workgroup: bias, P, dS, dz, dq, T
-//   keys_kernel   64 keys of a head per wave: dk, dv from the stored P and dS
+//   keys_kernel   64 keys of a head per wave: dk, dv from the stored P
 // then the token products of backward.hip.
 //
 // Operands are fp16, not bf16: 11 significant bits where bf16 has 8, at the same rate, so
@@ -268,9 +268,9 @@ __global__ void __launch_bounds__(64) pack_kernel(FastBackArgs a) {
 //      (pair_bias), z staying in the registers; the bias goes through LDS
 //      [head][row][key];
 //   2. the waves split the heads: S = K Q^T, P = exp2(S + bias - lse), dP = V dO^T,
-//      dS = P (dP - D), dq += K^T dS; P and dS, transposed on the matrix cores
-//      (the accumulator's registers as the A operand of a product with the identity:
-//      exact), go to memory as the operands of the keys kernel, and dS to LDS
+//      dS = P (dP - D), dq += K^T dS; P, transposed on the matrix cores (the
+//      accumulator's registers as the A operand of a product with the identity:
+//      exact), goes to memory as an operand of the keys kernel, and dS to LDS
 //      [key][row][head];
 //   3. the waves split the keys again: dzh = W''^T dS, dz = rstd (dzh - zh t) with
 //      t = sum_h dS_h b_h / c_z (the mean of dzh zh; W'' is centred, so dzh has no mean),
@@ -318,7 +318,7 @@ __global__ void __launch_bounds__(256, 2) pairs_kernel(FastBackArgs a) {
     const int k = 4 * wave + kk;
     const int at = (bits >> k) & 1u ? zoff + (int)(t * 16 + k) * (kCz * 2) : kOutOfRange;
 #pragma unroll
-    for (int x = 0; x < 4; ++x) z[x] = __builtin_amdgcn_raw_buffer_load_b128(zres, at + 64 * x, 0, 2);
+    for (int x = 0; x < 4; ++x) z[x] = __builtin_amdgcn_raw_buffer_load_b128(zres, at + 64 * x, 0, 0);
   };
   u32x4 z[4][4];
 #pragma unroll
@@ -415,8 +415,7 @@ __global__ void __launch_bounds__(256, 2) pairs_kernel(FastBackArgs a) {
       dq[j][0] = mfma16h(__builtin_bit_cast(f16x4, kt0), ds16, dq[j][0]);
       dq[j][1] = mfma16h(__builtin_bit_cast(f16x4, kt1), ds16, dq[j][1]);
       const u32x2 pt = __builtin_bit_cast(u32x2, to_f16(mfma16h(p16, id, zero)));
-      const u32x2 dt = __builtin_bit_cast(u32x2, to_f16(mfma16h(ds16, id, zero)));
-      a.pd[(((int64_t)h * (a.chunk_pad >> 4) + (r0 >> 4)) * n_tiles + t) * 64 + lane] = u32x4{pt[0], pt[1], dt[0], dt[1]};
+      a.p[(((int64_t)h * (a.chunk_pad >> 4) + (r0 >> 4)) * n_tiles + t) * 64 + lane] = pt;
     }
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
@@ -514,7 +513,9 @@ __global__ void __launch_bounds__(256, 2) pairs_kernel(FastBackArgs a) {
 
 // ----------------------------------------------------------------------------- keys
 // dk and dv of 64 keys of one head over a share of the chunk's row tiles: the four waves
-// take every fourth of them, and their sums meet in LDS. Bound by the reads of P and dS.
+// take every fourth of them, and their sums meet in LDS. dS = P (dP - D) is formed again
+// from P and one more product, dP = dO V^T: stored beside P it took as many bytes again,
+// written and read, and 32 bytes a pair are what bounds this kernel.
 __global__ void __launch_bounds__(256) keys_kernel(FastBackArgs a) {
   __shared__ f32x4 s_sum[16][64];
   const int lane = threadIdx.x & 63, n = lane & 15, g = lane >> 4;
@@ -524,24 +525,37 @@ __global__ void __launch_bounds__(256) keys_kernel(FastBackArgs a) {
   int64_t count, first;
   chunk_of((a.rows + 15) / 16, a.kv_splits, split, &count, &first);
   f32x4 acc[4][2][2];  // [key tile][dk, dv][channels 0..15, 16..31]
+  const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-  for (int x = 0; x < 16; ++x) acc[x >> 2][(x >> 1) & 1][x & 1] = f32x4{0.f, 0.f, 0.f, 0.f};
+  for (int x = 0; x < 16; ++x) acc[x >> 2][(x >> 1) & 1][x & 1] = zero;
+  f16x8 v[4];
+#pragma unroll
+  for (int k = 0; k < 4; ++k)
+    v[k] = as_f16x8(reinterpret_cast<const u32x4*>(a.vf)[((int64_t)h * n_tiles + min(t0 + k, n_tiles - 1)) * 64 + 4 * n + g]);
   for (int64_t r = first + wave; r < first + count; r += 4) {
     const int64_t row_tile = (int64_t)h * (a.nq_pad >> 4) + (a.row0 >> 4) + r;
+    const u32x2* pp = a.p + (((int64_t)h * (a.chunk_pad >> 4) + r) * n_tiles + t0) * 64 + lane;
+    u32x2 x[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) x[k] = t0 + k < n_tiles ? __builtin_nontemporal_load(pp + 64 * k) : u32x2{0u, 0u};
     const u32x4 qt = reinterpret_cast<const u32x4*>(a.qt)[row_tile * 64 + lane];
     const u32x4 ot = reinterpret_cast<const u32x4*>(a.ot)[row_tile * 64 + lane];
-    const u32x4* pd = a.pd + (((int64_t)h * (a.chunk_pad >> 4) + r) * n_tiles + t0) * 64 + lane;
-    u32x4 x[4];
+    const f16x8 o = as_f16x8(reinterpret_cast<const u32x4*>(a.of)[row_tile * 64 + 4 * n + g]);
+    const f32x4 dot = *reinterpret_cast<const f32x4*>(a.dot + row_tile * 16 + 4 * g);
 #pragma unroll
-    for (int k = 0; k < 4; ++k) x[k] = t0 + k < n_tiles ? __builtin_nontemporal_load(pd + 64 * k) : u32x4{0u, 0u, 0u, 0u};
+    for (int k = 0; k < 4; ++k) {
+      // accumulator rows = query rows 4g..4g+3, column = key n: as P lies
+      const f32x4 dp = mfma32h(o, v[k], zero);
+      const f16x4 p = __builtin_bit_cast(f16x4, x[k]);
+      f32x4 d;
 #pragma unroll
-    for (int u = 0; u < 2; ++u) {
-      const u32x2 qu = {qt[2 * u], qt[2 * u + 1]}, ou = {ot[2 * u], ot[2 * u + 1]};
+      for (int i = 0; i < 4; ++i) d[i] = (float)p[i] * ((dp[i] - dot[i]) * (1.0f / (1 << (kDsShift + kPShift))));
+      const f16x4 ds = to_f16(d);
 #pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        const u32x2 p = {x[k][0], x[k][1]}, ds = {x[k][2], x[k][3]};
-        acc[k][0][u] = mfma16h(__builtin_bit_cast(f16x4, ds), __builtin_bit_cast(f16x4, qu), acc[k][0][u]);
-        acc[k][1][u] = mfma16h(__builtin_bit_cast(f16x4, p), __builtin_bit_cast(f16x4, ou), acc[k][1][u]);
+      for (int u = 0; u < 2; ++u) {
+        const u32x2 qu = {qt[2 * u], qt[2 * u + 1]}, ou = {ot[2 * u], ot[2 * u + 1]};
+        acc[k][0][u] = mfma16h(ds, __builtin_bit_cast(f16x4, qu), acc[k][0][u]);
+        acc[k][1][u] = mfma16h(p, __builtin_bit_cast(f16x4, ou), acc[k][1][u]);
       }
     }
   }

@@ -1122,10 +1122,10 @@ int dcp_layer_norm_backward(int64_t n_rows, int32_t c, int32_t in_dtype, int32_t
 // ----------------------------------------------------------------------------- attention backward
 namespace {
 
-// Most bytes of P and dS kept at a time: the stripe's rows are taken in chunks of as
-// many as fit, at least one (the fused path: 16).
+// Most bytes of P and dS (the fused path: of P) kept at a time: the stripe's rows are
+// taken in chunks of as many as fit, at least one (16).
 constexpr size_t kBackGenBytes = (size_t)256 << 20;
-constexpr size_t kBackFastBytes = (size_t)2 << 30;
+constexpr size_t kBackFastBytes = (size_t)1 << 30;
 
 struct BackLayout {
   int64_t chunk, nq_pad, n_pad;  // chunk: rows at a time
@@ -1171,7 +1171,7 @@ void back_layout(const dcp_shape* sh, Path path, int64_t n_q, BackLayout* L) {
   if (path == kPathFast) {
     L->nq_pad = (n_q + 15) / 16 * 16;
     L->n_pad = (N + 15) / 16 * 16;
-    const size_t per_tile = (size_t)16 * L->n_pad * H * 4;  // P and dS of 16 rows, fp16
+    const size_t per_tile = (size_t)16 * L->n_pad * H * 2;  // P of 16 rows, fp16
     L->chunk = 16 * (int64_t)(kBackFastBytes / per_tile);
     if (L->chunk < 16) L->chunk = 16;
     if (L->chunk > L->nq_pad) L->chunk = L->nq_pad;
@@ -1351,7 +1351,7 @@ int dcp_pair_bias_attention_backward(const dcp_shape* shape, const dcp_weights* 
     ba.chunk_pad = L.chunk;
     ba.n_parts = L.dq_parts;
     ba.kv_splits = L.kv_splits;
-    ba.pd = reinterpret_cast<dcp::u32x4*>(ws + L.off_p);
+    ba.p = reinterpret_cast<dcp::u32x2*>(ws + L.off_p);
     ba.dz = static_cast<uint16_t*>(grads->dz_rows);
     ba.dq_parts = dq_parts;
     ba.t_parts = t_parts;

@@ -318,7 +318,7 @@ struct FastBackArgs {
   // per chunk of rows
   int64_t row0, rows, chunk_pad;  // row0 and chunk_pad multiples of 16
   int32_t n_parts, kv_splits, first;
-  u32x4* pd;               // [H][chunk_pad / 16][n_pad / 16][64]: P and dS of 16 rows by 16 keys
+  u32x2* p;                // [H][chunk_pad / 16][n_pad / 16][64]: P of 16 rows by 16 keys
   uint16_t* dz;            // as z, or null
   float* dq_parts;         // [n_parts][n_q][384]
   float* t_parts;          // [n_parts * row tiles][16][128]
