@@ -516,7 +516,7 @@ __global__ void __launch_bounds__(256, 2) pairs_kernel(FastBackArgs a) {
 // take every fourth of them, and their sums meet in LDS. dS = P (dP - D) is formed again
 // from P and one more product, dP = dO V^T: stored beside P it took as many bytes again,
 // written and read, and 32 bytes a pair are what bounds this kernel.
-__global__ void __launch_bounds__(256) keys_kernel(FastBackArgs a) {
+__global__ void __launch_bounds__(256, 3) keys_kernel(FastBackArgs a) {
   __shared__ f32x4 s_sum[16][64];
   const int lane = threadIdx.x & 63, n = lane & 15, g = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -532,28 +532,40 @@ __global__ void __launch_bounds__(256) keys_kernel(FastBackArgs a) {
 #pragma unroll
   for (int k = 0; k < 4; ++k)
     v[k] = as_f16x8(reinterpret_cast<const u32x4*>(a.vf)[((int64_t)h * n_tiles + min(t0 + k, n_tiles - 1)) * 64 + 4 * n + g]);
-  for (int64_t r = first + wave; r < first + count; r += 4) {
+  // a row tile's operands, loaded one step ahead
+  u32x2 x[4];
+  u32x4 qt, ot, of;
+  f32x4 dt;
+  auto load = [&](int64_t r) {
     const int64_t row_tile = (int64_t)h * (a.nq_pad >> 4) + (a.row0 >> 4) + r;
     const u32x2* pp = a.p + (((int64_t)h * (a.chunk_pad >> 4) + r) * n_tiles + t0) * 64 + lane;
-    u32x2 x[4];
 #pragma unroll
     for (int k = 0; k < 4; ++k) x[k] = t0 + k < n_tiles ? __builtin_nontemporal_load(pp + 64 * k) : u32x2{0u, 0u};
-    const u32x4 qt = reinterpret_cast<const u32x4*>(a.qt)[row_tile * 64 + lane];
-    const u32x4 ot = reinterpret_cast<const u32x4*>(a.ot)[row_tile * 64 + lane];
-    const f16x8 o = as_f16x8(reinterpret_cast<const u32x4*>(a.of)[row_tile * 64 + 4 * n + g]);
-    const f32x4 dot = *reinterpret_cast<const f32x4*>(a.dot + row_tile * 16 + 4 * g);
+    qt = reinterpret_cast<const u32x4*>(a.qt)[row_tile * 64 + lane];
+    ot = reinterpret_cast<const u32x4*>(a.ot)[row_tile * 64 + lane];
+    of = reinterpret_cast<const u32x4*>(a.of)[row_tile * 64 + 4 * n + g];
+    dt = *reinterpret_cast<const f32x4*>(a.dot + row_tile * 16 + 4 * g);
+  };
+  if (wave < count) load(first + wave);
+  for (int64_t r = first + wave; r < first + count; r += 4) {
+    const f16x4 pk[4] = {__builtin_bit_cast(f16x4, x[0]), __builtin_bit_cast(f16x4, x[1]), __builtin_bit_cast(f16x4, x[2]),
+                         __builtin_bit_cast(f16x4, x[3])};
+    const u32x4 q = qt, og = ot;
+    const f16x8 o = as_f16x8(of);
+    const f32x4 dot = dt;
+    if (r + 4 < first + count) load(r + 4);
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
       // accumulator rows = query rows 4g..4g+3, column = key n: as P lies
       const f32x4 dp = mfma32h(o, v[k], zero);
-      const f16x4 p = __builtin_bit_cast(f16x4, x[k]);
+      const f16x4 p = pk[k];
       f32x4 d;
 #pragma unroll
       for (int i = 0; i < 4; ++i) d[i] = (float)p[i] * ((dp[i] - dot[i]) * (1.0f / (1 << (kDsShift + kPShift))));
       const f16x4 ds = to_f16(d);
 #pragma unroll
       for (int u = 0; u < 2; ++u) {
-        const u32x2 qu = {qt[2 * u], qt[2 * u + 1]}, ou = {ot[2 * u], ot[2 * u + 1]};
+        const u32x2 qu = {q[2 * u], q[2 * u + 1]}, ou = {og[2 * u], og[2 * u + 1]};
         acc[k][0][u] = mfma16h(ds, __builtin_bit_cast(f16x4, qu), acc[k][0][u]);
         acc[k][1][u] = mfma16h(p, __builtin_bit_cast(f16x4, ou), acc[k][1][u]);
       }
