@@ -181,69 +181,86 @@ __device__ __forceinline__ void pack_out(const PackTile& t, int h, int64_t tile,
 __global__ void __launch_bounds__(64) pack_kernel(FastBackArgs a) {
   __shared__ PackTile s_x[4], s_y[4];
   const int lane = threadIdx.x, h = 4 * blockIdx.y + (lane >> 4);
+  const bool is_row = blockIdx.x < a.nq_pad / 16;
+  const int64_t tile = (int64_t)blockIdx.x - (is_row ? 0 : a.nq_pad / 16), tok = tile * 16 + (lane & 15);
+  // every load before the first use of one
+  float tops[4];
+#pragma unroll
+  for (int x = 0; x < 4; ++x) tops[x] = __uint_as_float(a.tops[kBackTops * x + lane]);
+  f32x4 in[4][kD / 4];  // rows: q, g, acc, dout; keys: k, v
+  float l = 0.0f, m = 0.0f;
+  const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
+  const int64_t at = tok * kHD + h * kD;
+  const bool there = is_row ? tok < a.n_q : tok < a.n_tok && (!a.mask || a.mask[tok] != 0);
+  if (is_row) {
+    if (there) {
+      l = a.l[(int64_t)h * a.n_q + tok];
+      m = a.m[(int64_t)h * a.n_q + tok];
+    }
+#pragma unroll
+    for (int e = 0; e < kD / 4; ++e) {
+      in[0][e] = there ? *reinterpret_cast<const f32x4*>(a.q + at + 4 * e) : zero;
+      in[1][e] = there ? *reinterpret_cast<const f32x4*>(a.g + at + 4 * e) : zero;
+      in[2][e] = there ? *reinterpret_cast<const f32x4*>(a.acc + at + 4 * e) : zero;
+    }
+    if (a.dout_bf16) {
+#pragma unroll
+      for (int e = 0; e < kD / 8; ++e) {
+        const u32x4 r = there ? *reinterpret_cast<const u32x4*>(static_cast<const uint16_t*>(a.dout) + at + 8 * e) : u32x4{0u, 0u, 0u, 0u};
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+          in[3][2 * e + (i >> 2)][i & 3] = __uint_as_float(i & 1 ? r[i >> 1] & 0xFFFF0000u : r[i >> 1] << 16);
+      }
+    } else {
+#pragma unroll
+      for (int e = 0; e < kD / 4; ++e)
+        in[3][e] = there ? *reinterpret_cast<const f32x4*>(static_cast<const float*>(a.dout) + at + 4 * e) : zero;
+    }
+  } else {
+#pragma unroll
+    for (int e = 0; e < kD / 4; ++e) {
+      in[0][e] = there ? *reinterpret_cast<const f32x4*>(a.k + at + 4 * e) : zero;
+      in[1][e] = there ? *reinterpret_cast<const f32x4*>(a.v + at + 4 * e) : zero;
+    }
+  }
   int e2[4];  // powers of two of q (with its factor), k, v, and of dout for do (|do| <= |dout|)
 #pragma unroll
   for (int x = 0; x < 4; ++x) {
-    float top = __uint_as_float(a.tops[kBackTops * x + lane]);
+    float top = tops[x];
 #pragma unroll
     for (int o = 32; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor(top, o));
     e2[x] = scale_exp(x == 0 ? top * (kLog2e * kInvSqrtD) : top);
     if (blockIdx.x == 0 && blockIdx.y == 0 && lane == 0) a.exps[x] = e2[x];
   }
-  const bool is_row = blockIdx.x < a.nq_pad / 16;
-  const int64_t tile = (int64_t)blockIdx.x - (is_row ? 0 : a.nq_pad / 16);
   float x[kD], y[kD];
   if (is_row) {
-    const int64_t row = tile * 16 + (lane & 15), at = row * kHD + h * kD;
-    const bool there = row < a.n_q;
-    float dot = 0.0f, lse = INFINITY;
+    const float inv_l = l == 0.0f ? 0.0f : 1.0f / l;
+    float dot = 0.0f;
 #pragma unroll
-    for (int e = 0; e < kD; ++e) x[e] = y[e] = 0.0f;
-    if (there) {
-      const float l = a.l[(int64_t)h * a.n_q + row], m = a.m[(int64_t)h * a.n_q + row];
-      const float inv_l = l == 0.0f ? 0.0f : 1.0f / l;
-      if (l != 0.0f) lse = fmaf(m, kLog2e, log2f(l));
+    for (int e = 0; e < kD; e += 4) {
+      f32x4 dg;
 #pragma unroll
-      for (int e = 0; e < kD; e += 4) {
-        const f32x4 q = *reinterpret_cast<const f32x4*>(a.q + at + e), gt = *reinterpret_cast<const f32x4*>(a.g + at + e);
-        const f32x4 ac = *reinterpret_cast<const f32x4*>(a.acc + at + e);
-        f32x4 up;
-        if (a.dout_bf16) {
-          const u32x2 r = *reinterpret_cast<const u32x2*>(static_cast<const uint16_t*>(a.dout) + at + e);
-          up = f32x4{__uint_as_float(r[0] << 16), __uint_as_float(r[0] & 0xFFFF0000u), __uint_as_float(r[1] << 16),
-                     __uint_as_float(r[1] & 0xFFFF0000u)};
-        } else {
-          up = *reinterpret_cast<const f32x4*>(static_cast<const float*>(a.dout) + at + e);
-        }
-        f32x4 dg;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const float o = l == 0.0f ? 0.0f : ac[i] * inv_l, d = gt[i] * up[i];
-          x[e + i] = q[i] * (kLog2e * kInvSqrtD);
-          y[e + i] = d;
-          dot = fmaf(d, o, dot);
-          dg[i] = up[i] * o * gt[i] * (1.0f - gt[i]);
-        }
+      for (int i = 0; i < 4; ++i) {
+        const float gt = in[1][e / 4][i], up = in[3][e / 4][i];
+        const float o = l == 0.0f ? 0.0f : in[2][e / 4][i] * inv_l, d = gt * up;
+        x[e + i] = in[0][e / 4][i] * (kLog2e * kInvSqrtD);
+        y[e + i] = d;
+        dot = fmaf(d, o, dot);
+        dg[i] = up * o * gt * (1.0f - gt);
+      }
+      if (there) {
         u32x2 hi, lo;
         split4(dg, hi, lo);
         *reinterpret_cast<u32x2*>(a.dg + at + e) = hi;
         *reinterpret_cast<u32x2*>(a.dg + a.n_q * kHD + at + e) = lo;
       }
     }
-    a.lse[(int64_t)h * a.nq_pad + row] = lse;
-    a.dot[(int64_t)h * a.nq_pad + row] = ldexpf(dot, e2[2] + e2[3]);
+    a.lse[(int64_t)h * a.nq_pad + tok] = l == 0.0f ? INFINITY : fmaf(m, kLog2e, log2f(l));  // rows past the last: l = 0
+    a.dot[(int64_t)h * a.nq_pad + tok] = ldexpf(dot, e2[2] + e2[3]);
   } else {
-    const int64_t key = tile * 16 + (lane & 15), at = key * kHD + h * kD;
-    const bool valid = key < a.n_tok && (!a.mask || a.mask[key] != 0);
 #pragma unroll
-    for (int e = 0; e < kD; e += 4) {
-      const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
-      const f32x4 k = valid ? *reinterpret_cast<const f32x4*>(a.k + at + e) : zero;
-      const f32x4 v = valid ? *reinterpret_cast<const f32x4*>(a.v + at + e) : zero;
-#pragma unroll
-      for (int i = 0; i < 4; ++i) x[e + i] = k[i], y[e + i] = v[i];
-    }
-    const uint32_t bits = (uint32_t)(__ballot(valid) & 0xFFFFull);
+    for (int e = 0; e < kD; ++e) x[e] = in[0][e / 4][e % 4], y[e] = in[1][e / 4][e % 4];
+    const uint32_t bits = (uint32_t)(__ballot(there) & 0xFFFFull);
     if (blockIdx.y == 0 && lane == 0) a.tile_valid[tile] = bits;
   }
   pack_row(x, e2[is_row ? 0 : 1], s_x[lane >> 4], lane & 15);
