@@ -21,6 +21,8 @@
 #include <math.h>
 #include <stdint.h>
 
+#include <type_traits>
+
 #include "cdna4.h"
 #include "dcp_internal.h"
 
@@ -180,7 +182,7 @@ struct Raw4 {
 };
 
 template <int CT, int NH, bool BF16>
-__global__ void __launch_bounds__(256, CT <= 8 && NH == 1 ? 3 : CT <= 8 ? 2 : 1) back_pairs_kernel(BackPairsArgs a) {
+__global__ void __launch_bounds__(256, CT <= 8 && CT * NH < 32 ? 2 : 1) back_pairs_kernel(BackPairsArgs a) {
   constexpr int CZ = 16 * CT, HP = 4 * NH;
   constexpr bool kHeld = CT * HP <= 8;  // W' of the lane's channels stays in registers
   __shared__ __attribute__((aligned(16))) float s_w[HP * CZ];
@@ -193,6 +195,7 @@ __global__ void __launch_bounds__(256, CT <= 8 && NH == 1 ? 3 : CT <= 8 ? 2 : 1)
   const float inv_c = 1.0f / (float)c_z, scale = 1.0f / sqrtf((float)d);
   const int z_vec = c_z % 4 == 0;
   const bool whole = c_z == CZ;
+  const int chunks = a.dp / 8;
   for (int x = tid; x < HP * CZ; x += 256) {
     const int h = x / CZ, c = x % CZ;
     s_w[x] = h < H && c < c_z ? a.w_b[(int64_t)h * c_z + c] * (a.gamma ? a.gamma[c] : 1.0f) : 0.0f;
@@ -255,6 +258,19 @@ __global__ void __launch_bounds__(256, CT <= 8 && NH == 1 ? 3 : CT <= 8 ? 2 : 1)
       asm volatile("" ::: "memory");  // q, do and W' come from LDS again for each tile, not from registers
       const int64_t j = t * kBackKeys + key, jj = min(j, a.n_tok - 1);
       const bool there = j < a.n_tok, valid = there && attends != 0;
+      // k and v of the lane's heads, eight channels at a time, two such pieces in flight; the
+      // first head's during the statistics and the bias
+      f32x4 kk[2][2], vv[2][2];
+      auto load_kv = [&](int i, int c, int buf) {
+        const int64_t at = ((int64_t)min(4 * i + qd, H - 1) * a.n_tok + jj) * a.dp + 8 * c;
+#pragma unroll
+        for (int x = 0; x < 2; ++x) {
+          kk[buf][x] = *reinterpret_cast<const f32x4*>(a.k + at + 4 * x);
+          vv[buf][x] = *reinterpret_cast<const f32x4*>(a.v + at + 4 * x);
+        }
+      };
+      load_kv(0, 0, 0);
+      load_kv(0, 1, 1);
       f32x4 zh[CT];
       float s = 0.0f, v = 0.0f;
       int c4 = 4 * qd;
@@ -299,24 +315,28 @@ __global__ void __launch_bounds__(256, CT <= 8 && NH == 1 ? 3 : CT <= 8 ? 2 : 1)
         }
         const int h = 4 * i + qd;
         f32x4 lg = {0.f, 0.f, 0.f, 0.f}, dp = {0.f, 0.f, 0.f, 0.f};
-        const int64_t kv = ((int64_t)min(h, H - 1) * a.n_tok + jj) * a.dp;
-        for (int e0 = 0; e0 < a.dp; e0 += 8) {
-          f32x4 kk[2], vv[2];
+        if (i > 0) {
+          load_kv(i, 0, 0);
+          load_kv(i, 1, 1);
+        }
+        auto dots = [&](int c, auto buf) {
+          constexpr int kBuf = decltype(buf)::value;
 #pragma unroll
           for (int x = 0; x < 2; ++x) {
-            kk[x] = *reinterpret_cast<const f32x4*>(a.k + kv + e0 + 4 * x);
-            vv[x] = *reinterpret_cast<const f32x4*>(a.v + kv + e0 + 4 * x);
-          }
-#pragma unroll
-          for (int x = 0; x < 2; ++x) {
-            const f32x4 q = *reinterpret_cast<const f32x4*>(&s_q[h * kHeadStride + e0 + 4 * x]);
-            const f32x4 o = *reinterpret_cast<const f32x4*>(&s_do[h * kHeadStride + e0 + 4 * x]);
+            const f32x4 q = *reinterpret_cast<const f32x4*>(&s_q[h * kHeadStride + 8 * c + 4 * x]);
+            const f32x4 o = *reinterpret_cast<const f32x4*>(&s_do[h * kHeadStride + 8 * c + 4 * x]);
 #pragma unroll
             for (int y = 0; y < 4; ++y) {
-              lg[y] = fmaf(q[y], kk[x][y], lg[y]);
-              dp[y] = fmaf(o[y], vv[x][y], dp[y]);
+              lg[y] = fmaf(q[y], kk[kBuf][x][y], lg[y]);
+              dp[y] = fmaf(o[y], vv[kBuf][x][y], dp[y]);
             }
           }
+          if (c + 2 < chunks) load_kv(i, c + 2, kBuf);
+        };
+#pragma unroll 1
+        for (int c = 0; c < chunks; c += 2) {
+          dots(c, std::integral_constant<int, 0>());
+          dots(c + 1, std::integral_constant<int, 1>());
         }
         float ds = 0.0f, p = 0.0f;
         if (valid && h < H) {

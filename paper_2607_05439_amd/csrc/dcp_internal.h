@@ -251,7 +251,7 @@ struct LayerNormBackArgs {
 
 // Backward pass of the attention (backward.hip). Rows are those of the stripe;
 // [H][n_q][dp] holds a head's channels padded with zeros to dp.
-constexpr int kBackMaxGroups = 768;  // workgroups (one T each) of the general pair kernel: three fit a CU
+constexpr int kBackMaxGroups = 512;  // workgroups (one T each) of the general pair kernel: two fit a CU
 
 struct BackRowsArgs {
   int64_t n_q;
