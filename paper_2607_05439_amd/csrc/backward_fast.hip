@@ -14,7 +14,8 @@
 // range is served by powers of two: every tensor is scaled so that its largest
 // magnitude lies in [2^11, 2^12) (P, at most 1, by 2^14; dS then by what keeps it below
 // 2^16), fp16 holds 11 bits down to 2^-26 of that, and the fp32 results are scaled
-// back exactly. Only z enters as the bf16 it is, against bias weights split into
+// back exactly. Every row of dout has a power of its own for what stays in the row (dS,
+// dz, dq), and joins the others at the tensor's where rows are summed. Only z enters as the bf16 it is, against bias weights split into
 // bf16 hi + lo (pair_bias.h).
 #include <hip/hip_runtime.h>
 #include <math.h>
@@ -61,7 +62,8 @@ __device__ __forceinline__ int scale_exp(float top) {
 }
 
 // ----------------------------------------------------------------------------- weights, dout
-// Block 0: the bias weights. Blocks 1 .. kBackTops: the largest |dout| of a share each.
+// Block 0: the bias weights. Blocks 1 .. kBackTops: the largest |dout| of each row and of a
+// share of the rows.
 // The others: the projections' weights split into bf16 hi + lo, four a thread.
 __global__ void __launch_bounds__(256) prep_kernel(FastBackArgs a) {
   const int tid = threadIdx.x, lane = tid & 63;
@@ -78,21 +80,34 @@ __global__ void __launch_bounds__(256) prep_kernel(FastBackArgs a) {
     return;
   }
   if (blockIdx.x > 0) {
-    const int64_t n8 = a.n_q * kHD / 8;  // 16-byte pieces of bf16, pairs of them of fp32
+    // 16 lanes a row, 24 channels a lane
+    const int sub = tid & 15;
     float top = 0.0f;
-    for (int64_t x = (int64_t)(blockIdx.x - 1) * 256 + tid; x < n8; x += (int64_t)kBackTops * 256) {
-      if (a.dout_bf16) {
-        const u32x4 r = reinterpret_cast<const u32x4*>(a.dout)[x];
+    for (int64_t r = (int64_t)(blockIdx.x - 1) * 16 + (tid >> 4); r < a.nq_pad; r += 16 * kBackTops) {
+      float row_top = 0.0f;
+      if (r < a.n_q) {
+        if (a.dout_bf16) {
+          const u32x4* from = reinterpret_cast<const u32x4*>(static_cast<const uint16_t*>(a.dout) + r * kHD) + sub;
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
-          top = fmaxf(top, fmaxf(fabsf(__uint_as_float(r[i] << 16)), fabsf(__uint_as_float(r[i] & 0xFFFF0000u))));
-      } else {
+          for (int x = 0; x < kHD / 128; ++x) {
+            const u32x4 v = from[16 * x];
 #pragma unroll
-        for (int j = 0; j < 2; ++j) {
-          const f32x4 r = reinterpret_cast<const f32x4*>(a.dout)[2 * x + j];
-          top = fmaxf(top, fmaxf(fmaxf(fabsf(r[0]), fabsf(r[1])), fmaxf(fabsf(r[2]), fabsf(r[3]))));
+            for (int i = 0; i < 4; ++i)
+              row_top = fmaxf(row_top, fmaxf(fabsf(__uint_as_float(v[i] << 16)), fabsf(__uint_as_float(v[i] & 0xFFFF0000u))));
+          }
+        } else {
+          const f32x4* from = reinterpret_cast<const f32x4*>(static_cast<const float*>(a.dout) + r * kHD) + sub;
+#pragma unroll
+          for (int x = 0; x < kHD / 64; ++x) {
+            const f32x4 v = from[16 * x];
+            row_top = fmaxf(row_top, fmaxf(fmaxf(fabsf(v[0]), fabsf(v[1])), fmaxf(fabsf(v[2]), fabsf(v[3]))));
+          }
         }
+#pragma unroll
+        for (int o = 8; o > 0; o >>= 1) row_top = fmaxf(row_top, __shfl_xor(row_top, o));
       }
+      if (sub == 0) a.row_exp[r] = scale_exp(row_top);
+      top = fmaxf(top, row_top);
     }
 #pragma unroll
     for (int o = 32; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor(top, o));
@@ -166,11 +181,13 @@ __device__ __forceinline__ void pack_row(const float (&x)[kD], int e2, PackTile&
 #pragma unroll
   for (int j = 0; j < 4; ++j) to.w[tok][j] = __builtin_bit_cast(u32x4, v[j]);
 }
-__device__ __forceinline__ void pack_out(const PackTile& t, int h, int64_t tile, int64_t padded, int lane, uint16_t* rows,
-                                         uint16_t* transposed) {
+__device__ __forceinline__ void pack_out(const PackTile& t, int h, int64_t tile, int64_t padded, int lane, uint16_t* rows) {
   const int64_t at = ((int64_t)h * (padded >> 4) + tile) * 64 + lane;  // 1 KB per head and tile in both layouts
   reinterpret_cast<u32x4*>(rows)[at] = (&t.w[0][0])[lane];
-  if (!transposed) return;
+}
+__device__ __forceinline__ void pack_transposed(const PackTile& t, int h, int64_t tile, int64_t padded, int lane,
+                                                uint16_t* transposed) {
+  const int64_t at = ((int64_t)h * (padded >> 4) + tile) * 64 + lane;
   const int n = lane & 15, g = lane >> 4;
   const uint32_t from = lds_addr(&t) + 64 * (4 * g + (n >> 2)) + 8 * (n & 3);
   const u32x2 a = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4)(uintptr_t)from));
@@ -179,7 +196,7 @@ __device__ __forceinline__ void pack_out(const PackTile& t, int h, int64_t tile,
 }
 
 __global__ void __launch_bounds__(64) pack_kernel(FastBackArgs a) {
-  __shared__ PackTile s_x[4], s_y[4];
+  __shared__ PackTile s_x[4], s_y[4], s_t[4];  // q or k; do or v; do at the tensor's power
   const int lane = threadIdx.x, h = 4 * blockIdx.y + (lane >> 4);
   const bool is_row = blockIdx.x < a.nq_pad / 16;
   const int64_t tile = (int64_t)blockIdx.x - (is_row ? 0 : a.nq_pad / 16), tok = tile * 16 + (lane & 15);
@@ -189,6 +206,7 @@ __global__ void __launch_bounds__(64) pack_kernel(FastBackArgs a) {
   for (int x = 0; x < 4; ++x) tops[x] = __uint_as_float(a.tops[kBackTops * x + lane]);
   f32x4 in[4][kD / 4];  // rows: q, g, acc, dout; keys: k, v
   float l = 0.0f, m = 0.0f;
+  const int er = is_row ? a.row_exp[tok] : 0;  // the power of two of the row's do
   const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
   const int64_t at = tok * kHD + h * kD;
   const bool there = is_row ? tok < a.n_q : tok < a.n_tok && (!a.mask || a.mask[tok] != 0);
@@ -256,7 +274,9 @@ __global__ void __launch_bounds__(64) pack_kernel(FastBackArgs a) {
       }
     }
     a.lse[(int64_t)h * a.nq_pad + tok] = l == 0.0f ? INFINITY : fmaf(m, kLog2e, log2f(l));  // rows past the last: l = 0
-    a.dot[(int64_t)h * a.nq_pad + tok] = ldexpf(dot, e2[2] + e2[3]);
+    a.dot[(int64_t)h * a.nq_pad + tok] = ldexpf(dot, e2[2] + er);
+    if (h == 0) a.row_scale[tok] = ldexpf(1.0f, e2[3] - er);
+    pack_row(y, e2[3], s_t[lane >> 4], lane & 15);
   } else {
 #pragma unroll
     for (int e = 0; e < kD; ++e) x[e] = in[0][e / 4][e % 4], y[e] = in[1][e / 4][e % 4];
@@ -264,17 +284,20 @@ __global__ void __launch_bounds__(64) pack_kernel(FastBackArgs a) {
     if (blockIdx.y == 0 && lane == 0) a.tile_valid[tile] = bits;
   }
   pack_row(x, e2[is_row ? 0 : 1], s_x[lane >> 4], lane & 15);
-  pack_row(y, e2[is_row ? 3 : 2], s_y[lane >> 4], lane & 15);
+  pack_row(y, is_row ? er : e2[2], s_y[lane >> 4], lane & 15);
   __syncthreads();
 #pragma unroll
   for (int j = 0; j < 4; ++j) {
     const int hh = 4 * blockIdx.y + j;
     if (is_row) {
-      pack_out(s_x[j], hh, tile, a.nq_pad, lane, a.qf, a.qt);
-      pack_out(s_y[j], hh, tile, a.nq_pad, lane, a.of, a.ot);
+      pack_out(s_x[j], hh, tile, a.nq_pad, lane, a.qf);
+      pack_transposed(s_x[j], hh, tile, a.nq_pad, lane, a.qt);
+      pack_out(s_y[j], hh, tile, a.nq_pad, lane, a.of);
+      pack_transposed(s_t[j], hh, tile, a.nq_pad, lane, a.ot);
     } else {
-      pack_out(s_x[j], hh, tile, a.n_pad, lane, a.kf, a.kt);
-      pack_out(s_y[j], hh, tile, a.n_pad, lane, a.vf, nullptr);
+      pack_out(s_x[j], hh, tile, a.n_pad, lane, a.kf);
+      pack_transposed(s_x[j], hh, tile, a.n_pad, lane, a.kt);
+      pack_out(s_y[j], hh, tile, a.n_pad, lane, a.vf);
     }
   }
 }
@@ -307,6 +330,8 @@ struct PairLds {
   u32x4 w[8][64];                      // 8 KB: bias weights, hi then lo
   u32x2 wt[8][64];                     // 4 KB: W'' for dz
   float stat[kH][kTileQ][2];           // 2 KB: log-sum-exp and D of the rows
+  float row_scale[kTileQ];             // from a row's power of two to the tensor's
+  int row_exp[kTileQ];                 // the power of two of a row's dS
 };
 
 __global__ void __launch_bounds__(256, 2) pairs_kernel(FastBackArgs a) {
@@ -323,7 +348,6 @@ __global__ void __launch_bounds__(256, 2) pairs_kernel(FastBackArgs a) {
   uint32_t bits = t_begin < t_end ? a.tile_valid[t_begin] : 0u;
   const int eq = a.exps[0], ek = a.exps[1], ev = a.exps[2], ed = a.exps[3], ew = a.exps[4];
   const float s_scale = ldexpf(1.0f, -eq - ek);
-  const int ds_exp = ev + ed - kDsShift;          // the stored dS is dS 2^ds_exp
   const float t_scale = ldexpf(kLn2 / kCz, ew);   // sum dS b (base 2) -> t, in dzh's units
   f16x4 id;
 #pragma unroll
@@ -363,6 +387,10 @@ __global__ void __launch_bounds__(256, 2) pairs_kernel(FastBackArgs a) {
     }
     s.stat[tid >> 4][n][0] = a.lse[at];
     s.stat[tid >> 4][n][1] = a.dot[at];
+    if (tid < kTileQ) {
+      s.row_scale[n] = a.row_scale[q0 + n];
+      s.row_exp[n] = a.row_exp[q0 + n] + ev - kDsShift;
+    }
   }
   f32x4 dq[kHw][2], T[8];
   const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
@@ -426,7 +454,9 @@ __global__ void __launch_bounds__(256, 2) pairs_kernel(FastBackArgs a) {
       f32x4 p, ds;
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        p[i] = __builtin_amdgcn_exp2f(fmaf(x[i], s_scale, bias[i] - lse));
+        // at most 1: logits in the thousands, which the forward forms in bf16, differ from its
+        // sum by so much that P would leave fp16's range (NaN stays)
+        p[i] = __builtin_elementwise_minimum(__builtin_amdgcn_exp2f(fmaf(x[i], s_scale, bias[i] - lse)), 1.0f);
         ds[i] = p[i] * (dp[i] - dot) * (1.0f / (1 << kDsShift));
         p[i] *= (float)(1 << kPShift);
         tp[i] = fmaf(ds[i], p[i] == 0.0f ? 0.0f : bias[i], tp[i]);
@@ -455,8 +485,8 @@ __global__ void __launch_bounds__(256, 2) pairs_kernel(FastBackArgs a) {
       const bool valid = (bits >> k) & 1u;
       const f16x4 d8 = __builtin_bit_cast(f16x4, s.ds[k][n][g]);
       const float tt = ((s.t[0][k][n] + s.t[1][k][n]) + (s.t[2][k][n] + s.t[3][k][n])) * t_scale;
-      const f16x4 dst = to_f16(mfma16h(d8, id, zero));
-      const float shift = -mu[kk] * rstd[kk], out_scale = ldexpf(rstd[kk], -ds_exp - ew);
+      const f16x4 dst = to_f16(mfma16h(d8, id, zero) * *reinterpret_cast<const f32x4*>(&s.row_scale[4 * g]));
+      const float shift = -mu[kk] * rstd[kk], out_scale = ldexpf(rstd[kk], -s.row_exp[n] - ew);
 #pragma unroll
       for (int x = 0; x < 4; ++x) {
         bf16x8 r;
@@ -503,7 +533,7 @@ __global__ void __launch_bounds__(256, 2) pairs_kernel(FastBackArgs a) {
         if (u == 1 && g >= 2) break;  // channels 24 .. 31
         f32x4 v;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) v[i] = ldexpf(dq[j][u][i] * kInvSqrtD, -ds_exp - ek);
+        for (int i = 0; i < 4; ++i) v[i] = ldexpf(dq[j][u][i] * kInvSqrtD, -s.row_exp[n] - ek);
         *reinterpret_cast<f32x4*>(to + 16 * u + 4 * g) = v;
       }
     }
@@ -528,7 +558,7 @@ __global__ void __launch_bounds__(256, 2) pairs_kernel(FastBackArgs a) {
   }
   float* to = a.t_parts + ((int64_t)blockIdx.y * gridDim.x + blockIdx.x) * kH * kCz;
   for (int x = tid; x < kH * kCz; x += 256) {
-    const float v = ldexpf(st[x], -ds_exp);
+    const float v = ldexpf(st[x], kDsShift - ev - ed);
     to[x] = a.first ? v : to[x] + v;
   }
 }
@@ -557,7 +587,7 @@ __global__ void __launch_bounds__(256, 3) keys_kernel(FastBackArgs a) {
   // a row tile's operands, loaded one step ahead
   u32x2 x[4];
   u32x4 qt, ot, of;
-  f32x4 dt;
+  f32x4 dt, rs;
   auto load = [&](int64_t r) {
     const int64_t row_tile = (int64_t)h * (a.nq_pad >> 4) + (a.row0 >> 4) + r;
     const u32x2* pp = a.p + (((int64_t)h * (a.chunk_pad >> 4) + r) * n_tiles + t0) * 64 + lane;
@@ -567,6 +597,7 @@ __global__ void __launch_bounds__(256, 3) keys_kernel(FastBackArgs a) {
     ot = reinterpret_cast<const u32x4*>(a.ot)[row_tile * 64 + lane];
     of = reinterpret_cast<const u32x4*>(a.of)[row_tile * 64 + 4 * n + g];
     dt = *reinterpret_cast<const f32x4*>(a.dot + row_tile * 16 + 4 * g);
+    rs = *reinterpret_cast<const f32x4*>(a.row_scale + a.row0 + r * 16 + 4 * g);
   };
   if (wave < count) load(first + wave);
   for (int64_t r = first + wave; r < first + count; r += 4) {
@@ -574,7 +605,7 @@ __global__ void __launch_bounds__(256, 3) keys_kernel(FastBackArgs a) {
                          __builtin_bit_cast(f16x4, x[3])};
     const u32x4 q = qt, og = ot;
     const f16x8 o = as_f16x8(of);
-    const f32x4 dot = dt;
+    const f32x4 dot = dt, scale = rs * (1.0f / (1 << (kDsShift + kPShift)));  // dS at the tensor's power of two
     if (r + 4 < first + count) load(r + 4);
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
@@ -583,7 +614,7 @@ __global__ void __launch_bounds__(256, 3) keys_kernel(FastBackArgs a) {
       const f16x4 p = pk[k];
       f32x4 d;
 #pragma unroll
-      for (int i = 0; i < 4; ++i) d[i] = (float)p[i] * ((dp[i] - dot[i]) * (1.0f / (1 << (kDsShift + kPShift))));
+      for (int i = 0; i < 4; ++i) d[i] = (float)p[i] * ((dp[i] - dot[i]) * scale[i]);
       const f16x4 ds = to_f16(d);
 #pragma unroll
       for (int u = 0; u < 2; ++u) {

@@ -1131,7 +1131,7 @@ struct BackLayout {
   int64_t chunk, nq_pad, n_pad;  // chunk: rows at a time
   int dp, dq_parts, t_parts, kv_splits, ds_splits, w_splits;
   // projections, general and fused rows' operands, fused keys' operands
-  size_t off_q, off_k, off_v, off_g, off_qp, off_dop, off_kp, off_vp, off_stat, off_qf, off_qt, off_of, off_ot, off_lse, off_dot, off_kf,
+  size_t off_q, off_k, off_v, off_g, off_qp, off_dop, off_kp, off_vp, off_stat, off_qf, off_qt, off_of, off_ot, off_lse, off_dot, off_rexp, off_rscale, off_kf,
       off_kt, off_vf, off_tv, off_tops, off_exps, off_wops, off_wsplit;
   size_t off_p, off_ds, off_dq_parts, off_t_parts, off_kv_parts, off_dq, off_dkv, off_dg, off_t, off_ds_parts, off_w_parts,
       total;
@@ -1184,6 +1184,8 @@ void back_layout(const dcp_shape* sh, Path path, int64_t n_q, BackLayout* L) {
     for (size_t* o : {&L->off_kf, &L->off_kt, &L->off_vf}) *o = take(keys);
     L->off_lse = take((size_t)H * L->nq_pad * 4);
     L->off_dot = take((size_t)H * L->nq_pad * 4);
+    L->off_rexp = take((size_t)L->nq_pad * 4);
+    L->off_rscale = take((size_t)L->nq_pad * 4);
     L->off_tv = take((size_t)(L->n_pad / 16) * 4);
     L->off_tops = take(4 * dcp::kBackTops * 4);
     L->off_exps = take(5 * 4);
@@ -1340,6 +1342,8 @@ int dcp_pair_bias_attention_backward(const dcp_shape* shape, const dcp_weights* 
     ba.vf = half(L.off_vf);
     ba.lse = at(L.off_lse);
     ba.dot = at(L.off_dot);
+    ba.row_exp = reinterpret_cast<int32_t*>(ws + L.off_rexp);
+    ba.row_scale = at(L.off_rscale);
     ba.w[0] = w->w_q;
     ba.w[1] = w->w_k;
     ba.w[2] = w->w_v;

@@ -310,6 +310,8 @@ struct FastBackArgs {
   u32x4* w_ops;            // [768]: bias weights, W''
   uint16_t *qf, *qt, *of, *ot, *kf, *kt, *vf;
   float *lse, *dot;        // [H][nq_pad]
+  int32_t* row_exp;        // [nq_pad]: the power of two of each row's do
+  float* row_scale;        // [nq_pad]: from there to the tensor's
   const float* w[4];       // W_q, W_k, W_v, W_g [384][c_s]
   int32_t c_s;
   uint16_t *w_split, *dg;  // [2][4][384][c_s], [2][n_q][384]: bf16 hi, then lo

@@ -217,6 +217,48 @@ def test_gradients_of_any_size(widths, tol, scale):
 
 
 @pytest.mark.parametrize("widths,tol", [(F32, 2e-5), (BF16, 1e-2)], ids=["f32", "bf16"])
+def test_rows_of_dout_of_any_size(widths, tol):
+    """Rows of dout 2^0 to 2^-60 of the largest, and one of zeros: dz of every row to the tolerance by
+    itself, the shared gradients as a whole."""
+    import torch
+    x = make(64, 3, 50, **widths, masked=4, seed=18)
+    x["dout"] = x["dout"] * 2.0 ** (-60 * ((torch.arange(50) * 7) % 50) / 49).floor()[:, None].to(x["dout"].dtype)
+    x["dout"][20] = 0
+    want, got = reference(x), Call(x)()
+    check(got, want, tol)
+    err = (got["dz"].cpu().double() - want["dz"]).flatten(1).norm(dim=1)
+    assert (err <= tol * want["dz"].flatten(1).norm(dim=1)).all(), err / want["dz"].flatten(1).norm(dim=1)
+
+
+@pytest.mark.parametrize("widths", [F32, BF16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("bad", [float("nan"), float("inf")])
+def test_a_row_of_dout_that_is_not_finite(widths, bad):
+    """It is kept to what it meets: dz of the other rows has the bits it has without it, and its own
+    and the shared gradients are not finite."""
+    import torch
+    x = make(40, 0, 20, **widths, seed=19)
+    want = Call(x)()
+    x["dout"][7, 3] = bad
+    got = Call(x)()
+    others = [r for r in range(20) if r != 7]
+    assert torch.equal(got["dz"][others], want["dz"][others])
+    assert not torch.isfinite(got["dz"][7]).any() and not all(torch.isfinite(got[k]).all() for k in ("w_q", "w_k"))
+    assert not torch.isfinite(got["w_v"]).all() and not torch.isfinite(got["w_g"]).all()
+
+
+@pytest.mark.parametrize("widths", [F32, BF16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("factor", [2.0 ** 7, 2.0 ** 10, 2.0 ** 14])
+def test_logits_in_the_thousands(widths, factor):
+    """The softmax picks one key of each row and a forward in bf16 may pick another than fp32 logits
+    do: gradients stay finite."""
+    import torch
+    x = make(60, 0, 60, **widths, masked=1, seed=20)
+    x["w_q"] = x["w_q"] * factor
+    for k, v in Call(x)().items():
+        assert torch.isfinite(v).all(), k
+
+
+@pytest.mark.parametrize("widths,tol", [(F32, 2e-5), (BF16, 1e-2)], ids=["f32", "bf16"])
 def test_weights_of_other_sizes(widths, tol):
     """Projections whose outputs are tiny or large: q small and k large (their product stays), v large."""
     x = make(50, 0, 50, **widths, seed=4)
@@ -263,6 +305,43 @@ def test_stripes_add_up(widths, tol):
         for k in NAMES[1:]:
             total[k] += got[k].cpu().double()
     check(total, want, tol)
+
+
+@pytest.mark.parametrize("n,widths", [(4200, dict(dtype="bf16", c_s=16, c_z=256, h=2, d=8)), (6000, BF16)],
+                         ids=["general", "fused"])
+def test_a_layer_of_more_than_2_32_pair_channels(n, widths):
+    """All rows at once, in several chunks of rows, from one state: dz is that of two stripes' calls (up
+    to a last bit of bf16, 2^-7 of the value), and the shared gradients are the stripes' sums (fp32 sums
+    in another order: the tolerance of fp32)."""
+    import torch
+    c_z, h, d = widths["c_z"], widths["h"], widths["d"]
+    assert n * n * c_z > 2 ** 32
+    x = make(n, 0, 1, **widths, masked=70, seed=21)
+    gen = torch.Generator("cuda").manual_seed(22)
+    x["z"] = torch.empty((n, n, c_z), dtype=torch.bfloat16, device="cuda")
+    for r in range(0, n, 600):
+        x["z"][r:r + 600] = torch.randn(x["z"][r:r + 600].shape, generator=gen, device="cuda")
+    x["dout"] = torch.randn((n, h * d), generator=gen, device="cuda").bfloat16()
+
+    def stripe(row0, rows):
+        part = {**x, "z": x["z"][row0:row0 + rows], "dout": x["dout"][row0:row0 + rows].contiguous()}
+        part["dims"] = (n, row0, rows) + x["dims"][3:]
+        return Call(part, grad_dtype=0)
+
+    whole = stripe(0, n)
+    got = whole()
+    total = {k: torch.zeros_like(got[k]) for k in NAMES[1:]}
+    for row0, end in ((0, 1001), (1001, n)):
+        call = stripe(row0, end - row0)
+        call.m, call.l, call.acc = (whole.m[:, row0:end].contiguous(), whole.l[:, row0:end].contiguous(),
+                                    whole.acc[row0:end].clone())
+        part = call()
+        for r in range(row0, end, 500):
+            a, b = got["dz"][r:min(r + 500, end)].float(), part["dz"][r - row0:min(r + 500, end) - row0].float()
+            assert b.any() and float((a - b).norm()) <= 2.0 ** -7 * float(b.norm()), r
+        for k in total:
+            total[k] += part[k]
+    check({k: got[k] for k in total}, {k: v.cpu().double() for k, v in total.items()}, 2e-5)
 
 
 @pytest.mark.parametrize("widths", [F32, BF16], ids=["f32", "bf16"])
