@@ -204,8 +204,8 @@ typedef struct {
 int dcp_pair_bias_attention_backward_workspace_size(const dcp_shape* shape, int64_t n_q, size_t* bytes);
 
 /* Gradients of the query stripe [q_row0, q_row0 + n_q) of
- * dcp_pair_bias_attention (without rows: zeros). shape, weights, s, z_rows and key_mask are the
- * forward's (out_dtype is the type of dout).
+ * dcp_pair_bias_attention (without rows: zeros, and the rows' pointers may be NULL).
+ * shape, weights, s, z_rows and key_mask are the forward's (out_dtype is the type of dout).
  *   m, l, acc   [H, n_q], [H, n_q], [n_q, H, d] fp32: the stripe's softmax state
  *               over all keys, as dcp_pair_bias_attention_partial writes it for
  *               [0, N) or dcp_block_merge for the parts of a ring; 16-byte aligned.
@@ -215,8 +215,13 @@ int dcp_pair_bias_attention_backward_workspace_size(const dcp_shape* shape, int6
  *               gated output
  *   workspace   at least dcp_pair_bias_attention_backward_workspace_size() bytes,
  *               256-byte aligned; contents on entry are ignored
- * Supported shapes, alignment of the weights and precision are the forward's:
- * fp32 arithmetic throughout on the general path. */
+ * Supported shapes and alignment of the weights are the forward's. Precision: fp32
+ * arithmetic throughout on the general path. The fused path multiplies in fp16 (11
+ * significant bits) with fp32 sums: q, k, v and the rows of dout each scaled by a power
+ * of two so that the largest magnitude (of a row of dout: its own) has the most range,
+ * 26 binades below which bits are lost; z with split weights as the forward, and the
+ * products with s and the projections' weights in bf16 pairs of 16 bits. P and sums
+ * over rows are the state's: a logit that the forward formed otherwise moves them. */
 int dcp_pair_bias_attention_backward(const dcp_shape* shape, const dcp_weights* weights, const void* s,
                                      const void* z_rows, const uint8_t* key_mask, int64_t q_row0, int64_t n_q,
                                      const float* m, const float* l, const float* acc, const void* dout,

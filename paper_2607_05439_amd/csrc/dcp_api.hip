@@ -1257,7 +1257,7 @@ int dcp_pair_bias_attention_backward(const dcp_shape* shape, const dcp_weights* 
   if (!w || !grads) return fail(DCP_ERR_INVALID_ARGUMENT, "weights and gradients are required");
   if (!w->w_q || !w->w_k || !w->w_v || !w->w_g || !w->w_b)
     return fail(DCP_ERR_INVALID_ARGUMENT, "w_q, w_k, w_v, w_g and w_b are required");
-  if (!s || !z_rows || !m || !l || !acc || !dout)
+  if (n_q > 0 && (!s || !z_rows || !m || !l || !acc || !dout))
     return fail(DCP_ERR_INVALID_ARGUMENT, "s, z_rows, m, l, acc and dout are required");
   if (grads->dtype != DCP_F32 && grads->dtype != DCP_BF16)
     return fail(DCP_ERR_INVALID_ARGUMENT, "the gradients' dtype must be DCP_F32 or DCP_BF16");
@@ -1265,7 +1265,7 @@ int dcp_pair_bias_attention_backward(const dcp_shape* shape, const dcp_weights* 
                        grads->dln_gamma};
   bool any = false;
   for (void* p : out) any = any || p;
-  if (!any) return fail(DCP_ERR_INVALID_ARGUMENT, "no gradient is asked for");
+  if (!any && n_q > 0) return fail(DCP_ERR_INVALID_ARGUMENT, "no gradient is asked for");
   if (!aligned(s, 16) || !aligned(z_rows, 16) || !aligned(dout, 16) || !aligned(m, 16) || !aligned(l, 16) || !aligned(acc, 16))
     return fail(DCP_ERR_INVALID_ARGUMENT, "s, z_rows, m, l, acc and dout must be 16-byte aligned");
   for (void* p : out)

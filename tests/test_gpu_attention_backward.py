@@ -356,6 +356,13 @@ def test_a_stripe_without_rows(widths):
                                          g["dout"], grads, None, 0)
     torch.cuda.synchronize()
     assert all(not out[k].any() for k in NAMES[1:])
+    # as empty tensors, whose addresses are NULL
+    empty, out = torch.empty(0, device="cuda"), call.outputs()
+    grads = dcp.make_gradients(empty, *[out[k] for k in NAMES[1:]], dtype=call.grad_code)
+    dcp.dcp_pair_bias_attention_backward(call.shape, call.weights, g["s"], empty, None, 20, 0, empty, empty, empty, empty,
+                                         grads, None, 0)
+    torch.cuda.synchronize()
+    assert all(not out[k].any() for k in NAMES[1:])
 
 
 @pytest.mark.parametrize("widths", [F32, BF16], ids=["f32", "bf16"])
@@ -416,6 +423,28 @@ def test_captured_and_replayed(widths):
         step()
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(got, results()))
+
+
+@pytest.mark.parametrize("widths", [F32, BF16], ids=["f32", "bf16"])
+def test_two_graphs_share_a_workspace(widths):
+    """Two layers' backward passes of different sizes, each captured with the same workspace and replayed
+    in turn on one stream: the bits of eager calls."""
+    import torch
+    calls = [Call(make(90, 0, 90, **widths, masked=3, seed=30)), Call(make(50, 10, 17, **widths, seed=31))]
+    want, outs = [c() for c in calls], [c.outputs() for c in calls]
+    ws = max((c.workspace() for c in calls), key=lambda t: t.numel())
+    torch.cuda.synchronize()
+    graphs = []
+    for call, out in zip(calls, outs):
+        graphs.append(torch.cuda.CUDAGraph())
+        with torch.cuda.graph(graphs[-1]):
+            call(ws=ws, out=out)
+    for i in (0, 1, 1, 0, 1):
+        for v in outs[i].values():
+            v.fill_(7.0)
+        graphs[i].replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(outs[i][k], want[i][k]) for k in NAMES)
 
 
 def test_a_training_step_against_the_definition():

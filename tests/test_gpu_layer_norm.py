@@ -219,3 +219,33 @@ def test_replayed_on_another_stream():
         torch.cuda.synchronize()
         assert torch.equal(y, forward(x, gamma, beta, "bf16"))
         assert all(torch.equal(a, b) for a, b in zip((dx, dg, db), backward(x, gamma, dy)))
+
+
+def test_more_than_2_32_elements():
+    """2^25 + 3 rows of 128: the last rows have the bits of a call on them alone, in place as well, and the
+    sums over the rows are those in 64 bits: a chain of 2^25 / 2^14 additions leaves at most 2^-24 sqrt(2^11)
+    of a partial sum, 3e-6, and 1e-5 is asserted of the norm."""
+    import torch
+    rows, c = 2 ** 25 + 3, 128
+    gen = torch.Generator("cuda").manual_seed(5)
+    x, dy = (torch.empty((rows, c), dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    for r in range(0, rows, 2 ** 22):
+        for t in (x, dy):
+            t[r:r + 2 ** 22] = torch.randn(t[r:r + 2 ** 22].shape, generator=gen, device="cuda")
+    gamma, beta = (torch.rand(c, generator=gen, device="cuda") + 0.5 for _ in range(2))
+    want = [torch.zeros(c, dtype=torch.float64, device="cuda") for _ in range(2)]
+    for r in range(0, rows, 2 ** 20):
+        a, b = x[r:r + 2 ** 20].double(), dy[r:r + 2 ** 20].double()
+        a -= a.mean(dim=1, keepdim=True)
+        a /= torch.sqrt((a ** 2).mean(dim=1, keepdim=True) + EPS)
+        want[0] += (a * b).sum(dim=0)
+        want[1] += b.sum(dim=0)
+    tail = slice(rows - 1000, rows)
+    y_tail = forward(x[tail].clone(), gamma, beta, "bf16")
+    dx_tail = backward(x[tail].clone(), gamma, dy[tail].clone())[0]
+    dx, dgamma, dbeta = backward(x, gamma, dy)
+    assert torch.equal(dx[tail], dx_tail)
+    for got, sum64 in zip((dgamma, dbeta), want):
+        assert float((got.double() - sum64).norm()) <= 1e-5 * float(sum64.norm())
+    del dx, dy
+    assert torch.equal(forward(x, gamma, beta, "bf16", out=x)[tail], y_tail)
