@@ -77,18 +77,20 @@ __device__ __forceinline__ float quad_sum(float x) {
 // Eight lanes per row and head: do, q in padded rows of dp floats per head, the
 // statistics {m, 1 / L, D, -}, and dg. A row without keys (L = 0) gets weights of 0. All
 // loads before the first store, which the compiler could not tell from them. The
-// blocks behind those lay out k and v in padded rows too, with zeros for masked keys,
-// which may hold anything, so that a weight of 0 times them is 0.
+// blocks behind those lay out k and v, with zeros for masked keys, which may hold
+// anything, so that a weight of 0 times them is 0: k in padded rows for dq, both as the
+// pair kernel's lanes read them, [heads / 4][keys / 16][dp / 4][16 keys][4 heads][4] with
+// zeros for the heads and keys that are not there.
 __global__ void __launch_bounds__(256) back_rows_kernel(BackRowsArgs a) {
   constexpr int kMost = kGenMaxD / 8;
   if (blockIdx.x >= a.row_blocks) {
-    // a piece of four channels a thread: [H][N][dp / 4]
+    // a piece of four channels a thread
     const int64_t x = (int64_t)(blockIdx.x - a.row_blocks) * 256 + threadIdx.x;
-    const int pieces = a.dp / 4, c = 4 * (int)(x % pieces);
-    const int64_t hj = x / pieces, j = hj % a.n_tok;
-    const int h = (int)(hj / a.n_tok);
-    if (h >= a.n_heads) return;
-    const bool valid = !a.mask || a.mask[j] != 0;
+    const int pieces = a.dp / 4, piece = (int)(x % pieces), c = 4 * piece;
+    const int64_t n_keys = back_keys_padded(a.n_tok), hj = x / pieces, j = hj % n_keys;
+    const int h = (int)(hj / n_keys);
+    if (h >= back_heads_padded(a.n_heads)) return;
+    const bool here = h < a.n_heads && j < a.n_tok, valid = here && (!a.mask || a.mask[j] != 0);
     const int64_t at = (j * a.n_heads + h) * a.head_dim;
     f32x4 k = {0.f, 0.f, 0.f, 0.f}, v = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
@@ -97,8 +99,10 @@ __global__ void __launch_bounds__(256) back_rows_kernel(BackRowsArgs a) {
         k[i] = a.k[at + c + i];
         v[i] = a.v[at + c + i];
       }
-    reinterpret_cast<f32x4*>(a.kp)[x] = k;
-    reinterpret_cast<f32x4*>(a.vp)[x] = v;
+    const int64_t to = (((h >> 2) * (n_keys >> 4) + (j >> 4)) * pieces + piece) * 64 + 4 * (j & 15) + (h & 3);
+    if (here) reinterpret_cast<f32x4*>(a.kr)[((int64_t)h * a.n_tok + j) * pieces + piece] = k;
+    reinterpret_cast<f32x4*>(a.kp)[to] = k;
+    reinterpret_cast<f32x4*>(a.vp)[to] = v;
     return;
   }
   const int64_t t = ((int64_t)blockIdx.x * 256 + threadIdx.x) >> 3;
@@ -140,7 +144,6 @@ __global__ void __launch_bounds__(256) back_rows_kernel(BackRowsArgs a) {
 // and dz, and its heads for the logits and dS; T is then a sum over the tile's keys
 // by output element, written once per workgroup. CT: pieces of 16 channels of z; NH:
 // heads per lane.
-constexpr int kBackKeys = 64;
 constexpr int kHeadStride = kGenMaxD + 4;
 
 // Four consecutive elements from i0 of a row of len as loaded: whole pieces (len a
@@ -202,6 +205,19 @@ __global__ void __launch_bounds__(256, CT <= 8 && CT * NH < 32 ? 2 : 1) back_pai
   }
   for (int x = tid; x < HP * kHeadStride; x += 256) s_q[x] = s_do[x] = 0.0f;
   __syncthreads();
+  {
+    // W' less its mean over the channels, 16 lanes a head: the bias stays (zh has no mean)
+    // and dzh has no mean either
+    const int h = tid >> 4;
+    float sum = 0.0f;
+    if (h < HP)
+      for (int c = tid & 15; c < c_z; c += 16) sum += s_w[h * CZ + c];
+#pragma unroll
+    for (int o = 8; o > 0; o >>= 1) sum += __shfl_xor(sum, o);
+    if (h < HP)
+      for (int c = tid & 15; c < c_z; c += 16) s_w[h * CZ + c] -= sum * inv_c;
+  }
+  __syncthreads();
   f32x4 w_held[kHeld ? HP : 1][kHeld ? CT : 1];
   if constexpr (kHeld)
 #pragma unroll
@@ -256,31 +272,33 @@ __global__ void __launch_bounds__(256, CT <= 8 && CT * NH < 32 ? 2 : 1) back_pai
     __syncthreads();
     for (int64_t t = t_first; t < t_end; ++t) {
       asm volatile("" ::: "memory");  // q, do and W' come from LDS again for each tile, not from registers
-      const int64_t j = t * kBackKeys + key, jj = min(j, a.n_tok - 1);
+      const int64_t j = t * kBackKeys + key;
       const bool there = j < a.n_tok, valid = there && attends != 0;
       // k and v of the lane's heads, eight channels at a time, two such pieces in flight; the
       // first head's during the statistics and the bias
       f32x4 kk[2][2], vv[2][2];
       auto load_kv = [&](int i, int c, int buf) {
-        const int64_t at = ((int64_t)min(4 * i + qd, H - 1) * a.n_tok + jj) * a.dp + 8 * c;
+        const int64_t at = (((int64_t)i * 4 * tiles + 4 * t + wave) * (a.dp >> 2) + 2 * c) * 64 + lane;
 #pragma unroll
         for (int x = 0; x < 2; ++x) {
-          kk[buf][x] = *reinterpret_cast<const f32x4*>(a.k + at + 4 * x);
-          vv[buf][x] = *reinterpret_cast<const f32x4*>(a.v + at + 4 * x);
+          kk[buf][x] = reinterpret_cast<const f32x4*>(a.k)[at + 64 * x];
+          vv[buf][x] = reinterpret_cast<const f32x4*>(a.v)[at + 64 * x];
         }
       };
       load_kv(0, 0, 0);
       load_kv(0, 1, 1);
       f32x4 zh[CT];
-      float s = 0.0f, v = 0.0f;
+      float s = 0.0f, v = 0.0f, t_sum = 0.0f;
+      const bool plain = whole && __ballot(valid) == ~0ull;  // nothing of the wave's keys to leave out
       int c4 = 4 * qd;
       asm volatile("" : "+v"(c4));  // (as above)
 #pragma unroll
       for (int m = 0; m < CT; ++m) {
         const int c = 16 * m + c4;
         zh[m] = raw[m].get();
+        if (!plain)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) zh[m][i] = valid && (whole || c + i < c_z) ? zh[m][i] : 0.0f;
+          for (int i = 0; i < 4; ++i) zh[m][i] = valid && (whole || c + i < c_z) ? zh[m][i] : 0.0f;
         s += (zh[m][0] + zh[m][1]) + (zh[m][2] + zh[m][3]);
       }
       const float mu = quad_sum(s) * inv_c;
@@ -288,7 +306,8 @@ __global__ void __launch_bounds__(256, CT <= 8 && CT * NH < 32 ? 2 : 1) back_pai
       for (int m = 0; m < CT; ++m)
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          zh[m][i] = whole || 16 * m + c4 + i < c_z ? zh[m][i] - mu : 0.0f;
+          zh[m][i] = zh[m][i] - mu;
+          if (!plain) zh[m][i] = whole || 16 * m + c4 + i < c_z ? zh[m][i] : 0.0f;
           v = fmaf(zh[m][i], zh[m][i], v);
         }
       const float rstd = valid ? 1.0f / sqrtf(fmaf(quad_sum(v), inv_c, a.eps)) : 0.0f;
@@ -300,6 +319,7 @@ __global__ void __launch_bounds__(256, CT <= 8 && CT * NH < 32 ? 2 : 1) back_pai
 #pragma unroll
       for (int i = 0; i < NH; ++i) {
         // the bias of heads 4i .. 4i + 3, summed over the quad; this lane keeps head 4i + qd
+        if (i > 0) asm volatile("" ::: "memory");  // (W' of four heads at a time)
         float b = 0.0f;
 #pragma unroll
         for (int x = 0; x < 4; ++x) {
@@ -345,6 +365,7 @@ __global__ void __launch_bounds__(256, CT <= 8 && CT * NH < 32 ? 2 : 1) back_pai
           p = stat[1] == 0.0f ? 0.0f : expf(l - stat[0]) * stat[1];
           ds = p * (((dp[0] + dp[1]) + (dp[2] + dp[3])) - stat[2]);
         }
+        t_sum = fmaf(ds, b, t_sum);
         s_ds[key * (HP + 4) + h] = ds;
         if (there && h < H) {
           const int64_t at = ((int64_t)h * a.rows + r) * a.n_tok + j;
@@ -362,13 +383,15 @@ __global__ void __launch_bounds__(256, CT <= 8 && CT * NH < 32 ? 2 : 1) back_pai
         int at = key;
         asm volatile("" : "+v"(at));  // (formed here, not held from the top)
         const int64_t off = (row * a.n_tok + t * kBackKeys + at) * c_z;
+        // dz = rstd (dzh - zh t), t = the mean of dzh zh = sum_h dS_h b_h / c_z
         f32x4 acc[CT];
-        float s1 = 0.0f, s2 = 0.0f;
+        const float t_mean = quad_sum(t_sum) * inv_c * rstd;
 #pragma unroll
         for (int m = 0; m < CT; ++m) acc[m] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int i = 0; i < NH; ++i) {
-          const f32x4 ds = *reinterpret_cast<const f32x4*>(&s_ds[key * (HP + 4) + 4 * i]);
+          if (i > 0) asm volatile("" ::: "memory");  // (W' of four heads at a time)
+          const f32x4 ds = *reinterpret_cast<const f32x4*>(&s_ds[key * (HP + 4) + 4 * i]) * rstd;
 #pragma unroll
           for (int x = 0; x < 4; ++x)
 #pragma unroll
@@ -377,22 +400,15 @@ __global__ void __launch_bounds__(256, CT <= 8 && CT * NH < 32 ? 2 : 1) back_pai
 #pragma unroll
               for (int e = 0; e < 4; ++e) acc[m][e] = fmaf(ds[x], w[e], acc[m][e]);
             }
+#pragma unroll
+          for (int m = 0; m < CT; ++m) asm volatile("" : "+v"(acc[m]));  // (summed here: W' is not held until the stores)
         }
-#pragma unroll
-        for (int m = 0; m < CT; ++m)
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            s1 += acc[m][e];  // 0 past the row's end, as W' is
-            s2 = fmaf(acc[m][e], zh[m][e], s2);
-          }
-        s1 = quad_sum(s1) * inv_c;
-        s2 = quad_sum(s2) * inv_c;
 #pragma unroll
         for (int m = 0; m < CT; ++m) {
           const int c = 16 * m + c4;
           f32x4 g;
 #pragma unroll
-          for (int e = 0; e < 4; ++e) g[e] = valid ? rstd * (acc[m][e] - s1 - zh[m][e] * s2) : 0.0f;
+          for (int e = 0; e < 4; ++e) g[e] = fmaf(-zh[m][e], t_mean, acc[m][e]);  // 0 for a key that does not attend
           if (z_vec) {
             if (c < c_z) {
               if (BF16) {
@@ -753,9 +769,9 @@ __global__ void __launch_bounds__(256) back_finish_kernel(BackFinishArgs a) {
 
 template <int CT, bool BF16>
 hipError_t pairs_go(const BackPairsArgs& a, unsigned grid, hipStream_t st) {
-  if (a.n_heads <= 4)
+  if (back_heads_padded(a.n_heads) == 4)
     hipLaunchKernelGGL((back_pairs_kernel<CT, 1, BF16>), dim3(grid), dim3(256), 0, st, a);
-  else if (a.n_heads <= 8)
+  else if (back_heads_padded(a.n_heads) == 8)
     hipLaunchKernelGGL((back_pairs_kernel<CT, 2, BF16>), dim3(grid), dim3(256), 0, st, a);
   else
     hipLaunchKernelGGL((back_pairs_kernel<CT, 4, BF16>), dim3(grid), dim3(256), 0, st, a);
@@ -773,7 +789,7 @@ unsigned blocks_of(int64_t items) { return (unsigned)((items + 255) / 256); }
 hipError_t launch_back_rows(const BackRowsArgs& a, hipStream_t st) {
   BackRowsArgs b = a;
   b.row_blocks = blocks_of(8 * a.n_q * a.n_heads);
-  const unsigned key_blocks = blocks_of(a.n_tok * a.n_heads * (a.dp / 4));
+  const unsigned key_blocks = blocks_of(back_keys_padded(a.n_tok) * back_heads_padded(a.n_heads) * (a.dp / 4));
   hipLaunchKernelGGL(back_rows_kernel, dim3(b.row_blocks + key_blocks), dim3(256), 0, st, b);
   return hipGetLastError();
 }

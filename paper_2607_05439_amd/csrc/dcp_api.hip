@@ -1131,7 +1131,7 @@ struct BackLayout {
   int64_t chunk, nq_pad, n_pad;  // chunk: rows at a time
   int dp, dq_parts, t_parts, kv_splits, ds_splits, w_splits;
   // projections, general and fused rows' operands, fused keys' operands
-  size_t off_q, off_k, off_v, off_g, off_qp, off_dop, off_kp, off_vp, off_stat, off_qf, off_qt, off_of, off_ot, off_lse, off_dot, off_rexp, off_rscale, off_kf,
+  size_t off_q, off_k, off_v, off_g, off_qp, off_dop, off_kr, off_kp, off_vp, off_stat, off_qf, off_qt, off_of, off_ot, off_lse, off_dot, off_rexp, off_rscale, off_kf,
       off_kt, off_vf, off_tv, off_tops, off_exps, off_wops, off_wsplit;
   size_t off_p, off_ds, off_dq_parts, off_t_parts, off_kv_parts, off_dq, off_dkv, off_dg, off_t, off_ds_parts, off_w_parts,
       total;
@@ -1202,8 +1202,10 @@ void back_layout(const dcp_shape* sh, Path path, int64_t n_q, BackLayout* L) {
     L->t_parts = dcp::back_pairs_groups(L->chunk, N);
     L->off_qp = take((size_t)H * n_q * L->dp * 4);
     L->off_dop = take((size_t)H * n_q * L->dp * 4);
-    L->off_kp = take((size_t)H * N * L->dp * 4);
-    L->off_vp = take((size_t)H * N * L->dp * 4);
+    const size_t keys = (size_t)dcp::back_heads_padded(sh->n_heads) * dcp::back_keys_padded(N) * L->dp * 4;
+    L->off_kr = take((size_t)H * N * L->dp * 4);
+    L->off_kp = take(keys);
+    L->off_vp = take(keys);
     L->off_stat = take((size_t)H * n_q * 16);
     L->off_p = take((size_t)H * L->chunk * N * 4);
     L->off_ds = take((size_t)H * L->chunk * N * 4);
@@ -1432,6 +1434,7 @@ int dcp_pair_bias_attention_backward(const dcp_shape* shape, const dcp_weights* 
     ra.mask = key_mask;
     ra.k = pa.k;
     ra.v = pa.v;
+    ra.kr = at(L.off_kr);
     ra.kp = at(L.off_kp);
     ra.vp = at(L.off_vp);
     if ((e = dcp::launch_back_rows(ra, st)) != hipSuccess)
@@ -1480,7 +1483,7 @@ int dcp_pair_bias_attention_backward(const dcp_shape* shape, const dcp_weights* 
       ka.n_splits = L.kv_splits;
       ka.first = row == 0;
       ka.kv_parts = kv_parts;
-      ka.k = ra.kp;
+      ka.k = ra.kr;
       ka.dq = at(L.off_dq);
       if ((e = dcp::launch_back_keys(ka, L.dp, st)) != hipSuccess)
         return fail(DCP_ERR_HIP, "key gradient launch failed: %s", hipGetErrorString(e));

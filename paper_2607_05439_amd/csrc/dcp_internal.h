@@ -253,6 +253,10 @@ struct LayerNormBackArgs {
 // [H][n_q][dp] holds a head's channels padded with zeros to dp.
 constexpr int kBackMaxGroups = 512;  // workgroups (one T each) of the general pair kernel: two fit a CU
 
+constexpr int kBackKeys = 64;        // its keys per tile
+__host__ __device__ constexpr int64_t back_keys_padded(int64_t n_tok) { return (n_tok + kBackKeys - 1) / kBackKeys * kBackKeys; }
+__host__ __device__ constexpr int back_heads_padded(int n_heads) { return n_heads <= 4 ? 4 : n_heads <= 8 ? 8 : 16; }
+
 struct BackRowsArgs {
   int64_t n_q;
   int32_t n_heads, head_dim, dp, dout_bf16;
@@ -265,7 +269,8 @@ struct BackRowsArgs {
   int64_t n_tok;
   const uint8_t* mask;     // [N] or null
   const float *k, *v;      // [N][hd]
-  float *kp, *vp;          // [H][N][dp], zeros for masked keys
+  float* kr;               // [H][N][dp], zeros for masked keys
+  float *kp, *vp;          // in the order of the pair kernel's lanes, back_heads_padded x back_keys_padded x dp
   uint32_t row_blocks;     // set by the launcher
 };
 
@@ -274,7 +279,7 @@ struct BackPairsArgs {
   int32_t z_bf16;
   const uint8_t* mask;     // [N] or null
   const float *w_b, *gamma;
-  const float *k, *v;      // [H][N][dp]
+  const float *k, *v;      // as BackRowsArgs::kp, vp
   const float *qp, *dop, *stat;
   int64_t n_tok, n_q, row0, rows;  // rows [row0, row0 + rows) of the stripe
   int32_t c_z, n_heads, head_dim, dp, first;
