@@ -86,9 +86,12 @@ __global__ void __launch_bounds__(256) back_rows_kernel(BackRowsArgs a) {
   if (blockIdx.x >= a.row_blocks) {
     // a piece of four channels a thread
     const int64_t x = (int64_t)(blockIdx.x - a.row_blocks) * 256 + threadIdx.x;
-    const int pieces = a.dp / 4, piece = (int)(x % pieces), c = 4 * piece;
-    const int64_t n_keys = back_keys_padded(a.n_tok), hj = x / pieces, j = hj % n_keys;
-    const int h = (int)(hj / n_keys);
+    // (rows of at least 64 bytes in memory: fewer than 2^32)
+    const int pieces = a.dp / 4, shift = __builtin_ctz(pieces), piece = (int)x & (pieces - 1), c = 4 * piece;
+    const int64_t n_keys = back_keys_padded(a.n_tok);
+    const uint32_t hj = (uint32_t)(x >> shift);
+    const int h = (int)(hj / (uint32_t)n_keys);
+    const int64_t j = hj % (uint32_t)n_keys;
     if (h >= back_heads_padded(a.n_heads)) return;
     const bool here = h < a.n_heads && j < a.n_tok, valid = here && (!a.mask || a.mask[j] != 0);
     const int64_t at = (j * a.n_heads + h) * a.head_dim;
@@ -108,7 +111,7 @@ __global__ void __launch_bounds__(256) back_rows_kernel(BackRowsArgs a) {
   const int64_t t = ((int64_t)blockIdx.x * 256 + threadIdx.x) >> 3;
   if (t >= a.n_q * a.n_heads) return;  // eight lanes alike
   const int sub = threadIdx.x & 7, d = a.head_dim;
-  const int64_t row = t / a.n_heads;
+  const int64_t row = (uint32_t)t / (uint32_t)a.n_heads;
   const int h = (int)(t - row * a.n_heads);
   const int64_t at = row * a.n_heads * d + (int64_t)h * d, to = ((int64_t)h * a.n_q + row) * a.dp;
   const float l = a.l[(int64_t)h * a.n_q + row], inv_l = l == 0.0f ? 0.0f : 1.0f / l;
@@ -237,8 +240,8 @@ __global__ void __launch_bounds__(256, CT <= 8 && CT * NH < 32 ? 2 : 1) back_pai
   for (int y = 0; y < kTiles; ++y) T[y] = f32x4{0.f, 0.f, 0.f, 0.f};
   const int64_t tiles = (a.n_tok + kBackKeys - 1) / kBackKeys;  // of a row
   int64_t share, begin;
-  chunk_of(a.rows * tiles, gridDim.x, blockIdx.x, &share, &begin);
-  int64_t r = begin / tiles, t_first = begin - r * tiles, left = share;  // row of the stripe's chunk, tile
+  chunk_of_32((uint32_t)(a.rows * tiles), gridDim.x, blockIdx.x, &share, &begin);
+  int64_t r = (uint32_t)begin / (uint32_t)tiles, t_first = begin - r * tiles, left = share;  // row of the stripe's chunk, tile
   // z and the mask of a tile, keys past the last reading that one's
   Raw4<BF16> raw[CT];
   uint8_t attends = 1;
@@ -510,7 +513,7 @@ __global__ void __launch_bounds__(256) back_keys_kernel(BackKeysArgs a) {
   const int64_t j0 = (int64_t)(blockIdx.x / a.n_splits) * 64 + 16 * wave;
   const int split = blockIdx.x % a.n_splits;
   int64_t count, first;
-  chunk_of(a.rows, a.n_splits, split, &count, &first);
+  chunk_of_32((uint32_t)a.rows, a.n_splits, split, &count, &first);
   const int64_t jj = min(j0 + n, a.n_tok - 1), end = first + count;
   const float *q = a.qp + ((int64_t)h * a.n_q + a.row0) * DP + n, *o = a.dop + ((int64_t)h * a.n_q + a.row0) * DP + n;
   f32x4 dk[U], dv[U];
@@ -619,15 +622,15 @@ __global__ void __launch_bounds__(256) back_gemm_kernel(BackGemmArgs a) {
   const int tid = threadIdx.x, lane = tid & 63, n = lane & 15, g = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int c_tiles = (a.c_s + kGemm - 1) / kGemm;
-  int64_t b = blockIdx.x;
+  uint32_t b = blockIdx.x;
   const bool is_ds = b < a.ds_blocks;
-  if (!is_ds) b -= a.ds_blocks;
+  if (!is_ds) b -= (uint32_t)a.ds_blocks;
   const int c0 = (int)(b % c_tiles) * kGemm;
   b /= c_tiles;
   const int splits = is_ds ? a.ds_splits : a.w_splits, split = (int)(b % splits);
   b /= splits;
   const int hd_deep = (a.hd + kDeep - 1) / kDeep * kDeep;
-  const int64_t m0 = is_ds ? b * kGemm : 0;                            // first token
+  const int64_t m0 = is_ds ? (int64_t)b * kGemm : 0;                            // first token
   const int o_tiles = (a.hd + kGemm - 1) / kGemm;
   const int mat = is_ds ? 0 : (int)(b / o_tiles), o0 = is_ds ? 0 : (int)(b % o_tiles) * kGemm;
   // terms of ds in the order k, v, q, g; the matrices of dW in the order q, k, v, g
@@ -637,7 +640,7 @@ __global__ void __launch_bounds__(256) back_gemm_kernel(BackGemmArgs a) {
   const float* dx = mat == 0 ? a.dq : mat == 1 ? a.dk : mat == 2 ? a.dv : a.dg;
   const int64_t depth = is_ds ? (int64_t)hd_deep * (with_rows ? 4 : 2) : (w_rows + kDeep - 1) / kDeep * kDeep;
   int64_t steps, first;
-  chunk_of(depth / kDeep, splits, split, &steps, &first);
+  chunk_of_32((uint32_t)(depth / kDeep), splits, split, &steps, &first);
   const int hd_vec = a.hd % 4 == 0, s_vec = a.c_s % 4 == 0;
   const int r16 = tid >> 4, x4 = (tid & 15) * 4;  // 16 deep by 64 wide, four a thread, twice
   f32x4 av[2], bv[2];
@@ -646,8 +649,7 @@ __global__ void __launch_bounds__(256) back_gemm_kernel(BackGemmArgs a) {
 #pragma unroll
     for (int u = 0; u < 2; ++u) {
       if (is_ds) {
-        const int64_t k0 = step * kDeep;
-        const int term = (int)(k0 / hd_deep), o = (int)(k0 % hd_deep) + 16 * u;
+        const int k0 = (int)step * kDeep, term = k0 / hd_deep, o = k0 - term * hd_deep + 16 * u;
         const float* x = term == 0 ? a.dk : term == 1 ? a.dv : term == 2 ? a.dq : a.dg;
         const float* w = term == 0 ? a.w_k : term == 1 ? a.w_v : term == 2 ? a.w_q : a.w_g;
         // A: token tid / 4, outputs o + 4 (tid % 4) ..

@@ -341,7 +341,7 @@ __global__ void __launch_bounds__(256, 2) pairs_kernel(FastBackArgs a) {
   const int part = blockIdx.y;
   const int64_t r0 = (int64_t)blockIdx.x * kTileQ, q0 = a.row0 + r0;  // within the chunk, within the stripe
   int64_t t_count, t_begin;
-  chunk_of(a.n_pad / 16, a.n_parts, part, &t_count, &t_begin);
+  chunk_of_32((uint32_t)(a.n_pad / 16), a.n_parts, part, &t_count, &t_begin);
   const int64_t t_end = t_begin + t_count;
   constexpr int kHw = kH / 4;
 
@@ -575,7 +575,7 @@ __global__ void __launch_bounds__(256, 3) keys_kernel(FastBackArgs a) {
   const int h = blockIdx.y, split = blockIdx.z, n_tiles = (int)(a.n_pad / 16);
   const int t0 = blockIdx.x * 4;
   int64_t count, first;
-  chunk_of((a.rows + 15) / 16, a.kv_splits, split, &count, &first);
+  chunk_of_32((uint32_t)((a.rows + 15) / 16), a.kv_splits, split, &count, &first);
   f32x4 acc[4][2][2];  // [key tile][dk, dv][channels 0..15, 16..31]
   const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll

@@ -38,6 +38,13 @@ __host__ __device__ inline void chunk_of(int64_t total, int64_t parts, int64_t p
   *size = q + (p < r ? 1 : 0);
   *start = p * q + (p < r ? p : r);
 }
+// The same where the counts fit 32 bits: 64-bit divisions at the start of short kernels took
+// 0.5 us of the 34.5 of a backward pass of 128 tokens.
+__device__ inline void chunk_of_32(uint32_t total, uint32_t parts, uint32_t p, int64_t* size, int64_t* start) {
+  const uint32_t q = total / parts, r = total % parts;
+  *size = q + (p < r ? 1 : 0);
+  *start = (int64_t)p * q + (p < r ? p : r);
+}
 
 struct FastProjArgs {
   const uint16_t* s;  // [N, c_s] bf16

@@ -189,9 +189,9 @@ __global__ void __launch_bounds__(256) token_grad_kernel(TokenArgs p) {
   const int tid = threadIdx.x, lane = tid & 63, n = lane & 15, g = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int c_tiles = (p.c_s + kTile - 1) / kTile;
-  int64_t b = blockIdx.x;
+  uint32_t b = blockIdx.x;
   const bool is_ds = b < p.ds_blocks;
-  if (!is_ds) b -= p.ds_blocks;
+  if (!is_ds) b -= (uint32_t)p.ds_blocks;
   const int c0 = (int)(b % c_tiles) * kTile;
   b /= c_tiles;
   const int splits = is_ds ? p.ds_splits : p.w_splits, split = (int)(b % splits);
@@ -204,14 +204,14 @@ __global__ void __launch_bounds__(256) token_grad_kernel(TokenArgs p) {
   int64_t m0, m_end;
   float* out;
   if (is_ds) {
-    m0 = b * kTile;
+    m0 = (int64_t)b * kTile;
     m_end = p.n_tok;
     out = p.ds_parts + (int64_t)split * p.n_tok * p.c_s;
     // the terms k, v, and q, g where the tile holds rows of the stripe
     const bool with_rows = m0 < p.q_row0 + p.n_q && m0 + kTile > p.q_row0;
     constexpr int kSteps = kHD / kDeep;
     int64_t steps, first;
-    chunk_of(kSteps * (with_rows ? 4 : 2), splits, split, &steps, &first);
+    chunk_of_32(kSteps * (with_rows ? 4 : 2), splits, split, &steps, &first);
     const int64_t t = m0 + (tid >> 2), tq = t - p.q_row0, w_lo = (int64_t)4 * kHD * p.c_s;
     const bool kv_in = t < p.n_tok, q_in = tq >= 0 && tq < p.n_q;
     const int64_t kv_at = t * kHD + 8 * (tid & 3), q_at = tq * kHD + 8 * (tid & 3), w_at = (int64_t)(tid >> 3) * p.c_s + c;
@@ -234,7 +234,7 @@ __global__ void __launch_bounds__(256) token_grad_kernel(TokenArgs p) {
     const int64_t rows = stripe ? p.n_q : p.n_tok, s_row0 = stripe ? p.q_row0 : 0;
     const uint16_t* x = mat == 0 ? p.dq : mat == 1 ? p.dkv : mat == 2 ? p.dkv + p.n_tok * kHD : p.dg;
     int64_t steps, first;
-    chunk_of((rows + kDeep - 1) / kDeep, splits, split, &steps, &first);
+    chunk_of_32((uint32_t)((rows + kDeep - 1) / kDeep), splits, split, &steps, &first);
     const int64_t t0 = first * kDeep + (tid >> 3);
     const uint16_t *xp = x + t0 * kHD + m0 + 8 * (tid & 7), *sp = p.s + (s_row0 + t0) * p.c_s + c;
     product<false, true, false, false>(
