@@ -1214,7 +1214,7 @@ void back_layout(const dcp_shape* sh, Path path, int64_t n_q, BackLayout* L) {
   }
   if (splits > most) splits = most;
   L->kv_splits = (int)(splits < 1 ? 1 : splits > 16 ? 16 : splits);
-  dcp::back_gemm_splits(N, (int32_t)hd, sh->c_s, path == kPathFast ? 256 : 64, &L->ds_splits, &L->w_splits);
+  dcp::back_gemm_splits(N, (int32_t)hd, sh->c_s, path == kPathFast ? 128 : 32, &L->ds_splits, &L->w_splits);
   L->off_dq_parts = path == kPathFast ? take((size_t)L->dq_parts * n_q * hd * 4) : 0;
   L->off_t_parts = take((size_t)L->t_parts * H * sh->c_z * 4);
   L->off_kv_parts = take((size_t)L->kv_splits * 2 * N * hd * 4);

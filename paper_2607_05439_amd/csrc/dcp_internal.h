@@ -414,7 +414,7 @@ hipError_t launch_fast_back_pack(const FastBackArgs& a, hipStream_t st);
 hipError_t launch_fast_back_pairs(const FastBackArgs& a, hipStream_t st);
 hipError_t launch_fast_back_keys(const FastBackArgs& a, hipStream_t st);
 hipError_t launch_back_sum(const BackSumArgs& a, hipStream_t st);
-void back_gemm_splits(int64_t n_tok, int32_t hd, int32_t c_s, int32_t min_depth, int* ds_splits, int* w_splits);
+void back_gemm_splits(int64_t n_tok, int32_t hd, int32_t c_s, int32_t step, int* ds_splits, int* w_splits);
 hipError_t launch_back_gemm(const BackGemmArgs& a, hipStream_t st);
 hipError_t launch_token_proj(const TokenArgs& a, hipStream_t st);
 hipError_t launch_token_grad(const TokenArgs& a, hipStream_t st);
