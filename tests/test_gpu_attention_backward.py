@@ -365,6 +365,38 @@ def test_a_stripe_without_rows(widths):
     assert all(not out[k].any() for k in NAMES[1:])
 
 
+@pytest.mark.parametrize("case", [
+    dict(n=77, row0=3, rows=33, masked=2, **BF16), dict(n=77, row0=3, rows=33, masked=2, **F32),
+    dict(n=35, row0=0, rows=35, dtype="f32", c_s=37, c_z=19, h=3, d=5),
+    dict(n=35, row0=0, rows=35, dtype="bf16", c_s=24, c_z=256, h=16, d=8),
+], ids=["fused", "f32", "odd", "wide"])
+@pytest.mark.parametrize("grad_dtype", [0, 1])
+def test_nothing_is_written_outside(case, grad_dtype):
+    """The outputs and a workspace of exactly the size asked for, each between 4 KB that stay as they were,
+    and inputs that stay as they were."""
+    import torch
+    call = Call(make(**case, seed=40), grad_dtype=grad_dtype)
+    want = call()
+    held = []
+
+    def guarded(t):
+        nbytes = t.numel() * t.element_size()
+        room = torch.full((8192 + (nbytes + 255) // 256 * 256,), 171, dtype=torch.uint8, device="cuda")
+        held.append((room, nbytes))
+        return room[4096:4096 + nbytes].view(t.dtype).view(t.shape)
+
+    out = {k: guarded(v) for k, v in call.outputs().items()}
+    ws = guarded(torch.empty(call.dcp.dcp_pair_bias_attention_backward_workspace_size(call.shape, call.dims[2]),
+                             dtype=torch.uint8))
+    inputs = [t for t in (*call.x.values(), call.m, call.l, call.acc) if isinstance(t, torch.Tensor)]
+    before = [t.clone() for t in inputs]
+    call(ws=ws, out=out)
+    assert all(torch.equal(out[k], want[k]) for k in NAMES)
+    assert all(torch.equal(a, b) for a, b in zip(inputs, before))
+    for room, nbytes in held:
+        assert (room[:4096] == 171).all() and (room[4096 + nbytes:] == 171).all()
+
+
 @pytest.mark.parametrize("widths", [F32, BF16], ids=["f32", "bf16"])
 def test_twice_the_same_bits_on_two_streams(widths):
     """Two calls at once with workspaces of their own: the bits of one call alone."""
