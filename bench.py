@@ -27,7 +27,8 @@ sys.path.insert(0, ROOT)
 
 METRIC = "ms/layer + achieved HBM GB/s (% peak) for pair-biased attention at N tokens"
 PEAK_HBM_GBPS = 8000.0  # MI355X HBM3E, published
-KERNEL_SOURCES = ("paper_2607_05439_amd/csrc/fast.hip", "paper_2607_05439_amd/csrc/cdna4.h")
+KERNEL_SOURCES = ("paper_2607_05439_amd/csrc/fast.hip", "paper_2607_05439_amd/csrc/pair_bias.h",
+                  "paper_2607_05439_amd/csrc/cdna4.h")
 SPARSE_SOURCES = ("paper_2607_05439_amd/csrc/sparse.hip", "paper_2607_05439_amd/csrc/cdna4.h")
 SPARSE_METRIC = "ms/layer + gathered GB/s for sparse kNN pair-biased atom attention"
 KNN_SOURCES = ("paper_2607_05439_amd/csrc/knn.hip",)
