@@ -2,12 +2,13 @@
 // activations (gfx950). The formulas are in backward.hip.
 //
 // Kernels, in order:
-//   prep_kernel   the bias weights as operands; the largest |dout|
-//   (the fp32 projections of the general path, which also leave the largest |q|, |k|, |v|)
+//   prep_kernel   the weights as operands; the largest |dout| of each row
+//   (token_gemm.hip: q, k, v, g, and the largest |q|, |k|, |v|)
 //   pack_kernel   q, do of the rows and k, v of the keys as fp16 operands; the row statistics
 //   pairs_kernel  16 query rows and a range of keys per workgroup: bias, P, dS, dz, dq, T
-//   keys_kernel   64 keys of a head per wave: dk, dv from the stored P
-// then the token products of backward.hip.
+//   keys_kernel   64 keys of a head per workgroup: dk, dv from the stored P
+// then sums of parts (backward.hip), ds and dW (token_gemm.hip) and the gradients in their
+// own types (backward.hip).
 //
 // Operands are fp16, not bf16: 11 significant bits where bf16 has 8, at the same rate, so
 // that the roundings inside stay an eighth of the result's own rounding to bf16. Their
@@ -319,6 +320,9 @@ __global__ void __launch_bounds__(64) pack_kernel(FastBackArgs a) {
 //      as its dz is formed.
 // The rows' q and do stay in LDS: read again from L2 for each tile, 1024 tokens took 210
 // us (208 so) and 2400 rows of 4800 1662 (1635).
+// Bound by memory: 2400 rows of 4800 tokens 1387 us for 3.06 GB read and 3.37 written (z and
+// dz 2.95 each, P 0.37), 4.7 TB/s where a copy of 8 GiB reaches 4.5. 1024 tokens, where
+// 512 workgroups have eight tiles each: 138 us, 4.2 TB/s.
 struct PairLds {
   union {
     f32x4 bias[kH][kTileQ][4];         // 16 KB: [head][row][4 keys, chunk ^ row / 4]
@@ -567,7 +571,8 @@ __global__ void __launch_bounds__(256, 2) pairs_kernel(FastBackArgs a) {
 // dk and dv of 64 keys of one head over a share of the chunk's row tiles: the four waves
 // take every fourth of them, and their sums meet in LDS. dS = P (dP - D) is formed again
 // from P and one more product, dP = dO V^T: stored beside P it took as many bytes again,
-// written and read, and 32 bytes a pair are what bounds this kernel.
+// written and read (the whole call 1784 us then, 1672 so, for 2400 rows of 4800 tokens),
+// and P's 32 bytes a pair are what bounds this kernel: 102 us there, 3.6 TB/s.
 __global__ void __launch_bounds__(256, 3) keys_kernel(FastBackArgs a) {
   __shared__ f32x4 s_sum[16][64];
   const int lane = threadIdx.x & 63, n = lane & 15, g = lane >> 4;

@@ -1122,8 +1122,10 @@ int dcp_layer_norm_backward(int64_t n_rows, int32_t c, int32_t in_dtype, int32_t
 // ----------------------------------------------------------------------------- attention backward
 namespace {
 
-// Most bytes of P and dS (the fused path: of P) kept at a time: the stripe's rows are
-// taken in chunks of as many as fit, at least one (16).
+// Most bytes of P and dS (the fused path: of P) kept at a time, a bound on the workspace:
+// the stripe's rows are taken in chunks of as many as fit, at least one (16). Chunks
+// small enough for the cache between the kernels that write and read P took longer: each
+// launch ends with idle workgroups.
 constexpr size_t kBackGenBytes = (size_t)256 << 20;
 constexpr size_t kBackFastBytes = (size_t)1 << 30;
 
