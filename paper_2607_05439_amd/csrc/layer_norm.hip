@@ -399,9 +399,13 @@ int64_t ln_rounds(int64_t n_rows, int c) {
 
 }  // namespace
 
+// Workgroups of the backward: four a CU, two where they would have little more than a round
+// each, since a workgroup's start and its sums take as long as some. 4800 rows of 384 (1200
+// rounds) in 512 10.2 us, in 1024 11.3; 16384 of 128 (1024) 9.6 and 10.8; 100000 of 32 fp32 (1563)
+// 13.0 and 12.5; a million of 128 167 and 149, in 2048 166.
 int layer_norm_back_groups(int64_t n_rows, int32_t c) {
-  const int64_t rounds = ln_rounds(n_rows, c);
-  return (int)(rounds < 1024 ? rounds : 1024);
+  const int64_t rounds = ln_rounds(n_rows, c), most = rounds <= 1280 ? 512 : 1024;
+  return (int)(rounds < most ? rounds : most);
 }
 
 hipError_t launch_layer_norm(const LayerNormArgs& a, bool x_bf16, bool y_bf16, hipStream_t st) {
