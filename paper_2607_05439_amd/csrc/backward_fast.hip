@@ -4,8 +4,10 @@
 // Kernels, in order:
 //   prep_kernel   the weights as operands; the largest |dout| of each row
 //   (token_gemm.hip: q, k, v, g, and the largest |q|, |k|, |v|)
-//   pack_kernel   q, do of the rows and k, v of the keys as fp16 operands; the row statistics
-//   pairs_kernel  16 query rows and a range of keys per workgroup: bias, P, dS, dz, dq, T
+//   pack_kernel   q, do of the rows and k, v of the keys as fp16 operands; dg
+//   stats_kernel  16 query rows and a range of keys per workgroup: maximum and sum of the
+//                 weights, and sum P dP, of the logits that pairs_kernel forms
+//   pairs_kernel  the same rows and keys again: bias, P, dS, dz, dq, T
 //   keys_kernel   64 keys of a head per workgroup: dk, dv from the stored P
 // then sums of parts (backward.hip), ds and dW (token_gemm.hip) and the gradients in their
 // own types (backward.hip).
@@ -14,7 +16,7 @@
 // that the roundings inside stay an eighth of the result's own rounding to bf16. Their
 // range is served by powers of two: every tensor is scaled so that its largest
 // magnitude lies in [2^11, 2^12) (P, at most 1, by 2^14; dS then by what keeps it below
-// 2^16), fp16 holds 11 bits down to 2^-26 of that, and the fp32 results are scaled
+// 2^16), fp16 holds 11 bits down to 2^-25 of that, and the fp32 results are scaled
 // back exactly. Every row of dout has a power of its own for what stays in the row (dS,
 // dz, dq), and joins the others at the tensor's where rows are summed. Only z enters as the bf16 it is, against bias weights split into
 // bf16 hi + lo (pair_bias.h).
@@ -206,16 +208,13 @@ __global__ void __launch_bounds__(64) pack_kernel(FastBackArgs a) {
 #pragma unroll
   for (int x = 0; x < 4; ++x) tops[x] = __uint_as_float(a.tops[kBackTops * x + lane]);
   f32x4 in[4][kD / 4];  // rows: q, g, acc, dout; keys: k, v
-  float l = 0.0f, m = 0.0f;
+  float l = 0.0f;
   const int er = is_row ? a.row_exp[tok] : 0;  // the power of two of the row's do
   const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
   const int64_t at = tok * kHD + h * kD;
   const bool there = is_row ? tok < a.n_q : tok < a.n_tok && (!a.mask || a.mask[tok] != 0);
   if (is_row) {
-    if (there) {
-      l = a.l[(int64_t)h * a.n_q + tok];
-      m = a.m[(int64_t)h * a.n_q + tok];
-    }
+    if (there) l = a.l[(int64_t)h * a.n_q + tok];
 #pragma unroll
     for (int e = 0; e < kD / 4; ++e) {
       in[0][e] = there ? *reinterpret_cast<const f32x4*>(a.q + at + 4 * e) : zero;
@@ -254,17 +253,15 @@ __global__ void __launch_bounds__(64) pack_kernel(FastBackArgs a) {
   float x[kD], y[kD];
   if (is_row) {
     const float inv_l = l == 0.0f ? 0.0f : 1.0f / l;
-    float dot = 0.0f;
 #pragma unroll
     for (int e = 0; e < kD; e += 4) {
       f32x4 dg;
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         const float gt = in[1][e / 4][i], up = in[3][e / 4][i];
-        const float o = l == 0.0f ? 0.0f : in[2][e / 4][i] * inv_l, d = gt * up;
+        const float o = l == 0.0f ? 0.0f : in[2][e / 4][i] * inv_l;
         x[e + i] = in[0][e / 4][i] * (kLog2e * kInvSqrtD);
-        y[e + i] = d;
-        dot = fmaf(d, o, dot);
+        y[e + i] = gt * up;
         dg[i] = up * o * gt * (1.0f - gt);
       }
       if (there) {
@@ -274,8 +271,6 @@ __global__ void __launch_bounds__(64) pack_kernel(FastBackArgs a) {
         *reinterpret_cast<u32x2*>(a.dg + a.n_q * kHD + at + e) = lo;
       }
     }
-    a.lse[(int64_t)h * a.nq_pad + tok] = l == 0.0f ? INFINITY : fmaf(m, kLog2e, log2f(l));  // rows past the last: l = 0
-    a.dot[(int64_t)h * a.nq_pad + tok] = ldexpf(dot, e2[2] + er);
     if (h == 0) a.row_scale[tok] = ldexpf(1.0f, e2[3] - er);
     pack_row(y, e2[3], s_t[lane >> 4], lane & 15);
   } else {
@@ -303,13 +298,134 @@ __global__ void __launch_bounds__(64) pack_kernel(FastBackArgs a) {
   }
 }
 
+// One key's z for 16 rows as an operand; a key that does not attend reads nothing, and is 0.
+__device__ __forceinline__ void load_key(__amdgpu_buffer_rsrc_t zres, int zoff, int64_t t, int k, uint32_t bits, u32x4 (&z)[4]) {
+  const int at = (bits >> k) & 1u ? zoff + (int)(t * 16 + k) * (kCz * 2) : kOutOfRange;
+#pragma unroll
+  for (int x = 0; x < 4; ++x) z[x] = __builtin_amdgcn_raw_buffer_load_b128(zres, at + 64 * x, 0, 0);
+}
+
+// ----------------------------------------------------------------------------- row statistics
+// M, L = sum 2^(S - M) and sum 2^(S - M) dP of every row and head over a part's keys, S in base 2.
+// The forward's saved m, l and acc will not do for them: it forms S from bf16 q and k and sums
+// bf16 v, so that P = exp(S - m) / l with the S of fp16 operands has rows that do not sum to 1,
+// and D = do . acc / l is not sum P dP, by 2^-9 of the logits' size: gradients were off by 1.4e-2 at
+// logits of 22 and 2.9e-2 at 44, with these sums by 2.0e-3 and 2.5e-3. That takes z once more
+// (2400 rows of 4800 tokens 1613 us, so 2205; 1024 tokens 210, so 274). Of the state there
+// remain o for dg (pack_kernel) and the rows whose l is 0.
+// A workgroup's four waves split a tile's keys for the bias, which goes through LDS in two
+// buffers, and the heads for the rest, as in pairs_kernel; a lane keeps a running maximum of its
+// own (row n, keys 4g..4g+3), and the four lanes of a row meet at the end.
+constexpr float kLowest = -3e38f;  // below every logit, and finite: kLowest - kLowest is 0
+
+__global__ void __launch_bounds__(256, 2) stats_kernel(FastBackArgs a) {
+  __shared__ f32x4 s_bias[2][kH][kTileQ][4];  // [buffer][head][row][4 keys, chunk ^ row / 4]
+  const int tid = threadIdx.x, lane = tid & 63, n = lane & 15, g = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int64_t q0 = (int64_t)blockIdx.x * kTileQ;
+  int64_t t_count, t_begin;
+  chunk_of_32((uint32_t)(a.n_pad / 16), a.stat_parts, blockIdx.y, &t_count, &t_begin);
+  const int64_t t_end = t_begin + t_count;
+  constexpr int kHw = kH / 4;
+  uint32_t bits = t_begin < t_end ? a.tile_valid[t_begin] : 0u;
+  const float s_scale = ldexpf(1.0f, -a.exps[0] - a.exps[1]);
+  const int64_t rows_here = min((int64_t)kTileQ, a.n_q - q0);
+  const int row_bytes = (int)(a.n_tok * (kCz * 2));
+  const __amdgpu_buffer_rsrc_t zres = __builtin_amdgcn_make_buffer_rsrc(
+      const_cast<uint16_t*>(a.z) + q0 * a.n_tok * kCz, 0, (int)(rows_here * row_bytes), kRawBufferFlags);
+  const int zoff = n * row_bytes + 16 * g, n_tiles = (int)(a.n_pad / 16);
+  u32x4 z[4][4];
+#pragma unroll
+  for (int kk = 0; kk < 4; ++kk) load_key(zres, zoff, t_begin, 4 * wave + kk, bits, z[kk]);
+  const __amdgpu_buffer_rsrc_t kres = __builtin_amdgcn_make_buffer_rsrc(a.kf, 0, (int)(kH * a.n_pad * kDp * 2), kRawBufferFlags);
+  const __amdgpu_buffer_rsrc_t vres = __builtin_amdgcn_make_buffer_rsrc(a.vf, 0, (int)(kH * a.n_pad * kDp * 2), kRawBufferFlags);
+  bf16x8 whi[4], wlo[4];
+#pragma unroll
+  for (int x = 0; x < 4; ++x) {
+    whi[x] = as_bf16x8(a.w_ops[64 * x + lane]);
+    wlo[x] = as_bf16x8(a.w_ops[64 * (4 + x) + lane]);
+  }
+  f16x8 q[kHw], o[kHw];
+  float top[kHw], sum[kHw], dot[kHw];
+#pragma unroll
+  for (int j = 0; j < kHw; ++j) {
+    const int64_t at = ((int64_t)(kHw * wave + j) * a.nq_pad + q0 + n) * 4 + g;
+    q[j] = as_f16x8(reinterpret_cast<const u32x4*>(a.qf)[at]);
+    o[j] = as_f16x8(reinterpret_cast<const u32x4*>(a.of)[at]);
+    top[j] = kLowest;
+    sum[j] = dot[j] = 0.0f;
+  }
+  const f32x4 wsum = bias_weight_sums(whi, wlo), zero = {0.f, 0.f, 0.f, 0.f};
+  const bool row_there = n < rows_here;
+  int buf = 0;
+  for (int64_t t = t_begin; t < t_end; ++t, buf ^= 1) {
+    const uint32_t bits_next = t + 1 < t_end ? a.tile_valid[t + 1] : 0u;
+    f16x8 k[kHw], v[kHw];  // in flight during the bias
+#pragma unroll
+    for (int j = 0; j < kHw; ++j) {
+      const int so = ((kHw * wave + j) * n_tiles + (int)t) * 1024;
+      k[j] = as_f16x8(__builtin_amdgcn_raw_buffer_load_b128(kres, 64 * n + 16 * g, so, 0));
+      v[j] = as_f16x8(__builtin_amdgcn_raw_buffer_load_b128(vres, 64 * n + 16 * g, so, 0));
+    }
+    f32x4 b[4];
+#pragma unroll
+    for (int kk = 0; kk < 4; ++kk) {
+      f32x4 acc;
+      float rstd, mu;
+      pair_bias(z[kk], whi, wlo, wsum, a.eps, n, acc, rstd, mu);
+      load_key(zres, zoff, t + 1, 4 * wave + kk, bits_next, z[kk]);
+      const bool valid = row_there && ((bits >> (4 * wave + kk)) & 1u);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) b[i][kk] = valid ? acc[i] * rstd : -INFINITY;
+    }
+    bits = bits_next;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) s_bias[buf][4 * g + i][n][wave ^ (n >> 2)] = b[i];
+    barrier_lds();  // and every wave is through with the other buffer's tile before last
+#pragma unroll
+    for (int j = 0; j < kHw; ++j) {
+      const f32x4 bias = s_bias[buf][kHw * wave + j][n][g ^ (n >> 2)];
+      const f32x4 x = mfma32h(k[j], q[j], zero), dp = mfma32h(v[j], o[j], zero);
+      f32x4 l;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) l[i] = fmaf(x[i], s_scale, bias[i]);
+      const float m = fmaxf(fmaxf(fmaxf(l[0], l[1]), fmaxf(l[2], l[3])), top[j]);
+      const float c = __builtin_amdgcn_exp2f(top[j] - m);
+      sum[j] *= c;
+      dot[j] *= c;
+      top[j] = m;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const float e = __builtin_amdgcn_exp2f(l[i] - m);
+        sum[j] += e;
+        dot[j] = fmaf(e, dp[i], dot[j]);
+      }
+    }
+  }
+  const int64_t plane = kH * a.nq_pad;
+#pragma unroll
+  for (int j = 0; j < kHw; ++j) {
+    const int h = kHw * wave + j;
+    const float m = max4(top[j]), c = __builtin_amdgcn_exp2f(top[j] - m);
+    const float l = sum4(sum[j] * c), d = sum4(dot[j] * c);
+    // no weights where the state has none
+    const bool keys = row_there && a.l[(int64_t)h * a.n_q + q0 + min(n, (int)rows_here - 1)] != 0.0f;
+    float* to = a.stats + 3 * blockIdx.y * plane + (int64_t)h * a.nq_pad + q0 + n;
+    if (g == 0) {
+      to[0] = keys ? m : kLowest;
+      to[plane] = keys ? l : 0.0f;
+      to[2 * plane] = keys ? d : 0.0f;
+    }
+  }
+}
+
 // ----------------------------------------------------------------------------- pairs
 // A workgroup of four waves takes 16 query rows and a range of 16-key tiles. Per tile:
 //   1. the waves split the keys: LayerNorm statistics and bias of all heads
 //      (pair_bias), z staying in the registers; the bias goes through LDS
 //      [head][row][key];
-//   2. the waves split the heads: S = K Q^T, P = exp2(S + bias - lse), dP = V dO^T,
-//      dS = P (dP - D), dq += K^T dS; P, transposed on the matrix cores (the
+//   2. the waves split the heads: S = K Q^T + bias, P = exp2(S - M) / L, dP = V dO^T,
+//      dS = P (dP - D) with M, L and D = sum P dP of all parts of stats_kernel, dq += K^T dS; P, transposed on the matrix cores (the
 //      accumulator's registers as the A operand of a product with the identity:
 //      exact), goes to memory as an operand of the keys kernel, and dS to LDS
 //      [key][row][head];
@@ -333,7 +449,7 @@ struct PairLds {
   float t[4][kTileK][kTileQ];          // 4 KB: each wave's heads' share of sum dS b
   u32x4 w[8][64];                      // 8 KB: bias weights, hi then lo
   u32x2 wt[8][64];                     // 4 KB: W'' for dz
-  float stat[kH][kTileQ][2];           // 2 KB: log-sum-exp and D of the rows
+  float stat[kH][kTileQ][3];           // 3 KB: M, 2^kPShift / L and D of the rows
   float row_scale[kTileQ];             // from a row's power of two to the tensor's
   int row_exp[kTileQ];                 // the power of two of a row's dS
 };
@@ -364,15 +480,9 @@ __global__ void __launch_bounds__(256, 2) pairs_kernel(FastBackArgs a) {
   const __amdgpu_buffer_rsrc_t dzres = __builtin_amdgcn_make_buffer_rsrc(
       a.dz ? a.dz + q0 * a.n_tok * kCz : nullptr, 0, a.dz ? (int)(rows_here * row_bytes) : 0, kRawBufferFlags);
   const int zoff = n * row_bytes + 16 * g;
-  auto load_z = [&](int64_t t, uint32_t bits, int kk, u32x4 (&z)[4]) {
-    const int k = 4 * wave + kk;
-    const int at = (bits >> k) & 1u ? zoff + (int)(t * 16 + k) * (kCz * 2) : kOutOfRange;
-#pragma unroll
-    for (int x = 0; x < 4; ++x) z[x] = __builtin_amdgcn_raw_buffer_load_b128(zres, at + 64 * x, 0, 0);
-  };
   u32x4 z[4][4];
 #pragma unroll
-  for (int kk = 0; kk < 4; ++kk) load_z(t_begin, bits, kk, z[kk]);
+  for (int kk = 0; kk < 4; ++kk) load_key(zres, zoff, t_begin, 4 * wave + kk, bits, z[kk]);
   for (int x = tid; x < 512; x += 256) {
     (&s.w[0][0])[x] = a.w_ops[x];
     (&s.wt[0][0])[x] = reinterpret_cast<const u32x2*>(a.w_ops + 512)[x];
@@ -389,8 +499,24 @@ __global__ void __launch_bounds__(256, 2) pairs_kernel(FastBackArgs a) {
       s.q[tid >> 4][n][x ^ (n >> 2)] = reinterpret_cast<const u32x4*>(a.qf)[at * 4 + x];
       s.o[tid >> 4][n][x ^ (n >> 2)] = reinterpret_cast<const u32x4*>(a.of)[at * 4 + x];
     }
-    s.stat[tid >> 4][n][0] = a.lse[at];
-    s.stat[tid >> 4][n][1] = a.dot[at];
+    // M, L and D from the parts, in order
+    float top = kLowest, sum = 0.0f, dot = 0.0f;
+    const int64_t plane = kH * a.nq_pad;
+#pragma unroll 4
+    for (int p = 0; p < a.stat_parts; ++p) {
+      const float* from = a.stats + 3 * p * plane + at;
+      const float m = from[0], l = from[plane], d = from[2 * plane];
+      const float both = fmaxf(top, m), c0 = __builtin_amdgcn_exp2f(top - both), c1 = __builtin_amdgcn_exp2f(m - both);
+      sum = fmaf(sum, c0, l * c1);
+      dot = fmaf(dot, c0, d * c1);
+      top = both;
+    }
+    const bool keys = sum != 0.0f;  // (NaN too)
+    const float inv = keys ? 1.0f / sum : 0.0f;
+    s.stat[tid >> 4][n][0] = keys ? top : INFINITY;
+    s.stat[tid >> 4][n][1] = inv * (float)(1 << kPShift);
+    s.stat[tid >> 4][n][2] = dot * inv;
+    if (part == 0) a.dot[at] = dot * inv;  // for keys_kernel
     if (tid < kTileQ) {
       s.row_scale[n] = a.row_scale[q0 + n];
       s.row_exp[n] = a.row_exp[q0 + n] + ev - kDsShift;
@@ -453,16 +579,14 @@ __global__ void __launch_bounds__(256, 2) pairs_kernel(FastBackArgs a) {
       const f16x8 q = as_f16x8(s.q[h][n][g ^ (n >> 2)]), o = as_f16x8(s.o[h][n][g ^ (n >> 2)]);
       const u32x4 kt = __builtin_amdgcn_raw_buffer_load_b128(ktres, 16 * lane, so, 0);
       const f32x4 bias = s.bias[h][n][g ^ (n >> 2)];
-      const float lse = s.stat[h][n][0], dot = s.stat[h][n][1];
+      const float top = s.stat[h][n][0], inv_l = s.stat[h][n][1], dot = s.stat[h][n][2];
       const f32x4 x = mfma32h(k, q, zero), dp = mfma32h(v, o, zero);
       f32x4 p, ds;
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        // at most 1: logits in the thousands, which the forward forms in bf16, differ from its
-        // sum by so much that P would leave fp16's range (NaN stays)
-        p[i] = __builtin_elementwise_minimum(__builtin_amdgcn_exp2f(fmaf(x[i], s_scale, bias[i] - lse)), 1.0f);
-        ds[i] = p[i] * (dp[i] - dot) * (1.0f / (1 << kDsShift));
-        p[i] *= (float)(1 << kPShift);
+        // P times 2^kPShift, dS times 2^-kDsShift
+        p[i] = __builtin_amdgcn_exp2f(fmaf(x[i], s_scale, bias[i]) - top) * inv_l;
+        ds[i] = p[i] * (dp[i] - dot) * (1.0f / (1 << (kPShift + kDsShift)));
         tp[i] = fmaf(ds[i], p[i] == 0.0f ? 0.0f : bias[i], tp[i]);
       }
       const f16x4 p16 = to_f16(p), ds16 = to_f16(ds);
@@ -510,7 +634,7 @@ __global__ void __launch_bounds__(256, 2) pairs_kernel(FastBackArgs a) {
         }
         s.out[wave][n][(4 * x + g) ^ n] = __builtin_bit_cast(u32x4, r);
       }
-      load_z(t + 1, bits_next, kk, z[kk]);
+      load_key(zres, zoff, t + 1, k, bits_next, z[kk]);
       if (a.dz) {
         // the wave's own LDS: its writes complete before its reads, in order
         const bool there = t * 16 + k < a.n_tok;
@@ -670,6 +794,11 @@ hipError_t launch_fast_back_prep(const FastBackArgs& a, hipStream_t st) {
 
 hipError_t launch_fast_back_pack(const FastBackArgs& a, hipStream_t st) {
   hipLaunchKernelGGL(pack_kernel, dim3((unsigned)((a.nq_pad + a.n_pad) / 16), kH / 4), dim3(64), 0, st, a);
+  return hipGetLastError();
+}
+
+hipError_t launch_fast_back_stats(const FastBackArgs& a, hipStream_t st) {
+  hipLaunchKernelGGL(stats_kernel, dim3((unsigned)(a.nq_pad / 16), (unsigned)a.stat_parts), dim3(256), 0, st, a);
   return hipGetLastError();
 }
 

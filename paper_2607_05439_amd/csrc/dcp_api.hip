@@ -1131,9 +1131,9 @@ constexpr size_t kBackFastBytes = (size_t)1 << 30;
 
 struct BackLayout {
   int64_t chunk, nq_pad, n_pad;  // chunk: rows at a time
-  int dp, dq_parts, t_parts, kv_splits, ds_splits, w_splits;
+  int dp, stat_parts, dq_parts, t_parts, kv_splits, ds_splits, w_splits;
   // projections, general and fused rows' operands, fused keys' operands
-  size_t off_q, off_k, off_v, off_g, off_qp, off_dop, off_kr, off_kp, off_vp, off_stat, off_qf, off_qt, off_of, off_ot, off_lse, off_dot, off_rexp, off_rscale, off_kf,
+  size_t off_q, off_k, off_v, off_g, off_qp, off_dop, off_kr, off_kp, off_vp, off_stat, off_qf, off_qt, off_of, off_ot, off_stats, off_dot, off_rexp, off_rscale, off_kf,
       off_kt, off_vf, off_tv, off_tops, off_exps, off_wops, off_wsplit;
   size_t off_p, off_ds, off_dq_parts, off_t_parts, off_kv_parts, off_dq, off_dkv, off_dg, off_t, off_ds_parts, off_w_parts,
       total;
@@ -1144,8 +1144,8 @@ struct BackLayout {
 // tile's time for its start and end; the fewest parts within 1% of the cheapest. 750
 // rows of 12000 tokens (47 row tiles): 1450 us in 10 parts, 1411 in 21, 1502 in 16, 1863
 // in 11; 1024 tokens: 213 us in 8, 232 in 16, 239 in 4; 333 tokens: 69 us in 21, 71 in 11.
-int fast_back_parts(int64_t groups, int64_t tiles) {
-  const int64_t cap = tiles < 64 ? tiles : 64;
+int fast_back_parts(int64_t groups, int64_t tiles, int64_t most) {
+  const int64_t cap = tiles < most ? tiles : most;
   int64_t cost[65], best = 0;
   for (int64_t p = 1; p <= cap; ++p) {
     cost[p] = (groups * p + 511) / 512 * ((tiles + p - 1) / p + 1);
@@ -1179,12 +1179,14 @@ void back_layout(const dcp_shape* sh, Path path, int64_t n_q, BackLayout* L) {
     if (L->chunk < 16) L->chunk = 16;
     if (L->chunk > L->nq_pad) L->chunk = L->nq_pad;
     const int64_t groups = L->chunk / 16;
-    L->dq_parts = fast_back_parts(groups, L->n_pad / 16);
+    L->dq_parts = fast_back_parts(groups, L->n_pad / 16, 64);
+    // (few: every workgroup behind them adds them up)
+    L->stat_parts = fast_back_parts(L->nq_pad / 16, L->n_pad / 16, 16);
     L->t_parts = (int)groups * L->dq_parts;
     const size_t rows = (size_t)H * L->nq_pad * dcp::kFastDp * 2, keys = (size_t)H * L->n_pad * dcp::kFastDp * 2;
     for (size_t* o : {&L->off_qf, &L->off_qt, &L->off_of, &L->off_ot}) *o = take(rows);
     for (size_t* o : {&L->off_kf, &L->off_kt, &L->off_vf}) *o = take(keys);
-    L->off_lse = take((size_t)H * L->nq_pad * 4);
+    L->off_stats = take((size_t)L->stat_parts * 3 * H * L->nq_pad * 4);
     L->off_dot = take((size_t)H * L->nq_pad * 4);
     L->off_rexp = take((size_t)L->nq_pad * 4);
     L->off_rscale = take((size_t)L->nq_pad * 4);
@@ -1325,7 +1327,6 @@ int dcp_pair_bias_attention_backward(const dcp_shape* shape, const dcp_weights* 
     ba.g = at(L.off_g);
     ba.k = at(L.off_k);
     ba.v = at(L.off_v);
-    ba.m = m;
     ba.l = l;
     ba.acc = acc;
     ba.dout = dout;
@@ -1344,7 +1345,8 @@ int dcp_pair_bias_attention_backward(const dcp_shape* shape, const dcp_weights* 
     ba.kf = half(L.off_kf);
     ba.kt = half(L.off_kt);
     ba.vf = half(L.off_vf);
-    ba.lse = at(L.off_lse);
+    ba.stat_parts = L.stat_parts;
+    ba.stats = at(L.off_stats);
     ba.dot = at(L.off_dot);
     ba.row_exp = reinterpret_cast<int32_t*>(ws + L.off_rexp);
     ba.row_scale = at(L.off_rscale);
@@ -1388,6 +1390,8 @@ int dcp_pair_bias_attention_backward(const dcp_shape* shape, const dcp_weights* 
       return fail(DCP_ERR_HIP, "projection launch failed: %s", hipGetErrorString(e));
     if ((e = dcp::launch_fast_back_pack(ba, st)) != hipSuccess)
       return fail(DCP_ERR_HIP, "operand launch failed: %s", hipGetErrorString(e));
+    if ((e = dcp::launch_fast_back_stats(ba, st)) != hipSuccess)
+      return fail(DCP_ERR_HIP, "row statistics launch failed: %s", hipGetErrorString(e));
     for (ba.row0 = 0; ba.row0 < n_q; ba.row0 += L.chunk) {
       ba.rows = ba.row0 + L.chunk <= n_q ? L.chunk : n_q - ba.row0;
       ba.first = ba.row0 == 0;

@@ -313,7 +313,7 @@ struct FastBackArgs {
   const uint8_t* mask;     // [N] or null
   const float *w_b, *gamma;
   const float *q, *g, *k, *v;  // [n_q][384], [N][384] fp32
-  const float *m, *l, *acc;
+  const float *l, *acc;
   const void* dout;
   int32_t dout_bf16;
   int64_t n_tok, n_q, nq_pad, n_pad;
@@ -321,7 +321,9 @@ struct FastBackArgs {
   int32_t* exps;           // [5]: the powers of two of q, k, v, do and W''
   u32x4* w_ops;            // [768]: bias weights, W''
   uint16_t *qf, *qt, *of, *ot, *kf, *kt, *vf;
-  float *lse, *dot;        // [H][nq_pad]
+  int32_t stat_parts;
+  float* stats;            // [stat_parts][3][H][nq_pad]: M, L and sum P dP of a part of the keys
+  float* dot;              // [H][nq_pad]: D
   int32_t* row_exp;        // [nq_pad]: the power of two of each row's do
   float* row_scale;        // [nq_pad]: from there to the tensor's
   const float* w[4];       // W_q, W_k, W_v, W_g [384][c_s]
@@ -411,6 +413,7 @@ hipError_t launch_back_pairs(const BackPairsArgs& a, int groups, hipStream_t st)
 hipError_t launch_back_keys(const BackKeysArgs& a, int dp, hipStream_t st);
 hipError_t launch_fast_back_prep(const FastBackArgs& a, hipStream_t st);
 hipError_t launch_fast_back_pack(const FastBackArgs& a, hipStream_t st);
+hipError_t launch_fast_back_stats(const FastBackArgs& a, hipStream_t st);
 hipError_t launch_fast_back_pairs(const FastBackArgs& a, hipStream_t st);
 hipError_t launch_fast_back_keys(const FastBackArgs& a, hipStream_t st);
 hipError_t launch_back_sum(const BackSumArgs& a, hipStream_t st);
