@@ -56,9 +56,10 @@ __device__ __forceinline__ f16x4 to_f16(f32x4 v) {
 }
 
 // The power of two that takes a largest magnitude into [2^kTop, 2^(kTop + 1)): 1 where
-// there is none (all zero) or it is not finite.
+// there is none (all zero). It is taken over the finite values: one that is not stays so at
+// any power, and the others keep theirs.
 __device__ __forceinline__ int scale_exp(float top) {
-  if (!(top > 0.0f) || top == INFINITY) return 0;
+  if (!(top > 0.0f)) return 0;
   int e;
   (void)frexpf(top, &e);  // top = f 2^e, f in [0.5, 1)
   return max(-100, min(100, kTop + 1 - e));
@@ -96,14 +97,14 @@ __global__ void __launch_bounds__(256) prep_kernel(FastBackArgs a) {
             const u32x4 v = from[16 * x];
 #pragma unroll
             for (int i = 0; i < 4; ++i)
-              row_top = fmaxf(row_top, fmaxf(fabsf(__uint_as_float(v[i] << 16)), fabsf(__uint_as_float(v[i] & 0xFFFF0000u))));
+              row_top = fmaxf(row_top, fmaxf(finite_abs(__uint_as_float(v[i] << 16)), finite_abs(__uint_as_float(v[i] & 0xFFFF0000u))));
           }
         } else {
           const f32x4* from = reinterpret_cast<const f32x4*>(static_cast<const float*>(a.dout) + r * kHD) + sub;
 #pragma unroll
           for (int x = 0; x < kHD / 64; ++x) {
             const f32x4 v = from[16 * x];
-            row_top = fmaxf(row_top, fmaxf(fmaxf(fabsf(v[0]), fabsf(v[1])), fmaxf(fabsf(v[2]), fabsf(v[3]))));
+            row_top = fmaxf(row_top, fmaxf(fmaxf(finite_abs(v[0]), finite_abs(v[1])), fmaxf(finite_abs(v[2]), finite_abs(v[3]))));
           }
         }
 #pragma unroll
@@ -149,7 +150,7 @@ __global__ void __launch_bounds__(256) prep_kernel(FastBackArgs a) {
 #pragma unroll
     for (int m = 0; m < 8; ++m) {
       w[i][m] -= sum * (1.0f / kCz);
-      top = fmaxf(top, fabsf(w[i][m]));
+      top = fmaxf(top, finite_abs(w[i][m]));
     }
   }
 #pragma unroll

@@ -3,6 +3,7 @@
 #pragma once
 
 #include <hip/hip_runtime.h>
+#include <math.h>
 #include <stdint.h>
 
 #include "cdna4.h"
@@ -45,6 +46,9 @@ __device__ inline void chunk_of_32(uint32_t total, uint32_t parts, uint32_t p, i
   *size = q + (p < r ? 1 : 0);
   *start = (int64_t)p * q + (p < r ? p : r);
 }
+
+// |x|, and 0 where x is not finite.
+__device__ inline float finite_abs(float x) { return fabsf(x) < INFINITY ? fabsf(x) : 0.0f; }
 
 struct FastProjArgs {
   const uint16_t* s;  // [N, c_s] bf16

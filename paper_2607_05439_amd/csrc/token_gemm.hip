@@ -174,7 +174,7 @@ __global__ void __launch_bounds__(256) token_proj_kernel(TokenArgs p) {
 #pragma unroll
       for (int x = 0; x < 2; ++x) {
         float v = acc[u][x][i];
-        if (!masked) top = fmaxf(top, fabsf(v));  // (leaves NaN out)
+        if (!masked) top = fmaxf(top, finite_abs(v));
         if (q_side && second) v = 1.0f / (1.0f + expf(-v));
         dst[t * kHD + o0 + 32 * (wave & 1) + 16 * x + n] = v;
       }
