@@ -182,8 +182,9 @@ int dcp_pair_bias_attention_partial(const dcp_shape* shape, const dcp_weights* w
 
 /* Device pointers that receive gradients, each 16-byte aligned, or NULL for one
  * that is not wanted (at least one is). They must not overlap the inputs, the
- * workspace or each other. All are overwritten; those of the shared tensors
- * are the stripe's share, to be added over the stripes by the caller. */
+ * workspace or each other, nor the workspace the inputs: such a call is refused.
+ * All are overwritten; those of the shared tensors are the stripe's share, to be
+ * added over the stripes by the caller. */
 typedef struct {
   void* dz_rows;   /* [n_q, N, c_z] act_dtype; 0 for masked keys                  */
   void* ds;        /* [N, c_s] dtype: as queries and gates the stripe's rows, as  */

@@ -1043,6 +1043,25 @@ size_t layer_norm_back_ws(int64_t n_rows, int32_t c) {
 
 size_t elem(int32_t dtype) { return dtype == DCP_BF16 ? 2 : 4; }
 
+// Device memory of a call, for the refusal of what overlaps.
+struct Extent {
+  const char* name;
+  const void* p;
+  size_t bytes;
+};
+bool overlap(const Extent& a, const Extent& b) {
+  const uintptr_t x = reinterpret_cast<uintptr_t>(a.p), y = reinterpret_cast<uintptr_t>(b.p);
+  return a.p && b.p && a.bytes > 0 && b.bytes > 0 && x < y + b.bytes && y < x + a.bytes;
+}
+// The first n of `all` are written, the others read: the written ones lie apart from all.
+int check_apart(const Extent* all, int total, int n) {
+  for (int i = 0; i < n; ++i)
+    for (int j = i + 1; j < total; ++j)
+      if (overlap(all[i], all[j]))
+        return fail(DCP_ERR_INVALID_ARGUMENT, "%s and %s overlap", all[i].name, all[j].name);
+  return DCP_OK;
+}
+
 }  // namespace
 
 extern "C" {
@@ -1285,11 +1304,25 @@ int dcp_pair_bias_attention_backward(const dcp_shape* shape, const dcp_weights* 
     return fail(DCP_ERR_WORKSPACE, "workspace must be a 256-byte aligned device pointer");
   if (workspace_bytes < L.total)
     return fail(DCP_ERR_WORKSPACE, "workspace too small: %zu bytes given, %zu needed", workspace_bytes, L.total);
+  const int64_t N = shape->n_tokens;
+  const int hd = shape->n_heads * shape->head_dim;
+  {
+    const size_t act = elem(shape->act_dtype), gr = elem(grads->dtype), tok = (size_t)N * shape->c_s, row = (size_t)n_q * hd;
+    const size_t w1 = (size_t)hd * shape->c_s, wb = (size_t)shape->n_heads * shape->c_z, pairs = (size_t)n_q * N * shape->c_z;
+    const size_t stat = (size_t)shape->n_heads * n_q * 4;
+    const Extent all[] = {{"dz_rows", grads->dz_rows, pairs * act}, {"ds", grads->ds, tok * gr},
+                          {"dw_q", grads->dw_q, w1 * gr}, {"dw_k", grads->dw_k, w1 * gr}, {"dw_v", grads->dw_v, w1 * gr},
+                          {"dw_g", grads->dw_g, w1 * gr}, {"dw_b", grads->dw_b, wb * gr},
+                          {"dln_gamma", grads->dln_gamma, shape->c_z * gr}, {"workspace", workspace, L.total},
+                          {"s", s, tok * act}, {"z_rows", z_rows, pairs * act}, {"key_mask", key_mask, (size_t)N},
+                          {"m", m, stat}, {"l", l, stat}, {"acc", acc, row * 4}, {"dout", dout, row * elem(shape->out_dtype)},
+                          {"w_q", w->w_q, w1 * 4}, {"w_k", w->w_k, w1 * 4}, {"w_v", w->w_v, w1 * 4}, {"w_g", w->w_g, w1 * 4},
+                          {"w_b", w->w_b, wb * 4}, {"ln_gamma", w->ln_gamma, shape->c_z * sizeof(float)}};
+    if ((rc = check_apart(all, sizeof(all) / sizeof(all[0]), 9))) return rc;
+  }
   char* ws = static_cast<char*>(workspace);
   auto at = [&](size_t off) { return reinterpret_cast<float*>(ws + off); };
   hipStream_t st = static_cast<hipStream_t>(stream);
-  const int64_t N = shape->n_tokens;
-  const int hd = shape->n_heads * shape->head_dim;
   const bool act_bf16 = shape->act_dtype == DCP_BF16;
   hipError_t e;
   dcp::BackFinishArgs fa{};

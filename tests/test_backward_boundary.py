@@ -133,3 +133,51 @@ def test_attention_backward_workspace():
     assert L.dcp_pair_bias_attention_backward_workspace_size(ctypes.byref(sh), 10, None) == BAD
     assert L.dcp_pair_bias_attention_backward_workspace_size(None, 10, ctypes.byref(out)) == BAD
     assert L.dcp_pair_bias_attention_backward_workspace_size(ctypes.byref(sh), 602, ctypes.byref(out)) == BAD
+
+
+# ----------------------------------------------------------------------------- gradients that overlap
+PLACES = {"s": 1, "z": 2, "m": 3, "l": 4, "acc": 5, "dout": 6, "mask": 7, "w_q": 8, "w_k": 9, "w_v": 10, "w_g": 11, "w_b": 12,
+          "ln_gamma": 13, "ws": 14, "dz_rows": 15, "ds": 16, "dw_q": 17, "dw_k": 18, "dw_v": 19, "dw_g": 20, "dw_b": 21,
+          "dln_gamma": 22}
+GRADS = ("dz_rows", "ds", "dw_q", "dw_k", "dw_v", "dw_g", "dw_b", "dln_gamma")
+N_Q = 300
+
+
+def sizes(base, grad):
+    """Bytes of each tensor of a call of N_Q rows with gradients of `grad` bytes an element."""
+    n, c_s, c_z, h, hd = base["n_tokens"], base["c_s"], base["c_z"], base["n_heads"], base["n_heads"] * base["head_dim"]
+    act, out = (2 if base["act_dtype"] else 4), (2 if base["out_dtype"] else 4)
+    b = {"s": n * c_s * act, "z": N_Q * n * c_z * act, "m": h * N_Q * 4, "l": h * N_Q * 4, "acc": N_Q * hd * 4,
+         "dout": N_Q * hd * out, "mask": n, "w_b": h * c_z * 4, "ln_gamma": c_z * 4,
+         "ws": dcp.dcp_pair_bias_attention_backward_workspace_size(dcp.make_shape(**base), N_Q),
+         "dz_rows": N_Q * n * c_z * act, "ds": n * c_s * grad, "dw_b": h * c_z * grad, "dln_gamma": c_z * grad}
+    b.update({k: hd * c_s * 4 for k in ("w_q", "w_k", "w_v", "w_g")})
+    b.update({k: hd * c_s * grad for k in ("dw_q", "dw_k", "dw_v", "dw_g")})
+    return b
+
+
+def placed(base, grad_dtype, at):
+    sh = dcp.make_shape(**base)
+    w = dcp.make_weights(**{k: at[k] for k in ("w_q", "w_k", "w_v", "w_g", "w_b", "ln_gamma")})
+    g = dcp.make_gradients(**{k: at[k] for k in GRADS}, dtype=grad_dtype)
+    return dcp.lib().dcp_pair_bias_attention_backward(
+        ctypes.byref(sh), ctypes.byref(w), at["s"], at["z"], at["mask"], 0, N_Q, at["m"], at["l"], at["acc"], at["dout"],
+        ctypes.byref(g), at["ws"], 1 << 50, None)
+
+
+@pytest.mark.parametrize("base", [GENERAL, FUSED], ids=["general", "fused"])
+@pytest.mark.parametrize("grad_dtype", [0, 1])
+def test_gradients_that_overlap_are_refused(base, grad_dtype):
+    """Each gradient and the workspace at the start of every other tensor and at its last piece; a range
+    that only touches another is none, so that the refusal names a third one, put on s."""
+    apart = {k: v << 40 for k, v in PLACES.items()}
+    size = sizes(base, 2 if grad_dtype else 4)
+    for a in GRADS + ("ws",):
+        for b in (k for k in PLACES if k != a):
+            last = (size[b] - 1) // 256 * 256
+            for at in (0, last):
+                assert placed(base, grad_dtype, {**apart, a: apart[b] + at}) == BAD, (a, b)
+                assert "overlap" in dcp.dcp_last_error(), (a, b, dcp.dcp_last_error())
+            third = next(k for k in GRADS if k not in (a, b))
+            assert placed(base, grad_dtype, {**apart, a: apart[b] + last + 256, third: apart["s"]}) == BAD
+            assert third in dcp.dcp_last_error().replace(",", " ").split(), (a, b, third, dcp.dcp_last_error())
