@@ -129,8 +129,12 @@ def _ptr(x: Ptr) -> Optional[int]:
 def _stream(stream) -> Optional[int]:
     if stream is None:
         import torch
-        # the current stream's handle without the Stream object around it, which took 3 us a call
-        return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device()) or None
+        # the current stream's handle without the Stream object around it, which takes 3 us a call, where
+        # this torch has that; it is no public name of torch's
+        raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+        if raw is None:
+            return torch.cuda.current_stream().cuda_stream or None
+        return raw(torch.cuda.current_device()) or None
     if isinstance(stream, int):
         return stream or None
     return stream.cuda_stream or None
