@@ -317,6 +317,7 @@ __device__ __forceinline__ void load_key(__amdgpu_buffer_rsrc_t zres, int zoff, 
 // A workgroup's four waves split a tile's keys for the bias, which goes through LDS in two
 // buffers, and the heads for the rest, as in pairs_kernel; a lane keeps a running maximum of its
 // own (row n, keys 4g..4g+3), and the four lanes of a row meet at the end.
+typedef const __attribute__((address_space(4))) uint32_t* const_u32_ptr;
 constexpr float kLowest = -3e38f;  // below every logit, and finite: kLowest - kLowest is 0
 
 __global__ void __launch_bounds__(256, 2) stats_kernel(FastBackArgs a) {
@@ -328,7 +329,9 @@ __global__ void __launch_bounds__(256, 2) stats_kernel(FastBackArgs a) {
   chunk_of_32((uint32_t)(a.n_pad / 16), a.stat_parts, blockIdx.y, &t_count, &t_begin);
   const int64_t t_end = t_begin + t_count;
   constexpr int kHw = kH / 4;
-  uint32_t bits = t_begin < t_end ? a.tile_valid[t_begin] : 0u;
+  // (a scalar load: a vector load's wait would be for all of z that came before it)
+  const const_u32_ptr valid_bits = (const_u32_ptr)(uintptr_t)a.tile_valid;
+  uint32_t bits = t_begin < t_end ? valid_bits[t_begin] : 0u;
   const float s_scale = ldexpf(1.0f, -a.exps[0] - a.exps[1]);
   const int64_t rows_here = min((int64_t)kTileQ, a.n_q - q0);
   const int row_bytes = (int)(a.n_tok * (kCz * 2));
@@ -360,14 +363,15 @@ __global__ void __launch_bounds__(256, 2) stats_kernel(FastBackArgs a) {
   const bool row_there = n < rows_here;
   int buf = 0;
   for (int64_t t = t_begin; t < t_end; ++t, buf ^= 1) {
-    const uint32_t bits_next = t + 1 < t_end ? a.tile_valid[t + 1] : 0u;
-    f16x8 k[kHw], v[kHw];  // in flight during the bias
+    const uint32_t bits_next = t + 1 < t_end ? valid_bits[t + 1] : 0u;
+    f16x8 k[kHw], v[kHw];  // in flight during the bias, and ahead of the next z, which their waits leave in flight
 #pragma unroll
     for (int j = 0; j < kHw; ++j) {
       const int so = ((kHw * wave + j) * n_tiles + (int)t) * 1024;
       k[j] = as_f16x8(__builtin_amdgcn_raw_buffer_load_b128(kres, 64 * n + 16 * g, so, 0));
       v[j] = as_f16x8(__builtin_amdgcn_raw_buffer_load_b128(vres, 64 * n + 16 * g, so, 0));
     }
+    __builtin_amdgcn_sched_barrier(0);
     f32x4 b[4];
 #pragma unroll
     for (int kk = 0; kk < 4; ++kk) {
