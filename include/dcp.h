@@ -454,7 +454,7 @@ int dcp_scatter_mean(int64_t n_atoms, int64_t n_tokens, int32_t c, int32_t in_dt
  *   x        [n_rows, c] in_dtype
  *   ln_gamma, ln_beta  [c] fp32 or NULL (= 1 / 0)
  *   y        [n_rows, c] out_dtype; may be x itself where the types are the same,
- *            and must not overlap it otherwise
+ *            and must not overlap it otherwise, nor the weights
  *   c        1 <= c <= 4096
  * Device pointers aligned to their element size; rows of whole 16-byte pieces
  * (c a multiple of 8 in bf16, of 4 in fp32) in 16-byte aligned tensors are read
@@ -473,7 +473,8 @@ int dcp_layer_norm_backward_workspace_size(int64_t n_rows, int32_t c, size_t* by
  *              that depends on n_rows, c and alignment only (n_rows = 0 gives 0)
  *   workspace  at least dcp_layer_norm_backward_workspace_size() bytes, 256-byte
  *              aligned; may be NULL when dln_gamma and dln_beta are
- * At least one gradient is wanted. The statistics are formed again from x. */
+ * dln_gamma, dln_beta and the workspace must not overlap each other or the other
+ * tensors, nor dx the weights. At least one gradient is wanted. The statistics are formed again from x. */
 int dcp_layer_norm_backward(int64_t n_rows, int32_t c, int32_t in_dtype, int32_t out_dtype, float ln_eps, const void* x,
                             const float* ln_gamma, const void* dy, void* dx, float* dln_gamma, float* dln_beta,
                             void* workspace, size_t workspace_bytes, void* stream);

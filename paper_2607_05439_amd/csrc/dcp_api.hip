@@ -1076,6 +1076,9 @@ int dcp_layer_norm(int64_t n_rows, int32_t c, int32_t in_dtype, int32_t out_dtyp
     return fail(DCP_ERR_INVALID_ARGUMENT, "x, y, ln_gamma and ln_beta must be aligned to their element size");
   if (!apart_or_same(x, (size_t)n_rows * c * elem(in_dtype), y, (size_t)n_rows * c * elem(out_dtype)))
     return fail(DCP_ERR_INVALID_ARGUMENT, "y must equal x, in the same type, or not overlap it");
+  const Extent all[] = {{"y", y, (size_t)n_rows * c * elem(out_dtype)}, {"ln_gamma", ln_gamma, c * sizeof(float)},
+                        {"ln_beta", ln_beta, c * sizeof(float)}};
+  if (const int overlaps = check_apart(all, 3, 1)) return overlaps;
   dcp::LayerNormArgs a{};
   a.n_rows = n_rows;
   a.c = c;
@@ -1130,6 +1133,12 @@ int dcp_layer_norm_backward(int64_t n_rows, int32_t c, int32_t in_dtype, int32_t
       return fail(DCP_ERR_WORKSPACE, "workspace too small: %zu bytes given, %zu needed", workspace_bytes, need);
     a.parts = static_cast<float*>(workspace);
   }
+  const Extent all[] = {{"dln_gamma", dln_gamma, c * sizeof(float)}, {"dln_beta", dln_beta, c * sizeof(float)},
+                        {"workspace", a.parts, a.parts ? layer_norm_back_ws(n_rows, c) : 0}, {"dx", dx, xb},
+                        {"ln_gamma", ln_gamma, c * sizeof(float)}, {"x", x, xb}, {"dy", dy, yb}};
+  int overlaps = check_apart(all, 7, 3);
+  if (!overlaps) overlaps = check_apart(all + 3, 2, 1);  // dx may be x or dy (above), not the weights
+  if (overlaps) return overlaps;
   const hipError_t e = dcp::launch_layer_norm_back(a, in_dtype == DCP_BF16, out_dtype == DCP_BF16,
                                                    static_cast<hipStream_t>(stream));
   if (e != hipSuccess) return fail(DCP_ERR_HIP, "LayerNorm backward launch failed: %s", hipGetErrorString(e));

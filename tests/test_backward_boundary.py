@@ -181,3 +181,19 @@ def test_gradients_that_overlap_are_refused(base, grad_dtype):
             third = next(k for k in GRADS if k not in (a, b))
             assert placed(base, grad_dtype, {**apart, a: apart[b] + last + 256, third: apart["s"]}) == BAD
             assert third in dcp.dcp_last_error().replace(",", " ").split(), (a, b, third, dcp.dcp_last_error())
+
+
+@pytest.mark.parametrize("in_t,out_t", [(0, 0), (1, 1), (0, 1), (1, 0)])
+def test_layer_norm_s_sums_and_workspace_lie_apart(in_t, out_t):
+    """dln_gamma, dln_beta and the workspace on each other and on the rows' tensors, and rows written onto
+    weights: refused."""
+    rows, c = 1000, 64
+    at = {k: (i + 1) << 40 for i, k in enumerate(("x", "dy", "dx", "gamma", "dgamma", "dbeta", "ws"))}
+    size = {"x": rows * c * (2 if in_t else 4), "dy": rows * c * (2 if out_t else 4), "dx": rows * c * (2 if in_t else 4),
+            "gamma": c * 4, "dgamma": c * 4, "dbeta": c * 4, "ws": dcp.dcp_layer_norm_backward_workspace_size(rows, c)}
+    for a, b in [(a, b) for a in ("dgamma", "dbeta", "ws") for b in at if b != a] + [("dx", "gamma")]:
+        for off in (0, (size[b] - 1) // 256 * 256):
+            assert layer_norm_back(rows, c, in_t, out_t, **{**at, a: at[b] + off}) == BAD, (a, b)
+            assert "overlap" in dcp.dcp_last_error(), (a, b)
+    for b in ("gamma", "beta"):
+        assert layer_norm(rows, c, in_t, out_t, x=FAKE, y=FAR, **{b: FAR + 512}) == BAD and "overlap" in dcp.dcp_last_error()
