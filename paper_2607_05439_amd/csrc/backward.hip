@@ -1,8 +1,8 @@
 // Backward pass of the pair-biased gated attention: the steps that every shape
 // shares, and the pair kernels of the general fp32 path (gfx950).
 //
-// With P = exp(l - m) / L recomputed from the saved state, o = acc / L, and
-// dout the gradient of the gated output:
+// With P = exp(l - m) / L recomputed from the saved state (the fused shape sums its own
+// M, L and D: backward_fast.hip), o = acc / L, and dout the gradient of the gated output:
 //   do = g dout, D = do . o, dP = do . v, dS = P (dP - D),
 //   dq_i = sum_j dS k_j / sqrt(d), dk_j = sum_i dS q_i / sqrt(d), dv_j = sum_i P do_i,
 //   dg = dout o g (1 - g)                      (before the sigmoid)
@@ -845,9 +845,9 @@ hipError_t launch_back_sum(const BackSumArgs& a, hipStream_t st) {
 
 // Splits of the token products' depths: one workgroup a CU where they are `step` deep,
 // about four where they are twice that; dW, whose depth grows with the tokens and whose
-// tiles do not, in up to four all the same. Fused, step 128: 128 tokens with ds in 12
-// splits 54 us, in 6 56; 333 in 7 68, in 12 69; 1024 in 5 208, in 2 211, and with dW in 4
-// 208, in 7 210. General, step 32 (64): 128 tokens 33 us (34), 601 175 (177).
+// tiles do not, in up to four all the same. Fused, step 128, us of a call: 128 tokens with ds in
+// 12 splits 62, in 6 64; 333 in 7 or 12 81; 1024 in 5 272, in 2 278, and with dW in 4 272, in
+// 7 274, in one 280. General, step 32 (64): 128 tokens 33 us (34), 601 175 (177).
 void back_gemm_splits(int64_t n_tok, int32_t hd, int32_t c_s, int32_t step, int* ds_splits, int* w_splits) {
   const int64_t c_tiles = (c_s + kGemm - 1) / kGemm, o_tiles = (hd + kGemm - 1) / kGemm;
   const int64_t ds_tiles = (n_tok + kGemm - 1) / kGemm * c_tiles, w_tiles = 4 * o_tiles * c_tiles, ds_depth = 4 * (int64_t)hd;

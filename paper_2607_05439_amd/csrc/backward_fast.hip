@@ -18,8 +18,8 @@
 // magnitude lies in [2^11, 2^12) (P, at most 1, by 2^14; dS then by what keeps it below
 // 2^16), fp16 holds 11 bits down to 2^-25 of that, and the fp32 results are scaled
 // back exactly. Every row of dout has a power of its own for what stays in the row (dS,
-// dz, dq), and joins the others at the tensor's where rows are summed. Only z enters as the bf16 it is, against bias weights split into
-// bf16 hi + lo (pair_bias.h).
+// dz, dq), and joins the others at the tensor's where rows are summed. Only z enters as
+// the bf16 it is, against bias weights split into bf16 hi + lo (pair_bias.h).
 #include <hip/hip_runtime.h>
 #include <math.h>
 #include <stdint.h>
@@ -311,9 +311,11 @@ __device__ __forceinline__ void load_key(__amdgpu_buffer_rsrc_t zres, int zoff, 
 // The forward's saved m, l and acc will not do for them: it forms S from bf16 q and k and sums
 // bf16 v, so that P = exp(S - m) / l with the S of fp16 operands has rows that do not sum to 1,
 // and D = do . acc / l is not sum P dP, by 2^-9 of the logits' size: gradients were off by 1.4e-2 at
-// logits of 22 and 2.9e-2 at 44, with these sums by 2.0e-3 and 2.5e-3. That takes z once more
-// (2400 rows of 4800 tokens 1613 us, so 2205; 1024 tokens 210, so 274). Of the state there
-// remain o for dg (pack_kernel) and the rows whose l is 0.
+// logits of 22 and 2.9e-2 at 44, with these sums by 2.0e-3 and 2.5e-3. That takes z once more:
+// 2400 rows of 4800 tokens 535 us in a call of 2162, 1024 tokens 59 in 273, 333 tokens 12.5 in
+// 81. Of the state there remain o for dg (pack_kernel) and the rows whose l is 0.
+// Bound by memory: 2.98 GB at 5.6 TB/s for those 2400 rows, 60% of the waves' time waiting
+// for it.
 // A workgroup's four waves split a tile's keys for the bias, which goes through LDS in two
 // buffers, and the heads for the rest, as in pairs_kernel; a lane keeps a running maximum of its
 // own (row n, keys 4g..4g+3), and the four lanes of a row meet at the end.
@@ -439,11 +441,13 @@ __global__ void __launch_bounds__(256, 2) stats_kernel(FastBackArgs a) {
 //      and T += dS^T zh over the rows. dz leaves through LDS, four whole rows of 256
 //      bytes to a store. A key's registers are refilled with the next tile's z as soon
 //      as its dz is formed.
-// The rows' q and do stay in LDS: read again from L2 for each tile, 1024 tokens took 210
-// us (208 so) and 2400 rows of 4800 1662 (1635).
-// Bound by memory: 2400 rows of 4800 tokens 1387 us for 3.06 GB read and 3.37 written (z and
-// dz 2.95 each, P 0.37), 4.7 TB/s where a copy of 8 GiB reaches 4.5. 1024 tokens, where
-// 512 workgroups have eight tiles each: 138 us, 4.2 TB/s.
+// The rows' q and do stay in LDS: read again from L2 for each tile, calls took 2 us more for
+// 1024 tokens and 27 for 2400 rows of 4800.
+// 2400 rows of 4800 tokens: 1417 us for 3.14 GB read and 3.37 written (z and dz 2.95 each, P
+// 0.37), 4.6 TB/s, where LayerNorm's kernels read and write at 5.4. Of the waves' time a vector
+// instruction is active a fifth and waits are a third; registers and LDS allow two workgroups a
+// CU, with three barriers a tile. 1024 tokens, where 512 workgroups have eight tiles each: 143
+// us, 4.1 TB/s.
 struct PairLds {
   union {
     f32x4 bias[kH][kTileQ][4];         // 16 KB: [head][row][4 keys, chunk ^ row / 4]
@@ -700,8 +704,8 @@ __global__ void __launch_bounds__(256, 2) pairs_kernel(FastBackArgs a) {
 // dk and dv of 64 keys of one head over a share of the chunk's row tiles: the four waves
 // take every fourth of them, and their sums meet in LDS. dS = P (dP - D) is formed again
 // from P and one more product, dP = dO V^T: stored beside P it took as many bytes again,
-// written and read (the whole call 1784 us then, 1672 so, for 2400 rows of 4800 tokens),
-// and P's 32 bytes a pair are what bounds this kernel: 102 us there, 3.6 TB/s.
+// written and read (112 us more in a call for 2400 rows of 4800 tokens), and P's 32 bytes a
+// pair are what bounds this kernel: 102 us there, 3.6 TB/s.
 __global__ void __launch_bounds__(256, 3) keys_kernel(FastBackArgs a) {
   __shared__ f32x4 s_sum[16][64];
   const int lane = threadIdx.x & 63, n = lane & 15, g = lane >> 4;

@@ -1169,9 +1169,12 @@ struct BackLayout {
 
 // Parts that the fused backward splits a row tile's keys into: two workgroups fit a CU,
 // so a launch runs in rounds of 512, each as long as its part's tiles and about one
-// tile's time for its start and end; the fewest parts within 1% of the cheapest. 750
-// rows of 12000 tokens (47 row tiles): 1450 us in 10 parts, 1411 in 21, 1502 in 16, 1863
-// in 11; 1024 tokens: 213 us in 8, 232 in 16, 239 in 4; 333 tokens: 69 us in 21, 71 in 11.
+// tile's time for its start and end; the fewest parts within 1% of the cheapest, and `most`
+// at most. The gradients' (64 at most), us of a call: 750 rows of 12000 tokens (47 row tiles)
+// 1856 in 21 parts, 1901 in 10, 1962 in 16, 2313 in 11; 1024 tokens 273 in 8, 290 in 16, 312
+// in 4; 333 tokens 81 in 21, 83 in 11. The row statistics' (16 at most): 750 rows of 12000
+// 1860 in 10, 1844 in 16, 1932 in 8, 1989 in 11; 2400 of 4800 2208 in 10, 2230 in 3, 2276 in 7,
+// 2253 in 24; 1024 tokens 272 in 8, 276 in 4, 279 in 16; 333 tokens 81 in 11, 84 in 16, 87 in 4.
 int fast_back_parts(int64_t groups, int64_t tiles, int64_t most) {
   const int64_t cap = tiles < most ? tiles : most;
   int64_t cost[65], best = 0;
@@ -1208,7 +1211,7 @@ void back_layout(const dcp_shape* sh, Path path, int64_t n_q, BackLayout* L) {
     if (L->chunk > L->nq_pad) L->chunk = L->nq_pad;
     const int64_t groups = L->chunk / 16;
     L->dq_parts = fast_back_parts(groups, L->n_pad / 16, 64);
-    // (few: every workgroup behind them adds them up)
+    // (every workgroup behind them adds them up)
     L->stat_parts = fast_back_parts(L->nq_pad / 16, L->n_pad / 16, 16);
     L->t_parts = (int)groups * L->dq_parts;
     const size_t rows = (size_t)H * L->nq_pad * dcp::kFastDp * 2, keys = (size_t)H * L->n_pad * dcp::kFastDp * 2;

@@ -389,9 +389,10 @@ bool ln_vec(int c, bool x_bf16, const void* x, const void* o, const void* o2) {
   return c % (x_bf16 ? 8 : 4) == 0 && p % 16 == 0;
 }
 
-// Rows per round of a workgroup (as if its rows took 16-byte pieces of 2 bytes: the
-// count of workgroups must not depend on alignment, which the workspace query does
-// not know).
+// Rounds of workgroups over the rows, counted as if a row lay in pieces of eight elements:
+// the count of workgroups must not depend on the type or the alignment, which the workspace
+// query does not know. fp32 rows lie in pieces of four, so rows of up to 256 channels take
+// twice the rounds that are counted, and rows read element by element more.
 int64_t ln_rounds(int64_t n_rows, int c) {
   const int per_group = 64 * kLnWaves / ln_split(c, 8).lanes;
   return (n_rows + per_group - 1) / per_group;
@@ -399,10 +400,15 @@ int64_t ln_rounds(int64_t n_rows, int c) {
 
 }  // namespace
 
-// Workgroups of the backward: four a CU, two where they would have little more than a round
-// each, since a workgroup's start and its sums take as long as some. 4800 rows of 384 (1200
-// rounds) in 512 10.2 us, in 1024 11.3; 16384 of 128 (1024) 9.6 and 10.8; 100000 of 32 fp32 (1563)
-// 13.0 and 12.5; a million of 128 167 and 149, in 2048 166.
+// Workgroups of the backward: four a CU, two up to 1280 counted rounds, since a workgroup's start
+// and its sums take as long as some rounds. us a call in 512 and in 1024 workgroups, with the
+// rounds counted, below the cut: bf16 4800 rows of 384 (1200) 10.4 and 12.3, 16384 of 128 (1024)
+// 9.7 and 11.1; fp32 4800 of 384 (1200) 11.5 and 13.6, 16384 of 128 (1024) 11.6 and 12.1, 60000 of
+// 32 (938) 10.8 and 11.0. Beyond it: bf16 8000 of 384 (2000) 12.7 and 14.1, 40000 of 128 (2500)
+// 14.1 and 14.2, 24000 of 384 (6000) 22.3 and 20.8, a million of 128 167 and 149 (in 2048 166);
+// fp32 8000 of 384 13.9 and 15.5, 20500 of 128 (1282) 12.5 and 12.7, 40000 of 128 (2500) 17.4 and
+// 16.8, 100000 of 32 (1563) 13.3 and 12.8. So the cut is right for narrow fp32 rows, which take
+// twice the rounds counted, and up to twice too low for the others, which lose up to 17% there.
 int layer_norm_back_groups(int64_t n_rows, int32_t c) {
   const int64_t rounds = ln_rounds(n_rows, c), most = rounds <= 1280 ? 512 : 1024;
   return (int)(rounds < most ? rounds : most);
