@@ -213,8 +213,8 @@ def _own_checkpoint(st):
     codes = _kept(st, "codes", lambda: torch.empty((rows, c), dtype=torch.int8, device="cuda"))
     exponents = _kept(st, "exponents", lambda: torch.empty((rows, -(-c // BLOCK)), dtype=torch.uint8, device="cuda"))
     y = _kept(st, "y", lambda: torch.empty_like(x))
-    dcp.dcp_checkpoint8_pack(rows, c, code, x, codes, exponents)
-    dcp.dcp_checkpoint8_unpack(rows, c, code, codes, exponents, y)
+    dcp.dcp_checkpoint_pack(rows, c, code, x, codes, exponents)
+    dcp.dcp_checkpoint_unpack(rows, c, code, codes, exponents, y)
     return y
 
 
