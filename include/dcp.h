@@ -479,6 +479,121 @@ int dcp_layer_norm_backward(int64_t n_rows, int32_t c, int32_t in_dtype, int32_t
                             const float* ln_gamma, const void* dy, void* dx, float* dln_gamma, float* dln_beta,
                             void* workspace, size_t workspace_bytes, void* stream);
 
+/* ---------------------------------------------------------------------------
+ * Backward pass of the pair transition: the gradients of a scalar with respect to the
+ * transition's input and weights, from its gradient with respect to the output. A, B and
+ * everything else of the hidden width is formed again from z; nothing but z is kept
+ * between the passes, as it is or as an 8-bit checkpoint (below).
+ * ------------------------------------------------------------------------- */
+
+/* Device pointers that receive gradients, aligned as their tensors are, or NULL for one
+ * that is not wanted (at least one is). All are overwritten; those of the weights are these
+ * pairs' share, to be added over the stripes by the caller. */
+typedef struct {
+  void* dz;        /* [n_pairs, c_z] act_dtype; may be dz_out itself              */
+  void* dw1;       /* [hidden, c_z] dtype                                         */
+  void* dw2;       /* [hidden, c_z] dtype                                         */
+  void* dw3;       /* [c_z, hidden] dtype                                         */
+  void* dln_gamma; /* [c_z] dtype                                                 */
+  void* dln_beta;  /* [c_z] dtype                                                 */
+  int32_t dtype;   /* dcp_dtype of all but dz                                     */
+} dcp_transition_gradients;
+
+/* Workspace bytes of dcp_pair_transition_backward (written to *bytes). Host-only. */
+int dcp_pair_transition_backward_workspace_size(int64_t n_pairs, int32_t c_z, int32_t hidden, int32_t act_dtype,
+                                                size_t* bytes);
+
+/* Gradients of z_out = z + W3 (SiLU(W1 N) * W2 N), N = LayerNorm(z), as dcp_pair_transition
+ * computes it (weights, ln_eps and supported shapes are its).
+ *   z            [n_pairs, c_z] act_dtype: the transition's input; or, where z_exponents is
+ *                not NULL, its checkpoint's int8 codes [n_pairs, c_z]
+ *   z_exponents  [n_pairs, ceil(c_z / 32)] uint8: the checkpoint's exponents, or NULL
+ *   dz_out       [n_pairs, c_z] act_dtype: the gradient of the transition's output
+ *   workspace    at least dcp_pair_transition_backward_workspace_size() bytes, 256-byte
+ *                aligned; contents on entry are ignored
+ * In bf16, z, dz_out and dz are 16-byte aligned and z_exponents 4-byte; in fp32 all are
+ * aligned to their element size, and 16 bytes are fastest. What is written (the gradients
+ * and the workspace) must not overlap the inputs or each other, but for dz = dz_out.
+ * Without pairs the weights' gradients are 0, and z and dz_out may be NULL.
+ * act_dtype = F32: fp32 throughout. */
+int dcp_pair_transition_backward(int64_t n_pairs, int32_t c_z, int32_t hidden, int32_t act_dtype, float ln_eps,
+                                 const float* w1, const float* w2, const float* w3, const float* ln_gamma,
+                                 const float* ln_beta, const void* z, const uint8_t* z_exponents, const void* dz_out,
+                                 const dcp_transition_gradients* grads, void* workspace, size_t workspace_bytes,
+                                 void* stream);
+
+/* ---------------------------------------------------------------------------
+ * Activation checkpoints in 8 bits: rows kept between a forward and its backward pass in
+ * half the memory of bf16. Every 32 consecutive channels of a row (the last block of a row
+ * may be shorter) share a power of two:
+ *   e = the least integer >= -126 for which rint(max |x| 2^-e) <= 127 over the block, at most 121,
+ *   code = rint(x 2^-e) (ties to even), exponent byte = e + 127, value read back = code 2^e
+ * (magnitudes over 127 2^121 = 3.38e38, of which the codes would pass 127, read back as that).
+ * The values read back are off by at most 2^(e-1), which is between 1/255 and 1/127.5 of
+ * the block's largest magnitude, and are exact in bf16 and fp32. A block with a NaN or an
+ * infinity has the byte 255 and reads back as NaN. dcp_pair_transition_backward reads
+ * checkpoints itself; for other uses they are read back, whole or a stripe of rows.
+ * ------------------------------------------------------------------------- */
+
+/*   x          [n_rows, c] dtype
+ *   codes      [n_rows, c] int8
+ *   exponents  [n_rows, ceil(c / 32)] uint8
+ *   c          1 <= c <= 65536
+ * Device pointers aligned to their element size; whole blocks (c a multiple of 32) in
+ * 16-byte aligned tensors (the exponents 4-byte) are fastest. What is written must not
+ * overlap the rest. n_rows = 0 is a no-op. */
+int dcp_checkpoint_pack(int64_t n_rows, int32_t c, int32_t dtype, const void* x, int8_t* codes, uint8_t* exponents,
+                        void* stream);
+int dcp_checkpoint_unpack(int64_t n_rows, int32_t c, int32_t dtype, const int8_t* codes, const uint8_t* exponents,
+                          void* x, void* stream);
+
+/* ---------------------------------------------------------------------------
+ * Relative position encoding of the pair track, and its table's gradient (Appendix,
+ * relative-position sub-chunking: one-hots of the residue offset and the token offset
+ * clipped to +-32, the chain hop clipped to +-2 and the same entity, through a linear layer
+ * without bias). A one-hot times the layer's weights is a row of them, so the call takes the
+ * transposed weights as a table and adds its rows; no one-hot is formed.
+ *   bucket_f(i, j) = clamp(position_f[i] - position_f[j], -r_f, r_f) + r_f  where group_f[i] = group_f[j],
+ *                    2 r_f + 1                                              elsewhere,
+ *   z_out[i, j, :] = z_in[i, j, :] + sum over f of table[first_f + bucket_f(i, j), :]
+ * with first_f the sum of (2 r_k + 2) over the fields k before f. (The same entity: a field
+ * with radius 0 whose positions are all alike and whose groups are the entities.)
+ * ------------------------------------------------------------------------- */
+typedef struct {
+  const int32_t* position; /* [n_tokens]                                          */
+  const int32_t* group;    /* [n_tokens], or NULL: all tokens are of one group    */
+  int32_t radius;          /* 0 <= r <= 127                                       */
+} dcp_relative_field;
+
+/* The encoding of rows [row0, row0 + n_rows) of the pair track.
+ *   fields   [n_fields] in host memory, 1 <= n_fields <= 4
+ *   table    [sum of (2 r_f + 2), c] fp32
+ *   z_in     [n_rows, n_tokens, c] dtype, or NULL (= 0); may be z_out itself
+ *   z_out    [n_rows, n_tokens, c] dtype; must not overlap the rest
+ *   c        1 <= c <= 1024
+ * The rows of the table are added in the fields' order in fp32, the sum to z, and the result
+ * is rounded once. Device pointers aligned to their element size; rows of whole 16-byte
+ * pieces in 16-byte aligned tensors are fastest. n_rows = 0 is a no-op. No workspace. */
+int dcp_relative_position(int64_t n_tokens, int64_t row0, int64_t n_rows, int32_t c, int32_t dtype, int32_t n_fields,
+                          const dcp_relative_field* fields, const float* table, const void* z_in, void* z_out,
+                          void* stream);
+
+/* Workspace bytes of dcp_relative_position_backward (written to *bytes). Host-only; of the
+ * fields only the radii are read. */
+int dcp_relative_position_backward_workspace_size(int64_t n_tokens, int64_t n_rows, int32_t c, int32_t n_fields,
+                                                  const dcp_relative_field* fields, size_t* bytes);
+
+/* The table's gradient (arguments as above) from that of z_out, which is that of z_in too:
+ *   dz_rows    [n_rows, n_tokens, c] dtype (may be NULL without rows)
+ *   dtable     [sum of (2 r_f + 2), c] fp32, overwritten: dtable[first_f + b, :] is the sum of
+ *              dz over the pairs whose bucket of field f is b (0 for one that none has), in
+ *              fp32 and in a fixed order; the stripe's share, to be added over the stripes
+ *   workspace  at least dcp_relative_position_backward_workspace_size() bytes, 256-byte aligned
+ * What is written must not overlap the rest. */
+int dcp_relative_position_backward(int64_t n_tokens, int64_t row0, int64_t n_rows, int32_t c, int32_t dtype,
+                                   int32_t n_fields, const dcp_relative_field* fields, const void* dz_rows,
+                                   float* dtable, void* workspace, size_t workspace_bytes, void* stream);
+
 /* Optional timing hook: when both are non-NULL hipEvent_t handles, the calling
  * thread's next dcp_pair_bias_attention, dcp_sparse_pair_bias_attention,
  * dcp_knn_topk, dcp_pair_transition and dcp_scatter_mean calls record

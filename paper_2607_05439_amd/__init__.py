@@ -8,7 +8,10 @@ used for device memory and streams. The functions carry the C names
 ``dcp_pair_transition``, ``dcp_transition_workspace_size``, ``dcp_scatter_mean``,
 ``dcp_scatter_mean_workspace_size``, ``dcp_layer_norm``, ``dcp_layer_norm_backward``,
 ``dcp_layer_norm_backward_workspace_size``, ``dcp_pair_bias_attention_backward``,
-``dcp_pair_bias_attention_backward_workspace_size``) and accept torch tensors (device pointers are taken
+``dcp_pair_bias_attention_backward_workspace_size``, ``dcp_pair_transition_backward``,
+``dcp_pair_transition_backward_workspace_size``, ``dcp_checkpoint_pack``, ``dcp_checkpoint_unpack``,
+``dcp_relative_position``, ``dcp_relative_position_backward``,
+``dcp_relative_position_backward_workspace_size``) and accept torch tensors (device pointers are taken
 from ``data_ptr()``) or plain integer addresses. Loading fails loudly when the
 library has not been built: there is no fallback.
 """
@@ -29,6 +32,9 @@ EXPORTS = ("dcp_workspace_size", "dcp_workspace_bytes", "dcp_pair_bias_attention
            "dcp_transition_workspace_size", "dcp_pair_transition", "dcp_scatter_mean_workspace_size",
            "dcp_scatter_mean", "dcp_layer_norm", "dcp_layer_norm_backward_workspace_size", "dcp_layer_norm_backward",
            "dcp_pair_bias_attention_backward_workspace_size", "dcp_pair_bias_attention_backward",
+           "dcp_pair_transition_backward_workspace_size", "dcp_pair_transition_backward",
+           "dcp_checkpoint_pack", "dcp_checkpoint_unpack", "dcp_relative_position",
+           "dcp_relative_position_backward_workspace_size", "dcp_relative_position_backward",
            "dcp_set_timing_events",
            "dcp_last_error", "dcp_version")
 
@@ -52,6 +58,15 @@ class DcpWeights(ctypes.Structure):
 class DcpGradients(ctypes.Structure):
     _fields_ = [(n, ctypes.c_void_p) for n in ("dz_rows", "ds", "dw_q", "dw_k", "dw_v", "dw_g", "dw_b", "dln_gamma")]
     _fields_.append(("dtype", ctypes.c_int32))
+
+
+class DcpTransitionGradients(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in ("dz", "dw1", "dw2", "dw3", "dln_gamma", "dln_beta")]
+    _fields_.append(("dtype", ctypes.c_int32))
+
+
+class DcpRelativeField(ctypes.Structure):
+    _fields_ = [("position", ctypes.c_void_p), ("group", ctypes.c_void_p), ("radius", ctypes.c_int32)]
 
 
 class DcpSparseShape(ctypes.Structure):
@@ -97,6 +112,15 @@ def lib() -> ctypes.CDLL:
         L.dcp_pair_bias_attention_backward_workspace_size.argtypes = [P(DcpShape), i64, P(sz)]
         L.dcp_pair_bias_attention_backward.argtypes = [P(DcpShape), P(DcpWeights), vp, vp, vp, i64, i64, vp, vp, vp, vp,
                                                        P(DcpGradients), vp, sz, vp]
+        L.dcp_pair_transition_backward_workspace_size.argtypes = [i64, i32, i32, i32, P(sz)]
+        L.dcp_pair_transition_backward.argtypes = [i64, i32, i32, i32, ctypes.c_float, vp, vp, vp, vp, vp, vp, vp, vp,
+                                                   P(DcpTransitionGradients), vp, sz, vp]
+        L.dcp_checkpoint_pack.argtypes = [i64, i32, i32, vp, vp, vp, vp]
+        L.dcp_checkpoint_unpack.argtypes = [i64, i32, i32, vp, vp, vp, vp]
+        L.dcp_relative_position.argtypes = [i64, i64, i64, i32, i32, i32, P(DcpRelativeField), vp, vp, vp, vp]
+        L.dcp_relative_position_backward_workspace_size.argtypes = [i64, i64, i32, i32, P(DcpRelativeField), P(sz)]
+        L.dcp_relative_position_backward.argtypes = [i64, i64, i64, i32, i32, i32, P(DcpRelativeField), vp, vp, vp, sz,
+                                                     vp]
         L.dcp_set_timing_events.argtypes = [vp, vp]
         for f in (L.dcp_workspace_size, L.dcp_pair_bias_attention, L.dcp_pair_bias_attention_noalloc,
                   L.dcp_pair_bias_attention_partial,
@@ -105,7 +129,10 @@ def lib() -> ctypes.CDLL:
                   L.dcp_transition_workspace_size, L.dcp_pair_transition, L.dcp_scatter_mean_workspace_size,
                   L.dcp_scatter_mean, L.dcp_layer_norm, L.dcp_layer_norm_backward_workspace_size,
                   L.dcp_layer_norm_backward, L.dcp_pair_bias_attention_backward_workspace_size,
-                  L.dcp_pair_bias_attention_backward, L.dcp_set_timing_events):
+                  L.dcp_pair_bias_attention_backward, L.dcp_pair_transition_backward_workspace_size,
+                  L.dcp_pair_transition_backward, L.dcp_checkpoint_pack, L.dcp_checkpoint_unpack,
+                  L.dcp_relative_position, L.dcp_relative_position_backward_workspace_size,
+                  L.dcp_relative_position_backward, L.dcp_set_timing_events):
             f.restype = ctypes.c_int
         L.dcp_last_error.restype = ctypes.c_char_p
         L.dcp_last_error.argtypes = []
@@ -310,6 +337,59 @@ def dcp_pair_bias_attention_backward(shape: DcpShape, weights: DcpWeights, s: Pt
                                                   _ptr(key_mask), q_row0, n_q, _ptr(m), _ptr(l), _ptr(acc),
                                                   _ptr(dout), ctypes.byref(grads), _ptr(workspace), workspace_bytes,
                                                   _stream(stream)))
+
+
+def make_transition_gradients(dz: Ptr = None, dw1: Ptr = None, dw2: Ptr = None, dw3: Ptr = None, dln_gamma: Ptr = None,
+                              dln_beta: Ptr = None, dtype: int = DCP_F32) -> DcpTransitionGradients:
+    return DcpTransitionGradients(*[_ptr(x) for x in (dz, dw1, dw2, dw3, dln_gamma, dln_beta)], dtype)
+
+
+def dcp_pair_transition_backward_workspace_size(n_pairs: int, c_z: int, hidden: int, act_dtype: int) -> int:
+    out = ctypes.c_size_t()
+    _check(lib().dcp_pair_transition_backward_workspace_size(n_pairs, c_z, hidden, act_dtype, ctypes.byref(out)))
+    return out.value
+
+
+def dcp_pair_transition_backward(n_pairs: int, c_z: int, hidden: int, act_dtype: int, ln_eps: float, w1: Ptr, w2: Ptr,
+                                 w3: Ptr, ln_gamma: Ptr, ln_beta: Ptr, z: Ptr, z_exponents: Ptr, dz_out: Ptr,
+                                 grads: DcpTransitionGradients, workspace: Ptr, workspace_bytes: int,
+                                 stream=None) -> None:
+    _check(lib().dcp_pair_transition_backward(n_pairs, c_z, hidden, act_dtype, ln_eps, _ptr(w1), _ptr(w2), _ptr(w3),
+                                              _ptr(ln_gamma), _ptr(ln_beta), _ptr(z), _ptr(z_exponents), _ptr(dz_out),
+                                              ctypes.byref(grads), _ptr(workspace), workspace_bytes, _stream(stream)))
+
+
+def dcp_checkpoint_pack(n_rows: int, c: int, dtype: int, x: Ptr, codes: Ptr, exponents: Ptr, stream=None) -> None:
+    _check(lib().dcp_checkpoint_pack(n_rows, c, dtype, _ptr(x), _ptr(codes), _ptr(exponents), _stream(stream)))
+
+
+def dcp_checkpoint_unpack(n_rows: int, c: int, dtype: int, codes: Ptr, exponents: Ptr, x: Ptr, stream=None) -> None:
+    _check(lib().dcp_checkpoint_unpack(n_rows, c, dtype, _ptr(codes), _ptr(exponents), _ptr(x), _stream(stream)))
+
+
+def make_relative_fields(fields) -> ctypes.Array:
+    """(position, group or None, radius) of each field, in the table's order."""
+    return (DcpRelativeField * len(fields))(*[DcpRelativeField(_ptr(p), _ptr(g), r) for p, g, r in fields])
+
+
+def dcp_relative_position(n_tokens: int, row0: int, n_rows: int, c: int, dtype: int, fields: ctypes.Array, table: Ptr,
+                          z_in: Ptr, z_out: Ptr, stream=None) -> None:
+    _check(lib().dcp_relative_position(n_tokens, row0, n_rows, c, dtype, len(fields), fields, _ptr(table), _ptr(z_in),
+                                       _ptr(z_out), _stream(stream)))
+
+
+def dcp_relative_position_backward_workspace_size(n_tokens: int, n_rows: int, c: int, fields: ctypes.Array) -> int:
+    out = ctypes.c_size_t()
+    _check(lib().dcp_relative_position_backward_workspace_size(n_tokens, n_rows, c, len(fields), fields,
+                                                               ctypes.byref(out)))
+    return out.value
+
+
+def dcp_relative_position_backward(n_tokens: int, row0: int, n_rows: int, c: int, dtype: int, fields: ctypes.Array,
+                                   dz_rows: Ptr, dtable: Ptr, workspace: Ptr, workspace_bytes: int,
+                                   stream=None) -> None:
+    _check(lib().dcp_relative_position_backward(n_tokens, row0, n_rows, c, dtype, len(fields), fields, _ptr(dz_rows),
+                                                _ptr(dtable), _ptr(workspace), workspace_bytes, _stream(stream)))
 
 
 def dcp_set_timing_events(start_event: Optional[int], stop_event: Optional[int]) -> None:

@@ -10,6 +10,7 @@
 
 #include <mutex>
 
+#include "checkpoint.h"
 #include "dcp.h"
 #include "dcp_internal.h"
 
@@ -1598,6 +1599,311 @@ int dcp_pair_bias_attention_backward(const dcp_shape* shape, const dcp_weights* 
   fa.t = sa.t;
   if ((e = dcp::launch_back_finish(fa, st)) != hipSuccess)
     return fail(DCP_ERR_HIP, "gradient output launch failed: %s", hipGetErrorString(e));
+  return ok();
+}
+
+}  // extern "C"
+
+// ----------------------------------------------------------------------------- transition backward
+namespace {
+
+struct TransBackLayout {
+  int splits;
+  size_t off_prep, off_parts, off_affine, total;
+};
+void trans_back_layout(int64_t n_pairs, int32_t c, int32_t hidden, TransBackLayout* L) {
+  const size_t cp = round_up(c, 16), hp = round_up(hidden, 16);
+  L->splits = n_pairs > 0 ? dcp::trans_back_gen_splits(n_pairs, c, hidden) : 0;
+  size_t o = 0;
+  auto take = [&](size_t floats) {
+    const size_t at = o;
+    o += round_up(floats * sizeof(float), 256);
+    return at;
+  };
+  L->off_prep = take(5 * cp * hp + 2 * cp);
+  L->off_parts = take((size_t)L->splits * (3 * cp * hp + 2 * hp));
+  L->off_affine = take((size_t)(hidden + 1) / 2 * 2 * c);
+  L->total = o;
+}
+
+int check_transition_back(int64_t n_pairs, int32_t c_z, int32_t hidden, int32_t act_dtype) {
+  bool fast;
+  const int rc = check_transition(c_z, hidden, act_dtype, &fast);
+  if (rc) return rc;
+  if (n_pairs < 0) return fail(DCP_ERR_INVALID_ARGUMENT, "n_pairs must be >= 0");
+  if (n_pairs > (int64_t)1 << 34) return fail(DCP_ERR_INVALID_ARGUMENT, "n_pairs too large");
+  return DCP_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+int dcp_pair_transition_backward_workspace_size(int64_t n_pairs, int32_t c_z, int32_t hidden, int32_t act_dtype,
+                                                size_t* bytes) {
+  if (!bytes) return fail(DCP_ERR_INVALID_ARGUMENT, "bytes is NULL");
+  if (const int rc = check_transition_back(n_pairs, c_z, hidden, act_dtype)) return rc;
+  TransBackLayout L;
+  trans_back_layout(n_pairs, c_z, hidden, &L);
+  *bytes = L.total;
+  return ok();
+}
+
+int dcp_pair_transition_backward(int64_t n_pairs, int32_t c_z, int32_t hidden, int32_t act_dtype, float ln_eps,
+                                 const float* w1, const float* w2, const float* w3, const float* ln_gamma,
+                                 const float* ln_beta, const void* z, const uint8_t* z_exponents, const void* dz_out,
+                                 const dcp_transition_gradients* grads, void* workspace, size_t workspace_bytes,
+                                 void* stream) {
+  if (const int rc = check_transition_back(n_pairs, c_z, hidden, act_dtype)) return rc;
+  if (!(ln_eps >= 0.0f) || !isfinite(ln_eps)) return fail(DCP_ERR_INVALID_ARGUMENT, "ln_eps must be finite and >= 0");
+  if (!grads) return fail(DCP_ERR_INVALID_ARGUMENT, "grads is NULL");
+  if (grads->dtype != DCP_F32 && grads->dtype != DCP_BF16)
+    return fail(DCP_ERR_INVALID_ARGUMENT, "the gradients' dtype must be DCP_F32 or DCP_BF16");
+  const bool sums = grads->dw1 || grads->dw2 || grads->dw3 || grads->dln_gamma || grads->dln_beta;
+  if (!sums && !grads->dz) return fail(DCP_ERR_INVALID_ARGUMENT, "at least one gradient is required");
+  if (!w1 || !w2 || !w3) return fail(DCP_ERR_INVALID_ARGUMENT, "w1, w2 and w3 are required");
+  if (n_pairs > 0 && (!z || !dz_out)) return fail(DCP_ERR_INVALID_ARGUMENT, "z and dz_out are required");
+  const bool bf16 = act_dtype == DCP_BF16;
+  const size_t act_align = bf16 ? 16 : 4, ge = elem(grads->dtype);
+  if (!aligned(z, z_exponents && !bf16 ? 1 : act_align) || !aligned(dz_out, act_align) || !aligned(grads->dz, act_align) ||
+      (bf16 && !aligned(z_exponents, 4)))
+    return fail(DCP_ERR_INVALID_ARGUMENT, "z, z_exponents, dz_out and dz must be aligned (16, 4, 16 and 16 bytes in bf16)");
+  if (!aligned(w1, 4) || !aligned(w2, 4) || !aligned(w3, 4) || !aligned(ln_gamma, 4) || !aligned(ln_beta, 4) ||
+      !aligned(grads->dw1, ge) || !aligned(grads->dw2, ge) || !aligned(grads->dw3, ge) || !aligned(grads->dln_gamma, ge) ||
+      !aligned(grads->dln_beta, ge))
+    return fail(DCP_ERR_INVALID_ARGUMENT, "weights and their gradients must be aligned to their element size");
+  if (n_pairs == 0 && !sums) return ok();
+  TransBackLayout L;
+  trans_back_layout(n_pairs, c_z, hidden, &L);
+  if (!workspace || !aligned(workspace, 256))
+    return fail(DCP_ERR_WORKSPACE, "workspace must be a 256-byte aligned device pointer");
+  if (workspace_bytes < L.total)
+    return fail(DCP_ERR_WORKSPACE, "workspace too small: %zu bytes given, %zu needed", workspace_bytes, L.total);
+  const size_t rows = (size_t)n_pairs * c_z, wb = (size_t)c_z * hidden, cb = c_z;
+  const Extent all[] = {{"dz", grads->dz, rows * elem(act_dtype)},
+                        {"dw1", grads->dw1, wb * ge},
+                        {"dw2", grads->dw2, wb * ge},
+                        {"dw3", grads->dw3, wb * ge},
+                        {"dln_gamma", grads->dln_gamma, cb * ge},
+                        {"dln_beta", grads->dln_beta, cb * ge},
+                        {"workspace", workspace, L.total},
+                        {"z", z, rows * (z_exponents ? 1 : elem(act_dtype))},
+                        {"z_exponents", z_exponents, (size_t)n_pairs * dcp::checkpoint_blocks(c_z)},
+                        {"w1", w1, wb * 4},
+                        {"w2", w2, wb * 4},
+                        {"w3", w3, wb * 4},
+                        {"ln_gamma", ln_gamma, cb * 4},
+                        {"ln_beta", ln_beta, cb * 4},
+                        {"dz_out", dz_out, rows * elem(act_dtype)}};
+  int overlaps = check_apart(all + 1, 14, 6);  // what is written but dz, against all behind it
+  if (!overlaps) overlaps = check_apart(all, grads->dz == dz_out ? 14 : 15, 1);
+  if (overlaps) return overlaps;
+  dcp::TransBackArgs a{};
+  a.n_pairs = n_pairs;
+  a.c = c_z;
+  a.hidden = hidden;
+  a.eps = ln_eps;
+  a.w1 = w1;
+  a.w2 = w2;
+  a.w3 = w3;
+  a.gamma = ln_gamma;
+  a.beta = ln_beta;
+  a.z = z;
+  a.dout = dz_out;
+  a.exponents = z_exponents;
+  a.dz = grads->dz;
+  a.dw1 = grads->dw1;
+  a.dw2 = grads->dw2;
+  a.dw3 = grads->dw3;
+  a.dgamma = grads->dln_gamma;
+  a.dbeta = grads->dln_beta;
+  a.bf16 = bf16;
+  a.grads_bf16 = grads->dtype == DCP_BF16;
+  a.z_vec = c_z % 4 == 0 && aligned(z, z_exponents ? 4 : 16);
+  a.d_vec = c_z % 4 == 0 && aligned(dz_out, 16) && aligned(grads->dz, 16);
+  a.splits = L.splits;
+  char* ws = static_cast<char*>(workspace);
+  a.prep = reinterpret_cast<float*>(ws + L.off_prep);
+  a.parts = reinterpret_cast<float*>(ws + L.off_parts);
+  a.affine_parts = reinterpret_cast<float*>(ws + L.off_affine);
+  hipStream_t st = static_cast<hipStream_t>(stream);
+  hipError_t e;
+  if (n_pairs > 0 && (e = dcp::launch_trans_back_gen(a, st)) != hipSuccess)
+    return fail(DCP_ERR_HIP, "transition backward launch failed: %s", hipGetErrorString(e));
+  if (sums && (e = dcp::launch_trans_back_finish(a, st)) != hipSuccess)
+    return fail(DCP_ERR_HIP, "transition gradient launch failed: %s", hipGetErrorString(e));
+  return ok();
+}
+
+}  // extern "C"
+
+// ----------------------------------------------------------------------------- checkpoints in 8 bits
+namespace {
+
+int checkpoint(bool pack, int64_t n_rows, int32_t c, int32_t dtype, const void* x, void* y, const void* codes,
+               const void* exponents, void* stream) {
+  if (n_rows < 0) return fail(DCP_ERR_INVALID_ARGUMENT, "n_rows must be >= 0 (got %lld)", (long long)n_rows);
+  if (c < 1) return fail(DCP_ERR_INVALID_ARGUMENT, "c must be >= 1");
+  if (dtype != DCP_F32 && dtype != DCP_BF16) return fail(DCP_ERR_INVALID_ARGUMENT, "dtype must be DCP_F32 or DCP_BF16");
+  if (c > 65536) return fail(DCP_ERR_UNSUPPORTED, "c must be <= 65536 (got %d)", c);
+  if (n_rows > ((int64_t)1 << 38) / dcp::checkpoint_blocks(c)) return fail(DCP_ERR_INVALID_ARGUMENT, "n_rows too large");
+  if (n_rows == 0) return ok();
+  const void* rows = pack ? x : y;
+  if (!rows || !codes || !exponents) return fail(DCP_ERR_INVALID_ARGUMENT, "x, codes and exponents are required");
+  if (!aligned(rows, elem(dtype))) return fail(DCP_ERR_INVALID_ARGUMENT, "x must be aligned to its element size");
+  const Extent xe = {"x", rows, (size_t)n_rows * c * elem(dtype)}, ce = {"codes", codes, (size_t)n_rows * c},
+               ee = {"exponents", exponents, (size_t)n_rows * dcp::checkpoint_blocks(c)};
+  const Extent packing[] = {ce, ee, xe}, reading[] = {xe, ce, ee};
+  if (const int overlaps = pack ? check_apart(packing, 3, 2) : check_apart(reading, 3, 1)) return overlaps;
+  dcp::CheckpointArgs a{};
+  a.n_rows = n_rows;
+  a.c = c;
+  a.x = x;
+  a.y = y;
+  a.codes = const_cast<int8_t*>(static_cast<const int8_t*>(codes));
+  a.exponents = const_cast<uint8_t*>(static_cast<const uint8_t*>(exponents));
+  const bool bf16 = dtype == DCP_BF16;
+  hipStream_t st = static_cast<hipStream_t>(stream);
+  const hipError_t e = pack ? dcp::launch_checkpoint_pack(a, bf16, st) : dcp::launch_checkpoint_unpack(a, bf16, st);
+  if (e != hipSuccess) return fail(DCP_ERR_HIP, "checkpoint launch failed: %s", hipGetErrorString(e));
+  return ok();
+}
+
+}  // namespace
+
+extern "C" {
+
+int dcp_checkpoint_pack(int64_t n_rows, int32_t c, int32_t dtype, const void* x, int8_t* codes, uint8_t* exponents,
+                        void* stream) {
+  return checkpoint(true, n_rows, c, dtype, x, nullptr, codes, exponents, stream);
+}
+
+int dcp_checkpoint_unpack(int64_t n_rows, int32_t c, int32_t dtype, const int8_t* codes, const uint8_t* exponents,
+                          void* x, void* stream) {
+  return checkpoint(false, n_rows, c, dtype, nullptr, x, codes, exponents, stream);
+}
+
+}  // extern "C"
+
+// ----------------------------------------------------------------------------- relative positions
+namespace {
+
+int check_relative(int64_t n_tokens, int64_t row0, int64_t n_rows, int32_t c, int32_t n_fields,
+                   const dcp_relative_field* fields, dcp::RelativeArgs* a) {
+  if (n_tokens < 1 || n_tokens > INT32_MAX) return fail(DCP_ERR_INVALID_ARGUMENT, "n_tokens must be in [1, 2^31)");
+  if (n_rows < 0 || row0 < 0 || row0 > n_tokens || n_rows > n_tokens - row0)
+    return fail(DCP_ERR_INVALID_ARGUMENT, "rows must lie in [0, n_tokens)");
+  if (n_rows * n_tokens > (int64_t)1 << 38) return fail(DCP_ERR_INVALID_ARGUMENT, "too many pairs");
+  if (c < 1) return fail(DCP_ERR_INVALID_ARGUMENT, "c must be >= 1");
+  if (c > dcp::kRelativeMaxC) return fail(DCP_ERR_UNSUPPORTED, "c must be <= %d (got %d)", dcp::kRelativeMaxC, c);
+  if (n_fields < 1) return fail(DCP_ERR_INVALID_ARGUMENT, "n_fields must be >= 1");
+  if (n_fields > dcp::kRelativeFields)
+    return fail(DCP_ERR_UNSUPPORTED, "n_fields must be <= %d (got %d)", dcp::kRelativeFields, n_fields);
+  if (!fields) return fail(DCP_ERR_INVALID_ARGUMENT, "fields is NULL");
+  *a = dcp::RelativeArgs{};
+  a->n_tok = n_tokens;
+  a->row0 = row0;
+  a->n_rows = n_rows;
+  a->c = c;
+  a->n_fields = n_fields;
+  for (int f = 0; f < n_fields; ++f) {
+    if (fields[f].radius < 0) return fail(DCP_ERR_INVALID_ARGUMENT, "radius must be >= 0 (field %d)", f);
+    if (fields[f].radius > dcp::kRelativeMaxRadius)
+      return fail(DCP_ERR_UNSUPPORTED, "radius must be <= %d (field %d: %d)", dcp::kRelativeMaxRadius, f, fields[f].radius);
+    a->position[f] = fields[f].position;
+    a->group[f] = fields[f].group;
+    a->radius[f] = fields[f].radius;
+    a->first[f] = a->n_buckets;
+    a->n_buckets += 2 * fields[f].radius + 2;
+  }
+  return DCP_OK;
+}
+
+int check_relative_call(const dcp::RelativeArgs& a, int32_t dtype) {
+  if (dtype != DCP_F32 && dtype != DCP_BF16) return fail(DCP_ERR_INVALID_ARGUMENT, "dtype must be DCP_F32 or DCP_BF16");
+  if (a.n_rows > 0)
+    for (int f = 0; f < a.n_fields; ++f) {
+      if (!a.position[f]) return fail(DCP_ERR_INVALID_ARGUMENT, "position of field %d is NULL", f);
+      if (!aligned(a.position[f], 4) || !aligned(a.group[f], 4))
+        return fail(DCP_ERR_INVALID_ARGUMENT, "positions and groups must be 4-byte aligned (field %d)", f);
+    }
+  return DCP_OK;
+}
+
+// What a call writes, `out` and a workspace, against what it reads
+int check_relative_apart(const dcp::RelativeArgs& a, const Extent& out, const Extent& ws, const Extent& in) {
+  Extent all[3 + 2 * dcp::kRelativeFields] = {out, ws, in};
+  int n = 3;
+  for (int f = 0; f < a.n_fields; ++f) {
+    all[n++] = {"a field's position", a.position[f], (size_t)a.n_tok * 4};
+    all[n++] = {"a field's group", a.group[f], (size_t)a.n_tok * 4};
+  }
+  return check_apart(all, n, 2);
+}
+
+}  // namespace
+
+extern "C" {
+
+int dcp_relative_position(int64_t n_tokens, int64_t row0, int64_t n_rows, int32_t c, int32_t dtype, int32_t n_fields,
+                          const dcp_relative_field* fields, const float* table, const void* z_in, void* z_out,
+                          void* stream) {
+  dcp::RelativeArgs a;
+  int rc = check_relative(n_tokens, row0, n_rows, c, n_fields, fields, &a);
+  if (!rc) rc = check_relative_call(a, dtype);
+  if (rc) return rc;
+  if (n_rows == 0) return ok();
+  if (!table || !z_out) return fail(DCP_ERR_INVALID_ARGUMENT, "table and z_out are required");
+  if (!aligned(table, 4) || !aligned(z_in, elem(dtype)) || !aligned(z_out, elem(dtype)))
+    return fail(DCP_ERR_INVALID_ARGUMENT, "table, z_in and z_out must be aligned to their element size");
+  const size_t zb = (size_t)n_rows * n_tokens * c * elem(dtype);
+  const Extent out = {"z_out", z_out, zb}, in = {"z_in", z_in == z_out ? nullptr : z_in, zb};
+  if ((rc = check_relative_apart(a, out, {"table", nullptr, 0}, in))) return rc;
+  const Extent two[] = {out, {"table", table, (size_t)a.n_buckets * c * 4}};
+  if ((rc = check_apart(two, 2, 1))) return rc;
+  a.table = table;
+  a.z_in = z_in;
+  a.z_out = z_out;
+  const hipError_t e = dcp::launch_relative(a, dtype == DCP_BF16, static_cast<hipStream_t>(stream));
+  if (e != hipSuccess) return fail(DCP_ERR_HIP, "relative position launch failed: %s", hipGetErrorString(e));
+  return ok();
+}
+
+int dcp_relative_position_backward_workspace_size(int64_t n_tokens, int64_t n_rows, int32_t c, int32_t n_fields,
+                                                  const dcp_relative_field* fields, size_t* bytes) {
+  if (!bytes) return fail(DCP_ERR_INVALID_ARGUMENT, "bytes is NULL");
+  dcp::RelativeArgs a;
+  if (const int rc = check_relative(n_tokens, 0, n_rows, c, n_fields, fields, &a)) return rc;
+  *bytes = round_up((size_t)dcp::relative_back_parts(n_tokens, n_rows, c, a.n_buckets) * a.n_buckets * c * sizeof(float), 256);
+  return ok();
+}
+
+int dcp_relative_position_backward(int64_t n_tokens, int64_t row0, int64_t n_rows, int32_t c, int32_t dtype,
+                                   int32_t n_fields, const dcp_relative_field* fields, const void* dz_rows,
+                                   float* dtable, void* workspace, size_t workspace_bytes, void* stream) {
+  dcp::RelativeArgs a;
+  int rc = check_relative(n_tokens, row0, n_rows, c, n_fields, fields, &a);
+  if (!rc) rc = check_relative_call(a, dtype);
+  if (rc) return rc;
+  if (!dtable || (n_rows > 0 && !dz_rows)) return fail(DCP_ERR_INVALID_ARGUMENT, "dz_rows and dtable are required");
+  if (!aligned(dtable, 4) || !aligned(dz_rows, elem(dtype)))
+    return fail(DCP_ERR_INVALID_ARGUMENT, "dz_rows and dtable must be aligned to their element size");
+  a.n_parts = dcp::relative_back_parts(n_tokens, n_rows, c, a.n_buckets);
+  const size_t need = (size_t)a.n_parts * a.n_buckets * c * sizeof(float);
+  if (n_rows > 0) {
+    if (!workspace || !aligned(workspace, 256))
+      return fail(DCP_ERR_WORKSPACE, "workspace must be a 256-byte aligned device pointer");
+    if (workspace_bytes < round_up(need, 256))
+      return fail(DCP_ERR_WORKSPACE, "workspace too small: %zu bytes given, %zu needed", workspace_bytes, round_up(need, 256));
+  }
+  rc = check_relative_apart(a, {"dtable", dtable, (size_t)a.n_buckets * c * 4}, {"workspace", workspace, need},
+                            {"dz_rows", dz_rows, (size_t)n_rows * n_tokens * c * elem(dtype)});
+  if (rc) return rc;
+  a.dz = dz_rows;
+  a.dtable = dtable;
+  a.parts = static_cast<float*>(workspace);
+  const hipError_t e = dcp::launch_relative_back(a, dtype == DCP_BF16, static_cast<hipStream_t>(stream));
+  if (e != hipSuccess) return fail(DCP_ERR_HIP, "relative position gradient launch failed: %s", hipGetErrorString(e));
   return ok();
 }
 

@@ -390,6 +390,51 @@ struct BackFinishArgs {
   uint32_t sum_blocks;               // set by the launcher
 };
 
+// Backward pass of the pair transition
+struct TransBackArgs {
+  int64_t n_pairs;
+  int32_t c, hidden;
+  float eps;
+  const float *w1, *w2, *w3, *gamma, *beta;  // gamma, beta or null
+  const void *z, *dout;      // [n_pairs][c]; z as codes where exponents is not null
+  const uint8_t* exponents;  // [n_pairs][checkpoint_blocks(c)] or null
+  void* dz;                  // or null, as all gradients
+  void *dw1, *dw2, *dw3, *dgamma, *dbeta;
+  int32_t bf16, grads_bf16;
+  int32_t z_vec, d_vec;      // rows of z, of dout and dz in whole aligned groups of four channels
+  int32_t splits;            // shares of the pairs that are summed on their own
+  float* prep;               // weights as operands
+  float* parts;              // [splits]: T1, T2, T3 [hp][cp], S1, S2 [hp] (hidden and c filled up to 16)
+  float* affine_parts;       // [(hidden + 1) / 2][2][c]
+};
+
+struct CheckpointArgs {
+  int64_t n_rows;
+  int32_t c;
+  const void* x;  // pack
+  void* y;        // unpack
+  int8_t* codes;  // [n_rows][c]
+  uint8_t* exponents;
+};
+
+constexpr int kRelativeFields = 4;
+constexpr int kRelativeMaxRadius = 127;  // a bucket fits a byte
+constexpr int kRelativeMaxC = 1024;
+struct RelativeArgs {
+  int64_t n_tok, row0, n_rows;
+  int32_t c, n_fields, n_buckets;
+  const int32_t* position[kRelativeFields];  // [n_tok]
+  const int32_t* group[kRelativeFields];     // [n_tok] or null
+  int32_t radius[kRelativeFields], first[kRelativeFields];
+  const float* table;  // [n_buckets][c]
+  const void* z_in;    // or null
+  void* z_out;
+  const void* dz;
+  float* dtable;
+  float* parts;  // [n_parts][n_buckets][c]
+  int32_t n_parts;
+};
+
 size_t fast_proj_split_bytes(int32_t c_s);
 bool fast_proj_small(int64_t key_tiles, int64_t query_tiles);  // one kernel, w_split unused
 hipError_t launch_fast_proj(const FastProjArgs& a, hipStream_t st);
@@ -426,6 +471,14 @@ hipError_t launch_back_gemm(const BackGemmArgs& a, hipStream_t st);
 hipError_t launch_token_proj(const TokenArgs& a, hipStream_t st);
 hipError_t launch_token_grad(const TokenArgs& a, hipStream_t st);
 hipError_t launch_back_finish(const BackFinishArgs& a, hipStream_t st);
+int trans_back_gen_splits(int64_t n_pairs, int32_t c, int32_t hidden);
+hipError_t launch_trans_back_gen(const TransBackArgs& a, hipStream_t st);
+hipError_t launch_trans_back_finish(const TransBackArgs& a, hipStream_t st);
+hipError_t launch_checkpoint_pack(const CheckpointArgs& a, bool bf16, hipStream_t st);
+hipError_t launch_checkpoint_unpack(const CheckpointArgs& a, bool bf16, hipStream_t st);
+hipError_t launch_relative(const RelativeArgs& a, bool bf16, hipStream_t st);
+int relative_back_parts(int64_t n_tok, int64_t n_rows, int32_t c, int32_t n_buckets);
+hipError_t launch_relative_back(const RelativeArgs& a, bool bf16, hipStream_t st);
 int scatter_order_flags(int64_t n_atoms);  // plan workgroups (one flag each) for n_atoms (<= kScatterFlags)
 
 }  // namespace dcp
