@@ -1611,24 +1611,23 @@ struct TransBackLayout {
   int splits;
   size_t off_prep, off_parts, off_affine, total;
 };
-void trans_back_layout(int64_t n_pairs, int32_t c, int32_t hidden, TransBackLayout* L) {
+void trans_back_layout(int64_t n_pairs, int32_t c, int32_t hidden, bool fast, TransBackLayout* L) {
   const size_t cp = round_up(c, 16), hp = round_up(hidden, 16);
-  L->splits = n_pairs > 0 ? dcp::trans_back_gen_splits(n_pairs, c, hidden) : 0;
+  L->splits = n_pairs == 0 ? 0 : fast ? dcp::trans_back_fast_splits(n_pairs) : dcp::trans_back_gen_splits(n_pairs, c, hidden);
   size_t o = 0;
   auto take = [&](size_t floats) {
     const size_t at = o;
     o += round_up(floats * sizeof(float), 256);
     return at;
   };
-  L->off_prep = take(5 * cp * hp + 2 * cp);
+  L->off_prep = take(fast ? dcp::trans_back_fast_prep_bytes() / sizeof(float) : 5 * cp * hp + 2 * cp);
   L->off_parts = take((size_t)L->splits * (3 * cp * hp + 2 * hp));
   L->off_affine = take((size_t)(hidden + 1) / 2 * 2 * c);
   L->total = o;
 }
 
-int check_transition_back(int64_t n_pairs, int32_t c_z, int32_t hidden, int32_t act_dtype) {
-  bool fast;
-  const int rc = check_transition(c_z, hidden, act_dtype, &fast);
+int check_transition_back(int64_t n_pairs, int32_t c_z, int32_t hidden, int32_t act_dtype, bool* fast) {
+  const int rc = check_transition(c_z, hidden, act_dtype, fast);
   if (rc) return rc;
   if (n_pairs < 0) return fail(DCP_ERR_INVALID_ARGUMENT, "n_pairs must be >= 0");
   if (n_pairs > (int64_t)1 << 34) return fail(DCP_ERR_INVALID_ARGUMENT, "n_pairs too large");
@@ -1642,9 +1641,10 @@ extern "C" {
 int dcp_pair_transition_backward_workspace_size(int64_t n_pairs, int32_t c_z, int32_t hidden, int32_t act_dtype,
                                                 size_t* bytes) {
   if (!bytes) return fail(DCP_ERR_INVALID_ARGUMENT, "bytes is NULL");
-  if (const int rc = check_transition_back(n_pairs, c_z, hidden, act_dtype)) return rc;
+  bool fast;
+  if (const int rc = check_transition_back(n_pairs, c_z, hidden, act_dtype, &fast)) return rc;
   TransBackLayout L;
-  trans_back_layout(n_pairs, c_z, hidden, &L);
+  trans_back_layout(n_pairs, c_z, hidden, fast, &L);
   *bytes = L.total;
   return ok();
 }
@@ -1654,7 +1654,8 @@ int dcp_pair_transition_backward(int64_t n_pairs, int32_t c_z, int32_t hidden, i
                                  const float* ln_beta, const void* z, const uint8_t* z_exponents, const void* dz_out,
                                  const dcp_transition_gradients* grads, void* workspace, size_t workspace_bytes,
                                  void* stream) {
-  if (const int rc = check_transition_back(n_pairs, c_z, hidden, act_dtype)) return rc;
+  bool fast;
+  if (const int rc = check_transition_back(n_pairs, c_z, hidden, act_dtype, &fast)) return rc;
   if (!(ln_eps >= 0.0f) || !isfinite(ln_eps)) return fail(DCP_ERR_INVALID_ARGUMENT, "ln_eps must be finite and >= 0");
   if (!grads) return fail(DCP_ERR_INVALID_ARGUMENT, "grads is NULL");
   if (grads->dtype != DCP_F32 && grads->dtype != DCP_BF16)
@@ -1674,7 +1675,7 @@ int dcp_pair_transition_backward(int64_t n_pairs, int32_t c_z, int32_t hidden, i
     return fail(DCP_ERR_INVALID_ARGUMENT, "weights and their gradients must be aligned to their element size");
   if (n_pairs == 0 && !sums) return ok();
   TransBackLayout L;
-  trans_back_layout(n_pairs, c_z, hidden, &L);
+  trans_back_layout(n_pairs, c_z, hidden, fast, &L);
   if (!workspace || !aligned(workspace, 256))
     return fail(DCP_ERR_WORKSPACE, "workspace must be a 256-byte aligned device pointer");
   if (workspace_bytes < L.total)
@@ -1717,7 +1718,6 @@ int dcp_pair_transition_backward(int64_t n_pairs, int32_t c_z, int32_t hidden, i
   a.dw3 = grads->dw3;
   a.dgamma = grads->dln_gamma;
   a.dbeta = grads->dln_beta;
-  a.bf16 = bf16;
   a.grads_bf16 = grads->dtype == DCP_BF16;
   a.z_vec = c_z % 4 == 0 && aligned(z, z_exponents ? 4 : 16);
   a.d_vec = c_z % 4 == 0 && aligned(dz_out, 16) && aligned(grads->dz, 16);
@@ -1728,7 +1728,8 @@ int dcp_pair_transition_backward(int64_t n_pairs, int32_t c_z, int32_t hidden, i
   a.affine_parts = reinterpret_cast<float*>(ws + L.off_affine);
   hipStream_t st = static_cast<hipStream_t>(stream);
   hipError_t e;
-  if (n_pairs > 0 && (e = dcp::launch_trans_back_gen(a, st)) != hipSuccess)
+  if (fast && n_pairs > 0) dcp::trans_back_fast_units(a.prep, &a.unit_a, &a.unit_b);
+  if (n_pairs > 0 && (e = fast ? dcp::launch_trans_back_fast(a, st) : dcp::launch_trans_back_gen(a, st)) != hipSuccess)
     return fail(DCP_ERR_HIP, "transition backward launch failed: %s", hipGetErrorString(e));
   if (sums && (e = dcp::launch_trans_back_finish(a, st)) != hipSuccess)
     return fail(DCP_ERR_HIP, "transition gradient launch failed: %s", hipGetErrorString(e));

@@ -400,11 +400,12 @@ struct TransBackArgs {
   const uint8_t* exponents;  // [n_pairs][checkpoint_blocks(c)] or null
   void* dz;                  // or null, as all gradients
   void *dw1, *dw2, *dw3, *dgamma, *dbeta;
-  int32_t bf16, grads_bf16;
-  int32_t z_vec, d_vec;      // rows of z, of dout and dz in whole aligned groups of four channels
+  int32_t grads_bf16;
+  int32_t z_vec, d_vec;      // fp32: rows of z, of dout and dz in whole aligned groups of four channels
   int32_t splits;            // shares of the pairs that are summed on their own
   float* prep;               // weights as operands
   float* parts;              // [splits]: T1, T2, T3 [hp][cp], S1, S2 [hp] (hidden and c filled up to 16)
+  const float *unit_a, *unit_b;  // [hidden]: T2 and S2 times unit_a, T1 and S1 times unit_b, T3 times both; null: 1
   float* affine_parts;       // [(hidden + 1) / 2][2][c]
 };
 
@@ -473,6 +474,10 @@ hipError_t launch_token_grad(const TokenArgs& a, hipStream_t st);
 hipError_t launch_back_finish(const BackFinishArgs& a, hipStream_t st);
 int trans_back_gen_splits(int64_t n_pairs, int32_t c, int32_t hidden);
 hipError_t launch_trans_back_gen(const TransBackArgs& a, hipStream_t st);
+size_t trans_back_fast_prep_bytes();
+void trans_back_fast_units(const float* prep, const float** unit_a, const float** unit_b);
+int trans_back_fast_splits(int64_t n_pairs);
+hipError_t launch_trans_back_fast(const TransBackArgs& a, hipStream_t st);
 hipError_t launch_trans_back_finish(const TransBackArgs& a, hipStream_t st);
 hipError_t launch_checkpoint_pack(const CheckpointArgs& a, bool bf16, hipStream_t st);
 hipError_t launch_checkpoint_unpack(const CheckpointArgs& a, bool bf16, hipStream_t st);

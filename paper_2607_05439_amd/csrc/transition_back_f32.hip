@@ -74,9 +74,6 @@ __device__ __forceinline__ f32x4 load4(const TransBackArgs& a, const void* x, bo
     } else {
       for (int i = 0; i < n; ++i) v[i] = (float)q[i] * scale;
     }
-  } else if (a.bf16) {
-    const uint16_t* q = static_cast<const uint16_t*>(x) + at;
-    for (int i = 0; i < n; ++i) v[i] = __uint_as_float((uint32_t)q[i] << 16);
   } else if (vec) {
     v = *reinterpret_cast<const f32x4*>(static_cast<const float*>(x) + at);
   } else {
@@ -358,9 +355,7 @@ __global__ void __launch_bounds__(256, CT > 8 ? 1 : 2) trans_back_pairs_kernel(T
     f32x4 o;
 #pragma unroll
     for (int i = 0; i < 4; ++i) o[i] = dv[i] + rstd * (gr[j][i] - m0 - zh[j][i] * m1);
-    if (a.bf16) {
-      for (int i = 0; i < min(4, a.c - c0); ++i) static_cast<uint16_t*>(a.dz)[at + i] = __builtin_bit_cast(uint16_t, (__bf16)o[i]);
-    } else if (a.d_vec) {
+    if (a.d_vec) {
       *reinterpret_cast<f32x4*>(static_cast<float*>(a.dz) + at) = o;
     } else {
       for (int i = 0; i < min(4, a.c - c0); ++i) static_cast<float*>(a.dz)[at + i] = o[i];
@@ -395,6 +390,13 @@ __global__ void __launch_bounds__(256) trans_back_finish_kernel(TransBackArgs a)
       t[2] += p[2 * size];
       s1 += ps[0];
       s2 += ps[hp];
+    }
+    if (a.unit_a) {
+      t[0] *= a.unit_b[u];
+      t[1] *= a.unit_a[u];
+      t[2] *= a.unit_a[u] * a.unit_b[u];
+      s1 *= a.unit_b[u];
+      s2 *= a.unit_a[u];
     }
     const float ga = a.gamma ? a.gamma[c] : 1.0f, be = a.beta ? a.beta[c] : 0.0f;
     const int64_t at = (int64_t)u * a.c + c;
