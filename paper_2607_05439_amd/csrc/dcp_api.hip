@@ -1609,7 +1609,7 @@ namespace {
 
 struct TransBackLayout {
   int splits;
-  size_t off_prep, off_parts, off_affine, total;
+  size_t off_prep, off_parts, off_affine, off_zh, total;
 };
 void trans_back_layout(int64_t n_pairs, int32_t c, int32_t hidden, bool fast, TransBackLayout* L) {
   const size_t cp = round_up(c, 16), hp = round_up(hidden, 16);
@@ -1623,6 +1623,7 @@ void trans_back_layout(int64_t n_pairs, int32_t c, int32_t hidden, bool fast, Tr
   L->off_prep = take(fast ? dcp::trans_back_fast_prep_bytes() / sizeof(float) : 5 * cp * hp + 2 * cp);
   L->off_parts = take((size_t)L->splits * (3 * cp * hp + 2 * hp));
   L->off_affine = take((size_t)(hidden + 1) / 2 * 2 * c);
+  L->off_zh = take(fast ? dcp::trans_back_fast_zh_bytes(n_pairs) / sizeof(float) : 0);
   L->total = o;
 }
 
@@ -1726,6 +1727,7 @@ int dcp_pair_transition_backward(int64_t n_pairs, int32_t c_z, int32_t hidden, i
   a.prep = reinterpret_cast<float*>(ws + L.off_prep);
   a.parts = reinterpret_cast<float*>(ws + L.off_parts);
   a.affine_parts = reinterpret_cast<float*>(ws + L.off_affine);
+  a.zh = ws + L.off_zh;
   hipStream_t st = static_cast<hipStream_t>(stream);
   hipError_t e;
   if (fast && n_pairs > 0) dcp::trans_back_fast_units(a.prep, &a.unit_a, &a.unit_b);

@@ -407,6 +407,8 @@ struct TransBackArgs {
   float* parts;              // [splits]: T1, T2, T3 [hp][cp], S1, S2 [hp] (hidden and c filled up to 16)
   const float *unit_a, *unit_b;  // [hidden]: T2 and S2 times unit_a, T1 and S1 times unit_b, T3 times both; null: 1
   float* affine_parts;       // [(hidden + 1) / 2][2][c]
+  char* zh;                  // bf16: 512 B a pair, and set by the launcher: whether dz's kernel writes them,
+  int32_t store_zh, add_parts;  // whether the sums are added to the parts
 };
 
 struct CheckpointArgs {
@@ -477,6 +479,7 @@ hipError_t launch_trans_back_gen(const TransBackArgs& a, hipStream_t st);
 size_t trans_back_fast_prep_bytes();
 void trans_back_fast_units(const float* prep, const float** unit_a, const float** unit_b);
 int trans_back_fast_splits(int64_t n_pairs);
+size_t trans_back_fast_zh_bytes(int64_t n_pairs);
 hipError_t launch_trans_back_fast(const TransBackArgs& a, hipStream_t st);
 hipError_t launch_trans_back_finish(const TransBackArgs& a, hipStream_t st);
 hipError_t launch_checkpoint_pack(const CheckpointArgs& a, bool bf16, hipStream_t st);

@@ -151,6 +151,76 @@ __device__ __forceinline__ u32x4 decode8(u32x2 q, float scale) {
   return __builtin_bit_cast(u32x4, v);
 }
 
+// ----------------------------------------------------------------------------- rows
+// A lane (pair n of a tile of 16, group g) holds channels 32 ks + 8g .. + 7 of a row, ks = 0..3.
+template <bool CODES>
+__device__ __forceinline__ void load_row(const TransBackArgs& a, int64_t pair, int g, u32x4 (&z)[4]) {
+  if (CODES) {
+    const int8_t* q = static_cast<const int8_t*>(a.z) + pair * kCz + 8 * g;
+    const uint32_t e = *reinterpret_cast<const uint32_t*>(a.exponents + pair * 4);
+#pragma unroll
+    for (int ks = 0; ks < 4; ++ks)
+      z[ks] = decode8(*reinterpret_cast<const u32x2*>(q + 32 * ks), checkpoint_scale((e >> (8 * ks)) & 255));
+  } else {
+    const uint16_t* q = static_cast<const uint16_t*>(a.z) + pair * kCz + 8 * g;
+#pragma unroll
+    for (int ks = 0; ks < 4; ++ks) z[ks] = *reinterpret_cast<const u32x4*>(q + 32 * ks);
+  }
+}
+// zh in fp16 and bf16, and the statistics.
+__device__ __forceinline__ void normalise(const u32x4 (&z)[4], float eps, f16x8 (&zf)[4], bf16x8 (&zb)[4], float& mu, float& rstd) {
+  float x[4][8], s = 0.0f, v = 0.0f;
+#pragma unroll
+  for (int ks = 0; ks < 4; ++ks)
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      x[ks][i] = i & 1 ? hi_bf16(z[ks][i >> 1]) : lo_bf16(z[ks][i >> 1]);
+      s += x[ks][i];
+    }
+  mu = sum4(s) * (1.0f / kCz);
+#pragma unroll
+  for (int ks = 0; ks < 4; ++ks)
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      x[ks][i] -= mu;
+      v = fmaf(x[ks][i], x[ks][i], v);
+    }
+  rstd = __builtin_amdgcn_rsqf(sum4(v) * (1.0f / kCz) + eps);
+#pragma unroll
+  for (int ks = 0; ks < 4; ++ks)
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const float zh = x[ks][i] * rstd;
+      zf[ks][i] = (_Float16)zh;
+      zb[ks][i] = (__bf16)zh;
+    }
+}
+// zh of a tile of 16 pairs for the sums, 8 KB: [ks][lane] 16 B in fp16, as A operands; then the same in bf16, with
+// the pairs of odd groups 8 places on, which spreads the LDS reads of columns over all banks.
+__device__ __forceinline__ int column_lane(int n, int g) { return 16 * g + (n ^ (8 * (g & 1))); }
+__device__ __forceinline__ void store_zh(const TransBackArgs& a, int64_t tile, int n, int g, const f16x8 (&zf)[4], const bf16x8 (&zb)[4]) {
+  u32x4* const to = reinterpret_cast<u32x4*>(a.zh) + tile * 512;
+#pragma unroll
+  for (int ks = 0; ks < 4; ++ks) {
+    to[ks * 64 + 16 * g + n] = __builtin_bit_cast(u32x4, zf[ks]);
+    to[256 + ks * 64 + column_lane(n, g)] = __builtin_bit_cast(u32x4, zb[ks]);
+  }
+}
+
+// zh alone, where dz is not wanted or takes dout's place (the sums, which need zh, then come before it). One tile a wave.
+template <bool CODES>
+__global__ void __launch_bounds__(256) trans_back_rows_kernel(TransBackArgs a) {
+  const int lane = threadIdx.x & 63, n = lane & 15, g = lane >> 4;
+  const int64_t tile = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+  u32x4 z[4];
+  load_row<CODES>(a, min(tile * 16 + n, a.n_pairs - 1), g, z);
+  f16x8 zf[4];
+  bf16x8 zb[4];
+  float mu, rstd;
+  normalise(z, a.eps, zf, zb, mu, rstd);
+  store_zh(a, tile, n, g, zf, zb);
+}
+
 // ----------------------------------------------------------------------------- dz
 // A workgroup of 8 waves takes groups of 256 pairs, 32 a wave (two tiles of 16), persistently. zh (fp16) and dout
 // (bf16) are B operands in registers: lane (pair n, group g) holds channels 32 ks + 8g .. + 7. For every 32 units: A', B'
@@ -186,52 +256,27 @@ __global__ void __launch_bounds__(64 * kWaves) trans_back_pairs_fast_kernel(Tran
   for (; grp < n_groups; grp += gridDim.x) {
     const bool last_group = grp + gridDim.x >= n_groups;
     const int64_t pair0 = grp * kGroupPairs + wave * 32;
-    u32x4 dv[2][4], zz[2][4];
-#pragma unroll
-    for (int p = 0; p < 2; ++p) {
-      const int64_t pr = min(pair0 + 16 * p + n, a.n_pairs - 1);  // pairs past the end are not stored
-      if (CODES) {
-        const int8_t* q = static_cast<const int8_t*>(a.z) + pr * kCz + 8 * g;
-        const uint32_t e = *reinterpret_cast<const uint32_t*>(a.exponents + pr * 4);
-#pragma unroll
-        for (int ks = 0; ks < 4; ++ks)
-          zz[p][ks] = decode8(*reinterpret_cast<const u32x2*>(q + 32 * ks), checkpoint_scale((e >> (8 * ks)) & 255));
-      } else {
-        const uint16_t* q = static_cast<const uint16_t*>(a.z) + pr * kCz + 8 * g;
-#pragma unroll
-        for (int ks = 0; ks < 4; ++ks) zz[p][ks] = *reinterpret_cast<const u32x4*>(q + 32 * ks);
-      }
-      const uint16_t* d = static_cast<const uint16_t*>(a.dout) + pr * kCz + 8 * g;
-#pragma unroll
-      for (int ks = 0; ks < 4; ++ks) dv[p][ks] = *reinterpret_cast<const u32x4*>(d + 32 * ks);
-    }
+    u32x4 dv[2][4];
     f16x8 nv[2][4];
     float mu[2], rstd[2];
+    {
+      u32x4 zz[2][4];
 #pragma unroll
-    for (int p = 0; p < 2; ++p) {
-      float x[4][8], s = 0.0f, v = 0.0f;
+      for (int p = 0; p < 2; ++p) {
+        const int64_t pr = min(pair0 + 16 * p + n, a.n_pairs - 1);  // pairs past the end are not stored
+        load_row<CODES>(a, pr, g, zz[p]);
+        const uint16_t* d = static_cast<const uint16_t*>(a.dout) + pr * kCz + 8 * g;
 #pragma unroll
-      for (int ks = 0; ks < 4; ++ks) {
-        s_z[wave][4 * p + ks][lane] = zz[p][ks];
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          x[ks][i] = i & 1 ? hi_bf16(zz[p][ks][i >> 1]) : lo_bf16(zz[p][ks][i >> 1]);
-          s += x[ks][i];
-        }
+        for (int ks = 0; ks < 4; ++ks) dv[p][ks] = *reinterpret_cast<const u32x4*>(d + 32 * ks);
       }
-      mu[p] = sum4(s) * (1.0f / kCz);
 #pragma unroll
-      for (int ks = 0; ks < 4; ++ks)
+      for (int p = 0; p < 2; ++p) {
+        bf16x8 zb[4];
+        normalise(zz[p], a.eps, nv[p], zb, mu[p], rstd[p]);
+        if (a.store_zh) store_zh(a, pair0 / 16 + p, n, g, nv[p], zb);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          x[ks][i] -= mu[p];
-          v = fmaf(x[ks][i], x[ks][i], v);
-        }
-      rstd[p] = __builtin_amdgcn_rsqf(sum4(v) * (1.0f / kCz) + a.eps);
-#pragma unroll
-      for (int ks = 0; ks < 4; ++ks)
-#pragma unroll
-        for (int i = 0; i < 8; ++i) nv[p][ks][i] = (_Float16)(x[ks][i] * rstd[p]);
+        for (int ks = 0; ks < 4; ++ks) s_z[wave][4 * p + ks][lane] = zz[p][ks];
+      }
     }
     f32x4 acc[8][2];
 #pragma unroll
@@ -365,194 +410,221 @@ __global__ void __launch_bounds__(64 * kWaves) trans_back_pairs_fast_kernel(Tran
 // transposing reads bring: 16 lanes read four rows of 16 channels, and get four rows of one channel each.
 constexpr int kStep = 32;
 constexpr int kSlice = 128;
+constexpr int kStepBytes = 24 * 1024;  // zh in fp16, zh in bf16, dout: 8 KB each, two tiles of 4 KB
+constexpr int kAheadSteps = 2;
+constexpr int kStepSlots = kAheadSteps + 2;  // and those whose products and whose sums are formed
+constexpr int kStepDma = kStepBytes / 1024 / 4;
+constexpr int kOpBytes = 4 * 6 * 1024;  // dA', dB', H' of a step
 
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
 
-// 16-byte chunk `c` of row r of a [32][16] tile. A row is the LDS's banks once over: rows read together (16 at one
-// chunk, or four at two chunks) have other chunks in other rows.
-__device__ __forceinline__ int chunk_of_row(int r, int c) { return r * 16 + (c ^ (2 * (r & 7) + ((r >> 3) & 1))); }
-
-template <int CTRL>
-__device__ __forceinline__ float add_dpp(float x) {
-  return x + __uint_as_float((uint32_t)__builtin_amdgcn_update_dpp(0, (int)__float_as_uint(x), CTRL, 0xF, 0xF, true));
-}
-// Sum over 8 consecutive lanes, the same bits in each.
-__device__ __forceinline__ float sum8(float x) { return add_dpp<0x141>(add_dpp<0x4E>(add_dpp<0xB1>(x))); }
-
-template <bool CODES>
-__global__ void __launch_bounds__(256, 1) trans_back_sums_fast_kernel(TransBackArgs a) {
-  __shared__ __attribute__((aligned(16))) u32x4 s_x[2][3][kStep * 16];  // zh in fp16, zh in bf16, dout
+__global__ void __launch_bounds__(512, 2) trans_back_sums_fast_kernel(TransBackArgs a) {
+  __shared__ __attribute__((aligned(16))) char s_x[kStepSlots * kStepBytes];
+  __shared__ __attribute__((aligned(16))) char s_op[2 * kOpBytes];
   const int tid = threadIdx.x, lane = tid & 63, n = lane & 15, g = lane >> 4;
-  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int hp = blockIdx.y * (kSlice / 32) + wave;  // this wave's 32 units
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), share = wave & 3;
+  const int hp = blockIdx.y * (kSlice / 32) + share;  // this wave's 32 units
   const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
-  f16x8 w1[2][4], w2[2][4];
-  bf16x8 w3[2][4];
-  float k[2], kl[2], ba[2], bb[2];
-  {
-    const u32x4* base = reinterpret_cast<const u32x4*>(reinterpret_cast<const char*>(a.prep) + (size_t)hp * kPairBytes) + lane;
-    const float* units = reinterpret_cast<const float*>(reinterpret_cast<const char*>(a.prep) + (size_t)kHp * kPairBytes) + 32 * hp + n;
+  const int64_t steps = (a.n_pairs + kStep - 1) / kStep;
+  const int count = (int)((steps - blockIdx.x + gridDim.x - 1) / gridDim.x);  // of this workgroup, at least one
+  constexpr int64_t kSize = (int64_t)kHid * kCz;
+  float* const part = a.parts + blockIdx.x * (3 * kSize + 2 * kHid);
+  char* const my_op = s_op + share * 6 * 1024 + lane * 16;
+  if (wave < 4) {
+    // ---- A', B', dH and what follows from them
+    f16x8 w1[2][4], w2[2][4];
+    bf16x8 w3[2][4];
+    float k[2], kl[2], ba[2], bb[2];
+    {
+      const u32x4* base = reinterpret_cast<const u32x4*>(reinterpret_cast<const char*>(a.prep) + (size_t)hp * kPairBytes) + lane;
+      const float* units = reinterpret_cast<const float*>(reinterpret_cast<const char*>(a.prep) + (size_t)kHp * kPairBytes) + 32 * hp + n;
 #pragma unroll
-    for (int ut = 0; ut < 2; ++ut) {
+      for (int ut = 0; ut < 2; ++ut) {
 #pragma unroll
-      for (int ks = 0; ks < 4; ++ks) {
-        w1[ut][ks] = as_f16x8(base[(ut * 4 + ks) * 192]);
-        w2[ut][ks] = as_f16x8(base[(ut * 4 + ks) * 192 + 64]);
-        w3[ut][ks] = as_bf16x8(base[(ut * 4 + ks) * 192 + 128]);
+        for (int ks = 0; ks < 4; ++ks) {
+          w1[ut][ks] = as_f16x8(base[(ut * 4 + ks) * 192]);
+          w2[ut][ks] = as_f16x8(base[(ut * 4 + ks) * 192 + 64]);
+          w3[ut][ks] = as_bf16x8(base[(ut * 4 + ks) * 192 + 128]);
+        }
+        kl[ut] = units[kUnitLog * kHid + 16 * ut];
+        k[ut] = units[kUnitA * kHid + 16 * ut];
+        ba[ut] = units[kUnitBiasA * kHid + 16 * ut];
+        bb[ut] = units[kUnitBiasB * kHid + 16 * ut];
       }
-      kl[ut] = units[kUnitLog * kHid + 16 * ut];
-      k[ut] = units[kUnitA * kHid + 16 * ut];
-      ba[ut] = units[kUnitBiasA * kHid + 16 * ut];
-      bb[ut] = units[kUnitBiasB * kHid + 16 * ut];
     }
-  }
-  f32x4 t[3][2][8], s[2][2];
+    auto sum_at = [&](int m, int ut, int i) { return 3 * kSize + m * kHid + 32 * hp + 16 * ut + 4 * g + i; };
+    f32x4 s[2][2];  // S1, S2: every column of dA^T ones
 #pragma unroll
-  for (int ut = 0; ut < 2; ++ut) {
-    s[0][ut] = s[1][ut] = zero;
+    for (int m = 0; m < 2; ++m)
+#pragma unroll
+      for (int ut = 0; ut < 2; ++ut)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) s[m][ut][i] = a.add_parts ? part[sum_at(m, ut, i)] : 0.0f;
+    bf16x8 ones;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) ones[i] = (__bf16)1.0f;
+    const int row_at = lane * 16, drow_at = 16384 + column_lane(n, g) * 16;
+    const char* cur = s_x;
+    for (int it = 0; it < count; ++it) {
+      barrier_lds();
+      // the first tile of pairs, then the second, and between its products what follows from the first
+      auto row = [&](int q) { return *reinterpret_cast<const u32x4*>(cur + (q >> 2) * 4096 + (q & 3) * 1024 + row_at); };
+      auto drow = [&](int q) { return *reinterpret_cast<const u32x4*>(cur + (q >> 2) * 4096 + (q & 3) * 1024 + drow_at); };
+      f32x4 h[3][2][2];
+      bf16x8 op[3][2];
+      auto gate = [&](int ut, int p, int i) {
+        const Gated r = gated(h[0][ut][p][i], h[1][ut][p][i], h[2][ut][p][i], k[ut], kl[ut]);
+        op[0][ut][4 * p + i] = (__bf16)r.da;
+        op[1][ut][4 * p + i] = (__bf16)r.db;
+        op[2][ut][4 * p + i] = (__bf16)r.h;
+      };
+      constexpr int kQueue = 3;
+      u32x4 zq[kQueue], dq[kQueue];
+#pragma unroll
+      for (int q = 0; q < kQueue - 1; ++q) {
+        zq[q] = row(q);
+        dq[q] = drow(q);
+      }
+#pragma unroll
+      for (int q = 0; q < 8; ++q) {
+        const int p = q >> 2, ks = q & 3;
+        if (q + kQueue - 1 < 8) {
+          zq[(q + kQueue - 1) % kQueue] = row(q + kQueue - 1);
+          dq[(q + kQueue - 1) % kQueue] = drow(q + kQueue - 1);
+        }
+        const f16x8 za = as_f16x8(zq[q % kQueue]);
+        const bf16x8 d = as_bf16x8(dq[q % kQueue]);
+#pragma unroll
+        for (int ut = 0; ut < 2; ++ut) {
+          h[0][ut][p] = mfma_f16(za, w1[ut][ks], ks ? h[0][ut][p] : f32x4{ba[ut], ba[ut], ba[ut], ba[ut]});
+          h[1][ut][p] = mfma_f16(za, w2[ut][ks], ks ? h[1][ut][p] : f32x4{bb[ut], bb[ut], bb[ut], bb[ut]});
+          h[2][ut][p] = mfma32(d, w3[ut][ks], ks ? h[2][ut][p] : zero);
+        }
+        if (q >= 4) {
+          gate(0, 0, q - 4);
+          gate(1, 0, q - 4);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+      }
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        gate(0, 1, i);
+        gate(1, 1, i);
+      }
+#pragma unroll
+      for (int m = 0; m < 3; ++m)
+#pragma unroll
+        for (int ut = 0; ut < 2; ++ut)
+          *reinterpret_cast<u32x4*>(my_op + (it & 1) * kOpBytes + (m * 2 + ut) * 1024) = __builtin_bit_cast(u32x4, op[m][ut]);
+#pragma unroll
+      for (int m = 0; m < 2; ++m)
+#pragma unroll
+        for (int ut = 0; ut < 2; ++ut) s[m][ut] = mfma32(op[m][ut], ones, s[m][ut]);
+      cur = cur + kStepBytes == s_x + kStepSlots * kStepBytes ? s_x : cur + kStepBytes;
+    }
+    barrier_lds();
+    if (n == 0)
+#pragma unroll
+      for (int m = 0; m < 2; ++m)
+#pragma unroll
+        for (int ut = 0; ut < 2; ++ut)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) part[sum_at(m, ut, i)] = s[m][ut][i];
+    return;
+  }
+  // ---- the sums of the step before, and the copies of the steps to come
+  // This wave's share of a step's copies: pieces 6 share .. of 24 (piece = 4 KB tile, then ks)
+  auto copy = [&](int it) {
+    const int64_t step = blockIdx.x + (int64_t)it * gridDim.x;
+    const uint32_t to = lds_addr(s_x) + (uint32_t)((it & (kStepSlots - 1)) * kStepBytes);
+    const __amdgpu_buffer_rsrc_t zres = __builtin_amdgcn_make_buffer_rsrc(a.zh + step * (2 * 8192), 0, 2 * 8192, kRawBufferFlags);
+    // pairs past the end read as zeros
+    const int left = (int)min((int64_t)kStep, a.n_pairs - step * kStep);
+    const __amdgpu_buffer_rsrc_t dres = __builtin_amdgcn_make_buffer_rsrc(
+        const_cast<char*>(static_cast<const char*>(a.dout) + step * (kStep * kCz * 2)), 0, left * kCz * 2, kRawBufferFlags);
+#pragma unroll
+    for (int i = 0; i < kStepDma; ++i) {
+      const int piece = share * kStepDma + i, kind = piece >> 3, tile = (piece >> 2) & 1, ks = piece & 3;
+      if (kind < 2)
+        dma_b128(zres, tile * 8192 + kind * 4096 + ks * 1024 + lane * 16, to + (uint32_t)(piece * 1024));
+      else
+        dma_b128(dres, (16 * tile + (n ^ (8 * (g & 1)))) * (kCz * 2) + 64 * ks + 16 * g, to + (uint32_t)(piece * 1024));
+    }
+  };
+  static_assert((kStepSlots & (kStepSlots - 1)) == 0, "slots by a mask");
+#pragma unroll
+  for (int it = 0; it < kAheadSteps; ++it)
+    if (it < count) copy(it);
+  auto part_at = [&](int m, int ut, int ct, int i) { return m * kSize + (32 * hp + 16 * ut + 4 * g + i) * kCz + 16 * ct + n; };
+  f32x4 t[3][2][8];
+#pragma unroll
+  for (int m = 0; m < 3; ++m)
+#pragma unroll
+    for (int ut = 0; ut < 2; ++ut)
+#pragma unroll
+      for (int ct = 0; ct < 8; ++ct) t[m][ut][ct] = zero;
+  if (a.add_parts)  // the pairs before these
 #pragma unroll
     for (int m = 0; m < 3; ++m)
 #pragma unroll
-      for (int ct = 0; ct < 8; ++ct) t[m][ut][ct] = zero;
-  }
-  bf16x8 ones;
+      for (int ut = 0; ut < 2; ++ut)
 #pragma unroll
-  for (int i = 0; i < 8; ++i) ones[i] = (__bf16)1.0f;
-
-  // staging: thread (pair sp of the step, sixteen channels from 16 sq)
-  const int sp = tid >> 3, sq = tid & 7;
-  const int64_t steps = (a.n_pairs + kStep - 1) / kStep;
-  u32x4 zr[2], dr[2];
-  float scale = 1.0f;
-  bool there = false;
-  auto fetch = [&](int64_t step) {
-    const int64_t pair = step * kStep + sp, pr = min(pair, a.n_pairs - 1);
-    there = pair < a.n_pairs;
-    if (CODES) {
-      zr[0] = *reinterpret_cast<const u32x4*>(static_cast<const int8_t*>(a.z) + pr * kCz + 16 * sq);
-      scale = checkpoint_scale(a.exponents[pr * 4 + (sq >> 1)]);
-    } else {
-      const u32x4* q = reinterpret_cast<const u32x4*>(static_cast<const uint16_t*>(a.z) + pr * kCz) + 2 * sq;
-      zr[0] = q[0];
-      zr[1] = q[1];
-    }
-    const u32x4* d = reinterpret_cast<const u32x4*>(static_cast<const uint16_t*>(a.dout) + pr * kCz) + 2 * sq;
-    dr[0] = d[0];
-    dr[1] = d[1];
-  };
-  auto stage = [&](int b) {
-    float x[16], sum = 0.0f, var = 0.0f;
+        for (int ct = 0; ct < 8; ++ct)
 #pragma unroll
-    for (int i = 0; i < 16; ++i) {
-      if (CODES)
-        x[i] = (float)(int8_t)(zr[0][i >> 2] >> (8 * (i & 3))) * scale;
-      else
-        x[i] = i & 1 ? hi_bf16(zr[i >> 3][(i >> 1) & 3]) : lo_bf16(zr[i >> 3][(i >> 1) & 3]);
-      sum += x[i];
-    }
-    const float mu = sum8(sum) * (1.0f / kCz);
+          for (int i = 0; i < 4; ++i) t[m][ut][ct][i] = part[part_at(m, ut, ct, i)];
+  // a column read's piece: pair 4g + n / 4, channels 4 (n % 4) .. of 16; the chunk of 8 is that of group 2 (ct % 2) + n / 2 % 2
+  const int piece_odd = (n >> 1) & 1;
+  const int col_at = piece_odd * 256 + ((4 * g + (n >> 2)) ^ (8 * piece_odd)) * 16 + 8 * (n & 1);
+  const char* prev = s_x;
+  for (int it = 0; it <= count; ++it) {
+    // this wave's copies of step `it` have landed: at most those of the one after it are in flight
+    if (it + 1 < count)
+      wait_vm<kStepDma>();
+    else
+      wait_vm<0>();
+    barrier_lds();  // and every other wave's; the step before the last has been read
+    if (it + kAheadSteps < count) copy(it + kAheadSteps);
+    if (it == 0) continue;
+    bf16x8 op[3][2];
 #pragma unroll
-    for (int i = 0; i < 16; ++i) {
-      x[i] -= mu;
-      var = fmaf(x[i], x[i], var);
-    }
-    const float rstd = __builtin_amdgcn_rsqf(sum8(var) * (1.0f / kCz) + a.eps);
+    for (int m = 0; m < 3; ++m)
 #pragma unroll
-    for (int half = 0; half < 2; ++half) {
-      f16x8 zf;
-      bf16x8 zb;
+      for (int ut = 0; ut < 2; ++ut)
+        op[m][ut] = as_bf16x8(*reinterpret_cast<const u32x4*>(my_op + ((it - 1) & 1) * kOpBytes + (m * 2 + ut) * 1024));
+    auto columns = [&](int q) {  // q = 2 ct: zh, 2 ct + 1: dout
+      u32x4 v;
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        const float zh = there ? x[8 * half + i] * rstd : 0.0f;
-        zf[i] = (_Float16)zh;
-        zb[i] = (__bf16)zh;
+      for (int half = 0; half < 2; ++half) {
+        const s16x4 x = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+            (lds_s16x4*)(prev + 8192 + (q & 1) * 8192 + half * 4096 + (q >> 2) * 1024 + ((q >> 1) & 1) * 512 + col_at));
+        const u32x2 w = __builtin_bit_cast(u32x2, x);
+        v[2 * half] = w[0];
+        v[2 * half + 1] = w[1];
       }
-      const int at = chunk_of_row(sp, 2 * sq + half);
-      s_x[b][0][at] = __builtin_bit_cast(u32x4, zf);
-      s_x[b][1][at] = __builtin_bit_cast(u32x4, zb);
-      s_x[b][2][at] = there ? dr[half] : u32x4{0u, 0u, 0u, 0u};
-    }
-  };
-  // columns of 16 channels, over the 32 pairs of tile m in buffer b
-  const int tr = n >> 2, tq = n & 3;
-  auto columns = [&](int b, int m, int ct) {
-    u32x4 v;
+      return as_bf16x8(v);
+    };
+    constexpr int kQueue = 3;
+    bf16x8 cq[kQueue];
 #pragma unroll
-    for (int half = 0; half < 2; ++half) {
-      const int at = chunk_of_row(16 * half + 4 * g + tr, 2 * ct + (tq >> 1));
-      const s16x4 x = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(reinterpret_cast<char*>(&s_x[b][m][at]) + 8 * (tq & 1)));
-      const u32x2 w = __builtin_bit_cast(u32x2, x);
-      v[2 * half] = w[0];
-      v[2 * half + 1] = w[1];
-    }
-    return as_bf16x8(v);
-  };
-
-  int64_t step = blockIdx.x;
-  if (step < steps) {
-    fetch(step);
-    stage(0);
-    if (step + gridDim.x < steps) fetch(step + gridDim.x);
-  }
-  __syncthreads();
-  for (int b = 0; step < steps; step += gridDim.x, b ^= 1) {
-    f32x4 h[3][2][2];  // A', B', dH [unit tile][pair tile]
+    for (int q = 0; q < kQueue - 1; ++q) cq[q] = columns(q);
 #pragma unroll
-    for (int ut = 0; ut < 2; ++ut)
-#pragma unroll
-      for (int p = 0; p < 2; ++p) {
-        h[0][ut][p] = f32x4{ba[ut], ba[ut], ba[ut], ba[ut]};
-        h[1][ut][p] = f32x4{bb[ut], bb[ut], bb[ut], bb[ut]};
-        h[2][ut][p] = zero;
-      }
-#pragma unroll
-    for (int ks = 0; ks < 4; ++ks)
-#pragma unroll
-      for (int p = 0; p < 2; ++p) {
-        const int at = chunk_of_row(16 * p + n, 4 * ks + g);
-        const f16x8 zf = as_f16x8(s_x[b][0][at]);
-        const bf16x8 dv = as_bf16x8(s_x[b][2][at]);
-#pragma unroll
-        for (int ut = 0; ut < 2; ++ut) {
-          h[0][ut][p] = mfma_f16(zf, w1[ut][ks], h[0][ut][p]);
-          h[1][ut][p] = mfma_f16(zf, w2[ut][ks], h[1][ut][p]);
-          h[2][ut][p] = mfma32(dv, w3[ut][ks], h[2][ut][p]);
-        }
-      }
-    bf16x8 hv[2], da[2], db[2];
-#pragma unroll
-    for (int ut = 0; ut < 2; ++ut)
-#pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        const Gated r = gated(h[0][ut][j >> 2][j & 3], h[1][ut][j >> 2][j & 3], h[2][ut][j >> 2][j & 3], k[ut], kl[ut]);
-        hv[ut][j] = (__bf16)r.h;
-        da[ut][j] = (__bf16)r.da;
-        db[ut][j] = (__bf16)r.db;
-      }
-#pragma unroll
-    for (int ut = 0; ut < 2; ++ut) {
-      s[0][ut] = mfma32(da[ut], ones, s[0][ut]);
-      s[1][ut] = mfma32(db[ut], ones, s[1][ut]);
-    }
-#pragma unroll
-    for (int ct = 0; ct < 8; ++ct) {
-      const bf16x8 zc = columns(b, 1, ct), dc = columns(b, 2, ct);
+    for (int q = 0; q < 16; ++q) {
+      if (q + kQueue - 1 < 16) cq[(q + kQueue - 1) % kQueue] = columns(q + kQueue - 1);
+      const int ct = q >> 1;
 #pragma unroll
       for (int ut = 0; ut < 2; ++ut) {
-        t[0][ut][ct] = mfma32(da[ut], zc, t[0][ut][ct]);
-        t[1][ut][ct] = mfma32(db[ut], zc, t[1][ut][ct]);
-        t[2][ut][ct] = mfma32(hv[ut], dc, t[2][ut][ct]);
+        if (q & 1) {
+          t[2][ut][ct] = mfma32(op[2][ut], cq[q % kQueue], t[2][ut][ct]);
+        } else {
+          t[0][ut][ct] = mfma32(op[0][ut], cq[q % kQueue], t[0][ut][ct]);
+          t[1][ut][ct] = mfma32(op[1][ut], cq[q % kQueue], t[1][ut][ct]);
+        }
       }
+      __builtin_amdgcn_sched_barrier(0);
     }
-    if (step + gridDim.x < steps) {
-      stage(b ^ 1);
-      if (step + 2 * gridDim.x < steps) fetch(step + 2 * gridDim.x);
-    }
-    __syncthreads();
+    prev = prev + kStepBytes == s_x + kStepSlots * kStepBytes ? s_x : prev + kStepBytes;
   }
-  constexpr int64_t kSize = (int64_t)kHid * kCz;
-  float* part = a.parts + blockIdx.x * (3 * kSize + 2 * kHid);
 #pragma unroll
   for (int m = 0; m < 3; ++m)
 #pragma unroll
@@ -560,14 +632,7 @@ __global__ void __launch_bounds__(256, 1) trans_back_sums_fast_kernel(TransBackA
 #pragma unroll
       for (int ct = 0; ct < 8; ++ct)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) part[m * kSize + (32 * hp + 16 * ut + 4 * g + i) * kCz + 16 * ct + n] = t[m][ut][ct][i];
-  if (n == 0)
-#pragma unroll
-    for (int m = 0; m < 2; ++m)
-#pragma unroll
-      for (int ut = 0; ut < 2; ++ut)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) part[3 * kSize + m * kHid + 32 * hp + 16 * ut + 4 * g + i] = s[m][ut][i];
+        for (int i = 0; i < 4; ++i) part[part_at(m, ut, ct, i)] = t[m][ut][ct][i];
 }
 
 }  // namespace
@@ -584,27 +649,53 @@ int trans_back_fast_splits(int64_t n_pairs) {
   return (int)(steps < 64 ? steps : 64);
 }
 
-hipError_t launch_trans_back_fast(const TransBackArgs& a, hipStream_t st) {
+// Pairs at a time: 512 B of zh each in the workspace.
+constexpr int64_t kChunkPairs = (int64_t)1 << 20;
+size_t trans_back_fast_zh_bytes(int64_t n_pairs) {
+  const int64_t groups = ((n_pairs < kChunkPairs ? n_pairs : kChunkPairs) + kGroupPairs - 1) / kGroupPairs;
+  return (size_t)groups * kGroupPairs * 512;
+}
+
+hipError_t launch_trans_back_fast(const TransBackArgs& whole, hipStream_t st) {
   hipError_t e;
-  hipLaunchKernelGGL(trans_back_prep_fast_kernel, dim3(kHid / 16), dim3(256), 0, st, a);
+  hipLaunchKernelGGL(trans_back_prep_fast_kernel, dim3(kHid / 16), dim3(256), 0, st, whole);
   if ((e = hipGetLastError()) != hipSuccess) return e;
-  // The sums read dout, which dz may take the place of: they come first.
-  if (a.dw1 || a.dw2 || a.dw3 || a.dgamma || a.dbeta) {
-    const dim3 grid((unsigned)a.splits, kHid / kSlice);
-    if (a.exponents)
-      hipLaunchKernelGGL(trans_back_sums_fast_kernel<true>, grid, dim3(256), 0, st, a);
-    else
-      hipLaunchKernelGGL(trans_back_sums_fast_kernel<false>, grid, dim3(256), 0, st, a);
-    if ((e = hipGetLastError()) != hipSuccess) return e;
+  const bool sums = whole.dw1 || whole.dw2 || whole.dw3 || whole.dgamma || whole.dbeta;
+  const bool sums_first = whole.dz == whole.dout || !whole.dz;
+  for (int64_t p0 = 0; p0 < whole.n_pairs; p0 += kChunkPairs) {
+    TransBackArgs a = whole;
+    a.n_pairs = whole.n_pairs - p0 < kChunkPairs ? whole.n_pairs - p0 : kChunkPairs;
+    a.z = static_cast<const char*>(whole.z) + p0 * kCz * (whole.exponents ? 1 : 2);
+    a.dout = static_cast<const char*>(whole.dout) + p0 * kCz * 2;
+    if (whole.exponents) a.exponents += p0 * 4;
+    if (whole.dz) a.dz = static_cast<char*>(whole.dz) + p0 * kCz * 2;
+    a.store_zh = sums && !sums_first;
+    a.add_parts = p0 > 0;
+    const int64_t n_groups = (a.n_pairs + kGroupPairs - 1) / kGroupPairs;
+    const dim3 pairs_grid((unsigned)(n_groups < 256 ? n_groups : 256)), rows_grid((unsigned)(n_groups * 4));
+    const dim3 sums_grid((unsigned)a.splits, kHid / kSlice);
+    if (sums && sums_first) {
+      if (a.exponents)
+        hipLaunchKernelGGL(trans_back_rows_kernel<true>, rows_grid, dim3(256), 0, st, a);
+      else
+        hipLaunchKernelGGL(trans_back_rows_kernel<false>, rows_grid, dim3(256), 0, st, a);
+      if ((e = hipGetLastError()) != hipSuccess) return e;
+      hipLaunchKernelGGL(trans_back_sums_fast_kernel, sums_grid, dim3(512), 0, st, a);
+      if ((e = hipGetLastError()) != hipSuccess) return e;
+    }
+    if (a.dz) {
+      if (a.exponents)
+        hipLaunchKernelGGL(trans_back_pairs_fast_kernel<true>, pairs_grid, dim3(64 * kWaves), 0, st, a);
+      else
+        hipLaunchKernelGGL(trans_back_pairs_fast_kernel<false>, pairs_grid, dim3(64 * kWaves), 0, st, a);
+      if ((e = hipGetLastError()) != hipSuccess) return e;
+    }
+    if (sums && !sums_first) {
+      hipLaunchKernelGGL(trans_back_sums_fast_kernel, sums_grid, dim3(512), 0, st, a);
+      if ((e = hipGetLastError()) != hipSuccess) return e;
+    }
   }
-  if (!a.dz) return hipSuccess;
-  const int64_t n_groups = (a.n_pairs + kGroupPairs - 1) / kGroupPairs;
-  const dim3 grid((unsigned)(n_groups < 256 ? n_groups : 256));
-  if (a.exponents)
-    hipLaunchKernelGGL(trans_back_pairs_fast_kernel<true>, grid, dim3(64 * kWaves), 0, st, a);
-  else
-    hipLaunchKernelGGL(trans_back_pairs_fast_kernel<false>, grid, dim3(64 * kWaves), 0, st, a);
-  return hipGetLastError();
+  return hipSuccess;
 }
 
 }  // namespace dcp

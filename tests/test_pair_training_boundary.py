@@ -57,8 +57,8 @@ def test_transition_backward_workspace():
     size = dcp.dcp_pair_transition_backward_workspace_size
     need = size(1000, 128, 512, 1)
     assert need > 0 and backward(ws_bytes=need - 1) == WORKSPACE
-    # the gradients' sums of shares of the pairs, not the pairs, size it but for the statistics of each pair
-    assert size(1 << 24, 128, 512, 1) < 256e6 and size(1 << 24, 32, 128, 0) < 256e6
+    # bounded: shares' sums and, in bf16, 512 B for each of at most 2^20 pairs
+    assert size(1 << 34, 128, 512, 1) == size(1 << 20, 128, 512, 1) < 640e6 and size(1 << 34, 32, 128, 0) < 256e6
     out, lib = ctypes.c_size_t(), dcp.lib()
     query = lib.dcp_pair_transition_backward_workspace_size
     assert query(10, 128, 512, 1, None) == BAD and query(-1, 128, 512, 1, ctypes.byref(out)) == BAD
