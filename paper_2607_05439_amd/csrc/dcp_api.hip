@@ -1622,7 +1622,7 @@ void trans_back_layout(int64_t n_pairs, int32_t c, int32_t hidden, bool fast, Tr
   };
   L->off_prep = take(fast ? dcp::trans_back_fast_prep_bytes() / sizeof(float) : 5 * cp * hp + 2 * cp);
   L->off_parts = take((size_t)L->splits * (3 * cp * hp + 2 * hp));
-  L->off_affine = take((size_t)(hidden + 1) / 2 * 2 * c);
+  L->off_affine = take((size_t)hidden * 2 * c);
   L->off_zh = take(fast ? dcp::trans_back_fast_zh_bytes(n_pairs) / sizeof(float) : 0);
   L->total = o;
 }
@@ -1767,7 +1767,7 @@ int checkpoint(bool pack, int64_t n_rows, int32_t c, int32_t dtype, const void* 
   a.exponents = const_cast<uint8_t*>(static_cast<const uint8_t*>(exponents));
   const bool bf16 = dtype == DCP_BF16;
   hipStream_t st = static_cast<hipStream_t>(stream);
-  const hipError_t e = pack ? dcp::launch_checkpoint_pack(a, bf16, st) : dcp::launch_checkpoint_unpack(a, bf16, st);
+  const hipError_t e = dcp::launch_checkpoint(a, bf16, st);
   if (e != hipSuccess) return fail(DCP_ERR_HIP, "checkpoint launch failed: %s", hipGetErrorString(e));
   return ok();
 }
@@ -1818,7 +1818,12 @@ int check_relative(int64_t n_tokens, int64_t row0, int64_t n_rows, int32_t c, in
     a->radius[f] = fields[f].radius;
     a->first[f] = a->n_buckets;
     a->n_buckets += 2 * fields[f].radius + 2;
+    for (int t = 0; 16 * t < 2 * fields[f].radius + 2; ++t) {
+      a->tile_field[a->n_tiles] = (uint8_t)f;
+      a->tile_of_field[a->n_tiles++] = (uint8_t)t;
+    }
   }
+  dcp::relative_back_split(a);
   return DCP_OK;
 }
 
@@ -1831,6 +1836,10 @@ int check_relative_call(const dcp::RelativeArgs& a, int32_t dtype) {
         return fail(DCP_ERR_INVALID_ARGUMENT, "positions and groups must be 4-byte aligned (field %d)", f);
     }
   return DCP_OK;
+}
+
+size_t relative_back_bytes(const dcp::RelativeArgs& a) {
+  return round_up((size_t)a.n_parts * a.n_tiles * 16 * a.c * sizeof(float), 256);
 }
 
 // What a call writes, `out` and a workspace, against what it reads
@@ -1877,7 +1886,7 @@ int dcp_relative_position_backward_workspace_size(int64_t n_tokens, int64_t n_ro
   if (!bytes) return fail(DCP_ERR_INVALID_ARGUMENT, "bytes is NULL");
   dcp::RelativeArgs a;
   if (const int rc = check_relative(n_tokens, 0, n_rows, c, n_fields, fields, &a)) return rc;
-  *bytes = round_up((size_t)dcp::relative_back_parts(n_tokens, n_rows, c, a.n_buckets) * a.n_buckets * c * sizeof(float), 256);
+  *bytes = relative_back_bytes(a);
   return ok();
 }
 
@@ -1891,13 +1900,12 @@ int dcp_relative_position_backward(int64_t n_tokens, int64_t row0, int64_t n_row
   if (!dtable || (n_rows > 0 && !dz_rows)) return fail(DCP_ERR_INVALID_ARGUMENT, "dz_rows and dtable are required");
   if (!aligned(dtable, 4) || !aligned(dz_rows, elem(dtype)))
     return fail(DCP_ERR_INVALID_ARGUMENT, "dz_rows and dtable must be aligned to their element size");
-  a.n_parts = dcp::relative_back_parts(n_tokens, n_rows, c, a.n_buckets);
-  const size_t need = (size_t)a.n_parts * a.n_buckets * c * sizeof(float);
+  const size_t need = relative_back_bytes(a);
   if (n_rows > 0) {
     if (!workspace || !aligned(workspace, 256))
       return fail(DCP_ERR_WORKSPACE, "workspace must be a 256-byte aligned device pointer");
-    if (workspace_bytes < round_up(need, 256))
-      return fail(DCP_ERR_WORKSPACE, "workspace too small: %zu bytes given, %zu needed", workspace_bytes, round_up(need, 256));
+    if (workspace_bytes < need)
+      return fail(DCP_ERR_WORKSPACE, "workspace too small: %zu bytes given, %zu needed", workspace_bytes, need);
   }
   rc = check_relative_apart(a, {"dtable", dtable, (size_t)a.n_buckets * c * 4}, {"workspace", workspace, need},
                             {"dz_rows", dz_rows, (size_t)n_rows * n_tokens * c * elem(dtype)});

@@ -406,7 +406,7 @@ struct TransBackArgs {
   float* prep;               // weights as operands
   float* parts;              // [splits]: T1, T2, T3 [hp][cp], S1, S2 [hp] (hidden and c filled up to 16)
   const float *unit_a, *unit_b;  // [hidden]: T2 and S2 times unit_a, T1 and S1 times unit_b, T3 times both; null: 1
-  float* affine_parts;       // [(hidden + 1) / 2][2][c]
+  float* affine_parts;       // [hidden][2][c]
   char* zh;                  // bf16: 512 B a pair, and set by the launcher: whether dz's kernel writes them,
   int32_t store_zh, add_parts;  // whether the sums are added to the parts
 };
@@ -414,8 +414,8 @@ struct TransBackArgs {
 struct CheckpointArgs {
   int64_t n_rows;
   int32_t c;
-  const void* x;  // pack
-  void* y;        // unpack
+  const void* x;  // to be packed, or null
+  void* y;        // where to unpack, or null
   int8_t* codes;  // [n_rows][c]
   uint8_t* exponents;
 };
@@ -434,8 +434,11 @@ struct RelativeArgs {
   void* z_out;
   const void* dz;
   float* dtable;
-  float* parts;  // [n_parts][n_buckets][c]
-  int32_t n_parts;
+  // The gradient's buckets in tiles of 16, each of one field: the field, and the tile's place in it
+  uint8_t tile_field[kRelativeFields * 16], tile_of_field[kRelativeFields * 16];
+  int32_t n_tiles;
+  float* parts;  // [n_parts][16 n_tiles][c]
+  int32_t n_groups, n_parts;  // workgroups over the pairs, and sums of their own
 };
 
 size_t fast_proj_split_bytes(int32_t c_s);
@@ -482,10 +485,9 @@ int trans_back_fast_splits(int64_t n_pairs);
 size_t trans_back_fast_zh_bytes(int64_t n_pairs);
 hipError_t launch_trans_back_fast(const TransBackArgs& a, hipStream_t st);
 hipError_t launch_trans_back_finish(const TransBackArgs& a, hipStream_t st);
-hipError_t launch_checkpoint_pack(const CheckpointArgs& a, bool bf16, hipStream_t st);
-hipError_t launch_checkpoint_unpack(const CheckpointArgs& a, bool bf16, hipStream_t st);
+hipError_t launch_checkpoint(const CheckpointArgs& a, bool bf16, hipStream_t st);
 hipError_t launch_relative(const RelativeArgs& a, bool bf16, hipStream_t st);
-int relative_back_parts(int64_t n_tok, int64_t n_rows, int32_t c, int32_t n_buckets);
+void relative_back_split(RelativeArgs* a);  // sets n_groups and n_parts
 hipError_t launch_relative_back(const RelativeArgs& a, bool bf16, hipStream_t st);
 int scatter_order_flags(int64_t n_atoms);  // plan workgroups (one flag each) for n_atoms (<= kScatterFlags)
 

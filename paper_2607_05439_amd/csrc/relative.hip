@@ -63,58 +63,346 @@ __global__ void __launch_bounds__(256) relative_any_kernel(RelativeArgs a) {
   }
 }
 
-// One thread per channel and share of the pairs: a bucket's sum in the workspace, in order.
-template <typename T>
-__global__ void __launch_bounds__(64) relative_back_any_kernel(RelativeArgs a) {
-  const int c = blockIdx.y * 64 + threadIdx.x;
-  if (c >= a.c) return;
-  float* const part = a.parts + (int64_t)blockIdx.x * a.n_buckets * a.c + c;
-  for (int b = 0; b < a.n_buckets; ++b) part[(int64_t)b * a.c] = 0.0f;
-  for (int64_t row = blockIdx.x; row < a.n_rows; row += gridDim.x)
-    for (int64_t j = 0; j < a.n_tok; ++j) {
-      const uint32_t t = buckets_of(a, a.row0 + row, j);
-      const float v = load_f32(static_cast<const T*>(a.dz) + (row * a.n_tok + j) * a.c + c);
-      for (int f = 0; f < a.n_fields; ++f) part[(int64_t)(a.first[f] + (int)(t >> (8 * f) & 255)) * a.c] += v;
+// Rows of whole 16-byte pieces: 2^k lanes a pair, a piece each, and so 64 / 2^k pairs at a time; the lanes of a pair
+// go through 2^k consecutive ones. The sum of the table's rows is kept while the buckets stay the same, as they do
+// where the offsets are clipped or the chains differ; else its rows come from the caches (71 KB of the paper's
+// fields at 128 channels). Bound by memory.
+template <typename T, int LANES>
+__global__ void __launch_bounds__(256) relative_kernel(RelativeArgs a) {
+  constexpr int kVec = 16 / sizeof(T), kBatch = LANES < 8 ? LANES : 8;
+  const int lane = threadIdx.x & 63, piece = lane & (LANES - 1), base = lane & ~(LANES - 1);
+  const int64_t unit = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int64_t blocks = (a.n_tok + 63) / 64;
+  if (unit >= a.n_rows * blocks) return;
+  const int64_t row = unit / blocks, j0 = (unit - row * blocks) * 64;
+  const int left = (int)min((int64_t)64, a.n_tok - j0);
+  const uint32_t mine = buckets_of(a, a.row0 + row, min(j0 + lane, a.n_tok - 1));
+  const bool holds = piece * kVec < a.c;
+  const int pieces = a.c / kVec;
+  const int64_t first = (row * a.n_tok + j0 + base) * pieces + piece;
+  const float* const table = a.table + piece * kVec;
+  float sum[kVec];
+  uint32_t last = 0;
+  bool any = false;
+#pragma unroll 1
+  for (int k0 = 0; k0 < LANES; k0 += kBatch) {
+    u32x4 z[kBatch];
+#pragma unroll
+    for (int k = 0; k < kBatch; ++k) {
+      z[k] = u32x4{0u, 0u, 0u, 0u};
+      if (a.z_in && holds && base + k0 + k < left)
+        z[k] = __builtin_nontemporal_load(static_cast<const u32x4*>(a.z_in) + first + (int64_t)(k0 + k) * pieces);
     }
+#pragma unroll
+    for (int k = 0; k < kBatch; ++k) {
+      const uint32_t t = (uint32_t)__shfl((int)mine, base + k0 + k);
+      if (!holds || base + k0 + k >= left) continue;
+      if (!any || t != last) {
+        any = true;
+        last = t;
+#pragma unroll
+        for (int e = 0; e < kVec; ++e) sum[e] = 0.0f;
+#pragma unroll
+        for (int f = 0; f < kRelativeFields; ++f)
+          if (f < a.n_fields) {
+            const float* r = table + (int64_t)(a.first[f] + (int)(t >> (8 * f) & 255)) * a.c;
+#pragma unroll
+            for (int e = 0; e < kVec; e += 4) {
+              const f32x4 v = *reinterpret_cast<const f32x4*>(r + e);
+#pragma unroll
+              for (int i = 0; i < 4; ++i) sum[e + i] += v[i];
+            }
+          }
+      }
+      u32x4 o;
+      if (kVec == 8) {
+        bf16x8 b;
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+          b[e] = (__bf16)(__uint_as_float(e & 1 ? z[k][e >> 1] & 0xFFFF0000u : z[k][e >> 1] << 16) + sum[e % kVec]);
+        o = __builtin_bit_cast(u32x4, b);
+      } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) o[e] = __float_as_uint(__uint_as_float(z[k][e]) + sum[e]);
+      }
+      __builtin_nontemporal_store(o, static_cast<u32x4*>(a.z_out) + first + (int64_t)(k0 + k) * pieces);
+    }
+  }
 }
 
+// ----------------------------------------------------------------------------- the table's gradient
+// dtable = one-hot^T dz on the matrix cores: v_mfma_f32_16x16x32_bf16 with 16 buckets of one field as rows, 32 pairs
+// as k-slots and 16 channels as columns. A one-hot's products are exact, and so are fp32 gradients in three bf16 pieces
+// (8 bits each); the sums are fp32, in an order that the sizes alone fix. Only the tiles of buckets that occur
+// among the 32 pairs are multiplied: near the diagonal three or four of twelve, elsewhere one a field.
+//   A workgroup takes a share of the tiles of 64 S pairs of a row and 32 CG channels (S CG = 4): CG waves take 32
+// channels each, and S such sets the pairs' 64ths, each with sums of its own. dz is copied through registers one
+// tile ahead into LDS as [pair][channel], whose transposing reads bring 16 channels of eight pairs as a B operand;
+// k-slot 8g + j is pair 4g + j of the 32 for j < 4, 16 + 4g + j - 4 for j >= 4. Buckets lie in LDS as bytes.
+//   A value that is not finite would make NaN of every bucket (0 times infinity): it enters as 0 and is added to its
+// own buckets afterwards. Bound by memory: 2400 rows of 4800 tokens read dz once.
+constexpr int kWindow = 12;  // tiles of buckets at a time: the paper's fields have 5 + 5 + 1 + 1
+
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
+
+template <typename T, int CG, bool VEC>
+__global__ void __launch_bounds__(256) relative_back_kernel(RelativeArgs a) {
+  constexpr int kVec = 16 / sizeof(T), S = 4 / CG, kPairs = 64 * S, kChannels = 32 * CG;
+  constexpr int kPlanes = sizeof(T) == 2 ? 1 : 3, kRow = 2 * kChannels + 32, kPlane = kPairs * kRow;
+  constexpr int kRowPieces = kChannels / kVec, kMine = kPairs * kRowPieces / 256;
+  __shared__ __attribute__((aligned(16))) char s_d[kPlanes * kPlane];
+  __shared__ __attribute__((aligned(16))) uint8_t s_b[4][kRelativeFields][64];
+  __shared__ __attribute__((aligned(16))) int s_bad[4];
+  const int tid = threadIdx.x, lane = tid & 63, n = lane & 15, g = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), cg = wave % CG, stream = wave / CG;
+  const int c0 = blockIdx.y * kChannels, w0 = blockIdx.z * kWindow;
+  const int64_t row_tiles = (a.n_tok + kPairs - 1) / kPairs, tiles = a.n_rows * row_tiles;
+  f32x4 acc[kWindow][2];
+#pragma unroll
+  for (int w = 0; w < kWindow; ++w) acc[w][0] = acc[w][1] = f32x4{0.f, 0.f, 0.f, 0.f};
+
+  u32x4 raw[kMine];
+  uint32_t mine = 0;
+  int64_t row = 0, j0 = 0;
+  const T* const dz = static_cast<const T*>(a.dz);
+  auto fetch = [&](int64_t tile) {
+    row = tile / row_tiles;
+    j0 = (tile - row * row_tiles) * kPairs;
+#pragma unroll
+    for (int k = 0; k < kMine; ++k) {
+      const int p = (tid + 256 * k) / kRowPieces, c = c0 + (tid + 256 * k) % kRowPieces * kVec;
+      raw[k] = u32x4{0u, 0u, 0u, 0u};
+      if (j0 + p >= a.n_tok || c >= a.c) continue;
+      const T* q = dz + (row * a.n_tok + j0 + p) * a.c + c;
+      if (VEC) {
+        raw[k] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(q));
+      } else {
+#pragma unroll
+        for (int e = 0; e < kVec; ++e)
+          if (c + e < a.c) {
+            if (sizeof(T) == 2)
+              raw[k][e >> 1] |= (uint32_t)__builtin_bit_cast(uint16_t, (__bf16)load_f32(q + e)) << (16 * (e & 1));
+            else
+              raw[k][e & 3] = __float_as_uint(load_f32(q + e));
+          }
+      }
+    }
+    mine = buckets_of(a, a.row0 + row, min(j0 + 64 * stream + lane, a.n_tok - 1));
+  };
+  int64_t tile = blockIdx.x;
+  if (tile < tiles) fetch(tile);
+  for (; tile < tiles; tile += gridDim.x) {
+    const uint32_t buckets = mine;
+    const int64_t this_row = row, this_j0 = j0;
+    __syncthreads();  // the tile before has been read
+    bool bad = false;
+#pragma unroll
+    for (int k = 0; k < kMine; ++k) {
+      char* const to = s_d + (tid + 256 * k) / kRowPieces * kRow + (tid + 256 * k) % kRowPieces * (2 * kVec);
+      if (sizeof(T) == 2) {
+        bool here = false;
+#pragma unroll
+        for (int d = 0; d < 4; ++d)
+          here |= (raw[k][d] & 0x7F800000u) == 0x7F800000u || (raw[k][d] & 0x7F80u) == 0x7F80u;
+        if (here) {
+#pragma unroll
+          for (int d = 0; d < 4; ++d) {
+            if ((raw[k][d] & 0x7F800000u) == 0x7F800000u) raw[k][d] &= 0xFFFFu;
+            if ((raw[k][d] & 0x7F80u) == 0x7F80u) raw[k][d] &= 0xFFFF0000u;
+          }
+          bad = true;
+        }
+        *reinterpret_cast<u32x4*>(to) = raw[k];
+      } else {
+        uint32_t piece[3][2];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          float v = __uint_as_float(raw[k][e]);
+          if ((raw[k][e] & 0x7F800000u) == 0x7F800000u) {
+            v = 0.0f;
+            bad = true;
+          }
+#pragma unroll
+          for (int q = 0; q < 3; ++q) {
+            const uint32_t top = __float_as_uint(v) & 0xFFFF0000u;
+            v -= __uint_as_float(top);
+            piece[q][e >> 1] = e & 1 ? piece[q][e >> 1] | top : top >> 16;
+          }
+        }
+#pragma unroll
+        for (int q = 0; q < kPlanes; ++q) *reinterpret_cast<u32x2*>(to + q * kPlane) = u32x2{piece[q][0], piece[q][1]};
+      }
+    }
+#pragma unroll
+    for (int f = 0; f < kRelativeFields; ++f) s_b[wave][f][lane] = (uint8_t)(buckets >> (8 * f));
+    const uint64_t any_bad = __builtin_amdgcn_ballot_w64(bad);
+    if (lane == 0) s_bad[wave] = any_bad != 0;
+    __syncthreads();
+    if (tile + gridDim.x < tiles) fetch(tile + gridDim.x);
+#pragma unroll
+    for (int ks = 0; ks < 2; ++ks) {
+      bf16x8 d[kPlanes][2];
+#pragma unroll
+      for (int q = 0; q < kPlanes; ++q)
+#pragma unroll
+        for (int ct = 0; ct < 2; ++ct) {
+          u32x4 v;
+#pragma unroll
+          for (int half = 0; half < 2; ++half) {
+            const s16x4 x = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+                (lds_s16x4*)(s_d + q * kPlane + (64 * stream + 32 * ks + 16 * half + 4 * g + (n >> 2)) * kRow + 64 * cg + 32 * ct +
+                             8 * (n & 3)));
+            const u32x2 w = __builtin_bit_cast(u32x2, x);
+            v[2 * half] = w[0];
+            v[2 * half + 1] = w[1];
+          }
+          d[q][ct] = as_bf16x8(v);
+        }
+#pragma unroll
+      for (int w = 0; w < kWindow; ++w) {
+        if (w0 + w >= a.n_tiles) continue;
+        const int f = a.tile_field[w0 + w], t = a.tile_of_field[w0 + w];
+        const uint64_t hit = __builtin_amdgcn_ballot_w64((buckets >> (8 * f + 4) & 15) == (uint32_t)t);
+        if ((uint32_t)(hit >> (32 * ks)) == 0) continue;
+        const uint32_t want = (uint32_t)(16 * t + n);
+        u32x4 hot;
+#pragma unroll
+        for (int half = 0; half < 2; ++half) {
+          const uint32_t b = *reinterpret_cast<const uint32_t*>(&s_b[wave][f][32 * ks + 16 * half + 4 * g]);
+#pragma unroll
+          for (int i = 0; i < 2; ++i)
+            hot[2 * half + i] = ((b >> (16 * i) & 255) == want ? 0x3F80u : 0u) | ((b >> (16 * i + 8) & 255) == want ? 0x3F800000u : 0u);
+        }
+#pragma unroll
+        for (int q = 0; q < kPlanes; ++q)
+#pragma unroll
+          for (int ct = 0; ct < 2; ++ct) acc[w][ct] = mfma32(as_bf16x8(hot), d[q][ct], acc[w][ct]);
+      }
+    }
+    if (s_bad[0] | s_bad[1] | s_bad[2] | s_bad[3]) {
+      for (int p = 0; p < 64; ++p) {
+        const int64_t j = this_j0 + 64 * stream + p;
+        if (j >= a.n_tok) break;
+        const uint32_t b = (uint32_t)__builtin_amdgcn_readlane((int)buckets, p);
+#pragma unroll
+        for (int ct = 0; ct < 2; ++ct) {
+          const int c = c0 + 32 * cg + 16 * ct + n;
+          const float v = c < a.c ? load_f32(dz + (this_row * a.n_tok + j) * a.c + c) : 0.0f;
+          const bool add = (__float_as_uint(v) & 0x7F800000u) == 0x7F800000u;
+          if (!__builtin_amdgcn_ballot_w64(add)) continue;
+#pragma unroll
+          for (int w = 0; w < kWindow; ++w) {
+            if (w0 + w >= a.n_tiles) continue;
+            const uint32_t of_tile = (b >> (8 * a.tile_field[w0 + w]) & 255) - 16u * a.tile_of_field[w0 + w];
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+              if (add && of_tile == (uint32_t)(4 * g + i)) acc[w][ct][i] += v;
+          }
+        }
+      }
+    }
+  }
+  const int64_t part = (int64_t)blockIdx.x * S + stream;
+#pragma unroll
+  for (int w = 0; w < kWindow; ++w) {
+    if (w0 + w >= a.n_tiles) continue;
+#pragma unroll
+    for (int ct = 0; ct < 2; ++ct) {
+      const int c = c0 + 32 * cg + 16 * ct + n;
+      if (c < a.c)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) a.parts[(part * a.n_tiles * 16 + (w0 + w) * 16 + 4 * g + i) * a.c + c] = acc[w][ct][i];
+    }
+  }
+}
+
+// A bucket and 64 channels a workgroup: four waves each add up every fourth part, in order.
 __global__ void __launch_bounds__(256) relative_sum_kernel(RelativeArgs a) {
-  const int64_t t = (int64_t)blockIdx.x * 256 + threadIdx.x, n = (int64_t)a.n_buckets * a.c;
-  if (t >= n) return;
+  __shared__ float s_sum[4][64];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, c = blockIdx.y * 64 + lane;
+  int f = 0, b = blockIdx.x, tile = 0;
+  while (b >= 2 * a.radius[f] + 2) {
+    b -= 2 * a.radius[f] + 2;
+    tile += (2 * a.radius[f] + 17) / 16;
+    ++f;
+  }
+  const int64_t rows = 16 * a.n_tiles, at = (16 * tile + b) * (int64_t)a.c + c;
   float sum = 0.0f;
-  for (int p = 0; p < a.n_parts; ++p) sum += a.parts[p * n + t];
-  a.dtable[t] = sum;
+  if (c < a.c)
+#pragma unroll 8
+    for (int p = wave; p < a.n_parts; p += 4) sum += a.parts[p * rows * a.c + at];
+  s_sum[wave][lane] = sum;
+  __syncthreads();
+  if (wave == 0 && c < a.c)
+    a.dtable[(int64_t)blockIdx.x * a.c + c] = (s_sum[0][lane] + s_sum[1][lane]) + (s_sum[2][lane] + s_sum[3][lane]);
+}
+
+bool at16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
+
+template <typename T>
+hipError_t launch_forward(const RelativeArgs& a, hipStream_t st) {
+  constexpr int kVec = 16 / sizeof(T);
+  const int64_t units = a.n_rows * ((a.n_tok + 63) / 64);
+  const dim3 grid((unsigned)((units + 3) / 4)), block(256);
+  const int pieces = a.c / kVec;
+  if (a.c % kVec || pieces > 64 || !at16(a.table) || !at16(a.z_in) || !at16(a.z_out))
+    hipLaunchKernelGGL(relative_any_kernel<T>, grid, block, 0, st, a);
+  else if (pieces > 32)
+    hipLaunchKernelGGL((relative_kernel<T, 64>), grid, block, 0, st, a);
+  else if (pieces > 16)
+    hipLaunchKernelGGL((relative_kernel<T, 32>), grid, block, 0, st, a);
+  else if (pieces > 8)
+    hipLaunchKernelGGL((relative_kernel<T, 16>), grid, block, 0, st, a);
+  else if (pieces > 4)
+    hipLaunchKernelGGL((relative_kernel<T, 8>), grid, block, 0, st, a);
+  else
+    hipLaunchKernelGGL((relative_kernel<T, 4>), grid, block, 0, st, a);
+  return hipGetLastError();
+}
+
+int channel_sets(int32_t c) { return c > 64 ? 4 : c > 32 ? 2 : 1; }
+
+template <typename T, bool VEC>
+void launch_backward(const RelativeArgs& a, hipStream_t st) {
+  const int cg = channel_sets(a.c);
+  const dim3 grid((unsigned)a.n_groups, (unsigned)((a.c + 32 * cg - 1) / (32 * cg)), (unsigned)((a.n_tiles + kWindow - 1) / kWindow));
+  if (cg == 4)
+    hipLaunchKernelGGL((relative_back_kernel<T, 4, VEC>), grid, dim3(256), 0, st, a);
+  else if (cg == 2)
+    hipLaunchKernelGGL((relative_back_kernel<T, 2, VEC>), grid, dim3(256), 0, st, a);
+  else
+    hipLaunchKernelGGL((relative_back_kernel<T, 1, VEC>), grid, dim3(256), 0, st, a);
 }
 
 }  // namespace
 
 hipError_t launch_relative(const RelativeArgs& a, bool bf16, hipStream_t st) {
-  const int64_t units = a.n_rows * ((a.n_tok + 63) / 64);
-  const dim3 grid((unsigned)((units + 3) / 4));
-  if (bf16)
-    hipLaunchKernelGGL(relative_any_kernel<uint16_t>, grid, dim3(256), 0, st, a);
-  else
-    hipLaunchKernelGGL(relative_any_kernel<float>, grid, dim3(256), 0, st, a);
-  return hipGetLastError();
+  return bf16 ? launch_forward<uint16_t>(a, st) : launch_forward<float>(a, st);
 }
 
-int relative_back_parts(int64_t n_tok, int64_t n_rows, int32_t c, int32_t n_buckets) {
-  (void)n_tok, (void)c, (void)n_buckets;
-  return (int)(n_rows < 256 ? n_rows : 256);
+void relative_back_split(RelativeArgs* a) {
+  const int cg = channel_sets(a->c), s = 4 / cg;
+  const int64_t tiles = a->n_rows * ((a->n_tok + 64 * s - 1) / (64 * s));
+  const int64_t per = (int64_t)((a->c + 32 * cg - 1) / (32 * cg)) * ((a->n_tiles + kWindow - 1) / kWindow);
+  int64_t most = 768 / per;
+  if (most < 64) most = 64;
+  const int64_t want = (tiles + 3) / 4;
+  a->n_groups = (int32_t)(want < most ? want : most);
+  a->n_parts = a->n_groups * s;
 }
 
 hipError_t launch_relative_back(const RelativeArgs& a, bool bf16, hipStream_t st) {
-  if (a.n_parts > 0) {
-    const dim3 grid((unsigned)a.n_parts, (unsigned)((a.c + 63) / 64));
+  if (a.n_groups > 0) {
+    const bool vec = at16(a.dz) && a.c % (bf16 ? 8 : 4) == 0;
     if (bf16)
-      hipLaunchKernelGGL(relative_back_any_kernel<uint16_t>, grid, dim3(64), 0, st, a);
+      vec ? launch_backward<uint16_t, true>(a, st) : launch_backward<uint16_t, false>(a, st);
     else
-      hipLaunchKernelGGL(relative_back_any_kernel<float>, grid, dim3(64), 0, st, a);
+      vec ? launch_backward<float, true>(a, st) : launch_backward<float, false>(a, st);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
   }
-  const int64_t n = (int64_t)a.n_buckets * a.c;
-  hipLaunchKernelGGL(relative_sum_kernel, dim3((unsigned)((n + 255) / 256)), dim3(256), 0, st, a);
+  hipLaunchKernelGGL(relative_sum_kernel, dim3((unsigned)a.n_buckets, (unsigned)((a.c + 63) / 64)), dim3(256), 0, st, a);
   return hipGetLastError();
 }
 

@@ -371,60 +371,73 @@ __device__ __forceinline__ void put(void* p, int64_t at, float v, bool bf16) {
     static_cast<float*>(p)[at] = v;
 }
 
-// Two units a workgroup, all channels: the splits' sums in order, dW1, dW2 and dW3, and these units'
-// shares of dgamma and dbeta.
+// One unit a workgroup: the splits' sums, dW1, dW2 and dW3, and the unit's shares of dgamma and dbeta. Threads of
+// four channels take every `ways`-th split, and their sums are added in order: 64 splits of 512 x 128 in 8 us, where
+// one thread per channel over all splits took 24.
 __global__ void __launch_bounds__(256) trans_back_finish_kernel(TransBackArgs a) {
-  __shared__ float s_g[2][kGenMaxCz], s_b[2][kGenMaxCz];
-  const int cp = (a.c + 15) & ~15, hp = (a.hidden + 15) & ~15;
+  __shared__ f32x4 s_t[3][256];
+  __shared__ float s_s[2][64];
+  const int cp = (a.c + 15) & ~15, hp = (a.hidden + 15) & ~15, u = blockIdx.x;
+  const int quads = cp / 4, ways = 256 / quads, way = threadIdx.x / quads, q = threadIdx.x - way * quads;
   const int64_t size = (int64_t)hp * cp, stride = 3 * size + 2 * hp;
-  for (int k = threadIdx.x; k < 2 * a.c; k += 256) {
-    const int which = k / a.c, c = k - which * a.c, u = blockIdx.x * 2 + which;
-    s_g[which][c] = s_b[which][c] = 0.0f;
-    if (u >= a.hidden) continue;
-    float t[3] = {0.f, 0.f, 0.f}, s1 = 0.0f, s2 = 0.0f;
-    const float* p = a.parts + (int64_t)u * cp + c;
-    const float* ps = a.parts + 3 * size + u;
-    for (int sp = 0; sp < a.splits; ++sp, p += stride, ps += stride) {
-      t[0] += p[0];
-      t[1] += p[size];
-      t[2] += p[2 * size];
-      s1 += ps[0];
-      s2 += ps[hp];
+  if (way < ways) {
+    f32x4 t[3] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
+    float s1 = 0.0f, s2 = 0.0f;
+#pragma unroll 4
+    for (int sp = way; sp < a.splits; sp += ways) {
+      const float* p = a.parts + sp * stride + (int64_t)u * cp + 4 * q;
+#pragma unroll
+      for (int m = 0; m < 3; ++m) t[m] += *reinterpret_cast<const f32x4*>(p + m * size);
+      s1 += a.parts[sp * stride + 3 * size + u];
+      s2 += a.parts[sp * stride + 3 * size + hp + u];
     }
-    if (a.unit_a) {
-      t[0] *= a.unit_b[u];
-      t[1] *= a.unit_a[u];
-      t[2] *= a.unit_a[u] * a.unit_b[u];
-      s1 *= a.unit_b[u];
-      s2 *= a.unit_a[u];
+#pragma unroll
+    for (int m = 0; m < 3; ++m) s_t[m][threadIdx.x] = t[m];
+    if (q == 0) {
+      s_s[0][way] = s1;
+      s_s[1][way] = s2;
     }
-    const float ga = a.gamma ? a.gamma[c] : 1.0f, be = a.beta ? a.beta[c] : 0.0f;
-    const int64_t at = (int64_t)u * a.c + c;
-    if (a.dw1) put(a.dw1, at, fmaf(t[0], ga, s1 * be), a.grads_bf16);
-    if (a.dw2) put(a.dw2, at, fmaf(t[1], ga, s2 * be), a.grads_bf16);
-    if (a.dw3) put(a.dw3, (int64_t)c * a.hidden + u, t[2], a.grads_bf16);
-    const float w1 = a.w1[at], w2 = a.w2[at];
-    s_g[which][c] = fmaf(w1, t[0], w2 * t[1]);
-    s_b[which][c] = fmaf(w1, s1, w2 * s2);
   }
   __syncthreads();
-  for (int c = threadIdx.x; c < a.c; c += 256) {
-    a.affine_parts[(int64_t)blockIdx.x * 2 * a.c + c] = s_g[0][c] + s_g[1][c];
-    a.affine_parts[((int64_t)blockIdx.x * 2 + 1) * a.c + c] = s_b[0][c] + s_b[1][c];
+  const int c = threadIdx.x;
+  if (c >= a.c) return;
+  float t[3] = {0.f, 0.f, 0.f}, s[2] = {0.f, 0.f};
+  for (int w = 0; w < ways; ++w) {
+#pragma unroll
+    for (int m = 0; m < 3; ++m) t[m] += reinterpret_cast<const float*>(&s_t[m][w * quads])[c];
+#pragma unroll
+    for (int m = 0; m < 2; ++m) s[m] += s_s[m][w];
   }
+  if (a.unit_a) {
+    t[0] *= a.unit_b[u];
+    t[1] *= a.unit_a[u];
+    t[2] *= a.unit_a[u] * a.unit_b[u];
+    s[0] *= a.unit_b[u];
+    s[1] *= a.unit_a[u];
+  }
+  const float ga = a.gamma ? a.gamma[c] : 1.0f, be = a.beta ? a.beta[c] : 0.0f;
+  const int64_t at = (int64_t)u * a.c + c;
+  if (a.dw1) put(a.dw1, at, fmaf(t[0], ga, s[0] * be), a.grads_bf16);
+  if (a.dw2) put(a.dw2, at, fmaf(t[1], ga, s[1] * be), a.grads_bf16);
+  if (a.dw3) put(a.dw3, (int64_t)c * a.hidden + u, t[2], a.grads_bf16);
+  const float w1 = a.w1[at], w2 = a.w2[at];
+  a.affine_parts[(int64_t)u * 2 * a.c + c] = fmaf(w1, t[0], w2 * t[1]);
+  a.affine_parts[((int64_t)u * 2 + 1) * a.c + c] = fmaf(w1, s[0], w2 * s[1]);
 }
 
+// dgamma and dbeta: 16 of the 2 c sums a workgroup, 16 threads each.
 __global__ void __launch_bounds__(256) trans_back_affine_kernel(TransBackArgs a) {
-  __shared__ float s_sum[4][64];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, k = blockIdx.x * 64 + lane;
-  const int groups = (a.hidden + 1) / 2;
+  __shared__ float s_sum[16][17];
+  const int lane = threadIdx.x & 15, way = threadIdx.x >> 4, k = blockIdx.x * 16 + lane;
   float sum = 0.0f;
   if (k < 2 * a.c)
-    for (int p = wave; p < groups; p += 4) sum += a.affine_parts[(int64_t)p * 2 * a.c + k];
-  s_sum[wave][lane] = sum;
+#pragma unroll 8
+    for (int u = way; u < a.hidden; u += 16) sum += a.affine_parts[(int64_t)u * 2 * a.c + k];
+  s_sum[way][lane] = sum;
   __syncthreads();
-  if (wave > 0 || k >= 2 * a.c) return;
-  sum = (s_sum[0][lane] + s_sum[1][lane]) + (s_sum[2][lane] + s_sum[3][lane]);
+  if (way > 0 || k >= 2 * a.c) return;
+  sum = 0.0f;
+  for (int w = 0; w < 16; ++w) sum += s_sum[w][lane];
   void* out = k < a.c ? a.dgamma : a.dbeta;
   if (out) put(out, k < a.c ? k : k - a.c, sum, a.grads_bf16);
 }
@@ -467,10 +480,10 @@ hipError_t launch_trans_back_gen(const TransBackArgs& a, hipStream_t st) {
 }
 
 hipError_t launch_trans_back_finish(const TransBackArgs& a, hipStream_t st) {
-  hipLaunchKernelGGL(trans_back_finish_kernel, dim3((unsigned)((a.hidden + 1) / 2)), dim3(256), 0, st, a);
+  hipLaunchKernelGGL(trans_back_finish_kernel, dim3((unsigned)a.hidden), dim3(256), 0, st, a);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess || (!a.dgamma && !a.dbeta)) return e;
-  hipLaunchKernelGGL(trans_back_affine_kernel, dim3((unsigned)((2 * a.c + 63) / 64)), dim3(256), 0, st, a);
+  hipLaunchKernelGGL(trans_back_affine_kernel, dim3((unsigned)((2 * a.c + 15) / 16)), dim3(256), 0, st, a);
   return hipGetLastError();
 }
 
