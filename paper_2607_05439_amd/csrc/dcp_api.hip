@@ -1730,7 +1730,7 @@ int dcp_pair_transition_backward(int64_t n_pairs, int32_t c_z, int32_t hidden, i
   a.zh = ws + L.off_zh;
   hipStream_t st = static_cast<hipStream_t>(stream);
   hipError_t e;
-  if (fast && n_pairs > 0) dcp::trans_back_fast_units(a.prep, &a.unit_a, &a.unit_b);
+  if (fast && n_pairs > 0) dcp::trans_back_fast_units(a.prep, &a.unit_exponents, &a.dout_exponent);
   if (n_pairs > 0 && (e = fast ? dcp::launch_trans_back_fast(a, st) : dcp::launch_trans_back_gen(a, st)) != hipSuccess)
     return fail(DCP_ERR_HIP, "transition backward launch failed: %s", hipGetErrorString(e));
   if (sums && (e = dcp::launch_trans_back_finish(a, st)) != hipSuccess)

@@ -405,9 +405,11 @@ struct TransBackArgs {
   int32_t splits;            // shares of the pairs that are summed on their own
   float* prep;               // weights as operands
   float* parts;              // [splits]: T1, T2, T3 [hp][cp], S1, S2 [hp] (hidden and c filled up to 16)
-  const float *unit_a, *unit_b;  // [hidden]: T2 and S2 times unit_a, T1 and S1 times unit_b, T3 times both; null: 1
+  // Powers of two in the parts, or null: with e1, e2, e3 [hidden] and the exponent of dout d, T1 and S1 carry
+  // 2^(e2 + e3 + d), T2 and S2 2^(e1 + e3 + d), T3 2^(e1 + e2 + d)
+  const int *unit_exponents, *dout_exponent;
   float* affine_parts;       // [hidden][2][c]
-  char* zh;                  // bf16: 512 B a pair, and set by the launcher: whether dz's kernel writes them,
+  char* zh;                  // bf16: zh and dout, 512 B a pair; set by the launcher: whether dz's kernel writes them,
   int32_t store_zh, add_parts;  // whether the sums are added to the parts
 };
 
@@ -480,7 +482,7 @@ hipError_t launch_back_finish(const BackFinishArgs& a, hipStream_t st);
 int trans_back_gen_splits(int64_t n_pairs, int32_t c, int32_t hidden);
 hipError_t launch_trans_back_gen(const TransBackArgs& a, hipStream_t st);
 size_t trans_back_fast_prep_bytes();
-void trans_back_fast_units(const float* prep, const float** unit_a, const float** unit_b);
+void trans_back_fast_units(const float* prep, const int** unit_exponents, const int** dout_exponent);
 int trans_back_fast_splits(int64_t n_pairs);
 size_t trans_back_fast_zh_bytes(int64_t n_pairs);
 hipError_t launch_trans_back_fast(const TransBackArgs& a, hipStream_t st);

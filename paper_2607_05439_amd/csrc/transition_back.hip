@@ -7,13 +7,15 @@
 //   trans_back_pairs_fast_kernel  dz; the products are transposed (units by pairs)
 //   trans_back_sums_fast_kernel   T1 = sum dA zh^T, T2 = sum dB zh^T, T3 = sum H dout^T, S1, S2
 //
-// Operands. gamma is folded into the weights (W1 diag(gamma), W2 diag(gamma)) and W1 beta, W2 beta into
-// the first value of the accumulators, so zh, of at most sqrt(128), is all that is formed of z. zh and
-// the rows of W1 and W2 enter as fp16, 11 bits, each row times a power of two of its own; A and B are
-// then as exact as the results' roundings to bf16 need. dout is bf16 as given; W3, dA, dB, H, the
-// transposed weights and zh (where it meets dA and dB) are rounded to bf16, whose range leaves gradients of any size alone.
-// A row's powers of two stay in A and B and are taken out by the transposed weights and, from T and S,
-// at the end: exact.
+// Operands are fp16 (11 bits), with powers of two that keep them in its range, so that a result's error is little more
+// than its own rounding to bf16. gamma is folded into the weights (W1 diag(gamma), W2 diag(gamma)), and W1 beta, W2 beta
+// into the first value of the accumulators, so zh, of at most sqrt(128), is all that is formed of z.
+//   A unit's rows of W1 diag(gamma), W2 diag(gamma) and W3^T have powers of two 2^e1, 2^e2, 2^e3 that bring their
+//   largest magnitudes (and 1/16 of the biases) below 1: then |A'|, |B'| <= 144, |dH'| <= 128 for |dout'| <= 1, and
+//   dA', dB', H' stay under 2^15 whatever the weights are.
+//   dout has a power of two per pair where dz is formed, and one for all pairs where their products are summed.
+//   A unit's row in the transposed weights carries 2^-(e1 + e2 + e3), relative to the largest of all units.
+// All are taken out of the sums at the end, exactly.
 #include <hip/hip_runtime.h>
 #include <math.h>
 #include <stdint.h>
@@ -26,109 +28,165 @@ namespace dcp {
 namespace {
 
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+typedef _Float16 f16x4 __attribute__((ext_vector_type(4)));
 
 constexpr int kCz = kTransCz;       // 128
 constexpr int kHid = kTransHidden;  // 512
-constexpr int kHp = kHid / 32;      // pairs of hidden tiles
-constexpr int kPairBytes = 40 * 1024;  // operands of 32 units
+constexpr int kChunks = kHid / 32;  // of 32 units, two tiles of 16
+constexpr int kRowBytes = 24 * 1024, kTrBytes = 16 * 1024;  // a chunk's operands: rows, transposes
 constexpr float kLog2e = 1.44269504088896340736f;
 
-__device__ __forceinline__ f32x4 mfma_f16(f16x8 a, f16x8 b, f32x4 c) {
-  return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0);
-}
+__device__ __forceinline__ f32x4 mfma(f16x8 a, f16x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
 __device__ __forceinline__ f16x8 as_f16x8(u32x4 u) { return __builtin_bit_cast(f16x8, u); }
 __device__ __forceinline__ float lo_bf16(uint32_t w) { return __uint_as_float(w << 16); }
 __device__ __forceinline__ float hi_bf16(uint32_t w) { return __uint_as_float(w & 0xFFFF0000u); }
+__device__ __forceinline__ float bf16_of(u32x4 v, int i) { return i & 1 ? hi_bf16(v[i >> 1]) : lo_bf16(v[i >> 1]); }
 
 // Channel at accumulator row r of output tile ct (of 16 channels), so that lane group g of tiles 2 ks and
 // 2 ks + 1 holds channels 32 ks + 8 g .. + 7, those that it loads of a row.
 __host__ __device__ inline int out_channel(int ct, int r) { return 32 * (ct >> 1) + 8 * (r >> 2) + 4 * (ct & 1) + (r & 3); }
 
-// 2^-k for a row whose largest magnitude is in [2^(k-1), 2^k): from there to [1/2, 1)
-__device__ __forceinline__ float row_scale(float top) {
-  if (top == 0.0f) return 1.0f;
-  int e;
-  (void)frexpf(top, &e);
-  return ldexpf(1.0f, max(min(-e, 126), -126));
+// e for which top 2^e is in [1/2, 1); 0 for 0
+__device__ __forceinline__ int exponent_below_one(float top) {
+  int e = 0;
+  if (top > 0.0f) (void)frexpf(top, &e);
+  return -e;
 }
 
 // ----------------------------------------------------------------------------- weights
-// Operands of 32 units (40 KB): for each of their two tiles and each k-step ks the rows of W1 diag(gamma) and
-// W2 diag(gamma) (fp16) and of W3^T (bf16), [tile][ks][matrix][lane] 16 B (row = unit, k-slots = channels
-// 32 ks + 8 (lane / 16) .. + 7); then [ct][W1 | W2][lane] 16 B of their transposes (bf16; row = channel
-// out_channel(ct, lane % 16), k-slot j of lane group g = unit 4g + j of the first tile for j < 4, of the second for
-// j >= 4). After all operands, per unit, [kUnit*][512] fp32.
-enum { kUnitLog = 0, kUnitA = 1, kUnitBiasA = 2, kUnitBiasB = 3, kUnitB = 4, kUnitArrays = 5 };
-constexpr size_t kPrepBytes = (size_t)kHp * kPairBytes + kUnitArrays * kHid * sizeof(float);
+// In the workspace: rows of every chunk, [tile][ks][W1 | W2 | W3^T][lane] 16 B (row = unit, k-slots = channels
+// 32 ks + 8 (lane / 16) .. + 7); transposes of every chunk, [ct][W1 | W2][lane] 16 B (row = channel
+// out_channel(ct, lane % 16), k-slot j of lane group g = unit 4g + j of the first tile for j < 4, of the second for j >= 4);
+// then per unit, [kUnit*][512]; then the shares' largest |dout| and two exponents.
+enum { kUnitLog = 0, kUnitA = 1, kUnitBiasA = 2, kUnitBiasB = 3, kUnitE1 = 4, kUnitE2 = 5, kUnitE3 = 6, kUnitArrays = 7 };
+constexpr int kTops = 1024;
+constexpr size_t kRowsAt = 0, kTrAt = kRowsAt + (size_t)kChunks * kRowBytes, kUnitsAt = kTrAt + (size_t)kChunks * kTrBytes;
+constexpr size_t kTopsAt = kUnitsAt + kUnitArrays * kHid * 4, kExpAt = kTopsAt + kTops * 4, kPrepBytes = kExpAt + 16;
 
-// One workgroup per tile of 16 units; thread (n, q) holds channels 8 q .. + 7 of unit n.
-__global__ void __launch_bounds__(256) trans_back_prep_fast_kernel(TransBackArgs a) {
-  __shared__ float s_top[2][16][17], s_bias[2][16][17];
-  __shared__ float s_w[2][16][kCz + 4];
-  const int tid = threadIdx.x, n = tid & 15, q = tid >> 4, tile = blockIdx.x, unit = 16 * tile + n;
-  char* const base = reinterpret_cast<char*>(a.prep) + (size_t)(tile >> 1) * kPairBytes;
-  float* const units = reinterpret_cast<float*>(reinterpret_cast<char*>(a.prep) + (size_t)kHp * kPairBytes);
-  float w[2][8], top[2] = {0.f, 0.f}, bias[2] = {0.f, 0.f};
-  bf16x8 w3;
+template <typename T>
+__device__ __forceinline__ T* prep_at(const TransBackArgs& a, size_t at) {
+  return reinterpret_cast<T*>(reinterpret_cast<char*>(a.prep) + at);
+}
+__device__ __forceinline__ int& max_unit_exponent(const TransBackArgs& a) { return prep_at<int>(a, kExpAt)[0]; }
+__device__ __forceinline__ int& dout_exponent(const TransBackArgs& a) { return prep_at<int>(a, kExpAt)[1]; }
+
+// Workgroups 0..31: rows of a tile of 16 units, thread (n, q) channels 8 q .. + 7 of unit n. The others: the largest
+// finite |dout| of a share each.
+__global__ void __launch_bounds__(256) trans_back_rows_prep_kernel(TransBackArgs a) {
+  __shared__ float s_top[3][16][17], s_bias[2][16][17];
+  const int tid = threadIdx.x;
+  if (blockIdx.x >= kHid / 16) {
+    const int64_t n = a.n_pairs * (kCz / 8), stride = (int64_t)(gridDim.x - kHid / 16) * 256;
+    const u32x4* d = static_cast<const u32x4*>(a.dout);
+    uint32_t top = 0;  // of |dout|'s bits: finite ones are below 0x7F800000
+    for (int64_t i = (int64_t)(blockIdx.x - kHid / 16) * 256 + tid; i < n; i += 8 * stride) {
+      u32x4 v[8];
+#pragma unroll
+      for (int k = 0; k < 8; ++k) v[k] = d[min(i + k * stride, n - 1)];
+#pragma unroll
+      for (int k = 0; k < 8; ++k)
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+          const uint32_t lo = (v[k][w] << 16) & 0x7FFFFFFFu, hi = v[k][w] & 0x7FFF0000u;
+          top = max(top, lo < 0x7F800000u ? lo : 0u);
+          top = max(top, hi < 0x7F800000u ? hi : 0u);
+        }
+    }
+    for (int m = 32; m > 0; m >>= 1) top = max(top, (uint32_t)__shfl_xor((int)top, m));
+    __shared__ uint32_t s_max[4];
+    if ((tid & 63) == 0) s_max[tid >> 6] = top;
+    __syncthreads();
+    if (tid == 0) prep_at<uint32_t>(a, kTopsAt)[blockIdx.x - kHid / 16] = max(max(s_max[0], s_max[1]), max(s_max[2], s_max[3]));
+    return;
+  }
+  const int n = tid & 15, q = tid >> 4, tile = blockIdx.x, unit = 16 * tile + n;
+  float w[3][8], top[3] = {0.f, 0.f, 0.f}, bias[2] = {0.f, 0.f};
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
     const int c = 8 * q + i;
     const float ga = a.gamma ? a.gamma[c] : 1.0f, be = a.beta ? a.beta[c] : 0.0f;
     w[0][i] = a.w1[unit * kCz + c];
     w[1][i] = a.w2[unit * kCz + c];
-    w3[i] = (__bf16)a.w3[c * kHid + unit];
+    w[2][i] = a.w3[c * kHid + unit];
 #pragma unroll
     for (int m = 0; m < 2; ++m) {
       bias[m] = fmaf(w[m][i], be, bias[m]);
       w[m][i] *= ga;
-      top[m] = fmaxf(top[m], finite_abs(w[m][i]));
     }
+#pragma unroll
+    for (int m = 0; m < 3; ++m) top[m] = fmaxf(top[m], finite_abs(w[m][i]));
   }
 #pragma unroll
-  for (int m = 0; m < 2; ++m) {
-    s_top[m][n][q] = top[m];
-    s_bias[m][n][q] = bias[m];
-  }
+  for (int m = 0; m < 3; ++m) s_top[m][n][q] = top[m];
+#pragma unroll
+  for (int m = 0; m < 2; ++m) s_bias[m][n][q] = bias[m];
   __syncthreads();
-  float scale[2];
+  int e[3];
 #pragma unroll
-  for (int m = 0; m < 2; ++m) {
+  for (int m = 0; m < 3; ++m) {
     for (int k = 0; k < 16; ++k) top[m] = fmaxf(top[m], s_top[m][n][k]);
-    scale[m] = row_scale(top[m]);
-  }
-  const int ks = q >> 2, lane = n + 16 * (q & 3);
-  u32x4* const rows = reinterpret_cast<u32x4*>(base + (size_t)((tile & 1) * 4 + ks) * 3 * 1024) + lane;
-#pragma unroll
-  for (int m = 0; m < 2; ++m) {
-    f16x8 v;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      v[i] = (_Float16)(w[m][i] * scale[m]);
-      s_w[m][n][8 * q + i] = w[m][i] / scale[1 - m];
-    }
-    rows[m * 64] = __builtin_bit_cast(u32x4, v);
-  }
-  rows[2 * 64] = __builtin_bit_cast(u32x4, w3);
-  if (q == 0) {
-#pragma unroll
-    for (int m = 0; m < 2; ++m) {
+    if (m < 2) {
       bias[m] = 0.0f;
       for (int k = 0; k < 16; ++k) bias[m] += s_bias[m][n][k];
+      top[m] = fmaxf(top[m], finite_abs(bias[m]) * 0.0625f);
     }
-    units[kUnitLog * kHid + unit] = -kLog2e / scale[0];
-    units[kUnitA * kHid + unit] = 1.0f / scale[0];
-    units[kUnitB * kHid + unit] = 1.0f / scale[1];
-    units[kUnitBiasA * kHid + unit] = bias[0] * scale[0];
-    units[kUnitBiasB * kHid + unit] = bias[1] * scale[1];
+    e[m] = exponent_below_one(top[m]);
   }
-  __syncthreads();
-  // transposes: dA carries W2's power of two and dB W1's, which s_w has been divided by
-  for (int k = tid; k < 2 * 8 * 64; k += 256) {
-    const int m = k >> 9, ct = (k >> 6) & 7, l = k & 63, c = out_channel(ct, l & 15), u = 4 * (l >> 4);
-    bf16x4 v;
+  u32x4* const rows = prep_at<u32x4>(a, kRowsAt + (size_t)(tile >> 1) * kRowBytes + (size_t)((tile & 1) * 4 + (q >> 2)) * 3 * 1024) + n + 16 * (q & 3);
 #pragma unroll
-    for (int j = 0; j < 4; ++j) v[j] = (__bf16)s_w[m][u + j][c];
-    *reinterpret_cast<u32x2*>(base + 24 * 1024 + (ct * 2 + m) * 1024 + l * 16 + (tile & 1) * 8) = __builtin_bit_cast(u32x2, v);
+  for (int m = 0; m < 3; ++m) {
+    f16x8 v;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = (_Float16)ldexpf(w[m][i], e[m]);
+    rows[m * 64] = __builtin_bit_cast(u32x4, v);
+  }
+  if (q > 0) return;
+  float* const units = prep_at<float>(a, kUnitsAt) + unit;
+  units[kUnitLog * kHid] = ldexpf(-kLog2e, -e[0]);
+  units[kUnitA * kHid] = ldexpf(1.0f, -e[0]);
+  units[kUnitBiasA * kHid] = ldexpf(bias[0], e[0]);
+  units[kUnitBiasB * kHid] = ldexpf(bias[1], e[1]);
+#pragma unroll
+  for (int m = 0; m < 3; ++m) reinterpret_cast<int*>(units)[(kUnitE1 + m) * kHid] = e[m];
+}
+
+// The transposes of a chunk's rows from their fragments: a workgroup a chunk; the first also the exponent of dout.
+__global__ void __launch_bounds__(256) trans_back_transpose_kernel(TransBackArgs a, int n_tops) {
+  __shared__ int s_max[256];
+  __shared__ uint32_t s_top[256];
+  const int tid = threadIdx.x;
+  const int* const e = prep_at<int>(a, kUnitsAt) + kUnitE1 * kHid;
+  auto unit_exponent = [&](int u) { return -(e[u] + e[kHid + u] + e[2 * kHid + u]); };
+  s_max[tid] = max(unit_exponent(tid), unit_exponent(tid + 256));
+  uint32_t top = 0;
+  if (blockIdx.x == 0)
+    for (int k = tid; k < n_tops; k += 256) top = max(top, prep_at<uint32_t>(a, kTopsAt)[k]);
+  s_top[tid] = top;
+  __syncthreads();
+  for (int m = 128; m > 0; m >>= 1) {
+    if (tid < m) {
+      s_max[tid] = max(s_max[tid], s_max[tid + m]);
+      s_top[tid] = max(s_top[tid], s_top[tid + m]);
+    }
+    __syncthreads();
+  }
+  const int most = s_max[0];
+  if (blockIdx.x == 0 && tid == 0) {
+    max_unit_exponent(a) = most;
+    dout_exponent(a) = max(min(exponent_below_one(__uint_as_float(s_top[0])), 126), -126);
+  }
+  const _Float16* const rows = prep_at<_Float16>(a, kRowsAt + (size_t)blockIdx.x * kRowBytes);
+  u32x4* const to = prep_at<u32x4>(a, kTrAt + (size_t)blockIdx.x * kTrBytes);
+  for (int k = tid; k < 8 * 2 * 64; k += 256) {
+    const int ct = k >> 7, m = (k >> 6) & 1, l = k & 63, c = out_channel(ct, l & 15);
+    f16x8 v;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const int n = 4 * (l >> 4) + (j & 3), tile = j >> 2, lane = n + 16 * ((c >> 3) & 3);
+      const float w = (float)rows[((((tile * 4 + (c >> 5)) * 3 + m) * 64) + lane) * 8 + (c & 7)];
+      v[j] = (_Float16)ldexpf(w, unit_exponent(32 * blockIdx.x + 16 * tile + n) - most);
+    }
+    to[k] = __builtin_bit_cast(u32x4, v);
   }
 }
 
@@ -143,6 +201,7 @@ __device__ __forceinline__ Gated gated(float h0, float h1, float dh, float k, fl
   return {silu * h1, dh * h1 * fmaf(silu, fmaf(-k, s, k), s), dh * silu};
 }
 
+// ----------------------------------------------------------------------------- rows
 // Eight codes (two words) with one power of two, as bf16: exact.
 __device__ __forceinline__ u32x4 decode8(u32x2 q, float scale) {
   bf16x8 v;
@@ -150,11 +209,9 @@ __device__ __forceinline__ u32x4 decode8(u32x2 q, float scale) {
   for (int i = 0; i < 8; ++i) v[i] = (__bf16)((float)(int8_t)(q[i >> 2] >> (8 * (i & 3))) * scale);
   return __builtin_bit_cast(u32x4, v);
 }
-
-// ----------------------------------------------------------------------------- rows
 // A lane (pair n of a tile of 16, group g) holds channels 32 ks + 8g .. + 7 of a row, ks = 0..3.
 template <bool CODES>
-__device__ __forceinline__ void load_row(const TransBackArgs& a, int64_t pair, int g, u32x4 (&z)[4]) {
+__device__ __forceinline__ void load_z(const TransBackArgs& a, int64_t pair, int g, u32x4 (&z)[4]) {
   if (CODES) {
     const int8_t* q = static_cast<const int8_t*>(a.z) + pair * kCz + 8 * g;
     const uint32_t e = *reinterpret_cast<const uint32_t*>(a.exponents + pair * 4);
@@ -167,14 +224,18 @@ __device__ __forceinline__ void load_row(const TransBackArgs& a, int64_t pair, i
     for (int ks = 0; ks < 4; ++ks) z[ks] = *reinterpret_cast<const u32x4*>(q + 32 * ks);
   }
 }
-// zh in fp16 and bf16, and the statistics.
-__device__ __forceinline__ void normalise(const u32x4 (&z)[4], float eps, f16x8 (&zf)[4], bf16x8 (&zb)[4], float& mu, float& rstd) {
+__device__ __forceinline__ void load_dout(const TransBackArgs& a, int64_t pair, int g, u32x4 (&d)[4]) {
+  const uint16_t* q = static_cast<const uint16_t*>(a.dout) + pair * kCz + 8 * g;
+#pragma unroll
+  for (int ks = 0; ks < 4; ++ks) d[ks] = *reinterpret_cast<const u32x4*>(q + 32 * ks);
+}
+__device__ __forceinline__ void normalise(const u32x4 (&z)[4], float eps, f16x8 (&zf)[4], float& mu, float& rstd) {
   float x[4][8], s = 0.0f, v = 0.0f;
 #pragma unroll
   for (int ks = 0; ks < 4; ++ks)
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-      x[ks][i] = i & 1 ? hi_bf16(z[ks][i >> 1]) : lo_bf16(z[ks][i >> 1]);
+      x[ks][i] = bf16_of(z[ks], i);
       s += x[ks][i];
     }
   mu = sum4(s) * (1.0f / kCz);
@@ -190,196 +251,226 @@ __device__ __forceinline__ void normalise(const u32x4 (&z)[4], float eps, f16x8 
   for (int ks = 0; ks < 4; ++ks)
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-      const float zh = x[ks][i] * rstd;
+      // rounded to fp32 first in every kernel: the compiler would fold some of these into one rounding
+      float zh = x[ks][i] * rstd;
+      asm("" : "+v"(zh));
       zf[ks][i] = (_Float16)zh;
-      zb[ks][i] = (__bf16)zh;
     }
 }
-// zh of a tile of 16 pairs for the sums, 8 KB: [ks][lane] 16 B in fp16, as A operands; then the same in bf16, with
-// the pairs of odd groups 8 places on, which spreads the LDS reads of columns over all banks.
+__device__ __forceinline__ f16x8 scaled(u32x4 d, float scale) {
+  f16x8 v;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) v[i] = (_Float16)(bf16_of(d, i) * scale);
+  return v;
+}
+__device__ __forceinline__ float power(int e) { return ldexpf(1.0f, e); }
+
+// What the sums read of a tile of 16 pairs, 8 KB: [zh | dout][ks][lane] 16 B in fp16, with the pairs of odd groups 8
+// places on, which spreads the LDS reads of columns over all banks. Pairs past the last hold a dout of 0.
 __device__ __forceinline__ int column_lane(int n, int g) { return 16 * g + (n ^ (8 * (g & 1))); }
-__device__ __forceinline__ void store_zh(const TransBackArgs& a, int64_t tile, int n, int g, const f16x8 (&zf)[4], const bf16x8 (&zb)[4]) {
-  u32x4* const to = reinterpret_cast<u32x4*>(a.zh) + tile * 512;
+__device__ __forceinline__ void store_rows(const TransBackArgs& a, int64_t tile, int n, int g, const f16x8 (&zf)[4], const u32x4 (&d)[4],
+                                           float scale) {
+  u32x4* const to = reinterpret_cast<u32x4*>(a.zh) + tile * 512 + column_lane(n, g);
+  const bool there = tile * 16 + n < a.n_pairs;
 #pragma unroll
   for (int ks = 0; ks < 4; ++ks) {
-    to[ks * 64 + 16 * g + n] = __builtin_bit_cast(u32x4, zf[ks]);
-    to[256 + ks * 64 + column_lane(n, g)] = __builtin_bit_cast(u32x4, zb[ks]);
+    to[ks * 64] = __builtin_bit_cast(u32x4, zf[ks]);
+    to[256 + ks * 64] = there ? __builtin_bit_cast(u32x4, scaled(d[ks], scale)) : u32x4{0u, 0u, 0u, 0u};
   }
 }
 
-// zh alone, where dz is not wanted or takes dout's place (the sums, which need zh, then come before it). One tile a wave.
+// These alone, where dz is not wanted or takes dout's place (the sums then come before it). One tile a wave.
 template <bool CODES>
 __global__ void __launch_bounds__(256) trans_back_rows_kernel(TransBackArgs a) {
   const int lane = threadIdx.x & 63, n = lane & 15, g = lane >> 4;
-  const int64_t tile = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
-  u32x4 z[4];
-  load_row<CODES>(a, min(tile * 16 + n, a.n_pairs - 1), g, z);
+  const int64_t tile = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6), pair = min(tile * 16 + n, a.n_pairs - 1);
+  u32x4 z[4], d[4];
+  load_z<CODES>(a, pair, g, z);
+  load_dout(a, pair, g, d);
   f16x8 zf[4];
-  bf16x8 zb[4];
   float mu, rstd;
-  normalise(z, a.eps, zf, zb, mu, rstd);
-  store_zh(a, tile, n, g, zf, zb);
+  normalise(z, a.eps, zf, mu, rstd);
+  store_rows(a, tile, n, g, zf, d, power(dout_exponent(a)));
 }
 
 // ----------------------------------------------------------------------------- dz
-// A workgroup of 8 waves takes groups of 256 pairs, 32 a wave (two tiles of 16), persistently. zh (fp16) and dout
-// (bf16) are B operands in registers: lane (pair n, group g) holds channels 32 ks + 8g .. + 7. For every 32 units: A', B'
-// and dH (units by pairs), dA' and dB' in registers, which are the B operands of the products with the
-// transposed weights; their sum is gamma dN, at the channels that the lane holds of z and dout. The weights stream
-// through two 40 KB LDS buffers by direct-to-LDS loads one chunk ahead; z waits in LDS for the end.
-constexpr int kWaves = 8;
-constexpr int kGroupPairs = 32 * kWaves;
-constexpr int kDmaPerWave = kPairBytes / 1024 / kWaves;
-
-template <bool CODES>
-__global__ void __launch_bounds__(64 * kWaves) trans_back_pairs_fast_kernel(TransBackArgs a) {
-  __shared__ __attribute__((aligned(16))) char s_w[2][kPairBytes];
-  __shared__ __attribute__((aligned(16))) u32x4 s_z[kWaves][8][64];
-  __shared__ __attribute__((aligned(16))) float s_u[4][kHid];  // kUnitLog, kUnitA, kUnitBiasA, kUnitBiasB
+// A workgroup takes groups of 64 TILES pairs, persistently: four waves form A', B' and dH' (units by pairs) of TILES tiles
+// of 16 pairs each and, from them, dA' and dB', which are the B operands of the products with the transposed weights;
+// those four other waves form, a chunk of 32 units later, and at a group's end dz. So every weight fragment is read from
+// LDS once for TILES tiles of pairs, and on every SIMD the vector work of one wave lies beside the products of another:
+// with each wave doing all of it for two tiles, the LDS reads alone took as long as the products (1024 tokens: 880 us).
+// The weights stream through LDS by direct-to-LDS loads, the rows one chunk ahead.
+template <bool CODES, int TILES>
+__global__ void __launch_bounds__(512, 2) trans_back_pairs_fast_kernel(TransBackArgs a) {
+  constexpr int kGroup = 64 * TILES;
+  __shared__ __attribute__((aligned(16))) char s_rows[2][kRowBytes];
+  __shared__ __attribute__((aligned(16))) char s_tr[2][kTrBytes];
+  __shared__ __attribute__((aligned(16))) u32x4 s_op[2][4][2][TILES][64];  // [chunk parity][wave][dA' | dB'][tile][lane]
+  __shared__ __attribute__((aligned(16))) float s_u[4][kHid];              // kUnitLog, kUnitA, kUnitBiasA, kUnitBiasB
+  __shared__ float s_stat[2][3][kGroup];                                   // [group parity]: mean, rstd, dout's exponent
   const int tid = threadIdx.x, lane = tid & 63, n = lane & 15, g = lane >> 4;
-  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int64_t n_groups = (a.n_pairs + kGroupPairs - 1) / kGroupPairs;
-  const __amdgpu_buffer_rsrc_t wres = __builtin_amdgcn_make_buffer_rsrc(a.prep, 0, kHp * kPairBytes, kRawBufferFlags);
-  auto chunk_dma = [&](int c, int b) {
-    const uint32_t base = lds_addr(&s_w[b][0]) + (uint32_t)(wave * kDmaPerWave * 1024);
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), share = wave & 3;
+  const int64_t n_groups = (a.n_pairs + kGroup - 1) / kGroup;
+  const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
+  for (int k = tid; k < 4 * kHid; k += 512) (&s_u[0][0])[k] = prep_at<float>(a, kUnitsAt)[k];
+  if (wave < 4) {
+    int parity = 0;
+    const float to_all = power(dout_exponent(a));
+    for (int64_t grp = blockIdx.x; grp < n_groups; grp += gridDim.x, parity ^= 1) {
+      barrier_lds();
+      f16x8 nv[TILES][4], dv[TILES][4];
+      {
+        u32x4 z[TILES][4], d[TILES][4];
 #pragma unroll
-    for (int i = 0; i < kDmaPerWave; ++i)
-      dma_b128(wres, c * kPairBytes + (wave * kDmaPerWave + i) * 1024 + lane * 16, base + (uint32_t)(i * 1024));
-  };
-  {
-    const float* units = reinterpret_cast<const float*>(reinterpret_cast<const char*>(a.prep) + (size_t)kHp * kPairBytes);
-    for (int k = tid; k < 4 * kHid; k += 64 * kWaves) (&s_u[0][0])[k] = units[k];
-  }
-  int64_t grp = blockIdx.x;
-  int seq = 0;
-  chunk_dma(0, 0);
-  for (; grp < n_groups; grp += gridDim.x) {
-    const bool last_group = grp + gridDim.x >= n_groups;
-    const int64_t pair0 = grp * kGroupPairs + wave * 32;
-    u32x4 dv[2][4];
-    f16x8 nv[2][4];
-    float mu[2], rstd[2];
-    {
-      u32x4 zz[2][4];
+        for (int p = 0; p < TILES; ++p) {
+          const int64_t pair = min(grp * kGroup + (share * TILES + p) * 16 + n, a.n_pairs - 1);
+          load_z<CODES>(a, pair, g, z[p]);
+          load_dout(a, pair, g, d[p]);
+        }
 #pragma unroll
-      for (int p = 0; p < 2; ++p) {
-        const int64_t pr = min(pair0 + 16 * p + n, a.n_pairs - 1);  // pairs past the end are not stored
-        load_row<CODES>(a, pr, g, zz[p]);
-        const uint16_t* d = static_cast<const uint16_t*>(a.dout) + pr * kCz + 8 * g;
+        for (int p = 0; p < TILES; ++p) {
+          float mu, rstd, top = 0.0f;
+          normalise(z[p], a.eps, nv[p], mu, rstd);
+          if (a.store_zh) store_rows(a, grp * (4 * TILES) + share * TILES + p, n, g, nv[p], d[p], to_all);
 #pragma unroll
-        for (int ks = 0; ks < 4; ++ks) dv[p][ks] = *reinterpret_cast<const u32x4*>(d + 32 * ks);
-      }
+          for (int ks = 0; ks < 4; ++ks)
 #pragma unroll
-      for (int p = 0; p < 2; ++p) {
-        bf16x8 zb[4];
-        normalise(zz[p], a.eps, nv[p], zb, mu[p], rstd[p]);
-        if (a.store_zh) store_zh(a, pair0 / 16 + p, n, g, nv[p], zb);
+            for (int i = 0; i < 8; ++i) top = fmaxf(top, finite_abs(bf16_of(d[p][ks], i)));
+          const int e = max(min(exponent_below_one(max4(top)), 126), -126);
+          const float scale = power(e);
 #pragma unroll
-        for (int ks = 0; ks < 4; ++ks) s_z[wave][4 * p + ks][lane] = zz[p][ks];
-      }
-    }
-    f32x4 acc[8][2];
-#pragma unroll
-    for (int ct = 0; ct < 8; ++ct) acc[ct][0] = acc[ct][1] = f32x4{0.f, 0.f, 0.f, 0.f};
-    f32x4 h[3][2][2];  // A', B', dH [tile][pair tile]
-    bf16x8 da[2], db[2];
-    for (int c = 0; c < kHp; ++c) {
-      const int b = seq & 1;
-      barrier_lds();  // every wave is done with buffer b ^ 1
-      const bool more = c + 1 < kHp || !last_group;
-      if (more) {
-        chunk_dma((c + 1) % kHp, b ^ 1);
-        wait_vm<kDmaPerWave>();  // this wave's loads of chunk c have landed
-      } else {
-        wait_vm<0>();
-      }
-      barrier_lds();  // and every other wave's
-      const char* chunk = s_w[b];
-      constexpr int kFrags = 40, kAhead = 4;
-      auto frag = [&](int f) { return *reinterpret_cast<const u32x4*>(chunk + f * 1024 + lane * 16); };
-      u32x4 wq[kAhead];
-#pragma unroll
-      for (int f = 0; f < kAhead; ++f) wq[f] = frag(f);
-#pragma unroll
-      for (int tt = 0; tt < 2; ++tt) {
-        const int u = 32 * c + 16 * tt + 4 * g;
-        const f32x4 ba = *reinterpret_cast<const f32x4*>(&s_u[kUnitBiasA][u]), bb = *reinterpret_cast<const f32x4*>(&s_u[kUnitBiasB][u]);
-#pragma unroll
-        for (int p = 0; p < 2; ++p) {
-          h[0][tt][p] = ba;
-          h[1][tt][p] = bb;
-          h[2][tt][p] = f32x4{0.f, 0.f, 0.f, 0.f};
+          for (int ks = 0; ks < 4; ++ks) dv[p][ks] = scaled(d[p][ks], scale);
+          if (g == 0) {
+            const int at = (share * TILES + p) * 16 + n;
+            s_stat[parity][0][at] = mu;
+            s_stat[parity][1][at] = rstd;
+            s_stat[parity][2][at] = __int_as_float(e);
+          }
         }
       }
+#pragma unroll 1
+      for (int c = 0; c < kChunks; ++c) {
+        barrier_lds();
+        const char* const chunk = s_rows[c & 1] + lane * 16;
+        constexpr int kFrags = 24, kAhead = 4;
+        auto frag = [&](int f) { return *reinterpret_cast<const u32x4*>(chunk + f * 1024); };
+        u32x4 wq[kAhead];
 #pragma unroll
-      for (int f = 0; f < kFrags; ++f) {
-        const u32x4 w = wq[f % kAhead];
-        if (f + kAhead < kFrags) wq[f % kAhead] = frag(f + kAhead);
-        if (f < 24) {
-          const int tt = f / 12, ks = f / 3 % 4, m = f % 3;
+        for (int f = 0; f < kAhead; ++f) wq[f] = frag(f);
+        f32x4 h[3][TILES];
 #pragma unroll
-          for (int p = 0; p < 2; ++p)
-            h[m][tt][p] = m < 2 ? mfma_f16(as_f16x8(w), nv[p][ks], h[m][tt][p])
-                                : mfma32(as_bf16x8(w), as_bf16x8(dv[p][ks]), h[m][tt][p]);
-        } else {
-          if (f == 24) {
+        for (int f = 0; f < kFrags; ++f) {
+          const int tt = f / 12, ks = f / 3 % 4, m = f % 3, u = 32 * c + 16 * tt + 4 * g;
+          const f16x8 w = as_f16x8(wq[f % kAhead]);
+          if (f + kAhead < kFrags) wq[f % kAhead] = frag(f + kAhead);
+          f32x4 start = zero;
+          if (ks == 0 && m < 2) start = *reinterpret_cast<const f32x4*>(&s_u[m == 0 ? kUnitBiasA : kUnitBiasB][u]);
 #pragma unroll
-            for (int tt = 0; tt < 2; ++tt) {
-              const int u = 32 * c + 16 * tt + 4 * g;
-              const f32x4 kl = *reinterpret_cast<const f32x4*>(&s_u[kUnitLog][u]), ka = *reinterpret_cast<const f32x4*>(&s_u[kUnitA][u]);
+          for (int p = 0; p < TILES; ++p) h[m][p] = mfma(w, m < 2 ? nv[p][ks] : dv[p][ks], ks ? h[m][p] : start);
+          if (f % 12 == 11) {
+            const f32x4 kl = *reinterpret_cast<const f32x4*>(&s_u[kUnitLog][u]), ka = *reinterpret_cast<const f32x4*>(&s_u[kUnitA][u]);
 #pragma unroll
-              for (int p = 0; p < 2; ++p)
+            for (int p = 0; p < TILES; ++p) {
+              f16x4 da, db;
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                  const Gated r = gated(h[0][tt][p][i], h[1][tt][p][i], h[2][tt][p][i], ka[i], kl[i]);
-                  da[p][4 * tt + i] = (__bf16)r.da;
-                  db[p][4 * tt + i] = (__bf16)r.db;
-                }
+              for (int i = 0; i < 4; ++i) {
+                const Gated r = gated(h[0][p][i], h[1][p][i], h[2][p][i], ka[i], kl[i]);
+                da[i] = (_Float16)r.da;
+                db[i] = (_Float16)r.db;
+              }
+              reinterpret_cast<u32x2*>(&s_op[c & 1][share][0][p][lane])[tt] = __builtin_bit_cast(u32x2, da);
+              reinterpret_cast<u32x2*>(&s_op[c & 1][share][1][p][lane])[tt] = __builtin_bit_cast(u32x2, db);
             }
           }
-          const int ct = (f - 24) / 2, m = f % 2;
-#pragma unroll
-          for (int p = 0; p < 2; ++p) acc[ct][p] = mfma32(as_bf16x8(w), m ? db[p] : da[p], acc[ct][p]);
+          __builtin_amdgcn_sched_barrier(0);
         }
-        __builtin_amdgcn_sched_barrier(0);
       }
-      ++seq;
     }
-    // acc (ct = 2 ks + s, register i) is gamma dN at channel 32 ks + 8g + 4s + i of pair 16p + n
-    uint32_t o[2][4][4];
+    barrier_lds();
+    return;
+  }
+  // ---- the products with the transposes, dz, and the weights' copies
+  const __amdgpu_buffer_rsrc_t rows_res =
+      __builtin_amdgcn_make_buffer_rsrc(prep_at<char>(a, kRowsAt), 0, kChunks * kRowBytes, kRawBufferFlags);
+  const __amdgpu_buffer_rsrc_t tr_res =
+      __builtin_amdgcn_make_buffer_rsrc(prep_at<char>(a, kTrAt), 0, kChunks * kTrBytes, kRawBufferFlags);
+  auto copy_rows = [&](int c) {
 #pragma unroll
-    for (int p = 0; p < 2; ++p) {
+    for (int i = 0; i < kRowBytes / 4096; ++i) {
+      const int piece = share * (kRowBytes / 4096) + i;
+      dma_b128(rows_res, c * kRowBytes + piece * 1024 + lane * 16, lds_addr(&s_rows[c & 1][piece * 1024]));
+    }
+  };
+  auto copy_tr = [&](int c) {
+#pragma unroll
+    for (int i = 0; i < kTrBytes / 4096; ++i) {
+      const int piece = share * (kTrBytes / 4096) + i;
+      dma_b128(tr_res, c * kTrBytes + piece * 1024 + lane * 16, lds_addr(&s_tr[c & 1][piece * 1024]));
+    }
+  };
+  f32x4 acc[8][TILES];
+  auto products = [&](int c) {
+    const char* const chunk = s_tr[c & 1] + lane * 16;
+    constexpr int kFrags = 16, kAhead = 4;
+    auto frag = [&](int f) { return *reinterpret_cast<const u32x4*>(chunk + f * 1024); };
+    f16x8 op[2][TILES];
+#pragma unroll
+    for (int m = 0; m < 2; ++m)
+#pragma unroll
+      for (int p = 0; p < TILES; ++p) op[m][p] = as_f16x8(s_op[c & 1][share][m][p][lane]);
+    u32x4 wq[kAhead];
+#pragma unroll
+    for (int f = 0; f < kAhead; ++f) wq[f] = frag(f);
+#pragma unroll
+    for (int f = 0; f < kFrags; ++f) {
+      const f16x8 w = as_f16x8(wq[f % kAhead]);
+      if (f + kAhead < kFrags) wq[f % kAhead] = frag(f + kAhead);
+#pragma unroll
+      for (int p = 0; p < TILES; ++p) acc[f / 2][p] = mfma(w, op[f & 1][p], acc[f / 2][p]);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+  };
+  const int most = max_unit_exponent(a);
+  // acc (ct = 2 ks + s, register i) is gamma dN at channel 32 ks + 8g + 4s + i of pair 16p + n
+  auto finish = [&](int64_t grp, int parity) {
+    u32x4 z[4], d[4];
+    auto load = [&](int p) {
+      const int64_t pair = min(grp * kGroup + (share * TILES + p) * 16 + n, a.n_pairs - 1);
+      load_z<CODES>(a, pair, g, z);
+      load_dout(a, pair, g, d);
+    };
+    load(0);
+#pragma unroll
+    for (int p = 0; p < TILES; ++p) {
+      const int at = (share * TILES + p) * 16 + n;
+      const float mu = s_stat[parity][0][at], rstd = s_stat[parity][1][at];
+      const int e = most - __float_as_int(s_stat[parity][2][at]);
       float zh[4][8], m0 = 0.0f, m1 = 0.0f;
 #pragma unroll
-      for (int ks = 0; ks < 4; ++ks) {
-        const u32x4 w = s_z[wave][4 * p + ks][lane];
+      for (int ks = 0; ks < 4; ++ks)
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-          zh[ks][i] = ((i & 1 ? hi_bf16(w[i >> 1]) : lo_bf16(w[i >> 1])) - mu[p]) * rstd[p];
+          zh[ks][i] = (bf16_of(z[ks], i) - mu) * rstd;
           const float gr = acc[2 * ks + (i >> 2)][p][i & 3];
           m0 += gr;
           m1 = fmaf(gr, zh[ks][i], m1);
         }
-      }
       m0 = sum4(m0) * (1.0f / kCz);
       m1 = sum4(m1) * (1.0f / kCz);
+      uint32_t o[4][4];
 #pragma unroll
       for (int ks = 0; ks < 4; ++ks) {
         bf16x8 v;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          const float d = i & 1 ? hi_bf16(dv[p][ks][i >> 1]) : lo_bf16(dv[p][ks][i >> 1]);
-          v[i] = (__bf16)fmaf(rstd[p], acc[2 * ks + (i >> 2)][p][i & 3] - m0 - zh[ks][i] * m1, d);
-        }
+        for (int i = 0; i < 8; ++i)
+          v[i] = (__bf16)(bf16_of(d[ks], i) + ldexpf(rstd * (acc[2 * ks + (i >> 2)][p][i & 3] - m0 - zh[ks][i] * m1), e));
         const u32x4 w = __builtin_bit_cast(u32x4, v);
 #pragma unroll
-        for (int d = 0; d < 4; ++d) o[p][ks][d] = w[d];
+        for (int k = 0; k < 4; ++k) o[ks][k] = w[k];
       }
-    }
-    // regrouped across lanes so that a store writes 8 pairs x one whole 128-byte line
-    const bool upper = (lane & 4) != 0;
-#pragma unroll
-    for (int p = 0; p < 2; ++p)
+      if (p + 1 < TILES) load(p + 1);
+      // regrouped across lanes so that a store writes 8 pairs x one whole 128-byte line
+      const bool upper = (lane & 4) != 0;
 #pragma unroll
       for (int half = 0; half < 2; ++half) {
         const int src = 8 * half + (lane >> 3) + 16 * (lane & 3);
@@ -387,34 +478,64 @@ __global__ void __launch_bounds__(64 * kWaves) trans_back_pairs_fast_kernel(Tran
         for (int line = 0; line < 2; ++line) {
           u32x4 v;
 #pragma unroll
-          for (int d = 0; d < 4; ++d) {
-            const uint32_t lo = (uint32_t)__builtin_amdgcn_ds_bpermute(4 * src, (int)o[p][2 * line][d]);
-            const uint32_t hi = (uint32_t)__builtin_amdgcn_ds_bpermute(4 * src, (int)o[p][2 * line + 1][d]);
-            v[d] = upper ? hi : lo;
+          for (int k = 0; k < 4; ++k) {
+            const uint32_t lo = (uint32_t)__builtin_amdgcn_ds_bpermute(4 * src, (int)o[2 * line][k]);
+            const uint32_t hi = (uint32_t)__builtin_amdgcn_ds_bpermute(4 * src, (int)o[2 * line + 1][k]);
+            v[k] = upper ? hi : lo;
           }
-          const int64_t pr = pair0 + 16 * p + 8 * half + (lane >> 3);
-          if (pr < a.n_pairs)
-            __builtin_nontemporal_store(v, reinterpret_cast<u32x4*>(static_cast<uint16_t*>(a.dz) + pr * kCz) + 8 * line + (lane & 7));
+          const int64_t pair = grp * kGroup + (share * TILES + p) * 16 + 8 * half + (lane >> 3);
+          if (pair < a.n_pairs)
+            __builtin_nontemporal_store(v, reinterpret_cast<u32x4*>(static_cast<uint16_t*>(a.dz) + pair * kCz) + 8 * line + (lane & 7));
         }
       }
-  }
+    }
+  };
+  copy_rows(0);
   wait_vm<0>();
+  int parity = 0;
+  int64_t before = -1;
+  for (int64_t grp = blockIdx.x; grp < n_groups; grp += gridDim.x, parity ^= 1) {
+    barrier_lds();
+    if (before >= 0) {
+      products(kChunks - 1);
+      finish(before, parity ^ 1);
+    }
+#pragma unroll
+    for (int ct = 0; ct < 8; ++ct)
+#pragma unroll
+      for (int p = 0; p < TILES; ++p) acc[ct][p] = zero;
+#pragma unroll 1
+    for (int c = 0; c < kChunks; ++c) {
+      barrier_lds();
+      // rows of the next chunk (the next group's first after the last), in the room of the one before; this chunk's
+      // transposes in that of the last but one
+      copy_rows(c + 1 == kChunks ? 0 : c + 1);
+      copy_tr(c);
+      if (c > 0) products(c - 1);
+      wait_vm<0>();
+    }
+    before = grp;
+  }
+  barrier_lds();
+  products(kChunks - 1);
+  finish(before, parity ^ 1);
 }
 
 // ----------------------------------------------------------------------------- sums over the pairs
-// A workgroup of 4 waves, one per SIMD, takes 128 units (32 a wave) and a share of the steps of 32 pairs. A wave keeps
-// its units' operands (96 registers) and its sums (192, of 512) throughout; zh and dout of a step, in LDS, serve
-// all four. A', B' and dH come out as pairs (rows) by units: lane (unit n, group g) holds pairs 4g .. of both
-// tiles, and so dA', dB' and H' are the A operands of the products over the pairs, k-slot 8g + j = pair 4g + j of
-// the first tile for j < 4, of the second for j >= 4. Their B operands are columns of zh and dout, which the LDS's
-// transposing reads bring: 16 lanes read four rows of 16 channels, and get four rows of one channel each.
+// A workgroup takes 128 units, 32 each of four shares, and a part of the steps of 32 pairs. Of a share, one wave
+// keeps the rows of the weights in registers and forms A', B' and dH' (pairs by units: lane (unit n, group g) holds pairs
+// 4g .. of both tiles) and dA', dB', H', which are then A operands, k-slot 8g + j = pair 4g + j of the first tile for j < 4,
+// of the second for j >= 4; another keeps the sums (192 registers) and adds the products a step later. Their B operands
+// are columns of zh and dout, which the LDS's transposing reads bring: 16 lanes read four rows of 16 channels, and
+// get four rows of one channel each. The two waves share a SIMD: vector work beside products. (One wave for both, alone
+// on its SIMD, took 1110 us for 1024 tokens.)
 constexpr int kStep = 32;
 constexpr int kSlice = 128;
-constexpr int kStepBytes = 24 * 1024;  // zh in fp16, zh in bf16, dout: 8 KB each, two tiles of 4 KB
-constexpr int kAheadSteps = 2;
+constexpr int kStepBytes = 16 * 1024;  // two tiles of 16 pairs: zh, dout
+constexpr int kOpBytes = 4 * 6 * 1024;  // dA', dB', H'
+constexpr int kAheadSteps = 4;
 constexpr int kStepSlots = kAheadSteps + 2;  // and those whose products and whose sums are formed
 constexpr int kStepDma = kStepBytes / 1024 / 4;
-constexpr int kOpBytes = 4 * 6 * 1024;  // dA', dB', H' of a step
 
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
@@ -424,36 +545,30 @@ __global__ void __launch_bounds__(512, 2) trans_back_sums_fast_kernel(TransBackA
   __shared__ __attribute__((aligned(16))) char s_op[2 * kOpBytes];
   const int tid = threadIdx.x, lane = tid & 63, n = lane & 15, g = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), share = wave & 3;
-  const int hp = blockIdx.y * (kSlice / 32) + share;  // this wave's 32 units
+  const int chunk = blockIdx.y * (kSlice / 32) + share;  // this wave's 32 units
   const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
   const int64_t steps = (a.n_pairs + kStep - 1) / kStep;
-  const int count = (int)((steps - blockIdx.x + gridDim.x - 1) / gridDim.x);  // of this workgroup, at least one
+  const int count = (int)((steps - blockIdx.x + gridDim.x - 1) / gridDim.x);  // of this workgroup
   constexpr int64_t kSize = (int64_t)kHid * kCz;
   float* const part = a.parts + blockIdx.x * (3 * kSize + 2 * kHid);
   char* const my_op = s_op + share * 6 * 1024 + lane * 16;
   if (wave < 4) {
-    // ---- A', B', dH and what follows from them
-    f16x8 w1[2][4], w2[2][4];
-    bf16x8 w3[2][4];
+    f16x8 w[3][2][4];
     float k[2], kl[2], ba[2], bb[2];
-    {
-      const u32x4* base = reinterpret_cast<const u32x4*>(reinterpret_cast<const char*>(a.prep) + (size_t)hp * kPairBytes) + lane;
-      const float* units = reinterpret_cast<const float*>(reinterpret_cast<const char*>(a.prep) + (size_t)kHp * kPairBytes) + 32 * hp + n;
 #pragma unroll
-      for (int ut = 0; ut < 2; ++ut) {
+    for (int ut = 0; ut < 2; ++ut) {
+      const u32x4* rows = prep_at<u32x4>(a, kRowsAt + (size_t)chunk * kRowBytes) + ut * 4 * 192 + lane;
+      const float* units = prep_at<float>(a, kUnitsAt) + 32 * chunk + 16 * ut + n;
 #pragma unroll
-        for (int ks = 0; ks < 4; ++ks) {
-          w1[ut][ks] = as_f16x8(base[(ut * 4 + ks) * 192]);
-          w2[ut][ks] = as_f16x8(base[(ut * 4 + ks) * 192 + 64]);
-          w3[ut][ks] = as_bf16x8(base[(ut * 4 + ks) * 192 + 128]);
-        }
-        kl[ut] = units[kUnitLog * kHid + 16 * ut];
-        k[ut] = units[kUnitA * kHid + 16 * ut];
-        ba[ut] = units[kUnitBiasA * kHid + 16 * ut];
-        bb[ut] = units[kUnitBiasB * kHid + 16 * ut];
-      }
+      for (int ks = 0; ks < 4; ++ks)
+#pragma unroll
+        for (int m = 0; m < 3; ++m) w[m][ut][ks] = as_f16x8(rows[ks * 192 + m * 64]);
+      kl[ut] = units[kUnitLog * kHid];
+      k[ut] = units[kUnitA * kHid];
+      ba[ut] = units[kUnitBiasA * kHid];
+      bb[ut] = units[kUnitBiasB * kHid];
     }
-    auto sum_at = [&](int m, int ut, int i) { return 3 * kSize + m * kHid + 32 * hp + 16 * ut + 4 * g + i; };
+    auto sum_at = [&](int m, int ut, int i) { return 3 * kSize + m * kHid + 32 * chunk + 16 * ut + 4 * g + i; };
     f32x4 s[2][2];  // S1, S2: every column of dA^T ones
 #pragma unroll
     for (int m = 0; m < 2; ++m)
@@ -461,45 +576,42 @@ __global__ void __launch_bounds__(512, 2) trans_back_sums_fast_kernel(TransBackA
       for (int ut = 0; ut < 2; ++ut)
 #pragma unroll
         for (int i = 0; i < 4; ++i) s[m][ut][i] = a.add_parts ? part[sum_at(m, ut, i)] : 0.0f;
-    bf16x8 ones;
+    f16x8 ones;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) ones[i] = (__bf16)1.0f;
-    const int row_at = lane * 16, drow_at = 16384 + column_lane(n, g) * 16;
+    for (int i = 0; i < 8; ++i) ones[i] = (_Float16)1.0f;
+    const int row_at = column_lane(n, g) * 16;
     const char* cur = s_x;
     for (int it = 0; it < count; ++it) {
       barrier_lds();
       // the first tile of pairs, then the second, and between its products what follows from the first
-      auto row = [&](int q) { return *reinterpret_cast<const u32x4*>(cur + (q >> 2) * 4096 + (q & 3) * 1024 + row_at); };
-      auto drow = [&](int q) { return *reinterpret_cast<const u32x4*>(cur + (q >> 2) * 4096 + (q & 3) * 1024 + drow_at); };
+      auto row = [&](int q, int m) { return as_f16x8(*reinterpret_cast<const u32x4*>(cur + (q >> 2) * 8192 + m * 4096 + (q & 3) * 1024 + row_at)); };
       f32x4 h[3][2][2];
-      bf16x8 op[3][2];
+      f16x8 op[3][2];
       auto gate = [&](int ut, int p, int i) {
         const Gated r = gated(h[0][ut][p][i], h[1][ut][p][i], h[2][ut][p][i], k[ut], kl[ut]);
-        op[0][ut][4 * p + i] = (__bf16)r.da;
-        op[1][ut][4 * p + i] = (__bf16)r.db;
-        op[2][ut][4 * p + i] = (__bf16)r.h;
+        op[0][ut][4 * p + i] = (_Float16)r.da;
+        op[1][ut][4 * p + i] = (_Float16)r.db;
+        op[2][ut][4 * p + i] = (_Float16)r.h;
       };
       constexpr int kQueue = 3;
-      u32x4 zq[kQueue], dq[kQueue];
+      f16x8 zq[kQueue], dq[kQueue];
 #pragma unroll
       for (int q = 0; q < kQueue - 1; ++q) {
-        zq[q] = row(q);
-        dq[q] = drow(q);
+        zq[q] = row(q, 0);
+        dq[q] = row(q, 1);
       }
 #pragma unroll
       for (int q = 0; q < 8; ++q) {
         const int p = q >> 2, ks = q & 3;
         if (q + kQueue - 1 < 8) {
-          zq[(q + kQueue - 1) % kQueue] = row(q + kQueue - 1);
-          dq[(q + kQueue - 1) % kQueue] = drow(q + kQueue - 1);
+          zq[(q + kQueue - 1) % kQueue] = row(q + kQueue - 1, 0);
+          dq[(q + kQueue - 1) % kQueue] = row(q + kQueue - 1, 1);
         }
-        const f16x8 za = as_f16x8(zq[q % kQueue]);
-        const bf16x8 d = as_bf16x8(dq[q % kQueue]);
 #pragma unroll
         for (int ut = 0; ut < 2; ++ut) {
-          h[0][ut][p] = mfma_f16(za, w1[ut][ks], ks ? h[0][ut][p] : f32x4{ba[ut], ba[ut], ba[ut], ba[ut]});
-          h[1][ut][p] = mfma_f16(za, w2[ut][ks], ks ? h[1][ut][p] : f32x4{bb[ut], bb[ut], bb[ut], bb[ut]});
-          h[2][ut][p] = mfma32(d, w3[ut][ks], ks ? h[2][ut][p] : zero);
+          h[0][ut][p] = mfma(zq[q % kQueue], w[0][ut][ks], ks ? h[0][ut][p] : f32x4{ba[ut], ba[ut], ba[ut], ba[ut]});
+          h[1][ut][p] = mfma(zq[q % kQueue], w[1][ut][ks], ks ? h[1][ut][p] : f32x4{bb[ut], bb[ut], bb[ut], bb[ut]});
+          h[2][ut][p] = mfma(dq[q % kQueue], w[2][ut][ks], ks ? h[2][ut][p] : zero);
         }
         if (q >= 4) {
           gate(0, 0, q - 4);
@@ -520,7 +632,7 @@ __global__ void __launch_bounds__(512, 2) trans_back_sums_fast_kernel(TransBackA
 #pragma unroll
       for (int m = 0; m < 2; ++m)
 #pragma unroll
-        for (int ut = 0; ut < 2; ++ut) s[m][ut] = mfma32(op[m][ut], ones, s[m][ut]);
+        for (int ut = 0; ut < 2; ++ut) s[m][ut] = mfma(op[m][ut], ones, s[m][ut]);
       cur = cur + kStepBytes == s_x + kStepSlots * kStepBytes ? s_x : cur + kStepBytes;
     }
     barrier_lds();
@@ -533,30 +645,23 @@ __global__ void __launch_bounds__(512, 2) trans_back_sums_fast_kernel(TransBackA
           for (int i = 0; i < 4; ++i) part[sum_at(m, ut, i)] = s[m][ut][i];
     return;
   }
-  // ---- the sums of the step before, and the copies of the steps to come
-  // This wave's share of a step's copies: pieces 6 share .. of 24 (piece = 4 KB tile, then ks)
+  // ---- the sums of the step before, and the copies of the steps to come: pieces 4 share .. of a step's 16
+  int slot = 0;
   auto copy = [&](int it) {
     const int64_t step = blockIdx.x + (int64_t)it * gridDim.x;
-    const uint32_t to = lds_addr(s_x) + (uint32_t)((it & (kStepSlots - 1)) * kStepBytes);
-    const __amdgpu_buffer_rsrc_t zres = __builtin_amdgcn_make_buffer_rsrc(a.zh + step * (2 * 8192), 0, 2 * 8192, kRawBufferFlags);
-    // pairs past the end read as zeros
-    const int left = (int)min((int64_t)kStep, a.n_pairs - step * kStep);
-    const __amdgpu_buffer_rsrc_t dres = __builtin_amdgcn_make_buffer_rsrc(
-        const_cast<char*>(static_cast<const char*>(a.dout) + step * (kStep * kCz * 2)), 0, left * kCz * 2, kRawBufferFlags);
+    const uint32_t to = lds_addr(s_x) + (uint32_t)(slot * kStepBytes);
+    slot = slot + 1 == kStepSlots ? 0 : slot + 1;
+    const __amdgpu_buffer_rsrc_t res = __builtin_amdgcn_make_buffer_rsrc(a.zh + step * kStepBytes, 0, kStepBytes, kRawBufferFlags);
 #pragma unroll
     for (int i = 0; i < kStepDma; ++i) {
-      const int piece = share * kStepDma + i, kind = piece >> 3, tile = (piece >> 2) & 1, ks = piece & 3;
-      if (kind < 2)
-        dma_b128(zres, tile * 8192 + kind * 4096 + ks * 1024 + lane * 16, to + (uint32_t)(piece * 1024));
-      else
-        dma_b128(dres, (16 * tile + (n ^ (8 * (g & 1)))) * (kCz * 2) + 64 * ks + 16 * g, to + (uint32_t)(piece * 1024));
+      const int piece = share * kStepDma + i;
+      dma_b128(res, piece * 1024 + lane * 16, to + (uint32_t)(piece * 1024));
     }
   };
-  static_assert((kStepSlots & (kStepSlots - 1)) == 0, "slots by a mask");
 #pragma unroll
   for (int it = 0; it < kAheadSteps; ++it)
     if (it < count) copy(it);
-  auto part_at = [&](int m, int ut, int ct, int i) { return m * kSize + (32 * hp + 16 * ut + 4 * g + i) * kCz + 16 * ct + n; };
+  auto part_at = [&](int m, int ut, int ct, int i) { return m * kSize + (32 * chunk + 16 * ut + 4 * g + i) * kCz + 16 * ct + n; };
   f32x4 t[3][2][8];
 #pragma unroll
   for (int m = 0; m < 3; ++m)
@@ -578,34 +683,34 @@ __global__ void __launch_bounds__(512, 2) trans_back_sums_fast_kernel(TransBackA
   const int col_at = piece_odd * 256 + ((4 * g + (n >> 2)) ^ (8 * piece_odd)) * 16 + 8 * (n & 1);
   const char* prev = s_x;
   for (int it = 0; it <= count; ++it) {
-    // this wave's copies of step `it` have landed: at most those of the one after it are in flight
-    if (it + 1 < count)
-      wait_vm<kStepDma>();
+    // this wave's copies of step `it` have landed: at most those of the ones after it are in flight
+    if (it + kAheadSteps - 1 < count)
+      wait_vm<(kAheadSteps - 1) * kStepDma>();
     else
       wait_vm<0>();
     barrier_lds();  // and every other wave's; the step before the last has been read
     if (it + kAheadSteps < count) copy(it + kAheadSteps);
     if (it == 0) continue;
-    bf16x8 op[3][2];
+    f16x8 op[3][2];
 #pragma unroll
     for (int m = 0; m < 3; ++m)
 #pragma unroll
       for (int ut = 0; ut < 2; ++ut)
-        op[m][ut] = as_bf16x8(*reinterpret_cast<const u32x4*>(my_op + ((it - 1) & 1) * kOpBytes + (m * 2 + ut) * 1024));
+        op[m][ut] = as_f16x8(*reinterpret_cast<const u32x4*>(my_op + ((it - 1) & 1) * kOpBytes + (m * 2 + ut) * 1024));
     auto columns = [&](int q) {  // q = 2 ct: zh, 2 ct + 1: dout
       u32x4 v;
 #pragma unroll
       for (int half = 0; half < 2; ++half) {
         const s16x4 x = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-            (lds_s16x4*)(prev + 8192 + (q & 1) * 8192 + half * 4096 + (q >> 2) * 1024 + ((q >> 1) & 1) * 512 + col_at));
+            (lds_s16x4*)(prev + half * 8192 + (q & 1) * 4096 + (q >> 2) * 1024 + ((q >> 1) & 1) * 512 + col_at));
         const u32x2 w = __builtin_bit_cast(u32x2, x);
         v[2 * half] = w[0];
         v[2 * half + 1] = w[1];
       }
-      return as_bf16x8(v);
+      return as_f16x8(v);
     };
     constexpr int kQueue = 3;
-    bf16x8 cq[kQueue];
+    f16x8 cq[kQueue];
 #pragma unroll
     for (int q = 0; q < kQueue - 1; ++q) cq[q] = columns(q);
 #pragma unroll
@@ -615,10 +720,10 @@ __global__ void __launch_bounds__(512, 2) trans_back_sums_fast_kernel(TransBackA
 #pragma unroll
       for (int ut = 0; ut < 2; ++ut) {
         if (q & 1) {
-          t[2][ut][ct] = mfma32(op[2][ut], cq[q % kQueue], t[2][ut][ct]);
+          t[2][ut][ct] = mfma(op[2][ut], cq[q % kQueue], t[2][ut][ct]);
         } else {
-          t[0][ut][ct] = mfma32(op[0][ut], cq[q % kQueue], t[0][ut][ct]);
-          t[1][ut][ct] = mfma32(op[1][ut], cq[q % kQueue], t[1][ut][ct]);
+          t[0][ut][ct] = mfma(op[0][ut], cq[q % kQueue], t[0][ut][ct]);
+          t[1][ut][ct] = mfma(op[1][ut], cq[q % kQueue], t[1][ut][ct]);
         }
       }
       __builtin_amdgcn_sched_barrier(0);
@@ -635,13 +740,26 @@ __global__ void __launch_bounds__(512, 2) trans_back_sums_fast_kernel(TransBackA
         for (int i = 0; i < 4; ++i) part[part_at(m, ut, ct, i)] = t[m][ut][ct][i];
 }
 
+// Tiles per wave of dz's kernel: as many pairs a workgroup as leave none of the 256 CUs idle (a chunk of weights takes
+// 0.9 us for one tile a wave and 1.7 for four).
+template <bool CODES>
+void launch_pairs(const TransBackArgs& a, hipStream_t st) {
+  const int64_t one = (a.n_pairs + 63) / 64;
+  if (one <= 256)
+    hipLaunchKernelGGL((trans_back_pairs_fast_kernel<CODES, 1>), dim3((unsigned)one), dim3(512), 0, st, a);
+  else if (one <= 512)
+    hipLaunchKernelGGL((trans_back_pairs_fast_kernel<CODES, 2>), dim3((unsigned)((one + 1) / 2)), dim3(512), 0, st, a);
+  else
+    hipLaunchKernelGGL((trans_back_pairs_fast_kernel<CODES, 4>), dim3((unsigned)((one + 3) / 4 < 256 ? (one + 3) / 4 : 256)), dim3(512), 0, st, a);
+}
+
 }  // namespace
 
 size_t trans_back_fast_prep_bytes() { return kPrepBytes; }
-void trans_back_fast_units(const float* prep, const float** unit_a, const float** unit_b) {
-  const float* units = reinterpret_cast<const float*>(reinterpret_cast<const char*>(prep) + (size_t)kHp * kPairBytes);
-  *unit_a = units + kUnitA * kHid;
-  *unit_b = units + kUnitB * kHid;
+void trans_back_fast_units(const float* prep, const int** unit_exponents, const int** dout_exponent) {
+  const char* at = reinterpret_cast<const char*>(prep);
+  *unit_exponents = reinterpret_cast<const int*>(at + kUnitsAt) + kUnitE1 * kHid;
+  *dout_exponent = reinterpret_cast<const int*>(at + kExpAt) + 1;
 }
 
 int trans_back_fast_splits(int64_t n_pairs) {
@@ -649,16 +767,20 @@ int trans_back_fast_splits(int64_t n_pairs) {
   return (int)(steps < 64 ? steps : 64);
 }
 
-// Pairs at a time: 512 B of zh each in the workspace.
+// Pairs at a time: 512 B each in the workspace.
 constexpr int64_t kChunkPairs = (int64_t)1 << 20;
 size_t trans_back_fast_zh_bytes(int64_t n_pairs) {
-  const int64_t groups = ((n_pairs < kChunkPairs ? n_pairs : kChunkPairs) + kGroupPairs - 1) / kGroupPairs;
-  return (size_t)groups * kGroupPairs * 512;
+  const int64_t groups = ((n_pairs < kChunkPairs ? n_pairs : kChunkPairs) + 255) / 256;
+  return (size_t)groups * 256 * 512;
 }
 
 hipError_t launch_trans_back_fast(const TransBackArgs& whole, hipStream_t st) {
   hipError_t e;
-  hipLaunchKernelGGL(trans_back_prep_fast_kernel, dim3(kHid / 16), dim3(256), 0, st, whole);
+  const int64_t shares = (whole.n_pairs * (kCz / 8) + 2047) / 2048;  // eight 16-byte pieces a thread
+  const int n_tops = (int)(shares < kTops ? shares : kTops);
+  hipLaunchKernelGGL(trans_back_rows_prep_kernel, dim3(kHid / 16 + n_tops), dim3(256), 0, st, whole);
+  if ((e = hipGetLastError()) != hipSuccess) return e;
+  hipLaunchKernelGGL(trans_back_transpose_kernel, dim3(kChunks), dim3(256), 0, st, whole, n_tops);
   if ((e = hipGetLastError()) != hipSuccess) return e;
   const bool sums = whole.dw1 || whole.dw2 || whole.dw3 || whole.dgamma || whole.dbeta;
   const bool sums_first = whole.dz == whole.dout || !whole.dz;
@@ -671,9 +793,7 @@ hipError_t launch_trans_back_fast(const TransBackArgs& whole, hipStream_t st) {
     if (whole.dz) a.dz = static_cast<char*>(whole.dz) + p0 * kCz * 2;
     a.store_zh = sums && !sums_first;
     a.add_parts = p0 > 0;
-    const int64_t n_groups = (a.n_pairs + kGroupPairs - 1) / kGroupPairs;
-    const dim3 pairs_grid((unsigned)(n_groups < 256 ? n_groups : 256)), rows_grid((unsigned)(n_groups * 4));
-    const dim3 sums_grid((unsigned)a.splits, kHid / kSlice);
+    const dim3 rows_grid((unsigned)((a.n_pairs + 255) / 256 * 4)), sums_grid((unsigned)a.splits, kHid / kSlice);
     if (sums && sums_first) {
       if (a.exponents)
         hipLaunchKernelGGL(trans_back_rows_kernel<true>, rows_grid, dim3(256), 0, st, a);
@@ -684,10 +804,7 @@ hipError_t launch_trans_back_fast(const TransBackArgs& whole, hipStream_t st) {
       if ((e = hipGetLastError()) != hipSuccess) return e;
     }
     if (a.dz) {
-      if (a.exponents)
-        hipLaunchKernelGGL(trans_back_pairs_fast_kernel<true>, pairs_grid, dim3(64 * kWaves), 0, st, a);
-      else
-        hipLaunchKernelGGL(trans_back_pairs_fast_kernel<false>, pairs_grid, dim3(64 * kWaves), 0, st, a);
+      a.exponents ? launch_pairs<true>(a, st) : launch_pairs<false>(a, st);
       if ((e = hipGetLastError()) != hipSuccess) return e;
     }
     if (sums && !sums_first) {

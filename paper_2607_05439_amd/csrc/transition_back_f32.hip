@@ -408,12 +408,13 @@ __global__ void __launch_bounds__(256) trans_back_finish_kernel(TransBackArgs a)
 #pragma unroll
     for (int m = 0; m < 2; ++m) s[m] += s_s[m][w];
   }
-  if (a.unit_a) {
-    t[0] *= a.unit_b[u];
-    t[1] *= a.unit_a[u];
-    t[2] *= a.unit_a[u] * a.unit_b[u];
-    s[0] *= a.unit_b[u];
-    s[1] *= a.unit_a[u];
+  if (a.unit_exponents) {
+    const int e1 = a.unit_exponents[u], e2 = a.unit_exponents[a.hidden + u], e3 = a.unit_exponents[2 * a.hidden + u], d = *a.dout_exponent;
+    t[0] = ldexpf(t[0], -(e2 + e3 + d));
+    s[0] = ldexpf(s[0], -(e2 + e3 + d));
+    t[1] = ldexpf(t[1], -(e1 + e3 + d));
+    s[1] = ldexpf(s[1], -(e1 + e3 + d));
+    t[2] = ldexpf(t[2], -(e1 + e2 + d));
   }
   const float ga = a.gamma ? a.gamma[c] : 1.0f, be = a.beta ? a.beta[c] : 0.0f;
   const int64_t at = (int64_t)u * a.c + c;
