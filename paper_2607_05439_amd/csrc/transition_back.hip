@@ -28,7 +28,7 @@ namespace dcp {
 namespace {
 
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
-typedef _Float16 f16x4 __attribute__((ext_vector_type(4)));
+typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
 
 constexpr int kCz = kTransCz;       // 128
 constexpr int kHid = kTransHidden;  // 512
@@ -143,7 +143,7 @@ __global__ void __launch_bounds__(256) trans_back_rows_prep_kernel(TransBackArgs
   if (q > 0) return;
   float* const units = prep_at<float>(a, kUnitsAt) + unit;
   units[kUnitLog * kHid] = ldexpf(-kLog2e, -e[0]);
-  units[kUnitA * kHid] = ldexpf(1.0f, -e[0]);
+  units[kUnitA * kHid] = fminf(ldexpf(1.0f, -e[0]), 32768.0f);  // in fp16's range: past it the slope is that of 0 or 1
   units[kUnitBiasA * kHid] = ldexpf(bias[0], e[0]);
   units[kUnitBiasB * kHid] = ldexpf(bias[1], e[1]);
 #pragma unroll
@@ -190,15 +190,20 @@ __global__ void __launch_bounds__(256) trans_back_transpose_kernel(TransBackArgs
   }
 }
 
-// h0 = A and h1 = B with their powers of two (k: A's inverse, log: -log2(e) times it). With s = sigmoid(A) and
-// A' = h0: H' = A' s B', dB' = dH A' s, dA' = dH B' (s + k A' s (1 - s)).
+// Two elements' h0 = A and h1 = B with their powers of two (k: A's inverse, log: -log2(e) times it). With s = sigmoid(A)
+// and A' = h0: H' = A' s B', dB' = dH A' s, dA' = dH B' (s + k A' s (1 - s)). The sigmoid is fp32, what follows packed fp16: the
+// seven roundings of 2^-12 in dA' together are a third of its rounding to bf16, and the vector work, which does not overlap
+// with the products, falls by a quarter.
+typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
 struct Gated {
-  float h, da, db;
+  f16x2 h, da, db;
 };
-__device__ __forceinline__ Gated gated(float h0, float h1, float dh, float k, float log) {
-  const float s = __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(h0 * log));
-  const float silu = h0 * s;
-  return {silu * h1, dh * h1 * fmaf(silu, fmaf(-k, s, k), s), dh * silu};
+__device__ __forceinline__ Gated gated(float a0, float a1, float b0, float b1, float d0, float d1, f16x2 k, float log0, float log1) {
+  const f16x2 s = {(_Float16)__builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(a0 * log0)),
+                   (_Float16)__builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(a1 * log1))};
+  const f16x2 a = {(_Float16)a0, (_Float16)a1}, b = {(_Float16)b0, (_Float16)b1}, d = {(_Float16)d0, (_Float16)d1};
+  const f16x2 silu = a * s, slope = __builtin_elementwise_fma(silu, __builtin_elementwise_fma(-k, s, k), s);
+  return {silu * b, d * b * slope, d * silu};
 }
 
 // ----------------------------------------------------------------------------- rows
@@ -257,26 +262,42 @@ __device__ __forceinline__ void normalise(const u32x4 (&z)[4], float eps, f16x8 
       zf[ks][i] = (_Float16)zh;
     }
 }
-__device__ __forceinline__ f16x8 scaled(u32x4 d, float scale) {
-  f16x8 v;
+// A row of dout in fp16 with a power of two of its own; e: that.
+__device__ __forceinline__ void scale_row(const u32x4 (&d)[4], f16x8 (&v)[4], int& e) {
+  u16x2 most = {0, 0};
 #pragma unroll
-  for (int i = 0; i < 8; ++i) v[i] = (_Float16)(bf16_of(d, i) * scale);
-  return v;
+  for (int ks = 0; ks < 4; ++ks)
+#pragma unroll
+    for (int k = 0; k < 4; ++k) most = __builtin_elementwise_max(most, __builtin_bit_cast(u16x2, d[ks][k] & 0x7FFF7FFFu));
+  float top = __uint_as_float((uint32_t)(most[0] > most[1] ? most[0] : most[1]) << 16);
+  top = max4(top);
+  if (!(top < INFINITY)) {  // of the finite ones
+    top = 0.0f;
+#pragma unroll
+    for (int ks = 0; ks < 4; ++ks)
+#pragma unroll
+      for (int i = 0; i < 8; ++i) top = fmaxf(top, finite_abs(bf16_of(d[ks], i)));
+    top = max4(top);
+  }
+  e = max(min(exponent_below_one(top), 126), -126);
+  const float scale = ldexpf(1.0f, e);
+#pragma unroll
+  for (int ks = 0; ks < 4; ++ks)
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[ks][i] = (_Float16)(bf16_of(d[ks], i) * scale);
 }
-__device__ __forceinline__ float power(int e) { return ldexpf(1.0f, e); }
 
 // What the sums read of a tile of 16 pairs, 8 KB: [zh | dout][ks][lane] 16 B in fp16, with the pairs of odd groups 8
-// places on, which spreads the LDS reads of columns over all banks. Pairs past the last hold a dout of 0.
+// places on, which spreads the LDS reads of columns over all banks. dout has the power of two of all pairs, to which
+// `factor` takes the row's (0 for pairs past the last).
 __device__ __forceinline__ int column_lane(int n, int g) { return 16 * g + (n ^ (8 * (g & 1))); }
-__device__ __forceinline__ void store_rows(const TransBackArgs& a, int64_t tile, int n, int g, const f16x8 (&zf)[4], const u32x4 (&d)[4],
-                                           float scale) {
-  u32x4* const to = reinterpret_cast<u32x4*>(a.zh) + tile * 512 + column_lane(n, g);
-  const bool there = tile * 16 + n < a.n_pairs;
-#pragma unroll
-  for (int ks = 0; ks < 4; ++ks) {
-    to[ks * 64] = __builtin_bit_cast(u32x4, zf[ks]);
-    to[256 + ks * 64] = there ? __builtin_bit_cast(u32x4, scaled(d[ks], scale)) : u32x4{0u, 0u, 0u, 0u};
-  }
+__device__ __forceinline__ _Float16 row_factor(const TransBackArgs& a, int64_t pair, int e) {
+  return pair < a.n_pairs ? (_Float16)ldexpf(1.0f, dout_exponent(a) - e) : (_Float16)0.0f;
+}
+__device__ __forceinline__ void store_rows(const TransBackArgs& a, int64_t tile, int ks, int n, int g, f16x8 zf, f16x8 d, _Float16 factor) {
+  u32x4* const to = reinterpret_cast<u32x4*>(a.zh) + tile * 512 + ks * 64 + column_lane(n, g);
+  to[0] = __builtin_bit_cast(u32x4, zf);
+  to[256] = __builtin_bit_cast(u32x4, (f16x8)(d * factor));
 }
 
 // These alone, where dz is not wanted or takes dout's place (the sums then come before it). One tile a wave.
@@ -287,10 +308,14 @@ __global__ void __launch_bounds__(256) trans_back_rows_kernel(TransBackArgs a) {
   u32x4 z[4], d[4];
   load_z<CODES>(a, pair, g, z);
   load_dout(a, pair, g, d);
-  f16x8 zf[4];
+  f16x8 zf[4], dv[4];
   float mu, rstd;
+  int e;
   normalise(z, a.eps, zf, mu, rstd);
-  store_rows(a, tile, n, g, zf, d, power(dout_exponent(a)));
+  scale_row(d, dv, e);
+  const _Float16 factor = row_factor(a, tile * 16 + n, e);
+#pragma unroll
+  for (int ks = 0; ks < 4; ++ks) store_rows(a, tile, ks, n, g, zf[ks], dv[ks], factor);
 }
 
 // ----------------------------------------------------------------------------- dz
@@ -315,38 +340,38 @@ __global__ void __launch_bounds__(512, 2) trans_back_pairs_fast_kernel(TransBack
   for (int k = tid; k < 4 * kHid; k += 512) (&s_u[0][0])[k] = prep_at<float>(a, kUnitsAt)[k];
   if (wave < 4) {
     int parity = 0;
-    const float to_all = power(dout_exponent(a));
     for (int64_t grp = blockIdx.x; grp < n_groups; grp += gridDim.x, parity ^= 1) {
       barrier_lds();
       f16x8 nv[TILES][4], dv[TILES][4];
-      {
-        u32x4 z[TILES][4], d[TILES][4];
+      constexpr int kPart = TILES < 2 ? TILES : 2;  // tiles whose rows are in flight: more do not fit the registers
 #pragma unroll
-        for (int p = 0; p < TILES; ++p) {
-          const int64_t pair = min(grp * kGroup + (share * TILES + p) * 16 + n, a.n_pairs - 1);
-          load_z<CODES>(a, pair, g, z[p]);
-          load_dout(a, pair, g, d[p]);
+      for (int p0 = 0; p0 < TILES; p0 += kPart) {
+        u32x4 z[kPart][4], d[kPart][4];
+#pragma unroll
+        for (int q = 0; q < kPart; ++q) {
+          const int64_t pair = min(grp * kGroup + (share * TILES + p0 + q) * 16 + n, a.n_pairs - 1);
+          load_z<CODES>(a, pair, g, z[q]);
+          load_dout(a, pair, g, d[q]);
         }
 #pragma unroll
-        for (int p = 0; p < TILES; ++p) {
-          float mu, rstd, top = 0.0f;
-          normalise(z[p], a.eps, nv[p], mu, rstd);
-          if (a.store_zh) store_rows(a, grp * (4 * TILES) + share * TILES + p, n, g, nv[p], d[p], to_all);
+        for (int q = 0; q < kPart; ++q) {
+          const int p = p0 + q, at = (share * TILES + p) * 16 + n;
+          float mu, rstd;
+          int e;
+          normalise(z[q], a.eps, nv[p], mu, rstd);
+          scale_row(d[q], dv[p], e);
+          if (a.store_zh) {
+            const _Float16 factor = row_factor(a, grp * kGroup + at, e);
 #pragma unroll
-          for (int ks = 0; ks < 4; ++ks)
-#pragma unroll
-            for (int i = 0; i < 8; ++i) top = fmaxf(top, finite_abs(bf16_of(d[p][ks], i)));
-          const int e = max(min(exponent_below_one(max4(top)), 126), -126);
-          const float scale = power(e);
-#pragma unroll
-          for (int ks = 0; ks < 4; ++ks) dv[p][ks] = scaled(d[p][ks], scale);
+            for (int ks = 0; ks < 4; ++ks) store_rows(a, grp * (4 * TILES) + share * TILES + p, ks, n, g, nv[p][ks], dv[p][ks], factor);
+          }
           if (g == 0) {
-            const int at = (share * TILES + p) * 16 + n;
             s_stat[parity][0][at] = mu;
             s_stat[parity][1][at] = rstd;
             s_stat[parity][2][at] = __int_as_float(e);
           }
         }
+        __builtin_amdgcn_sched_barrier(0);
       }
 #pragma unroll 1
       for (int c = 0; c < kChunks; ++c) {
@@ -371,15 +396,16 @@ __global__ void __launch_bounds__(512, 2) trans_back_pairs_fast_kernel(TransBack
             const f32x4 kl = *reinterpret_cast<const f32x4*>(&s_u[kUnitLog][u]), ka = *reinterpret_cast<const f32x4*>(&s_u[kUnitA][u]);
 #pragma unroll
             for (int p = 0; p < TILES; ++p) {
-              f16x4 da, db;
+              u32x2 da, db;
 #pragma unroll
-              for (int i = 0; i < 4; ++i) {
-                const Gated r = gated(h[0][p][i], h[1][p][i], h[2][p][i], ka[i], kl[i]);
-                da[i] = (_Float16)r.da;
-                db[i] = (_Float16)r.db;
+              for (int i = 0; i < 4; i += 2) {
+                const Gated r = gated(h[0][p][i], h[0][p][i + 1], h[1][p][i], h[1][p][i + 1], h[2][p][i], h[2][p][i + 1],
+                                      f16x2{(_Float16)ka[i], (_Float16)ka[i + 1]}, kl[i], kl[i + 1]);
+                da[i >> 1] = __builtin_bit_cast(uint32_t, r.da);
+                db[i >> 1] = __builtin_bit_cast(uint32_t, r.db);
               }
-              reinterpret_cast<u32x2*>(&s_op[c & 1][share][0][p][lane])[tt] = __builtin_bit_cast(u32x2, da);
-              reinterpret_cast<u32x2*>(&s_op[c & 1][share][1][p][lane])[tt] = __builtin_bit_cast(u32x2, db);
+              reinterpret_cast<u32x2*>(&s_op[c & 1][share][0][p][lane])[tt] = da;
+              reinterpret_cast<u32x2*>(&s_op[c & 1][share][1][p][lane])[tt] = db;
             }
           }
           __builtin_amdgcn_sched_barrier(0);
@@ -440,17 +466,19 @@ __global__ void __launch_bounds__(512, 2) trans_back_pairs_fast_kernel(TransBack
       load_dout(a, pair, g, d);
     };
     load(0);
+    products(kChunks - 1);
 #pragma unroll
     for (int p = 0; p < TILES; ++p) {
       const int at = (share * TILES + p) * 16 + n;
       const float mu = s_stat[parity][0][at], rstd = s_stat[parity][1][at];
       const int e = most - __float_as_int(s_stat[parity][2][at]);
+      const float shift = -mu * rstd, half = ldexpf(1.0f, e >> 1), rest = ldexpf(rstd, e - (e >> 1));  // 2^e alone may pass fp32's range
       float zh[4][8], m0 = 0.0f, m1 = 0.0f;
 #pragma unroll
       for (int ks = 0; ks < 4; ++ks)
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-          zh[ks][i] = (bf16_of(z[ks], i) - mu) * rstd;
+          zh[ks][i] = fmaf(bf16_of(z[ks], i), rstd, shift);
           const float gr = acc[2 * ks + (i >> 2)][p][i & 3];
           m0 += gr;
           m1 = fmaf(gr, zh[ks][i], m1);
@@ -463,7 +491,7 @@ __global__ void __launch_bounds__(512, 2) trans_back_pairs_fast_kernel(TransBack
         bf16x8 v;
 #pragma unroll
         for (int i = 0; i < 8; ++i)
-          v[i] = (__bf16)(bf16_of(d[ks], i) + ldexpf(rstd * (acc[2 * ks + (i >> 2)][p][i & 3] - m0 - zh[ks][i] * m1), e));
+          v[i] = (__bf16)fmaf(half * fmaf(-zh[ks][i], m1, acc[2 * ks + (i >> 2)][p][i & 3] - m0), rest, bf16_of(d[ks], i));
         const u32x4 w = __builtin_bit_cast(u32x4, v);
 #pragma unroll
         for (int k = 0; k < 4; ++k) o[ks][k] = w[k];
@@ -496,10 +524,7 @@ __global__ void __launch_bounds__(512, 2) trans_back_pairs_fast_kernel(TransBack
   int64_t before = -1;
   for (int64_t grp = blockIdx.x; grp < n_groups; grp += gridDim.x, parity ^= 1) {
     barrier_lds();
-    if (before >= 0) {
-      products(kChunks - 1);
-      finish(before, parity ^ 1);
-    }
+    if (before >= 0) finish(before, parity ^ 1);
 #pragma unroll
     for (int ct = 0; ct < 8; ++ct)
 #pragma unroll
@@ -517,7 +542,6 @@ __global__ void __launch_bounds__(512, 2) trans_back_pairs_fast_kernel(TransBack
     before = grp;
   }
   barrier_lds();
-  products(kChunks - 1);
   finish(before, parity ^ 1);
 }
 
@@ -554,7 +578,8 @@ __global__ void __launch_bounds__(512, 2) trans_back_sums_fast_kernel(TransBackA
   char* const my_op = s_op + share * 6 * 1024 + lane * 16;
   if (wave < 4) {
     f16x8 w[3][2][4];
-    float k[2], kl[2], ba[2], bb[2];
+    f16x2 k[2];
+    float kl[2], ba[2], bb[2];
 #pragma unroll
     for (int ut = 0; ut < 2; ++ut) {
       const u32x4* rows = prep_at<u32x4>(a, kRowsAt + (size_t)chunk * kRowBytes) + ut * 4 * 192 + lane;
@@ -564,7 +589,7 @@ __global__ void __launch_bounds__(512, 2) trans_back_sums_fast_kernel(TransBackA
 #pragma unroll
         for (int m = 0; m < 3; ++m) w[m][ut][ks] = as_f16x8(rows[ks * 192 + m * 64]);
       kl[ut] = units[kUnitLog * kHid];
-      k[ut] = units[kUnitA * kHid];
+      k[ut] = f16x2{(_Float16)units[kUnitA * kHid], (_Float16)units[kUnitA * kHid]};
       ba[ut] = units[kUnitBiasA * kHid];
       bb[ut] = units[kUnitBiasB * kHid];
     }
@@ -586,12 +611,13 @@ __global__ void __launch_bounds__(512, 2) trans_back_sums_fast_kernel(TransBackA
       // the first tile of pairs, then the second, and between its products what follows from the first
       auto row = [&](int q, int m) { return as_f16x8(*reinterpret_cast<const u32x4*>(cur + (q >> 2) * 8192 + m * 4096 + (q & 3) * 1024 + row_at)); };
       f32x4 h[3][2][2];
-      f16x8 op[3][2];
-      auto gate = [&](int ut, int p, int i) {
-        const Gated r = gated(h[0][ut][p][i], h[1][ut][p][i], h[2][ut][p][i], k[ut], kl[ut]);
-        op[0][ut][4 * p + i] = (_Float16)r.da;
-        op[1][ut][4 * p + i] = (_Float16)r.db;
-        op[2][ut][4 * p + i] = (_Float16)r.h;
+      u32x4 op[3][2];
+      auto gate = [&](int ut, int p, int i) {  // pairs i, i + 1 of this lane's four
+        const Gated r = gated(h[0][ut][p][i], h[0][ut][p][i + 1], h[1][ut][p][i], h[1][ut][p][i + 1], h[2][ut][p][i], h[2][ut][p][i + 1],
+                              k[ut], kl[ut], kl[ut]);
+        op[0][ut][2 * p + i / 2] = __builtin_bit_cast(uint32_t, r.da);
+        op[1][ut][2 * p + i / 2] = __builtin_bit_cast(uint32_t, r.db);
+        op[2][ut][2 * p + i / 2] = __builtin_bit_cast(uint32_t, r.h);
       };
       constexpr int kQueue = 3;
       f16x8 zq[kQueue], dq[kQueue];
@@ -613,26 +639,22 @@ __global__ void __launch_bounds__(512, 2) trans_back_sums_fast_kernel(TransBackA
           h[1][ut][p] = mfma(zq[q % kQueue], w[1][ut][ks], ks ? h[1][ut][p] : f32x4{bb[ut], bb[ut], bb[ut], bb[ut]});
           h[2][ut][p] = mfma(dq[q % kQueue], w[2][ut][ks], ks ? h[2][ut][p] : zero);
         }
-        if (q >= 4) {
-          gate(0, 0, q - 4);
-          gate(1, 0, q - 4);
-        }
+        if (q >= 4) gate(q & 1, 0, (q - 4) & 2);
         __builtin_amdgcn_sched_barrier(0);
       }
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
+      for (int i = 0; i < 4; i += 2) {
         gate(0, 1, i);
         gate(1, 1, i);
       }
 #pragma unroll
       for (int m = 0; m < 3; ++m)
 #pragma unroll
-        for (int ut = 0; ut < 2; ++ut)
-          *reinterpret_cast<u32x4*>(my_op + (it & 1) * kOpBytes + (m * 2 + ut) * 1024) = __builtin_bit_cast(u32x4, op[m][ut]);
+        for (int ut = 0; ut < 2; ++ut) *reinterpret_cast<u32x4*>(my_op + (it & 1) * kOpBytes + (m * 2 + ut) * 1024) = op[m][ut];
 #pragma unroll
       for (int m = 0; m < 2; ++m)
 #pragma unroll
-        for (int ut = 0; ut < 2; ++ut) s[m][ut] = mfma(op[m][ut], ones, s[m][ut]);
+        for (int ut = 0; ut < 2; ++ut) s[m][ut] = mfma(as_f16x8(op[m][ut]), ones, s[m][ut]);
       cur = cur + kStepBytes == s_x + kStepSlots * kStepBytes ? s_x : cur + kStepBytes;
     }
     barrier_lds();
