@@ -16,11 +16,10 @@
 namespace dcp {
 namespace {
 
-// The bucket of tokens with positions p, q in groups g, h. The difference of two int32 fits 64 bits.
+// The bucket of tokens with positions p, q in groups g, h. A difference past 32 bits saturates, far outside +-r.
 __device__ __forceinline__ uint32_t bucket_of(int32_t p, int32_t q, int32_t g, int32_t h, int32_t r) {
-  const int64_t d = (int64_t)p - q;
-  const int32_t clipped = d > r ? r : d < -r ? -r : (int32_t)d;
-  return (uint32_t)(g == h ? clipped + r : 2 * r + 1);
+  const int32_t d = __builtin_elementwise_sub_sat(p, q);
+  return (uint32_t)(g == h ? max(min(d, r), -r) + r : 2 * r + 1);
 }
 
 // Buckets of a pair, a byte per field (at most 2 * 127 + 1)
@@ -135,91 +134,129 @@ __global__ void __launch_bounds__(256) relative_kernel(RelativeArgs a) {
 // as k-slots and 16 channels as columns. A one-hot's products are exact, and so are fp32 gradients in three bf16 pieces
 // (8 bits each); the sums are fp32, in an order that the sizes alone fix. Only the tiles of buckets that occur
 // among the 32 pairs are multiplied: near the diagonal three or four of twelve, elsewhere one a field.
-//   A workgroup takes a share of the tiles of 64 S pairs of a row and 32 CG channels (S CG = 4): CG waves take 32
-// channels each, and S such sets the pairs' 64ths, each with sums of its own. dz is copied through registers one
-// tile ahead into LDS as [pair][channel], whose transposing reads bring 16 channels of eight pairs as a B operand;
-// k-slot 8g + j is pair 4g + j of the 32 for j < 4, 16 + 4g + j - 4 for j >= 4. Buckets lie in LDS as bytes.
+//   A workgroup takes consecutive tiles of 128 S pairs of a row (fp32: 64 S) and 32 CG channels (S CG = 4): CG
+// waves take 32 channels each, and S such sets a share of the pairs, each with sums of its own. dz comes through
+// registers, a tile ahead, into LDS as [pair][channel], whose transposing reads bring 16 channels of eight pairs as a B operand;
+// k-slot 8g + j is pair 4g + j of the 32 for j < 4, 16 + 4g + j - 4 for j >= 4. Wave f finds the buckets of field f, a
+// byte of each pair's word in LDS.
 //   A value that is not finite would make NaN of every bucket (0 times infinity): it enters as 0 and is added to its
-// own buckets afterwards. Bound by memory: 2400 rows of 4800 tokens read dz once.
+// own buckets afterwards. Bound by memory.
 constexpr int kWindow = 12;  // tiles of buckets at a time: the paper's fields have 5 + 5 + 1 + 1
 
+typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
 
+// Pairs of a tile that a set of waves has to itself: a tile is 32 KB, which are in flight while the one before is worked on.
+constexpr int relative_own_pairs(bool bf16) { return bf16 ? 128 : 64; }
+
 template <typename T, int CG, bool VEC>
-__global__ void __launch_bounds__(256) relative_back_kernel(RelativeArgs a) {
-  constexpr int kVec = 16 / sizeof(T), S = 4 / CG, kPairs = 64 * S, kChannels = 32 * CG;
+__global__ void __launch_bounds__(256, 2) relative_back_kernel(RelativeArgs a) {
+  constexpr int kVec = 16 / sizeof(T), S = 4 / CG, kOwn = relative_own_pairs(sizeof(T) == 2), kPairs = kOwn * S, kChannels = 32 * CG;
   constexpr int kPlanes = sizeof(T) == 2 ? 1 : 3, kRow = 2 * kChannels + 32, kPlane = kPairs * kRow;
   constexpr int kRowPieces = kChannels / kVec, kMine = kPairs * kRowPieces / 256;
   __shared__ __attribute__((aligned(16))) char s_d[kPlanes * kPlane];
-  __shared__ __attribute__((aligned(16))) uint8_t s_b[4][kRelativeFields][64];
+  __shared__ __attribute__((aligned(16))) uint32_t s_b[kPairs];
   __shared__ __attribute__((aligned(16))) int s_bad[4];
   const int tid = threadIdx.x, lane = tid & 63, n = lane & 15, g = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), cg = wave % CG, stream = wave / CG;
   const int c0 = blockIdx.y * kChannels, w0 = blockIdx.z * kWindow;
-  const int64_t row_tiles = (a.n_tok + kPairs - 1) / kPairs, tiles = a.n_rows * row_tiles;
+  const int64_t row_tiles = (a.n_tok + kPairs - 1) / kPairs;
+  int64_t todo, first;
+  chunk_of(a.n_rows * row_tiles, gridDim.x, blockIdx.x, &todo, &first);
   f32x4 acc[kWindow][2];
 #pragma unroll
   for (int w = 0; w < kWindow; ++w) acc[w][0] = acc[w][1] = f32x4{0.f, 0.f, 0.f, 0.f};
 
-  u32x4 raw[kMine];
-  uint32_t mine = 0;
-  int64_t row = 0, j0 = 0;
-  const T* const dz = static_cast<const T*>(a.dz);
-  auto fetch = [&](int64_t tile) {
-    row = tile / row_tiles;
-    j0 = (tile - row * row_tiles) * kPairs;
+  // this window's tiles: where the field's byte is, and the tile's place among the field's (16 for none)
+  int shift[kWindow];
+  uint32_t place[kWindow];
 #pragma unroll
-    for (int k = 0; k < kMine; ++k) {
-      const int p = (tid + 256 * k) / kRowPieces, c = c0 + (tid + 256 * k) % kRowPieces * kVec;
-      raw[k] = u32x4{0u, 0u, 0u, 0u};
-      if (j0 + p >= a.n_tok || c >= a.c) continue;
-      const T* q = dz + (row * a.n_tok + j0 + p) * a.c + c;
-      if (VEC) {
-        raw[k] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(q));
-      } else {
+  for (int w = 0; w < kWindow; ++w) {
+    const bool there = w0 + w < a.n_tiles;
+    shift[w] = __builtin_amdgcn_readfirstlane(there ? 8 * a.tile_field[w0 + w] : 0);
+    place[w] = (uint32_t)__builtin_amdgcn_readfirstlane(there ? a.tile_of_field[w0 + w] : 16);
+  }
+  // the tile to be fetched next, and the one that is worked on
+  int64_t row = first / row_tiles, j0 = (first - row * row_tiles) * kPairs, this_row = row, this_j0 = j0;
+  const int field = min(wave, a.n_fields - 1);
+  const int32_t *const position = a.position[field], *const group = a.group[field];
+  const T* const dz = static_cast<const T*>(a.dz);
+  int offset[kMine];  // bytes in a tile
+#pragma unroll
+  for (int k = 0; k < kMine; ++k) {
+    const int p = (tid + 256 * k) / kRowPieces, c = c0 + (tid + 256 * k) % kRowPieces * kVec;
+    offset[k] = c < a.c ? (p * a.c + c) * (int)sizeof(T) : kOutOfRange;
+  }
+  constexpr int kLanes = kPairs / 64;  // pairs of a tile that a lane finds the bucket of
+  u32x4 raw[kMine];
+  int32_t pos_i, grp_i, pos_j[kLanes], grp_j[kLanes];
+  auto fetch = [&]() {
+    const T* const base = dz + (row * a.n_tok + j0) * a.c;
+    const int left = (int)min((int64_t)kPairs, a.n_tok - j0);
+    if (VEC) {
+      const __amdgpu_buffer_rsrc_t res =
+          __builtin_amdgcn_make_buffer_rsrc(const_cast<T*>(base), 0, left * a.c * (int)sizeof(T), kRawBufferFlags);
+#pragma unroll
+      for (int k = 0; k < kMine; ++k) raw[k] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(res, offset[k], 0, 2));
+    } else {
+#pragma unroll
+      for (int k = 0; k < kMine; ++k) {
+        const int p = (tid + 256 * k) / kRowPieces, c = c0 + (tid + 256 * k) % kRowPieces * kVec;
+        raw[k] = u32x4{0u, 0u, 0u, 0u};
+        if (p >= left) continue;
 #pragma unroll
         for (int e = 0; e < kVec; ++e)
           if (c + e < a.c) {
+            const float v = load_f32(base + p * a.c + c + e);
             if (sizeof(T) == 2)
-              raw[k][e >> 1] |= (uint32_t)__builtin_bit_cast(uint16_t, (__bf16)load_f32(q + e)) << (16 * (e & 1));
+              raw[k][e >> 1] |= (__float_as_uint(v) >> 16) << (16 * (e & 1));
             else
-              raw[k][e & 3] = __float_as_uint(load_f32(q + e));
+              raw[k][e & 3] = __float_as_uint(v);
           }
       }
     }
-    mine = buckets_of(a, a.row0 + row, min(j0 + 64 * stream + lane, a.n_tok - 1));
+    pos_i = position[a.row0 + row];
+    grp_i = group ? group[a.row0 + row] : 0;
+#pragma unroll
+    for (int s = 0; s < kLanes; ++s) {
+      const int64_t j = min(j0 + 64 * s + lane, a.n_tok - 1);
+      pos_j[s] = position[j];
+      grp_j[s] = group ? group[j] : 0;
+    }
+    j0 += kPairs;
+    if (j0 >= a.n_tok) {
+      j0 = 0;
+      ++row;
+    }
   };
-  int64_t tile = blockIdx.x;
-  if (tile < tiles) fetch(tile);
-  for (; tile < tiles; tile += gridDim.x) {
-    const uint32_t buckets = mine;
-    const int64_t this_row = row, this_j0 = j0;
-    __syncthreads();  // the tile before has been read
+  if (todo > 0) fetch();
+  for (int64_t k_tile = 0; k_tile < todo; ++k_tile) {
+    barrier_lds();  // the tile before has been read
     bool bad = false;
 #pragma unroll
     for (int k = 0; k < kMine; ++k) {
       char* const to = s_d + (tid + 256 * k) / kRowPieces * kRow + (tid + 256 * k) % kRowPieces * (2 * kVec);
+      u32x4 r = raw[k];
       if (sizeof(T) == 2) {
-        bool here = false;
+        u16x2 top = {0, 0};
 #pragma unroll
-        for (int d = 0; d < 4; ++d)
-          here |= (raw[k][d] & 0x7F800000u) == 0x7F800000u || (raw[k][d] & 0x7F80u) == 0x7F80u;
-        if (here) {
+        for (int d = 0; d < 4; ++d) top = __builtin_elementwise_max(top, __builtin_bit_cast(u16x2, r[d] & 0x7FFF7FFFu));
+        if (max(top[0], top[1]) >= 0x7F80) {
 #pragma unroll
           for (int d = 0; d < 4; ++d) {
-            if ((raw[k][d] & 0x7F800000u) == 0x7F800000u) raw[k][d] &= 0xFFFFu;
-            if ((raw[k][d] & 0x7F80u) == 0x7F80u) raw[k][d] &= 0xFFFF0000u;
+            if ((r[d] & 0x7F800000u) == 0x7F800000u) r[d] &= 0xFFFFu;
+            if ((r[d] & 0x7F80u) == 0x7F80u) r[d] &= 0xFFFF0000u;
           }
           bad = true;
         }
-        *reinterpret_cast<u32x4*>(to) = raw[k];
+        *reinterpret_cast<u32x4*>(to) = r;
       } else {
         uint32_t piece[3][2];
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-          float v = __uint_as_float(raw[k][e]);
-          if ((raw[k][e] & 0x7F800000u) == 0x7F800000u) {
+          float v = __uint_as_float(r[e]);
+          if ((r[e] & 0x7F800000u) == 0x7F800000u) {
             v = 0.0f;
             bad = true;
           }
@@ -234,14 +271,19 @@ __global__ void __launch_bounds__(256) relative_back_kernel(RelativeArgs a) {
         for (int q = 0; q < kPlanes; ++q) *reinterpret_cast<u32x2*>(to + q * kPlane) = u32x2{piece[q][0], piece[q][1]};
       }
     }
+    if (wave < a.n_fields)
 #pragma unroll
-    for (int f = 0; f < kRelativeFields; ++f) s_b[wave][f][lane] = (uint8_t)(buckets >> (8 * f));
+      for (int s = 0; s < kLanes; ++s)
+        reinterpret_cast<uint8_t*>(s_b)[4 * (64 * s + lane) + wave] =
+            (uint8_t)bucket_of(pos_i, pos_j[s], grp_i, grp_j[s], a.radius[field]);
     const uint64_t any_bad = __builtin_amdgcn_ballot_w64(bad);
     if (lane == 0) s_bad[wave] = any_bad != 0;
-    __syncthreads();
-    if (tile + gridDim.x < tiles) fetch(tile + gridDim.x);
-#pragma unroll
-    for (int ks = 0; ks < 2; ++ks) {
+    barrier_lds();
+    if (k_tile + 1 < todo) fetch();
+#pragma unroll 1
+    for (int ks = 0; ks < kOwn / 32; ++ks) {
+      const int p0 = kOwn * stream + 32 * ks;  // these 32 pairs
+      const uint32_t buckets = s_b[p0 + (lane & 31)];
       bf16x8 d[kPlanes][2];
 #pragma unroll
       for (int q = 0; q < kPlanes; ++q)
@@ -251,7 +293,7 @@ __global__ void __launch_bounds__(256) relative_back_kernel(RelativeArgs a) {
 #pragma unroll
           for (int half = 0; half < 2; ++half) {
             const s16x4 x = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-                (lds_s16x4*)(s_d + q * kPlane + (64 * stream + 32 * ks + 16 * half + 4 * g + (n >> 2)) * kRow + 64 * cg + 32 * ct +
+                (lds_s16x4*)(s_d + q * kPlane + (p0 + 16 * half + 4 * g + (n >> 2)) * kRow + 64 * cg + 32 * ct +
                              8 * (n & 3)));
             const u32x2 w = __builtin_bit_cast(u32x2, x);
             v[2 * half] = w[0];
@@ -259,20 +301,26 @@ __global__ void __launch_bounds__(256) relative_back_kernel(RelativeArgs a) {
           }
           d[q][ct] = as_bf16x8(v);
         }
+      const u32x4 b0 = *reinterpret_cast<const u32x4*>(&s_b[p0 + 4 * g]), b1 = *reinterpret_cast<const u32x4*>(&s_b[p0 + 16 + 4 * g]);
+      const uint32_t one = (uint32_t)__builtin_amdgcn_readfirstlane((int)buckets);
+      const bool alike = __builtin_amdgcn_ballot_w64(buckets != one) == 0;
 #pragma unroll
       for (int w = 0; w < kWindow; ++w) {
-        if (w0 + w >= a.n_tiles) continue;
-        const int f = a.tile_field[w0 + w], t = a.tile_of_field[w0 + w];
-        const uint64_t hit = __builtin_amdgcn_ballot_w64((buckets >> (8 * f + 4) & 15) == (uint32_t)t);
-        if ((uint32_t)(hit >> (32 * ks)) == 0) continue;
-        const uint32_t want = (uint32_t)(16 * t + n);
         u32x4 hot;
+        if (alike) {
+          const uint32_t b = one >> shift[w] & 255;
+          if (b >> 4 != place[w]) continue;
+          const uint32_t v = (b & 15) == (uint32_t)n ? 0x3F803F80u : 0u;
+          hot = u32x4{v, v, v, v};
+        } else {
+          if (__builtin_amdgcn_ballot_w64((buckets >> shift[w] >> 4 & 15) == place[w]) == 0) continue;
+          const uint32_t want = 16 * place[w] + (uint32_t)n;
+          auto is = [&](uint32_t b, uint32_t v) { return (b >> shift[w] & 255) == want ? v : 0u; };
 #pragma unroll
-        for (int half = 0; half < 2; ++half) {
-          const uint32_t b = *reinterpret_cast<const uint32_t*>(&s_b[wave][f][32 * ks + 16 * half + 4 * g]);
-#pragma unroll
-          for (int i = 0; i < 2; ++i)
-            hot[2 * half + i] = ((b >> (16 * i) & 255) == want ? 0x3F80u : 0u) | ((b >> (16 * i + 8) & 255) == want ? 0x3F800000u : 0u);
+          for (int i = 0; i < 2; ++i) {
+            hot[i] = is(b0[2 * i], 0x3F80u) | is(b0[2 * i + 1], 0x3F800000u);
+            hot[2 + i] = is(b1[2 * i], 0x3F80u) | is(b1[2 * i + 1], 0x3F800000u);
+          }
         }
 #pragma unroll
         for (int q = 0; q < kPlanes; ++q)
@@ -281,10 +329,11 @@ __global__ void __launch_bounds__(256) relative_back_kernel(RelativeArgs a) {
       }
     }
     if (s_bad[0] | s_bad[1] | s_bad[2] | s_bad[3]) {
-      for (int p = 0; p < 64; ++p) {
-        const int64_t j = this_j0 + 64 * stream + p;
+#pragma unroll 1
+      for (int p = 0; p < kOwn; ++p) {
+        const int64_t j = this_j0 + kOwn * stream + p;
         if (j >= a.n_tok) break;
-        const uint32_t b = (uint32_t)__builtin_amdgcn_readlane((int)buckets, p);
+        const uint32_t b = (uint32_t)__builtin_amdgcn_readfirstlane((int)s_b[kOwn * stream + p]);
 #pragma unroll
         for (int ct = 0; ct < 2; ++ct) {
           const int c = c0 + 32 * cg + 16 * ct + n;
@@ -293,14 +342,18 @@ __global__ void __launch_bounds__(256) relative_back_kernel(RelativeArgs a) {
           if (!__builtin_amdgcn_ballot_w64(add)) continue;
 #pragma unroll
           for (int w = 0; w < kWindow; ++w) {
-            if (w0 + w >= a.n_tiles) continue;
-            const uint32_t of_tile = (b >> (8 * a.tile_field[w0 + w]) & 255) - 16u * a.tile_of_field[w0 + w];
+            const uint32_t of_tile = (b >> shift[w] & 255) - 16u * place[w];  // of none: not below 16
 #pragma unroll
             for (int i = 0; i < 4; ++i)
               if (add && of_tile == (uint32_t)(4 * g + i)) acc[w][ct][i] += v;
           }
         }
       }
+    }
+    this_j0 += kPairs;
+    if (this_j0 >= a.n_tok) {
+      this_j0 = 0;
+      ++this_row;
     }
   }
   const int64_t part = (int64_t)blockIdx.x * S + stream;
@@ -382,12 +435,13 @@ hipError_t launch_relative(const RelativeArgs& a, bool bf16, hipStream_t st) {
 }
 
 void relative_back_split(RelativeArgs* a) {
-  const int cg = channel_sets(a->c), s = 4 / cg;
-  const int64_t tiles = a->n_rows * ((a->n_tok + 64 * s - 1) / (64 * s));
+  // the workspace's size does not know the type: tiles of the larger of the two, as in bf16
+  const int cg = channel_sets(a->c), s = 4 / cg, pairs = relative_own_pairs(true) * s;
+  const int64_t tiles = a->n_rows * ((a->n_tok + pairs - 1) / pairs);
   const int64_t per = (int64_t)((a->c + 32 * cg - 1) / (32 * cg)) * ((a->n_tiles + kWindow - 1) / kWindow);
-  int64_t most = 768 / per;
+  int64_t most = 512 / per;  // two workgroups a CU
   if (most < 64) most = 64;
-  const int64_t want = (tiles + 3) / 4;
+  const int64_t want = (tiles + 1) / 2;
   a->n_groups = (int32_t)(want < most ? want : most);
   a->n_parts = a->n_groups * s;
 }
