@@ -29,8 +29,10 @@ __device__ __forceinline__ f32x4 mfma4(float a, float b, f32x4 c) {
 struct Gated {
   float h, da, db;
 };
+// The hardware's exp2 and reciprocal are off by 2^-23 of the result, and log2(e) a by 2^-24 of itself, so the sigmoid by
+// 2^-22 + 2^-24 |a| at most.
 __device__ __forceinline__ Gated gated(float a, float b, float dh) {
-  const float s = 1.0f / (1.0f + expf(-a)), silu = a * s;
+  const float s = __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(-1.44269504088896340736f * a)), silu = a * s;
   return {silu * b, dh * b * (s + silu * (1.0f - s)), dh * silu};
 }
 
@@ -88,7 +90,7 @@ __device__ __forceinline__ f32x4 load4(const TransBackArgs& a, const void* x, bo
 // (rows) of unit n (column), which is the A operand of the products over the pairs: step i has
 // pair 4g + i in k-slot g. Their B operand is zh or dout of that pair at channel 16j + n, from LDS.
 template <int CT>
-__global__ void __launch_bounds__(256, CT > 4 ? 1 : 2) trans_back_sums_kernel(TransBackArgs a) {
+__global__ void __launch_bounds__(256, CT > 8 ? 1 : 2) trans_back_sums_kernel(TransBackArgs a) {
   constexpr int kC = 16 * CT, kRow = kC + 4;
   __shared__ f32x4 s_n[CT][64], s_d[CT][64];  // N and dout as operands: lane (pair n, g), channels 16j + 4g ..
   __shared__ float s_zh[16][kRow], s_do[16][kRow];
@@ -199,6 +201,131 @@ __global__ void __launch_bounds__(256, CT > 4 ? 1 : 2) trans_back_sums_kernel(Tr
   if (!active) return;
   const int64_t size = (int64_t)hp * cp;
   float* part = a.parts + blockIdx.y * (3 * size + 2 * hp);
+#pragma unroll
+  for (int m = 0; m < 3; ++m)
+#pragma unroll
+    for (int j = 0; j < CT; ++j)
+      if (16 * j < cp)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) part[m * size + (int64_t)(u0 + 4 * g + i) * cp + 16 * j + n] = t[m][j][i];
+  s1 = sum4(s1);
+  s2 = sum4(s2);
+  if (g == 0) {
+    part[3 * size + u0 + n] = s1;
+    part[3 * size + hp + u0 + n] = s2;
+  }
+}
+
+// The same for 65 to 128 channels: there the weights and sums of a wave leave no room for a second wave on its SIMD (36864
+// pairs of 128 channels and 512 units: 410 us). The weights of the 64 units lie in LDS instead, for eight waves,
+// of which four take one tile of 16 pairs and four another, with sums of their own: a workgroup's two parts.
+constexpr int kWideTiles = 8;  // of 16 channels
+__global__ void __launch_bounds__(512, 2) trans_back_sums_wide_kernel(TransBackArgs a) {
+  constexpr int CT = kWideTiles, kRow = 16 * CT + 4;
+  __shared__ f32x4 s_w[4][3][CT][64];
+  __shared__ __attribute__((aligned(16))) float s_x[3][2][16][kRow];  // N, zh, dout of both tiles
+  const int tid = threadIdx.x, lane = tid & 63, n = lane & 15, g = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), ut = wave & 3, half = wave >> 2;
+  const int cp = (a.c + 15) & ~15, hp = (a.hidden + 15) & ~15;
+  const int64_t size = (int64_t)hp * cp;
+  const int u0 = blockIdx.x * 64 + ut * 16;
+  const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
+  for (int k = tid; k < 4 * 3 * CT * 64; k += 512) {
+    const int l = k & 63, j = (k >> 6) % CT, m = (k / (64 * CT)) % 3, t = k / (64 * CT * 3), u = blockIdx.x * 64 + 16 * t + (l & 15);
+    (&s_w[0][0][0][0])[k] = u < hp && 16 * j < cp ? *reinterpret_cast<const f32x4*>(a.prep + m * size + (int64_t)u * cp + 16 * j + 4 * (l >> 4)) : zero;
+  }
+  f32x4 t[3][CT];
+#pragma unroll
+  for (int m = 0; m < 3; ++m)
+#pragma unroll
+    for (int j = 0; j < CT; ++j) t[m][j] = zero;
+  float s1 = 0.0f, s2 = 0.0f;
+  // staging: 16 threads a pair, thread q of them channels 4 q and 4 (q + 16)
+  const int sh = tid >> 8, sp = (tid >> 4) & 15, sq = tid & 15;
+  const float* gb = a.prep + 5 * size;
+  f32x4 ga[2], be[2], z[2], d[2];
+#pragma unroll
+  for (int k = 0; k < 2; ++k) {
+    const int c0 = 4 * (sq + 16 * k);
+    ga[k] = c0 < cp ? *reinterpret_cast<const f32x4*>(gb + c0) : zero;
+    be[k] = c0 < cp ? *reinterpret_cast<const f32x4*>(gb + cp + c0) : zero;
+  }
+  const int64_t tiles = (a.n_pairs + 31) / 32;
+  auto fetch = [&](int64_t tile) {
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+      z[k] = load4(a, a.z, a.exponents != nullptr, a.z_vec, tile * 32 + 16 * sh + sp, 4 * (sq + 16 * k));
+      d[k] = load4(a, a.dout, false, a.d_vec, tile * 32 + 16 * sh + sp, 4 * (sq + 16 * k));
+    }
+  };
+  int64_t tile = blockIdx.y;
+  if (tile < tiles) fetch(tile);
+  for (; tile < tiles; tile += gridDim.y) {
+    float sum = 0.0f, var = 0.0f;
+#pragma unroll
+    for (int k = 0; k < 2; ++k) sum += (z[k][0] + z[k][1]) + (z[k][2] + z[k][3]);
+    for (int m = 8; m > 0; m >>= 1) sum += __shfl_xor(sum, m);
+    const float mu = sum / (float)a.c;
+    const bool there = tile * 32 + 16 * sh + sp < a.n_pairs;
+#pragma unroll
+    for (int k = 0; k < 2; ++k)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        z[k][i] = there && 4 * (sq + 16 * k) + i < a.c ? z[k][i] - mu : 0.0f;
+        var = fmaf(z[k][i], z[k][i], var);
+      }
+    for (int m = 8; m > 0; m >>= 1) var += __shfl_xor(var, m);
+    const float rstd = there ? 1.0f / sqrtf(var / (float)a.c + a.eps) : 0.0f;
+    barrier_lds();  // the tiles before have been read
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+      const int c0 = 4 * (sq + 16 * k);
+      f32x4 nv;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        z[k][i] *= rstd;
+        nv[i] = there && c0 + i < a.c ? fmaf(z[k][i], ga[k][i], be[k][i]) : 0.0f;
+      }
+      *reinterpret_cast<f32x4*>(&s_x[0][sh][sp][c0]) = nv;
+      *reinterpret_cast<f32x4*>(&s_x[1][sh][sp][c0]) = z[k];
+      *reinterpret_cast<f32x4*>(&s_x[2][sh][sp][c0]) = d[k];
+    }
+    barrier_lds();
+    if (tile + gridDim.y < tiles) fetch(tile + gridDim.y);
+    f32x4 x = zero, y = zero, h = zero;
+#pragma unroll
+    for (int j = 0; j < CT; ++j) {
+      const f32x4 nv = *reinterpret_cast<const f32x4*>(&s_x[0][half][n][16 * j + 4 * g]);
+      const f32x4 dv = *reinterpret_cast<const f32x4*>(&s_x[2][half][n][16 * j + 4 * g]);
+      const f32x4 w1 = s_w[ut][0][j][lane], w2 = s_w[ut][1][j][lane], w3 = s_w[ut][2][j][lane];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        x = mfma4(nv[i], w1[i], x);
+        y = mfma4(nv[i], w2[i], y);
+        h = mfma4(dv[i], w3[i], h);
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const Gated r = gated(x[i], y[i], h[i]);
+      h[i] = r.h;
+      x[i] = r.da;
+      y[i] = r.db;
+      s1 += r.da;
+      s2 += r.db;
+    }
+#pragma unroll
+    for (int j = 0; j < CT; ++j)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const float zh = s_x[1][half][4 * g + i][16 * j + n], dv = s_x[2][half][4 * g + i][16 * j + n];
+        t[0][j] = mfma4(x[i], zh, t[0][j]);
+        t[1][j] = mfma4(y[i], zh, t[1][j]);
+        t[2][j] = mfma4(h[i], dv, t[2][j]);
+      }
+  }
+  if (u0 >= hp) return;
+  float* part = a.parts + (2 * (int64_t)blockIdx.y + half) * (3 * size + 2 * hp);
 #pragma unroll
   for (int m = 0; m < 3; ++m)
 #pragma unroll
@@ -383,7 +510,7 @@ __global__ void __launch_bounds__(256) trans_back_finish_kernel(TransBackArgs a)
   if (way < ways) {
     f32x4 t[3] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
     float s1 = 0.0f, s2 = 0.0f;
-#pragma unroll 4
+#pragma unroll 8
     for (int sp = way; sp < a.splits; sp += ways) {
       const float* p = a.parts + sp * stride + (int64_t)u * cp + 4 * q;
 #pragma unroll
@@ -456,13 +583,17 @@ hipError_t launch_sums(const TransBackArgs& a, hipStream_t st) {
   return hipGetLastError();
 }
 
+// One round of workgroups, of which a CU holds two where rows are of at most 64 channels and one where they are wider; those
+// of the wide kernel give two parts.
+bool wide(int32_t c) { return c > 64 && c <= 16 * kWideTiles; }
+
 }  // namespace
 
 int trans_back_gen_splits(int64_t n_pairs, int32_t c, int32_t hidden) {
-  (void)c;
-  const int64_t tiles = (n_pairs + 15) / 16, groups = (hidden + 63) / 64;
-  const int64_t most = (512 + groups - 1) / groups;
-  return (int)(tiles < most ? tiles : most);
+  const int pairs = wide(c) ? 32 : 16;
+  const int64_t tiles = (n_pairs + pairs - 1) / pairs, groups = (hidden + 63) / 64, room = c > 64 ? 256 : 512;
+  const int64_t most = room > groups ? room / groups : 1;
+  return (int)(tiles < most ? tiles : most) * (wide(c) ? 2 : 1);
 }
 
 hipError_t launch_trans_back_gen(const TransBackArgs& a, hipStream_t st) {
@@ -470,7 +601,9 @@ hipError_t launch_trans_back_gen(const TransBackArgs& a, hipStream_t st) {
   hipLaunchKernelGGL(trans_back_prep_kernel, dim3(128), dim3(256), 0, st, a);
   if ((e = hipGetLastError()) != hipSuccess) return e;
   if (a.dw1 || a.dw2 || a.dw3 || a.dgamma || a.dbeta) {
-    e = a.c > 128 ? launch_sums<16>(a, st) : a.c > 64 ? launch_sums<8>(a, st) : a.c > 32 ? launch_sums<4>(a, st) : launch_sums<2>(a, st);
+    if (wide(a.c))
+      hipLaunchKernelGGL(trans_back_sums_wide_kernel, dim3((unsigned)((a.hidden + 63) / 64), (unsigned)(a.splits / 2)), dim3(512), 0, st, a);
+    e = wide(a.c) ? hipGetLastError() : a.c > 128 ? launch_sums<16>(a, st) : a.c > 32 ? launch_sums<4>(a, st) : launch_sums<2>(a, st);
     if (e != hipSuccess) return e;
   }
   if (!a.dz) return hipSuccess;
