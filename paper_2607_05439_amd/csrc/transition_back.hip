@@ -46,9 +46,9 @@ __device__ __forceinline__ float bf16_of(u32x4 v, int i) { return i & 1 ? hi_bf1
 // 2 ks + 1 holds channels 32 ks + 8 g .. + 7, those that it loads of a row.
 __host__ __device__ inline int out_channel(int ct, int r) { return 32 * (ct >> 1) + 8 * (r >> 2) + 4 * (ct & 1) + (r & 3); }
 
-// e for which top 2^e is in [1/2, 1); 0 for 0
+// e for which top 2^e is in [1/2, 1); for 0 one past all of these, so that what is 0 never sets the power of two of others
 __device__ __forceinline__ int exponent_below_one(float top) {
-  int e = 0;
+  int e = -400;
   if (top > 0.0f) (void)frexpf(top, &e);
   return -e;
 }

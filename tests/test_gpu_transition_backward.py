@@ -351,3 +351,35 @@ def test_more_than_2_31_elements():
     assert not got["dz"][:-tail].any()
     got["dz"] = got["dz"][-tail:]
     check(got, want, "bf16", "2^24 pairs")
+
+
+@pytest.mark.parametrize("factor", [2.0 ** -12, 2.0 ** -70])
+@pytest.mark.parametrize("t,c,hidden", [("f32", 32, 64), ("bf16", 128, 512)])
+def test_pairs_without_a_gradient_beside_small_ones(t, c, hidden, factor):
+    """Masked pairs: rows of zeros in dout get exact zeros and add nothing, however small the others are."""
+    x = make(700, c, hidden, t, seed=17)
+    x["dout"] = x["dout"] * factor
+    x["dout"][::3] = 0.0
+    got = Call(x, "f32")()
+    assert not got["dz"][::3].any()
+    check(got, reference(x), t, factor)
+
+
+@pytest.mark.parametrize("what", ["w1", "w2", "w3", "all"])
+@pytest.mark.parametrize("t,c,hidden", [("f32", 32, 64), ("bf16", 128, 512)])
+def test_units_without_weights_beside_small_ones(t, c, hidden, what, monkeypatch):
+    """A hidden width that is filled up with zeros: those units neither add anything nor cost the others their
+    precision, however small the others' weights are. z is small and its LayerNorm without eps, so that what the
+    weights make of dz is not hidden by dout; beta is left out, of which W1 and W2 would make values of other sizes."""
+    import sys
+    monkeypatch.setattr(sys.modules[__name__], "EPS", 0.0)
+    x = make(400, c, hidden, t, seed=18)
+    x["beta"] = None
+    x["z"] = x["z"] * 2.0 ** -60
+    for k in ("w1", "w2", "w3"):
+        x[k] = x[k] * 2.0 ** -14
+        if what in (k, "all"):
+            (x[k].T if k == "w3" else x[k])[hidden // 3:] = 0.0
+    got, want = Call(x, "f32")(), reference(x)
+    assert float((want["dz"] - x["dout"].double()).norm()) > 8 * float(x["dout"].double().norm())
+    check(got, want, t, what)
