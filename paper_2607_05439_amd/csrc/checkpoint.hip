@@ -39,7 +39,7 @@ template <typename T>
 __global__ void __launch_bounds__(256) pack_kernel(CheckpointArgs a, int64_t n_pieces) {
   constexpr int kVec = 16 / sizeof(T);
   const u32x4* x = static_cast<const u32x4*>(a.x);
-  const int64_t first = (int64_t)blockIdx.x * (256 * kPieces) + threadIdx.x;
+  const int64_t first = (a.first_block + blockIdx.x) * (256 * kPieces) + threadIdx.x;
   u32x4 raw[kPieces];
 #pragma unroll
   for (int k = 0; k < kPieces; ++k) raw[k] = __builtin_nontemporal_load(x + min(first + 256 * k, n_pieces - 1));
@@ -77,7 +77,7 @@ __global__ void __launch_bounds__(256) pack_kernel(CheckpointArgs a, int64_t n_p
 template <typename T>
 __global__ void __launch_bounds__(256) unpack_kernel(CheckpointArgs a, int64_t n_pieces) {
   constexpr int kVec = 16 / sizeof(T), kLanes = kCheckpointBlock / kVec;
-  const int64_t first = (int64_t)blockIdx.x * (256 * kPieces) + threadIdx.x;
+  const int64_t first = (a.first_block + blockIdx.x) * (256 * kPieces) + threadIdx.x;
   u32x2 q[kPieces];
   uint32_t exponent[kPieces];
 #pragma unroll
@@ -113,7 +113,7 @@ __global__ void __launch_bounds__(256) unpack_kernel(CheckpointArgs a, int64_t n
 // A lane per channel, 32 lanes a block: any width and alignment.
 template <typename T>
 __global__ void __launch_bounds__(256) pack_any_kernel(CheckpointArgs a) {
-  const int64_t t = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5);
+  const int64_t t = (a.first_block + blockIdx.x) * 8 + (threadIdx.x >> 5);
   const int blocks = checkpoint_blocks(a.c);
   if (t >= a.n_rows * blocks) return;  // 32 lanes together
   const int64_t row = t / blocks;
@@ -128,7 +128,7 @@ __global__ void __launch_bounds__(256) pack_any_kernel(CheckpointArgs a) {
 
 template <typename T>
 __global__ void __launch_bounds__(256) unpack_any_kernel(CheckpointArgs a) {
-  const int64_t t = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5);
+  const int64_t t = (a.first_block + blockIdx.x) * 8 + (threadIdx.x >> 5);
   const int blocks = checkpoint_blocks(a.c);
   if (t >= a.n_rows * blocks) return;
   const int64_t row = t / blocks;
@@ -137,21 +137,26 @@ __global__ void __launch_bounds__(256) unpack_any_kernel(CheckpointArgs a) {
 }
 
 template <typename T>
-hipError_t launch(const CheckpointArgs& a, hipStream_t st) {
+hipError_t launch(CheckpointArgs a, hipStream_t st) {
   constexpr int kVec = 16 / sizeof(T);
   const auto at = [](const void* p, uintptr_t n) { return (reinterpret_cast<uintptr_t>(p) & (n - 1)) == 0; };
   const bool whole = a.c % kCheckpointBlock == 0 && at(a.x, 16) && at(a.y, 16) && at(a.codes, kVec);
   const int64_t n_pieces = a.n_rows * a.c / kVec, blocks = a.n_rows * checkpoint_blocks(a.c);
-  const dim3 grid((unsigned)(whole ? (n_pieces + 256 * kPieces - 1) / (256 * kPieces) : (blocks + 7) / 8));
-  if (a.x && whole)
-    hipLaunchKernelGGL(pack_kernel<T>, grid, dim3(256), 0, st, a, n_pieces);
-  else if (a.x)
-    hipLaunchKernelGGL(pack_any_kernel<T>, grid, dim3(256), 0, st, a);
-  else if (whole)
-    hipLaunchKernelGGL(unpack_kernel<T>, grid, dim3(256), 0, st, a, n_pieces);
-  else
-    hipLaunchKernelGGL(unpack_any_kernel<T>, grid, dim3(256), 0, st, a);
-  return hipGetLastError();
+  const int64_t total = whole ? (n_pieces + 256 * kPieces - 1) / (256 * kPieces) : (blocks + 7) / 8;
+  hipError_t e = hipSuccess;
+  for (; a.first_block < total && e == hipSuccess; a.first_block += kLaunchBlocks) {
+    const dim3 grid((unsigned)(total - a.first_block < kLaunchBlocks ? total - a.first_block : kLaunchBlocks));
+    if (a.x && whole)
+      hipLaunchKernelGGL(pack_kernel<T>, grid, dim3(256), 0, st, a, n_pieces);
+    else if (a.x)
+      hipLaunchKernelGGL(pack_any_kernel<T>, grid, dim3(256), 0, st, a);
+    else if (whole)
+      hipLaunchKernelGGL(unpack_kernel<T>, grid, dim3(256), 0, st, a, n_pieces);
+    else
+      hipLaunchKernelGGL(unpack_any_kernel<T>, grid, dim3(256), 0, st, a);
+    e = hipGetLastError();
+  }
+  return e;
 }
 
 }  // namespace

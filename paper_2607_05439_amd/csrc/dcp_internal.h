@@ -402,6 +402,7 @@ struct TransBackArgs {
   void *dw1, *dw2, *dw3, *dgamma, *dbeta;
   int32_t grads_bf16;
   int32_t z_vec, d_vec;      // fp32: rows of z, of dout and dz in whole aligned groups of four channels
+  int64_t first_block;       // fp32, of a launch for dz
   int32_t splits;            // shares of the pairs that are summed on their own
   float* prep;               // weights as operands
   float* parts;              // [splits]: T1, T2, T3 [hp][cp], S1, S2 [hp] (hidden and c filled up to 16)
@@ -413,8 +414,12 @@ struct TransBackArgs {
   int32_t store_zh, add_parts;  // whether the sums are added to the parts
 };
 
+// Blocks of 256 threads in one launch: a launch holds fewer than 2^32 threads. Kernels with a grid of the data's size take
+// their first block as an argument.
+constexpr int64_t kLaunchBlocks = (int64_t)1 << 23;
+
 struct CheckpointArgs {
-  int64_t n_rows;
+  int64_t n_rows, first_block;
   int32_t c;
   const void* x;  // to be packed, or null
   void* y;        // where to unpack, or null
@@ -426,7 +431,7 @@ constexpr int kRelativeFields = 4;
 constexpr int kRelativeMaxRadius = 127;  // a bucket fits a byte
 constexpr int kRelativeMaxC = 1024;
 struct RelativeArgs {
-  int64_t n_tok, row0, n_rows;
+  int64_t n_tok, row0, n_rows, first_block;  // first_block: of a launch of the encoding
   int32_t c, n_fields, n_buckets;
   const int32_t* position[kRelativeFields];  // [n_tok]
   const int32_t* group[kRelativeFields];     // [n_tok] or null

@@ -43,7 +43,7 @@ __device__ __forceinline__ void store_f32(float v, uint16_t* p) { *p = __builtin
 template <typename T>
 __global__ void __launch_bounds__(256) relative_any_kernel(RelativeArgs a) {
   const int lane = threadIdx.x & 63;
-  const int64_t unit = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int64_t unit = (a.first_block + blockIdx.x) * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int64_t blocks = (a.n_tok + 63) / 64;
   if (unit >= a.n_rows * blocks) return;
   const int64_t row = unit / blocks, j0 = (unit - row * blocks) * 64;
@@ -70,7 +70,7 @@ template <typename T, int LANES>
 __global__ void __launch_bounds__(256) relative_kernel(RelativeArgs a) {
   constexpr int kVec = 16 / sizeof(T), kBatch = LANES < 8 ? LANES : 8;
   const int lane = threadIdx.x & 63, piece = lane & (LANES - 1), base = lane & ~(LANES - 1);
-  const int64_t unit = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int64_t unit = (a.first_block + blockIdx.x) * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int64_t blocks = (a.n_tok + 63) / 64;
   if (unit >= a.n_rows * blocks) return;
   const int64_t row = unit / blocks, j0 = (unit - row * blocks) * 64;
@@ -230,6 +230,7 @@ __global__ void __launch_bounds__(256, 2) relative_back_kernel(RelativeArgs a) {
       ++row;
     }
   };
+  for (int k = tid; k < kPairs; k += 256) s_b[k] = 0;  // bytes of fields that are not there: alike in all pairs
   if (todo > 0) fetch();
   for (int64_t k_tile = 0; k_tile < todo; ++k_tile) {
     barrier_lds();  // the tile before has been read
@@ -394,24 +395,29 @@ __global__ void __launch_bounds__(256) relative_sum_kernel(RelativeArgs a) {
 bool at16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
 
 template <typename T>
-hipError_t launch_forward(const RelativeArgs& a, hipStream_t st) {
+hipError_t launch_forward(RelativeArgs a, hipStream_t st) {
   constexpr int kVec = 16 / sizeof(T);
-  const int64_t units = a.n_rows * ((a.n_tok + 63) / 64);
-  const dim3 grid((unsigned)((units + 3) / 4)), block(256);
+  const int64_t units = a.n_rows * ((a.n_tok + 63) / 64), total = (units + 3) / 4;
+  const dim3 block(256);
   const int pieces = a.c / kVec;
-  if (a.c % kVec || pieces > 64 || !at16(a.table) || !at16(a.z_in) || !at16(a.z_out))
-    hipLaunchKernelGGL(relative_any_kernel<T>, grid, block, 0, st, a);
-  else if (pieces > 32)
-    hipLaunchKernelGGL((relative_kernel<T, 64>), grid, block, 0, st, a);
-  else if (pieces > 16)
-    hipLaunchKernelGGL((relative_kernel<T, 32>), grid, block, 0, st, a);
-  else if (pieces > 8)
-    hipLaunchKernelGGL((relative_kernel<T, 16>), grid, block, 0, st, a);
-  else if (pieces > 4)
-    hipLaunchKernelGGL((relative_kernel<T, 8>), grid, block, 0, st, a);
-  else
-    hipLaunchKernelGGL((relative_kernel<T, 4>), grid, block, 0, st, a);
-  return hipGetLastError();
+  hipError_t e = hipSuccess;
+  for (; a.first_block < total && e == hipSuccess; a.first_block += kLaunchBlocks) {
+    const dim3 grid((unsigned)(total - a.first_block < kLaunchBlocks ? total - a.first_block : kLaunchBlocks));
+    if (a.c % kVec || pieces > 64 || !at16(a.table) || !at16(a.z_in) || !at16(a.z_out))
+      hipLaunchKernelGGL(relative_any_kernel<T>, grid, block, 0, st, a);
+    else if (pieces > 32)
+      hipLaunchKernelGGL((relative_kernel<T, 64>), grid, block, 0, st, a);
+    else if (pieces > 16)
+      hipLaunchKernelGGL((relative_kernel<T, 32>), grid, block, 0, st, a);
+    else if (pieces > 8)
+      hipLaunchKernelGGL((relative_kernel<T, 16>), grid, block, 0, st, a);
+    else if (pieces > 4)
+      hipLaunchKernelGGL((relative_kernel<T, 8>), grid, block, 0, st, a);
+    else
+      hipLaunchKernelGGL((relative_kernel<T, 4>), grid, block, 0, st, a);
+    e = hipGetLastError();
+  }
+  return e;
 }
 
 int channel_sets(int32_t c) { return c > 64 ? 4 : c > 32 ? 2 : 1; }

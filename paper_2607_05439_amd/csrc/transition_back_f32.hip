@@ -357,7 +357,7 @@ __global__ void __launch_bounds__(256, CT > 8 ? 1 : 2) trans_back_pairs_kernel(T
   const int lane = threadIdx.x & 63, n = lane & 15, g = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int cp = (a.c + 15) & ~15, hp = (a.hidden + 15) & ~15;
-  const int64_t size = (int64_t)hp * cp, tile0 = (int64_t)blockIdx.x * P;
+  const int64_t size = (int64_t)hp * cp, tile0 = (a.first_block + blockIdx.x) * P;
   const float* gb = a.prep + 5 * size;
   const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
   auto chunk = [](const float* p) { return *reinterpret_cast<const f32x4*>(p); };
@@ -571,10 +571,15 @@ __global__ void __launch_bounds__(256) trans_back_affine_kernel(TransBackArgs a)
 }
 
 template <int CT, int P>
-hipError_t launch_pairs(const TransBackArgs& a, hipStream_t st) {
-  hipLaunchKernelGGL((trans_back_pairs_kernel<CT, P>), dim3((unsigned)((a.n_pairs + 16 * P - 1) / (16 * P))), dim3(256), 0,
-                     st, a);
-  return hipGetLastError();
+hipError_t launch_pairs(TransBackArgs a, hipStream_t st) {
+  const int64_t total = (a.n_pairs + 16 * P - 1) / (16 * P);
+  hipError_t e = hipSuccess;
+  for (; a.first_block < total && e == hipSuccess; a.first_block += kLaunchBlocks) {
+    const dim3 grid((unsigned)(total - a.first_block < kLaunchBlocks ? total - a.first_block : kLaunchBlocks));
+    hipLaunchKernelGGL((trans_back_pairs_kernel<CT, P>), grid, dim3(256), 0, st, a);
+    e = hipGetLastError();
+  }
+  return e;
 }
 template <int CT>
 hipError_t launch_sums(const TransBackArgs& a, hipStream_t st) {

@@ -168,3 +168,17 @@ def test_in_a_graph_and_on_another_stream():
         g.replay()
         torch.cuda.synchronize()
         assert torch.equal(y2, unpack(*pack(x), torch.bfloat16))
+
+
+def test_more_threads_than_one_launch_holds():
+    """A row a block of one channel: 2^27 rows are 2^32 threads. The last rows are written too."""
+    import torch
+    n, tail = (1 << 27) + 77, 1000
+    x = torch.zeros((n, 1), dtype=torch.bfloat16, device="cuda")
+    x[-tail:, 0] = torch.arange(1, tail + 1, device="cuda").to(torch.bfloat16)
+    codes, exps = pack(x)
+    assert not codes[:-tail].any() and (exps[:-tail] == 1).all()
+    want = pack(x[-tail:].clone())
+    assert torch.equal(codes[-tail:], want[0]) and torch.equal(exps[-tail:], want[1])
+    y = unpack(codes, exps, torch.bfloat16)
+    assert not y[:-tail].any() and torch.equal(y[-tail:], unpack(*want, torch.bfloat16))

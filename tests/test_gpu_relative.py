@@ -259,3 +259,16 @@ def test_more_than_2_32_elements():
     want = forward(n, row0 + rows - 2, 2, 128, "bf16", fields, table, z[-2:])
     forward(n, row0, rows, 128, "bf16", fields, table, z, out=z)
     assert torch.equal(z[-2:], want)
+
+
+def test_more_threads_than_one_launch_holds():
+    """66000 tokens of one channel: more than 2^32 pairs, a lane each. Rows of all launches."""
+    import torch
+    import paper_2607_05439_amd as dcp
+    n = 66000
+    fields = [(torch.arange(n, dtype=torch.int32, device="cuda"), None, 1)]
+    table = torch.tensor([[1.0], [2.0], [3.0], [4.0]], device="cuda")
+    z = torch.full((n, n, 1), 7.0, dtype=torch.bfloat16, device="cuda")
+    dcp.dcp_relative_position(n, 0, n, 1, dcp.DCP_BF16, dcp.make_relative_fields(fields), table, None, z)
+    for rows in (slice(0, 100), slice(30000, 30100), slice(n - 2000, n)):
+        assert torch.equal(z[rows, :, 0].float(), table[:, 0][buckets(fields, rows.start, rows.stop - rows.start)[0]])

@@ -383,3 +383,17 @@ def test_units_without_weights_beside_small_ones(t, c, hidden, what, monkeypatch
     got, want = Call(x, "f32")(), reference(x)
     assert float((want["dz"] - x["dout"].double()).norm()) > 8 * float(x["dout"].double().norm())
     check(got, want, t, what)
+
+
+def test_f32_more_threads_than_one_launch_holds():
+    """2^29 pairs and more, of which a thread takes an eighth of one. The last thousand, the others without a gradient."""
+    import torch
+    n, tail = (1 << 29) + 1003, 1000
+    x = make(tail, 2, 3, "f32", seed=19)
+    big = {k: torch.zeros((n, 2), device="cuda") for k in ("z", "dout")}
+    for k in big:
+        big[k][-tail:] = x[k]
+    got, want = Call({**x, **big})(), reference(x)
+    assert not got["dz"][:-tail].any()
+    got["dz"] = got["dz"][-tail:]
+    check(got, want, "f32", "2^29 pairs")
