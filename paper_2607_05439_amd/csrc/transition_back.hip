@@ -324,13 +324,14 @@ __global__ void __launch_bounds__(256) trans_back_rows_kernel(TransBackArgs a) {
 // those four other waves form, a chunk of 32 units later, and at a group's end dz. So every weight fragment is read from
 // LDS once for TILES tiles of pairs, and on every SIMD the vector work of one wave lies beside the products of another:
 // with each wave doing all of it for two tiles, the LDS reads alone took as long as the products (1024 tokens: 880 us).
-// The weights stream through LDS by direct-to-LDS loads, the rows one chunk ahead.
-template <bool CODES, int TILES>
+// The weights stream through LDS by direct-to-LDS loads, the rows one chunk ahead. SPLIT 2, for few pairs: two waves form a tile
+// of pairs, 16 units of a chunk each, and two of the others multiply; more loads in flight or chunks ahead gain nothing there.
+template <bool CODES, int TILES, int SPLIT>
 __global__ void __launch_bounds__(512, 2) trans_back_pairs_fast_kernel(TransBackArgs a) {
-  constexpr int kGroup = 64 * TILES;
+  constexpr int kGroup = 64 * TILES / SPLIT;
   __shared__ __attribute__((aligned(16))) char s_rows[2][kRowBytes];
   __shared__ __attribute__((aligned(16))) char s_tr[2][kTrBytes];
-  __shared__ __attribute__((aligned(16))) u32x4 s_op[2][4][2][TILES][64];  // [chunk parity][wave][dA' | dB'][tile][lane]
+  __shared__ __attribute__((aligned(16))) u32x4 s_op[2][4 / SPLIT][2][TILES][64];  // [chunk parity][pairs' share][dA' | dB'][tile][lane]
   __shared__ __attribute__((aligned(16))) float s_u[4][kHid];              // kUnitLog, kUnitA, kUnitBiasA, kUnitBiasB
   __shared__ float s_stat[2][3][kGroup];                                   // [group parity]: mean, rstd, dout's exponent
   const int tid = threadIdx.x, lane = tid & 63, n = lane & 15, g = lane >> 4;
@@ -339,6 +340,7 @@ __global__ void __launch_bounds__(512, 2) trans_back_pairs_fast_kernel(TransBack
   const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
   for (int k = tid; k < 4 * kHid; k += 512) (&s_u[0][0])[k] = prep_at<float>(a, kUnitsAt)[k];
   if (wave < 4) {
+    const int pairs_share = share / SPLIT, only = share % SPLIT;  // SPLIT 2: the tile of 16 units that this wave takes
     int parity = 0;
     for (int64_t grp = blockIdx.x; grp < n_groups; grp += gridDim.x, parity ^= 1) {
       barrier_lds();
@@ -349,23 +351,23 @@ __global__ void __launch_bounds__(512, 2) trans_back_pairs_fast_kernel(TransBack
         u32x4 z[kPart][4], d[kPart][4];
 #pragma unroll
         for (int q = 0; q < kPart; ++q) {
-          const int64_t pair = min(grp * kGroup + (share * TILES + p0 + q) * 16 + n, a.n_pairs - 1);
+          const int64_t pair = min(grp * kGroup + (pairs_share * TILES + p0 + q) * 16 + n, a.n_pairs - 1);
           load_z<CODES>(a, pair, g, z[q]);
           load_dout(a, pair, g, d[q]);
         }
 #pragma unroll
         for (int q = 0; q < kPart; ++q) {
-          const int p = p0 + q, at = (share * TILES + p) * 16 + n;
+          const int p = p0 + q, at = (pairs_share * TILES + p) * 16 + n;
           float mu, rstd;
           int e;
           normalise(z[q], a.eps, nv[p], mu, rstd);
           scale_row(d[q], dv[p], e);
-          if (a.store_zh) {
+          if (a.store_zh && only == 0) {
             const _Float16 factor = row_factor(a, grp * kGroup + at, e);
 #pragma unroll
-            for (int ks = 0; ks < 4; ++ks) store_rows(a, grp * (4 * TILES) + share * TILES + p, ks, n, g, nv[p][ks], dv[p][ks], factor);
+            for (int ks = 0; ks < 4; ++ks) store_rows(a, grp * (kGroup / 16) + pairs_share * TILES + p, ks, n, g, nv[p][ks], dv[p][ks], factor);
           }
-          if (g == 0) {
+          if (g == 0 && only == 0) {
             s_stat[parity][0][at] = mu;
             s_stat[parity][1][at] = rstd;
             s_stat[parity][2][at] = __int_as_float(e);
@@ -376,8 +378,8 @@ __global__ void __launch_bounds__(512, 2) trans_back_pairs_fast_kernel(TransBack
 #pragma unroll 1
       for (int c = 0; c < kChunks; ++c) {
         barrier_lds();
-        const char* const chunk = s_rows[c & 1] + lane * 16;
-        constexpr int kFrags = 24, kAhead = 4;
+        const char* const chunk = s_rows[c & 1] + only * (kRowBytes / 2) + lane * 16;
+        constexpr int kFrags = 24 / SPLIT, kAhead = 4;
         auto frag = [&](int f) { return *reinterpret_cast<const u32x4*>(chunk + f * 1024); };
         u32x4 wq[kAhead];
 #pragma unroll
@@ -385,7 +387,7 @@ __global__ void __launch_bounds__(512, 2) trans_back_pairs_fast_kernel(TransBack
         f32x4 h[3][TILES];
 #pragma unroll
         for (int f = 0; f < kFrags; ++f) {
-          const int tt = f / 12, ks = f / 3 % 4, m = f % 3, u = 32 * c + 16 * tt + 4 * g;
+          const int tt = SPLIT == 2 ? only : f / 12, ks = f / 3 % 4, m = f % 3, u = 32 * c + 16 * tt + 4 * g;
           const f16x8 w = as_f16x8(wq[f % kAhead]);
           if (f + kAhead < kFrags) wq[f % kAhead] = frag(f + kAhead);
           f32x4 start = zero;
@@ -404,8 +406,8 @@ __global__ void __launch_bounds__(512, 2) trans_back_pairs_fast_kernel(TransBack
                 da[i >> 1] = __builtin_bit_cast(uint32_t, r.da);
                 db[i >> 1] = __builtin_bit_cast(uint32_t, r.db);
               }
-              reinterpret_cast<u32x2*>(&s_op[c & 1][share][0][p][lane])[tt] = da;
-              reinterpret_cast<u32x2*>(&s_op[c & 1][share][1][p][lane])[tt] = db;
+              reinterpret_cast<u32x2*>(&s_op[c & 1][pairs_share][0][p][lane])[tt] = da;
+              reinterpret_cast<u32x2*>(&s_op[c & 1][pairs_share][1][p][lane])[tt] = db;
             }
           }
           __builtin_amdgcn_sched_barrier(0);
@@ -434,6 +436,7 @@ __global__ void __launch_bounds__(512, 2) trans_back_pairs_fast_kernel(TransBack
       dma_b128(tr_res, c * kTrBytes + piece * 1024 + lane * 16, lds_addr(&s_tr[c & 1][piece * 1024]));
     }
   };
+  const bool multiplies = share < 4 / SPLIT;
   f32x4 acc[8][TILES];
   auto products = [&](int c) {
     const char* const chunk = s_tr[c & 1] + lane * 16;
@@ -524,7 +527,7 @@ __global__ void __launch_bounds__(512, 2) trans_back_pairs_fast_kernel(TransBack
   int64_t before = -1;
   for (int64_t grp = blockIdx.x; grp < n_groups; grp += gridDim.x, parity ^= 1) {
     barrier_lds();
-    if (before >= 0) finish(before, parity ^ 1);
+    if (before >= 0 && multiplies) finish(before, parity ^ 1);
 #pragma unroll
     for (int ct = 0; ct < 8; ++ct)
 #pragma unroll
@@ -536,13 +539,13 @@ __global__ void __launch_bounds__(512, 2) trans_back_pairs_fast_kernel(TransBack
       // transposes in that of the last but one
       copy_rows(c + 1 == kChunks ? 0 : c + 1);
       copy_tr(c);
-      if (c > 0) products(c - 1);
+      if (c > 0 && multiplies) products(c - 1);
       wait_vm<0>();
     }
     before = grp;
   }
   barrier_lds();
-  finish(before, parity ^ 1);
+  if (multiplies) finish(before, parity ^ 1);
 }
 
 // ----------------------------------------------------------------------------- sums over the pairs
@@ -762,17 +765,19 @@ __global__ void __launch_bounds__(512, 2) trans_back_sums_fast_kernel(TransBackA
         for (int i = 0; i < 4; ++i) part[part_at(m, ut, ct, i)] = t[m][ut][ct][i];
 }
 
-// Tiles per wave of dz's kernel: as many pairs a workgroup as leave none of the 256 CUs idle (a chunk of weights takes
-// 0.9 us for one tile a wave and 1.7 for four).
+// As many pairs a workgroup as leave none of the 256 CUs idle. A chunk of weights takes 0.9 us for a tile that two waves share
+// (8192 pairs: 19 us, 2025: 17), 1.1 for one tile a wave (22, 21), 1.7 for four.
 template <bool CODES>
 void launch_pairs(const TransBackArgs& a, hipStream_t st) {
   const int64_t one = (a.n_pairs + 63) / 64;
-  if (one <= 256)
-    hipLaunchKernelGGL((trans_back_pairs_fast_kernel<CODES, 1>), dim3((unsigned)one), dim3(512), 0, st, a);
+  if (one <= 128)
+    hipLaunchKernelGGL((trans_back_pairs_fast_kernel<CODES, 1, 2>), dim3((unsigned)((a.n_pairs + 31) / 32)), dim3(512), 0, st, a);
+  else if (one <= 256)
+    hipLaunchKernelGGL((trans_back_pairs_fast_kernel<CODES, 1, 1>), dim3((unsigned)one), dim3(512), 0, st, a);
   else if (one <= 512)
-    hipLaunchKernelGGL((trans_back_pairs_fast_kernel<CODES, 2>), dim3((unsigned)((one + 1) / 2)), dim3(512), 0, st, a);
+    hipLaunchKernelGGL((trans_back_pairs_fast_kernel<CODES, 2, 1>), dim3((unsigned)((one + 1) / 2)), dim3(512), 0, st, a);
   else
-    hipLaunchKernelGGL((trans_back_pairs_fast_kernel<CODES, 4>), dim3((unsigned)((one + 3) / 4 < 256 ? (one + 3) / 4 : 256)), dim3(512), 0, st, a);
+    hipLaunchKernelGGL((trans_back_pairs_fast_kernel<CODES, 4, 1>), dim3((unsigned)((one + 3) / 4 < 256 ? (one + 3) / 4 : 256)), dim3(512), 0, st, a);
 }
 
 }  // namespace
