@@ -401,58 +401,121 @@ __global__ void __launch_bounds__(256, CT > 8 ? 1 : 2) trans_back_pairs_kernel(T
     }
   }
   __syncthreads();
-  f32x4 dn[P][CT];
+  // a product waits for the one before it on the same sum: with one tile of pairs two sums, of even and of odd steps (4096 pairs of
+  // 128 channels: 53 -> 48 us)
+  constexpr int kWays = P == 1 && CT <= 8 ? 2 : 1;
+  f32x4 dn[P * kWays][CT];
 #pragma unroll
-  for (int p = 0; p < P; ++p)
+  for (int p = 0; p < P * kWays; ++p)
 #pragma unroll
     for (int j = 0; j < CT; ++j) dn[p][j] = zero;
-  for (int ht = wave; ht < hp / 16; ht += 4) {
-    const float* w = a.prep + (int64_t)(16 * ht + n) * cp + 4 * g;
-    f32x4 x[P], y[P], dh[P];
+  if constexpr (CT > 8) {  // one wave a SIMD: loads as far ahead as 512 registers let the compiler place them (a queue: half as fast)
+    for (int ht = wave; ht < hp / 16; ht += 4) {
+      const float* w = a.prep + (int64_t)(16 * ht + n) * cp + 4 * g;
+      f32x4 x[P], y[P], dh[P];
 #pragma unroll
-    for (int p = 0; p < P; ++p) x[p] = y[p] = dh[p] = zero;
+      for (int p = 0; p < P; ++p) x[p] = y[p] = dh[p] = zero;
 #pragma unroll
-    for (int j = 0; j < CT; ++j) {
-      if (16 * j >= cp) continue;
-      const f32x4 w1 = chunk(w + 16 * j), w2 = chunk(w + size + 16 * j), w3 = chunk(w + 2 * size + 16 * j);
+      for (int j = 0; j < CT; ++j) {
+        if (16 * j >= cp) continue;
+        const f32x4 w1 = chunk(w + 16 * j), w2 = chunk(w + size + 16 * j), w3 = chunk(w + 2 * size + 16 * j);
 #pragma unroll
-      for (int p = 0; p < P; ++p) {
-        const f32x4 nv = s.in.n[p][j][lane], dv = s.in.d[p][j][lane];
+        for (int p = 0; p < P; ++p) {
+          const f32x4 nv = s.in.n[p][j][lane], dv = s.in.d[p][j][lane];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          x[p] = mfma4(w1[i], nv[i], x[p]);
-          y[p] = mfma4(w2[i], nv[i], y[p]);
-          dh[p] = mfma4(w3[i], dv[i], dh[p]);
+          for (int i = 0; i < 4; ++i) {
+            x[p] = mfma4(w1[i], nv[i], x[p]);
+            y[p] = mfma4(w2[i], nv[i], y[p]);
+            dh[p] = mfma4(w3[i], dv[i], dh[p]);
+          }
         }
       }
-    }
-#pragma unroll
-    for (int p = 0; p < P; ++p)
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const Gated r = gated(x[p][i], y[p][i], dh[p][i]);
-        x[p][i] = r.da;
-        y[p][i] = r.db;
-      }
-    const float* wt = a.prep + 3 * size + (int64_t)n * hp + 16 * ht + 4 * g;
-#pragma unroll
-    for (int j = 0; j < CT; ++j) {
-      if (16 * j >= cp) continue;
-      const f32x4 w1 = chunk(wt + (int64_t)16 * j * hp), w2 = chunk(wt + size + (int64_t)16 * j * hp);
 #pragma unroll
       for (int p = 0; p < P; ++p)
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          dn[p][j] = mfma4(w1[i], x[p][i], dn[p][j]);
-          dn[p][j] = mfma4(w2[i], y[p][i], dn[p][j]);
+          const Gated r = gated(x[p][i], y[p][i], dh[p][i]);
+          x[p][i] = r.da;
+          y[p][i] = r.db;
         }
+      const float* wt = a.prep + 3 * size + (int64_t)n * hp + 16 * ht + 4 * g;
+#pragma unroll
+      for (int j = 0; j < CT; ++j) {
+        if (16 * j >= cp) continue;
+        const f32x4 w1 = chunk(wt + (int64_t)16 * j * hp), w2 = chunk(wt + size + (int64_t)16 * j * hp);
+#pragma unroll
+        for (int p = 0; p < P; ++p)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            dn[p][j] = mfma4(w1[i], x[p][i], dn[p][j]);
+            dn[p][j] = mfma4(w2[i], y[p][i], dn[p][j]);
+          }
+      }
+    }
+  } else {
+    // Weights of a tile of units in the order of their use: rows of W1, W2 and W3^T at 16 channels each, then of the
+    // transposes. They come from L2, five ahead across the tiles (36864 pairs: 316 us without, 20 ahead spill).
+    constexpr int kFrags = 5 * CT, kAhead = 5;
+    const int last = hp / 16 - 1;
+    auto frag = [&](int ht, int f) {
+      const int j = f < 3 * CT ? f / 3 : (f - 3 * CT) / 2, m = f < 3 * CT ? f % 3 : 3 + (f - 3 * CT) % 2, in = 16 * j < cp ? j : 0;
+      ht = min(ht, last);
+      return chunk(a.prep + m * size + (m < 3 ? (int64_t)(16 * ht + n) * cp + 16 * in : (int64_t)(16 * in + n) * hp + 16 * ht) + 4 * g);
+    };
+    f32x4 wq[kAhead];
+#pragma unroll
+    for (int f = 0; f < kAhead; ++f) wq[f] = frag(wave, f);
+#pragma unroll 1
+    for (int ht = wave; ht <= last; ht += 4) {
+      f32x4 h[3][P * kWays];
+#pragma unroll
+      for (int m = 0; m < 3; ++m)
+#pragma unroll
+        for (int p = 0; p < P * kWays; ++p) h[m][p] = zero;
+#pragma unroll
+      for (int f = 0; f < kFrags; ++f) {
+        const f32x4 w = wq[f % kAhead];
+        wq[f % kAhead] = f + kAhead < kFrags ? frag(ht, f + kAhead) : frag(ht + 4, f + kAhead - kFrags);
+        if (f < 3 * CT) {
+          const int j = f / 3, m = f % 3;
+          f32x4 v[P];
+          if (16 * j < cp)
+#pragma unroll
+            for (int p = 0; p < P; ++p) v[p] = m < 2 ? s.in.n[p][j][lane] : s.in.d[p][j][lane];
+          if (16 * j < cp)
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+#pragma unroll
+              for (int p = 0; p < P; ++p) h[m][p + i % kWays] = mfma4(w[i], v[p][i], h[m][p + i % kWays]);
+        } else {
+          const int j = (f - 3 * CT) / 2, m = (f - 3 * CT) % 2;
+          if (16 * j < cp)
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+#pragma unroll
+              for (int p = 0; p < P; ++p) dn[p + i % kWays][j] = mfma4(w[i], h[m][p][i], dn[p + i % kWays][j]);
+        }
+        if (f == 3 * CT - 1)
+#pragma unroll
+          for (int p = 0; p < P; ++p)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              if (kWays == 2)
+#pragma unroll
+                for (int m = 0; m < 3; ++m) h[m][p][i] += h[m][p + kWays - 1][i];
+              const Gated r = gated(h[0][p][i], h[1][p][i], h[2][p][i]);
+              h[0][p][i] = r.da;
+              h[1][p][i] = r.db;
+            }
+        __builtin_amdgcn_sched_barrier(0);
+      }
     }
   }
   __syncthreads();  // N and dout have been read
 #pragma unroll
   for (int p = 0; p < P; ++p)
 #pragma unroll
-    for (int j = 0; j < CT; ++j) s.red[wave][p][j][lane] = dn[p][j];
+    for (int j = 0; j < CT; ++j) s.red[wave][p][j][lane] = kWays == 2 ? dn[p][j] + dn[p + kWays - 1][j] : dn[p][j];
   __syncthreads();
   if (wave >= P) return;
   const int64_t pair = (tile0 + wave) * 16 + n;
@@ -612,10 +675,11 @@ hipError_t launch_trans_back_gen(const TransBackArgs& a, hipStream_t st) {
     if (e != hipSuccess) return e;
   }
   if (!a.dz) return hipSuccess;
-  if (a.c > 128) return launch_pairs<16, 1>(a, st);
+  // Two tiles of pairs share the weights' loads, unless that leaves CUs idle (256 channels: 4096 pairs 250 us with one, 326 with
+  // two; 20000 pairs 1208 and 971).
   if (a.n_pairs <= 4096)
-    return a.c > 64 ? launch_pairs<8, 1>(a, st) : a.c > 32 ? launch_pairs<4, 1>(a, st) : launch_pairs<2, 1>(a, st);
-  return a.c > 64 ? launch_pairs<8, 2>(a, st) : a.c > 32 ? launch_pairs<4, 2>(a, st) : launch_pairs<2, 2>(a, st);
+    return a.c > 128 ? launch_pairs<16, 1>(a, st) : a.c > 64 ? launch_pairs<8, 1>(a, st) : a.c > 32 ? launch_pairs<4, 1>(a, st) : launch_pairs<2, 1>(a, st);
+  return a.c > 128 ? launch_pairs<16, 2>(a, st) : a.c > 64 ? launch_pairs<8, 2>(a, st) : a.c > 32 ? launch_pairs<4, 2>(a, st) : launch_pairs<2, 2>(a, st);
 }
 
 hipError_t launch_trans_back_finish(const TransBackArgs& a, hipStream_t st) {
