@@ -515,7 +515,14 @@ int dcp_pair_transition_backward_workspace_size(int64_t n_pairs, int32_t c_z, in
  * aligned to their element size, and 16 bytes are fastest. What is written (the gradients
  * and the workspace) must not overlap the inputs or each other, but for dz = dz_out.
  * Without pairs the weights' gradients are 0, and z and dz_out may be NULL.
- * act_dtype = F32: fp32 throughout. */
+ * act_dtype = F32: fp32 throughout. act_dtype = BF16: the products' operands have 11 bits
+ * (fp16 with powers of two of each pair and each unit, so of any magnitude), sigmoids, sums
+ * and statistics are fp32, and a gradient's error is little more than its own rounding. dz
+ * has that precision for each pair; in the sums over the pairs dz_out counts down to 2^-24
+ * of the largest of all pairs, and a unit's part of dz down to 2^-24 of what the largest
+ * weights of all units could make of it.
+ * The results do not depend on the stream or on which gradients are asked for, and repeat
+ * bit by bit. */
 int dcp_pair_transition_backward(int64_t n_pairs, int32_t c_z, int32_t hidden, int32_t act_dtype, float ln_eps,
                                  const float* w1, const float* w2, const float* w3, const float* ln_gamma,
                                  const float* ln_beta, const void* z, const uint8_t* z_exponents, const void* dz_out,

@@ -5,8 +5,8 @@ the transition's weights and the attention's bias. Against 64 bits (GPU).
 
 Tolerances, of the 2-norm of the error relative to that of the result. The reference takes z as the encoding rounds it, and
 what the checkpoint reads back as the transition's input, so neither counts. fp32: 2e-5, twice that of one backward pass
-alone. bf16: the table's gradient is a sum of two gradients, each rounded to bf16 with what its pass is off by (7.4e-3 the
-transition's, 1e-2 the attention's), of independent errors: 1.3e-2; the others as in their own tests."""
+alone. bf16: the table's gradient is a sum of two gradients, each rounded to bf16 with what its pass is off by (3.6e-3 the
+transition's, 1e-2 the attention's), of independent errors: 1.1e-2; the others as in their own tests."""
 import math
 
 import pytest
@@ -118,4 +118,4 @@ def test_a_step(t):
     e = {"table": err(dtable, want_table), "w_b": err(dw_b, want_b), "grad": err(grad, back[0])}
     e.update({k: err(a, b) for k, a, b in zip(("w1", "w2", "w3", "gamma", "beta"), dw, back[1:])})
     print(t, {k: "%.2e" % v for k, v in e.items()}, flush=True)
-    assert all(v <= (2e-5 if t == "f32" else 1.3e-2 if k == "table" else 1e-2 if k == "w_b" else 7.4e-3) for k, v in e.items()), e
+    assert all(v <= (2e-5 if t == "f32" else 1.1e-2 if k == "table" else 1e-2 if k == "w_b" else 3.6e-3) for k, v in e.items()), e
