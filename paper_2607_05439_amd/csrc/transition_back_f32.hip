@@ -88,7 +88,8 @@ __device__ __forceinline__ f32x4 load4(const TransBackArgs& a, const void* x, bo
 // A workgroup takes 64 units (16 a wave) and a share of the tiles of 16 pairs. A wave keeps its
 // units' rows of W1, W2 and W3^T and its sums in registers. A, B and dH come out as pairs 4g + i
 // (rows) of unit n (column), which is the A operand of the products over the pairs: step i has
-// pair 4g + i in k-slot g. Their B operand is zh or dout of that pair at channel 16j + n, from LDS.
+// pair 4g + i in k-slot g. Their B operand is zh or dout of that pair at channel 16j + n, from LDS. Bound by the matrix cores where
+// there are many pairs (65536 of 32 channels and 128 units 53 us), by the loads' latency of a tile below (16384: 21 us).
 template <int CT>
 __global__ void __launch_bounds__(256, CT > 8 ? 1 : 2) trans_back_sums_kernel(TransBackArgs a) {
   constexpr int kC = 16 * CT, kRow = kC + 4;
@@ -218,7 +219,8 @@ __global__ void __launch_bounds__(256, CT > 8 ? 1 : 2) trans_back_sums_kernel(Tr
 
 // The same for 65 to 128 channels: there the weights and sums of a wave leave no room for a second wave on its SIMD (36864
 // pairs of 128 channels and 512 units: 410 us). The weights of the 64 units lie in LDS instead, for eight waves,
-// of which four take one tile of 16 pairs and four another, with sums of their own: a workgroup's two parts.
+// of which four take one tile of 16 pairs and four another, with sums of their own: a workgroup's two parts. 298 us, the matrix
+// cores 72% busy; they wait for the rows' statistics, which all waves form between two barriers.
 constexpr int kWideTiles = 8;  // of 16 channels
 __global__ void __launch_bounds__(512, 2) trans_back_sums_wide_kernel(TransBackArgs a) {
   constexpr int CT = kWideTiles, kRow = 16 * CT + 4;
@@ -345,7 +347,8 @@ __global__ void __launch_bounds__(512, 2) trans_back_sums_wide_kernel(TransBackA
 // A workgroup takes P tiles of 16 pairs; its waves take every fourth tile of 16 units. The
 // products are transposed (units by pairs), so that A, B and dH lie as the B operands of the
 // products with W1^T and W2^T, and dN as z does: channels 16j + 4g .. of pair n. The waves' dN
-// meet in LDS.
+// meet in LDS. 36864 pairs of 128 channels and 512 units: 277 us, the matrix cores 72% busy; 1152 workgroups are two rounds
+// and a quarter.
 template <int CT, int P>
 __global__ void __launch_bounds__(256, CT > 8 ? 1 : 2) trans_back_pairs_kernel(TransBackArgs a) {
   __shared__ union {
