@@ -132,16 +132,17 @@ __global__ void __launch_bounds__(256) relative_kernel(RelativeArgs a) {
 // ----------------------------------------------------------------------------- the table's gradient
 // dtable = one-hot^T dz on the matrix cores: v_mfma_f32_16x16x32_bf16 with 16 buckets of one field as rows, 32 pairs
 // as k-slots and 16 channels as columns. A one-hot's products are exact, and so are fp32 gradients in three bf16 pieces
-// (8 bits each); the sums are fp32, in an order that the sizes alone fix. Only the tiles of buckets that occur
-// among the 32 pairs are multiplied: near the diagonal three or four of twelve, elsewhere one a field.
+// (8 bits each); the sums are fp32, in an order that the sizes and the fields alone fix. Only the tiles of buckets that
+// occur among the 32 pairs are multiplied, near the diagonal three or four of twelve. Where the 32 pairs are alike in all
+// fields, as most are far from it, their sum alone is formed, on as long as the next 32 are like them, and then added to its
+// buckets: with a product per field and twelve comparisons every time 2400 x 4800 pairs took 909 us, twice what the loads alone do.
 //   A workgroup takes consecutive tiles of 128 S pairs of a row (fp32: 64 S) and 32 CG channels (S CG = 4): CG
 // waves take 32 channels each, and S such sets a share of the pairs, each with sums of its own. dz comes through
 // registers, a tile ahead, into LDS as [pair][channel], whose transposing reads bring 16 channels of eight pairs as a B operand;
 // k-slot 8g + j is pair 4g + j of the 32 for j < 4, 16 + 4g + j - 4 for j >= 4. Wave f finds the buckets of field f, a
 // byte of each pair's word in LDS.
 //   A value that is not finite would make NaN of every bucket (0 times infinity): it enters as 0 and is added to its
-// own buckets afterwards. 2400 x 4800 pairs of 128 channels in bf16: 909 us, 3.3 TB/s, bound by the latency of a tile's
-// loads, LDS and barriers at two workgroups a CU; the sums of twelve tiles of buckets leave no registers for a third.
+// own buckets afterwards. 2400 x 4800 pairs of 128 channels in bf16: 470 us, 6.3 TB/s, bound by memory (453 without the sums).
 constexpr int kWindow = 12;  // tiles of buckets at a time: the paper's fields have 5 + 5 + 1 + 1
 
 typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
@@ -192,6 +193,16 @@ __global__ void __launch_bounds__(256, 2) relative_back_kernel(RelativeArgs a) {
   constexpr int kLanes = kPairs / 64;  // pairs of a tile that a lane finds the bucket of
   u32x4 raw[kMine];
   int32_t pos_i, grp_i, pos_j[kLanes], grp_j[kLanes];
+  auto places = [&](int64_t row, int64_t j0) {
+    pos_i = position[a.row0 + row];
+    grp_i = group ? group[a.row0 + row] : 0;
+#pragma unroll
+    for (int s = 0; s < kLanes; ++s) {
+      const int64_t j = min(j0 + 64 * s + lane, a.n_tok - 1);
+      pos_j[s] = position[j];
+      grp_j[s] = group ? group[j] : 0;
+    }
+  };
   auto fetch = [&]() {
     const T* const base = dz + (row * a.n_tok + j0) * a.c;
     const int left = (int)min((int64_t)kPairs, a.n_tok - j0);
@@ -217,20 +228,16 @@ __global__ void __launch_bounds__(256, 2) relative_back_kernel(RelativeArgs a) {
           }
       }
     }
-    pos_i = position[a.row0 + row];
-    grp_i = group ? group[a.row0 + row] : 0;
-#pragma unroll
-    for (int s = 0; s < kLanes; ++s) {
-      const int64_t j = min(j0 + 64 * s + lane, a.n_tok - 1);
-      pos_j[s] = position[j];
-      grp_j[s] = group ? group[j] : 0;
-    }
+    if (VEC) places(row, j0);
     j0 += kPairs;
     if (j0 >= a.n_tok) {
       j0 = 0;
       ++row;
     }
   };
+  // 32 pairs that are alike in all fields are summed whole, and on as long as the next are like them
+  f32x4 run[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
+  uint32_t run_of = 0;  // their buckets; sums of 0 at first
   for (int k = tid; k < kPairs; k += 256) s_b[k] = 0;  // bytes of fields that are not there: alike in all pairs
   if (todo > 0) fetch();
   for (int64_t k_tile = 0; k_tile < todo; ++k_tile) {
@@ -273,6 +280,7 @@ __global__ void __launch_bounds__(256, 2) relative_back_kernel(RelativeArgs a) {
         for (int q = 0; q < kPlanes; ++q) *reinterpret_cast<u32x2*>(to + q * kPlane) = u32x2{piece[q][0], piece[q][1]};
       }
     }
+    if (!VEC) places(this_row, this_j0);  // a tile ahead there are no registers for them
     if (wave < a.n_fields)
 #pragma unroll
       for (int s = 0; s < kLanes; ++s)
@@ -306,28 +314,39 @@ __global__ void __launch_bounds__(256, 2) relative_back_kernel(RelativeArgs a) {
       const u32x4 b0 = *reinterpret_cast<const u32x4*>(&s_b[p0 + 4 * g]), b1 = *reinterpret_cast<const u32x4*>(&s_b[p0 + 16 + 4 * g]);
       const uint32_t one = (uint32_t)__builtin_amdgcn_readfirstlane((int)buckets);
       const bool alike = __builtin_amdgcn_ballot_w64(buckets != one) == 0;
+      if (!alike || one != run_of) {
 #pragma unroll
-      for (int w = 0; w < kWindow; ++w) {
-        u32x4 hot;
-        if (alike) {
-          const uint32_t b = one >> shift[w] & 255;
-          if (b >> 4 != place[w]) continue;
-          const uint32_t v = (b & 15) == (uint32_t)n ? 0x3F803F80u : 0u;
-          hot = u32x4{v, v, v, v};
-        } else {
-          if (__builtin_amdgcn_ballot_w64((buckets >> shift[w] >> 4 & 15) == place[w]) == 0) continue;
+        for (int w = 0; w < kWindow; ++w) {
+          if ((run_of >> shift[w] >> 4 & 15) == place[w]) {
+            const int row = (int)(run_of >> shift[w] & 15) - 4 * g;
+#pragma unroll
+            for (int ct = 0; ct < 2; ++ct)
+#pragma unroll
+              for (int i = 0; i < 4; ++i) acc[w][ct][i] += row == i ? run[ct][i] : 0.0f;
+          }
+          if (alike || __builtin_amdgcn_ballot_w64((buckets >> shift[w] >> 4 & 15) == place[w]) == 0) continue;
           const uint32_t want = 16 * place[w] + (uint32_t)n;
           auto is = [&](uint32_t b, uint32_t v) { return (b >> shift[w] & 255) == want ? v : 0u; };
+          u32x4 hot;
 #pragma unroll
           for (int i = 0; i < 2; ++i) {
             hot[i] = is(b0[2 * i], 0x3F80u) | is(b0[2 * i + 1], 0x3F800000u);
             hot[2 + i] = is(b1[2 * i], 0x3F80u) | is(b1[2 * i + 1], 0x3F800000u);
           }
+#pragma unroll
+          for (int q = 0; q < kPlanes; ++q)
+#pragma unroll
+            for (int ct = 0; ct < 2; ++ct) acc[w][ct] = mfma32(as_bf16x8(hot), d[q][ct], acc[w][ct]);
         }
+        run_of = one;
+        run[0] = run[1] = f32x4{0.f, 0.f, 0.f, 0.f};
+      }
+      if (alike) {
+        const bf16x8 ones = as_bf16x8(u32x4{0x3F803F80u, 0x3F803F80u, 0x3F803F80u, 0x3F803F80u});
 #pragma unroll
         for (int q = 0; q < kPlanes; ++q)
 #pragma unroll
-          for (int ct = 0; ct < 2; ++ct) acc[w][ct] = mfma32(as_bf16x8(hot), d[q][ct], acc[w][ct]);
+          for (int ct = 0; ct < 2; ++ct) run[ct] = mfma32(ones, d[q][ct], run[ct]);
       }
     }
     if (s_bad[0] | s_bad[1] | s_bad[2] | s_bad[3]) {
@@ -362,12 +381,15 @@ __global__ void __launch_bounds__(256, 2) relative_back_kernel(RelativeArgs a) {
 #pragma unroll
   for (int w = 0; w < kWindow; ++w) {
     if (w0 + w >= a.n_tiles) continue;
+    const uint32_t of_tile = (run_of >> shift[w] & 255) - 16u * place[w];  // of none: not below 16
 #pragma unroll
     for (int ct = 0; ct < 2; ++ct) {
       const int c = c0 + 32 * cg + 16 * ct + n;
       if (c < a.c)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) a.parts[(part * a.n_tiles * 16 + (w0 + w) * 16 + 4 * g + i) * a.c + c] = acc[w][ct][i];
+        for (int i = 0; i < 4; ++i)
+          a.parts[(part * a.n_tiles * 16 + (w0 + w) * 16 + 4 * g + i) * a.c + c] =
+              acc[w][ct][i] + (of_tile == (uint32_t)(4 * g + i) ? run[ct][i] : 0.0f);
     }
   }
 }

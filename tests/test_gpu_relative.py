@@ -91,8 +91,9 @@ def gradient(fields, row0, rows, dz):
     count = torch.zeros(n_buckets(fields), dtype=torch.float64, device="cuda")
     flat = dz.reshape(-1, dz.shape[2]).double()
     for b in buckets(fields, row0, rows):
-        out.index_add_(0, b.flatten(), flat)
-        count.index_add_(0, b.flatten(), torch.ones(b.numel(), dtype=torch.float64, device="cuda"))
+        hot = torch.zeros((out.shape[0], b.numel()), dtype=torch.float64, device="cuda").scatter_(0, b.flatten()[None], 1.0)
+        out += hot @ flat
+        count += hot.sum(dim=1)
     return out, count
 
 
@@ -272,3 +273,24 @@ def test_more_threads_than_one_launch_holds():
     dcp.dcp_relative_position(n, 0, n, 1, dcp.DCP_BF16, dcp.make_relative_fields(fields), table, None, z)
     for rows in (slice(0, 100), slice(30000, 30100), slice(n - 2000, n)):
         assert torch.equal(z[rows, :, 0].float(), table[:, 0][buckets(fields, rows.start, rows.stop - rows.start)[0]])
+
+
+@pytest.mark.parametrize("t", ["f32", "bf16"])
+@pytest.mark.parametrize("radii", [(0,), (32, 32, 2, 0), (127, 127)])
+def test_long_runs_of_alike_pairs(radii, t):
+    """Few groups, so that most blocks of pairs are alike in all fields, over rows and tiles, and the runs end in each way:
+    at a group's end, at the diagonal, at a value that is not finite and at a workgroup's last pair."""
+    import torch
+    n = 700
+    token = torch.arange(n)
+    fields = [((token // 7).int().cuda(), (token // (100 * (f + 1))).int().cuda(), r) for f, r in enumerate(radii)]
+    dz = torch.randn((n, n, 40), generator=torch.Generator().manual_seed(23)).to(dtypes()[t]).cuda()
+    clean = Backward(n, 0, n, 40, t, fields, dz)().clone()
+    check_gradient(clean, fields, 0, n, dz, (radii, t))
+    dz[300, 650, 7] = float("-inf")
+    got, hit = Backward(n, 0, n, 40, t, fields, dz)(), torch.zeros_like(clean, dtype=torch.bool)
+    for b in buckets(fields, 300, 1):
+        hit[b[0, 650], 7] = True
+    assert (got[hit] == float("-inf")).all()
+    dz[300, 650, 7] = 0.0
+    assert torch.equal(got[~hit], Backward(n, 0, n, 40, t, fields, dz)()[~hit])
