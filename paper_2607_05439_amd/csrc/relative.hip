@@ -133,16 +133,19 @@ __global__ void __launch_bounds__(256) relative_kernel(RelativeArgs a) {
 // dtable = one-hot^T dz on the matrix cores: v_mfma_f32_16x16x32_bf16 with 16 buckets of one field as rows, 32 pairs
 // as k-slots and 16 channels as columns. A one-hot's products are exact, and so are fp32 gradients in three bf16 pieces
 // (8 bits each); the sums are fp32, in an order that the sizes and the fields alone fix. Only the tiles of buckets that
-// occur among the 32 pairs are multiplied, near the diagonal three or four of twelve. Where the 32 pairs are alike in all
-// fields, as most are far from it, their sum alone is formed, on as long as the next 32 are like them, and then added to its
-// buckets: with a product per field and twelve comparisons every time 2400 x 4800 pairs took 909 us, twice what the loads alone do.
+// occur among the 32 pairs are multiplied, near the diagonal three or four of twelve. 32 pairs with the same buckets in all
+// fields, or with two kinds of them, as most have far from the diagonal, are summed by kind ("class"), up to 16 kinds
+// side by side in one tile, and the kinds' sums added to their buckets when there is no room for another and at the end: two
+// products where a product per field took eight and twelve comparisons. (2400 x 4800 pairs of 60 chains: 909 us so, 749 with one kind at
+// a time, which is the better for one long chain, 500 to 635.)
 //   A workgroup takes consecutive tiles of 128 S pairs of a row (fp32: 64 S) and 32 CG channels (S CG = 4): CG
 // waves take 32 channels each, and S such sets a share of the pairs, each with sums of its own. dz comes through
 // registers, a tile ahead, into LDS as [pair][channel], whose transposing reads bring 16 channels of eight pairs as a B operand;
 // k-slot 8g + j is pair 4g + j of the 32 for j < 4, 16 + 4g + j - 4 for j >= 4. Wave f finds the buckets of field f, a
 // byte of each pair's word in LDS.
 //   A value that is not finite would make NaN of every bucket (0 times infinity): it enters as 0 and is added to its
-// own buckets afterwards. 2400 x 4800 pairs of 128 channels in bf16: 470 us, 6.3 TB/s, bound by memory (453 without the sums).
+// own buckets afterwards. 2400 x 4800 pairs of 128 channels in bf16: 600 us, 5.0 TB/s; 453 without the products, 6.5: bound by memory and
+// by the chains of comparisons between them.
 constexpr int kWindow = 12;  // tiles of buckets at a time: the paper's fields have 5 + 5 + 1 + 1
 
 typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
@@ -235,9 +238,34 @@ __global__ void __launch_bounds__(256, 2) relative_back_kernel(RelativeArgs a) {
       ++row;
     }
   };
-  // 32 pairs that are alike in all fields are summed whole, and on as long as the next are like them
+  // Sums of up to 16 classes, of pairs that are alike in all fields: row n of `run` is that of the buckets `cls` of lane n
   f32x4 run[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
-  uint32_t run_of = 0;  // their buckets; sums of 0 at first
+  uint32_t cls = 0;
+  int n_cls = 0;
+  // Their sums to those of the buckets of window tile w: a class is k-slot g of step i = 4g + i, so that `run` is the B operands as
+  // it lies. of: the classes' buckets, of this lane's k-slots.
+  auto clamp_run = [&]() {  // past fp32's range: as its largest number, as 0 times infinity would make NaN of other buckets
+#pragma unroll
+    for (int ct = 0; ct < 2; ++ct)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) run[ct][i] = __builtin_amdgcn_fmed3f(run[ct][i], -3.402823466e38f, 3.402823466e38f);
+  };
+  auto end_classes = [&](const uint32_t (&of)[4], int w, f32x4 (&to)[2]) {
+    float hot[4];
+    bool any = false;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const bool here = 4 * g + i < n_cls && (of[i] >> shift[w] >> 4 & 15) == place[w];
+      hot[i] = here && (of[i] >> shift[w] & 15) == (uint32_t)n ? 1.0f : 0.0f;
+      any |= here;
+    }
+    if (__builtin_amdgcn_ballot_w64(any) == 0) return;
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+      for (int ct = 0; ct < 2; ++ct)
+        to[ct] = __builtin_amdgcn_mfma_f32_16x16x4f32(hot[i], run[ct][i], to[ct], 0, 0, 0);
+  };
   for (int k = tid; k < kPairs; k += 256) s_b[k] = 0;  // bytes of fields that are not there: alike in all pairs
   if (todo > 0) fetch();
   for (int64_t k_tile = 0; k_tile < todo; ++k_tile) {
@@ -313,18 +341,20 @@ __global__ void __launch_bounds__(256, 2) relative_back_kernel(RelativeArgs a) {
         }
       const u32x4 b0 = *reinterpret_cast<const u32x4*>(&s_b[p0 + 4 * g]), b1 = *reinterpret_cast<const u32x4*>(&s_b[p0 + 16 + 4 * g]);
       const uint32_t one = (uint32_t)__builtin_amdgcn_readfirstlane((int)buckets);
-      const bool alike = __builtin_amdgcn_ballot_w64(buckets != one) == 0;
-      if (!alike || one != run_of) {
+      const uint32_t two = (uint32_t)__builtin_amdgcn_readlane((int)buckets, 31);
+      const bool few = __builtin_amdgcn_ballot_w64(buckets != one && buckets != two) == 0;
+      const bool has_one = (__builtin_amdgcn_ballot_w64(cls == one) & ((1u << n_cls) - 1)) != 0, has_two = (__builtin_amdgcn_ballot_w64(cls == two) & ((1u << n_cls) - 1)) != 0;
+      const bool full = few && !(has_one && has_two) && n_cls > 14;
+      if (!few || full) {
+        uint32_t of[4] = {0, 0, 0, 0};
+        if (full) clamp_run();
+        if (full)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) of[i] = (uint32_t)__shfl((int)cls, 4 * g + i);
 #pragma unroll
         for (int w = 0; w < kWindow; ++w) {
-          if ((run_of >> shift[w] >> 4 & 15) == place[w]) {
-            const int row = (int)(run_of >> shift[w] & 15) - 4 * g;
-#pragma unroll
-            for (int ct = 0; ct < 2; ++ct)
-#pragma unroll
-              for (int i = 0; i < 4; ++i) acc[w][ct][i] += row == i ? run[ct][i] : 0.0f;
-          }
-          if (alike || __builtin_amdgcn_ballot_w64((buckets >> shift[w] >> 4 & 15) == place[w]) == 0) continue;
+          if (full) end_classes(of, w, acc[w]);
+          if (few || __builtin_amdgcn_ballot_w64((buckets >> shift[w] >> 4 & 15) == place[w]) == 0) continue;
           const uint32_t want = 16 * place[w] + (uint32_t)n;
           auto is = [&](uint32_t b, uint32_t v) { return (b >> shift[w] & 255) == want ? v : 0u; };
           u32x4 hot;
@@ -338,16 +368,32 @@ __global__ void __launch_bounds__(256, 2) relative_back_kernel(RelativeArgs a) {
 #pragma unroll
             for (int ct = 0; ct < 2; ++ct) acc[w][ct] = mfma32(as_bf16x8(hot), d[q][ct], acc[w][ct]);
         }
-        run_of = one;
+        if (!few) continue;
         run[0] = run[1] = f32x4{0.f, 0.f, 0.f, 0.f};
+        n_cls = 0;
       }
-      if (alike) {
-        const bf16x8 ones = as_bf16x8(u32x4{0x3F803F80u, 0x3F803F80u, 0x3F803F80u, 0x3F803F80u});
-#pragma unroll
-        for (int q = 0; q < kPlanes; ++q)
-#pragma unroll
-          for (int ct = 0; ct < 2; ++ct) run[ct] = mfma32(ones, d[q][ct], run[ct]);
+      if (full || !has_one) {
+        cls = n == n_cls ? one : cls;
+        ++n_cls;
       }
+      if ((full || !has_two) && two != one) {
+        cls = n == n_cls ? two : cls;
+        ++n_cls;
+      }
+      const bool used = n < n_cls;
+      auto is = [&](uint32_t b, uint32_t v) { return used && b == cls ? v : 0u; };
+      const uint32_t v = is(one, 0x3F803F80u);
+      u32x4 hot = {v, v, v, v};
+      if (one != two)
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          hot[i] = is(b0[2 * i], 0x3F80u) | is(b0[2 * i + 1], 0x3F800000u);
+          hot[2 + i] = is(b1[2 * i], 0x3F80u) | is(b1[2 * i + 1], 0x3F800000u);
+        }
+#pragma unroll
+      for (int q = 0; q < kPlanes; ++q)
+#pragma unroll
+        for (int ct = 0; ct < 2; ++ct) run[ct] = mfma32(as_bf16x8(hot), d[q][ct], run[ct]);
     }
     if (s_bad[0] | s_bad[1] | s_bad[2] | s_bad[3]) {
 #pragma unroll 1
@@ -378,18 +424,20 @@ __global__ void __launch_bounds__(256, 2) relative_back_kernel(RelativeArgs a) {
     }
   }
   const int64_t part = (int64_t)blockIdx.x * S + stream;
+  uint32_t of[4];
+  clamp_run();
+#pragma unroll
+  for (int i = 0; i < 4; ++i) of[i] = (uint32_t)__shfl((int)cls, 4 * g + i);
 #pragma unroll
   for (int w = 0; w < kWindow; ++w) {
     if (w0 + w >= a.n_tiles) continue;
-    const uint32_t of_tile = (run_of >> shift[w] & 255) - 16u * place[w];  // of none: not below 16
+    end_classes(of, w, acc[w]);
 #pragma unroll
     for (int ct = 0; ct < 2; ++ct) {
       const int c = c0 + 32 * cg + 16 * ct + n;
       if (c < a.c)
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
-          a.parts[(part * a.n_tiles * 16 + (w0 + w) * 16 + 4 * g + i) * a.c + c] =
-              acc[w][ct][i] + (of_tile == (uint32_t)(4 * g + i) ? run[ct][i] : 0.0f);
+        for (int i = 0; i < 4; ++i) a.parts[(part * a.n_tiles * 16 + (w0 + w) * 16 + 4 * g + i) * a.c + c] = acc[w][ct][i];
     }
   }
 }

@@ -294,3 +294,31 @@ def test_long_runs_of_alike_pairs(radii, t):
     assert (got[hit] == float("-inf")).all()
     dz[300, 650, 7] = 0.0
     assert torch.equal(got[~hit], Backward(n, 0, n, 40, t, fields, dz)()[~hit])
+
+
+@pytest.mark.parametrize("t", ["f32", "bf16"])
+@pytest.mark.parametrize("width", [16, 31, 32, 77])
+def test_many_classes_of_alike_pairs(width, t):
+    """Blocks of pairs with two kinds of buckets at most, but more kinds in a stripe than are summed side by side."""
+    import torch
+    n, rows = 650, 90
+    token = torch.arange(n)
+    fields = [((token // width).int().cuda(), None, 127), ((token // width % 5).int().cuda(), (token // width % 3).int().cuda(), 3)]
+    dz = torch.randn((rows, n, 72), generator=torch.Generator().manual_seed(24)).to(dtypes()[t]).cuda()
+    got = Backward(n, 500, rows, 72, t, fields, dz)().clone()
+    check_gradient(got, fields, 500, rows, dz, (width, t))
+    assert torch.equal(Backward(n, 500, rows, 72, t, fields, dz)(), got)
+
+
+def test_sums_past_the_largest_number_stay_in_their_buckets():
+    import torch
+    n = 192
+    token = torch.arange(n, dtype=torch.int32, device="cuda")
+    fields = [(token // 64, None, 2)]
+    dz = torch.ones((n, n, 32), dtype=torch.bfloat16, device="cuda")
+    dz[64:128, :64, 3] = 3e38  # bucket 3: 1 to the left
+    got = Backward(n, 0, n, 32, "bf16", fields, dz)()
+    want = torch.tensor([1, 2, 3, 2, 1, 0], device="cuda")[:, None].expand(6, 32) * 4096.0
+    assert got[3, 3] >= 3e38
+    got[3, 3] = want[3, 3]
+    assert torch.equal(got, want)
