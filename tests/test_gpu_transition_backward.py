@@ -397,3 +397,39 @@ def test_f32_more_threads_than_one_launch_holds():
     assert not got["dz"][:-tail].any()
     got["dz"] = got["dz"][-tail:]
     check(got, want, "f32", "2^29 pairs")
+
+
+@pytest.mark.parametrize("saved", ["whole", "checkpoint"])
+def test_more_pairs_than_are_taken_at_a_time_in_place(saved):
+    """2^20 pairs and a few: in dout's place, and without dz, the bits of the call with a buffer of its own."""
+    import torch
+    n = (1 << 20) + 100
+    x = make(1, 128, 512, "bf16", seed=20)
+    g = torch.Generator(device="cuda").manual_seed(21)
+    for k in ("z", "dout"):
+        x[k] = torch.randn((n, 128), generator=g, device="cuda", dtype=torch.bfloat16)
+    x = checkpointed(x) if saved == "checkpoint" else x
+    want = {k: v.clone() for k, v in Call(x)().items()}
+    sums = Call(x, want=NAMES[1:])()
+    assert all(torch.equal(sums[k], want[k]) for k in NAMES[1:])
+    got = Call({**x, "dout": x["dout"].clone()}, in_place=True)()
+    assert all(torch.equal(got[k], want[k]) for k in NAMES)
+
+
+@pytest.mark.parametrize("t,c,hidden", [("f32", 32, 64), ("bf16", 128, 512)])
+def test_two_calls_at_once(t, c, hidden):
+    """Calls on two streams with workspaces of their own do not touch each other."""
+    import torch
+    calls = [Call(make(20000 + 777 * k, c, hidden, t, seed=22 + k)) for k in range(2)]
+    want = [{k: v.clone() for k, v in call().items()} for call in calls]
+    streams = [torch.cuda.Stream() for _ in calls]
+    for turn in range(3):
+        for call in calls:
+            for v in call.out.values():
+                v.fill_(7.0)
+        torch.cuda.synchronize()
+        for _ in range(4):
+            for call, stream in zip(calls, streams):
+                call(stream=stream)
+        torch.cuda.synchronize()
+        assert all(torch.equal(call.out[k], w[k]) for call, w in zip(calls, want) for k in NAMES), turn
