@@ -518,9 +518,11 @@ int dcp_pair_transition_backward_workspace_size(int64_t n_pairs, int32_t c_z, in
  * act_dtype = F32: fp32 throughout. act_dtype = BF16: the products' operands have 11 bits
  * (fp16 with powers of two of each pair and each unit, so of any magnitude), sigmoids, sums
  * and statistics are fp32, and a gradient's error is little more than its own rounding. dz
- * has that precision for each pair; in the sums over the pairs dz_out counts down to 2^-24
- * of the largest of all pairs, and a unit's part of dz down to 2^-24 of what the largest
- * weights of all units could make of it.
+ * has that precision for each pair; a unit's part of it counts in steps of 2^-24 of what an
+ * open gate and the largest weights of all units could make of it, so that a shut gate's part
+ * loses bits below a sigmoid of 2^-14 (A < -9.7). The weights' gradients have that precision
+ * for each unit by itself, down to sigmoids of e^-66; in them dz_out counts in steps of 2^-24 of
+ * the largest of all pairs.
  * The results do not depend on the stream or on which gradients are asked for, and repeat
  * bit by bit. */
 int dcp_pair_transition_backward(int64_t n_pairs, int32_t c_z, int32_t hidden, int32_t act_dtype, float ln_eps,

@@ -13,7 +13,9 @@
 //   A unit's rows of W1 diag(gamma), W2 diag(gamma) and W3^T have powers of two 2^e1, 2^e2, 2^e3 that bring their
 //   largest magnitudes (and 1/16 of the biases) below 1: then |A'|, |B'| <= 144, |dH'| <= 128 for |dout'| <= 1, and
 //   dA', dB', H' stay under 2^15 whatever the weights are.
-//   dout has a power of two per pair where dz is formed, and one for all pairs where their products are summed.
+//   dout has a power of two per pair where dz is formed, and one for all pairs where their products are summed. There the
+//   sigmoids, of which dA', dB' and H' each have one factor, have a power of two of the unit's where its gates are shut, so that
+//   the largest stays in fp16's range (trans_back_sums_fast_kernel).
 //   A unit's row in the transposed weights carries 2^-(e1 + e2 + e3), relative to the largest of all units.
 // All are taken out of the sums at the end, exactly.
 #include <hip/hip_runtime.h>
@@ -191,20 +193,32 @@ __global__ void __launch_bounds__(256) trans_back_transpose_kernel(TransBackArgs
   }
 }
 
-// Two elements' h0 = A and h1 = B with their powers of two (k: A's inverse, log: -log2(e) times it). With s = sigmoid(A)
-// and A' = h0: H' = A' s B', dB' = dH A' s, dA' = dH B' (s + k A' s (1 - s)). The sigmoid is fp32, what follows packed fp16: the
-// seven roundings of 2^-12 in dA' together are a third of its rounding to bf16, and the vector work, which does not overlap
-// with the products, falls by a quarter.
+// Two elements' A', B', dH' (a, b, d; k: the inverse of A's power of two). With s = sigmoid(A): H' = A' s B', dB' = dH' A' s,
+// dA' = dH' B' (s + k A' s (1 - s)). The sigmoid is fp32, what follows packed fp16: the seven roundings of at most 2^-11 in dA'
+// together are a third of its rounding to bf16, and the vector work, which does not overlap with the products, falls by a quarter.
+// k (1 - s) is formed in fp16 where dz is (an open gate's A > 7 multiplies s's rounding by A there: 1.2e-3 of dA in the root mean
+// square, bf16's rounding 1.6e-3); the sums over the pairs take 1 - s from fp32, and s with a factor of its own.
 typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
 struct Gated {
   f16x2 h, da, db;
 };
-__device__ __forceinline__ Gated gated(float a0, float a1, float b0, float b1, float d0, float d1, f16x2 k, float log0, float log1) {
-  const f16x2 s = {(_Float16)__builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(a0 * log0)),
-                   (_Float16)__builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(a1 * log1))};
-  const f16x2 a = {(_Float16)a0, (_Float16)a1}, b = {(_Float16)b0, (_Float16)b1}, d = {(_Float16)d0, (_Float16)d1};
-  const f16x2 silu = a * s, slope = __builtin_elementwise_fma(silu, __builtin_elementwise_fma(-k, s, k), s);
+__device__ __forceinline__ f16x2 pair_of(float x, float y) { return f16x2{(_Float16)x, (_Float16)y}; }
+__device__ __forceinline__ Gated gated(f16x2 a, f16x2 b, f16x2 d, f16x2 s, f16x2 k_rest) {
+  const f16x2 silu = a * s, slope = __builtin_elementwise_fma(silu, k_rest, s);
   return {silu * b, d * b * slope, d * silu};
+}
+__device__ __forceinline__ Gated gated_pairs(float a0, float a1, float b0, float b1, float d0, float d1, f16x2 k, float log0, float log1) {
+  const f16x2 s = pair_of(__builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(a0 * log0)),
+                          __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(a1 * log1)));
+  return gated(pair_of(a0, a1), pair_of(b0, b1), pair_of(d0, d1), s, __builtin_elementwise_fma(-k, s, k));
+}
+// For the sums: the sigmoids as s / shut, 1 / shut the unit's power of two; top: the largest yet.
+__device__ __forceinline__ Gated gated_sums(float a0, float a1, float b0, float b1, float d0, float d1, f16x2 k, float log, float shut,
+                                            float& top) {
+  const float s0 = __builtin_amdgcn_rcpf(fmaf(__builtin_amdgcn_exp2f(a0 * log), shut, shut));
+  const float s1 = __builtin_amdgcn_rcpf(fmaf(__builtin_amdgcn_exp2f(a1 * log), shut, shut));
+  top = fmaxf(fmaxf(top, s0), s1);
+  return gated(pair_of(a0, a1), pair_of(b0, b1), pair_of(d0, d1), pair_of(s0, s1), k * pair_of(fmaf(-shut, s0, 1.0f), fmaf(-shut, s1, 1.0f)));
 }
 
 // ----------------------------------------------------------------------------- rows
@@ -404,8 +418,8 @@ __global__ void __launch_bounds__(512, 2) trans_back_pairs_fast_kernel(TransBack
               u32x2 da, db;
 #pragma unroll
               for (int i = 0; i < 4; i += 2) {
-                const Gated r = gated(h[0][p][i], h[0][p][i + 1], h[1][p][i], h[1][p][i + 1], h[2][p][i], h[2][p][i + 1],
-                                      f16x2{(_Float16)ka[i], (_Float16)ka[i + 1]}, kl[i], kl[i + 1]);
+                const Gated r = gated_pairs(h[0][p][i], h[0][p][i + 1], h[1][p][i], h[1][p][i + 1], h[2][p][i], h[2][p][i + 1],
+                                            pair_of(ka[i], ka[i + 1]), kl[i], kl[i + 1]);
                 da[i >> 1] = __builtin_bit_cast(uint32_t, r.da);
                 db[i >> 1] = __builtin_bit_cast(uint32_t, r.db);
               }
@@ -566,6 +580,12 @@ constexpr int kOpBytes = 4 * 6 * 1024;  // dA', dB', H'
 constexpr int kAheadSteps = 4;
 constexpr int kStepSlots = kAheadSteps + 2;  // and those whose products and whose sums are formed
 constexpr int kStepDma = kStepBytes / 1024 / 4;
+// A unit's amplification 1 / shut = 2^k. |A'|, |B'| <= 144 and |dH'| <= 128 leave 3.5 for s (1 + |A|) / shut in fp16, and |A| is at
+// most 89 where s is not 0: s / shut may be kTop where k > 0 (1 where k = 0, as s (1 + |A| (1 - s)) is 1.1 at most). The largest of
+// a step is brought to 2^-8 at least, two to three bits below kTop, so that k seldom changes again.
+constexpr float kTop = 1.0f / 32;
+constexpr int kTopBits = 7;
+constexpr int kMostBits = 96;  // below this a gate loses its bits in the end
 
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
@@ -573,6 +593,9 @@ typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
 __global__ void __launch_bounds__(512, 2) trans_back_sums_fast_kernel(TransBackArgs a) {
   __shared__ __attribute__((aligned(16))) char s_x[kStepSlots * kStepBytes];
   __shared__ __attribute__((aligned(16))) char s_op[2 * kOpBytes];
+  __shared__ __attribute__((aligned(16))) float s_turn[2][4][32];  // [step parity][share]: factors of the units' sums before this step
+  __shared__ __attribute__((aligned(16))) float s_end[4][32];      // and after the last
+  __shared__ int s_turns[2][4];                                    // whether there are any
   const int tid = threadIdx.x, lane = tid & 63, n = lane & 15, g = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), share = wave & 3;
   const int chunk = blockIdx.y * (kSlice / 32) + share;  // this wave's 32 units
@@ -600,13 +623,9 @@ __global__ void __launch_bounds__(512, 2) trans_back_sums_fast_kernel(TransBackA
       bb[ut] = units[kUnitBiasB * kHid];
     }
     auto sum_at = [&](int m, int ut, int i) { return 3 * kSize + m * kHid + 32 * chunk + 16 * ut + 4 * g + i; };
-    f32x4 s[2][2];  // S1, S2: every column of dA^T ones
-#pragma unroll
-    for (int m = 0; m < 2; ++m)
-#pragma unroll
-      for (int ut = 0; ut < 2; ++ut)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) s[m][ut][i] = a.add_parts ? part[sum_at(m, ut, i)] : 0.0f;
+    f32x4 s[2][2] = {{zero, zero}, {zero, zero}};  // S1, S2: every column of dA^T ones
+    int bits[2] = {0, 0};                          // k of unit n
+    float shut[2] = {1.0f, 1.0f};                  // 2^-k
     f16x8 ones;
 #pragma unroll
     for (int i = 0; i < 8; ++i) ones[i] = (_Float16)1.0f;
@@ -614,45 +633,82 @@ __global__ void __launch_bounds__(512, 2) trans_back_sums_fast_kernel(TransBackA
     const char* cur = s_x;
     for (int it = 0; it < count; ++it) {
       barrier_lds();
-      // the first tile of pairs, then the second, and between its products what follows from the first
-      auto row = [&](int q, int m) { return as_f16x8(*reinterpret_cast<const u32x4*>(cur + (q >> 2) * 8192 + m * 4096 + (q & 3) * 1024 + row_at)); };
-      f32x4 h[3][2][2];
       u32x4 op[3][2];
-      auto gate = [&](int ut, int p, int i) {  // pairs i, i + 1 of this lane's four
-        const Gated r = gated(h[0][ut][p][i], h[0][ut][p][i + 1], h[1][ut][p][i], h[1][ut][p][i + 1], h[2][ut][p][i], h[2][ut][p][i + 1],
-                              k[ut], kl[ut], kl[ut]);
-        op[0][ut][2 * p + i / 2] = __builtin_bit_cast(uint32_t, r.da);
-        op[1][ut][2 * p + i / 2] = __builtin_bit_cast(uint32_t, r.db);
-        op[2][ut][2 * p + i / 2] = __builtin_bit_cast(uint32_t, r.h);
-      };
-      constexpr int kQueue = 3;
-      f16x8 zq[kQueue], dq[kQueue];
+      float turn[2] = {1.0f, 1.0f};
+      bool turned = false;
+      for (;;) {  // once, and again where a unit's k changes: at the first step to what its gates need, then down alone, at most to 0
+        float top[2] = {0.0f, 0.0f};
+        // the first tile of pairs, then the second, and between its products what follows from the first
+        auto row = [&](int q, int m) { return as_f16x8(*reinterpret_cast<const u32x4*>(cur + (q >> 2) * 8192 + m * 4096 + (q & 3) * 1024 + row_at)); };
+        f32x4 h[3][2][2];
+        auto gate = [&](int ut, int p, int i) {  // pairs i, i + 1 of this lane's four
+          const Gated r = gated_sums(h[0][ut][p][i], h[0][ut][p][i + 1], h[1][ut][p][i], h[1][ut][p][i + 1], h[2][ut][p][i], h[2][ut][p][i + 1],
+                                     k[ut], kl[ut], shut[ut], top[ut]);
+          op[0][ut][2 * p + i / 2] = __builtin_bit_cast(uint32_t, r.da);
+          op[1][ut][2 * p + i / 2] = __builtin_bit_cast(uint32_t, r.db);
+          op[2][ut][2 * p + i / 2] = __builtin_bit_cast(uint32_t, r.h);
 #pragma unroll
-      for (int q = 0; q < kQueue - 1; ++q) {
-        zq[q] = row(q, 0);
-        dq[q] = row(q, 1);
+          for (int m = 0; m < 3; ++m) asm volatile("" : "+v"(op[m][ut][2 * p + i / 2]));  // here, beside the products, not behind the loop
+        };
+        constexpr int kQueue = 3;
+        f16x8 zq[kQueue], dq[kQueue];
+#pragma unroll
+        for (int q = 0; q < kQueue - 1; ++q) {
+          zq[q] = row(q, 0);
+          dq[q] = row(q, 1);
+        }
+#pragma unroll
+        for (int q = 0; q < 8; ++q) {
+          const int p = q >> 2, ks = q & 3;
+          if (q + kQueue - 1 < 8) {
+            zq[(q + kQueue - 1) % kQueue] = row(q + kQueue - 1, 0);
+            dq[(q + kQueue - 1) % kQueue] = row(q + kQueue - 1, 1);
+          }
+#pragma unroll
+          for (int ut = 0; ut < 2; ++ut) {
+            h[0][ut][p] = mfma(zq[q % kQueue], w[0][ut][ks], ks ? h[0][ut][p] : f32x4{ba[ut], ba[ut], ba[ut], ba[ut]});
+            h[1][ut][p] = mfma(zq[q % kQueue], w[1][ut][ks], ks ? h[1][ut][p] : f32x4{bb[ut], bb[ut], bb[ut], bb[ut]});
+            h[2][ut][p] = mfma(dq[q % kQueue], w[2][ut][ks], ks ? h[2][ut][p] : zero);
+          }
+          if (q >= 4) gate(q & 1, 0, (q - 4) & 2);
+          __builtin_amdgcn_sched_barrier(0);
+        }
+#pragma unroll
+        for (int i = 0; i < 4; i += 2) {
+          gate(0, 1, i);
+          gate(1, 1, i);
+        }
+        const bool first = it == 0 && !turned;
+        if (!first && __builtin_amdgcn_ballot_w64((bits[0] > 0 && top[0] > kTop) || (bits[1] > 0 && top[1] > kTop)) == 0) break;
+        bool again = false;
+#pragma unroll
+        for (int ut = 0; ut < 2; ++ut) {
+          const float most = max4(top[ut]);
+          int e = -2 * kMostBits;
+          if (most > 0.0f) (void)frexpf(most, &e);
+          if (!first && !(bits[ut] > 0 && most > kTop)) continue;
+          const int to = min(max(bits[ut] - e - kTopBits, 0), kMostBits);
+          turn[ut] *= ldexpf(1.0f, to - bits[ut]);
+          again |= to != bits[ut];
+          bits[ut] = to;
+          shut[ut] = ldexpf(1.0f, -to);
+        }
+        if (__builtin_amdgcn_ballot_w64(again) == 0) break;
+        turned = true;
       }
-#pragma unroll
-      for (int q = 0; q < 8; ++q) {
-        const int p = q >> 2, ks = q & 3;
-        if (q + kQueue - 1 < 8) {
-          zq[(q + kQueue - 1) % kQueue] = row(q + kQueue - 1, 0);
-          dq[(q + kQueue - 1) % kQueue] = row(q + kQueue - 1, 1);
+      if (turned) {
+        if (g == 0) {
+          s_turn[it & 1][share][n] = turn[0];
+          s_turn[it & 1][share][16 + n] = turn[1];
         }
 #pragma unroll
         for (int ut = 0; ut < 2; ++ut) {
-          h[0][ut][p] = mfma(zq[q % kQueue], w[0][ut][ks], ks ? h[0][ut][p] : f32x4{ba[ut], ba[ut], ba[ut], ba[ut]});
-          h[1][ut][p] = mfma(zq[q % kQueue], w[1][ut][ks], ks ? h[1][ut][p] : f32x4{bb[ut], bb[ut], bb[ut], bb[ut]});
-          h[2][ut][p] = mfma(dq[q % kQueue], w[2][ut][ks], ks ? h[2][ut][p] : zero);
+          const f32x4 by = *reinterpret_cast<const f32x4*>(&s_turn[it & 1][share][16 * ut + 4 * g]);
+          s[0][ut] *= by;
+          s[1][ut] *= by;
         }
-        if (q >= 4) gate(q & 1, 0, (q - 4) & 2);
-        __builtin_amdgcn_sched_barrier(0);
       }
-#pragma unroll
-      for (int i = 0; i < 4; i += 2) {
-        gate(0, 1, i);
-        gate(1, 1, i);
-      }
+      s_turns[it & 1][share] = turned;
 #pragma unroll
       for (int m = 0; m < 3; ++m)
 #pragma unroll
@@ -663,14 +719,21 @@ __global__ void __launch_bounds__(512, 2) trans_back_sums_fast_kernel(TransBackA
         for (int ut = 0; ut < 2; ++ut) s[m][ut] = mfma(as_f16x8(op[m][ut]), ones, s[m][ut]);
       cur = cur + kStepBytes == s_x + kStepSlots * kStepBytes ? s_x : cur + kStepBytes;
     }
+    if (g == 0) {
+      s_end[share][n] = shut[0];
+      s_end[share][16 + n] = shut[1];
+    }
     barrier_lds();
     if (n == 0)
 #pragma unroll
-      for (int m = 0; m < 2; ++m)
+      for (int ut = 0; ut < 2; ++ut) {
+        const f32x4 end = *reinterpret_cast<const f32x4*>(&s_end[share][16 * ut + 4 * g]);
 #pragma unroll
-        for (int ut = 0; ut < 2; ++ut)
+        for (int m = 0; m < 2; ++m)
 #pragma unroll
-          for (int i = 0; i < 4; ++i) part[sum_at(m, ut, i)] = s[m][ut][i];
+          for (int i = 0; i < 4; ++i)
+            part[sum_at(m, ut, i)] = fmaf(s[m][ut][i], end[i], a.add_parts ? part[sum_at(m, ut, i)] : 0.0f);
+      }
     return;
   }
   // ---- the sums of the step before, and the copies of the steps to come: pieces 4 share .. of a step's 16
@@ -697,15 +760,6 @@ __global__ void __launch_bounds__(512, 2) trans_back_sums_fast_kernel(TransBackA
     for (int ut = 0; ut < 2; ++ut)
 #pragma unroll
       for (int ct = 0; ct < 8; ++ct) t[m][ut][ct] = zero;
-  if (a.add_parts)  // the pairs before these
-#pragma unroll
-    for (int m = 0; m < 3; ++m)
-#pragma unroll
-      for (int ut = 0; ut < 2; ++ut)
-#pragma unroll
-        for (int ct = 0; ct < 8; ++ct)
-#pragma unroll
-          for (int i = 0; i < 4; ++i) t[m][ut][ct][i] = part[part_at(m, ut, ct, i)];
   // a column read's piece: pair 4g + n / 4, channels 4 (n % 4) .. of 16; the chunk of 8 is that of group 2 (ct % 2) + n / 2 % 2
   const int piece_odd = (n >> 1) & 1;
   const int col_at = piece_odd * 256 + ((4 * g + (n >> 2)) ^ (8 * piece_odd)) * 16 + 8 * (n & 1);
@@ -719,6 +773,15 @@ __global__ void __launch_bounds__(512, 2) trans_back_sums_fast_kernel(TransBackA
     barrier_lds();  // and every other wave's; the step before the last has been read
     if (it + kAheadSteps < count) copy(it + kAheadSteps);
     if (it == 0) continue;
+    if (__builtin_amdgcn_readfirstlane(s_turns[(it - 1) & 1][share]))
+#pragma unroll
+      for (int ut = 0; ut < 2; ++ut) {
+        const f32x4 by = *reinterpret_cast<const f32x4*>(&s_turn[(it - 1) & 1][share][16 * ut + 4 * g]);
+#pragma unroll
+        for (int m = 0; m < 3; ++m)
+#pragma unroll
+          for (int ct = 0; ct < 8; ++ct) t[m][ut][ct] *= by;
+      }
     f16x8 op[3][2];
 #pragma unroll
     for (int m = 0; m < 3; ++m)
@@ -765,7 +828,11 @@ __global__ void __launch_bounds__(512, 2) trans_back_sums_fast_kernel(TransBackA
 #pragma unroll
       for (int ct = 0; ct < 8; ++ct)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) part[part_at(m, ut, ct, i)] = t[m][ut][ct][i];
+        for (int i = 0; i < 4; ++i) {
+          const float sum = t[m][ut][ct][i] * s_end[share][16 * ut + 4 * g + i];
+          float* const to = part + part_at(m, ut, ct, i);
+          *to = a.add_parts ? *to + sum : sum;  // the pairs before these
+        }
 }
 
 // As many pairs a workgroup as leave none of the 256 CUs idle. A chunk of weights takes 0.9 us for a tile that two waves share

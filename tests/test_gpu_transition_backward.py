@@ -433,3 +433,129 @@ def test_two_calls_at_once(t, c, hidden):
                 call(stream=stream)
         torch.cuda.synchronize()
         assert all(torch.equal(call.out[k], w[k]) for call, w in zip(calls, want) for k in NAMES), turn
+
+
+# ----------------------------------------------------------------------------- each unit by itself
+def unit_rows(grads):
+    """[3, hidden, c]: each unit's row of W1's and W2's gradients and column of W3's, in 64 bits."""
+    import torch
+    return torch.stack([grads["dw1"].double(), grads["dw2"].double(), grads["dw3"].double().T])
+
+
+def unit_scales(x):
+    """[2, 3, hidden], of the terms dA N, dB N and H dout of each unit and of those terms' slopes in A: the root of the sum of
+    their squares, or the norm of their sum where that is more."""
+    import torch
+    z, dout = values(x), x["dout"].double()
+    zh = (z - z.mean(dim=1, keepdim=True)) / torch.sqrt(z.var(dim=1, keepdim=True, correction=0) + EPS)
+    n = zh * x["gamma"].double() + x["beta"].double()
+    a, b, dh = n @ x["w1"].double().T, n @ x["w2"].double().T, dout @ x["w3"].double()
+    s = 1 / (1 + torch.exp(-a))
+    silu, slope, bend = a * s, s + a * s * (1 - s), s * (1 - s) * (2 + a * (1 - 2 * s))
+    terms = ((dh * b * slope, n), (dh * silu, n), (silu * b, dout)), ((dh * b * bend, n), (dh * slope, n), (slope * b, dout))
+    return torch.stack([torch.stack([torch.maximum((f.square() * v.square().sum(dim=1)[:, None]).sum(dim=0).sqrt(), (f.T @ v).norm(dim=1))
+                                     for f, v in t]) for t in terms])
+
+
+def check_units(x, got, want, t, what, units=slice(None), off=None):
+    """Each unit by itself. Its row is a sum over the pairs of terms of either sign, by chance far smaller than the terms make
+    likely (with a beta of 4 each row is mostly beta times a sum of numbers, which may be near 0 for one unit of many), or up to
+    three times larger. The errors of zh, dout and the gate are independent from pair to pair and add up to the terms' relative error
+    times the root of the sum of their squares; those of a unit's weights are the same for all pairs and add up to that
+    times the sum itself. The larger of the two is what the error is measured by. The terms' relative error is that of the
+    tensors. Beside it stands that of A, `off`, which their slopes in A multiply alike. bf16: A is a sum of c products w zh of two operands of 11 bits, each off by
+    0.42 2^-11 in the root mean square; here |w| < 0.3 and zh is about 1: 0.3 sqrt(2 128) 0.42 2^-11 = 1e-3; twice that, as
+    for the tensors. fp32: A's partial sums are up to 60 here, and A is off by 2^-22 60 at most."""
+    off = {"bf16": 2e-3, "f32": 60 * 2.0 ** -22}[t] if off is None else off
+    error, (term, slope) = (unit_rows(got) - unit_rows(want)).norm(dim=2), unit_scales(x)
+    most = (TOL[t] * term + off * slope).clamp(min=1e-300)
+    part, rel = (error / most)[:, units], (error / term.clamp(min=1e-300))[:, units]
+    print(what, "dw1, dw2, dw3: errors by the terms up to", ["%.2e" % float(v) for v in rel.max(dim=1).values],
+          "of the limit up to", ["%.2f" % float(v) for v in part.max(dim=1).values], flush=True)
+    assert float(part.max()) <= 1.0, what
+
+
+@pytest.mark.parametrize("saved", ["whole", "checkpoint"])
+@pytest.mark.parametrize("t,c,hidden", [("f32", 32, 64), ("bf16", 128, 512)])
+def test_units_whose_gates_are_shut_keep_their_precision(t, c, hidden, saved):
+    """Units with A ~ N(m, 1), m from 0 to -60: a shut gate's sigmoid is as small as e^-62, and so is all that its unit has of
+    a gradient; of its own size that is as precise as any other's."""
+    import torch
+    x = make(3000, c, hidden, t, seed=30, offset=0.0)
+    x["gamma"], x["beta"] = torch.ones(c, device="cuda"), torch.full((c,), 4.0, device="cuda")
+    m = torch.tensor([0.0, -4.0, -8.0, -10.0, -12.0, -14.0, -16.0, -18.0, -22.0, -30.0, -45.0, -60.0], device="cuda")
+    m = m[torch.arange(hidden, device="cuda") % len(m)]
+    x["w1"] = x["w1"] - x["w1"].mean(dim=1, keepdim=True) + m[:, None] / (4 * c)
+    x = checkpointed(x) if saved == "checkpoint" else x
+    check_units(x, Call(x, "f32")(), reference(x), t, (t, saved))
+
+
+@pytest.mark.parametrize("pairs", [2000, 20000, (1 << 20) + 5000])
+@pytest.mark.parametrize("order", ["open", "shut", "any"])
+def test_gates_that_open_or_shut_along_the_pairs(order, pairs):
+    """A from -57 to -3 in every fourth unit, from pair to pair in order, backwards or in any: what is small at first is
+    far more at the end, over steps, shares and the pairs that are taken at a time. The rows of z have a root mean square of 1
+    up to their own rounding, and zh is z times 1 + d, |d| < 2^-9: rounded to 11 bits much of a row loses the same part of up to 2^-12,
+    so its errors are not independent, and A's 30 of the first half against the second are off by 30 2^-12 at most."""
+    import torch
+    x = make(1, 128, 512, "bf16", seed=34)
+    g = torch.Generator(device="cuda").manual_seed(35)
+    x["gamma"], x["beta"] = torch.ones(128, device="cuda"), torch.full((128,), 4.0, device="cuda")
+    half = torch.cat([torch.ones(64, device="cuda"), -torch.ones(64, device="cuda")])
+    along = torch.linspace(-0.9, 0.9, pairs, device="cuda")
+    along = along.flip(0) if order == "shut" else along[torch.randperm(pairs, generator=g, device="cuda")] if order == "any" else along
+    z = torch.randn((pairs, 128), generator=g, device="cuda")
+    z = z - z.mean(dim=1, keepdim=True)
+    z = z - (z @ half / 128)[:, None] * half
+    z = z / z.square().mean(dim=1, keepdim=True).sqrt()
+    x["z"] = (along[:, None] * half + (1 - along.square()).sqrt()[:, None] * z).to(torch.bfloat16)
+    x["dout"] = torch.randn((pairs, 128), generator=g, device="cuda", dtype=torch.bfloat16)
+    units = torch.arange(512, device="cuda") % 4 == 0
+    w = x["w1"] - x["w1"].mean(dim=1, keepdim=True)
+    w = w - (w @ half / 128)[:, None] * half
+    x["w1"] = torch.where(units[:, None], w + (30.0 / 128) * half - 30.0 / 512, w)
+    got, want = Call(x, "f32")(), reference(x)
+    check_units(x, got, want, "bf16", (order, pairs), off=30 * 2.0 ** -12)
+    again = Call(x, "f32", want=NAMES[1:])()
+    assert all(torch.equal(again[k], got[k]) for k in NAMES[1:])
+
+
+def gradients_of_rounded_operands(x):
+    """The gradients in 64 bits by the formulas, with zh and the rows of W1 diag(gamma), W2 diag(gamma) and W3^T (each of a
+    power of two of its own) rounded to 11 bits as the products' operands are."""
+    import torch
+    half = lambda v: v.to(torch.float16).double()  # noqa: E731
+
+    def rows(w):
+        e = torch.frexp(w.abs().amax(dim=1, keepdim=True)).exponent.double()
+        return half(w * torch.pow(2.0, -e)) * torch.pow(2.0, e)
+
+    z, dout, ga, be = values(x), x["dout"].double(), x["gamma"].double(), x["beta"].double()
+    mu = z.mean(dim=1, keepdim=True)
+    rstd = 1 / torch.sqrt(((z - mu) ** 2).mean(dim=1, keepdim=True) + EPS)
+    exact, zh = (z - mu) * rstd, half((z - mu) * rstd)
+    w1, w2 = x["w1"].double(), x["w2"].double()
+    r1, r2, r3 = rows(w1 * ga), rows(w2 * ga), rows(x["w3"].double().T.contiguous())
+    a, b, dh = zh @ r1.T + w1 @ be, zh @ r2.T + w2 @ be, dout @ r3.T
+    s = 1 / (1 + torch.exp(-a))
+    h, db, da = a * s * b, dh * a * s, dh * b * (s + a * s * (1 - s))
+    g = da @ r1 + db @ r2
+    t1, t2, s1, s2 = da.T @ zh, db.T @ zh, da.sum(dim=0), db.sum(dim=0)
+    return {"dz": dout + rstd * (g - g.mean(dim=1, keepdim=True) - exact * (g * exact).mean(dim=1, keepdim=True)),
+            "dw1": t1 * ga + s1[:, None] * be, "dw2": t2 * ga + s2[:, None] * be, "dw3": dout.T @ h,
+            "dgamma": (w1 * t1 + w2 * t2).sum(dim=0), "dbeta": w1.T @ s1 + w2.T @ s2}
+
+
+@pytest.mark.parametrize("mean", [0.0, 3.0, 5.0, 8.0])
+@pytest.mark.parametrize("factor", [1.0, 4.0, 16.0])
+def test_open_and_saturated_gates(factor, mean):
+    """Large W1, and gates that are open (A ~ N(mean, factor)): sigmoid and slope have the error of A's operands, |A| times
+    theirs. Beside the gradients of operands that are rounded alike that is left out, and what remains are the roundings of the
+    gate and of the results: within the tensors' tolerance, whatever A is."""
+    import torch
+    x = make(2000, 128, 512, "bf16", seed=32, offset=0.0)
+    x["beta"] = torch.full((128,), 4.0, device="cuda")
+    x["w1"] = (x["w1"] - x["w1"].mean(dim=1, keepdim=True)) * factor + mean / 512
+    got, want = Call(x, "f32")(), gradients_of_rounded_operands(x)
+    check(got, want, "bf16", (factor, mean))
+    check_units(x, got, want, "bf16", (factor, mean), off=0.0)
