@@ -521,8 +521,9 @@ int dcp_pair_transition_backward_workspace_size(int64_t n_pairs, int32_t c_z, in
  * has that precision for each pair; a unit's part of it counts in steps of 2^-24 of what an
  * open gate and the largest weights of all units could make of it, so that a shut gate's part
  * loses bits below a sigmoid of 2^-14 (A < -9.7). The weights' gradients have that precision
- * for each unit by itself, down to sigmoids of e^-66; in them dz_out counts in steps of 2^-24 of
- * the largest of all pairs.
+ * for each unit by itself: there a pair's part, whose size is that of its largest |dz_out| times
+ * the unit's sigmoid, counts in steps of 2^-16 or less of the unit's largest part, as long as that
+ * is above 2^-96 of what the largest dz_out of all pairs makes at an open gate.
  * The results do not depend on the stream or on which gradients are asked for, and repeat
  * bit by bit. */
 int dcp_pair_transition_backward(int64_t n_pairs, int32_t c_z, int32_t hidden, int32_t act_dtype, float ln_eps,

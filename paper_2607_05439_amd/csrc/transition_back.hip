@@ -13,9 +13,9 @@
 //   A unit's rows of W1 diag(gamma), W2 diag(gamma) and W3^T have powers of two 2^e1, 2^e2, 2^e3 that bring their
 //   largest magnitudes (and 1/16 of the biases) below 1: then |A'|, |B'| <= 144, |dH'| <= 128 for |dout'| <= 1, and
 //   dA', dB', H' stay under 2^15 whatever the weights are.
-//   dout has a power of two per pair where dz is formed, and one for all pairs where their products are summed. There the
-//   sigmoids, of which dA', dB' and H' each have one factor, have a power of two of the unit's where its gates are shut, so that
-//   the largest stays in fp16's range (trans_back_sums_fast_kernel).
+//   dout has a power of two per pair, 2^e. In the sums over the pairs that is brought to 2^d, of the largest of all pairs, by
+//   2^(d - e) in the sigmoids, of which dA', dB' and H' each have one factor; and where a unit's gates are shut (or its pairs small)
+//   they have a power of two of the unit's on top, so that its largest stays in fp16's range (trans_back_sums_fast_kernel).
 //   A unit's row in the transposed weights carries 2^-(e1 + e2 + e3), relative to the largest of all units.
 // All are taken out of the sums at the end, exactly.
 #include <hip/hip_runtime.h>
@@ -212,13 +212,14 @@ __device__ __forceinline__ Gated gated_pairs(float a0, float a1, float b0, float
                           __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(a1 * log1)));
   return gated(pair_of(a0, a1), pair_of(b0, b1), pair_of(d0, d1), s, __builtin_elementwise_fma(-k, s, k));
 }
-// For the sums: the sigmoids as s / shut, 1 / shut the unit's power of two; top: the largest yet.
+// For the sums: the sigmoids as f s / shut, f each pair's factor (at most 1), 1 / shut the unit's; top: the largest yet.
 __device__ __forceinline__ Gated gated_sums(float a0, float a1, float b0, float b1, float d0, float d1, f16x2 k, float log, float shut,
-                                            float& top) {
+                                            float f0, float f1, float& top) {
   const float s0 = __builtin_amdgcn_rcpf(fmaf(__builtin_amdgcn_exp2f(a0 * log), shut, shut));
   const float s1 = __builtin_amdgcn_rcpf(fmaf(__builtin_amdgcn_exp2f(a1 * log), shut, shut));
-  top = fmaxf(fmaxf(top, s0), s1);
-  return gated(pair_of(a0, a1), pair_of(b0, b1), pair_of(d0, d1), pair_of(s0, s1), k * pair_of(fmaf(-shut, s0, 1.0f), fmaf(-shut, s1, 1.0f)));
+  const float t0 = s0 * f0, t1 = s1 * f1;
+  top = fmaxf(fmaxf(top, t0), t1);
+  return gated(pair_of(a0, a1), pair_of(b0, b1), pair_of(d0, d1), pair_of(t0, t1), k * pair_of(fmaf(-shut, s0, 1.0f), fmaf(-shut, s1, 1.0f)));
 }
 
 // ----------------------------------------------------------------------------- rows
@@ -303,16 +304,17 @@ __device__ __forceinline__ void scale_row(const u32x4 (&d)[4], f16x8 (&v)[4], in
 }
 
 // What the sums read of a tile of 16 pairs, 8 KB: [zh | dout][ks][lane] 16 B in fp16, with the pairs of odd groups 8
-// places on, which spreads the LDS reads of columns over all banks. dout has the power of two of all pairs, to which
-// `factor` takes the row's (0 for pairs past the last).
+// places on, which spreads the LDS reads of columns over all banks. dout has the power of two of its row, 2^e; the row's factor
+// takes that to the one of all pairs (0 for pairs past the last).
 __device__ __forceinline__ int column_lane(int n, int g) { return 16 * g + (n ^ (8 * (g & 1))); }
-__device__ __forceinline__ _Float16 row_factor(const TransBackArgs& a, int64_t pair, int e) {
-  return pair < a.n_pairs ? (_Float16)ldexpf(1.0f, dout_exponent(a) - e) : (_Float16)0.0f;
-}
-__device__ __forceinline__ void store_rows(const TransBackArgs& a, int64_t tile, int ks, int n, int g, f16x8 zf, f16x8 d, _Float16 factor) {
-  u32x4* const to = reinterpret_cast<u32x4*>(a.zh) + tile * 512 + ks * 64 + column_lane(n, g);
-  to[0] = __builtin_bit_cast(u32x4, zf);
-  to[256] = __builtin_bit_cast(u32x4, (f16x8)(d * factor));
+__device__ __forceinline__ void store_rows(const TransBackArgs& a, int64_t tile, int n, int g, const f16x8 (&zf)[4], const f16x8 (&d)[4], int e) {
+  u32x4* const to = reinterpret_cast<u32x4*>(a.zh) + tile * 512 + column_lane(n, g);
+#pragma unroll
+  for (int ks = 0; ks < 4; ++ks) {
+    to[ks * 64] = __builtin_bit_cast(u32x4, zf[ks]);
+    to[ks * 64 + 256] = __builtin_bit_cast(u32x4, d[ks]);
+  }
+  if (g == 0) a.factors[tile * 16 + n] = tile * 16 + n < a.n_pairs ? ldexpf(1.0f, dout_exponent(a) - e) : 0.0f;
 }
 
 // These alone, where dz is not wanted or takes dout's place (the sums then come before it). One tile a wave; bound by memory.
@@ -328,9 +330,7 @@ __global__ void __launch_bounds__(256) trans_back_rows_kernel(TransBackArgs a) {
   int e;
   normalise(z, a.eps, zf, mu, rstd);
   scale_row(d, dv, e);
-  const _Float16 factor = row_factor(a, tile * 16 + n, e);
-#pragma unroll
-  for (int ks = 0; ks < 4; ++ks) store_rows(a, tile, ks, n, g, zf[ks], dv[ks], factor);
+  store_rows(a, tile, n, g, zf, dv, e);
 }
 
 // ----------------------------------------------------------------------------- dz
@@ -379,11 +379,7 @@ __global__ void __launch_bounds__(512, 2) trans_back_pairs_fast_kernel(TransBack
           int e;
           normalise(z[q], a.eps, nv[p], mu, rstd);
           scale_row(d[q], dv[p], e);
-          if (a.store_zh && only == 0) {
-            const _Float16 factor = row_factor(a, grp * kGroup + at, e);
-#pragma unroll
-            for (int ks = 0; ks < 4; ++ks) store_rows(a, grp * (kGroup / 16) + pairs_share * TILES + p, ks, n, g, nv[p][ks], dv[p][ks], factor);
-          }
+          if (a.store_zh && only == 0) store_rows(a, grp * (kGroup / 16) + pairs_share * TILES + p, n, g, nv[p], dv[p], e);
           if (g == 0 && only == 0) {
             s_stat[parity][0][at] = mu;
             s_stat[parity][1][at] = rstd;
@@ -580,12 +576,12 @@ constexpr int kOpBytes = 4 * 6 * 1024;  // dA', dB', H'
 constexpr int kAheadSteps = 4;
 constexpr int kStepSlots = kAheadSteps + 2;  // and those whose products and whose sums are formed
 constexpr int kStepDma = kStepBytes / 1024 / 4;
-// A unit's amplification 1 / shut = 2^k. |A'|, |B'| <= 144 and |dH'| <= 128 leave 3.5 for s (1 + |A|) / shut in fp16, and |A| is at
-// most 89 where s is not 0: s / shut may be kTop where k > 0 (1 where k = 0, as s (1 + |A| (1 - s)) is 1.1 at most). The largest of
+// A unit's amplification 1 / shut = 2^k. |A'|, |B'| <= 144 and |dH'| <= 128 leave 3.5 for f s (1 + |A|) / shut in fp16, and |A| is at
+// most 89 where s is not 0: f s / shut may be kTop where k > 0 (1 where k = 0, as s (1 + |A| (1 - s)) is 1.1 at most). The largest of
 // a step is brought to 2^-8 at least, two to three bits below kTop, so that k seldom changes again.
 constexpr float kTop = 1.0f / 32;
 constexpr int kTopBits = 7;
-constexpr int kMostBits = 96;  // below this a gate loses its bits in the end
+constexpr int kMostBits = 96;  // below this a gate, or a pair, loses its bits in the end
 
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
@@ -626,6 +622,13 @@ __global__ void __launch_bounds__(512, 2) trans_back_sums_fast_kernel(TransBackA
     f32x4 s[2][2] = {{zero, zero}, {zero, zero}};  // S1, S2: every column of dA^T ones
     int bits[2] = {0, 0};                          // k of unit n
     float shut[2] = {1.0f, 1.0f};                  // 2^-k
+    // factors of pairs 4g .. of both tiles, a step ahead
+    const f32x4* factors = reinterpret_cast<const f32x4*>(a.factors + blockIdx.x * (int64_t)kStep) + g;
+    f32x4 f[2] = {zero, zero}, f_next[2] = {zero, zero};
+    if (count > 0) {
+      f_next[0] = factors[0];
+      f_next[1] = factors[4];
+    }
     f16x8 ones;
 #pragma unroll
     for (int i = 0; i < 8; ++i) ones[i] = (_Float16)1.0f;
@@ -633,6 +636,13 @@ __global__ void __launch_bounds__(512, 2) trans_back_sums_fast_kernel(TransBackA
     const char* cur = s_x;
     for (int it = 0; it < count; ++it) {
       barrier_lds();
+#pragma unroll
+      for (int p = 0; p < 2; ++p) f[p] = f_next[p];
+      factors += (int64_t)gridDim.x * (kStep / 4);
+      if (it + 1 < count) {
+        f_next[0] = factors[0];
+        f_next[1] = factors[4];
+      }
       u32x4 op[3][2];
       float turn[2] = {1.0f, 1.0f};
       bool turned = false;
@@ -643,7 +653,7 @@ __global__ void __launch_bounds__(512, 2) trans_back_sums_fast_kernel(TransBackA
         f32x4 h[3][2][2];
         auto gate = [&](int ut, int p, int i) {  // pairs i, i + 1 of this lane's four
           const Gated r = gated_sums(h[0][ut][p][i], h[0][ut][p][i + 1], h[1][ut][p][i], h[1][ut][p][i + 1], h[2][ut][p][i], h[2][ut][p][i + 1],
-                                     k[ut], kl[ut], shut[ut], top[ut]);
+                                     k[ut], kl[ut], shut[ut], f[p][i], f[p][i + 1], top[ut]);
           op[0][ut][2 * p + i / 2] = __builtin_bit_cast(uint32_t, r.da);
           op[1][ut][2 * p + i / 2] = __builtin_bit_cast(uint32_t, r.db);
           op[2][ut][2 * p + i / 2] = __builtin_bit_cast(uint32_t, r.h);
@@ -870,12 +880,10 @@ int trans_back_fast_splits(int64_t n_pairs) {
   return (int)(s < steps ? s : steps);
 }
 
-// Pairs at a time: 512 B each in the workspace.
+// Pairs at a time: 516 B each in the workspace, zh, dout and then the factors.
 constexpr int64_t kChunkPairs = (int64_t)1 << 20;
-size_t trans_back_fast_zh_bytes(int64_t n_pairs) {
-  const int64_t groups = ((n_pairs < kChunkPairs ? n_pairs : kChunkPairs) + 255) / 256;
-  return (size_t)groups * 256 * 512;
-}
+static int64_t rows_held(int64_t n_pairs) { return ((n_pairs < kChunkPairs ? n_pairs : kChunkPairs) + 255) / 256 * 256; }
+size_t trans_back_fast_zh_bytes(int64_t n_pairs) { return (size_t)rows_held(n_pairs) * (512 + sizeof(float)); }
 
 hipError_t launch_trans_back_fast(const TransBackArgs& whole, hipStream_t st) {
   hipError_t e;
@@ -895,6 +903,7 @@ hipError_t launch_trans_back_fast(const TransBackArgs& whole, hipStream_t st) {
     if (whole.exponents) a.exponents += p0 * 4;
     if (whole.dz) a.dz = static_cast<char*>(whole.dz) + p0 * kCz * 2;
     a.store_zh = sums && !sums_first;
+    a.factors = reinterpret_cast<float*>(a.zh + rows_held(whole.n_pairs) * 512);
     a.add_parts = p0 > 0;
     const dim3 rows_grid((unsigned)((a.n_pairs + 255) / 256 * 4)), sums_grid((unsigned)a.splits, kHid / kSlice);
     if (sums && sums_first) {

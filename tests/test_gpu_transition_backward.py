@@ -490,6 +490,35 @@ def test_units_whose_gates_are_shut_keep_their_precision(t, c, hidden, saved):
     check_units(x, Call(x, "f32")(), reference(x), t, (t, saved))
 
 
+@pytest.mark.parametrize("factor", [2.0 ** -10, 2.0 ** -14, 2.0 ** -18, 2.0 ** -26, 2.0 ** -40])
+@pytest.mark.parametrize("shut", [0.0, -8.0, -16.0])
+@pytest.mark.parametrize("t,c,hidden", [("f32", 32, 64), ("bf16", 128, 512)])
+def test_small_pairs_count_where_the_large_have_no_part(t, c, hidden, shut, factor):
+    """Every second pair has a gradient `factor` times as large as the others', whose gates are shut (A near -60) in every fourth
+    unit: what those units have of a gradient is of the small pairs alone, and as precise as any. `shut`: A of the small pairs there."""
+    import torch
+    n = 3000
+    x = make(n, c, hidden, t, seed=31, offset=0.0)
+    units = torch.arange(hidden, device="cuda") % 4 == 0
+    x["gamma"], x["beta"] = torch.ones(c, device="cuda"), torch.full((c,), 4.0, device="cuda")
+    # z = +-(1, .., -1, ..) + half as much of a normal one that is orthogonal to it; 1.118 = sqrt(1.25), the root mean square of its
+    # rows, so that A = shut - 30 -+ 30 in those units
+    side = torch.where(torch.arange(n, device="cuda") % 2 == 0, 1.0, -1.0)
+    half = torch.cat([torch.ones(c // 2, device="cuda"), -torch.ones(c - c // 2, device="cuda")])
+    z = x["z"].float()
+    z = z - z.mean(dim=1, keepdim=True)
+    z = z - (z @ half / c)[:, None] * half
+    z = z / z.square().mean(dim=1, keepdim=True).sqrt()
+    x["z"] = (z * 0.5 + side[:, None] * half).to(x["z"].dtype)
+    w = x["w1"] - x["w1"].mean(dim=1, keepdim=True)
+    w = w - (w @ half / c)[:, None] * half
+    x["w1"] = torch.where(units[:, None], w - (30.0 / c) * 1.118 * half + (shut - 30.0) / (4 * c), w)
+    x["dout"][1::2] *= factor
+    got, want = Call(x, "f32")(), reference(x)
+    check_units(x, got, want, t, (t, shut, factor, "units of the small pairs"), units)
+    check_units(x, got, want, t, (t, shut, factor, "the others"), ~units)
+
+
 @pytest.mark.parametrize("pairs", [2000, 20000, (1 << 20) + 5000])
 @pytest.mark.parametrize("order", ["open", "shut", "any"])
 def test_gates_that_open_or_shut_along_the_pairs(order, pairs):
