@@ -588,3 +588,44 @@ def test_open_and_saturated_gates(factor, mean):
     got, want = Call(x, "f32")(), gradients_of_rounded_operands(x)
     check(got, want, "bf16", (factor, mean))
     check_units(x, got, want, "bf16", (factor, mean), off=0.0)
+
+
+MANY_WIDE_F32 = [(4097, 128, 512), (9000, 128, 512), (5000, 100, 400), (4113, 256, 1024), (4100, 129, 260), (8200, 65, 130)]
+
+
+@pytest.mark.parametrize("saved", ["whole", "checkpoint"])
+@pytest.mark.parametrize("pairs,c,hidden", MANY_WIDE_F32)
+def test_f32_many_pairs_of_wide_rows(pairs, c, hidden, saved):
+    """More pairs than the workgroups of one round hold: two tiles of pairs a workgroup in dz's kernel, several turns of the
+    sums' loops."""
+    x = make(pairs, c, hidden, "f32", seed=pairs + c)
+    x = checkpointed(x) if saved == "checkpoint" else x
+    check(Call(x)(), reference(x), "f32", (pairs, c, hidden, saved))
+
+
+@pytest.mark.parametrize("pairs,c,hidden", [(300, 128, 512), (9000, 128, 512), (5000, 100, 400), (4500, 140, 300)])
+def test_f32_wide_rows_in_place_alone_and_again(pairs, c, hidden):
+    """The bits of a call that is repeated, of one in dout's place and of each gradient alone; nothing written behind dz and the
+    workspace."""
+    import torch
+    import paper_2607_05439_amd as dcp
+    x = make(pairs, c, hidden, "f32", seed=33)
+    call = Call(x)
+    dz = torch.full((pairs + 40, c), 7.0, device="cuda")
+    ws = torch.full((call.ws.numel() + 4096,), 255, dtype=torch.uint8, device="cuda")
+    call.out["dz"] = dz[:pairs]
+    call.grads = dcp.make_transition_gradients(*[call.out[k] for k in NAMES], dtype=0)
+    size, whole = call.ws.numel(), None
+    for turn in range(3):
+        dcp.dcp_pair_transition_backward(*call.dims, code("f32"), EPS, x["w1"], x["w2"], x["w3"], x["gamma"], x["beta"], x["z"],
+                                         None, x["dout"], call.grads, ws, size, None)
+        now = {k: v.clone() for k, v in call.out.items()}
+        assert turn == 0 or all(torch.equal(now[k], whole[k]) for k in NAMES), turn
+        whole = now
+    assert (dz[pairs:] == 7.0).all() and (ws[size:] == 255).all()
+    for k in NAMES:
+        got = Call(x, want=(k,))()
+        assert all(torch.equal(got[j], whole[j]) if j == k else (got[j] == 7.0).all() for j in NAMES), k
+    got = Call({**x, "dout": x["dout"].clone()}, in_place=True)()
+    assert all(torch.equal(got[k], whole[k]) for k in NAMES)
+    check(whole, reference(x), "f32", (pairs, c, hidden))
