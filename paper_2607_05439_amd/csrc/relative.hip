@@ -271,11 +271,13 @@ __global__ void __launch_bounds__(256, 2) relative_back_kernel(RelativeArgs a) {
   int n_cls = 0;
   // Their sums to those of the buckets of window tile w: a class is k-slot g of step i = 4g + i, so that `run` is the B operands as
   // it lies. of: the classes' buckets, of this lane's k-slots.
-  auto clamp_run = [&]() {  // past fp32's range: as its largest number, as 0 times infinity would make NaN of other buckets
+  // Halves, which the products take twice: a sum past fp32's range is then finite here, as 0 times infinity would make NaN of other
+  // buckets, and infinite in its own. (Exact from 2^-125 on.)
+  auto halve_run = [&]() {
 #pragma unroll
     for (int ct = 0; ct < 2; ++ct)
 #pragma unroll
-      for (int i = 0; i < 4; ++i) run[ct][i] = __builtin_amdgcn_fmed3f(run[ct][i], -3.402823466e38f, 3.402823466e38f);
+      for (int i = 0; i < 4; ++i) run[ct][i] = __builtin_amdgcn_fmed3f(0.5f * run[ct][i], -3.402823466e38f, 3.402823466e38f);
   };
   auto end_classes = [&](const uint32_t (&of)[4], int w, f32x4 (&to)[2]) {
     float hot[4];
@@ -283,7 +285,7 @@ __global__ void __launch_bounds__(256, 2) relative_back_kernel(RelativeArgs a) {
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       const bool here = 4 * g + i < n_cls && (of[i] >> shift[w] >> 4 & 15) == place[w];
-      hot[i] = here && (of[i] >> shift[w] & 15) == (uint32_t)n ? 1.0f : 0.0f;
+      hot[i] = here && (of[i] >> shift[w] & 15) == (uint32_t)n ? 2.0f : 0.0f;
       any |= here;
     }
     if (__builtin_amdgcn_ballot_w64(any) == 0) return;
@@ -374,7 +376,7 @@ __global__ void __launch_bounds__(256, 2) relative_back_kernel(RelativeArgs a) {
       const bool full = few && !(has_one && has_two) && n_cls > 14;
       if (!few || full) {
         uint32_t of[4] = {0, 0, 0, 0};
-        if (full) clamp_run();
+        if (full) halve_run();
         if (full)
 #pragma unroll
           for (int i = 0; i < 4; ++i) of[i] = (uint32_t)__shfl((int)cls, 4 * g + i);
@@ -452,7 +454,7 @@ __global__ void __launch_bounds__(256, 2) relative_back_kernel(RelativeArgs a) {
   }
   const int64_t part = (int64_t)blockIdx.x * S + stream;
   uint32_t of[4];
-  clamp_run();
+  halve_run();
 #pragma unroll
   for (int i = 0; i < 4; ++i) of[i] = (uint32_t)__shfl((int)cls, 4 * g + i);
 #pragma unroll

@@ -322,3 +322,44 @@ def test_sums_past_the_largest_number_stay_in_their_buckets():
     assert got[3, 3] >= 3e38
     got[3, 3] = want[3, 3]
     assert torch.equal(got, want)
+
+
+@pytest.mark.parametrize("t,c", [("f32", 32), ("bf16", 32), ("f32", 100), ("bf16", 128)])
+@pytest.mark.parametrize("kinds", ["alike", "two kinds", "mixed"])
+def test_sums_past_the_largest_number_are_infinite(kinds, t, c):
+    """Of either sign, in their own bucket alone, whether the pairs are summed by kind or each by itself; the largest finite
+    number alone stays itself."""
+    import torch
+    n = 192
+    top = 3.4028234663852886e38 if t == "f32" else 3.3895313892515355e38
+    token = torch.arange(n, dtype=torch.int32, device="cuda")
+    width = {"alike": 64, "two kinds": 24, "mixed": 1}[kinds]
+    fields = [(token // width, None, 2)]
+    dz = torch.ones((n, n, c), device="cuda").to(dtypes()[t])
+    where = buckets(fields, 0, n)[0]
+    for b, channel, value in ((3, 3, 3e38), (1, 5, -3e38)):
+        dz[..., channel] = torch.where(where == b, value, 1.0).to(dz.dtype)
+    dz[..., 9] = 0.0
+    i, j = (where == 4).nonzero()[0].tolist()
+    dz[i, j, 9] = top
+    got = Backward(n, 0, n, c, t, fields, dz)()
+    want = torch.bincount(where.flatten(), minlength=6).float()[:, None].repeat(1, c)
+    want[3, 3], want[1, 5], want[:, 9], want[4, 9] = float("inf"), float("-inf"), 0.0, top
+    print(kinds, t, got[:, [0, 3, 5, 9]].tolist(), flush=True)
+    assert torch.equal(got, want)
+
+
+@pytest.mark.parametrize("t,c", [("f32", 32), ("bf16", 32), ("bf16", 128)])
+def test_two_pairs_past_the_largest_number(t, c):
+    """One workgroup's sum alone passes it, of pairs that are alike in all fields; the buckets beside it stay as they are."""
+    import torch
+    n = 64
+    token = torch.arange(n, dtype=torch.int32, device="cuda")
+    fields = [(token // 32, None, 1), (token * 0, None, 0)]
+    dz = torch.ones((n, n, c), device="cuda").to(dtypes()[t])
+    dz[40, 50:52, 3], dz[40, 50:52, 5] = 3e38, -3e38
+    got = Backward(n, 0, n, c, t, fields, dz)()
+    want = torch.cat([torch.bincount(b.flatten(), minlength=6).float() for b in buckets(fields, 0, n)]).view(2, 6).sum(dim=0)[:, None].repeat(1, c)
+    for channel, value in ((3, float("inf")), (5, float("-inf"))):
+        want[1, channel] = want[4, channel] = value
+    assert torch.equal(got, want)
