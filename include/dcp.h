@@ -539,8 +539,10 @@ int dcp_pair_transition_backward(int64_t n_pairs, int32_t c_z, int32_t hidden, i
  *   e = the least integer >= -126 for which rint(max |x| 2^-e) <= 127 over the block, at most 121,
  *   code = rint(x 2^-e) (ties to even), exponent byte = e + 127, value read back = code 2^e
  * (magnitudes over 127 2^121 = 3.38e38, of which the codes would pass 127, read back as that).
- * The values read back are off by at most 2^(e-1), which is between 1/255 and 1/127.5 of
- * the block's largest magnitude, and are exact in bf16 and fp32. A block with a NaN or an
+ * The values read back are exact in bf16 and fp32 and off by at most 2^(e-1), which is between
+ * 1/255 and 1/127.5 of the block's largest magnitude where that is from 63.75 2^-126 to
+ * 127.5 2^121. In blocks below, they are off by at most 2^-127 (and all 0 where the largest is
+ * at most that); above, the largest by up to 2^121. A block with a NaN or an
  * infinity has the byte 255 and reads back as NaN. dcp_pair_transition_backward reads
  * checkpoints itself; for other uses they are read back, whole or a stripe of rows.
  * ------------------------------------------------------------------------- */

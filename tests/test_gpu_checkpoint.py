@@ -182,3 +182,22 @@ def test_more_threads_than_one_launch_holds():
     assert torch.equal(codes[-tail:], want[0]) and torch.equal(exps[-tail:], want[1])
     y = unpack(codes, exps, torch.bfloat16)
     assert not y[:-tail].any() and torch.equal(y[-tail:], unpack(*want, torch.bfloat16))
+
+
+def test_the_error_at_the_ends_of_the_range():
+    """Blocks whose largest magnitude is below 63.75 2^-126: at most 2^-127, all of a value below that. Over 127.5 2^121: 127 2^121
+    is the most that is read back, at most 2^121 less. Between the two ends, up to them, half a step."""
+    import torch
+    g = torch.Generator().manual_seed(4)
+    x = torch.rand((200, 32), generator=g, dtype=torch.float64) * 2 - 1
+    top = torch.cat([torch.logspace(-149, -121, 100, base=2, dtype=torch.float64), torch.linspace(100, 127.999, 100, dtype=torch.float64) * 2.0 ** 121])
+    x = (x * top[:, None]).float()
+    x[:, 0] = top.float()
+    y = unpack(*pack(x.cuda()), torch.float32).double().cpu()
+    off, most = (x.double() - y).abs().amax(dim=1), x.double().abs().amax(dim=1)
+    low, high = most < 63.75 * 2.0 ** -126, most > 127.5 * 2.0 ** 121
+    assert low.any() and high.any() and not (low | high).all()
+    assert (off[low] <= 2.0 ** -127).all() and (off[high] <= 2.0 ** 121).all()
+    assert (off[~(low | high)] <= most[~(low | high)] / 127.5).all()
+    assert (y[most < 2.0 ** -127] == 0).all()
+    assert (off[high] > 2.0 ** 120).any() and (off[low] > most[low] / 127.5).any()
