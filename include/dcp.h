@@ -584,8 +584,9 @@ typedef struct {
  *   z_out    [n_rows, n_tokens, c] dtype; must not overlap the rest
  *   c        1 <= c <= 1024
  * The rows of the table are added in the fields' order in fp32, the sum to z, and the result
- * is rounded once. Device pointers aligned to their element size; rows of whole 16-byte
- * pieces in 16-byte aligned tensors are fastest. n_rows = 0 is a no-op. No workspace. */
+ * is rounded once. Device pointers aligned to their element size; rows of 1 to 64 whole 16-byte
+ * pieces (c up to 512 in bf16, 256 in fp32) in 16-byte aligned tensors are fastest.
+ * n_rows = 0 is a no-op. No workspace. */
 int dcp_relative_position(int64_t n_tokens, int64_t row0, int64_t n_rows, int32_t c, int32_t dtype, int32_t n_fields,
                           const dcp_relative_field* fields, const float* table, const void* z_in, void* z_out,
                           void* stream);
@@ -599,9 +600,11 @@ int dcp_relative_position_backward_workspace_size(int64_t n_tokens, int64_t n_ro
  *   dz_rows    [n_rows, n_tokens, c] dtype (may be NULL without rows)
  *   dtable     [sum of (2 r_f + 2), c] fp32, overwritten: dtable[first_f + b, :] is the sum of
  *              dz over the pairs whose bucket of field f is b (0 for one that none has), in
- *              fp32 and in a fixed order; the stripe's share, to be added over the stripes
+ *              fp32 and in a fixed order (past fp32's range not finite, in that bucket and
+ *              channel alone); the stripe's share, to be added over the stripes
  *   workspace  at least dcp_relative_position_backward_workspace_size() bytes, 256-byte aligned
- * What is written must not overlap the rest. */
+ * What is written must not overlap the rest. dz is read once for every 12 tiles of 16 buckets
+ * of one field (radii 32, 32, 2 and 0 have 5 + 5 + 1 + 1): again from the 13th on. */
 int dcp_relative_position_backward(int64_t n_tokens, int64_t row0, int64_t n_rows, int32_t c, int32_t dtype,
                                    int32_t n_fields, const dcp_relative_field* fields, const void* dz_rows,
                                    float* dtable, void* workspace, size_t workspace_bytes, void* stream);
