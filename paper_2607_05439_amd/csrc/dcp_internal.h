@@ -410,7 +410,7 @@ struct TransBackArgs {
   // 2^(e2 + e3 + d), T2 and S2 2^(e1 + e3 + d), T3 2^(e1 + e2 + d)
   const int *unit_exponents, *dout_exponent;
   float* affine_parts;       // [hidden][2][c]
-  float* factors;            // bf16: of each pair, to take its dout to the power of two of all
+  float *factors, *factor_logs;  // bf16: the inverse of what takes each pair's dout to the power of two of all, and its logarithm
   char* zh;                  // bf16: zh and dout, 512 B a pair; set by the launcher: whether dz's kernel writes them,
   int32_t store_zh, add_parts;  // whether the sums are added to the parts
 };

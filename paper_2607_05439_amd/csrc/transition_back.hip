@@ -22,6 +22,8 @@
 #include <math.h>
 #include <stdint.h>
 
+#include <type_traits>
+
 #include "cdna4.h"
 #include "checkpoint.h"
 #include "dcp_internal.h"
@@ -212,14 +214,12 @@ __device__ __forceinline__ Gated gated_pairs(float a0, float a1, float b0, float
                           __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(a1 * log1)));
   return gated(pair_of(a0, a1), pair_of(b0, b1), pair_of(d0, d1), s, __builtin_elementwise_fma(-k, s, k));
 }
-// For the sums: the sigmoids as f s / shut, f each pair's factor (at most 1), 1 / shut the unit's; top: the largest yet.
-__device__ __forceinline__ Gated gated_sums(float a0, float a1, float b0, float b1, float d0, float d1, f16x2 k, float log, float shut,
-                                            float f0, float f1, float& top) {
-  const float s0 = __builtin_amdgcn_rcpf(fmaf(__builtin_amdgcn_exp2f(a0 * log), shut, shut));
-  const float s1 = __builtin_amdgcn_rcpf(fmaf(__builtin_amdgcn_exp2f(a1 * log), shut, shut));
-  const float t0 = s0 * f0, t1 = s1 * f1;
-  top = fmaxf(fmaxf(top, t0), t1);
-  return gated(pair_of(a0, a1), pair_of(b0, b1), pair_of(d0, d1), pair_of(t0, t1), k * pair_of(fmaf(-shut, s0, 1.0f), fmaf(-shut, s1, 1.0f)));
+// For the sums: the sigmoids divided by c, a power of two 2^l for each element.
+__device__ __forceinline__ Gated gated_sums(float a0, float a1, float b0, float b1, float d0, float d1, f16x2 k, float log, float c0, float c1,
+                                            float l0, float l1, float& s0, float& s1) {
+  s0 = __builtin_amdgcn_rcpf(c0 + __builtin_amdgcn_exp2f(fmaf(a0, log, l0)));
+  s1 = __builtin_amdgcn_rcpf(c1 + __builtin_amdgcn_exp2f(fmaf(a1, log, l1)));
+  return gated(pair_of(a0, a1), pair_of(b0, b1), pair_of(d0, d1), pair_of(s0, s1), k * pair_of(fmaf(-c0, s0, 1.0f), fmaf(-c1, s1, 1.0f)));
 }
 
 // ----------------------------------------------------------------------------- rows
@@ -305,7 +305,8 @@ __device__ __forceinline__ void scale_row(const u32x4 (&d)[4], f16x8 (&v)[4], in
 
 // What the sums read of a tile of 16 pairs, 8 KB: [zh | dout][ks][lane] 16 B in fp16, with the pairs of odd groups 8
 // places on, which spreads the LDS reads of columns over all banks. dout has the power of two of its row, 2^e; the row's factor
-// takes that to the one of all pairs (0 for pairs past the last).
+// takes that to the one of all pairs: the inverse of that is kept, and its
+// logarithm; at most 2^126, which leaves nothing (pairs past the last).
 __device__ __forceinline__ int column_lane(int n, int g) { return 16 * g + (n ^ (8 * (g & 1))); }
 __device__ __forceinline__ void store_rows(const TransBackArgs& a, int64_t tile, int n, int g, const f16x8 (&zf)[4], const f16x8 (&d)[4], int e) {
   u32x4* const to = reinterpret_cast<u32x4*>(a.zh) + tile * 512 + column_lane(n, g);
@@ -314,7 +315,11 @@ __device__ __forceinline__ void store_rows(const TransBackArgs& a, int64_t tile,
     to[ks * 64] = __builtin_bit_cast(u32x4, zf[ks]);
     to[ks * 64 + 256] = __builtin_bit_cast(u32x4, d[ks]);
   }
-  if (g == 0) a.factors[tile * 16 + n] = tile * 16 + n < a.n_pairs ? ldexpf(1.0f, dout_exponent(a) - e) : 0.0f;
+  if (g == 0) {
+    const int l = tile * 16 + n < a.n_pairs ? min(e - dout_exponent(a), 126) : 126;
+    a.factors[tile * 16 + n] = ldexpf(1.0f, l);
+    a.factor_logs[tile * 16 + n] = (float)l;
+  }
 }
 
 // These alone, where dz is not wanted or takes dout's place (the sums then come before it). One tile a wave; bound by memory.
@@ -576,10 +581,10 @@ constexpr int kOpBytes = 4 * 6 * 1024;  // dA', dB', H'
 constexpr int kAheadSteps = 4;
 constexpr int kStepSlots = kAheadSteps + 2;  // and those whose products and whose sums are formed
 constexpr int kStepDma = kStepBytes / 1024 / 4;
-// A unit's amplification 1 / shut = 2^k. |A'|, |B'| <= 144 and |dH'| <= 128 leave 3.5 for f s (1 + |A|) / shut in fp16, and |A| is at
-// most 89 where s is not 0: f s / shut may be kTop where k > 0 (1 where k = 0, as s (1 + |A| (1 - s)) is 1.1 at most). The largest of
-// a step is brought to 2^-8 at least, two to three bits below kTop, so that k seldom changes again.
-constexpr float kTop = 1.0f / 32;
+// A unit's amplification 2^k. |A'|, |B'| <= 144 and |dH'| <= 128 leave 3.5 for 2^k f s (1 + |A|) in fp16, f a pair's factor, and |A| is at
+// most 156 where 2^k f s is not 0 (2^(|A| log2(e) - k) is below 2^128): it may be kTop where k > 0, and 1 where k = 0, as s (1 + |A| (1 - s)) is
+// 1.1 at most. The largest of a step is brought to 2^-8 at least, one to two bits below kTop, so that k seldom changes again.
+constexpr float kTop = 1.0f / 64;
 constexpr int kTopBits = 7;
 constexpr int kMostBits = 96;  // below this a gate, or a pair, loses its bits in the end
 
@@ -621,14 +626,21 @@ __global__ void __launch_bounds__(512, 2) trans_back_sums_fast_kernel(TransBackA
     auto sum_at = [&](int m, int ut, int i) { return 3 * kSize + m * kHid + 32 * chunk + 16 * ut + 4 * g + i; };
     f32x4 s[2][2] = {{zero, zero}, {zero, zero}};  // S1, S2: every column of dA^T ones
     int bits[2] = {0, 0};                          // k of unit n
-    float shut[2] = {1.0f, 1.0f};                  // 2^-k
-    // factors of pairs 4g .. of both tiles, a step ahead
-    const f32x4* factors = reinterpret_cast<const f32x4*>(a.factors + blockIdx.x * (int64_t)kStep) + g;
-    f32x4 f[2] = {zero, zero}, f_next[2] = {zero, zero};
-    if (count > 0) {
-      f_next[0] = factors[0];
-      f_next[1] = factors[4];
-    }
+    bool plain = false;                            // no unit of this wave has one: the rest of the steps need no care
+    // inverse factors of pairs 4g .. of both tiles, and their logarithms
+    const int64_t factors_at = blockIdx.x * (int64_t)kStep + 4 * g;
+    const f32x4 *factors = reinterpret_cast<const f32x4*>(a.factors + factors_at), *logs = reinterpret_cast<const f32x4*>(a.factor_logs + factors_at);
+    f32x4 f[2] = {zero, zero}, lf[2] = {zero, zero};
+    auto load_factors = [&]() {
+#pragma unroll
+      for (int p = 0; p < 2; ++p) {
+        f[p] = factors[4 * p];
+        lf[p] = logs[4 * p];
+      }
+      factors += (int64_t)gridDim.x * (kStep / 4);
+      logs += (int64_t)gridDim.x * (kStep / 4);
+    };
+    if (count > 0) load_factors();
     f16x8 ones;
 #pragma unroll
     for (int i = 0; i < 8; ++i) ones[i] = (_Float16)1.0f;
@@ -636,29 +648,31 @@ __global__ void __launch_bounds__(512, 2) trans_back_sums_fast_kernel(TransBackA
     const char* cur = s_x;
     for (int it = 0; it < count; ++it) {
       barrier_lds();
-#pragma unroll
-      for (int p = 0; p < 2; ++p) f[p] = f_next[p];
-      factors += (int64_t)gridDim.x * (kStep / 4);
-      if (it + 1 < count) {
-        f_next[0] = factors[0];
-        f_next[1] = factors[4];
-      }
       u32x4 op[3][2];
-      float turn[2] = {1.0f, 1.0f};
-      bool turned = false;
-      for (;;) {  // once, and again where a unit's k changes: at the first step to what its gates need, then down alone, at most to 0
-        float top[2] = {0.0f, 0.0f};
-        // the first tile of pairs, then the second, and between its products what follows from the first
+      float top[2];
+      // the first tile of pairs, then the second, and between its products what follows from the first
+      auto form = [&](auto amplified) {
+        constexpr bool kAmplified = decltype(amplified)::value;
+        const float shut[2] = {ldexpf(1.0f, -bits[0]), ldexpf(1.0f, -bits[1])}, by[2] = {(float)-bits[0], (float)-bits[1]};
+        top[0] = top[1] = 0.0f;
         auto row = [&](int q, int m) { return as_f16x8(*reinterpret_cast<const u32x4*>(cur + (q >> 2) * 8192 + m * 4096 + (q & 3) * 1024 + row_at)); };
         f32x4 h[3][2][2];
         auto gate = [&](int ut, int p, int i) {  // pairs i, i + 1 of this lane's four
+          float c[2] = {f[p][i], f[p][i + 1]}, l[2] = {lf[p][i], lf[p][i + 1]}, t[2];
+          if (kAmplified)
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+              c[j] *= shut[ut];
+              l[j] += by[ut];
+            }
           const Gated r = gated_sums(h[0][ut][p][i], h[0][ut][p][i + 1], h[1][ut][p][i], h[1][ut][p][i + 1], h[2][ut][p][i], h[2][ut][p][i + 1],
-                                     k[ut], kl[ut], shut[ut], f[p][i], f[p][i + 1], top[ut]);
+                                     k[ut], kl[ut], c[0], c[1], l[0], l[1], t[0], t[1]);
+          if (kAmplified) top[ut] = fmaxf(fmaxf(top[ut], t[0]), t[1]);
           op[0][ut][2 * p + i / 2] = __builtin_bit_cast(uint32_t, r.da);
           op[1][ut][2 * p + i / 2] = __builtin_bit_cast(uint32_t, r.db);
           op[2][ut][2 * p + i / 2] = __builtin_bit_cast(uint32_t, r.h);
 #pragma unroll
-          for (int m = 0; m < 3; ++m) asm volatile("" : "+v"(op[m][ut][2 * p + i / 2]));  // here, beside the products, not behind the loop
+          for (int m = 0; m < 3; ++m) asm volatile("" : "+v"(op[m][ut][2 * p + i / 2]));  // here, beside the products, not behind them
         };
         constexpr int kQueue = 3;
         f16x8 zq[kQueue], dq[kQueue];
@@ -688,24 +702,30 @@ __global__ void __launch_bounds__(512, 2) trans_back_sums_fast_kernel(TransBackA
           gate(0, 1, i);
           gate(1, 1, i);
         }
+      };
+      float turn[2] = {1.0f, 1.0f};
+      bool turned = false;
+      if (plain) form(std::false_type());
+      while (!plain) {  // once, and again where a unit's k changes: at the first step to what its gates need, then down alone
+        form(std::true_type());
         const bool first = it == 0 && !turned;
-        if (!first && __builtin_amdgcn_ballot_w64((bits[0] > 0 && top[0] > kTop) || (bits[1] > 0 && top[1] > kTop)) == 0) break;
         bool again = false;
 #pragma unroll
         for (int ut = 0; ut < 2; ++ut) {
           const float most = max4(top[ut]);
+          if (!first && !(bits[ut] > 0 && most > kTop)) continue;
           int e = -2 * kMostBits;
           if (most > 0.0f) (void)frexpf(most, &e);
-          if (!first && !(bits[ut] > 0 && most > kTop)) continue;
           const int to = min(max(bits[ut] - e - kTopBits, 0), kMostBits);
           turn[ut] *= ldexpf(1.0f, to - bits[ut]);
           again |= to != bits[ut];
           bits[ut] = to;
-          shut[ut] = ldexpf(1.0f, -to);
         }
         if (__builtin_amdgcn_ballot_w64(again) == 0) break;
         turned = true;
       }
+      plain = __builtin_amdgcn_ballot_w64((bits[0] | bits[1]) != 0) == 0;
+      if (it + 1 < count) load_factors();  // the next step's
       if (turned) {
         if (g == 0) {
           s_turn[it & 1][share][n] = turn[0];
@@ -730,8 +750,8 @@ __global__ void __launch_bounds__(512, 2) trans_back_sums_fast_kernel(TransBackA
       cur = cur + kStepBytes == s_x + kStepSlots * kStepBytes ? s_x : cur + kStepBytes;
     }
     if (g == 0) {
-      s_end[share][n] = shut[0];
-      s_end[share][16 + n] = shut[1];
+      s_end[share][n] = ldexpf(1.0f, -bits[0]);
+      s_end[share][16 + n] = ldexpf(1.0f, -bits[1]);
     }
     barrier_lds();
     if (n == 0)
@@ -880,10 +900,10 @@ int trans_back_fast_splits(int64_t n_pairs) {
   return (int)(s < steps ? s : steps);
 }
 
-// Pairs at a time: 516 B each in the workspace, zh, dout and then the factors.
+// Pairs at a time: 520 B each in the workspace, zh, dout and then the factors.
 constexpr int64_t kChunkPairs = (int64_t)1 << 20;
 static int64_t rows_held(int64_t n_pairs) { return ((n_pairs < kChunkPairs ? n_pairs : kChunkPairs) + 255) / 256 * 256; }
-size_t trans_back_fast_zh_bytes(int64_t n_pairs) { return (size_t)rows_held(n_pairs) * (512 + sizeof(float)); }
+size_t trans_back_fast_zh_bytes(int64_t n_pairs) { return (size_t)rows_held(n_pairs) * (512 + 2 * sizeof(float)); }
 
 hipError_t launch_trans_back_fast(const TransBackArgs& whole, hipStream_t st) {
   hipError_t e;
@@ -904,6 +924,7 @@ hipError_t launch_trans_back_fast(const TransBackArgs& whole, hipStream_t st) {
     if (whole.dz) a.dz = static_cast<char*>(whole.dz) + p0 * kCz * 2;
     a.store_zh = sums && !sums_first;
     a.factors = reinterpret_cast<float*>(a.zh + rows_held(whole.n_pairs) * 512);
+    a.factor_logs = a.factors + rows_held(whole.n_pairs);
     a.add_parts = p0 > 0;
     const dim3 rows_grid((unsigned)((a.n_pairs + 255) / 256 * 4)), sums_grid((unsigned)a.splits, kHid / kSlice);
     if (sums && sums_first) {
