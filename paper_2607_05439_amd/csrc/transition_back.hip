@@ -343,9 +343,9 @@ __global__ void __launch_bounds__(256) trans_back_rows_kernel(TransBackArgs a) {
 // of 16 pairs each and, from them, dA' and dB', which are the B operands of the products with the transposed weights;
 // those the four other waves form, a chunk of 32 units later, and at a group's end dz. So every weight fragment is read from
 // LDS once for TILES tiles of pairs; with each wave doing all of it for two tiles the LDS reads alone took as long as the
-// products. 1024 tokens: 885 us, of which the matrix cores are busy 43% and vector work 49%: the two of a SIMD hardly
+// products. 1024 tokens: 900 us, of which the matrix cores are busy 41% and vector work 47%: the two of a SIMD hardly
 // overlap, and the gate's 18 vector instructions for two elements, four of them exponentials and reciprocals, are what bounds it
-// (2.2 TB/s; each row of z and dout is read twice, as the registers hold none through the chunks).
+// (2.1 TB/s; each row of z and dout is read twice, as the registers hold none through the chunks).
 // The weights stream through LDS by direct-to-LDS loads, the rows one chunk ahead. SPLIT 2, for few pairs: two waves form a tile
 // of pairs, 16 units of a chunk each, and two of the others multiply; more loads in flight or chunks ahead gain nothing there.
 template <bool CODES, int TILES, int SPLIT>
@@ -573,7 +573,8 @@ __global__ void __launch_bounds__(512, 2) trans_back_pairs_fast_kernel(TransBack
 // of the second for j >= 4; another keeps the sums (192 registers) and adds the products a step later. Their B operands
 // are columns of zh and dout, which the LDS's transposing reads bring: 16 lanes read four rows of 16 channels, and
 // get four rows of one channel each. The two waves share a SIMD: vector work beside products. (One wave for both, alone
-// on its SIMD, took 1110 us for 1024 tokens.) 1024 tokens: 765 us, the matrix cores 65% busy at 1.7 GHz, which is what bounds it.
+// on its SIMD, took 1110 us for 1024 tokens.) 1024 tokens: 850 us, the matrix cores 57% and vector work 47% busy at 1.7 GHz; the
+// waves with the gate, 21 vector instructions for two elements, are what bounds it. Shut gates: below.
 constexpr int kStep = 32;
 constexpr int kSlice = 128;
 constexpr int kStepBytes = 16 * 1024;  // two tiles of 16 pairs: zh, dout
